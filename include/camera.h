@@ -391,6 +391,68 @@ int camera_output_error(const float* y, const float* y_hat, int64_t n_tokens, in
 int camera_residual_norm(const void* x, int32_t dtype, const float* y, int64_t n_tokens, int32_t d_model, float eps,
                          void* out, void* cuda_stream);
 
+/*
+ * Recovery of a sliced model: what its output distribution says, and the loss that trains it towards the full model's.
+ * (The paper evaluates perplexity and leaves recovery out; these calls have no counterpart there.)
+ *
+ * Rows of logits: DEVICE [n_rows, vocab] in CAMERA_BF16 or CAMERA_F32, rows `ld` elements apart (ld >= vocab), any
+ * alignment of the element type.  vocab <= CAMERA_MAX_VOCAB.  The distribution of a row is softmax(x / temperature),
+ * 0 < temperature < infinity.  A logit of minus infinity is a token that cannot occur; a row of nothing else has no
+ * distribution ("empty", see each call).  A row with a NaN or a logit of plus infinity gives NaN.  All statistics are
+ * fp32 sums.  Results do not depend on other rows and are the same bits on every run.  No workspace.
+ */
+#define CAMERA_MAX_VOCAB (1 << 20)
+#define CAMERA_MAX_TOP 128
+
+/*
+ * Log-probability of one given token per row, the entropy of the row's distribution (both in nats) and its top_n
+ * alternatives.  targets: DEVICE int64 [n_rows]; logprob: DEVICE [n_rows]; both or neither may be NULL.  A target outside
+ * [0, vocab) (an ignore index such as -100) gives 0.  entropy: DEVICE [n_rows] or NULL.  top_idx / top_logprob: DEVICE
+ * [n_rows, top_n] int32 / fp32, by decreasing logit, ties by increasing index; entries beyond the tokens that can occur
+ * are -1 / minus infinity.  0 <= top_n <= CAMERA_MAX_TOP (else CAMERA_ERR_UNSUPPORTED_SHAPE).
+ * Empty row: logprob minus infinity, entropy 0, no alternatives.  Row with NaN: NaN, alternatives -1 / NaN.
+ */
+int camera_token_logprobs(const void* logits, int32_t dtype, int64_t ld, int64_t n_rows, int32_t vocab,
+                          const int64_t* targets, int32_t top_n, float temperature, float* logprob, float* entropy,
+                          int32_t* top_idx, float* top_logprob, void* cuda_stream);
+
+/* camera_distill_t.flags */
+enum { CAMERA_DISTILL_TAIL = 1u };  /* the probability outside the teacher's list is one more class (else the list is renormalised) */
+
+/* The student's logits and the teacher's top log-probabilities, as camera_token_logprobs writes them. */
+typedef struct {
+  const void* logits;             /* DEVICE [n_rows, vocab] */
+  int64_t ld;
+  int64_t n_rows;
+  int32_t dtype;                  /* camera_dtype_t */
+  int32_t vocab;
+  const int32_t* teacher_idx;     /* DEVICE [n_rows, k], distinct in a row; an index outside [0, vocab) is no entry */
+  const float* teacher_logprob;   /* DEVICE [n_rows, k] log-probabilities at the same temperature (without TAIL any constant may be added) */
+  int32_t k;                      /* 1 .. CAMERA_MAX_TOP */
+  float temperature;
+  uint32_t flags;
+} camera_distill_t;
+
+/*
+ * Kullback-Leibler divergence of the student from the teacher's list, per row:
+ *   loss = sum_j p_j (ln p_j - ln q_j),  p = softmax of the list;
+ *   CAMERA_DISTILL_TAIL: p = exp(teacher_logprob), plus rest (ln rest - ln R), rest = max(0, 1 - sum p), R = the
+ *   student's probability outside the list (dropped where the student has none there).
+ * forward: loss, and for a later backward lse (ln sum exp(x / temperature)) and, with TAIL, log_tail (the same sum over
+ *   the tokens outside the list); lse and log_tail may be NULL.  All DEVICE fp32 [n_rows].
+ * backward: d_logits = d_loss[r] d loss_r / d x, rows d_ld elements apart, dtype of the logits; d_logits may be the
+ *   logits themselves (then d_ld == ld).
+ * step: both from one call, for a d_loss known beforehand (a mean over tokens, a mask); loss of a row with d_loss 0 is 0.
+ * A row with d_loss 0 has a gradient of 0 and its logits are not read.  An empty row has loss and gradient 0, and so has
+ * one whose logits all overflow fp32 to minus infinity when divided by the temperature and multiplied by log2(e).
+ * The factor temperature^2 that some recipes put before the loss goes into d_loss.
+ */
+int camera_distill_forward(const camera_distill_t* d, float* loss, float* lse, float* log_tail, void* cuda_stream);
+int camera_distill_backward(const camera_distill_t* d, const float* d_loss, const float* lse, const float* log_tail,
+                            void* d_logits, int64_t d_ld, void* cuda_stream);
+int camera_distill_step(const camera_distill_t* d, const float* d_loss, float* loss, void* d_logits, int64_t d_ld,
+                        void* cuda_stream);
+
 /* Scratch for camera_analyze_layer_host: score + select scratch for one batch of tokens, two staging
  * buffers for batches of x, and the results. */
 size_t camera_analyze_workspace_bytes(const camera_layer_t* layer, int64_t n_tokens, int32_t n_levels);

@@ -11,3 +11,5 @@ from .binding import (  # noqa: F401
     expert_offsets_tensor, camera_layer_forward, camera_score_forward_layer, camera_mask_down_columns, camera_pruned_output, camera_forward_workspace_bytes, camera_output_error, camera_residual_norm,
     camera_set_wait_limit_ns, camera_get_wait_limit_ns, camera_wait_probe, camera_select_prune_static,
     camera_layer_prepare, camera_layer_release, lib)
+from .recovery import (  # noqa: F401
+    camera_token_logprobs, camera_distill_forward, camera_distill_backward, camera_distill_step)

@@ -37,6 +37,12 @@ class camera_layer_t(C.Structure):
                 ("w_down_ld", C.POINTER(C.c_int32)), ("prepared", C.c_void_p)]
 
 
+class camera_distill_t(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("ld", C.c_int64), ("n_rows", C.c_int64), ("dtype", C.c_int32),
+                ("vocab", C.c_int32), ("teacher_idx", C.c_void_p), ("teacher_logprob", C.c_void_p), ("k", C.c_int32),
+                ("temperature", C.c_float), ("flags", C.c_uint32)]
+
+
 class camera_score_aux_t(C.Structure):
     _fields_ = [("phi2", C.c_void_p), ("phi_inf_sq", C.c_void_p), ("omega2", C.c_void_p),
                 ("topk_idx", C.c_void_p), ("topk_w", C.c_void_p), ("topk_idx_in", C.c_void_p),
@@ -131,6 +137,17 @@ def _load() -> C.CDLL:
     lib.camera_compact_weights.argtypes = [C.POINTER(camera_layer_t), C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
                                            C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
                                            C.POINTER(C.c_int32), C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.camera_token_logprobs.restype = C.c_int
+    lib.camera_token_logprobs.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int32,
+                                          C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.camera_distill_forward.restype = C.c_int
+    lib.camera_distill_forward.argtypes = [C.POINTER(camera_distill_t), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.camera_distill_backward.restype = C.c_int
+    lib.camera_distill_backward.argtypes = [C.POINTER(camera_distill_t), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                            C.c_int64, C.c_void_p]
+    lib.camera_distill_step.restype = C.c_int
+    lib.camera_distill_step.argtypes = [C.POINTER(camera_distill_t), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
+                                        C.c_void_p]
     return lib
 
 

@@ -1,0 +1,145 @@
+"""ctypes binding of the recovery operators (include/camera.h): log-probabilities of given tokens, distillation.
+
+Like binding.py: argument marshalling only, every function named as the C entry point it calls.  Tensors a call returns
+are allocated on the stream the call runs on.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import functools
+from typing import Dict, Optional, Tuple
+
+import torch
+
+from .binding import CAMERA_BF16, CAMERA_F32, _check, camera_distill_t, lib
+
+CAMERA_DISTILL_TAIL = 1
+CAMERA_MAX_TOP = 128
+_DTYPE = {torch.bfloat16: CAMERA_BF16, torch.float32: CAMERA_F32}
+
+
+def _on_stream(fn):
+    """Runs the call with `stream` (if given) as the current stream, so that what it allocates belongs there."""
+    @functools.wraps(fn)
+    def wrapper(*args, stream: Optional[torch.cuda.Stream] = None, **kw):
+        if stream is None:
+            return fn(*args, **kw)
+        with torch.cuda.stream(stream):
+            return fn(*args, **kw)
+    return wrapper
+
+
+def _stream() -> Optional[int]:
+    return torch.cuda.current_stream().cuda_stream or None
+
+
+def _rows(t: torch.Tensor, name: str) -> int:
+    """Distance of the rows of a [n_rows, vocab] tensor in elements."""
+    if not (t.is_cuda and t.dim() == 2 and t.dtype in _DTYPE):
+        raise ValueError(f"{name} must be a bf16 or fp32 [n_rows, vocab] tensor on the GPU")
+    rows, vocab = t.shape
+    ld = t.stride(0) if rows > 1 else max(t.stride(0), vocab)
+    if (vocab > 1 and t.stride(1) != 1) or ld < vocab:
+        raise ValueError(f"{name} must have contiguous, non-overlapping rows")
+    return ld
+
+
+def _vector(t: torch.Tensor, like: torch.Tensor, dtype, shape, name: str) -> int:
+    if not (t.is_contiguous() and t.dtype == dtype and t.device == like.device and tuple(t.shape) == shape):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on the device of the logits")
+    return t.data_ptr()
+
+
+@_on_stream
+def camera_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, *, top_n: int = 0,
+                          temperature: float = 1.0, entropy: bool = True) -> Dict[str, torch.Tensor]:
+    """Log-probability of targets[r] (int64 [n_rows]) under softmax(logits[r] / temperature), the entropy of that
+    distribution, and its top_n alternatives.  Returns a dict with logprob (if targets are given), entropy (unless
+    entropy=False), and for top_n > 0 top_idx (int32) and top_logprob [n_rows, top_n]."""
+    ld = _rows(logits, "logits")
+    rows, vocab = logits.shape
+    out: Dict[str, torch.Tensor] = {}
+    dev = logits.device
+    t_ptr = lp_ptr = h_ptr = i_ptr = v_ptr = None
+    if targets is not None:
+        t_ptr = _vector(targets, logits, torch.int64, (rows,), "targets")
+        out["logprob"] = t = torch.empty(rows, dtype=torch.float32, device=dev)
+        lp_ptr = t.data_ptr()
+    if entropy:
+        out["entropy"] = t = torch.empty(rows, dtype=torch.float32, device=dev)
+        h_ptr = t.data_ptr()
+    if top_n > 0:
+        out["top_idx"] = t = torch.empty((rows, top_n), dtype=torch.int32, device=dev)
+        i_ptr = t.data_ptr()
+        out["top_logprob"] = t = torch.empty((rows, top_n), dtype=torch.float32, device=dev)
+        v_ptr = t.data_ptr()
+    _check(lib.camera_token_logprobs(logits.data_ptr(), _DTYPE[logits.dtype], ld, rows, vocab, t_ptr, top_n, temperature,
+                                     lp_ptr, h_ptr, i_ptr, v_ptr, _stream()), "camera_token_logprobs")
+    return out
+
+
+def _distill(logits, teacher_idx, teacher_logprob, temperature, tail) -> camera_distill_t:
+    ld = _rows(logits, "logits")
+    rows, vocab = logits.shape
+    if teacher_idx.dim() != 2:
+        raise ValueError("teacher_idx must be [n_rows, k]")
+    k = int(teacher_idx.shape[1])
+    return camera_distill_t(logits.data_ptr(), ld, rows, _DTYPE[logits.dtype], vocab,
+                            _vector(teacher_idx, logits, torch.int32, (rows, k), "teacher_idx"),
+                            _vector(teacher_logprob, logits, torch.float32, (rows, k), "teacher_logprob"), k, temperature,
+                            CAMERA_DISTILL_TAIL if tail else 0)
+
+
+def _gradient(logits: torch.Tensor, d_logits: Optional[torch.Tensor], ld: int) -> Tuple[torch.Tensor, int]:
+    """The gradient's tensor (allocated with the pitch of the logits, so that both are aligned alike) and its pitch."""
+    if d_logits is None:
+        return torch.empty_strided(logits.shape, (ld, 1), dtype=logits.dtype, device=logits.device), ld
+    if d_logits.shape != logits.shape or d_logits.dtype != logits.dtype or d_logits.device != logits.device:
+        raise ValueError("d_logits must have the shape, dtype and device of the logits")
+    return d_logits, _rows(d_logits, "d_logits")
+
+
+@_on_stream
+def camera_distill_forward(logits: torch.Tensor, teacher_idx: torch.Tensor, teacher_logprob: torch.Tensor, *,
+                           temperature: float = 1.0, tail: bool = False) -> Dict[str, torch.Tensor]:
+    """Divergence of the student (softmax(logits / temperature)) from the teacher's list (int32 / fp32 [n_rows, k], as
+    camera_token_logprobs returns them) per row.  Returns a dict with loss [n_rows] and what camera_distill_backward
+    takes: lse and, with tail=True (the rest of the vocabulary as one more class), log_tail."""
+    d = _distill(logits, teacher_idx, teacher_logprob, temperature, tail)
+    out = {name: torch.empty(d.n_rows, dtype=torch.float32, device=logits.device)
+           for name in (("loss", "lse", "log_tail") if tail else ("loss", "lse"))}
+    _check(lib.camera_distill_forward(C.byref(d), out["loss"].data_ptr(), out["lse"].data_ptr(),
+                                      out["log_tail"].data_ptr() if tail else None, _stream()), "camera_distill_forward")
+    return out
+
+
+@_on_stream
+def camera_distill_backward(logits: torch.Tensor, teacher_idx: torch.Tensor, teacher_logprob: torch.Tensor,
+                            d_loss: torch.Tensor, lse: torch.Tensor, log_tail: Optional[torch.Tensor] = None, *,
+                            temperature: float = 1.0, tail: bool = False,
+                            d_logits: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient by the logits, d_loss [n_rows] being the gradient by the losses; lse and log_tail are the forward
+    call's.  d_logits may be the logits themselves."""
+    d = _distill(logits, teacher_idx, teacher_logprob, temperature, tail)
+    rows = (d.n_rows,)
+    if tail and log_tail is None:
+        raise ValueError("log_tail is needed with tail=True")
+    d_logits, d_ld = _gradient(logits, d_logits, d.ld)
+    _check(lib.camera_distill_backward(C.byref(d), _vector(d_loss, logits, torch.float32, rows, "d_loss"),
+                                       _vector(lse, logits, torch.float32, rows, "lse"),
+                                       _vector(log_tail, logits, torch.float32, rows, "log_tail") if tail else None,
+                                       d_logits.data_ptr(), d_ld, _stream()), "camera_distill_backward")
+    return d_logits
+
+
+@_on_stream
+def camera_distill_step(logits: torch.Tensor, teacher_idx: torch.Tensor, teacher_logprob: torch.Tensor,
+                        d_loss: torch.Tensor, *, temperature: float = 1.0, tail: bool = False,
+                        d_logits: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Loss and gradient from one call, for a d_loss known beforehand.  Returns (loss, d_logits)."""
+    d = _distill(logits, teacher_idx, teacher_logprob, temperature, tail)
+    d_logits, d_ld = _gradient(logits, d_logits, d.ld)
+    loss = torch.empty(d.n_rows, dtype=torch.float32, device=logits.device)
+    _check(lib.camera_distill_step(C.byref(d), _vector(d_loss, logits, torch.float32, (d.n_rows,), "d_loss"),
+                                   loss.data_ptr(), d_logits.data_ptr(), d_ld, _stream()), "camera_distill_step")
+    return loss, d_logits
