@@ -391,6 +391,42 @@ int camera_output_error(const float* y, const float* y_hat, int64_t n_tokens, in
 int camera_residual_norm(const void* x, int32_t dtype, const float* y, int64_t n_tokens, int32_t d_model, float eps,
                          void* out, void* cuda_stream);
 
+/* The gated feed-forward block of one expert (Eq. 1-2 without the router), for training it after the slicing or for
+ * running it as a dense layer.  bf16. */
+typedef struct {
+  int32_t d_model;              /* multiple of 8 */
+  int32_t d_ff;                 /* micro-experts, any number >= 1 (what camera_compact_weights left of the expert) */
+  int32_t down_ld;              /* leading dimension of w_down and its gradient, a multiple of 8, >= d_ff; 0 = d_ff */
+  const void* w_gate;           /* DEVICE [d_ff, d_model] bf16, 16-byte aligned like every matrix here */
+  const void* w_up;             /* DEVICE [d_ff, d_model] */
+  const void* w_down;           /* DEVICE [d_model, down_ld], columns from d_ff on are not read */
+} camera_ffn_t;
+
+/* Scratch of camera_ffn_forward (backward = 0) and of camera_ffn_backward (1, which serves forward as well); size of the
+ * gate and up products a forward call keeps for its backward call.  0 on invalid arguments.  The workspace starts with
+ * a status word that camera_read_status reads. */
+size_t camera_ffn_workspace_bytes(const camera_ffn_t* ffn, int64_t n_tokens, int32_t backward);
+size_t camera_ffn_saved_bytes(const camera_ffn_t* ffn, int64_t n_tokens);
+
+/*
+ * y = (SiLU(x W_gate^T) * (x W_up^T)) W_down^T.  x, y: DEVICE [n_tokens, d_model] bf16, 16-byte aligned.  saved: DEVICE,
+ * camera_ffn_saved_bytes, 32-byte aligned, or NULL when no backward call follows.  Products of bf16 with fp32
+ * accumulation; the gated product is rounded to bf16 between the two GEMMs, as in camera_layer_forward.
+ */
+int camera_ffn_forward(const camera_ffn_t* ffn, const void* x, int64_t n_tokens, void* y, void* saved, void* workspace,
+                       size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Gradients of that call by its inputs, given dy (DEVICE [n_tokens, d_model] bf16) and what the call saved: dx
+ * [n_tokens, d_model], dw_gate and dw_up [d_ff, d_model], dw_down [d_model, down_ld] (columns from d_ff on are not
+ * written), all bf16, overwritten.  dx may be NULL; dw_* may be NULL together.  The gate and up products are kept, and
+ * their gradients formed, in bf16 (rounded once from fp32); the sums over tokens and micro-experts are fp32.  `saved` is
+ * left as it is.  Results are the same bits on every run.
+ */
+int camera_ffn_backward(const camera_ffn_t* ffn, const void* x, const void* dy, int64_t n_tokens, const void* saved, void* dx,
+                        void* dw_gate, void* dw_up, void* dw_down, void* workspace, size_t workspace_bytes,
+                        void* cuda_stream);
+
 /*
  * Recovery of a sliced model: what its output distribution says, and the loss that trains it towards the full model's.
  * (The paper evaluates perplexity and leaves recovery out; these calls have no counterpart there.)

@@ -12,4 +12,5 @@ from .binding import (  # noqa: F401
     camera_set_wait_limit_ns, camera_get_wait_limit_ns, camera_wait_probe, camera_select_prune_static,
     camera_layer_prepare, camera_layer_release, lib)
 from .recovery import (  # noqa: F401
+    Ffn, camera_ffn_workspace_bytes, camera_ffn_saved_bytes, camera_ffn_forward, camera_ffn_backward,
     camera_token_logprobs, camera_distill_forward, camera_distill_backward, camera_distill_step)

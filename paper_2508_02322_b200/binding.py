@@ -37,6 +37,11 @@ class camera_layer_t(C.Structure):
                 ("w_down_ld", C.POINTER(C.c_int32)), ("prepared", C.c_void_p)]
 
 
+class camera_ffn_t(C.Structure):
+    _fields_ = [("d_model", C.c_int32), ("d_ff", C.c_int32), ("down_ld", C.c_int32), ("w_gate", C.c_void_p),
+                ("w_up", C.c_void_p), ("w_down", C.c_void_p)]
+
+
 class camera_distill_t(C.Structure):
     _fields_ = [("logits", C.c_void_p), ("ld", C.c_int64), ("n_rows", C.c_int64), ("dtype", C.c_int32),
                 ("vocab", C.c_int32), ("teacher_idx", C.c_void_p), ("teacher_logprob", C.c_void_p), ("k", C.c_int32),
@@ -137,6 +142,16 @@ def _load() -> C.CDLL:
     lib.camera_compact_weights.argtypes = [C.POINTER(camera_layer_t), C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
                                            C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
                                            C.POINTER(C.c_int32), C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.camera_ffn_workspace_bytes.restype = C.c_size_t
+    lib.camera_ffn_workspace_bytes.argtypes = [C.POINTER(camera_ffn_t), C.c_int64, C.c_int32]
+    lib.camera_ffn_saved_bytes.restype = C.c_size_t
+    lib.camera_ffn_saved_bytes.argtypes = [C.POINTER(camera_ffn_t), C.c_int64]
+    lib.camera_ffn_forward.restype = C.c_int
+    lib.camera_ffn_forward.argtypes = [C.POINTER(camera_ffn_t), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_size_t, C.c_void_p]
+    lib.camera_ffn_backward.restype = C.c_int
+    lib.camera_ffn_backward.argtypes = [C.POINTER(camera_ffn_t), C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p,
+                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.camera_token_logprobs.restype = C.c_int
     lib.camera_token_logprobs.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int32,
                                           C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]

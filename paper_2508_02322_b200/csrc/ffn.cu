@@ -1,0 +1,562 @@
+// The gated feed-forward block of one expert, forward and backward (Eq. 1-2 without the router):
+//   G = X Wg^T, U = X Wu^T, H = SiLU(G) * U, Y = H Wd^T
+//   dH = dY Wd,  dU = dH * SiLU(G),  dG = dH * U * s (1 + G (1 - s)) with s = sigmoid(G)
+//   dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X,  dWd = dY^T H
+//
+// Five GEMM shapes, one kernel (k_ffn_gemm) on CTA pairs (tcgen05 cta_group::2), which differ in the orientation of
+// their operands in memory and in the epilogue:
+//   GATE_UP  A = X, B = Wg and Wu, both with K (d_model) contiguous; epilogue writes H and, for a backward pass, G and U
+//   DOWN     A = H, B = Wd, K (d_ff) contiguous; epilogue writes Y
+//   DH       A = dY (K = d_model contiguous), B = Wd with N (d_ff) contiguous; epilogue reads G, U and writes dG, dU, H
+//   DX       A = dG then dU (K = d_ff contiguous), B = Wg then Wu with N (d_model) contiguous: one accumulator for both
+//   DW       three problems in one launch: A = dG / dU / dY, B = X / X / H, both with K (tokens) as the slow dimension
+// An operand whose M or N index is the contiguous one is loaded as boxes of 64 of those x 64 k and described to the MMA
+// as MN-major; nothing is transposed in memory.
+#include <cuda.h>
+#include <string.h>
+
+#include "common.cuh"
+#include "umma.cuh"
+#include "umma_pair.cuh"
+
+namespace camera {
+
+namespace {
+
+constexpr int G_THREADS = 192;               // warps 0-3 epilogue, warp 4 TMA producer, warp 5 MMA issuer
+constexpr int G_TILE_M = 256;                // rows of the output a pair computes: 128 per CTA
+constexpr int G_A_BYTES = 128 * 128;         // this CTA's 128 rows x 64 k
+constexpr int G_MAX_STAGES = 8;
+constexpr int G_RING_BYTES = 192 * 1024;
+constexpr int G_SMEM_BYTES = G_RING_BYTES + 256 + 1024;
+constexpr int G_GROUP_M = 16;                // row tiles that are walked together (see decode)
+constexpr int G_TMEM_COLS = 512;
+
+enum { FFN_GATE_UP = 0, FFN_DOWN = 1, FFN_DH = 2, FFN_DX = 3, FFN_DW = 4 };
+
+struct FfnProblem {
+  int m, n;                 // rows and columns of the output
+  int n_tiles, unit0;       // column tiles; first work unit of this problem
+  __nv_bfloat16* out;
+  long long ld;             // of out
+  int wide;                 // rows of out start on 32-byte boundaries
+};
+
+struct FfnGemm {
+  CUtensorMap a[3], b[3];   // per problem (DW) or per k segment (DX); GATE_UP: b[0] gate, b[1] up
+  FfnProblem prob[3];
+  int n_prob, n_units;
+  int n_kb;                 // k blocks per segment
+  int bn;                   // columns per B tile; a work unit has two of them
+  int n_stages, n_acc;      // ring depth; accumulator sets in tensor memory
+  __nv_bfloat16 *g, *u;     // GATE_UP: where to keep them (or null); DH: inputs
+  __nv_bfloat16 *dg, *du, *h;   // DH outputs; GATE_UP: h
+  long long act_ld, h_ld;   // pitch of g and u, dg and du; of h
+  PlanTotals* totals;
+  unsigned long long wait_limit_ns;
+};
+
+struct FfnUnit { int p, m0, n0, two; };
+
+// Units of a problem are numbered group by group of G_GROUP_M row tiles, inside a group column tile by column tile and
+// the row tile fastest: the pairs at work at one time share a few column tiles of B and a block of rows of A, both of
+// which stay in L2.
+__device__ __forceinline__ FfnUnit decode(const FfnGemm& q, int unit, bool dual) {
+  FfnUnit r;
+  r.p = 0;
+  while (r.p + 1 < q.n_prob && unit >= q.prob[r.p + 1].unit0) ++r.p;
+  const FfnProblem& pr = q.prob[r.p];
+  const int m_tiles = (pr.m + G_TILE_M - 1) / G_TILE_M;
+  int rem = unit - pr.unit0;
+  const int per_group = G_GROUP_M * pr.n_tiles;
+  const int grp = rem / per_group;
+  rem -= grp * per_group;
+  const int in_group = min(G_GROUP_M, m_tiles - grp * G_GROUP_M);
+  r.m0 = (grp * G_GROUP_M + rem % in_group) * G_TILE_M;
+  r.n0 = (rem / in_group) * (dual ? q.bn : 2 * q.bn);
+  r.two = dual || r.n0 + q.bn < pr.n;
+  return r;
+}
+
+// Shared-memory descriptor of an MN-major bf16 tile: boxes of 64 k rows x 128 bytes (64 m or n) with the 128-byte
+// swizzle.  Groups of 8 k lie 1024 bytes apart (stride offset), blocks of 64 m or n one box apart (leading offset).
+__device__ __forceinline__ unsigned long long make_smem_desc_mn(uint32_t addr) {
+  unsigned long long d = 0;
+  d |= (unsigned long long)((addr & 0x3ffffu) >> 4);
+  d |= (unsigned long long)(8192 >> 4) << 16;
+  d |= (unsigned long long)(1024 >> 4) << 32;
+  d |= (unsigned long long)1 << 46;
+  d |= (unsigned long long)2 << 61;
+  return d;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// 16 consecutive bf16 of one row; the row's pitch keeps them 32-byte aligned (wide) or 16-byte aligned.
+__device__ __forceinline__ void store16(__nv_bfloat16* p, const uint32_t* v, bool wide) {
+  if (wide) {
+    st_global_v8(p, v);
+  } else {
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+  }
+}
+__device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
+
+template <int MODE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_gemm(const __grid_constant__ FfnGemm q) {
+  constexpr bool A_MN = MODE == FFN_DW;
+  constexpr bool B_MN = MODE == FFN_DH || MODE == FFN_DX || MODE == FFN_DW;
+  constexpr bool DUAL = MODE == FFN_GATE_UP;
+  constexpr int SEGMENTS = MODE == FFN_DX ? 2 : 1;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t bars = base + G_RING_BYTES;
+  auto full_bar = [&](int s) { return bars + 8u * s; };                                 // first CTA
+  auto empty_bar = [&](int s) { return bars + 8u * (G_MAX_STAGES + s); };               // each CTA
+  auto tfull_bar = [&](int a) { return bars + 8u * (2 * G_MAX_STAGES + a); };           // each CTA
+  auto tempty_bar = [&](int a) { return bars + 8u * (2 * G_MAX_STAGES + 2 + a); };      // first CTA, 256 readers
+  uint8_t* const tail = base_ptr + G_RING_BYTES + 8 * (2 * G_MAX_STAGES + 4);
+  volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(tail + 8);
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int n_pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
+  const int half = q.bn >> 1;                               // columns of a B tile this CTA supplies
+  const int b_bytes = half * 128;
+  const int stage_bytes = G_A_BYTES + 2 * b_bytes;
+
+  if (tid == 0) {
+    for (int s = 0; s < q.n_stages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 256); }
+    wait_state_init(abort_flag, q.wait_limit_ns);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 5) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_slot)),
+                 "r"(G_TMEM_COLS)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();     // the other CTA's barriers are initialised before anything arrives on them
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  if (warp == 4) {
+    // ------------------------------------------------------------------ TMA producer (each CTA loads its own share)
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
+        const FfnUnit u = decode(q, unit, DUAL);
+        const int am = u.m0 + 128 * (int)rank, bn0 = u.n0 + half * (int)rank;
+        for (int seg = 0; ok && seg < SEGMENTS; ++seg) {
+          const CUtensorMap* const map_a = &q.a[MODE == FFN_DX ? seg : u.p];
+          const CUtensorMap* const map_b = &q.b[MODE == FFN_DX ? seg : u.p];
+          const CUtensorMap* const map_b2 = DUAL ? &q.b[1] : map_b;
+          const int bn1 = DUAL ? bn0 : bn0 + q.bn;
+          for (int kb = 0; kb < q.n_kb; ++kb) {
+            if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) { ok = false; break; }
+            const uint32_t dst = base + stage * stage_bytes;
+            const uint32_t full0 = map_to_cta(full_bar(stage), 0);
+            const int k0 = kb * UMMA_BK;
+            if (rank == 0) mbar_expect_tx(full_bar(stage), 2 * (G_A_BYTES + (u.two ? 2 : 1) * b_bytes));
+            // whatever lies past a matrix's last row or column arrives as zeros
+            if (A_MN) {
+              tma_load_2d_pair(dst, map_a, full0, am, k0);
+              tma_load_2d_pair(dst + 8192, map_a, full0, am + 64, k0);
+            } else {
+              tma_load_2d_pair(dst, map_a, full0, k0, am);
+            }
+            const uint32_t dst_b = dst + G_A_BYTES;
+            if (B_MN) {
+              for (int j = 0; j < half; j += 64) tma_load_2d_pair(dst_b + j * 128, map_b, full0, bn0 + j, k0);
+              if (u.two)
+                for (int j = 0; j < half; j += 64) tma_load_2d_pair(dst_b + b_bytes + j * 128, map_b2, full0, bn1 + j, k0);
+            } else {
+              tma_load_2d_pair(dst_b, map_b, full0, k0, bn0);
+              if (u.two) tma_load_2d_pair(dst_b + b_bytes, map_b2, full0, k0, bn1);
+            }
+            if (++stage == q.n_stages) { stage = 0; phase ^= 1u; }
+          }
+        }
+      }
+      if (!ok) {             // copies in flight land before the CTA's shared memory is given up
+        const unsigned long long t0 = globaltimer_ns();
+        while (globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
+      }
+    }
+  } else if (warp == 5) {
+    // ------------------------------------------------------------------ MMA issuer (first CTA of the pair only)
+    if (lane == 0 && rank == 0) {
+      int stage = 0, acc = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      bool ok = true;
+      const uint32_t idesc = make_idesc_pair(q.bn) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
+      constexpr unsigned long long A_STEP = A_MN ? 2048 >> 4 : 32 >> 4, B_STEP = B_MN ? 2048 >> 4 : 32 >> 4;
+      for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
+        const FfnUnit u = decode(q, unit, DUAL);
+        if (!mbar_wait_cluster(tempty_bar(acc), acc_phase ^ 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t d0 = tmem_base + (uint32_t)(acc * 2 * q.bn), d1 = d0 + (uint32_t)q.bn;
+        for (int kb = 0; kb < SEGMENTS * q.n_kb; ++kb) {
+          if (!mbar_wait(full_bar(stage), phase, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t a_addr = base + stage * stage_bytes;
+          const unsigned long long a_desc = A_MN ? make_smem_desc_mn(a_addr) : make_smem_desc(a_addr);
+          const unsigned long long b_desc = B_MN ? make_smem_desc_mn(a_addr + G_A_BYTES) : make_smem_desc(a_addr + G_A_BYTES);
+          const unsigned long long b2_desc = b_desc + (unsigned long long)(b_bytes >> 4);
+#pragma unroll
+          for (int k = 0; k < UMMA_BK / 16; ++k) {
+            const uint32_t accumulate = (uint32_t)((kb | k) != 0);
+            umma_bf16_pair(d0, a_desc + A_STEP * k, b_desc + B_STEP * k, idesc, accumulate);
+            if (u.two) umma_bf16_pair(d1, a_desc + A_STEP * k, b2_desc + B_STEP * k, idesc, accumulate);
+          }
+          umma_commit_pair(empty_bar(stage));
+          if (++stage == q.n_stages) { stage = 0; phase ^= 1u; }
+        }
+        if (!ok) break;
+        umma_commit_pair(tfull_bar(acc));
+        if (++acc == q.n_acc) { acc = 0; acc_phase ^= 1u; }
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ epilogue: a thread owns a row of the output
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    bool ok = true;
+    for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
+      const FfnUnit u = decode(q, unit, DUAL);
+      const FfnProblem& pr = q.prob[u.p];
+      const long long row = (long long)u.m0 + 128 * (int)rank + warp * 32 + lane;
+      const bool live = row < pr.m;
+      ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_phase, abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t t0 = tmem_base + ((uint32_t)(warp * 32) << 16) + (uint32_t)(acc * 2 * q.bn);
+      const int cols = min(pr.n - u.n0, DUAL ? q.bn : 2 * q.bn);
+      if constexpr (MODE == FFN_GATE_UP) {
+        __nv_bfloat16* const h = q.h + row * q.h_ld + u.n0;
+        __nv_bfloat16* const gp = q.g + row * q.act_ld + u.n0;
+        __nv_bfloat16* const up = q.u + row * q.act_ld + u.n0;
+        const bool keep = q.g != nullptr;
+        for (int c = 0; c < cols; c += 16) {
+          uint32_t vg[16], vu[16], p[8];
+          tmem_ld16(t0 + c, vg);
+          tmem_ld16(t0 + q.bn + c, vu);
+          tmem_ld_wait(vg, vu);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float g0 = __uint_as_float(vg[2 * j]), g1 = __uint_as_float(vg[2 * j + 1]);
+            p[j] = pack_bf16(g0 * sigmoid(g0) * __uint_as_float(vu[2 * j]), g1 * sigmoid(g1) * __uint_as_float(vu[2 * j + 1]));
+          }
+          if (live) st_global_v8(h + c, p);            // the pitches of h, g, u are multiples of 64: whole chunks fit
+          if (live && keep) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) p[j] = pack_bf16(__uint_as_float(vg[2 * j]), __uint_as_float(vg[2 * j + 1]));
+            st_global_v8(gp + c, p);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) p[j] = pack_bf16(__uint_as_float(vu[2 * j]), __uint_as_float(vu[2 * j + 1]));
+            st_global_v8(up + c, p);
+          }
+        }
+      } else if constexpr (MODE == FFN_DH) {
+        const long long at = row * q.act_ld + u.n0;
+        for (int c = 0; c < cols; c += 16) {
+          uint32_t v[16], pg[8], pu[8], ph[8];
+          tmem_ld16(t0 + c, v);
+          uint4 gi[2], ui[2];
+          if (live) {
+            gi[0] = reinterpret_cast<const uint4*>(q.g + at + c)[0]; gi[1] = reinterpret_cast<const uint4*>(q.g + at + c)[1];
+            ui[0] = reinterpret_cast<const uint4*>(q.u + at + c)[0]; ui[1] = reinterpret_cast<const uint4*>(q.u + at + c)[1];
+          }
+          tmem_ld_wait(v);
+          const uint32_t* const gw = reinterpret_cast<const uint32_t*>(gi);
+          const uint32_t* const uw = reinterpret_cast<const uint32_t*>(ui);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            float dg[2], du[2], h[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float g = __uint_as_float(e ? gw[j] & 0xffff0000u : gw[j] << 16);
+              const float up = __uint_as_float(e ? uw[j] & 0xffff0000u : uw[j] << 16);
+              const float dh = __uint_as_float(v[2 * j + e]), s = sigmoid(g), act = g * s;
+              h[e] = act * up;
+              du[e] = dh * act;
+              dg[e] = dh * up * fmaf(act, 1.f - s, s);
+            }
+            pg[j] = pack_bf16(dg[0], dg[1]);
+            pu[j] = pack_bf16(du[0], du[1]);
+            ph[j] = pack_bf16(h[0], h[1]);
+          }
+          if (live) {
+            st_global_v8(q.dg + at + c, pg);
+            st_global_v8(q.du + at + c, pu);
+            st_global_v8(q.h + row * q.h_ld + u.n0 + c, ph);
+          }
+        }
+      } else {
+        __nv_bfloat16* const out = pr.out + row * pr.ld + u.n0;
+        for (int c = 0; c < cols; c += 16) {
+          uint32_t v[16], p[8];
+          tmem_ld16(t0 + c, v);
+          tmem_ld_wait(v);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) p[j] = pack_bf16(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+          if (!live) continue;
+          if (c + 16 <= cols) {
+            store16(out + c, p, pr.wide);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (c + j < cols)
+                out[c + j] = __ushort_as_bfloat16((unsigned short)(j & 1 ? p[j >> 1] >> 16 : p[j >> 1] & 0xffffu));
+          }
+        }
+      }
+      tc_fence_before();
+      mbar_arrive_cluster(map_to_cta(tempty_bar(acc), 0));
+      if (++acc == q.n_acc) { acc = 0; acc_phase ^= 1u; }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag && tid == 0) atomicExch(&q.totals->status, (int)CAMERA_ERR_DEVICE_TIMEOUT);
+  cluster_sync_all();     // neither CTA leaves while the other may still read its shared or tensor memory
+  if (warp == 5) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(G_TMEM_COLS) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+struct FfnShape {
+  int64_t T;
+  int D, F, ld;
+  long long fp;             // pitch of h, g, u, dg, du: d_ff rounded up to whole 128-byte rows
+};
+
+int check_ffn(const camera_ffn_t* f, int64_t T, FfnShape* s) {
+  if (f == nullptr || T < 0 || f->d_model < 1 || f->d_ff < 1 || f->down_ld < 0) return CAMERA_ERR_INVALID_ARG;
+  s->T = T; s->D = f->d_model; s->F = f->d_ff; s->ld = f->down_ld ? f->down_ld : f->d_ff;
+  if (s->ld < s->F) return CAMERA_ERR_INVALID_ARG;
+  if (s->D % 8 != 0 || s->ld % 8 != 0 || T > (1ll << 30) || s->D > (1 << 20) || s->ld > (1 << 20))
+    return CAMERA_ERR_UNSUPPORTED_SHAPE;
+  if (f->w_gate == nullptr || f->w_up == nullptr || f->w_down == nullptr) return CAMERA_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(f->w_gate) | reinterpret_cast<uintptr_t>(f->w_up) | reinterpret_cast<uintptr_t>(f->w_down)) & 15)
+    return CAMERA_ERR_INVALID_ARG;
+  s->fp = (s->F + 63) & ~63;
+  return CAMERA_OK;
+}
+
+struct FfnLayout { size_t h, dg, du, total; };
+FfnLayout ffn_layout(const FfnShape& s, bool backward) {
+  FfnLayout l;
+  const size_t act = up256((size_t)2 * s.T * s.fp);
+  l.h = up256(sizeof(PlanTotals));
+  l.dg = l.h + act;
+  l.du = l.dg + act;
+  l.total = backward ? l.du + act : l.dg;
+  return l;
+}
+
+// Columns per B tile: 256 gives the least traffic per product (48 KB per CTA and k block for 8.4 Mflop), fewer columns
+// give more work units where the tiles would leave pairs idle in the last round.  The cost of a round is taken as the
+// longer of its products and its loads.
+int choose_bn(long long m_tiles, int n, bool dual, int min_bn, int n_pairs) {
+  int best = 256;
+  double best_cost = 1e300;
+  for (int bn = 256; bn >= min_bn; bn >>= 1) {
+    const int per = dual ? bn : 2 * bn;
+    const long long units = m_tiles * ((n + per - 1) / per);
+    const double mma = bn / 256.0, load = 0.8 * (16.0 + bn / 8.0) / 48.0;
+    const double cost = (double)((units + n_pairs - 1) / n_pairs) * (mma > load ? mma : load);
+    if (cost < best_cost * 0.97) { best = bn; best_cost = cost; }
+  }
+  return best;
+}
+
+bool enc(CUtensorMap* out, const void* p, long long rows, long long cols, long long pitch, int box_rows) {
+  return encode_bf16_2d_pitch(out, p, (uint64_t)rows, (uint64_t)cols, (uint64_t)pitch, (uint32_t)box_rows);
+}
+
+bool wide_rows(const void* p, long long ld) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0 && ld % 16 == 0; }
+
+template <int MODE>
+cudaError_t launch_gemm(FfnGemm& q, int bn, int n_pairs, cudaStream_t st) {
+  q.bn = bn;
+  q.n_acc = bn <= 128 ? 2 : 1;
+  const int stage = G_A_BYTES + bn * 128;
+  q.n_stages = G_RING_BYTES / stage < G_MAX_STAGES ? G_RING_BYTES / stage : G_MAX_STAGES;
+  int units = 0;
+  for (int p = 0; p < q.n_prob; ++p) {
+    const int per = MODE == FFN_GATE_UP ? bn : 2 * bn;
+    q.prob[p].n_tiles = (q.prob[p].n + per - 1) / per;
+    q.prob[p].unit0 = units;
+    units += ((q.prob[p].m + G_TILE_M - 1) / G_TILE_M) * q.prob[p].n_tiles;
+  }
+  q.n_units = units;
+  const cudaError_t e = cudaFuncSetAttribute(k_ffn_gemm<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, G_SMEM_BYTES);
+  if (e != cudaSuccess) return e;
+  const int pairs = units < n_pairs ? units : n_pairs;
+  k_ffn_gemm<MODE><<<2 * pairs, G_THREADS, G_SMEM_BYTES, st>>>(q);
+  return cudaGetLastError();
+}
+
+int sm_pairs() {
+  int dev = 0, sms = 148;
+  cudaGetDevice(&dev);
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  return sms / 2;
+}
+
+#define FFN_CK(expr)                               \
+  do {                                             \
+    if ((expr) != cudaSuccess) {                   \
+      cudaGetLastError();                          \
+      return CAMERA_ERR_CUDA;                      \
+    }                                              \
+  } while (0)
+
+}  // namespace
+}  // namespace camera
+
+extern "C" size_t camera_ffn_workspace_bytes(const camera_ffn_t* f, int64_t n_tokens, int32_t backward) {
+  camera::FfnShape s;
+  if (camera::check_ffn(f, n_tokens, &s) != CAMERA_OK) return 0;
+  return camera::ffn_layout(s, backward != 0).total;
+}
+
+extern "C" size_t camera_ffn_saved_bytes(const camera_ffn_t* f, int64_t n_tokens) {
+  camera::FfnShape s;
+  if (camera::check_ffn(f, n_tokens, &s) != CAMERA_OK) return 0;
+  return camera::up256((size_t)4 * s.T * s.fp + 1);
+}
+
+extern "C" int camera_ffn_forward(const camera_ffn_t* f, const void* x, int64_t n_tokens, void* y, void* saved,
+                                  void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  using namespace camera;
+  FfnShape s;
+  const int rc = check_ffn(f, n_tokens, &s);
+  if (rc != CAMERA_OK) return rc;
+  const FfnLayout l = ffn_layout(s, false);
+  if (workspace == nullptr || workspace_bytes < l.total || (reinterpret_cast<uintptr_t>(workspace) & 255)) return CAMERA_ERR_WORKSPACE;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  char* const ws = static_cast<char*>(workspace);
+  if (n_tokens > 0 && (x == nullptr || y == nullptr || ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(y)) & 15) ||
+                       (reinterpret_cast<uintptr_t>(saved) & 31)))
+    return CAMERA_ERR_INVALID_ARG;
+  FFN_CK(cudaMemsetAsync(ws, 0, sizeof(PlanTotals), st));
+  if (n_tokens == 0) return CAMERA_OK;
+  const int n_pairs = sm_pairs();
+  const long long m_tiles = (s.T + G_TILE_M - 1) / G_TILE_M;
+  FfnGemm q;
+  memset(&q, 0, sizeof(q));
+  q.totals = reinterpret_cast<PlanTotals*>(ws);
+  q.wait_limit_ns = current_wait_limit_ns();
+  q.h = reinterpret_cast<__nv_bfloat16*>(ws + l.h);
+  q.h_ld = s.fp;
+  q.act_ld = 2 * s.fp;
+  q.g = static_cast<__nv_bfloat16*>(saved);
+  q.u = saved ? q.g + s.fp : nullptr;
+  q.n_prob = 1;
+  q.prob[0] = FfnProblem{(int)s.T, s.F, 0, 0, nullptr, 0, 0};
+  q.n_kb = (s.D + UMMA_BK - 1) / UMMA_BK;
+  int bn = choose_bn(m_tiles, s.F, true, 32, n_pairs);
+  if (!enc(&q.a[0], x, s.T, s.D, s.D, 128) || !enc(&q.b[0], f->w_gate, s.F, s.D, s.D, bn / 2) ||
+      !enc(&q.b[1], f->w_up, s.F, s.D, s.D, bn / 2))
+    return CAMERA_ERR_CUDA;
+  FFN_CK(launch_gemm<FFN_GATE_UP>(q, bn, n_pairs, st));
+  q.prob[0] = FfnProblem{(int)s.T, s.D, 0, 0, static_cast<__nv_bfloat16*>(y), s.D, wide_rows(y, s.D)};
+  q.n_kb = (s.F + UMMA_BK - 1) / UMMA_BK;
+  bn = choose_bn(m_tiles, s.D, false, 32, n_pairs);
+  if (!enc(&q.a[0], q.h, s.T, s.F, s.fp, 128) || !enc(&q.b[0], f->w_down, s.D, s.F, s.ld, bn / 2)) return CAMERA_ERR_CUDA;
+  FFN_CK(launch_gemm<FFN_DOWN>(q, bn, n_pairs, st));
+  return CAMERA_OK;
+}
+
+extern "C" int camera_ffn_backward(const camera_ffn_t* f, const void* x, const void* dy, int64_t n_tokens, const void* saved,
+                                   void* dx, void* dw_gate, void* dw_up, void* dw_down, void* workspace,
+                                   size_t workspace_bytes, void* cuda_stream) {
+  using namespace camera;
+  FfnShape s;
+  const int rc = check_ffn(f, n_tokens, &s);
+  if (rc != CAMERA_OK) return rc;
+  const FfnLayout l = ffn_layout(s, true);
+  if (workspace == nullptr || workspace_bytes < l.total || (reinterpret_cast<uintptr_t>(workspace) & 255)) return CAMERA_ERR_WORKSPACE;
+  const bool weights = dw_gate != nullptr;
+  if ((dw_up != nullptr) != weights || (dw_down != nullptr) != weights || (!weights && dx == nullptr)) return CAMERA_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(dw_gate) | reinterpret_cast<uintptr_t>(dw_up) | reinterpret_cast<uintptr_t>(dw_down)) & 15)
+    return CAMERA_ERR_INVALID_ARG;
+  if (n_tokens > 0 && (x == nullptr || dy == nullptr || saved == nullptr || (reinterpret_cast<uintptr_t>(saved) & 31) ||
+                       ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(dy) | reinterpret_cast<uintptr_t>(dx)) & 15)))
+    return CAMERA_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  char* const ws = static_cast<char*>(workspace);
+  FFN_CK(cudaMemsetAsync(ws, 0, sizeof(PlanTotals), st));
+  if (n_tokens == 0) {                          // sums over no token
+    if (weights) {
+      FFN_CK(cudaMemsetAsync(dw_gate, 0, (size_t)2 * s.F * s.D, st));
+      FFN_CK(cudaMemsetAsync(dw_up, 0, (size_t)2 * s.F * s.D, st));
+      FFN_CK(cudaMemset2DAsync(dw_down, (size_t)2 * s.ld, 0, (size_t)2 * s.F, (size_t)s.D, st));
+    }
+    return CAMERA_OK;
+  }
+  const int n_pairs = sm_pairs();
+  const long long m_tiles = (s.T + G_TILE_M - 1) / G_TILE_M;
+  FfnGemm q;
+  memset(&q, 0, sizeof(q));
+  q.totals = reinterpret_cast<PlanTotals*>(ws);
+  q.wait_limit_ns = current_wait_limit_ns();
+  q.h = reinterpret_cast<__nv_bfloat16*>(ws + l.h);
+  q.h_ld = s.fp;
+  // g and u are interleaved row by row in `saved`, dg and du the same way in the workspace
+  q.act_ld = 2 * s.fp;
+  q.g = static_cast<__nv_bfloat16*>(const_cast<void*>(saved));
+  q.u = q.g + s.fp;
+  q.dg = reinterpret_cast<__nv_bfloat16*>(ws + l.dg);
+  q.du = q.dg + s.fp;
+  // dH and its element-wise part
+  q.n_prob = 1;
+  q.prob[0] = FfnProblem{(int)s.T, s.F, 0, 0, nullptr, 0, 0};
+  q.n_kb = (s.D + UMMA_BK - 1) / UMMA_BK;
+  int bn = choose_bn(m_tiles, s.F, false, 128, n_pairs);
+  if (!enc(&q.a[0], dy, s.T, s.D, s.D, 128) || !enc(&q.b[0], f->w_down, s.D, s.F, s.ld, 64)) return CAMERA_ERR_CUDA;
+  FFN_CK(launch_gemm<FFN_DH>(q, bn, n_pairs, st));
+  if (dx != nullptr) {
+    q.prob[0] = FfnProblem{(int)s.T, s.D, 0, 0, static_cast<__nv_bfloat16*>(dx), s.D, wide_rows(dx, s.D)};
+    q.n_kb = (s.F + UMMA_BK - 1) / UMMA_BK;
+    bn = choose_bn(m_tiles, s.D, false, 128, n_pairs);
+    if (!enc(&q.a[0], q.dg, s.T, s.F, q.act_ld, 128) || !enc(&q.a[1], q.du, s.T, s.F, q.act_ld, 128) ||
+        !enc(&q.b[0], f->w_gate, s.F, s.D, s.D, 64) || !enc(&q.b[1], f->w_up, s.F, s.D, s.D, 64))
+      return CAMERA_ERR_CUDA;
+    FFN_CK(launch_gemm<FFN_DX>(q, bn, n_pairs, st));
+  }
+  if (weights) {
+    q.n_prob = 3;
+    q.prob[0] = FfnProblem{s.F, s.D, 0, 0, static_cast<__nv_bfloat16*>(dw_gate), s.D, wide_rows(dw_gate, s.D)};
+    q.prob[1] = FfnProblem{s.F, s.D, 0, 0, static_cast<__nv_bfloat16*>(dw_up), s.D, wide_rows(dw_up, s.D)};
+    q.prob[2] = FfnProblem{s.D, s.F, 0, 0, static_cast<__nv_bfloat16*>(dw_down), s.ld, wide_rows(dw_down, s.ld)};
+    q.n_kb = (int)((s.T + UMMA_BK - 1) / UMMA_BK);
+    // the third problem has as many tiles as either of the others, up to their edges
+    bn = choose_bn(3ll * ((s.F + G_TILE_M - 1) / G_TILE_M), s.D, false, 128, n_pairs);
+    if (!enc(&q.a[0], q.dg, s.T, s.F, q.act_ld, 64) || !enc(&q.a[1], q.du, s.T, s.F, q.act_ld, 64) ||
+        !enc(&q.a[2], dy, s.T, s.D, s.D, 64) || !enc(&q.b[0], x, s.T, s.D, s.D, 64) || !enc(&q.b[2], q.h, s.T, s.F, s.fp, 64))
+      return CAMERA_ERR_CUDA;
+    q.b[1] = q.b[0];
+    FFN_CK(launch_gemm<FFN_DW>(q, bn, n_pairs, st));
+  }
+  return CAMERA_OK;
+}

@@ -1,4 +1,5 @@
-"""ctypes binding of the recovery operators (include/camera.h): log-probabilities of given tokens, distillation.
+"""ctypes binding of the recovery operators (include/camera.h): the gated feed-forward block of one expert with its
+backward pass, log-probabilities of given tokens, distillation from a teacher's top log-probabilities.
 
 Like binding.py: argument marshalling only, every function named as the C entry point it calls.  Tensors a call returns
 are allocated on the stream the call runs on.
@@ -11,7 +12,7 @@ from typing import Dict, Optional, Tuple
 
 import torch
 
-from .binding import CAMERA_BF16, CAMERA_F32, _check, camera_distill_t, lib
+from .binding import CAMERA_BF16, CAMERA_F32, CameraError, _check, alloc_workspace, camera_distill_t, camera_ffn_t, lib
 
 CAMERA_DISTILL_TAIL = 1
 CAMERA_MAX_TOP = 128
@@ -48,6 +49,100 @@ def _vector(t: torch.Tensor, like: torch.Tensor, dtype, shape, name: str) -> int
     if not (t.is_contiguous() and t.dtype == dtype and t.device == like.device and tuple(t.shape) == shape):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on the device of the logits")
     return t.data_ptr()
+
+
+class Ffn:
+    """Holds the matrices of one gated feed-forward block and the camera_ffn_t that points at them.
+
+    w_gate, w_up: [d_ff, d_model]; w_down: [d_model, down_ld] with down_ld >= d_ff (an expert that camera_compact_weights
+    sliced into a buffer of the original width; d_ff then says how many of its columns, and of the rows of w_gate and
+    w_up, are in use).
+    """
+
+    def __init__(self, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, d_ff: Optional[int] = None):
+        f = int(w_gate.shape[0]) if d_ff is None else int(d_ff)
+        for t in (w_gate, w_up, w_down):
+            if not (t.dim() == 2 and t.is_contiguous() and t.dtype == torch.bfloat16 and t.device == w_gate.device):
+                raise ValueError("w_gate, w_up and w_down must be contiguous bf16 matrices on one device")
+        d = int(w_gate.shape[1])
+        if w_up.shape[1] != d or w_down.shape[0] != d or min(w_gate.shape[0], w_up.shape[0], w_down.shape[1]) < f or f < 1:
+            raise ValueError("w_gate and w_up must be [>= d_ff, d_model], w_down [d_model, >= d_ff]")
+        self.w_gate, self.w_up, self.w_down = w_gate, w_up, w_down
+        self.d_model, self.d_ff, self.down_ld = d, f, int(w_down.shape[1])
+        self.device = w_gate.device
+        self.c = camera_ffn_t(d, f, self.down_ld, w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr())
+        self._ref = C.byref(self.c)
+
+
+def camera_ffn_workspace_bytes(ffn: Ffn, n_tokens: int, *, backward: bool = False) -> int:
+    n = int(lib.camera_ffn_workspace_bytes(ffn._ref, n_tokens, int(backward)))
+    if n == 0:
+        raise CameraError(-2, "camera_ffn_workspace_bytes")
+    return n
+
+
+def camera_ffn_saved_bytes(ffn: Ffn, n_tokens: int) -> int:
+    return int(lib.camera_ffn_saved_bytes(ffn._ref, n_tokens))
+
+
+def _tokens(t: torch.Tensor, ffn: Ffn, name: str) -> int:
+    if not (t.is_contiguous() and t.dtype == torch.bfloat16 and t.dim() == 2 and t.shape[1] == ffn.d_model
+            and t.device == ffn.device):
+        raise ValueError(f"{name} must be a contiguous bf16 [n_tokens, d_model] tensor on the device of the block")
+    return t.data_ptr()
+
+
+@_on_stream
+def camera_ffn_forward(ffn: Ffn, x: torch.Tensor, *, y: Optional[torch.Tensor] = None, saved: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y = (SiLU(x W_gate^T) * (x W_up^T)) W_down^T, bf16 [n_tokens, d_model].  `saved` (camera_ffn_saved_bytes bytes)
+    receives what camera_ffn_backward needs."""
+    xp = _tokens(x, ffn, "x")
+    n = x.shape[0]
+    if y is None:
+        y = torch.empty_like(x)
+    elif _tokens(y, ffn, "y") and y.shape[0] != n:
+        raise ValueError("y must have the shape of x")
+    if workspace is None:
+        workspace = alloc_workspace(camera_ffn_workspace_bytes(ffn, n), ffn.device)
+    if saved is not None and saved.numel() * saved.element_size() < camera_ffn_saved_bytes(ffn, n):
+        raise ValueError("saved is smaller than camera_ffn_saved_bytes")
+    _check(lib.camera_ffn_forward(ffn._ref, xp, n, y.data_ptr(), None if saved is None else saved.data_ptr(),
+                                  workspace.data_ptr(), workspace.numel(), _stream()), "camera_ffn_forward")
+    return y
+
+
+@_on_stream
+def camera_ffn_backward(ffn: Ffn, x: torch.Tensor, dy: torch.Tensor, saved: torch.Tensor, *, want_x: bool = True,
+                        want_weights: bool = True, out: Optional[Dict[str, torch.Tensor]] = None,
+                        workspace: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
+    """Gradients of camera_ffn_forward(ffn, x, saved=saved) given dy: a dict with x (want_x) and w_gate, w_up [d_ff,
+    d_model], w_down [d_model, down_ld] (want_weights; columns of w_down from d_ff on are not written).  `out` names
+    tensors of those shapes to write to."""
+    xp, dyp = _tokens(x, ffn, "x"), _tokens(dy, ffn, "dy")
+    n = x.shape[0]
+    if dy.shape[0] != n:
+        raise ValueError("dy must have the shape of x")
+    if saved.numel() * saved.element_size() < camera_ffn_saved_bytes(ffn, n):
+        raise ValueError("saved is smaller than camera_ffn_saved_bytes")
+    shapes = {"x": (n, ffn.d_model)} if want_x else {}
+    if want_weights:
+        shapes.update(w_gate=(ffn.d_ff, ffn.d_model), w_up=(ffn.d_ff, ffn.d_model), w_down=(ffn.d_model, ffn.down_ld))
+    res = {}
+    for name, shape in shapes.items():
+        t = None if out is None else out.get(name)
+        if t is None:
+            t = torch.empty(shape, dtype=torch.bfloat16, device=ffn.device)
+        elif not (t.is_contiguous() and t.dtype == torch.bfloat16 and tuple(t.shape) == shape and t.device == ffn.device):
+            raise ValueError(f"out[{name!r}] must be a contiguous bf16 tensor of shape {shape}")
+        res[name] = t
+    if workspace is None:
+        workspace = alloc_workspace(camera_ffn_workspace_bytes(ffn, n, backward=True), ffn.device)
+    ptr = {name: t.data_ptr() for name, t in res.items()}
+    _check(lib.camera_ffn_backward(ffn._ref, xp, dyp, n, saved.data_ptr(), ptr.get("x"), ptr.get("w_gate"), ptr.get("w_up"),
+                                   ptr.get("w_down"), workspace.data_ptr(), workspace.numel(), _stream()),
+           "camera_ffn_backward")
+    return res
 
 
 @_on_stream

@@ -63,3 +63,46 @@ def test_tensors_are_checked_in_python(P):
         P.camera_token_logprobs(z)                                     # not on the GPU
     with pytest.raises(ValueError):
         P.camera_distill_forward(z, torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, 2))
+
+
+def ffn_struct(P, d_model=64, d_ff=40, down_ld=48, w=4096):
+    from paper_2508_02322_b200.binding import camera_ffn_t
+    return camera_ffn_t(d_model, d_ff, down_ld, w, w, w)
+
+
+def test_ffn_refusals(P):
+    lib = P.lib
+    ok = ffn_struct(P)
+    size = lib.camera_ffn_workspace_bytes(C.byref(ok), 100, 0)
+    both = lib.camera_ffn_workspace_bytes(C.byref(ok), 100, 1)
+    assert both > size >= 100 * 40 * 2 and lib.camera_ffn_saved_bytes(C.byref(ok), 100) >= 2 * 100 * 40 * 2
+    assert lib.camera_ffn_workspace_bytes(None, 100, 0) == 0
+    for bad in (dict(d_model=60), dict(d_ff=0), dict(down_ld=32), dict(down_ld=44), dict(w=None), dict(w=4100), dict(d_ff=41, down_ld=0)):
+        assert lib.camera_ffn_workspace_bytes(C.byref(ffn_struct(P, **bad)), 100, 0) == 0, bad
+    assert lib.camera_ffn_workspace_bytes(C.byref(ok), -1, 0) == 0
+
+    def fwd(f=ok, x=4096, n=100, y=4096, saved=None, ws=4096, nbytes=size):
+        return lib.camera_ffn_forward(C.byref(f), x, n, y, saved, ws, nbytes, None)
+    assert fwd(ws=None) == -3 and fwd(nbytes=size - 1) == -3 and fwd(ws=4096 + 64) == -3
+    assert fwd(x=None) == -1 and fwd(y=None) == -1 and fwd(x=4104) == -1 and fwd(saved=4112) == -1
+    assert fwd(ffn_struct(P, d_model=60)) == -2 and fwd(ffn_struct(P, w=None)) == -1
+
+    def bwd(x=4096, dy=4096, n=100, saved=4096, dx=4096, dg=4096, du=4096, dd=4096, ws=4096, nbytes=both):
+        return lib.camera_ffn_backward(C.byref(ok), x, dy, n, saved, dx, dg, du, dd, ws, nbytes, None)
+    assert bwd(nbytes=size) == -3 and bwd(dg=None) == -1 and bwd(dd=None) == -1 and bwd(dd=4104) == -1
+    assert bwd(dx=None, dg=None, du=None, dd=None) == -1          # nothing asked for
+    assert bwd(saved=None) == -1 and bwd(dy=None) == -1 and bwd(dx=4104) == -1
+
+
+def test_ffn_tensors_are_checked_in_python(P):
+    w = torch.zeros(16, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        P.Ffn(w, w, torch.zeros(64, 8, dtype=torch.bfloat16))           # fewer columns than micro-experts
+    with pytest.raises(ValueError):
+        P.Ffn(w.float(), w, torch.zeros(64, 16, dtype=torch.bfloat16))
+    ffn = P.Ffn(w, w, torch.zeros(64, 16, dtype=torch.bfloat16))
+    with pytest.raises(ValueError):
+        P.camera_ffn_forward(ffn, torch.zeros(4, 32, dtype=torch.bfloat16))
+    with pytest.raises(P.CameraError):
+        P.camera_ffn_workspace_bytes(P.Ffn(torch.zeros(16, 60, dtype=torch.bfloat16), torch.zeros(16, 60, dtype=torch.bfloat16),
+                                           torch.zeros(60, 16, dtype=torch.bfloat16)), 8)
