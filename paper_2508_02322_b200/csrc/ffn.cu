@@ -49,7 +49,8 @@ struct FfnGemm {
   int n_kb;                 // k blocks per segment
   int bn;                   // columns per B tile; a work unit has two of them
   int n_stages, n_acc;      // ring depth; accumulator sets in tensor memory
-  __nv_bfloat16 *g, *u;     // GATE_UP: where to keep them (or null); DH: inputs
+  uint16_t *g, *u;          // GATE_UP: where to keep G and U (or null); DH: inputs.  Upper halves of the 24 bits kept,
+  long long lo_off;         // with the lower byte of element i of g at ((uint8_t*)base)[lo_off + i], base the start of g's buffer
   __nv_bfloat16 *dg, *du, *h;   // DH outputs; GATE_UP: h
   long long act_ld, h_ld;   // pitch of g and u, dg and du; of h
   PlanTotals* totals;
@@ -103,6 +104,26 @@ __device__ __forceinline__ void store16(__nv_bfloat16* p, const uint32_t* v, boo
     reinterpret_cast<uint4*>(p)[0] = make_uint4(v[0], v[1], v[2], v[3]);
     reinterpret_cast<uint4*>(p)[1] = make_uint4(v[4], v[5], v[6], v[7]);
   }
+}
+
+// G and U are kept for the backward pass with 24 of their 32 bits (15 of mantissa): rounding them to bf16 would add as
+// much error to the gradients as everything else together (relative error of the weight gradients against 64 bits
+// 3.5e-3 with bf16, 2.4e-3 with 24 bits, of which 1.7e-3 is the rounding of the result).  The cut is a truncation, so that NaN and infinity survive it.
+__device__ __forceinline__ void keep24(uint16_t* hi, uint8_t* lo, const uint32_t* v) {
+  uint32_t h[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) h[j] = __byte_perm(v[2 * j], v[2 * j + 1], 0x7632);
+  st_global_v8(hi, h);
+  uint32_t l[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    l[j] = __byte_perm(__byte_perm(v[4 * j], v[4 * j + 1], 0x0051), __byte_perm(v[4 * j + 2], v[4 * j + 3], 0x0051), 0x5410);
+  *reinterpret_cast<uint4*>(lo) = make_uint4(l[0], l[1], l[2], l[3]);
+}
+// Element j (0 .. 15) of a chunk of 16: h its 8 words of upper halves, l its 4 words of lower bytes.
+__device__ __forceinline__ float kept24(const uint32_t* h, const uint32_t* l, int j) {
+  const uint32_t top = j & 1 ? h[j >> 1] & 0xffff0000u : h[j >> 1] << 16;
+  return __uint_as_float(top | (((l[j >> 2] >> (8 * (j & 3))) & 0xffu) << 8));
 }
 __device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
 
@@ -246,9 +267,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
       const int cols = min(pr.n - u.n0, DUAL ? q.bn : 2 * q.bn);
       if constexpr (MODE == FFN_GATE_UP) {
         __nv_bfloat16* const h = q.h + row * q.h_ld + u.n0;
-        __nv_bfloat16* const gp = q.g + row * q.act_ld + u.n0;
-        __nv_bfloat16* const up = q.u + row * q.act_ld + u.n0;
         const bool keep = q.g != nullptr;
+        const long long g_at = row * q.act_ld + u.n0, u_at = g_at + (q.u - q.g);
+        uint8_t* const lo = reinterpret_cast<uint8_t*>(q.g) + q.lo_off;
         for (int c = 0; c < cols; c += 16) {
           uint32_t vg[16], vu[16], p[8];
           tmem_ld16(t0 + c, vg);
@@ -261,34 +282,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
           }
           if (live) st_global_v8(h + c, p);            // the pitches of h, g, u are multiples of 64: whole chunks fit
           if (live && keep) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] = pack_bf16(__uint_as_float(vg[2 * j]), __uint_as_float(vg[2 * j + 1]));
-            st_global_v8(gp + c, p);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] = pack_bf16(__uint_as_float(vu[2 * j]), __uint_as_float(vu[2 * j + 1]));
-            st_global_v8(up + c, p);
+            keep24(q.g + g_at + c, lo + g_at + c, vg);
+            keep24(q.g + u_at + c, lo + u_at + c, vu);
           }
         }
       } else if constexpr (MODE == FFN_DH) {
-        const long long at = row * q.act_ld + u.n0;
+        const long long at = row * q.act_ld + u.n0, u_off = q.u - q.g;
+        const uint8_t* const lo = reinterpret_cast<const uint8_t*>(q.g) + q.lo_off;
         for (int c = 0; c < cols; c += 16) {
           uint32_t v[16], pg[8], pu[8], ph[8];
           tmem_ld16(t0 + c, v);
-          uint4 gi[2], ui[2];
+          uint4 gi[2], ui[2], gl, ul;
           if (live) {
-            gi[0] = reinterpret_cast<const uint4*>(q.g + at + c)[0]; gi[1] = reinterpret_cast<const uint4*>(q.g + at + c)[1];
-            ui[0] = reinterpret_cast<const uint4*>(q.u + at + c)[0]; ui[1] = reinterpret_cast<const uint4*>(q.u + at + c)[1];
+            const uint4* const gp = reinterpret_cast<const uint4*>(q.g + at + c);
+            const uint4* const up = reinterpret_cast<const uint4*>(q.g + at + u_off + c);
+            gi[0] = gp[0]; gi[1] = gp[1];
+            ui[0] = up[0]; ui[1] = up[1];
+            gl = *reinterpret_cast<const uint4*>(lo + at + c);
+            ul = *reinterpret_cast<const uint4*>(lo + at + u_off + c);
           }
           tmem_ld_wait(v);
           const uint32_t* const gw = reinterpret_cast<const uint32_t*>(gi);
           const uint32_t* const uw = reinterpret_cast<const uint32_t*>(ui);
+          const uint32_t* const gb = reinterpret_cast<const uint32_t*>(&gl);
+          const uint32_t* const ub = reinterpret_cast<const uint32_t*>(&ul);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             float dg[2], du[2], h[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float g = __uint_as_float(e ? gw[j] & 0xffff0000u : gw[j] << 16);
-              const float up = __uint_as_float(e ? uw[j] & 0xffff0000u : uw[j] << 16);
+              const float g = kept24(gw, gb, 2 * j + e), up = kept24(uw, ub, 2 * j + e);
               const float dh = __uint_as_float(v[2 * j + e]), s = sigmoid(g), act = g * s;
               h[e] = act * up;
               du[e] = dh * act;
@@ -339,6 +362,154 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
   }
 }
 
+// ------------------------------------------------------------------------------------------------ few tokens
+// Up to 8 * NT tokens: the work is reading the weights once.  A tensor-core tile of 256 rows would be mostly padding and
+// its column tiles too few to keep every SM's loads in flight, so these kernels stream the weights from global memory
+// straight into the A fragments of mma.sync (m16n8k16): a lane loads 16 bytes = 8 consecutive k of its row, which is the
+// lane's share of two MMAs once the k index is permuted the same way in both operands; no shared memory, no barriers in
+// the loop.  The tokens are the n index; their fragments come the same way from x or h (small, L1 and L2 hits).
+// A CTA owns R tiles of 16 weight rows and splits k over its 8 warps; the partial sums meet in shared memory in a fixed
+// order.  GATE_UP tiles are 8 rows of Wg over the same 8 rows of Wu: a thread then holds gate and up of one element.
+constexpr int S_WARPS = 8;
+constexpr int S_THREADS = 32 * S_WARPS;
+
+struct FfnFew {
+  const __nv_bfloat16 *w0, *w1;    // GATE_UP: Wg, Wu; DOWN: Wd in both
+  const __nv_bfloat16* in;         // x or h
+  long long w_ld, in_ld, out_ld;
+  int rows, k, T;                  // weight rows (d_ff or d_model), length of the sums, tokens
+  __nv_bfloat16* out;              // h or y
+  uint16_t* g;                     // as in FfnGemm
+  long long u_off, lo_off, act_ld;
+  PlanTotals* totals;
+};
+
+__device__ __forceinline__ uint4 ld_weights(const void* p) {      // read once: past L1
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The first n (< 8) of 8 bf16, the others zero: what lies behind the last column of a pitched matrix may be anything.
+__device__ __forceinline__ uint4 first_n(uint4 v, int n) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] &= (2 * i < n ? 0xffffu : 0u) | (2 * i + 1 < n ? 0xffff0000u : 0u);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <bool GATE_UP, int R, int NT>
+__global__ void __launch_bounds__(S_THREADS) k_ffn_few(const FfnFew q) {
+  constexpr int UNROLL = R == 1 ? 4 : R == 2 ? 2 : 1;      // steps of 64 k whose loads are issued together
+  constexpr int VALS = R * NT * 4;
+  extern __shared__ float part[];                           // [S_WARPS][VALS][32]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, tg = lane & 3;
+  const int row0 = blockIdx.x * (GATE_UP ? 8 : 16) * R;
+  if (blockIdx.x == 0 && threadIdx.x == 0 && q.totals != nullptr) q.totals->status = 0;    // nothing here can fail
+  // rows of this lane: tile r, halves 0 / 1
+  const __nv_bfloat16* w[R][2];
+  bool has[R][2];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int row = GATE_UP ? row0 + 8 * r + g : row0 + 16 * r + 8 * e + g;
+      has[r][e] = row < q.rows;
+      w[r][e] = (GATE_UP && e ? q.w1 : q.w0) + (size_t)row * q.w_ld;
+    }
+  float acc[R][NT][4];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[r][n][i] = 0.f;
+
+  const int steps = (q.k + 63) / 64;
+  const int s0 = steps * warp / S_WARPS, s1 = steps * (warp + 1) / S_WARPS;
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  for (int s = s0; s < s1; s += UNROLL) {
+    uint4 a[UNROLL][R][2][2];
+#pragma unroll
+    for (int t = 0; t < UNROLL; ++t)
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int k = (s + t) * 64 + j * 32 + tg * 8;
+            a[t][r][e][j] = has[r][e] && s + t < s1 && k < q.k ? ld_weights(w[r][e] + k) : zero;
+          }
+#pragma unroll
+    for (int t = 0; t < UNROLL; ++t) {
+      if (s + t >= s1) break;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int k = (s + t) * 64 + j * 32 + tg * 8;
+        if (!GATE_UP && k + 8 > q.k) {
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) a[t][r][e][j] = first_n(a[t][r][e][j], q.k - k);
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const int tok = 8 * n + g;
+          uint4 b = zero;
+          if (tok < q.T && k < q.k) b = *reinterpret_cast<const uint4*>(q.in + (size_t)tok * q.in_ld + k);
+          if (!GATE_UP && k + 8 > q.k) b = first_n(b, q.k - k);
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const uint4 a0 = a[t][r][0][j], a1 = a[t][r][1][j];
+            mma16816(acc[r][n], a0.x, a1.x, a0.y, a1.y, b.x, b.y);
+            mma16816(acc[r][n], a0.z, a1.z, a0.w, a1.w, b.z, b.w);
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) part[(warp * VALS + (r * NT + n) * 4 + i) * 32 + lane] = acc[r][n][i];
+  __syncthreads();
+  // element (r, n, i) of lane l: weight row g (i < 2) or g + 8 of tile r, token 8 n + 2 (l % 4) + i % 2
+  for (int at = threadIdx.x; at < R * NT * 2 * 32; at += S_THREADS) {
+    const int l = at & 31, i = (at >> 5) & 1, rn = at >> 6;
+    float lo = 0.f, hi = 0.f;
+#pragma unroll
+    for (int v = 0; v < S_WARPS; ++v) {
+      lo += part[(v * VALS + rn * 4 + i) * 32 + l];
+      hi += part[(v * VALS + rn * 4 + 2 + i) * 32 + l];
+    }
+    const int r = rn / NT, tok = 8 * (rn % NT) + 2 * (l & 3) + i;
+    if (tok >= q.T) continue;
+    if (GATE_UP) {
+      const int f = row0 + 8 * r + (l >> 2);
+      if (f >= q.rows) continue;
+      q.out[(size_t)tok * q.out_ld + f] = __float2bfloat16_rn(lo * sigmoid(lo) * hi);
+      if (q.g != nullptr) {
+        const size_t ga = (size_t)tok * q.act_ld + f, ua = ga + q.u_off;
+        uint8_t* const low = reinterpret_cast<uint8_t*>(q.g) + q.lo_off;
+        const uint32_t gb = __float_as_uint(lo), ub = __float_as_uint(hi);
+        q.g[ga] = (uint16_t)(gb >> 16); low[ga] = (uint8_t)(gb >> 8);
+        q.g[ua] = (uint16_t)(ub >> 16); low[ua] = (uint8_t)(ub >> 8);
+      }
+    } else {
+      const int d = row0 + 16 * r + (l >> 2);
+      if (d < q.rows) q.out[(size_t)tok * q.out_ld + d] = __float2bfloat16_rn(lo);
+      if (d + 8 < q.rows) q.out[(size_t)tok * q.out_ld + d + 8] = __float2bfloat16_rn(hi);
+    }
+  }
+}
+
 // ------------------------------------------------------------------------------------------------ host side
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
@@ -360,6 +531,9 @@ int check_ffn(const camera_ffn_t* f, int64_t T, FfnShape* s) {
   s->fp = (s->F + 63) & ~63;
   return CAMERA_OK;
 }
+
+// `saved`: upper halves of G and U, [T][2 fp] 16-bit (a row holds G, then U), then their lower bytes, [T][2 fp].
+size_t saved_lo_offset(const FfnShape& s) { return up256((size_t)4 * s.T * s.fp + 1); }
 
 struct FfnLayout { size_t h, dg, du, total; };
 FfnLayout ffn_layout(const FfnShape& s, bool backward) {
@@ -422,6 +596,28 @@ int sm_pairs() {
   return sms / 2;
 }
 
+constexpr int FEW_TOKENS = 32;     // up to here the streaming kernels
+
+template <bool GATE_UP, int R>
+cudaError_t launch_few(const FfnFew& q, cudaStream_t st) {
+  const int per = (GATE_UP ? 8 : 16) * R;
+  const unsigned grid = (unsigned)((q.rows + per - 1) / per);
+  const int nt = (q.T + 7) / 8;
+  auto go = [&](auto kern, int n) {
+    const int smem = S_WARPS * R * n * 4 * 32 * (int)sizeof(float);
+    if (smem > 48 * 1024) {
+      const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      if (e != cudaSuccess) return e;
+    }
+    kern<<<grid, S_THREADS, smem, st>>>(q);
+    return cudaGetLastError();
+  };
+  if (nt <= 1) return go(k_ffn_few<GATE_UP, R, 1>, 1);
+  if (nt <= 2) return go(k_ffn_few<GATE_UP, R, 2>, 2);
+  if (nt <= 3) return go(k_ffn_few<GATE_UP, R, 3>, 3);
+  return go(k_ffn_few<GATE_UP, R, 4>, 4);
+}
+
 #define FFN_CK(expr)                               \
   do {                                             \
     if ((expr) != cudaSuccess) {                   \
@@ -442,7 +638,7 @@ extern "C" size_t camera_ffn_workspace_bytes(const camera_ffn_t* f, int64_t n_to
 extern "C" size_t camera_ffn_saved_bytes(const camera_ffn_t* f, int64_t n_tokens) {
   camera::FfnShape s;
   if (camera::check_ffn(f, n_tokens, &s) != CAMERA_OK) return 0;
-  return camera::up256((size_t)4 * s.T * s.fp + 1);
+  return camera::saved_lo_offset(s) + camera::up256((size_t)2 * s.T * s.fp + 1);
 }
 
 extern "C" int camera_ffn_forward(const camera_ffn_t* f, const void* x, int64_t n_tokens, void* y, void* saved,
@@ -458,6 +654,24 @@ extern "C" int camera_ffn_forward(const camera_ffn_t* f, const void* x, int64_t 
   if (n_tokens > 0 && (x == nullptr || y == nullptr || ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(y)) & 15) ||
                        (reinterpret_cast<uintptr_t>(saved) & 31)))
     return CAMERA_ERR_INVALID_ARG;
+  if (n_tokens > 0 && n_tokens <= FEW_TOKENS) {
+    FfnFew w;
+    w.w0 = static_cast<const __nv_bfloat16*>(f->w_gate); w.w1 = static_cast<const __nv_bfloat16*>(f->w_up);
+    w.in = static_cast<const __nv_bfloat16*>(x);
+    w.w_ld = s.D; w.in_ld = s.D; w.out_ld = s.fp;
+    w.rows = s.F; w.k = s.D; w.T = (int)s.T;
+    w.out = reinterpret_cast<__nv_bfloat16*>(ws + l.h);
+    w.g = static_cast<uint16_t*>(saved); w.u_off = s.fp; w.lo_off = (long long)saved_lo_offset(s); w.act_ld = 2 * s.fp;
+    w.totals = reinterpret_cast<PlanTotals*>(ws);
+    // one tile of rows per CTA while that gives each SM two or three CTAs, then more rows per CTA (fewer reads of x)
+    FFN_CK(s.F <= 4096 ? (launch_few<true, 1>(w, st)) : (launch_few<true, 2>(w, st)));
+    w.w0 = w.w1 = static_cast<const __nv_bfloat16*>(f->w_down);
+    w.in = w.out; w.out = static_cast<__nv_bfloat16*>(y);
+    w.w_ld = s.ld; w.in_ld = s.fp; w.out_ld = s.D; w.rows = s.D; w.k = s.F;
+    w.g = nullptr; w.totals = nullptr;
+    FFN_CK((launch_few<false, 1>(w, st)));
+    return CAMERA_OK;
+  }
   FFN_CK(cudaMemsetAsync(ws, 0, sizeof(PlanTotals), st));
   if (n_tokens == 0) return CAMERA_OK;
   const int n_pairs = sm_pairs();
@@ -469,8 +683,9 @@ extern "C" int camera_ffn_forward(const camera_ffn_t* f, const void* x, int64_t 
   q.h = reinterpret_cast<__nv_bfloat16*>(ws + l.h);
   q.h_ld = s.fp;
   q.act_ld = 2 * s.fp;
-  q.g = static_cast<__nv_bfloat16*>(saved);
+  q.g = static_cast<uint16_t*>(saved);
   q.u = saved ? q.g + s.fp : nullptr;
+  q.lo_off = (long long)saved_lo_offset(s);
   q.n_prob = 1;
   q.prob[0] = FfnProblem{(int)s.T, s.F, 0, 0, nullptr, 0, 0};
   q.n_kb = (s.D + UMMA_BK - 1) / UMMA_BK;
@@ -522,10 +737,10 @@ extern "C" int camera_ffn_backward(const camera_ffn_t* f, const void* x, const v
   q.wait_limit_ns = current_wait_limit_ns();
   q.h = reinterpret_cast<__nv_bfloat16*>(ws + l.h);
   q.h_ld = s.fp;
-  // g and u are interleaved row by row in `saved`, dg and du the same way in the workspace
-  q.act_ld = 2 * s.fp;
-  q.g = static_cast<__nv_bfloat16*>(const_cast<void*>(saved));
+  q.act_ld = 2 * s.fp;          // dg and du share rows in the workspace as G and U do in `saved`
+  q.g = static_cast<uint16_t*>(const_cast<void*>(saved));
   q.u = q.g + s.fp;
+  q.lo_off = (long long)saved_lo_offset(s);
   q.dg = reinterpret_cast<__nv_bfloat16*>(ws + l.dg);
   q.du = q.dg + s.fp;
   // dH and its element-wise part
