@@ -1,177 +1,436 @@
 // Operators over rows of vocabulary logits: the log-probability of a given token with the entropy and the top
 // alternatives of its distribution, and the distillation loss against a teacher's top log-probabilities with its gradient.
 //
-// With z = x / temperature, c = log2(e) / temperature and m the largest logit met so far, a thread keeps
-//   s = sum 2^((x - m) c)   and, for the entropy,   t = sum 2^((x - m) c) (x - m) c
-// and rescales both when m grows, so one pass over the row gives
-//   lse = m / temperature + ln s,   log p_v = ((x_v - m) c - log2 s) ln 2,   H = (log2 s - t / s) ln 2.
-// The difference is formed before the scaling: a row filled with the type's lowest value then has differences of 0 and
-// not of infinity minus infinity.  m starts at the lowest finite fp32 value, so a logit of minus infinity has the weight
-// 2^-inf = 0 and a row of them ends with s = 0.  A NaN or an infinite logit makes s NaN (infinity minus itself), which
-// is how such a row is recognised.  All sums are fp32 over at most a few hundred terms a thread, then a tree.
+// With z = x / temperature and c = log2(e) / temperature, a thread takes a reference m (x c for the largest x of the
+// first logits it reads) and sums over its share of the row
+//   s = sum 2^(x c - m)   and, for the entropy,   t = sum 2^(x c - m) (x c - m);
+// the threads' sums are joined by scaling with 2^(m_i - max m).  One pass over the row then gives
+//   ln sum exp z = (m + log2 s) ln 2,   log p_v = (x_v c - m - log2 s) ln 2,   H = (log2 s - t / s) ln 2.
+// The reference does not follow the maximum: fp32 holds 2^(x c - m) for any x c up to m + 127, and scaling loses no
+// precision, so no logit has to be compared.  A row whose sum ends outside
+// [2^-60, 2^120] (masked at the start, larger further on, all of it the type's lowest value, NaN, infinity: nothing an
+// ordinary row does) is walked again with differences formed before the scaling and a running maximum (walk_careful).
+// All sums are fp32 over at most a few hundred terms a thread, then a tree in a fixed order.
+//
+// Bound by reading the logits once; the arithmetic comes close behind (an exponential per logit: 16 a clock and SM), so
+// the multiply-adds run in pairs (f32x2) and the loop holds nothing else.  Few rows are split over the CTAs of a cluster,
+// which exchange their sums (and alternatives) through distributed shared memory.
 #include <float.h>
 #include <math.h>
 
+#include <atomic>
+#include <type_traits>
+
 #include "common.cuh"
+#include "umma_pair.cuh"
 
 namespace camera {
 
 namespace {
 
-constexpr int V_THREADS = 512;
+constexpr int V_THREADS = 256;
 constexpr int V_WARPS = V_THREADS / 32;
-constexpr int V_UNROLL = 4;                // 16-byte loads in flight per thread
-constexpr int V_CAND = 1024;               // candidates for the top alternatives kept in shared memory
+constexpr int V_MAX_SPLIT = 8;             // CTAs that can share a row
 constexpr float D_FLOOR = -150.f;          // 2^-150 is 0 in fp32: a floor for exponents that multiply a zero weight
+constexpr float LN2 = 0.693147180559945309f;
+constexpr float LOG2E = 1.44269504088896341f;
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-
-// A row of `n` logits as the threads walk it: up to 15 bytes of single elements before the first 16-byte boundary,
-// whole 16-byte vectors, single elements after the last.  Vector v belongs to thread v % V_THREADS, head and tail
-// element i to thread i.
-template <typename T>
-struct Row {
-  static constexpr int N = Vec16<T>::N;
-  const T* p;
-  int n, head, n_vec, tail;
-  __device__ __forceinline__ Row(const T* row, int len) : p(row), n(len) {
-    const int mis = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
-    head = mis ? min(N - mis, len) : 0;
-    n_vec = (len - head) / N;
-    tail = len - head - n_vec * N;
-  }
-  __device__ __forceinline__ const T* vec(int v) const { return p + head + (size_t)v * N; }
-  __device__ __forceinline__ int vec_index(int v) const { return head + v * N; }
-  __device__ __forceinline__ int tail_index(int i) const { return head + n_vec * N + i; }
-};
+__device__ __forceinline__ float max_nan(float a, float b) {      // NaN if either is
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(r)
+      : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)),
+        "l"(*reinterpret_cast<unsigned long long*>(&c)));
+  return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(r)
+      : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
+  return *reinterpret_cast<float2*>(&r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(r)
+      : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
+  return *reinterpret_cast<float2*>(&r);
+}
 
 __device__ __forceinline__ uint4 ld_stream(const void* p) {
   uint4 v;
   asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
   return v;
 }
-template <typename T> __device__ __forceinline__ void unpack(const uint4& v, float* out);
-template <> __device__ __forceinline__ void unpack<float>(const uint4& v, float* out) {
-  out[0] = __uint_as_float(v.x); out[1] = __uint_as_float(v.y); out[2] = __uint_as_float(v.z); out[3] = __uint_as_float(v.w);
-}
-template <> __device__ __forceinline__ void unpack<__nv_bfloat16>(const uint4& v, float* out) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    out[2 * i] = __uint_as_float(w[i] << 16);
-    out[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+
+// What depends on the element type: how a 16-byte vector becomes pairs of floats, its maximum, minus infinity.
+template <typename T> struct Elem;
+template <> struct Elem<float> {
+  static constexpr int N = 4;
+  static constexpr uint32_t NEG_INF = 0xff800000u;
+  __device__ __forceinline__ static void pairs(const uint4& v, float2* x) {
+    x[0] = make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
+    x[1] = make_float2(__uint_as_float(v.z), __uint_as_float(v.w));
   }
+  // running maximum in the raw form of two words; NaN is passed over
+  __device__ __forceinline__ static uint4 max4(const uint4& a, const uint4& b) {
+    return make_uint4(__float_as_uint(fmaxf(__uint_as_float(a.x), __uint_as_float(b.x))),
+                      __float_as_uint(fmaxf(__uint_as_float(a.y), __uint_as_float(b.y))),
+                      __float_as_uint(fmaxf(__uint_as_float(a.z), __uint_as_float(b.z))),
+                      __float_as_uint(fmaxf(__uint_as_float(a.w), __uint_as_float(b.w))));
+  }
+  __device__ __forceinline__ static float put(float v) { return v; }
+};
+template <> struct Elem<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static constexpr uint32_t NEG_INF = 0xff80ff80u;
+  __device__ __forceinline__ static void pairs(const uint4& v, float2* x) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+  }
+  __device__ __forceinline__ static uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  __device__ __forceinline__ static uint4 max4(const uint4& a, const uint4& b) {
+    return make_uint4(max2(a.x, b.x), max2(a.y, b.y), max2(a.z, b.z), max2(a.w, b.w));
+  }
+  __device__ __forceinline__ static __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
+};
+template <typename T>
+__device__ __forceinline__ float vec_max(const uint4& v) {
+  float2 x[Elem<T>::N / 2];
+  Elem<T>::pairs(v, x);
+  float m = fmaxf(x[0].x, x[0].y);
+#pragma unroll
+  for (int i = 1; i < Elem<T>::N / 2; ++i) m = fmaxf(m, fmaxf(x[i].x, x[i].y));
+  return m;
 }
 
-// The running sums of one thread (or of a whole row).
-struct Stats {
-  float m, s, t, r;      // r: the part of s from tokens outside the teacher's list
-  __device__ __forceinline__ void init() { m = -FLT_MAX; s = 0.f; t = 0.f; r = 0.f; }
-  template <bool ENT, bool REST>
-  __device__ __forceinline__ void raise(float to, float c) {      // to >= m
-    const float d = fmaxf((m - to) * c, D_FLOOR), f = ex2((m - to) * c);
-    if (ENT) t = f * fmaf(d, s, t);
-    s *= f;
-    if (REST) r *= f;
-    m = to;
+// A row of `n` logits, or the part of it that CTA `part` of 2^lg walks: single elements before the first 16-byte
+// boundary (part 0), whole 16-byte vectors [v_begin, v_end), single elements after the last (last part).  Vector v belongs to
+// thread (v - v_begin) % V_THREADS, single element i of head or tail to thread i.
+template <typename T>
+struct Row {
+  static constexpr int N = Elem<T>::N;
+  const T* p;
+  int first;                 // index of the first element of vector 0
+  int head, v_begin, v_end, tail, tail_at;
+  __device__ __forceinline__ Row(const T* row, int n, int part, int lg) : p(row) {
+    const int mis = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    first = mis ? min(N - mis, n) : 0;
+    const int n_vec = (n - first) / N;
+    v_begin = (n_vec * part) >> lg;
+    v_end = (n_vec * (part + 1)) >> lg;
+    head = part == 0 ? first : 0;
+    tail_at = first + n_vec * N;
+    tail = part + 1 == 1 << lg ? n - tail_at : 0;
   }
-  template <bool ENT>
-  __device__ __forceinline__ float add(float x, float c) {        // x <= m
-    const float d = (x - m) * c, e = ex2(d);
-    s += e;
-    if (ENT) t = fmaf(e, fmaxf(d, D_FLOOR), t);
-    return e;
-  }
-  template <bool ENT, bool REST>
-  __device__ __forceinline__ void merge(const Stats& o, float c) {
-    const float to = fmaxf(m, o.m);
-    Stats b = o;
-    raise<ENT, REST>(to, c);
-    b.raise<ENT, REST>(to, c);
-    s += b.s;
-    if (ENT) t += b.t;
-    if (REST) r += b.r;
+  __device__ __forceinline__ const T* vec(int v) const { return p + first + (size_t)v * N; }
+  __device__ __forceinline__ int vec_index(int v) const { return first + v * N; }
+  __device__ __forceinline__ bool holds(int i) const {       // is element i of the row in this part?
+    if (i < first) return head != 0;
+    if (i >= tail_at) return tail != 0;
+    const int v = (i - first) / N;
+    return v >= v_begin && v < v_end;
   }
 };
 
-// One thread's share of the row.  listed: a bit per element of the row that is on the teacher's list (REST only).
-template <typename T, bool ENT, bool REST>
-__device__ __forceinline__ Stats walk_row(const Row<T>& row, float c, const uint32_t* listed) {
-  constexpr int N = Row<T>::N;
-  Stats st;
-  st.init();
-  auto single = [&](int i) {
-    const float x = to_f32<T>(row.p[i]);
-    if (x > st.m) st.raise<ENT, REST>(x, c);
-    const float e = st.add<ENT>(x, c);
-    if (REST && !((listed[i >> 5] >> (i & 31)) & 1u)) st.r += e;
-  };
-  if ((int)threadIdx.x < row.head) single(threadIdx.x);
-  if ((int)threadIdx.x < row.tail) single(row.tail_index(threadIdx.x));
-  for (int v0 = threadIdx.x; v0 < row.n_vec; v0 += V_UNROLL * V_THREADS) {
-    uint4 raw[V_UNROLL];
-#pragma unroll
-    for (int u = 0; u < V_UNROLL; ++u) {
-      const int v = v0 + u * V_THREADS;
-      if (v < row.n_vec) raw[u] = ld_stream(row.vec(v));
-    }
-#pragma unroll
-    for (int u = 0; u < V_UNROLL; ++u) {
-      const int v = v0 + u * V_THREADS;
-      if (v >= row.n_vec) break;
-      float x[N];
-      unpack<T>(raw[u], x);
-      float top = x[0];
-#pragma unroll
-      for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
-      if (top > st.m) st.raise<ENT, REST>(top, c);
-      float e[N], es = 0.f;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float d = (x[i] - st.m) * c;
-        e[i] = ex2(d);
-        es += e[i];
-        if (ENT) st.t = fmaf(e[i], fmaxf(d, D_FLOOR), st.t);
-      }
-      st.s += es;
-      if (REST) {
-        const int i0 = row.vec_index(v);
-        const uint32_t bits = __funnelshift_r(listed[i0 >> 5], listed[(i0 >> 5) + 1], i0 & 31) & ((1u << N) - 1);
-        if (bits) {             // the others are added up again: subtracting the listed ones would cancel
-          es = 0.f;
-#pragma unroll
-          for (int i = 0; i < N; ++i)
-            if (!((bits >> i) & 1u)) es += e[i];
-        }
-        st.r += es;
-      }
-    }
+// Sums of a thread, a CTA or a row.  ref: the reference, in powers of two (or, of a careful walk, in logits); r: the part
+// of s from tokens outside the teacher's list.
+struct Sums {
+  float ref, s, t, r;
+};
+// The sums brought to the reference `to` >= ref; ENT and REST say whether t and r are in use.
+template <bool CAREFUL, bool ENT, bool REST>
+__device__ __forceinline__ void raise(Sums& a, float to, float c) {
+  const float d = CAREFUL ? (a.ref - to) * c : a.ref - to, f = ex2(d);
+  if (ENT) a.t = f * fmaf(fmaxf(d, D_FLOOR), a.s, a.t);
+  a.s *= f;
+  if (REST) a.r *= f;
+  a.ref = to;
+}
+
+// The rows first, first + stride, .. whose weight is not 0 (null: all rows).  Weights are read one row ahead, so that
+// nothing waits for one.
+struct RowWalk {
+  int at;
+  float ahead;
+  __device__ __forceinline__ void begin(const float* weight, int rows, int first) {
+    at = first;
+    ahead = weight != nullptr && at < rows ? weight[at] : 1.f;
   }
+  __device__ __forceinline__ int next(const float* weight, int rows, int stride) {
+    while (at < rows) {
+      const float w = ahead;
+      const int r = at;
+      at += stride;
+      if (weight != nullptr && at < rows) ahead = weight[at];
+      if (w != 0.f) return r;
+    }
+    return rows;
+  }
+};
+
+// Chunks of PER vectors a thread, SLOTS of them in the ring.  Both shapes are 96 KB, so that two CTAs fit an SM.  Larger
+// chunks cost fewer instructions an element; the finer ring leaves room for the next row while a part is held.
+template <int PER_, int SLOTS_>
+struct Ring {
+  static constexpr int PER = PER_, SLOTS = SLOTS_;
+  static constexpr int CHUNK = PER * V_THREADS;              // vectors
+  static constexpr int BYTES = SLOTS * CHUNK * 16;
+  static constexpr int HELD = (SLOTS - 1) * CHUNK;           // vectors of the longest part that stays between two passes
+};
+using RingStream = Ring<8, 3>;
+using RingHold = Ring<4, 6>;
+static_assert(RingStream::BYTES == 96 * 1024 && RingHold::BYTES == 96 * 1024, "two CTAs per SM");
+
+// The logits' way into the CTA: every thread copies its own 16-byte vectors with cp.async into its own places of a ring
+// in shared memory, over the ends of rows: while the sums of a row are joined and its results written, the next row is on
+// its way.  A thread reads only what it copied itself, so there is nothing to wait for but its own copies
+// (cp.async.wait_group) and no barrier.  One copy group is committed per chunk consumed.
+template <typename T, typename RG>
+struct Feed {
+  const T* logits;
+  long long ld;
+  const float* weight;               // rows with weight 0 are passed over (null: none are)
+  int rows, stride, vocab, part, lg;
+  int r;                             // row the next chunk belongs to
+  uint32_t dst0, dst;                // this thread's place in slot 0 and in the next slot
+  const T* src;                      // this thread's first vector of the next chunk
+  int whole;                         // vectors from the chunk's first to the end of the part
+  RowWalk walk;
+  __device__ __forceinline__ void begin(int first) {
+    dst = dst0;
+    walk.begin(weight, rows, first);
+    open();
+  }
+  __device__ __forceinline__ void open() {
+    r = walk.next(weight, rows, stride);
+    if (r >= rows) return;
+    const Row<T> row(logits + r * ld, vocab, part, lg);
+    src = row.vec(row.v_begin) + (size_t)threadIdx.x * Row<T>::N;
+    whole = row.v_end - row.v_begin;
+  }
+  __device__ __forceinline__ void copy(int u) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + (uint32_t)(u * V_THREADS * 16)),
+                 "l"(src + (size_t)u * V_THREADS * Row<T>::N)
+                 : "memory");
+  }
+  __device__ __forceinline__ void issue() {
+    if (r < rows) {
+      if (whole >= RG::CHUNK) {
+#pragma unroll
+        for (int u = 0; u < RG::PER; ++u) copy(u);
+      } else {
+#pragma unroll
+        for (int u = 0; u < RG::PER; ++u)
+          if ((int)threadIdx.x + u * V_THREADS < whole) copy(u);
+      }
+      src += (size_t)RG::CHUNK * Row<T>::N;
+      whole -= RG::CHUNK;
+      dst += RG::CHUNK * 16;
+      if (dst == dst0 + RG::BYTES) dst = dst0;
+      if (whole <= 0) open();
+    }
+    commit();
+  }
+  __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+  // the oldest chunk not yet consumed has landed
+  __device__ __forceinline__ static void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(RG::SLOTS - 1) : "memory"); }
+};
+// Chunks of a part, one at least; and the offset in the ring behind the chunk at `at`.
+template <typename RG>
+__device__ __forceinline__ int row_chunks(int n_vec) { return n_vec <= RG::CHUNK ? 1 : (n_vec + RG::CHUNK - 1) / RG::CHUNK; }
+template <typename RG>
+__device__ __forceinline__ int next_chunk(int at) { return at + RG::CHUNK * 16 == RG::BYTES ? 0 : at + RG::CHUNK * 16; }
+
+// One thread's share of the row, whose chunks lie in the ring from offset `at` on (moved past the row).  mark (REST): a
+// byte per vector of the part with a bit per element on the teacher's list.  TOP: *top receives the largest logit of the
+// share (minus infinity if it has none).  HOLD: the chunks stay in the ring; else each makes room for the next copy.
+template <typename T, typename RG, bool ENT, bool REST, bool TOP, bool HOLD>
+__device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>& feed, const uint8_t* ring, int& at,
+                                         const uint8_t* mark, const int* list, int k, float* top) {
+  constexpr int N = Elem<T>::N;
+  constexpr uint32_t NI = Elem<T>::NEG_INF;
+  const uint4 nothing = make_uint4(NI, NI, NI, NI);          // minus infinity has no weight
+  const int tid = threadIdx.x;
+  uint4 big = nothing;
+  float2 s2 = make_float2(0.f, 0.f), t2 = make_float2(0.f, 0.f);
+  const float2 c2 = make_float2(c, c);
+  float2 ref2 = make_float2(0.f, 0.f);
+  float single[2] = {-INFINITY, -INFINITY}, on_list = 0.f;
+  if (tid < row.head) single[0] = to_f32<T>(row.p[tid]);
+  if (tid < row.tail) single[1] = to_f32<T>(row.p[row.tail_at + tid]);
+  const uint8_t* mine = ring + tid * 16;
+  if (REST) mark += tid;
+  bool first = true;
+  int left = row.v_end - row.v_begin;                        // vectors of the part not yet walked
+  do {
+    Feed<T, RG>::wait();
+    uint4 raw[RG::PER];
+#pragma unroll
+    for (int u = 0; u < RG::PER; ++u) raw[u] = *reinterpret_cast<const uint4*>(mine + at + u * V_THREADS * 16);
+    if (left < RG::CHUNK) {
+#pragma unroll
+      for (int u = 0; u < RG::PER; ++u)
+        if (tid + u * V_THREADS >= left) raw[u] = nothing;
+    }
+    at = next_chunk<RG>(at);
+    if (TOP || first) {
+#pragma unroll
+      for (int u = 0; u < RG::PER; ++u) big = Elem<T>::max4(big, raw[u]);
+    }
+    if (first) {
+      const float m = fmaxf(fmaxf(vec_max<T>(big), fmaxf(single[0], single[1])) * c, -126.f);
+      ref2 = make_float2(-m, -m);
+      first = false;
+    }
+#pragma unroll
+    for (int u = 0; u < RG::PER; ++u) {
+      float2 x[N / 2];
+      Elem<T>::pairs(raw[u], x);
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) {
+        float2 d = fma2(x[i], c2, ref2);
+        if (ENT) d = make_float2(max_nan(d.x, D_FLOOR), max_nan(d.y, D_FLOOR));
+        x[i] = make_float2(ex2(d.x), ex2(d.y));
+        if (ENT) t2 = fma2(x[i], d, t2);
+      }
+      if (REST) {
+        const uint32_t bits = mark[u * V_THREADS];           // 0 past the part's end
+        if (bits) {
+#pragma unroll
+          for (int i = 0; i < N / 2; ++i) {
+            if ((bits >> (2 * i)) & 1u) { on_list += x[i].x; x[i].x = 0.f; }
+            if ((bits >> (2 * i + 1)) & 1u) { on_list += x[i].y; x[i].y = 0.f; }
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) s2 = add2(s2, x[i]);
+    }
+    if (REST) mark += RG::CHUNK;
+    if (HOLD) Feed<T, RG>::commit(); else feed.issue();
+    left -= RG::CHUNK;
+  } while (left > 0);
+  Sums st;
+  st.ref = -ref2.x;
+  st.s = s2.x + s2.y;
+  st.t = ENT ? t2.x + t2.y : 0.f;
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    if (tid >= (q == 0 ? row.head : row.tail)) continue;
+    float d = fmaf(single[q], c, ref2.x);
+    if (ENT) d = max_nan(d, D_FLOOR);
+    const float e = ex2(d);
+    if (ENT) st.t = fmaf(e, d, st.t);
+    bool listed = false;
+    if (REST) {
+      const int i = q == 0 ? tid : row.tail_at + tid;
+      for (int j = 0; j < k; ++j) listed |= list[j] == i;
+    }
+    if (listed) on_list += e; else st.s += e;
+  }
+  st.r = st.s;
+  if (REST) st.s += on_list;
+  if (TOP) *top = fmaxf(vec_max<T>(big), fmaxf(single[0], single[1]));
   return st;
 }
 
-// Joins the threads' sums; every thread gets the row's.
-template <bool ENT, bool REST>
-__device__ __forceinline__ Stats join(Stats st, float c, Stats* part) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    Stats b;
-    b.m = __shfl_xor_sync(0xffffffffu, st.m, o);
-    b.s = __shfl_xor_sync(0xffffffffu, st.s, o);
-    if (ENT) b.t = __shfl_xor_sync(0xffffffffu, st.t, o);
-    if (REST) b.r = __shfl_xor_sync(0xffffffffu, st.r, o);
-    st.merge<ENT, REST>(b, c);
-  }
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = st;
-  __syncthreads();
-  st = part[0];
-  for (int w = 1; w < V_WARPS; ++w) st.merge<ENT, REST>(part[w], c);
+// The same from global memory, with a running maximum and differences formed before the scaling: right for any row, and
+// how a NaN or an infinite logit (infinity minus itself) shows as a NaN sum, a row of minus infinities as s = 0.
+template <typename T, bool ENT, bool REST>
+__device__ __noinline__ Sums walk_careful(const Row<T> row, float c, const int* list, int k) {
+  Sums st{-FLT_MAX, 0.f, 0.f, 0.f};
+  auto one = [&](int i) {
+    const float x = to_f32<T>(row.p[i]);
+    if (x > st.ref) raise<true, ENT, REST>(st, x, c);
+    const float d = (x - st.ref) * c, e = ex2(d);
+    st.s += e;
+    if (ENT) st.t = fmaf(e, fmaxf(d, D_FLOOR), st.t);
+    if (REST) {
+      bool listed = false;
+      for (int j = 0; j < k; ++j) listed |= list[j] == i;
+      if (!listed) st.r += e;
+    }
+  };
+  if ((int)threadIdx.x < row.head) one(threadIdx.x);
+  if ((int)threadIdx.x < row.tail) one(row.tail_at + threadIdx.x);
+  for (int v = row.v_begin + threadIdx.x; v < row.v_end; v += V_THREADS)
+    for (int i = 0; i < Elem<T>::N; ++i) one(row.vec_index(v) + i);
   return st;
 }
+
+// Shared memory of a CTA that joins sums.
+struct JoinScratch {
+  Sums warp[2][V_WARPS];           // joins alternate, so that none overwrites what another thread still reads
+  Sums cta[2][V_MAX_SPLIT];        // of the CTAs that share the row, written by each of them; rows alternate
+};
+// The sums of WIDTH neighbouring lanes joined, in all of them.
+template <int WIDTH, bool CAREFUL, bool ENT, bool REST>
+__device__ __forceinline__ Sums join_lanes(Sums st, float c) {
+  float to = st.ref;
+#pragma unroll
+  for (int o = WIDTH / 2; o; o >>= 1) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, o));
+  raise<CAREFUL, ENT, REST>(st, to, c);
+#pragma unroll
+  for (int o = WIDTH / 2; o; o >>= 1) {
+    st.s += __shfl_xor_sync(0xffffffffu, st.s, o);
+    if (ENT) st.t += __shfl_xor_sync(0xffffffffu, st.t, o);
+    if (REST) st.r += __shfl_xor_sync(0xffffffffu, st.r, o);
+  }
+  return st;
+}
+// Sums of the CTA from those of its first V_THREADS threads, the same in every thread of the CTA.
+template <bool CAREFUL, bool ENT, bool REST>
+__device__ __forceinline__ Sums join_cta(Sums st, float c, int& join_turn, JoinScratch& js) {
+  Sums* const slots = js.warp[join_turn];
+  join_turn ^= 1;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (warp < V_WARPS) {
+    st = join_lanes<32, CAREFUL, ENT, REST>(st, c);
+    if (lane == 0) slots[warp] = st;
+  }
+  __syncthreads();
+  return join_lanes<V_WARPS, CAREFUL, ENT, REST>(slots[lane % V_WARPS], c);
+}
+// The CTAs of a cluster may write to each other's shared memory once all of them run: each says so when it starts and
+// waits for the others where it first needs them.
+__device__ __forceinline__ void cluster_started() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_all_started() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
+// Hands this CTA's sums to every CTA of the cluster; after the cluster's barrier join_split adds them up.
+__device__ __forceinline__ void publish_sums(const Sums& st, int part, int parts, int turn, JoinScratch& js) {
+  if ((int)threadIdx.x < parts) {
+    const uint32_t dst = map_to_cta(smem_u32(&js.cta[turn][part]), threadIdx.x);
+    st_cluster_u32(dst, __float_as_uint(st.ref));
+    st_cluster_u32(dst + 4, __float_as_uint(st.s));
+    st_cluster_u32(dst + 8, __float_as_uint(st.t));
+    st_cluster_u32(dst + 12, __float_as_uint(st.r));
+  }
+}
+template <bool CAREFUL, bool ENT, bool REST>
+__device__ __forceinline__ Sums join_split(int parts, float c, int turn, const JoinScratch& js) {
+  const int lane = threadIdx.x % V_MAX_SPLIT;
+  Sums st{CAREFUL ? -FLT_MAX : -INFINITY, 0.f, 0.f, 0.f};
+  if (lane < parts) st = js.cta[turn][lane];
+  return join_lanes<V_MAX_SPLIT, CAREFUL, ENT, REST>(st, c);
+}
+__device__ __forceinline__ bool sums_ordinary(const Sums& st) { return st.s >= 0x1p-60f && st.s <= 0x1p120f; }
 
 // Order-preserving image of a float (both zeros alike) and the 64-bit key by which alternatives are ranked: larger value
 // first, then lower index.
@@ -183,57 +442,125 @@ __device__ __forceinline__ unsigned long long rank_key(float x, int i) {
   return ((unsigned long long)value_key(x) << 32) | (uint32_t)~i;
 }
 constexpr uint32_t KEY_NEG_INF = 0x007fffffu;     // value_key(-inf)
+constexpr int V_BINS = 256;
 
+// CAND: candidates kept in shared memory.  A CTA that shares its row with others has fewer to look through and needs room
+// for the others' alternatives.
+template <int CAND_>
 struct TopScratch {
-  uint32_t group_key[V_THREADS];         // largest value of every thread's share
+  static constexpr int CAND = CAND_;
+  int hist[V_BINS];
   int active[V_THREADS];                 // the shares that can hold an alternative
-  unsigned long long cand[V_CAND];
-  int n_active, n_cand, count;
+  unsigned long long cand[CAND];
+  float w_max[V_WARPS], w_min[V_WARPS];
+  int last_bin, n_active, n_cand, count;
+  uint32_t floor_key;                    // smallest of the active shares' maxima
 };
 
 // Calls f(index, value) for every element of the shares listed in sc.active[0 .. n_active).
-template <typename T, typename F>
-__device__ __forceinline__ void for_active(const Row<T>& row, const TopScratch& sc, F f) {
-  constexpr int N = Row<T>::N;
-  const int per = (row.n_vec + V_THREADS - 1) / V_THREADS + 1;      // the last "vector" stands for head and tail
-  const int total = sc.n_active * per;
-  for (int q = threadIdx.x; q < total; q += V_THREADS) {
-    const int g = sc.active[q / per], k = q % per;
-    if (k == per - 1) {
-      if (g < row.head) f(g, to_f32<T>(row.p[g]));
-      if (g < row.tail) f(row.tail_index(g), to_f32<T>(row.p[row.tail_index(g)]));
-      continue;
-    }
-    const int v = g + k * V_THREADS;
-    if (v >= row.n_vec) continue;
-    float x[N];
-    unpack<T>(ld_stream(row.vec(v)), x);
+template <typename T, typename SC, typename F>
+__device__ __forceinline__ void for_active(const Row<T>& row, const SC& sc, F f) {
+  constexpr int N = Elem<T>::N;
+  const unsigned per = (unsigned)(row.v_end - row.v_begin + V_THREADS - 1) / V_THREADS;
+  const unsigned total = (unsigned)sc.n_active * per;
+  for (unsigned q0 = threadIdx.x; q0 < total; q0 += 4 * V_THREADS) {
+    uint4 raw[4];
+    int at[4];
 #pragma unroll
-    for (int i = 0; i < N; ++i) f(row.vec_index(v) + i, x[i]);
+    for (int u = 0; u < 4; ++u) {
+      const unsigned q = q0 + u * V_THREADS;
+      at[u] = -1;
+      if (q < total) {
+        const unsigned g = q / per;
+        const int v = row.v_begin + sc.active[g] + (int)(q - g * per) * V_THREADS;
+        if (v < row.v_end) { at[u] = row.vec_index(v); raw[u] = ld_stream(row.vec(v)); }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (at[u] < 0) continue;
+      float2 x[N / 2];
+      Elem<T>::pairs(raw[u], x);
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) { f(at[u] + 2 * i, x[i].x); f(at[u] + 2 * i + 1, x[i].y); }
+    }
+  }
+  for (int q = threadIdx.x; q < sc.n_active; q += V_THREADS) {
+    const int g = sc.active[q];
+    if (g < row.head) f(g, to_f32<T>(row.p[g]));
+    if (g < row.tail) f(row.tail_at + g, to_f32<T>(row.p[row.tail_at + g]));
   }
 }
 
-// The (up to) n elements of the row with the largest keys, logits of minus infinity left out, as sc.cand[0 .. sc.n_cand)
-// in any order; at least n of them (if the row has as many), possibly a few more.
+// The (up to) n elements of this CTA's part with the largest keys, logits of minus infinity left out, as
+// sc.cand[0 .. sc.n_cand) in any order; at least n of them (if there are as many), possibly more.
 // A share whose maximum is below the n-th largest of the shares' maxima holds none of the n largest elements, so only
-// about n of the V_THREADS shares are read again.  The threshold is found by bisection on the key bits; where the
-// elements at or above it outgrow the candidate list (long runs of equal logits), the bisection goes on over the
-// elements' 64-bit keys, which are all distinct.
-template <typename T>
-__device__ __forceinline__ void collect_top(const Row<T>& row, float own_max, bool own_any, int n, TopScratch& sc) {
-  const uint32_t mine = own_any ? value_key(own_max) : 0u;
-  uint32_t lo = KEY_NEG_INF + 1, hi = 0xffffffffu;    // invariant: count(>= lo) is enough (or lo is the lowest), count(>= hi) is not
-  __syncthreads();
-  while (hi - lo > 1) {
-    const uint32_t mid = lo + (hi - lo) / 2;
-    const int cnt = __syncthreads_count(mine >= mid);
-    if (cnt >= n) { lo = mid; if (cnt <= n + n / 4) break; } else hi = mid;
+// about n of the V_THREADS shares are read again.  A histogram of the maxima between their least and their largest finds
+// the threshold; where its bins are too coarse (one logit far above the rest), bisection over the key bits does.  Where
+// the elements at or above the threshold outgrow the candidate list (long runs of equal logits), the bisection goes on
+// over the elements' 64-bit keys, which are all distinct.
+template <typename T, typename SC>
+__device__ __noinline__ void collect_top(const Row<T> row, float own_max, int n, SC& sc) {
+  constexpr int V_CAND = SC::CAND;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const bool any = own_max > -INFINITY;
+  const uint32_t mine = any ? value_key(own_max) : 0u;
+  static_assert(V_BINS <= V_THREADS, "one bin per thread to clear");
+  if (tid < V_BINS) sc.hist[tid] = 0;
+  if (tid == 0) { sc.n_active = 0; sc.n_cand = 0; sc.floor_key = 0xffffffffu; sc.last_bin = V_BINS - 1; }
+  float hi = own_max, lo = any ? own_max : INFINITY;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
   }
-  if (threadIdx.x == 0) { sc.n_active = 0; sc.n_cand = 0; }
+  if (lane == 0) { sc.w_max[warp] = hi; sc.w_min[warp] = lo; }
   __syncthreads();
-  if (mine >= lo) sc.active[atomicAdd(&sc.n_active, 1)] = threadIdx.x;
+  hi = sc.w_max[0]; lo = sc.w_min[0];
+#pragma unroll
+  for (int w = 1; w < V_WARPS; ++w) { hi = fmaxf(hi, sc.w_max[w]); lo = fminf(lo, sc.w_min[w]); }
+  if (!(hi > -INFINITY)) return;                       // nothing but minus infinity in this part (uniform)
+  const float range = hi - lo;
+  const float scale = range > 0.f && range < FLT_MAX ? (V_BINS - 1) / range : 0.f;
+  const int bin = min(V_BINS - 1, (int)((hi - own_max) * scale));     // falls as own_max grows
+  if (any) atomicAdd(&sc.hist[bin], 1);
   __syncthreads();
-  unsigned long long klo = (unsigned long long)lo << 32, khi = ~0ull;
+  if (warp == 0) {
+    int c[V_BINS / 32], sum = 0;
+#pragma unroll
+    for (int i = 0; i < V_BINS / 32; ++i) { c[i] = sc.hist[lane * (V_BINS / 32) + i]; sum += c[i]; }
+    int before = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += v;
+    }
+    before -= sum;
+#pragma unroll
+    for (int i = 0; i < V_BINS / 32; ++i) {
+      if (before < n && before + c[i] >= n) sc.last_bin = lane * (V_BINS / 32) + i;
+      before += c[i];
+    }
+  }
+  __syncthreads();
+  bool active = any && bin <= sc.last_bin;
+  int n_active = __syncthreads_count(active);
+  if (n_active > 2 * n + 64) {
+    uint32_t klo = KEY_NEG_INF + 1, khi = 0xffffffffu;
+    while (khi - klo > 1) {                            // at most 32 rounds
+      const uint32_t mid = klo + (khi - klo) / 2;
+      const int cnt = __syncthreads_count(mine >= mid);
+      if (cnt >= n) { klo = mid; if (cnt <= n + n / 4) break; } else khi = mid;
+    }
+    active = any && mine >= klo;
+  }
+  if (active) {
+    sc.active[atomicAdd(&sc.n_active, 1)] = tid;
+    atomicMin(&sc.floor_key, mine);
+  }
+  __syncthreads();
+  // fewer shares than n with anything in them: their elements below the shares' maxima count as well
+  unsigned long long klo = (unsigned long long)(n_active < n ? KEY_NEG_INF + 1 : sc.floor_key) << 32, khi = ~0ull;
   for (int attempt = 0; attempt < 2; ++attempt) {
     for_active(row, sc, [&](int i, float x) {
       const unsigned long long k = rank_key(x, i);
@@ -248,7 +575,7 @@ __device__ __forceinline__ void collect_top(const Row<T>& row, float own_max, bo
     for (int it = 0; it < 64; ++it) {
       const unsigned long long mid = klo + (khi - klo) / 2;
       __syncthreads();
-      if (threadIdx.x == 0) { sc.count = 0; sc.n_cand = 0; }
+      if (tid == 0) { sc.count = 0; sc.n_cand = 0; }
       __syncthreads();
       int c = 0;
       for_active(row, sc, [&](int i, float x) { c += rank_key(x, i) >= mid; });
@@ -259,63 +586,155 @@ __device__ __forceinline__ void collect_top(const Row<T>& row, float own_max, bo
     }
     __syncthreads();
   }
-  if (threadIdx.x == 0) sc.n_cand = V_CAND;      // only if the logits changed while they were read
+  if (tid == 0) sc.n_cand = V_CAND;      // only if the logits changed while they were read
   __syncthreads();
 }
 
 struct LogprobArgs {
   const void* logits;
   long long ld;
-  int vocab, top_n;
+  int rows, vocab, top_n;
+  int lg;                   // 2^lg CTAs share a row
   float c, inv_tau;         // log2(e) / temperature, 1 / temperature
   const long long* targets;
   float *logprob, *entropy, *top_logprob;
   int* top_idx;
 };
 
-constexpr float LN2 = 0.693147180559945309f;
+// How log-probabilities and probabilities come from a row's logits: log2 q_v = x c - k, or for a row walked carefully
+// (x - m) c - log2s.
+struct Softmax {
+  float c, inv_tau, k, m, log2s;
+  bool careful;
+  __device__ __forceinline__ Softmax(const Sums& st, bool careful_, float c_, float inv_tau_) : c(c_), inv_tau(inv_tau_), careful(careful_) {
+    log2s = log2f(st.s);
+    m = st.ref;
+    k = st.ref + log2s;
+  }
+  __device__ __forceinline__ float q(float x) const { return ex2(careful ? (x - m) * c - log2s : fmaf(x, c, -k)); }
+  __device__ __forceinline__ float logprob(float x) const {
+    if (careful) return (x - m) * inv_tau - log2s * LN2;
+    const float d = fmaf(x, c, -m);
+    return d < -1e30f ? x * inv_tau : (d - log2s) * LN2;     // far below fp32's range once scaled, the rest does not count
+  }
+};
 
-template <typename T, bool ENT>
-__global__ void __launch_bounds__(V_THREADS) k_token_logprobs(const LogprobArgs a) {
-  __shared__ Stats part[V_WARPS];
-  __shared__ TopScratch sc;
-  const long long r = blockIdx.x;
-  const Row<T> row(static_cast<const T*>(a.logits) + r * a.ld, a.vocab);
-  const Stats own = walk_row<T, ENT, false>(row, a.c, nullptr);
-  const Stats st = join<ENT, false>(own, a.c, part);
-  const float log2s = log2f(st.s);
-  if (threadIdx.x == 0) {
-    if (a.logprob) {
-      const long long t = a.targets[r];
-      float lp = 0.f;
-      if (t >= 0 && t < a.vocab) {
-        lp = (to_f32<T>(row.p[t]) - st.m) * a.inv_tau - log2s * LN2;
-        if (st.s == 0.f) lp = -INFINITY;
+// A CTA, or (SPLIT) the CTAs of a cluster together, take row after row: blockIdx.x is the CTA's part of the row,
+// blockIdx.y its first row.
+template <typename T, bool ENT, bool TOP, bool SPLIT>
+__global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobArgs a) {
+  using RG = RingStream;
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ JoinScratch js;
+  using Scratch = TopScratch<SPLIT ? 512 : 1024>;
+  __shared__ typename std::conditional<TOP, Scratch, int>::type sc_raw;
+  __shared__ unsigned long long merged[TOP && SPLIT ? V_MAX_SPLIT * CAMERA_MAX_TOP : 1];    // 0: none
+  const int lg = SPLIT ? a.lg : 0, part = SPLIT ? blockIdx.x : 0, parts = 1 << lg;
+  const int tid = threadIdx.x;
+  if (SPLIT) cluster_started();
+  bool started = !SPLIT;
+  Feed<T, RG> feed;
+  feed.logits = static_cast<const T*>(a.logits);
+  feed.ld = a.ld; feed.weight = nullptr;
+  feed.rows = a.rows; feed.stride = gridDim.y; feed.vocab = a.vocab; feed.part = part; feed.lg = lg;
+  feed.dst0 = smem_u32(ring) + tid * 16;
+  feed.begin(blockIdx.y);
+#pragma unroll
+  for (int i = 0; i < RG::SLOTS; ++i) feed.issue();
+  int at = 0, turn = 0, join_turn = 0;
+  const bool first = part == 0 && tid == 0;
+  long long target = first && a.logprob && (int)blockIdx.y < a.rows ? a.targets[blockIdx.y] : -1;
+  for (int r = blockIdx.y; r < a.rows; r += gridDim.y, turn ^= 1) {
+    const Row<T> row(static_cast<const T*>(a.logits) + r * a.ld, a.vocab, part, lg);
+    // the target's logit, and the next row's target, on their way during the walk
+    const bool wanted = target >= 0 && target < a.vocab;
+    const float x_target = wanted ? to_f32<T>(row.p[target]) : 0.f;
+    if (first && a.logprob && r + (int)gridDim.y < a.rows) target = a.targets[r + gridDim.y];
+    float top = -INFINITY;
+    Sums st = walk_row<T, RG, ENT, false, TOP, false>(row, a.c, feed, ring, at, nullptr, nullptr, 0, &top);
+    st = join_cta<false, ENT, false>(st, a.c, join_turn, js);
+    if (SPLIT) {
+      if (!started) { cluster_all_started(); started = true; }
+      publish_sums(st, part, parts, turn, js);
+      cluster_sync_all();
+      st = join_split<false, ENT, false>(parts, a.c, turn, js);
+    }
+    const bool careful = !sums_ordinary(st);
+    if (careful) {
+      st = join_cta<true, ENT, false>(walk_careful<T, ENT, false>(row, a.c, nullptr, 0), a.c, join_turn, js);
+      if (SPLIT) {
+        cluster_sync_all();                              // every CTA has read the first round's sums
+        publish_sums(st, part, parts, turn, js);
+        cluster_sync_all();
+        st = join_split<true, ENT, false>(parts, a.c, turn, js);
       }
-      a.logprob[r] = lp;
     }
-    if (ENT) a.entropy[r] = st.s == 0.f ? 0.f : (log2s - st.t / st.s) * LN2;
-  }
-  if (a.top_n == 0) return;
-  int* const out_i = a.top_idx + r * a.top_n;
-  float* const out_v = a.top_logprob + r * a.top_n;
-  const bool usable = st.s > 0.f;                 // false for a NaN
-  if (usable) collect_top(row, own.m, own.s > 0.f, a.top_n, sc);
-  const int n_cand = usable ? sc.n_cand : 0;
-  for (int q = threadIdx.x; q < n_cand; q += V_THREADS) {
-    const unsigned long long k = sc.cand[q];
-    int rank = 0;
-    for (int j = 0; j < n_cand; ++j) rank += sc.cand[j] > k;
-    if (rank < a.top_n) {
-      const int i = (int)~(uint32_t)k;
-      out_i[rank] = i;
-      out_v[rank] = (to_f32<T>(row.p[i]) - st.m) * a.inv_tau - log2s * LN2;
+    const Softmax sm(st, careful, a.c, a.inv_tau);
+    if (first) {
+      if (a.logprob) a.logprob[r] = !wanted ? 0.f : st.s == 0.f ? -INFINITY : sm.logprob(x_target);
+      if (ENT) a.entropy[r] = st.s == 0.f ? 0.f : (sm.log2s - st.t / st.s) * LN2;
+    }
+    if constexpr (TOP) {
+      Scratch& sc = sc_raw;
+      const bool usable = st.s > 0.f;                    // false for a NaN
+      int n_cand = 0, n_out = 0;
+      const unsigned long long* cand = sc.cand;
+      if (usable) {
+        collect_top<T, Scratch>(row, top, a.top_n, sc);
+        __syncthreads();
+        n_cand = n_out = sc.n_cand;
+        if (SPLIT) {                                     // this part's best n go to the first CTA
+          for (int q = tid; q < max(n_cand, a.top_n); q += V_THREADS) {
+            const unsigned long long k = q < n_cand ? cand[q] : 0ull;
+            int rank = q;
+            if (q < n_cand) {
+              rank = 0;
+              for (int j = 0; j < n_cand; ++j) rank += cand[j] > k;
+            }
+            if (rank < a.top_n) {
+              const uint32_t dst = map_to_cta(smem_u32(&merged[part * a.top_n + rank]), 0);
+              st_cluster_u32(dst, (uint32_t)k);
+              st_cluster_u32(dst + 4, (uint32_t)(k >> 32));
+            }
+          }
+          cluster_sync_all();
+          cand = merged;
+          n_cand = n_out = parts * a.top_n;
+        }
+      }
+      if (part == 0) {
+        int* const out_i = a.top_idx + r * a.top_n;
+        float* const out_v = a.top_logprob + r * a.top_n;
+        for (int q = tid; q < n_cand; q += V_THREADS) {
+          const unsigned long long k = cand[q];
+          if (SPLIT && k == 0) continue;
+          int rank = 0;
+          for (int j = 0; j < n_cand; ++j) rank += cand[j] > k;
+          if (rank < a.top_n) {
+            const int i = (int)~(uint32_t)k;
+            out_i[rank] = i;
+            out_v[rank] = sm.logprob(to_f32<T>(row.p[i]));
+          }
+        }
+        if (SPLIT && usable) {                           // how many there are in all
+          int have = 0;
+          for (int q = tid; q < n_cand; q += V_THREADS) have += cand[q] != 0;
+          n_out = have;
+#pragma unroll
+          for (int o = 16; o; o >>= 1) n_out += __shfl_xor_sync(0xffffffffu, n_out, o);
+          if ((tid & 31) == 0) sc.hist[tid >> 5] = n_out;
+          __syncthreads();
+          n_out = 0;
+          for (int w = 0; w < V_WARPS; ++w) n_out += sc.hist[w];
+        }
+        for (int q = n_out + tid; q < a.top_n; q += V_THREADS) {
+          out_i[q] = -1;
+          out_v[q] = st.s == 0.f || usable ? -INFINITY : NAN;
+        }
+      }
     }
   }
-  for (int q = n_cand + threadIdx.x; q < a.top_n; q += V_THREADS) {
-    out_i[q] = -1;
-    out_v[q] = st.s == 0.f || usable ? -INFINITY : NAN;
-  }
+  if (SPLIT && !started) cluster_all_started();
 }
 
 // ---------------------------------------------------------------------------------------------- distillation
@@ -330,7 +749,9 @@ __global__ void __launch_bounds__(V_THREADS) k_token_logprobs(const LogprobArgs 
 struct DistillArgs {
   const void* logits;
   long long ld;
-  int vocab, k;
+  int rows, vocab, k;
+  int lg;                   // 2^lg CTAs share a row
+  int mark_bytes;           // of one set of marks: a byte per vector of a part, rounded up to whole chunks
   float c, inv_tau;
   const int* idx;
   const float* logprob;
@@ -371,9 +792,9 @@ __device__ __forceinline__ void load_teacher(const DistillArgs& a, long long r, 
   double sum = 0.0;
   if (TAIL) {
     for (int j = lane; j < a.k; j += 32) {
-      const double p = exp((double)tl.log_p[j]);
-      tl.p[j] = (float)p;
-      sum += p;
+      const float p = expf(tl.log_p[j]);
+      tl.p[j] = p;
+      sum += (double)p;                 // 1 - sum would lose the rest's digits in fp32
     }
     sum = warp_sum(sum);
     if (lane == 0) tl.rest = 1.0 - sum < 0.0 ? 0.0 : 1.0 - sum;      // keeps a NaN
@@ -381,169 +802,359 @@ __device__ __forceinline__ void load_teacher(const DistillArgs& a, long long r, 
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     if (top == -INFINITY) top = 0.f;                                  // nothing on the list
-    for (int j = lane; j < a.k; j += 32) sum += exp((double)(tl.log_p[j] - top));
+    for (int j = lane; j < a.k; j += 32) sum += (double)expf(tl.log_p[j] - top);
     sum = warp_sum(sum);
-    const double log_sum = log(sum);
+    const float log_sum = logf((float)sum);
     for (int j = lane; j < a.k; j += 32) {
-      const double lp = (double)(tl.log_p[j] - top) - log_sum;
-      tl.p[j] = sum > 0.0 || sum != sum ? (float)exp(lp) : 0.f;
-      tl.log_p[j] = (float)lp;
+      const float lp = tl.log_p[j] - top - log_sum;
+      tl.p[j] = sum > 0.0 || sum != sum ? expf(lp) : 0.f;
+      tl.log_p[j] = lp;
     }
     if (lane == 0) tl.rest = 0.0;
   }
 }
 
-// Writes scale * 2^((x - m) c - off) for every element of the row.
-template <typename T>
-__device__ __forceinline__ void write_row(const Row<T>& row, T* out, float m, float c, float off, float scale) {
-  constexpr int N = Row<T>::N;
-  auto grad = [&](float x) { return scale * ex2((x - m) * c - off); };
-  auto put = [&](int i, float v) {
-    if constexpr (sizeof(T) == 2) out[i] = __float2bfloat16_rn(v); else out[i] = v;
-  };
-  if ((int)threadIdx.x < row.head) put(threadIdx.x, grad(to_f32<T>(row.p[threadIdx.x])));
-  if ((int)threadIdx.x < row.tail) {
-    const int i = row.tail_index(threadIdx.x);
-    put(i, grad(to_f32<T>(row.p[i])));
-  }
-  const bool vec_out = (reinterpret_cast<uintptr_t>(out + row.head) & 15) == 0;
-  for (int v0 = threadIdx.x; v0 < row.n_vec; v0 += V_UNROLL * V_THREADS) {
-    uint4 raw[V_UNROLL];
-#pragma unroll
-    for (int u = 0; u < V_UNROLL; ++u) {
-      const int v = v0 + u * V_THREADS;
-      if (v < row.n_vec) raw[u] = ld_stream(row.vec(v));
-    }
-#pragma unroll
-    for (int u = 0; u < V_UNROLL; ++u) {
-      const int v = v0 + u * V_THREADS;
-      if (v >= row.n_vec) break;
-      float x[N];
-      unpack<T>(raw[u], x);
-#pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = grad(x[i]);
-      const int i0 = row.vec_index(v);
-      if (vec_out) {
-        uint4 o;
-        if constexpr (sizeof(T) == 2) {
-          __nv_bfloat162 h[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-          o = *reinterpret_cast<const uint4*>(h);
-        } else {
-          o = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-        }
-        *reinterpret_cast<uint4*>(out + i0) = o;
-      } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) put(i0 + i, x[i]);
-      }
-    }
+// Sets or clears the marks of the listed tokens among the part's vectors (one warp).
+template <typename T, bool SET>
+__device__ __forceinline__ void mark_list(const Row<T>& row, const TeacherList& tl, int k, uint8_t* mark) {
+  for (int j = threadIdx.x & 31; j < k; j += 32) {
+    const int i = tl.idx[j];
+    if (i < row.first || i >= row.tail_at) continue;
+    const int v = (i - row.first) / Row<T>::N, at = v - row.v_begin;
+    if (v < row.v_begin || v >= row.v_end) continue;
+    uint32_t* const word = reinterpret_cast<uint32_t*>(mark) + (at >> 2);
+    if (SET) atomicOr(word, 1u << (8 * (at & 3) + (i - row.first) % Row<T>::N)); else *word = 0u;
   }
 }
+template <typename T>
+__device__ __forceinline__ void store_vec(T* o, const float2* x, bool aligned) {
+  constexpr int N = Elem<T>::N;
+  if (aligned) {
+    uint4 w;
+    if constexpr (sizeof(T) == 2) {
+      __nv_bfloat162 h[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[i] = __float22bfloat162_rn(x[i]);
+      w = *reinterpret_cast<const uint4*>(h);
+    } else {
+      w = make_uint4(__float_as_uint(x[0].x), __float_as_uint(x[0].y), __float_as_uint(x[1].x), __float_as_uint(x[1].y));
+    }
+    __stcs(reinterpret_cast<uint4*>(o), w);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) { o[2 * i] = Elem<T>::put(x[i].x); o[2 * i + 1] = Elem<T>::put(x[i].y); }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void zero_row(const Row<T>& row, T* out) {
+  const int tid = threadIdx.x;
+  const bool aligned = (reinterpret_cast<uintptr_t>(out + row.first) & 15) == 0;
+  const float2 zero[Elem<T>::N / 2] = {};
+  if (tid < row.head) out[tid] = Elem<T>::put(0.f);
+  if (tid < row.tail) out[row.tail_at + tid] = Elem<T>::put(0.f);
+  for (int v = row.v_begin + tid; v < row.v_end; v += V_THREADS) store_vec<T>(out + row.vec_index(v), zero, aligned);
+}
 
-template <typename T, int MODE, bool TAIL>
-__global__ void __launch_bounds__(V_THREADS) k_distill(const DistillArgs a) {
+enum { FROM_RING = 0, FROM_FEED = 1, FROM_MEMORY = 2 };
+
+// Writes scale * q_v (or 0: blank) for every element of the part.  FROM_RING: its vectors lie in the ring from slot
+// `slot` on; FROM_FEED: they arrive there; either way they make room one chunk after the other.
+template <typename T, typename RG, int FROM>
+__device__ __forceinline__ void write_row(const Row<T>& row, T* out, const Softmax& sm, float scale, bool blank, Feed<T, RG>& feed,
+                                          const uint8_t* ring, int& ring_at) {
+  constexpr int N = Elem<T>::N;
+  const int tid = threadIdx.x, n_vec = row.v_end - row.v_begin, chunks = row_chunks<RG>(n_vec);
+  float single[2] = {0.f, 0.f};
+  if (tid < row.head) single[0] = to_f32<T>(row.p[tid]);
+  if (tid < row.tail) single[1] = to_f32<T>(row.p[row.tail_at + tid]);
+  const bool aligned = (reinterpret_cast<uintptr_t>(out + row.first) & 15) == 0;
+  const float2 c2 = make_float2(sm.c, sm.c), k2 = make_float2(-sm.k, -sm.k), s2 = make_float2(scale, scale);
+  const uint8_t* const mine = ring + tid * 16;
+  T* o = out + row.vec_index(row.v_begin + tid);
+  const bool plain = !blank && !sm.careful;
+  for (int ch = 0, left = n_vec - tid; ch < chunks; ++ch, left -= RG::CHUNK) {
+    if (FROM == FROM_FEED) Feed<T, RG>::wait();
+    uint4 raw[RG::PER];
+#pragma unroll
+    for (int u = 0; u < RG::PER; ++u) {
+      if (FROM == FROM_MEMORY) {
+        if (left > u * V_THREADS) raw[u] = ld_stream(row.vec(row.v_begin + ch * RG::CHUNK + u * V_THREADS + tid));
+      } else {
+        raw[u] = *reinterpret_cast<const uint4*>(mine + ring_at + u * V_THREADS * 16);
+      }
+    }
+    if (FROM != FROM_MEMORY) ring_at = next_chunk<RG>(ring_at);
+#pragma unroll
+    for (int u = 0; u < RG::PER; ++u) {
+      if (left <= u * V_THREADS) continue;
+      float2 x[N / 2];
+      Elem<T>::pairs(raw[u], x);
+      if (plain) {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+          const float2 d = fma2(x[i], c2, k2);
+          x[i] = mul2(make_float2(ex2(d.x), ex2(d.y)), s2);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i)
+          x[i] = blank ? make_float2(0.f, 0.f) : make_float2(scale * sm.q(x[i].x), scale * sm.q(x[i].y));
+      }
+      store_vec<T>(o + (size_t)u * V_THREADS * N, x, aligned);
+    }
+    o += (size_t)RG::CHUNK * N;
+    if (FROM != FROM_MEMORY) feed.issue();
+  }
+  if (tid < row.head) out[tid] = Elem<T>::put(blank ? 0.f : scale * sm.q(single[0]));
+  if (tid < row.tail) out[row.tail_at + tid] = Elem<T>::put(blank ? 0.f : scale * sm.q(single[1]));
+}
+
+// A CTA, or (SPLIT) the CTAs of a cluster together, take row after row, like k_token_logprobs.  HOLD (STEP, and the part
+// fits): the part stays in the ring between the pass that sums and the pass that writes the gradient, so a logit is read
+// from memory once.  The last warp looks after the teacher's lists: while the others sum a row it brings in the next
+// row's, and while they write the gradient it forms the loss.
+constexpr int VD_THREADS = V_THREADS + 32;
+constexpr int VD_LISTS = 3;
+
+template <typename T, int MODE, bool TAIL, bool SPLIT, bool HOLD>
+__global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) {
   constexpr bool STATS = MODE != DISTILL_BACKWARD;
   constexpr bool GRAD = MODE != DISTILL_FORWARD;
   constexpr bool REST = STATS && TAIL;
-  extern __shared__ uint32_t listed[];               // REST: a bit per token, set on the list
-  __shared__ Stats part[V_WARPS];
-  __shared__ TeacherList tl;
-  const long long r = blockIdx.x;
-  const Row<T> row(static_cast<const T*>(a.logits) + r * a.ld, a.vocab);
-  T* const out = GRAD ? static_cast<T*>(a.grad) + r * a.ld_grad : nullptr;
+  using RG = RingHold;
+  extern __shared__ __align__(16) uint8_t ring[];     // the ring, then (REST) two sets of marks
+  __shared__ JoinScratch js;
+  __shared__ TeacherList lists[VD_LISTS];
+  const int lg = SPLIT ? a.lg : 0, part = SPLIT ? blockIdx.x : 0, parts = 1 << lg;
   const int tid = threadIdx.x;
-  const float w = GRAD ? a.d_loss[r] * a.inv_tau : 0.f;
-  if (GRAD && a.d_loss[r] == 0.f) {                   // a row that does not count: its logits are not looked at
-    for (int i = tid; i < a.vocab; i += V_THREADS) {
-      if constexpr (sizeof(T) == 2) out[i] = __float2bfloat16_rn(0.f); else out[i] = 0.f;
-    }
-    if (STATS && tid == 0) a.loss[r] = 0.f;
-    return;
-  }
+  const bool lister = tid >= V_THREADS;
+  const T* const logits = static_cast<const T*>(a.logits);
+  uint8_t* const marks = ring + RG::BYTES;
+  if (SPLIT) cluster_started();
+  bool started = !SPLIT;
   if (REST)
-    for (int i = tid; i < (a.vocab >> 5) + 2; i += V_THREADS) listed[i] = 0u;
-  if (tid < 32) load_teacher<TAIL>(a, r, tl);
+    for (int i = tid; i < a.mark_bytes / 2; i += VD_THREADS) reinterpret_cast<uint32_t*>(marks)[i] = 0u;
+  Feed<T, RG> feed;
+  feed.logits = logits;
+  feed.ld = a.ld; feed.weight = GRAD ? a.d_loss : nullptr;
+  feed.rows = a.rows; feed.stride = gridDim.y; feed.vocab = a.vocab; feed.part = part; feed.lg = lg;
+  feed.dst0 = smem_u32(ring) + tid * 16;
+  feed.begin(lister ? a.rows : (int)blockIdx.y);
+#pragma unroll
+  for (int i = 0; i < RG::SLOTS; ++i) feed.issue();
+  if (GRAD && !lister) {                              // rows that do not count: their logits are not looked at
+    for (int r = blockIdx.y; r < a.rows; r += gridDim.y) {
+      if (a.d_loss[r] != 0.f) continue;
+      zero_row<T>(Row<T>(logits + r * a.ld, a.vocab, part, lg), static_cast<T*>(a.grad) + r * a.ld_grad);
+      if (STATS && part == 0 && tid == 0) a.loss[r] = 0.f;
+    }
+  }
+  auto bring_list = [&](int r, TeacherList& tl, uint8_t* mark) {      // one warp
+    if (r >= a.rows) return;
+    const Row<T> row(logits + r * a.ld, a.vocab, part, lg);
+    load_teacher<TAIL>(a, r, tl);
+    __syncwarp();
+    for (int j = tid & 31; j < a.k; j += 32) {
+      const int i = tl.idx[j];
+      tl.x[j] = i >= 0 ? to_f32<T>(row.p[i]) : 0.f;
+    }
+    if (REST) mark_list<T, true>(row, tl, a.k, mark);
+  };
+  RowWalk walk;
+  walk.begin(feed.weight, a.rows, blockIdx.y);
+  int r = walk.next(feed.weight, a.rows, gridDim.y);
   __syncthreads();
-  const int li = tid < a.k ? tl.idx[tid] : -1;
-  if (REST) {
-    if (li >= 0) atomicOr(&listed[li >> 5], 1u << (li & 31));
+  if (lister) bring_list(r, lists[0], marks);
+  if (!STATS && SPLIT) {
+    // in place: nobody writes to the first row before every CTA has its listed logits
+    cluster_all_started();
+    started = true;
+    cluster_sync_all();
+  } else {
     __syncthreads();
   }
-  if (tid < a.k) tl.x[tid] = li >= 0 ? to_f32<T>(row.p[li]) : 0.f;     // read before the gradient may overwrite it
-  float m, off, coef = 1.f;
-  bool empty;
-  if (STATS) {
-    Stats st = join<false, REST>(walk_row<T, false, REST>(row, a.c, listed), a.c, part);
-    // no distribution: every logit minus infinity, or all of them beyond fp32's range once scaled
-    empty = st.s == 0.f || st.m * a.c < -FLT_MAX;
-    m = st.m;
-    off = log2f(st.s);
-    if (REST && tl.rest != 0.0) coef = st.r > 0.f || st.r != st.r ? (float)(1.0 - tl.rest * ((double)st.s / (double)st.r)) : 0.f;
-    if (tid < 32) {
-      double loss = 0.0;
-      for (int j = tid; j < a.k; j += 32) {
-        const float p = tl.p[j];
-        if (tl.idx[j] < 0 || p == 0.f) continue;
-        loss += (double)p * ((double)tl.log_p[j] - (double)((tl.x[j] - m) * a.c - off) * 0.6931471805599453);
+  int at = 0, turn = 0, join_turn = 0, list = 0;
+  while (r < a.rows) {
+    const int r_next = walk.next(feed.weight, a.rows, gridDim.y);
+    const Row<T> row(logits + r * a.ld, a.vocab, part, lg);
+    const TeacherList& tl = lists[list];
+    const int list_next = list + 1 == VD_LISTS ? 0 : list + 1;
+    uint8_t* const mark = marks + turn * a.mark_bytes;
+    int at0 = at;
+    Sums st{-INFINITY, 0.f, 0.f, 0.f};
+    bool careful = false, empty;
+    float coef = 1.f;
+    if (lister) bring_list(r_next, lists[list_next], marks + (turn ^ 1) * a.mark_bytes);
+    if (STATS) {
+      if (!lister) st = walk_row<T, RG, false, REST, false, HOLD>(row, a.c, feed, ring, at, mark, tl.idx, a.k, nullptr);
+      st = join_cta<false, false, REST>(st, a.c, join_turn, js);
+      if (SPLIT) {
+        if (!started) { cluster_all_started(); started = true; }
+        publish_sums(st, part, parts, turn, js);
+        cluster_sync_all();
+        st = join_split<false, false, REST>(parts, a.c, turn, js);
       }
-      loss = warp_sum(loss);
-      if (tid == 0) {
-        if (REST && tl.rest != 0.0 && (st.r > 0.f || st.r != st.r))
-          loss += tl.rest * (log(tl.rest) - (double)(log2f(st.r) - off) * 0.6931471805599453);
-        a.loss[r] = empty ? 0.f : (float)loss;
-        if (MODE == DISTILL_FORWARD) {
-          if (a.lse) a.lse[r] = empty ? -INFINITY : (m * a.c + off) * LN2;
-          if (TAIL && a.log_tail) a.log_tail[r] = empty || st.r == 0.f ? -INFINITY : (m * a.c + log2f(st.r)) * LN2;
+      careful = !sums_ordinary(st);
+      if (careful) {
+        if (!lister) st = walk_careful<T, false, REST>(row, a.c, tl.idx, a.k);
+        st = join_cta<true, false, REST>(st, a.c, join_turn, js);
+        if (SPLIT) {
+          cluster_sync_all();                         // every CTA has read the first round's sums
+          publish_sums(st, part, parts, turn, js);
+          cluster_sync_all();
+          st = join_split<true, false, REST>(parts, a.c, turn, js);
         }
       }
     }
-  } else {
-    __syncthreads();                                 // the listed logits are read before any of them is overwritten
-    const float lse = a.lse[r];
-    empty = lse == -INFINITY;
-    m = 0.f;
-    off = lse * 1.44269504088896341f;
-    if (TAIL && tl.rest != 0.0) {
-      const float lt = a.log_tail[r];
-      coef = lt == -INFINITY ? 0.f : (float)(1.0 - tl.rest * exp((double)lse - (double)lt));
+    Softmax sm(st, careful, a.c, a.inv_tau);
+    if (STATS) {
+      // no distribution: every logit minus infinity, or all of them beyond fp32's range once scaled
+      empty = st.s == 0.f || (careful && st.ref * a.c < -FLT_MAX);
+      if (REST && tl.rest != 0.0) coef = st.r > 0.f || st.r != st.r ? 1.f - (float)tl.rest * (st.s / st.r) : 0.f;
+      if (lister) {
+        if (REST) mark_list<T, false>(row, tl, a.k, mark);
+        if (part == 0) {
+          double loss = 0.0;
+          for (int j = tid & 31; j < a.k; j += 32) {
+            const float p = tl.p[j], x = tl.x[j];
+            if (tl.idx[j] < 0 || p == 0.f) continue;
+            const float d = careful ? (x - sm.m) * a.inv_tau * LOG2E : fmaf(x, a.c, -sm.m);
+            loss += (double)p * ((double)tl.log_p[j] - ((double)d - (double)sm.log2s) * 0.6931471805599453);
+          }
+          loss = warp_sum(loss);
+          if (tid == V_THREADS) {
+            if (REST && tl.rest != 0.0 && (st.r > 0.f || st.r != st.r))
+              loss += tl.rest * (log(tl.rest) - log((double)st.r / (double)st.s));
+            a.loss[r] = empty ? 0.f : (float)loss;
+            if (MODE == DISTILL_FORWARD) {
+              const float ref = careful ? sm.m * a.inv_tau : sm.m * LN2;
+              if (a.lse) a.lse[r] = empty ? -INFINITY : ref + sm.log2s * LN2;
+              if (TAIL && a.log_tail) a.log_tail[r] = empty || st.r == 0.f ? -INFINITY : ref + log2f(st.r) * LN2;
+            }
+          }
+        }
+      }
+    } else {
+      const float lse = a.lse[r];
+      empty = lse == -INFINITY;
+      sm.k = lse * LOG2E;
+      if (TAIL && tl.rest != 0.0) {
+        const float lt = a.log_tail[r];
+        coef = lt == -INFINITY ? 0.f : 1.f - (float)tl.rest * expf(lse - lt);
+      }
     }
-  }
-  if (!GRAD) return;
-  if (empty) {
-    for (int i = tid; i < a.vocab; i += V_THREADS) {
-      if constexpr (sizeof(T) == 2) out[i] = __float2bfloat16_rn(0.f); else out[i] = 0.f;
+    if (GRAD) {
+      // In place: the barriers so far have seen every CTA of the row read its listed logits.
+      T* const out = static_cast<T*>(a.grad) + r * a.ld_grad;
+      const float w = a.d_loss[r] * a.inv_tau;
+      if (!lister) {
+        if (!STATS) write_row<T, RG, FROM_FEED>(row, out, sm, w * coef, empty, feed, ring, at);
+        else write_row<T, RG, HOLD ? FROM_RING : FROM_MEMORY>(row, out, sm, w * coef, empty, feed, ring, at0);
+      }
+      if (!STATS && SPLIT) cluster_sync_all(); else __syncthreads();
+      if (tid < a.k && !empty) {
+        const int i = tl.idx[tid];
+        if (i >= 0 && row.holds(i)) out[i] = Elem<T>::put(w * (sm.q(tl.x[tid]) - tl.p[tid]));
+      }
     }
-    return;
+    r = r_next;
+    turn ^= 1;
+    list = list_next;
   }
-  write_row<T>(row, out, m, a.c, off, w * coef);
-  __syncthreads();
-  if (li >= 0) {
-    const float g = w * (ex2((tl.x[tid] - m) * a.c - off) - tl.p[tid]);
-    if constexpr (sizeof(T) == 2) out[li] = __float2bfloat16_rn(g); else out[li] = g;
-  }
+  if (SPLIT && !started) cluster_all_started();
 }
 
+// ------------------------------------------------------------------------------------------------ launches
+int sm_count() {
+  int dev = 0, sms = 148;
+  cudaGetDevice(&dev);
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  return sms;
+}
+// CTAs that share a row when there are few: as many as keep the grid within two CTAs an SM and two vectors a thread.
+int split_for(int rows, int n_vec, int sms) {
+  int lg = 0;
+  while (1 << lg < V_MAX_SPLIT && (long long)rows << (lg + 1) <= 2ll * sms && n_vec >> lg >= 4 * V_THREADS) ++lg;
+  return lg;
+}
+
+// Clusters of 2^lg CTAs that run at one time (a cluster needs SMs of one GPC, so they do not always fill the GPU), asked
+// for once per kernel and size.
+template <typename K>
+int clusters_at_once(K kern, cudaLaunchConfig_t& cfg, int lg, std::atomic<int>* known) {
+  int n = known[lg].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) { cudaGetLastError(); n = 1; }
+    known[lg].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+template <auto KERN, typename A>
+cudaError_t launch_rows(const A& args, int threads, int smem, int sms, cudaStream_t st) {
+  static std::atomic<int> known[8];
+  const auto kern = KERN;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  const int split = 1 << args.lg;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)split, (unsigned)args.rows);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)split; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = split > 1 ? 1 : 0;
+  // two CTAs fit an SM (one where long rows need more marks); each walks rows until none is left
+  int clusters = 2 * sms / split;
+  if (split > 1 && args.rows > clusters / 2) clusters = clusters_at_once(kern, cfg, args.lg, known);
+  if (args.rows > clusters) cfg.gridDim.y = (unsigned)clusters;
+  return cudaLaunchKernelEx(&cfg, kern, args);
+}
+
+template <typename T, bool ENT, bool TOP>
+cudaError_t launch_logprobs(LogprobArgs& a, cudaStream_t st) {
+  const int sms = sm_count();
+  a.lg = split_for(a.rows, a.vocab / Elem<T>::N, sms);
+  return a.lg == 0 ? launch_rows<k_token_logprobs<T, ENT, TOP, false>>(a, V_THREADS, RingStream::BYTES, sms, st)
+                   : launch_rows<k_token_logprobs<T, ENT, TOP, true>>(a, V_THREADS, RingStream::BYTES, sms, st);
+}
+template <typename T>
+cudaError_t launch_logprobs(LogprobArgs& a, cudaStream_t st) {
+  if (a.entropy) return a.top_n ? launch_logprobs<T, true, true>(a, st) : launch_logprobs<T, true, false>(a, st);
+  return a.top_n ? launch_logprobs<T, false, true>(a, st) : launch_logprobs<T, false, false>(a, st);
+}
+
+template <typename T, int MODE, bool TAIL>
+cudaError_t launch_distill(DistillArgs& a, cudaStream_t st) {
+  constexpr bool REST = TAIL && MODE != DISTILL_BACKWARD, STEP = MODE == DISTILL_STEP;
+  const int sms = sm_count(), n_vec = a.vocab / Elem<T>::N;
+  a.lg = split_for(a.rows, n_vec, sms);
+  // STEP: so many CTAs that a row's parts fit their rings; a row too long for eight is read twice
+  if (STEP)
+    while (1 << a.lg < V_MAX_SPLIT && (n_vec >> a.lg) + 1 > RingHold::HELD) ++a.lg;
+  const bool hold = STEP && (n_vec >> a.lg) + 1 <= RingHold::HELD;
+  a.mark_bytes = REST ? ((n_vec >> a.lg) + RingHold::CHUNK) / RingHold::CHUNK * RingHold::CHUNK : 0;
+  const int smem = RingHold::BYTES + 2 * a.mark_bytes;
+  if (a.lg == 0)
+    return hold ? launch_rows<k_distill<T, MODE, TAIL, false, STEP>>(a, VD_THREADS, smem, sms, st)
+                : launch_rows<k_distill<T, MODE, TAIL, false, false>>(a, VD_THREADS, smem, sms, st);
+  return hold ? launch_rows<k_distill<T, MODE, TAIL, true, STEP>>(a, VD_THREADS, smem, sms, st)
+              : launch_rows<k_distill<T, MODE, TAIL, true, false>>(a, VD_THREADS, smem, sms, st);
+}
 template <int MODE>
-cudaError_t launch_distill(const DistillArgs& a, int dtype, bool tail, long long rows, cudaStream_t st) {
-  const size_t smem = tail && MODE != DISTILL_BACKWARD ? ((size_t)(a.vocab >> 5) + 2) * 4 : 0;
-  auto go = [&](auto kern) {
-    if (smem > 32 * 1024) {
-      const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-      if (e != cudaSuccess) return e;
-    }
-    kern<<<(unsigned)rows, V_THREADS, smem, st>>>(a);
-    return cudaGetLastError();
-  };
-  if (dtype == CAMERA_BF16) return tail ? go(k_distill<__nv_bfloat16, MODE, true>) : go(k_distill<__nv_bfloat16, MODE, false>);
-  return tail ? go(k_distill<float, MODE, true>) : go(k_distill<float, MODE, false>);
+cudaError_t launch_distill(DistillArgs& a, int dtype, bool tail, cudaStream_t st) {
+  if (dtype == CAMERA_BF16)
+    return tail ? launch_distill<__nv_bfloat16, MODE, true>(a, st) : launch_distill<__nv_bfloat16, MODE, false>(a, st);
+  return tail ? launch_distill<float, MODE, true>(a, st) : launch_distill<float, MODE, false>(a, st);
 }
 
 int check_logits(const void* logits, int dtype, int64_t ld, int64_t n_rows, int32_t vocab, float temperature) {
   if (dtype != CAMERA_F32 && dtype != CAMERA_BF16) return CAMERA_ERR_INVALID_ARG;
   if (n_rows < 0 || vocab < 1 || ld < vocab || !(temperature > 0.f) || isinf(temperature)) return CAMERA_ERR_INVALID_ARG;
-  if (vocab > CAMERA_MAX_VOCAB || n_rows > 0x7fffffff) return CAMERA_ERR_UNSUPPORTED_SHAPE;
+  if (vocab > CAMERA_MAX_VOCAB || n_rows > 0x3fffffff) return CAMERA_ERR_UNSUPPORTED_SHAPE;
   if (n_rows > 0 && (logits == nullptr || (reinterpret_cast<uintptr_t>(logits) & (dtype == CAMERA_BF16 ? 1 : 3))))
     return CAMERA_ERR_INVALID_ARG;
   return CAMERA_OK;
@@ -567,7 +1178,7 @@ bool grad_ok(const camera_distill_t* d, const void* grad, int64_t ld) {
 
 DistillArgs distill_args(const camera_distill_t* d) {
   DistillArgs a;
-  a.logits = d->logits; a.ld = d->ld; a.vocab = d->vocab; a.k = d->k;
+  a.logits = d->logits; a.ld = d->ld; a.rows = (int)d->n_rows; a.lg = 0; a.mark_bytes = 0; a.vocab = d->vocab; a.k = d->k;
   a.c = 1.44269504088896341f / d->temperature; a.inv_tau = 1.f / d->temperature;
   a.idx = d->teacher_idx; a.logprob = d->teacher_logprob;
   a.d_loss = nullptr; a.loss = a.lse = a.log_tail = nullptr; a.grad = nullptr; a.ld_grad = 0;
@@ -587,18 +1198,11 @@ extern "C" int camera_token_logprobs(const void* logits, int32_t dtype, int64_t 
   if (top_n > CAMERA_MAX_TOP) return CAMERA_ERR_UNSUPPORTED_SHAPE;
   if (n_rows == 0) return CAMERA_OK;
   if (top_n > 0 && (top_idx == nullptr || top_logprob == nullptr)) return CAMERA_ERR_INVALID_ARG;
-  LogprobArgs a{logits, ld, vocab, top_n, 1.44269504088896341f / temperature, 1.f / temperature, reinterpret_cast<const long long*>(targets),
+  LogprobArgs a{logits, ld, (int)n_rows, vocab, top_n, 0, 1.44269504088896341f / temperature, 1.f / temperature, reinterpret_cast<const long long*>(targets),
                 logprob, entropy, top_logprob, top_idx};
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const unsigned grid = (unsigned)n_rows;
-  if (dtype == CAMERA_BF16) {
-    if (entropy) k_token_logprobs<__nv_bfloat16, true><<<grid, V_THREADS, 0, st>>>(a);
-    else k_token_logprobs<__nv_bfloat16, false><<<grid, V_THREADS, 0, st>>>(a);
-  } else {
-    if (entropy) k_token_logprobs<float, true><<<grid, V_THREADS, 0, st>>>(a);
-    else k_token_logprobs<float, false><<<grid, V_THREADS, 0, st>>>(a);
-  }
-  return cudaGetLastError() == cudaSuccess ? CAMERA_OK : CAMERA_ERR_CUDA;
+  const cudaError_t e = dtype == CAMERA_BF16 ? launch_logprobs<__nv_bfloat16>(a, st) : launch_logprobs<float>(a, st);
+  return e == cudaSuccess ? CAMERA_OK : CAMERA_ERR_CUDA;
 }
 
 extern "C" int camera_distill_forward(const camera_distill_t* d, float* loss, float* lse, float* log_tail, void* cuda_stream) {
@@ -609,7 +1213,7 @@ extern "C" int camera_distill_forward(const camera_distill_t* d, float* loss, fl
   if (loss == nullptr) return CAMERA_ERR_INVALID_ARG;
   DistillArgs a = distill_args(d);
   a.loss = loss; a.lse = lse; a.log_tail = log_tail;
-  return launch_distill<DISTILL_FORWARD>(a, d->dtype, d->flags & CAMERA_DISTILL_TAIL, d->n_rows,
+  return launch_distill<DISTILL_FORWARD>(a, d->dtype, d->flags & CAMERA_DISTILL_TAIL,
                                          static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CAMERA_OK : CAMERA_ERR_CUDA;
 }
 
@@ -625,7 +1229,7 @@ extern "C" int camera_distill_backward(const camera_distill_t* d, const float* d
   DistillArgs a = distill_args(d);
   a.d_loss = d_loss; a.lse = const_cast<float*>(lse); a.log_tail = const_cast<float*>(log_tail);
   a.grad = d_logits; a.ld_grad = d_ld;
-  return launch_distill<DISTILL_BACKWARD>(a, d->dtype, d->flags & CAMERA_DISTILL_TAIL, d->n_rows,
+  return launch_distill<DISTILL_BACKWARD>(a, d->dtype, d->flags & CAMERA_DISTILL_TAIL,
                                           static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CAMERA_OK : CAMERA_ERR_CUDA;
 }
 
@@ -638,6 +1242,6 @@ extern "C" int camera_distill_step(const camera_distill_t* d, const float* d_los
   if (d_loss == nullptr || loss == nullptr || !grad_ok(d, d_logits, d_ld)) return CAMERA_ERR_INVALID_ARG;
   DistillArgs a = distill_args(d);
   a.d_loss = d_loss; a.loss = loss; a.grad = d_logits; a.ld_grad = d_ld;
-  return launch_distill<DISTILL_STEP>(a, d->dtype, d->flags & CAMERA_DISTILL_TAIL, d->n_rows,
+  return launch_distill<DISTILL_STEP>(a, d->dtype, d->flags & CAMERA_DISTILL_TAIL,
                                       static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CAMERA_OK : CAMERA_ERR_CUDA;
 }

@@ -16,7 +16,14 @@ from .binding import CAMERA_BF16, CAMERA_F32, CameraError, _check, alloc_workspa
 
 CAMERA_DISTILL_TAIL = 1
 CAMERA_MAX_TOP = 128
+_F32 = torch.float32
 _DTYPE = {torch.bfloat16: CAMERA_BF16, torch.float32: CAMERA_F32}
+
+
+# The current stream's handle; the same as torch.cuda.current_stream(device).cuda_stream without building a Stream
+# object, which takes longer than a small kernel.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def _on_stream(fn):
@@ -30,23 +37,21 @@ def _on_stream(fn):
     return wrapper
 
 
-def _stream() -> Optional[int]:
-    return torch.cuda.current_stream().cuda_stream or None
-
-
 def _rows(t: torch.Tensor, name: str) -> int:
     """Distance of the rows of a [n_rows, vocab] tensor in elements."""
     if not (t.is_cuda and t.dim() == 2 and t.dtype in _DTYPE):
         raise ValueError(f"{name} must be a bf16 or fp32 [n_rows, vocab] tensor on the GPU")
     rows, vocab = t.shape
-    ld = t.stride(0) if rows > 1 else max(t.stride(0), vocab)
-    if (vocab > 1 and t.stride(1) != 1) or ld < vocab:
+    ld, one = t.stride()
+    if rows <= 1 and ld < vocab:
+        ld = vocab
+    if (one != 1 and vocab > 1) or ld < vocab:
         raise ValueError(f"{name} must have contiguous, non-overlapping rows")
     return ld
 
 
 def _vector(t: torch.Tensor, like: torch.Tensor, dtype, shape, name: str) -> int:
-    if not (t.is_contiguous() and t.dtype == dtype and t.device == like.device and tuple(t.shape) == shape):
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.device != like.device:
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on the device of the logits")
     return t.data_ptr()
 
@@ -108,7 +113,7 @@ def camera_ffn_forward(ffn: Ffn, x: torch.Tensor, *, y: Optional[torch.Tensor] =
     if saved is not None and saved.numel() * saved.element_size() < camera_ffn_saved_bytes(ffn, n):
         raise ValueError("saved is smaller than camera_ffn_saved_bytes")
     _check(lib.camera_ffn_forward(ffn._ref, xp, n, y.data_ptr(), None if saved is None else saved.data_ptr(),
-                                  workspace.data_ptr(), workspace.numel(), _stream()), "camera_ffn_forward")
+                                  workspace.data_ptr(), workspace.numel(), _raw_stream(x.get_device())), "camera_ffn_forward")
     return y
 
 
@@ -140,8 +145,8 @@ def camera_ffn_backward(ffn: Ffn, x: torch.Tensor, dy: torch.Tensor, saved: torc
         workspace = alloc_workspace(camera_ffn_workspace_bytes(ffn, n, backward=True), ffn.device)
     ptr = {name: t.data_ptr() for name, t in res.items()}
     _check(lib.camera_ffn_backward(ffn._ref, xp, dyp, n, saved.data_ptr(), ptr.get("x"), ptr.get("w_gate"), ptr.get("w_up"),
-                                   ptr.get("w_down"), workspace.data_ptr(), workspace.numel(), _stream()),
-           "camera_ffn_backward")
+                                   ptr.get("w_down"), workspace.data_ptr(), workspace.numel(),
+                                   _raw_stream(x.get_device())), "camera_ffn_backward")
     return res
 
 
@@ -158,10 +163,10 @@ def camera_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] 
     t_ptr = lp_ptr = h_ptr = i_ptr = v_ptr = None
     if targets is not None:
         t_ptr = _vector(targets, logits, torch.int64, (rows,), "targets")
-        out["logprob"] = t = torch.empty(rows, dtype=torch.float32, device=dev)
+        out["logprob"] = t = torch.empty(rows, dtype=_F32, device=dev)
         lp_ptr = t.data_ptr()
     if entropy:
-        out["entropy"] = t = torch.empty(rows, dtype=torch.float32, device=dev)
+        out["entropy"] = t = torch.empty(rows, dtype=_F32, device=dev)
         h_ptr = t.data_ptr()
     if top_n > 0:
         out["top_idx"] = t = torch.empty((rows, top_n), dtype=torch.int32, device=dev)
@@ -169,7 +174,7 @@ def camera_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] 
         out["top_logprob"] = t = torch.empty((rows, top_n), dtype=torch.float32, device=dev)
         v_ptr = t.data_ptr()
     _check(lib.camera_token_logprobs(logits.data_ptr(), _DTYPE[logits.dtype], ld, rows, vocab, t_ptr, top_n, temperature,
-                                     lp_ptr, h_ptr, i_ptr, v_ptr, _stream()), "camera_token_logprobs")
+                                     lp_ptr, h_ptr, i_ptr, v_ptr, _raw_stream(logits.get_device())), "camera_token_logprobs")
     return out
 
 
@@ -204,7 +209,7 @@ def camera_distill_forward(logits: torch.Tensor, teacher_idx: torch.Tensor, teac
     out = {name: torch.empty(d.n_rows, dtype=torch.float32, device=logits.device)
            for name in (("loss", "lse", "log_tail") if tail else ("loss", "lse"))}
     _check(lib.camera_distill_forward(C.byref(d), out["loss"].data_ptr(), out["lse"].data_ptr(),
-                                      out["log_tail"].data_ptr() if tail else None, _stream()), "camera_distill_forward")
+                                      out["log_tail"].data_ptr() if tail else None, _raw_stream(logits.get_device())), "camera_distill_forward")
     return out
 
 
@@ -223,7 +228,7 @@ def camera_distill_backward(logits: torch.Tensor, teacher_idx: torch.Tensor, tea
     _check(lib.camera_distill_backward(C.byref(d), _vector(d_loss, logits, torch.float32, rows, "d_loss"),
                                        _vector(lse, logits, torch.float32, rows, "lse"),
                                        _vector(log_tail, logits, torch.float32, rows, "log_tail") if tail else None,
-                                       d_logits.data_ptr(), d_ld, _stream()), "camera_distill_backward")
+                                       d_logits.data_ptr(), d_ld, _raw_stream(logits.get_device())), "camera_distill_backward")
     return d_logits
 
 
@@ -236,5 +241,5 @@ def camera_distill_step(logits: torch.Tensor, teacher_idx: torch.Tensor, teacher
     d_logits, d_ld = _gradient(logits, d_logits, d.ld)
     loss = torch.empty(d.n_rows, dtype=torch.float32, device=logits.device)
     _check(lib.camera_distill_step(C.byref(d), _vector(d_loss, logits, torch.float32, (d.n_rows,), "d_loss"),
-                                   loss.data_ptr(), d_logits.data_ptr(), d_ld, _stream()), "camera_distill_step")
+                                   loss.data_ptr(), d_logits.data_ptr(), d_ld, _raw_stream(logits.get_device())), "camera_distill_step")
     return loss, d_logits
