@@ -84,13 +84,12 @@ template <> struct Elem<float> {
     x[0] = make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
     x[1] = make_float2(__uint_as_float(v.z), __uint_as_float(v.w));
   }
-  // running maximum in the raw form of two words; NaN is passed over
-  __device__ __forceinline__ static uint4 max4(const uint4& a, const uint4& b) {
-    return make_uint4(__float_as_uint(fmaxf(__uint_as_float(a.x), __uint_as_float(b.x))),
-                      __float_as_uint(fmaxf(__uint_as_float(a.y), __uint_as_float(b.y))),
-                      __float_as_uint(fmaxf(__uint_as_float(a.z), __uint_as_float(b.z))),
-                      __float_as_uint(fmaxf(__uint_as_float(a.w), __uint_as_float(b.w))));
+  // maxima in the raw form; NaN is passed over
+  __device__ __forceinline__ static uint32_t max_word(uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
   }
+  __device__ __forceinline__ static uint32_t max_vec(const uint4& v) { return max_word(max_word(v.x, v.y), max_word(v.z, v.w)); }
+  __device__ __forceinline__ static float max_of(uint32_t w) { return __uint_as_float(w); }
   __device__ __forceinline__ static float put(float v) { return v; }
 };
 template <> struct Elem<__nv_bfloat16> {
@@ -101,26 +100,17 @@ template <> struct Elem<__nv_bfloat16> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
   }
-  __device__ __forceinline__ static uint32_t max2(uint32_t a, uint32_t b) {
+  __device__ __forceinline__ static uint32_t max_word(uint32_t a, uint32_t b) {      // of two pairs, each its own maximum
     uint32_t r;
     asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
   }
-  __device__ __forceinline__ static uint4 max4(const uint4& a, const uint4& b) {
-    return make_uint4(max2(a.x, b.x), max2(a.y, b.y), max2(a.z, b.z), max2(a.w, b.w));
+  __device__ __forceinline__ static uint32_t max_vec(const uint4& v) { return max_word(max_word(v.x, v.y), max_word(v.z, v.w)); }
+  __device__ __forceinline__ static float max_of(uint32_t w) {
+    return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
   }
   __device__ __forceinline__ static __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
 };
-template <typename T>
-__device__ __forceinline__ float vec_max(const uint4& v) {
-  float2 x[Elem<T>::N / 2];
-  Elem<T>::pairs(v, x);
-  float m = fmaxf(x[0].x, x[0].y);
-#pragma unroll
-  for (int i = 1; i < Elem<T>::N / 2; ++i) m = fmaxf(m, fmaxf(x[i].x, x[i].y));
-  return m;
-}
-
 // A row of `n` logits, or the part of it that CTA `part` of 2^lg walks: single elements before the first 16-byte
 // boundary (part 0), whole 16-byte vectors [v_begin, v_end), single elements after the last (last part).  Vector v belongs to
 // thread (v - v_begin) % V_THREADS, single element i of head or tail to thread i.
@@ -193,10 +183,10 @@ struct Ring {
   static constexpr int PER = PER_, SLOTS = SLOTS_;
   static constexpr int CHUNK = PER * V_THREADS;              // vectors
   static constexpr int BYTES = SLOTS * CHUNK * 16;
-  static constexpr int HELD = (SLOTS - 1) * CHUNK;           // vectors of the longest part that stays between two passes
 };
 using RingStream = Ring<8, 3>;
 using RingHold = Ring<4, 6>;
+constexpr int HELD_VECS = (RingHold::SLOTS - 1) * RingHold::CHUNK;       // longest part that stays between two passes
 static_assert(RingStream::BYTES == 96 * 1024 && RingHold::BYTES == 96 * 1024, "two CTAs per SM");
 
 // The logits' way into the CTA: every thread copies its own 16-byte vectors with cp.async into its own places of a ring
@@ -260,8 +250,8 @@ template <typename RG>
 __device__ __forceinline__ int next_chunk(int at) { return at + RG::CHUNK * 16 == RG::BYTES ? 0 : at + RG::CHUNK * 16; }
 
 // One thread's share of the row, whose chunks lie in the ring from offset `at` on (moved past the row).  mark (REST): a
-// byte per vector of the part with a bit per element on the teacher's list.  TOP: *top receives the largest logit of the
-// share (minus infinity if it has none).  HOLD: the chunks stay in the ring; else each makes room for the next copy.
+// byte per vector of the part with a bit per element on the teacher's list.  TOP: top[u] receives the largest logit of
+// its vectors u of all chunks, single elements counted to u = 0 (minus infinity if there are none).  HOLD: the chunks stay in the ring; else each makes room for the next copy.
 template <typename T, typename RG, bool ENT, bool REST, bool TOP, bool HOLD>
 __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>& feed, const uint8_t* ring, int& at,
                                          const uint8_t* mark, const int* list, int k, float* top) {
@@ -269,7 +259,9 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
   constexpr uint32_t NI = Elem<T>::NEG_INF;
   const uint4 nothing = make_uint4(NI, NI, NI, NI);          // minus infinity has no weight
   const int tid = threadIdx.x;
-  uint4 big = nothing;
+  uint32_t big[RG::PER];                                     // running maxima in the raw form
+#pragma unroll
+  for (int u = 0; u < RG::PER; ++u) big[u] = NI;
   float2 s2 = make_float2(0.f, 0.f), t2 = make_float2(0.f, 0.f);
   const float2 c2 = make_float2(c, c);
   float2 ref2 = make_float2(0.f, 0.f);
@@ -293,10 +285,13 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
     at = next_chunk<RG>(at);
     if (TOP || first) {
 #pragma unroll
-      for (int u = 0; u < RG::PER; ++u) big = Elem<T>::max4(big, raw[u]);
+      for (int u = 0; u < RG::PER; ++u) big[u] = Elem<T>::max_word(big[u], Elem<T>::max_vec(raw[u]));
     }
     if (first) {
-      const float m = fmaxf(fmaxf(vec_max<T>(big), fmaxf(single[0], single[1])) * c, -126.f);
+      float m = fmaxf(single[0], single[1]);
+#pragma unroll
+      for (int u = 0; u < RG::PER; ++u) m = fmaxf(m, Elem<T>::max_of(big[u]));
+      m = fmaxf(m * c, -126.f);
       ref2 = make_float2(-m, -m);
       first = false;
     }
@@ -348,7 +343,11 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
   }
   st.r = st.s;
   if (REST) st.s += on_list;
-  if (TOP) *top = fmaxf(vec_max<T>(big), fmaxf(single[0], single[1]));
+  if (TOP) {
+#pragma unroll
+    for (int u = 0; u < RG::PER; ++u) top[u] = Elem<T>::max_of(big[u]);
+    top[0] = fmaxf(top[0], fmaxf(single[0], single[1]));
+  }
   return st;
 }
 
@@ -379,7 +378,8 @@ __device__ __noinline__ Sums walk_careful(const Row<T> row, float c, const int* 
 // Shared memory of a CTA that joins sums.
 struct JoinScratch {
   Sums warp[2][V_WARPS];           // joins alternate, so that none overwrites what another thread still reads
-  Sums cta[2][V_MAX_SPLIT];        // of the CTAs that share the row, written by each of them; rows alternate
+  alignas(16) Sums cta[3][V_MAX_SPLIT];    // of the CTAs that share the row, written by each of them (see Exchange)
+  unsigned long long bars[2];
 };
 // The sums of WIDTH neighbouring lanes joined, in all of them.
 template <int WIDTH, bool CAREFUL, bool ENT, bool REST>
@@ -411,24 +411,76 @@ __device__ __forceinline__ Sums join_cta(Sums st, float c, int& join_turn, JoinS
 }
 // The CTAs of a cluster may write to each other's shared memory once all of them run: each says so when it starts and
 // waits for the others where it first needs them.
-__device__ __forceinline__ void cluster_started() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_all_started() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
-// Hands this CTA's sums to every CTA of the cluster; after the cluster's barrier join_split adds them up.
-__device__ __forceinline__ void publish_sums(const Sums& st, int part, int parts, int turn, JoinScratch& js) {
-  if ((int)threadIdx.x < parts) {
-    const uint32_t dst = map_to_cta(smem_u32(&js.cta[turn][part]), threadIdx.x);
-    st_cluster_u32(dst, __float_as_uint(st.ref));
-    st_cluster_u32(dst + 4, __float_as_uint(st.s));
-    st_cluster_u32(dst + 8, __float_as_uint(st.t));
-    st_cluster_u32(dst + 12, __float_as_uint(st.r));
+__device__ __forceinline__ void cluster_started() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_all_started() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// How the CTAs that share a row exchange their sums: each writes its own into every CTA with a store that counts its bytes
+// on that CTA's barrier, and waits until all have come in.  (A cluster barrier would also wait for the gradients written
+// so far.)  Rows alternate between two places: a CTA sends the sums of row i + 2 only after those of row i + 1 have come
+// in from everyone, who had read row i's by then.
+struct Exchange {
+  uint32_t bar;                      // two mbarriers
+  uint32_t phase[2];
+  int turn;
+};
+constexpr unsigned long long EXCHANGE_LIMIT_NS = 1000000000ull;
+__device__ __forceinline__ void exchange_init(Exchange& ex, unsigned long long* bars) {
+  ex.bar = smem_u32(bars);
+  ex.phase[0] = ex.phase[1] = 0;
+  ex.turn = 0;
+  if (threadIdx.x == 0) {
+    mbar_init(ex.bar, 1);
+    mbar_init(ex.bar + 8, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  __syncthreads();
 }
 template <bool CAREFUL, bool ENT, bool REST>
-__device__ __forceinline__ Sums join_split(int parts, float c, int turn, const JoinScratch& js) {
+__device__ __forceinline__ Sums join_parts(const Sums* cta, int parts, float c) {
   const int lane = threadIdx.x % V_MAX_SPLIT;
   Sums st{CAREFUL ? -FLT_MAX : -INFINITY, 0.f, 0.f, 0.f};
-  if (lane < parts) st = js.cta[turn][lane];
+  if (lane < parts) st = cta[lane];
   return join_lanes<V_MAX_SPLIT, CAREFUL, ENT, REST>(st, c);
+}
+// The row's sums from this CTA's (in every thread of it).  A wait that runs out (it cannot while the cluster's CTAs run)
+// gives NaN.
+template <bool ENT, bool REST>
+__device__ __forceinline__ Sums exchange_sums(const Sums& own, int part, int parts, float c, Exchange& ex, JoinScratch& js) {
+  const uint32_t bar = ex.bar + 8 * ex.turn;
+  if (threadIdx.x == 0) mbar_expect_tx(bar, (uint32_t)parts * sizeof(Sums));
+  __syncwarp();
+  if ((int)threadIdx.x < parts) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+                 ::"r"(map_to_cta(smem_u32(&js.cta[ex.turn][part]), threadIdx.x)), "r"(__float_as_uint(own.ref)),
+                 "r"(__float_as_uint(own.s)), "r"(__float_as_uint(own.t)), "r"(__float_as_uint(own.r)),
+                 "r"(map_to_cta(bar, threadIdx.x))
+                 : "memory");
+  }
+  bool ok = mbar_try_wait_cluster(bar, ex.phase[ex.turn]);
+  if (!ok) {
+    const unsigned long long t0 = globaltimer_ns();
+    while (!(ok = mbar_try_wait_cluster(bar, ex.phase[ex.turn])) && globaltimer_ns() - t0 < EXCHANGE_LIMIT_NS) {}
+  }
+  ok = __all_sync(0xffffffffu, ok);
+  Sums st = join_parts<false, ENT, REST>(js.cta[ex.turn], parts, c);
+  if (!ok) st.s = NAN;
+  ex.phase[ex.turn] ^= 1;
+  ex.turn ^= 1;
+  return st;
+}
+// The same for the sums of a careful walk, which are rare: with barriers of the whole cluster.
+template <bool ENT, bool REST>
+__device__ __forceinline__ Sums exchange_careful(const Sums& own, int part, int parts, float c, JoinScratch& js) {
+  if ((int)threadIdx.x < parts) {
+    const uint32_t dst = map_to_cta(smem_u32(&js.cta[2][part]), threadIdx.x);
+    st_cluster_u32(dst, __float_as_uint(own.ref));
+    st_cluster_u32(dst + 4, __float_as_uint(own.s));
+    st_cluster_u32(dst + 8, __float_as_uint(own.t));
+    st_cluster_u32(dst + 12, __float_as_uint(own.r));
+  }
+  cluster_sync_all();
+  const Sums st = join_parts<true, ENT, REST>(js.cta[2], parts, c);
+  cluster_sync_all();                // nobody overwrites what another still reads
+  return st;
 }
 __device__ __forceinline__ bool sums_ordinary(const Sums& st) { return st.s >= 0x1p-60f && st.s <= 0x1p120f; }
 
@@ -444,40 +496,47 @@ __device__ __forceinline__ unsigned long long rank_key(float x, int i) {
 constexpr uint32_t KEY_NEG_INF = 0x007fffffu;     // value_key(-inf)
 constexpr int V_BINS = 256;
 
+// The key of an alternative back as its logit.
+__device__ __forceinline__ float key_value(unsigned long long key) {
+  const uint32_t k = (uint32_t)(key >> 32);
+  return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
+}
+
 // CAND: candidates kept in shared memory.  A CTA that shares its row with others has fewer to look through and needs room
 // for the others' alternatives.
-template <int CAND_>
+template <int CAND_, int SHARES_>
 struct TopScratch {
-  static constexpr int CAND = CAND_;
+  static constexpr int CAND = CAND_, SHARES = SHARES_;
   int hist[V_BINS];
-  int active[V_THREADS];                 // the shares that can hold an alternative
-  unsigned long long cand[CAND];
+  uint16_t active[SHARES];               // the shares that can hold an alternative
+  alignas(16) unsigned long long cand[CAND];
   float w_max[V_WARPS], w_min[V_WARPS];
-  int last_bin, n_active, n_cand, count;
+  int last_bin, n_bins, n_active, n_cand, count;
   uint32_t floor_key;                    // smallest of the active shares' maxima
 };
 
-// Calls f(index, value) for every element of the shares listed in sc.active[0 .. n_active).
-template <typename T, typename SC, typename F>
+// Calls f(index, value) for every element of the shares listed in sc.active[0 .. n_active).  Share u V_THREADS + t: vectors
+// u V_THREADS + t of every chunk; the single elements of thread t belong to share t.
+template <typename T, typename RG, typename SC, typename F>
 __device__ __forceinline__ void for_active(const Row<T>& row, const SC& sc, F f) {
-  constexpr int N = Elem<T>::N;
-  const unsigned per = (unsigned)(row.v_end - row.v_begin + V_THREADS - 1) / V_THREADS;
+  constexpr int N = Elem<T>::N, BATCH = 4;
+  const unsigned per = (unsigned)row_chunks<RG>(row.v_end - row.v_begin);
   const unsigned total = (unsigned)sc.n_active * per;
-  for (unsigned q0 = threadIdx.x; q0 < total; q0 += 4 * V_THREADS) {
-    uint4 raw[4];
-    int at[4];
+  for (unsigned q0 = threadIdx.x; q0 < total; q0 += BATCH * V_THREADS) {
+    uint4 raw[BATCH];
+    int at[BATCH];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < BATCH; ++u) {
       const unsigned q = q0 + u * V_THREADS;
       at[u] = -1;
       if (q < total) {
         const unsigned g = q / per;
-        const int v = row.v_begin + sc.active[g] + (int)(q - g * per) * V_THREADS;
+        const int v = row.v_begin + sc.active[g] + (int)(q - g * per) * RG::CHUNK;
         if (v < row.v_end) { at[u] = row.vec_index(v); raw[u] = ld_stream(row.vec(v)); }
       }
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < BATCH; ++u) {
       if (at[u] < 0) continue;
       float2 x[N / 2];
       Elem<T>::pairs(raw[u], x);
@@ -491,24 +550,37 @@ __device__ __forceinline__ void for_active(const Row<T>& row, const SC& sc, F f)
     if (g < row.tail) f(row.tail_at + g, to_f32<T>(row.p[row.tail_at + g]));
   }
 }
+__device__ __forceinline__ int sum_cta(int v, int* total) {       // *total is 0 before and stays the sum until reset
+  v = __reduce_add_sync(0xffffffffu, v);
+  if ((threadIdx.x & 31) == 0 && v) atomicAdd(total, v);
+  __syncthreads();
+  return *total;
+}
 
 // The (up to) n elements of this CTA's part with the largest keys, logits of minus infinity left out, as
 // sc.cand[0 .. sc.n_cand) in any order; at least n of them (if there are as many), possibly more.
 // A share whose maximum is below the n-th largest of the shares' maxima holds none of the n largest elements, so only
-// about n of the V_THREADS shares are read again.  A histogram of the maxima between their least and their largest finds
-// the threshold; where its bins are too coarse (one logit far above the rest), bisection over the key bits does.  Where
-// the elements at or above the threshold outgrow the candidate list (long runs of equal logits), the bisection goes on
-// over the elements' 64-bit keys, which are all distinct.
-template <typename T, typename SC>
-__device__ __noinline__ void collect_top(const Row<T> row, float own_max, int n, SC& sc) {
-  constexpr int V_CAND = SC::CAND;
+// about n of the SHARES shares are read again (2 to 6 % of the row; one share a thread would make it 8 times as much).  A
+// histogram of the maxima between their least and their largest finds the threshold; where its bins are too coarse (one
+// logit far above the rest), bisection over the key bits does.  Where the elements at or above the threshold outgrow the
+// candidate list (long runs of equal logits), the bisection goes on over the elements' 64-bit keys, which are all
+// distinct.
+template <typename T, typename RG, typename SC>
+__device__ __noinline__ void collect_top(const Row<T> row, const float* own_max, int n, SC& sc) {
+  constexpr int CAND = SC::CAND, PER = RG::PER;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const bool any = own_max > -INFINITY;
-  const uint32_t mine = any ? value_key(own_max) : 0u;
+  float own[PER];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) own[u] = own_max[u];
   static_assert(V_BINS <= V_THREADS, "one bin per thread to clear");
   if (tid < V_BINS) sc.hist[tid] = 0;
   if (tid == 0) { sc.n_active = 0; sc.n_cand = 0; sc.floor_key = 0xffffffffu; sc.last_bin = V_BINS - 1; }
-  float hi = own_max, lo = any ? own_max : INFINITY;
+  float hi = -INFINITY, lo = INFINITY;
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    hi = fmaxf(hi, own[u]);
+    if (own[u] > -INFINITY) lo = fminf(lo, own[u]);
+  }
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
     hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
@@ -516,14 +588,16 @@ __device__ __noinline__ void collect_top(const Row<T> row, float own_max, int n,
   }
   if (lane == 0) { sc.w_max[warp] = hi; sc.w_min[warp] = lo; }
   __syncthreads();
-  hi = sc.w_max[0]; lo = sc.w_min[0];
 #pragma unroll
-  for (int w = 1; w < V_WARPS; ++w) { hi = fmaxf(hi, sc.w_max[w]); lo = fminf(lo, sc.w_min[w]); }
+  for (int w = 0; w < V_WARPS; ++w) { hi = fmaxf(hi, sc.w_max[w]); lo = fminf(lo, sc.w_min[w]); }
   if (!(hi > -INFINITY)) return;                       // nothing but minus infinity in this part (uniform)
   const float range = hi - lo;
   const float scale = range > 0.f && range < FLT_MAX ? (V_BINS - 1) / range : 0.f;
-  const int bin = min(V_BINS - 1, (int)((hi - own_max) * scale));     // falls as own_max grows
-  if (any) atomicAdd(&sc.hist[bin], 1);
+  // falls as the maximum grows
+  auto bin_of = [&](float m) { return min(V_BINS - 1, (int)((hi - m) * scale)); };
+#pragma unroll
+  for (int u = 0; u < PER; ++u)
+    if (own[u] > -INFINITY) atomicAdd(&sc.hist[bin_of(own[u])], 1);
   __syncthreads();
   if (warp == 0) {
     int c[V_BINS / 32], sum = 0;
@@ -535,59 +609,80 @@ __device__ __noinline__ void collect_top(const Row<T> row, float own_max, int n,
       const int v = __shfl_up_sync(0xffffffffu, before, o);
       if (lane >= o) before += v;
     }
+    if (lane == 31) sc.n_bins = before;                // shares with anything in them, unless a bin reaches n
     before -= sum;
+    __syncwarp();
 #pragma unroll
     for (int i = 0; i < V_BINS / 32; ++i) {
-      if (before < n && before + c[i] >= n) sc.last_bin = lane * (V_BINS / 32) + i;
+      if (before < n && before + c[i] >= n) { sc.last_bin = lane * (V_BINS / 32) + i; sc.n_bins = before + c[i]; }
       before += c[i];
     }
   }
   __syncthreads();
-  bool active = any && bin <= sc.last_bin;
-  int n_active = __syncthreads_count(active);
+  const int last_bin = sc.last_bin, n_active = sc.n_bins;
+  uint32_t from = KEY_NEG_INF + 1;                     // shares with a maximum of at least this key, in a bin up to last_bin
   if (n_active > 2 * n + 64) {
-    uint32_t klo = KEY_NEG_INF + 1, khi = 0xffffffffu;
-    while (khi - klo > 1) {                            // at most 32 rounds
-      const uint32_t mid = klo + (khi - klo) / 2;
-      const int cnt = __syncthreads_count(mine >= mid);
-      if (cnt >= n) { klo = mid; if (cnt <= n + n / 4) break; } else khi = mid;
+    uint32_t to = 0xffffffffu;
+    while (to - from > 1) {                            // at most 32 rounds
+      const uint32_t mid = from + (to - from) / 2;
+      __syncthreads();
+      if (tid == 0) sc.count = 0;
+      __syncthreads();
+      int c = 0;
+#pragma unroll
+      for (int u = 0; u < PER; ++u) c += value_key(own[u]) >= mid;
+      const int cnt = sum_cta(c, &sc.count);
+      if (cnt >= n) { from = mid; if (cnt <= n + n / 4) break; } else to = mid;
     }
-    active = any && mine >= klo;
   }
-  if (active) {
-    sc.active[atomicAdd(&sc.n_active, 1)] = tid;
-    atomicMin(&sc.floor_key, mine);
+  uint32_t least = 0xffffffffu;
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const uint32_t key = value_key(own[u]);
+    if (own[u] > -INFINITY && key >= from && bin_of(own[u]) <= last_bin) {
+      sc.active[atomicAdd(&sc.n_active, 1)] = (uint16_t)(u * V_THREADS + tid);
+      least = min(least, key);
+    }
   }
+  if (least != 0xffffffffu) atomicMin(&sc.floor_key, least);
   __syncthreads();
   // fewer shares than n with anything in them: their elements below the shares' maxima count as well
   unsigned long long klo = (unsigned long long)(n_active < n ? KEY_NEG_INF + 1 : sc.floor_key) << 32, khi = ~0ull;
   for (int attempt = 0; attempt < 2; ++attempt) {
-    for_active(row, sc, [&](int i, float x) {
+    for_active<T, RG>(row, sc, [&](int i, float x) {
       const unsigned long long k = rank_key(x, i);
       if (k >= klo) {
         const int at = atomicAdd(&sc.n_cand, 1);
-        if (at < V_CAND) sc.cand[at] = k;
+        if (at < CAND) sc.cand[at] = k;
       }
     });
     __syncthreads();
-    if (sc.n_cand <= V_CAND) return;
-    // More than fit: raise klo until n .. V_CAND elements are left.  64 halvings of the key range always get there.
+    if (sc.n_cand <= CAND) return;
+    // More than fit: raise klo until n .. CAND elements are left.  64 halvings of the key range always get there.
     for (int it = 0; it < 64; ++it) {
       const unsigned long long mid = klo + (khi - klo) / 2;
       __syncthreads();
       if (tid == 0) { sc.count = 0; sc.n_cand = 0; }
       __syncthreads();
       int c = 0;
-      for_active(row, sc, [&](int i, float x) { c += rank_key(x, i) >= mid; });
-      if (c) atomicAdd(&sc.count, c);
-      __syncthreads();
-      const int all = sc.count;
-      if (all >= n) { klo = mid; if (all <= V_CAND) break; } else khi = mid;
+      for_active<T, RG>(row, sc, [&](int i, float x) { c += rank_key(x, i) >= mid; });
+      const int all = sum_cta(c, &sc.count);
+      if (all >= n) { klo = mid; if (all <= CAND) break; } else khi = mid;
     }
     __syncthreads();
   }
-  if (tid == 0) sc.n_cand = V_CAND;      // only if the logits changed while they were read
+  if (tid == 0) sc.n_cand = CAND;        // only if the logits changed while they were read
   __syncthreads();
+}
+// How many of the n keys are larger than k.
+__device__ __forceinline__ int rank_among(const unsigned long long* keys, int n, unsigned long long k) {
+  int rank = 0, j = 0;
+  for (; j + 4 <= n; j += 4) {
+    const ulonglong2 a = *reinterpret_cast<const ulonglong2*>(keys + j), b = *reinterpret_cast<const ulonglong2*>(keys + j + 2);
+    rank += (a.x > k) + (a.y > k) + (b.x > k) + (b.y > k);
+  }
+  for (; j < n; ++j) rank += keys[j] > k;
+  return rank;
 }
 
 struct LogprobArgs {
@@ -626,12 +721,16 @@ __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobAr
   using RG = RingStream;
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ JoinScratch js;
-  using Scratch = TopScratch<SPLIT ? 512 : 1024>;
+  using Scratch = TopScratch<SPLIT ? 512 : 1024, RG::PER * V_THREADS>;
   __shared__ typename std::conditional<TOP, Scratch, int>::type sc_raw;
-  __shared__ unsigned long long merged[TOP && SPLIT ? V_MAX_SPLIT * CAMERA_MAX_TOP : 1];    // 0: none
+  unsigned long long* const merged = reinterpret_cast<unsigned long long*>(ring + RG::BYTES);   // TOP && SPLIT: the parts' best; 0: none
   const int lg = SPLIT ? a.lg : 0, part = SPLIT ? blockIdx.x : 0, parts = 1 << lg;
   const int tid = threadIdx.x;
-  if (SPLIT) cluster_started();
+  Exchange ex;
+  if (SPLIT) {
+    exchange_init(ex, js.bars);
+    cluster_started();
+  }
   bool started = !SPLIT;
   Feed<T, RG> feed;
   feed.logits = static_cast<const T*>(a.logits);
@@ -641,33 +740,26 @@ __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobAr
   feed.begin(blockIdx.y);
 #pragma unroll
   for (int i = 0; i < RG::SLOTS; ++i) feed.issue();
-  int at = 0, turn = 0, join_turn = 0;
+  int at = 0, join_turn = 0;
   const bool first = part == 0 && tid == 0;
   long long target = first && a.logprob && (int)blockIdx.y < a.rows ? a.targets[blockIdx.y] : -1;
-  for (int r = blockIdx.y; r < a.rows; r += gridDim.y, turn ^= 1) {
+  for (int r = blockIdx.y; r < a.rows; r += gridDim.y) {
     const Row<T> row(static_cast<const T*>(a.logits) + r * a.ld, a.vocab, part, lg);
     // the target's logit, and the next row's target, on their way during the walk
     const bool wanted = target >= 0 && target < a.vocab;
     const float x_target = wanted ? to_f32<T>(row.p[target]) : 0.f;
     if (first && a.logprob && r + (int)gridDim.y < a.rows) target = a.targets[r + gridDim.y];
-    float top = -INFINITY;
-    Sums st = walk_row<T, RG, ENT, false, TOP, false>(row, a.c, feed, ring, at, nullptr, nullptr, 0, &top);
+    float top[RG::PER];
+    Sums st = walk_row<T, RG, ENT, false, TOP, false>(row, a.c, feed, ring, at, nullptr, nullptr, 0, top);
     st = join_cta<false, ENT, false>(st, a.c, join_turn, js);
     if (SPLIT) {
       if (!started) { cluster_all_started(); started = true; }
-      publish_sums(st, part, parts, turn, js);
-      cluster_sync_all();
-      st = join_split<false, ENT, false>(parts, a.c, turn, js);
+      st = exchange_sums<ENT, false>(st, part, parts, a.c, ex, js);
     }
     const bool careful = !sums_ordinary(st);
     if (careful) {
       st = join_cta<true, ENT, false>(walk_careful<T, ENT, false>(row, a.c, nullptr, 0), a.c, join_turn, js);
-      if (SPLIT) {
-        cluster_sync_all();                              // every CTA has read the first round's sums
-        publish_sums(st, part, parts, turn, js);
-        cluster_sync_all();
-        st = join_split<true, ENT, false>(parts, a.c, turn, js);
-      }
+      if (SPLIT) st = exchange_careful<ENT, false>(st, part, parts, a.c, js);
     }
     const Softmax sm(st, careful, a.c, a.inv_tau);
     if (first) {
@@ -680,17 +772,13 @@ __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobAr
       int n_cand = 0, n_out = 0;
       const unsigned long long* cand = sc.cand;
       if (usable) {
-        collect_top<T, Scratch>(row, top, a.top_n, sc);
+        collect_top<T, RG, Scratch>(row, top, a.top_n, sc);
         __syncthreads();
         n_cand = n_out = sc.n_cand;
         if (SPLIT) {                                     // this part's best n go to the first CTA
           for (int q = tid; q < max(n_cand, a.top_n); q += V_THREADS) {
             const unsigned long long k = q < n_cand ? cand[q] : 0ull;
-            int rank = q;
-            if (q < n_cand) {
-              rank = 0;
-              for (int j = 0; j < n_cand; ++j) rank += cand[j] > k;
-            }
+            const int rank = q < n_cand ? rank_among(cand, n_cand, k) : q;
             if (rank < a.top_n) {
               const uint32_t dst = map_to_cta(smem_u32(&merged[part * a.top_n + rank]), 0);
               st_cluster_u32(dst, (uint32_t)k);
@@ -708,12 +796,10 @@ __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobAr
         for (int q = tid; q < n_cand; q += V_THREADS) {
           const unsigned long long k = cand[q];
           if (SPLIT && k == 0) continue;
-          int rank = 0;
-          for (int j = 0; j < n_cand; ++j) rank += cand[j] > k;
+          const int rank = rank_among(cand, n_cand, k);
           if (rank < a.top_n) {
-            const int i = (int)~(uint32_t)k;
-            out_i[rank] = i;
-            out_v[rank] = sm.logprob(to_f32<T>(row.p[i]));
+            out_i[rank] = (int)~(uint32_t)k;
+            out_v[rank] = sm.logprob(key_value(k));
           }
         }
         if (SPLIT && usable) {                           // how many there are in all
@@ -751,6 +837,7 @@ struct DistillArgs {
   long long ld;
   int rows, vocab, k;
   int lg;                   // 2^lg CTAs share a row
+  int in_place;             // the gradient takes the logits' room
   int mark_bytes;           // of one set of marks: a byte per vector of a part, rounded up to whole chunks
   float c, inv_tau;
   const int* idx;
@@ -930,7 +1017,11 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
   const bool lister = tid >= V_THREADS;
   const T* const logits = static_cast<const T*>(a.logits);
   uint8_t* const marks = ring + RG::BYTES;
-  if (SPLIT) cluster_started();
+  Exchange ex;
+  if (SPLIT) {
+    exchange_init(ex, js.bars);
+    cluster_started();
+  }
   bool started = !SPLIT;
   if (REST)
     for (int i = tid; i < a.mark_bytes / 2; i += VD_THREADS) reinterpret_cast<uint32_t*>(marks)[i] = 0u;
@@ -965,8 +1056,8 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
   int r = walk.next(feed.weight, a.rows, gridDim.y);
   __syncthreads();
   if (lister) bring_list(r, lists[0], marks);
-  if (!STATS && SPLIT) {
-    // in place: nobody writes to the first row before every CTA has its listed logits
+  if (!STATS && SPLIT && a.in_place) {
+    // nobody writes to the first row before every CTA has its listed logits
     cluster_all_started();
     started = true;
     cluster_sync_all();
@@ -990,20 +1081,13 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
       st = join_cta<false, false, REST>(st, a.c, join_turn, js);
       if (SPLIT) {
         if (!started) { cluster_all_started(); started = true; }
-        publish_sums(st, part, parts, turn, js);
-        cluster_sync_all();
-        st = join_split<false, false, REST>(parts, a.c, turn, js);
+        st = exchange_sums<false, REST>(st, part, parts, a.c, ex, js);
       }
       careful = !sums_ordinary(st);
       if (careful) {
         if (!lister) st = walk_careful<T, false, REST>(row, a.c, tl.idx, a.k);
         st = join_cta<true, false, REST>(st, a.c, join_turn, js);
-        if (SPLIT) {
-          cluster_sync_all();                         // every CTA has read the first round's sums
-          publish_sums(st, part, parts, turn, js);
-          cluster_sync_all();
-          st = join_split<true, false, REST>(parts, a.c, turn, js);
-        }
+        if (SPLIT) st = exchange_careful<false, REST>(st, part, parts, a.c, js);
       }
     }
     Softmax sm(st, careful, a.c, a.inv_tau);
@@ -1051,7 +1135,7 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
         if (!STATS) write_row<T, RG, FROM_FEED>(row, out, sm, w * coef, empty, feed, ring, at);
         else write_row<T, RG, HOLD ? FROM_RING : FROM_MEMORY>(row, out, sm, w * coef, empty, feed, ring, at0);
       }
-      if (!STATS && SPLIT) cluster_sync_all(); else __syncthreads();
+      if (!STATS && SPLIT && a.in_place) cluster_sync_all(); else __syncthreads();
       if (tid < a.k && !empty) {
         const int i = tl.idx[tid];
         if (i >= 0 && row.holds(i)) out[i] = Elem<T>::put(w * (sm.q(tl.x[tid]) - tl.p[tid]));
@@ -1065,10 +1149,17 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
 }
 
 // ------------------------------------------------------------------------------------------------ launches
-int sm_count() {
-  int dev = 0, sms = 148;
-  cudaGetDevice(&dev);
-  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+int sm_count() {                     // of the process's GPUs, which are all alike
+  static std::atomic<int> known;
+  int sms = known.load(std::memory_order_relaxed);
+  if (sms == 0) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+      cudaGetLastError();
+      return 148;
+    }
+    known.store(sms, std::memory_order_relaxed);
+  }
   return sms;
 }
 // CTAs that share a row when there are few: as many as keep the grid within two CTAs an SM and two vectors a thread.
@@ -1092,10 +1183,17 @@ int clusters_at_once(K kern, cudaLaunchConfig_t& cfg, int lg, std::atomic<int>* 
 
 template <auto KERN, typename A>
 cudaError_t launch_rows(const A& args, int threads, int smem, int sms, cudaStream_t st) {
-  static std::atomic<int> known[8];
+  static std::atomic<int> known[8], allowed[64];      // per size of cluster; shared memory asked for so far, per device
   const auto kern = KERN;
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
+  std::atomic<int>& ok = allowed[dev & 63];
+  if (dev > 63 || ok.load(std::memory_order_relaxed) < smem) {
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    ok.store(smem, std::memory_order_relaxed);
+  }
   const int split = 1 << args.lg;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)split, (unsigned)args.rows);
@@ -1119,7 +1217,7 @@ cudaError_t launch_logprobs(LogprobArgs& a, cudaStream_t st) {
   const int sms = sm_count();
   a.lg = split_for(a.rows, a.vocab / Elem<T>::N, sms);
   return a.lg == 0 ? launch_rows<k_token_logprobs<T, ENT, TOP, false>>(a, V_THREADS, RingStream::BYTES, sms, st)
-                   : launch_rows<k_token_logprobs<T, ENT, TOP, true>>(a, V_THREADS, RingStream::BYTES, sms, st);
+                   : launch_rows<k_token_logprobs<T, ENT, TOP, true>>(a, V_THREADS, RingStream::BYTES + (a.top_n * 8 << a.lg), sms, st);
 }
 template <typename T>
 cudaError_t launch_logprobs(LogprobArgs& a, cudaStream_t st) {
@@ -1134,8 +1232,8 @@ cudaError_t launch_distill(DistillArgs& a, cudaStream_t st) {
   a.lg = split_for(a.rows, n_vec, sms);
   // STEP: so many CTAs that a row's parts fit their rings; a row too long for eight is read twice
   if (STEP)
-    while (1 << a.lg < V_MAX_SPLIT && (n_vec >> a.lg) + 1 > RingHold::HELD) ++a.lg;
-  const bool hold = STEP && (n_vec >> a.lg) + 1 <= RingHold::HELD;
+    while (1 << a.lg < V_MAX_SPLIT && (n_vec >> a.lg) + 1 > HELD_VECS) ++a.lg;
+  const bool hold = STEP && (n_vec >> a.lg) + 1 <= HELD_VECS;
   a.mark_bytes = REST ? ((n_vec >> a.lg) + RingHold::CHUNK) / RingHold::CHUNK * RingHold::CHUNK : 0;
   const int smem = RingHold::BYTES + 2 * a.mark_bytes;
   if (a.lg == 0)
@@ -1178,7 +1276,7 @@ bool grad_ok(const camera_distill_t* d, const void* grad, int64_t ld) {
 
 DistillArgs distill_args(const camera_distill_t* d) {
   DistillArgs a;
-  a.logits = d->logits; a.ld = d->ld; a.rows = (int)d->n_rows; a.lg = 0; a.mark_bytes = 0; a.vocab = d->vocab; a.k = d->k;
+  a.logits = d->logits; a.ld = d->ld; a.rows = (int)d->n_rows; a.lg = 0; a.in_place = 0; a.mark_bytes = 0; a.vocab = d->vocab; a.k = d->k;
   a.c = 1.44269504088896341f / d->temperature; a.inv_tau = 1.f / d->temperature;
   a.idx = d->teacher_idx; a.logprob = d->teacher_logprob;
   a.d_loss = nullptr; a.loss = a.lse = a.log_tail = nullptr; a.grad = nullptr; a.ld_grad = 0;
@@ -1228,7 +1326,7 @@ extern "C" int camera_distill_backward(const camera_distill_t* d, const float* d
     return CAMERA_ERR_INVALID_ARG;
   DistillArgs a = distill_args(d);
   a.d_loss = d_loss; a.lse = const_cast<float*>(lse); a.log_tail = const_cast<float*>(log_tail);
-  a.grad = d_logits; a.ld_grad = d_ld;
+  a.grad = d_logits; a.ld_grad = d_ld; a.in_place = d_logits == d->logits;
   return launch_distill<DISTILL_BACKWARD>(a, d->dtype, d->flags & CAMERA_DISTILL_TAIL,
                                           static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CAMERA_OK : CAMERA_ERR_CUDA;
 }
@@ -1241,7 +1339,7 @@ extern "C" int camera_distill_step(const camera_distill_t* d, const float* d_los
   if (d->n_rows == 0) return CAMERA_OK;
   if (d_loss == nullptr || loss == nullptr || !grad_ok(d, d_logits, d_ld)) return CAMERA_ERR_INVALID_ARG;
   DistillArgs a = distill_args(d);
-  a.d_loss = d_loss; a.loss = loss; a.grad = d_logits; a.ld_grad = d_ld;
+  a.d_loss = d_loss; a.loss = loss; a.grad = d_logits; a.ld_grad = d_ld; a.in_place = d_logits == d->logits;
   return launch_distill<DISTILL_STEP>(a, d->dtype, d->flags & CAMERA_DISTILL_TAIL,
                                       static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CAMERA_OK : CAMERA_ERR_CUDA;
 }
