@@ -91,6 +91,9 @@ template <> struct Elem<float> {
   __device__ __forceinline__ static uint32_t max_vec(const uint4& v) { return max_word(max_word(v.x, v.y), max_word(v.z, v.w)); }
   __device__ __forceinline__ static float max_of(uint32_t w) { return __uint_as_float(w); }
   __device__ __forceinline__ static float put(float v) { return v; }
+  __device__ __forceinline__ static uint4 pack(const float2* x) {
+    return make_uint4(__float_as_uint(x[0].x), __float_as_uint(x[0].y), __float_as_uint(x[1].x), __float_as_uint(x[1].y));
+  }
 };
 template <> struct Elem<__nv_bfloat16> {
   static constexpr int N = 8;
@@ -110,6 +113,12 @@ template <> struct Elem<__nv_bfloat16> {
     return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
   }
   __device__ __forceinline__ static __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
+  __device__ __forceinline__ static uint4 pack(const float2* x) {
+    __nv_bfloat162 h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __float22bfloat162_rn(x[i]);
+    return *reinterpret_cast<const uint4*>(h);
+  }
 };
 // A row of `n` logits, or the part of it that CTA `part` of 2^lg walks: single elements before the first 16-byte
 // boundary (part 0), whole 16-byte vectors [v_begin, v_end), single elements after the last (last part).  Vector v belongs to
@@ -176,18 +185,15 @@ struct RowWalk {
   }
 };
 
-// Chunks of PER vectors a thread, SLOTS of them in the ring.  Both shapes are 96 KB, so that two CTAs fit an SM.  Larger
-// chunks cost fewer instructions an element; the finer ring leaves room for the next row while a part is held.
+// Chunks of PER vectors a thread, SLOTS of them in the ring.
 template <int PER_, int SLOTS_>
 struct Ring {
   static constexpr int PER = PER_, SLOTS = SLOTS_;
   static constexpr int CHUNK = PER * V_THREADS;              // vectors
   static constexpr int BYTES = SLOTS * CHUNK * 16;
 };
-using RingStream = Ring<8, 3>;
-using RingHold = Ring<4, 6>;
-constexpr int HELD_VECS = (RingHold::SLOTS - 1) * RingHold::CHUNK;       // longest part that stays between two passes
-static_assert(RingStream::BYTES == 96 * 1024 && RingHold::BYTES == 96 * 1024, "two CTAs per SM");
+using RingStream = Ring<8, 3>;       // 96 KB: two CTAs fit an SM
+using RingDistill = Ring<4, 6>;
 
 // The logits' way into the CTA: every thread copies its own 16-byte vectors with cp.async into its own places of a ring
 // in shared memory, over the ends of rows: while the sums of a row are joined and its results written, the next row is on
@@ -200,17 +206,24 @@ struct Feed {
   const float* weight;               // rows with weight 0 are passed over (null: none are)
   int rows, stride, vocab, part, lg;
   int r;                             // row the next chunk belongs to
+  bool twice, again;                 // every row comes twice in a row; the second time now
   uint32_t dst0, dst;                // this thread's place in slot 0 and in the next slot
   const T* src;                      // this thread's first vector of the next chunk
   int whole;                         // vectors from the chunk's first to the end of the part
   RowWalk walk;
-  __device__ __forceinline__ void begin(int first) {
+  __device__ __forceinline__ void begin(int first, bool twice_ = false) {
     dst = dst0;
+    twice = twice_; again = false; r = -1;
     walk.begin(weight, rows, first);
     open();
   }
   __device__ __forceinline__ void open() {
-    r = walk.next(weight, rows, stride);
+    if (twice && !again && r >= 0) {
+      again = true;
+    } else {
+      again = false;
+      r = walk.next(weight, rows, stride);
+    }
     if (r >= rows) return;
     const Row<T> row(logits + r * ld, vocab, part, lg);
     src = row.vec(row.v_begin) + (size_t)threadIdx.x * Row<T>::N;
@@ -249,12 +262,20 @@ __device__ __forceinline__ int row_chunks(int n_vec) { return n_vec <= RG::CHUNK
 template <typename RG>
 __device__ __forceinline__ int next_chunk(int at) { return at + RG::CHUNK * 16 == RG::BYTES ? 0 : at + RG::CHUNK * 16; }
 
-// One thread's share of the row, whose chunks lie in the ring from offset `at` on (moved past the row).  mark (REST): a
-// byte per vector of the part with a bit per element on the teacher's list.  TOP: top[u] receives the largest logit of
-// its vectors u of all chunks, single elements counted to u = 0 (minus infinity if there are none).  HOLD: the chunks stay in the ring; else each makes room for the next copy.
-template <typename T, typename RG, bool ENT, bool REST, bool TOP, bool HOLD>
+// PER vectors of this thread from the ring.
+template <typename RG>
+__device__ __forceinline__ void read_chunk(const uint8_t* mine, int at, uint4* raw) {
+#pragma unroll
+  for (int u = 0; u < RG::PER; ++u) raw[u] = *reinterpret_cast<const uint4*>(mine + at + u * V_THREADS * 16);
+}
+
+// One thread's share of the row, whose chunks arrive in the ring from offset `at` on (moved past the row).  mark (REST): a
+// bit per vector of the part, set where it holds a token of the teacher's list; such vectors are left out.  TOP: top[u]
+// receives the largest logit of its vectors u of all chunks, single elements counted to u = 0 (minus infinity if there
+// are none).
+template <typename T, typename RG, bool ENT, bool REST, bool TOP>
 __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>& feed, const uint8_t* ring, int& at,
-                                         const uint8_t* mark, const int* list, int k, float* top) {
+                                         const uint32_t* mark, const int* list, int k, float* top) {
   constexpr int N = Elem<T>::N;
   constexpr uint32_t NI = Elem<T>::NEG_INF;
   const uint4 nothing = make_uint4(NI, NI, NI, NI);          // minus infinity has no weight
@@ -268,21 +289,31 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
   float single[2] = {-INFINITY, -INFINITY}, on_list = 0.f;
   if (tid < row.head) single[0] = to_f32<T>(row.p[tid]);
   if (tid < row.tail) single[1] = to_f32<T>(row.p[row.tail_at + tid]);
-  const uint8_t* mine = ring + tid * 16;
-  if (REST) mark += tid;
+  const uint8_t* const mine = ring + tid * 16;
+  if (REST) mark += tid >> 5;
   bool first = true;
   int left = row.v_end - row.v_begin;                        // vectors of the part not yet walked
   do {
-    Feed<T, RG>::wait();
     uint4 raw[RG::PER];
-#pragma unroll
-    for (int u = 0; u < RG::PER; ++u) raw[u] = *reinterpret_cast<const uint4*>(mine + at + u * V_THREADS * 16);
+    Feed<T, RG>::wait();
+    read_chunk<RG>(mine, at, raw);
+    at = next_chunk<RG>(at);
     if (left < RG::CHUNK) {
 #pragma unroll
       for (int u = 0; u < RG::PER; ++u)
         if (tid + u * V_THREADS >= left) raw[u] = nothing;
     }
-    at = next_chunk<RG>(at);
+    if (REST) {
+      uint32_t word[RG::PER], any = 0;
+#pragma unroll
+      for (int u = 0; u < RG::PER; ++u) { word[u] = mark[u * (V_THREADS / 32)]; any |= word[u]; }
+      if (any) {                                             // the same in the whole warp
+#pragma unroll
+        for (int u = 0; u < RG::PER; ++u)
+          if ((word[u] >> (tid & 31)) & 1u) raw[u] = nothing;
+      }
+      mark += RG::CHUNK / 32;
+    }
     if (TOP || first) {
 #pragma unroll
       for (int u = 0; u < RG::PER; ++u) big[u] = Elem<T>::max_word(big[u], Elem<T>::max_vec(raw[u]));
@@ -305,22 +336,10 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
         if (ENT) d = make_float2(max_nan(d.x, D_FLOOR), max_nan(d.y, D_FLOOR));
         x[i] = make_float2(ex2(d.x), ex2(d.y));
         if (ENT) t2 = fma2(x[i], d, t2);
+        s2 = add2(s2, x[i]);
       }
-      if (REST) {
-        const uint32_t bits = mark[u * V_THREADS];           // 0 past the part's end
-        if (bits) {
-#pragma unroll
-          for (int i = 0; i < N / 2; ++i) {
-            if ((bits >> (2 * i)) & 1u) { on_list += x[i].x; x[i].x = 0.f; }
-            if ((bits >> (2 * i + 1)) & 1u) { on_list += x[i].y; x[i].y = 0.f; }
-          }
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < N / 2; ++i) s2 = add2(s2, x[i]);
     }
-    if (REST) mark += RG::CHUNK;
-    if (HOLD) Feed<T, RG>::commit(); else feed.issue();
+    feed.issue();
     left -= RG::CHUNK;
   } while (left > 0);
   Sums st;
@@ -377,7 +396,7 @@ __device__ __noinline__ Sums walk_careful(const Row<T> row, float c, const int* 
 
 // Shared memory of a CTA that joins sums.
 struct JoinScratch {
-  Sums warp[2][V_WARPS];           // joins alternate, so that none overwrites what another thread still reads
+  Sums warp[2][2 * V_WARPS];       // joins alternate, so that none overwrites what another thread still reads
   alignas(16) Sums cta[3][V_MAX_SPLIT];    // of the CTAs that share the row, written by each of them (see Exchange)
   unsigned long long bars[2];
 };
@@ -396,23 +415,30 @@ __device__ __forceinline__ Sums join_lanes(Sums st, float c) {
   }
   return st;
 }
-// Sums of the CTA from those of its first V_THREADS threads, the same in every thread of the CTA.
-template <bool CAREFUL, bool ENT, bool REST>
+// Sums of the CTA from those of its threads, the same in every thread.  WARPS: how many warps there are.
+template <bool CAREFUL, bool ENT, bool REST, int WARPS>
 __device__ __forceinline__ Sums join_cta(Sums st, float c, int& join_turn, JoinScratch& js) {
+  constexpr int WIDTH = WARPS <= V_WARPS ? V_WARPS : 2 * V_WARPS;
   Sums* const slots = js.warp[join_turn];
   join_turn ^= 1;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (warp < V_WARPS) {
-    st = join_lanes<32, CAREFUL, ENT, REST>(st, c);
-    if (lane == 0) slots[warp] = st;
-  }
+  st = join_lanes<32, CAREFUL, ENT, REST>(st, c);
+  if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = st;
   __syncthreads();
-  return join_lanes<V_WARPS, CAREFUL, ENT, REST>(slots[lane % V_WARPS], c);
+  const int from = threadIdx.x % WIDTH;
+  st = Sums{CAREFUL ? -FLT_MAX : -INFINITY, 0.f, 0.f, 0.f};
+  if (from < WARPS) st = slots[from];
+  return join_lanes<WIDTH, CAREFUL, ENT, REST>(st, c);
 }
 // The CTAs of a cluster may write to each other's shared memory once all of them run: each says so when it starts and
-// waits for the others where it first needs them.
-__device__ __forceinline__ void cluster_started() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_all_started() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// waits for the others where it first needs them.  Barriers of the cluster without .aligned: their callers come out of
+// loops whose lanes end at different times, and the aligned form is an illegal instruction in a warp that is not together.
+__device__ __forceinline__ void cluster_started() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_all_started() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+__device__ __forceinline__ void cluster_barrier() {
+  __syncwarp();
+  cluster_started();
+  cluster_all_started();
+}
 // How the CTAs that share a row exchange their sums: each writes its own into every CTA with a store that counts its bytes
 // on that CTA's barrier, and waits until all have come in.  (A cluster barrier would also wait for the gradients written
 // so far.)  Rows alternate between two places: a CTA sends the sums of row i + 2 only after those of row i + 1 have come
@@ -477,9 +503,9 @@ __device__ __forceinline__ Sums exchange_careful(const Sums& own, int part, int 
     st_cluster_u32(dst + 8, __float_as_uint(own.t));
     st_cluster_u32(dst + 12, __float_as_uint(own.r));
   }
-  cluster_sync_all();
+  cluster_barrier();
   const Sums st = join_parts<true, ENT, REST>(js.cta[2], parts, c);
-  cluster_sync_all();                // nobody overwrites what another still reads
+  cluster_barrier();                // nobody overwrites what another still reads
   return st;
 }
 __device__ __forceinline__ bool sums_ordinary(const Sums& st) { return st.s >= 0x1p-60f && st.s <= 0x1p120f; }
@@ -750,15 +776,15 @@ __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobAr
     const float x_target = wanted ? to_f32<T>(row.p[target]) : 0.f;
     if (first && a.logprob && r + (int)gridDim.y < a.rows) target = a.targets[r + gridDim.y];
     float top[RG::PER];
-    Sums st = walk_row<T, RG, ENT, false, TOP, false>(row, a.c, feed, ring, at, nullptr, nullptr, 0, top);
-    st = join_cta<false, ENT, false>(st, a.c, join_turn, js);
+    Sums st = walk_row<T, RG, ENT, false, TOP>(row, a.c, feed, ring, at, nullptr, nullptr, 0, top);
+    st = join_cta<false, ENT, false, V_WARPS>(st, a.c, join_turn, js);
     if (SPLIT) {
       if (!started) { cluster_all_started(); started = true; }
       st = exchange_sums<ENT, false>(st, part, parts, a.c, ex, js);
     }
     const bool careful = !sums_ordinary(st);
     if (careful) {
-      st = join_cta<true, ENT, false>(walk_careful<T, ENT, false>(row, a.c, nullptr, 0), a.c, join_turn, js);
+      st = join_cta<true, ENT, false, V_WARPS>(walk_careful<T, ENT, false>(row, a.c, nullptr, 0), a.c, join_turn, js);
       if (SPLIT) st = exchange_careful<ENT, false>(st, part, parts, a.c, js);
     }
     const Softmax sm(st, careful, a.c, a.inv_tau);
@@ -785,7 +811,7 @@ __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobAr
               st_cluster_u32(dst + 4, (uint32_t)(k >> 32));
             }
           }
-          cluster_sync_all();
+          cluster_barrier();
           cand = merged;
           n_cand = n_out = parts * a.top_n;
         }
@@ -838,7 +864,7 @@ struct DistillArgs {
   int rows, vocab, k;
   int lg;                   // 2^lg CTAs share a row
   int in_place;             // the gradient takes the logits' room
-  int mark_bytes;           // of one set of marks: a byte per vector of a part, rounded up to whole chunks
+  int mark_words;           // of one set of marks: a bit per vector of a part, rounded up to whole chunks
   float c, inv_tau;
   const int* idx;
   const float* logprob;
@@ -901,32 +927,60 @@ __device__ __forceinline__ void load_teacher(const DistillArgs& a, long long r, 
   }
 }
 
-// Sets or clears the marks of the listed tokens among the part's vectors (one warp).
-template <typename T, bool SET>
-__device__ __forceinline__ void mark_list(const Row<T>& row, const TeacherList& tl, int k, uint8_t* mark) {
+// Marks the part's vectors that hold listed tokens and sums them, listed and other elements apart (one warp).  Each such
+// vector is looked after by its first entry on the list.
+template <typename T>
+__device__ __forceinline__ Sums mark_list(const Row<T>& row, const TeacherList& tl, int k, float c, uint32_t* mark) {
+  constexpr int N = Elem<T>::N;
+  Sums st{-126.f, 0.f, 0.f, 0.f};
   for (int j = threadIdx.x & 31; j < k; j += 32) {
     const int i = tl.idx[j];
     if (i < row.first || i >= row.tail_at) continue;
-    const int v = (i - row.first) / Row<T>::N, at = v - row.v_begin;
+    const int v = (i - row.first) / N, i0 = row.vec_index(v);
     if (v < row.v_begin || v >= row.v_end) continue;
-    uint32_t* const word = reinterpret_cast<uint32_t*>(mark) + (at >> 2);
-    if (SET) atomicOr(word, 1u << (8 * (at & 3) + (i - row.first) % Row<T>::N)); else *word = 0u;
+    const uint4 raw = ld_stream(row.vec(v));
+    uint32_t listed = 0;
+    bool mine = true;
+    for (int l = 0; l < k; ++l) {
+      const unsigned off = (unsigned)(tl.idx[l] - i0);
+      if (off < (unsigned)N) {
+        listed |= 1u << off;
+        mine &= l >= j;
+      }
+    }
+    if (!mine) continue;
+    const int at = v - row.v_begin;
+    atomicOr(mark + (at >> 5), 1u << (at & 31));
+    float2 x[N / 2];
+    Elem<T>::pairs(raw, x);
+    float m = x[0].x;
+#pragma unroll
+    for (int q = 0; q < N; ++q) m = fmaxf(m, q & 1 ? x[q >> 1].y : x[q >> 1].x);
+    m = fmaxf(m * c, -126.f);
+    if (m > st.ref) raise<false, false, true>(st, m, c);
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+      const float e = ex2(fmaf(q & 1 ? x[q >> 1].y : x[q >> 1].x, c, -st.ref));
+      st.s += e;
+      if (!((listed >> q) & 1u)) st.r += e;
+    }
+  }
+  return st;
+}
+template <typename T>
+__device__ __forceinline__ void unmark_list(const Row<T>& row, const TeacherList& tl, int k, uint32_t* mark) {
+  for (int j = threadIdx.x & 31; j < k; j += 32) {
+    const int i = tl.idx[j];
+    if (i < row.first || i >= row.tail_at) continue;
+    const int v = (i - row.first) / Row<T>::N;
+    if (v >= row.v_begin && v < row.v_end) mark[(v - row.v_begin) >> 5] = 0u;
   }
 }
 template <typename T>
 __device__ __forceinline__ void store_vec(T* o, const float2* x, bool aligned) {
   constexpr int N = Elem<T>::N;
   if (aligned) {
-    uint4 w;
-    if constexpr (sizeof(T) == 2) {
-      __nv_bfloat162 h[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) h[i] = __float22bfloat162_rn(x[i]);
-      w = *reinterpret_cast<const uint4*>(h);
-    } else {
-      w = make_uint4(__float_as_uint(x[0].x), __float_as_uint(x[0].y), __float_as_uint(x[1].x), __float_as_uint(x[1].y));
-    }
-    __stcs(reinterpret_cast<uint4*>(o), w);
+    __stcs(reinterpret_cast<uint4*>(o), Elem<T>::pack(x));
   } else {
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) { o[2 * i] = Elem<T>::put(x[i].x); o[2 * i + 1] = Elem<T>::put(x[i].y); }
@@ -942,15 +996,13 @@ __device__ __forceinline__ void zero_row(const Row<T>& row, T* out) {
   for (int v = row.v_begin + tid; v < row.v_end; v += V_THREADS) store_vec<T>(out + row.vec_index(v), zero, aligned);
 }
 
-enum { FROM_RING = 0, FROM_FEED = 1, FROM_MEMORY = 2 };
-
-// Writes scale * q_v (or 0: blank) for every element of the part.  FROM_RING: its vectors lie in the ring from slot
-// `slot` on; FROM_FEED: they arrive there; either way they make room one chunk after the other.
-template <typename T, typename RG, int FROM>
+// Writes scale * q_v (or 0: blank) for every element of the part, whose vectors arrive in the ring from offset `at` on
+// (moved past them).
+template <typename T, typename RG>
 __device__ __forceinline__ void write_row(const Row<T>& row, T* out, const Softmax& sm, float scale, bool blank, Feed<T, RG>& feed,
-                                          const uint8_t* ring, int& ring_at) {
+                                          const uint8_t* ring, int& at) {
   constexpr int N = Elem<T>::N;
-  const int tid = threadIdx.x, n_vec = row.v_end - row.v_begin, chunks = row_chunks<RG>(n_vec);
+  const int tid = threadIdx.x;
   float single[2] = {0.f, 0.f};
   if (tid < row.head) single[0] = to_f32<T>(row.p[tid]);
   if (tid < row.tail) single[1] = to_f32<T>(row.p[row.tail_at + tid]);
@@ -958,57 +1010,60 @@ __device__ __forceinline__ void write_row(const Row<T>& row, T* out, const Softm
   const float2 c2 = make_float2(sm.c, sm.c), k2 = make_float2(-sm.k, -sm.k), s2 = make_float2(scale, scale);
   const uint8_t* const mine = ring + tid * 16;
   T* o = out + row.vec_index(row.v_begin + tid);
-  const bool plain = !blank && !sm.careful;
-  for (int ch = 0, left = n_vec - tid; ch < chunks; ++ch, left -= RG::CHUNK) {
-    if (FROM == FROM_FEED) Feed<T, RG>::wait();
+  const bool plain = aligned && !blank && !sm.careful;
+  int left = row.v_end - row.v_begin;
+  do {
     uint4 raw[RG::PER];
+    Feed<T, RG>::wait();
+    read_chunk<RG>(mine, at, raw);
+    at = next_chunk<RG>(at);
+    if (plain && left >= RG::CHUNK) {        // no branch among the vectors: their exponentials overlap
 #pragma unroll
-    for (int u = 0; u < RG::PER; ++u) {
-      if (FROM == FROM_MEMORY) {
-        if (left > u * V_THREADS) raw[u] = ld_stream(row.vec(row.v_begin + ch * RG::CHUNK + u * V_THREADS + tid));
-      } else {
-        raw[u] = *reinterpret_cast<const uint4*>(mine + ring_at + u * V_THREADS * 16);
-      }
-    }
-    if (FROM != FROM_MEMORY) ring_at = next_chunk<RG>(ring_at);
-#pragma unroll
-    for (int u = 0; u < RG::PER; ++u) {
-      if (left <= u * V_THREADS) continue;
-      float2 x[N / 2];
-      Elem<T>::pairs(raw[u], x);
-      if (plain) {
+      for (int u = 0; u < RG::PER; ++u) {
+        float2 x[N / 2];
+        Elem<T>::pairs(raw[u], x);
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) {
           const float2 d = fma2(x[i], c2, k2);
           x[i] = mul2(make_float2(ex2(d.x), ex2(d.y)), s2);
         }
-      } else {
+        raw[u] = Elem<T>::pack(x);
+      }
+#pragma unroll
+      for (int u = 0; u < RG::PER; ++u) __stcs(reinterpret_cast<uint4*>(o + (size_t)u * V_THREADS * N), raw[u]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < RG::PER; ++u) {
+        if (left <= u * V_THREADS + tid) continue;
+        float2 x[N / 2];
+        Elem<T>::pairs(raw[u], x);
 #pragma unroll
         for (int i = 0; i < N / 2; ++i)
           x[i] = blank ? make_float2(0.f, 0.f) : make_float2(scale * sm.q(x[i].x), scale * sm.q(x[i].y));
+        store_vec<T>(o + (size_t)u * V_THREADS * N, x, aligned);
       }
-      store_vec<T>(o + (size_t)u * V_THREADS * N, x, aligned);
     }
     o += (size_t)RG::CHUNK * N;
-    if (FROM != FROM_MEMORY) feed.issue();
-  }
+    feed.issue();
+    left -= RG::CHUNK;
+  } while (left > 0);
   if (tid < row.head) out[tid] = Elem<T>::put(blank ? 0.f : scale * sm.q(single[0]));
   if (tid < row.tail) out[row.tail_at + tid] = Elem<T>::put(blank ? 0.f : scale * sm.q(single[1]));
 }
 
-// A CTA, or (SPLIT) the CTAs of a cluster together, take row after row, like k_token_logprobs.  HOLD (STEP, and the part
-// fits): the part stays in the ring between the pass that sums and the pass that writes the gradient, so a logit is read
-// from memory once.  The last warp looks after the teacher's lists: while the others sum a row it brings in the next
+// A CTA, or (SPLIT) the CTAs of a cluster together, take row after row, like k_token_logprobs.  STEP sends every row
+// through the ring twice, once to sum it and once to write the gradient; the second time it comes from L2 (see Feed).  The
+// last warp looks after the teacher's lists: while the others sum a row it brings in the next
 // row's, and while they write the gradient it forms the loss.
 constexpr int VD_THREADS = V_THREADS + 32;
 constexpr int VD_LISTS = 3;
 
-template <typename T, int MODE, bool TAIL, bool SPLIT, bool HOLD>
+template <typename T, int MODE, bool TAIL, bool SPLIT>
 __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) {
   constexpr bool STATS = MODE != DISTILL_BACKWARD;
   constexpr bool GRAD = MODE != DISTILL_FORWARD;
   constexpr bool REST = STATS && TAIL;
-  using RG = RingHold;
+  using RG = RingDistill;
   extern __shared__ __align__(16) uint8_t ring[];     // the ring, then (REST) two sets of marks
   __shared__ JoinScratch js;
   __shared__ TeacherList lists[VD_LISTS];
@@ -1016,7 +1071,7 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
   const int tid = threadIdx.x;
   const bool lister = tid >= V_THREADS;
   const T* const logits = static_cast<const T*>(a.logits);
-  uint8_t* const marks = ring + RG::BYTES;
+  uint32_t* const marks = reinterpret_cast<uint32_t*>(ring + RG::BYTES);
   Exchange ex;
   if (SPLIT) {
     exchange_init(ex, js.bars);
@@ -1024,13 +1079,13 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
   }
   bool started = !SPLIT;
   if (REST)
-    for (int i = tid; i < a.mark_bytes / 2; i += VD_THREADS) reinterpret_cast<uint32_t*>(marks)[i] = 0u;
+    for (int i = tid; i < 2 * a.mark_words; i += VD_THREADS) marks[i] = 0u;
   Feed<T, RG> feed;
   feed.logits = logits;
   feed.ld = a.ld; feed.weight = GRAD ? a.d_loss : nullptr;
   feed.rows = a.rows; feed.stride = gridDim.y; feed.vocab = a.vocab; feed.part = part; feed.lg = lg;
   feed.dst0 = smem_u32(ring) + tid * 16;
-  feed.begin(lister ? a.rows : (int)blockIdx.y);
+  feed.begin(lister ? a.rows : (int)blockIdx.y, MODE == DISTILL_STEP);
 #pragma unroll
   for (int i = 0; i < RG::SLOTS; ++i) feed.issue();
   if (GRAD && !lister) {                              // rows that do not count: their logits are not looked at
@@ -1040,7 +1095,8 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
       if (STATS && part == 0 && tid == 0) a.loss[r] = 0.f;
     }
   }
-  auto bring_list = [&](int r, TeacherList& tl, uint8_t* mark) {      // one warp
+  Sums listed{-126.f, 0.f, 0.f, 0.f}, listed_next = listed;          // the lister's: of the vectors with listed tokens
+  auto bring_list = [&](int r, TeacherList& tl, uint32_t* mark) {
     if (r >= a.rows) return;
     const Row<T> row(logits + r * a.ld, a.vocab, part, lg);
     load_teacher<TAIL>(a, r, tl);
@@ -1049,7 +1105,7 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
       const int i = tl.idx[j];
       tl.x[j] = i >= 0 ? to_f32<T>(row.p[i]) : 0.f;
     }
-    if (REST) mark_list<T, true>(row, tl, a.k, mark);
+    if (REST) listed_next = mark_list<T>(row, tl, a.k, a.c, mark);
   };
   RowWalk walk;
   walk.begin(feed.weight, a.rows, blockIdx.y);
@@ -1060,7 +1116,7 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
     // nobody writes to the first row before every CTA has its listed logits
     cluster_all_started();
     started = true;
-    cluster_sync_all();
+    cluster_barrier();
   } else {
     __syncthreads();
   }
@@ -1070,23 +1126,27 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
     const Row<T> row(logits + r * a.ld, a.vocab, part, lg);
     const TeacherList& tl = lists[list];
     const int list_next = list + 1 == VD_LISTS ? 0 : list + 1;
-    uint8_t* const mark = marks + turn * a.mark_bytes;
-    int at0 = at;
+    uint32_t* const mark = marks + turn * a.mark_words;
     Sums st{-INFINITY, 0.f, 0.f, 0.f};
     bool careful = false, empty;
     float coef = 1.f;
-    if (lister) bring_list(r_next, lists[list_next], marks + (turn ^ 1) * a.mark_bytes);
+    if (lister) {
+      listed = listed_next;
+      bring_list(r_next, lists[list_next], marks + (turn ^ 1) * a.mark_words);
+    }
     if (STATS) {
-      if (!lister) st = walk_row<T, RG, false, REST, false, HOLD>(row, a.c, feed, ring, at, mark, tl.idx, a.k, nullptr);
-      st = join_cta<false, false, REST>(st, a.c, join_turn, js);
+      if (!lister) st = walk_row<T, RG, false, REST, false>(row, a.c, feed, ring, at, mark, tl.idx, a.k, nullptr);
+      else if (REST) st = listed;
+      st = join_cta<false, false, REST, V_WARPS + 1>(st, a.c, join_turn, js);
       if (SPLIT) {
         if (!started) { cluster_all_started(); started = true; }
         st = exchange_sums<false, REST>(st, part, parts, a.c, ex, js);
       }
       careful = !sums_ordinary(st);
       if (careful) {
+        st = Sums{-FLT_MAX, 0.f, 0.f, 0.f};
         if (!lister) st = walk_careful<T, false, REST>(row, a.c, tl.idx, a.k);
-        st = join_cta<true, false, REST>(st, a.c, join_turn, js);
+        st = join_cta<true, false, REST, V_WARPS + 1>(st, a.c, join_turn, js);
         if (SPLIT) st = exchange_careful<false, REST>(st, part, parts, a.c, js);
       }
     }
@@ -1096,7 +1156,7 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
       empty = st.s == 0.f || (careful && st.ref * a.c < -FLT_MAX);
       if (REST && tl.rest != 0.0) coef = st.r > 0.f || st.r != st.r ? 1.f - (float)tl.rest * (st.s / st.r) : 0.f;
       if (lister) {
-        if (REST) mark_list<T, false>(row, tl, a.k, mark);
+        if (REST) unmark_list<T>(row, tl, a.k, mark);
         if (part == 0) {
           double loss = 0.0;
           for (int j = tid & 31; j < a.k; j += 32) {
@@ -1132,10 +1192,9 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
       T* const out = static_cast<T*>(a.grad) + r * a.ld_grad;
       const float w = a.d_loss[r] * a.inv_tau;
       if (!lister) {
-        if (!STATS) write_row<T, RG, FROM_FEED>(row, out, sm, w * coef, empty, feed, ring, at);
-        else write_row<T, RG, HOLD ? FROM_RING : FROM_MEMORY>(row, out, sm, w * coef, empty, feed, ring, at0);
+        write_row<T, RG>(row, out, sm, w * coef, empty, feed, ring, at);
       }
-      if (!STATS && SPLIT && a.in_place) cluster_sync_all(); else __syncthreads();
+      if (!STATS && SPLIT && a.in_place) cluster_barrier(); else __syncthreads();
       if (tid < a.k && !empty) {
         const int i = tl.idx[tid];
         if (i >= 0 && row.holds(i)) out[i] = Elem<T>::put(w * (sm.q(tl.x[tid]) - tl.p[tid]));
@@ -1227,20 +1286,13 @@ cudaError_t launch_logprobs(LogprobArgs& a, cudaStream_t st) {
 
 template <typename T, int MODE, bool TAIL>
 cudaError_t launch_distill(DistillArgs& a, cudaStream_t st) {
-  constexpr bool REST = TAIL && MODE != DISTILL_BACKWARD, STEP = MODE == DISTILL_STEP;
+  constexpr bool REST = TAIL && MODE != DISTILL_BACKWARD;
   const int sms = sm_count(), n_vec = a.vocab / Elem<T>::N;
   a.lg = split_for(a.rows, n_vec, sms);
-  // STEP: so many CTAs that a row's parts fit their rings; a row too long for eight is read twice
-  if (STEP)
-    while (1 << a.lg < V_MAX_SPLIT && (n_vec >> a.lg) + 1 > HELD_VECS) ++a.lg;
-  const bool hold = STEP && (n_vec >> a.lg) + 1 <= HELD_VECS;
-  a.mark_bytes = REST ? ((n_vec >> a.lg) + RingHold::CHUNK) / RingHold::CHUNK * RingHold::CHUNK : 0;
-  const int smem = RingHold::BYTES + 2 * a.mark_bytes;
-  if (a.lg == 0)
-    return hold ? launch_rows<k_distill<T, MODE, TAIL, false, STEP>>(a, VD_THREADS, smem, sms, st)
-                : launch_rows<k_distill<T, MODE, TAIL, false, false>>(a, VD_THREADS, smem, sms, st);
-  return hold ? launch_rows<k_distill<T, MODE, TAIL, true, STEP>>(a, VD_THREADS, smem, sms, st)
-              : launch_rows<k_distill<T, MODE, TAIL, true, false>>(a, VD_THREADS, smem, sms, st);
+  a.mark_words = REST ? ((n_vec >> a.lg) + RingDistill::CHUNK) / RingDistill::CHUNK * (RingDistill::CHUNK / 32) : 0;
+  const int smem = RingDistill::BYTES + 8 * a.mark_words;
+  return a.lg == 0 ? launch_rows<k_distill<T, MODE, TAIL, false>>(a, VD_THREADS, smem, sms, st)
+                   : launch_rows<k_distill<T, MODE, TAIL, true>>(a, VD_THREADS, smem, sms, st);
 }
 template <int MODE>
 cudaError_t launch_distill(DistillArgs& a, int dtype, bool tail, cudaStream_t st) {
@@ -1276,7 +1328,7 @@ bool grad_ok(const camera_distill_t* d, const void* grad, int64_t ld) {
 
 DistillArgs distill_args(const camera_distill_t* d) {
   DistillArgs a;
-  a.logits = d->logits; a.ld = d->ld; a.rows = (int)d->n_rows; a.lg = 0; a.in_place = 0; a.mark_bytes = 0; a.vocab = d->vocab; a.k = d->k;
+  a.logits = d->logits; a.ld = d->ld; a.rows = (int)d->n_rows; a.lg = 0; a.in_place = 0; a.mark_words = 0; a.vocab = d->vocab; a.k = d->k;
   a.c = 1.44269504088896341f / d->temperature; a.inv_tau = 1.f / d->temperature;
   a.idx = d->teacher_idx; a.logprob = d->teacher_logprob;
   a.d_loss = nullptr; a.loss = a.lse = a.log_tail = nullptr; a.grad = nullptr; a.ld_grad = 0;
