@@ -425,7 +425,7 @@ __device__ __forceinline__ Sums join_cta(Sums st, float c, int& join_turn, JoinS
   if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = st;
   __syncthreads();
   const int from = threadIdx.x % WIDTH;
-  st = Sums{CAREFUL ? -FLT_MAX : -INFINITY, 0.f, 0.f, 0.f};
+  st = Sums{-FLT_MAX, 0.f, 0.f, 0.f};
   if (from < WARPS) st = slots[from];
   return join_lanes<WIDTH, CAREFUL, ENT, REST>(st, c);
 }
@@ -463,7 +463,7 @@ __device__ __forceinline__ void exchange_init(Exchange& ex, unsigned long long* 
 template <bool CAREFUL, bool ENT, bool REST>
 __device__ __forceinline__ Sums join_parts(const Sums* cta, int parts, float c) {
   const int lane = threadIdx.x % V_MAX_SPLIT;
-  Sums st{CAREFUL ? -FLT_MAX : -INFINITY, 0.f, 0.f, 0.f};
+  Sums st{-FLT_MAX, 0.f, 0.f, 0.f};
   if (lane < parts) st = cta[lane];
   return join_lanes<V_MAX_SPLIT, CAREFUL, ENT, REST>(st, c);
 }
@@ -1127,7 +1127,7 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
     const TeacherList& tl = lists[list];
     const int list_next = list + 1 == VD_LISTS ? 0 : list + 1;
     uint32_t* const mark = marks + turn * a.mark_words;
-    Sums st{-INFINITY, 0.f, 0.f, 0.f};
+    Sums st{-FLT_MAX, 0.f, 0.f, 0.f};        // joins as nothing
     bool careful = false, empty;
     float coef = 1.f;
     if (lister) {
