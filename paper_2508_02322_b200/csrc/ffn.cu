@@ -15,6 +15,8 @@
 #include <cuda.h>
 #include <string.h>
 
+#include <atomic>
+
 #include "common.cuh"
 #include "umma.cuh"
 #include "umma_pair.cuh"
@@ -47,13 +49,14 @@ struct FfnGemm {
   FfnProblem prob[3];
   int n_prob, n_units;
   int n_kb;                 // k blocks per segment
-  int bn;                   // columns per B tile; a work unit has two of them
+  int bn, nb;               // columns per B tile; B tiles per work unit (GATE_UP: 2, one of each matrix)
   int n_stages, n_acc;      // ring depth; accumulator sets in tensor memory
   uint16_t *g, *u;          // GATE_UP: where to keep G and U (or null); DH: inputs.  Upper halves of the 24 bits kept,
   long long lo_off;         // with the lower byte of element i of g at ((uint8_t*)base)[lo_off + i], base the start of g's buffer
   __nv_bfloat16 *dg, *du, *h;   // DH outputs; GATE_UP: h
   long long act_ld, h_ld;   // pitch of g and u, dg and du; of h
   PlanTotals* totals;
+  int clear_status;         // first kernel of the call
   unsigned long long wait_limit_ns;
 };
 
@@ -74,8 +77,8 @@ __device__ __forceinline__ FfnUnit decode(const FfnGemm& q, int unit, bool dual)
   rem -= grp * per_group;
   const int in_group = min(G_GROUP_M, m_tiles - grp * G_GROUP_M);
   r.m0 = (grp * G_GROUP_M + rem % in_group) * G_TILE_M;
-  r.n0 = (rem / in_group) * (dual ? q.bn : 2 * q.bn);
-  r.two = dual || r.n0 + q.bn < pr.n;
+  r.n0 = (rem / in_group) * (dual ? q.bn : q.nb * q.bn);
+  r.two = dual || (q.nb == 2 && r.n0 + q.bn < pr.n);
   return r;
 }
 
@@ -150,7 +153,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
   const int n_pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
   const int half = q.bn >> 1;                               // columns of a B tile this CTA supplies
   const int b_bytes = half * 128;
-  const int stage_bytes = G_A_BYTES + 2 * b_bytes;
+  const int stage_bytes = G_A_BYTES + q.nb * b_bytes;
 
   if (tid == 0) {
     for (int s = 0; s < q.n_stages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
@@ -170,6 +173,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
   cluster_sync_all();     // the other CTA's barriers are initialised before anything arrives on them
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  // The next kernel of the call may take SMs as they fall free and set itself up; what it reads or writes beyond that
+  // waits for the kernels before it (here) to end.
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // The call's first kernel clears its status word.  A CTA that gives up records that at its end, 2 ms after the wait that
+  // ran out at the earliest, when every CTA of the grid (one per SM) has long started.
+  if (q.clear_status && blockIdx.x == 0 && tid == 0) atomicExch(&q.totals->status, 0);
 
   if (warp == 4) {
     // ------------------------------------------------------------------ TMA producer (each CTA loads its own share)
@@ -228,7 +238,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
         const FfnUnit u = decode(q, unit, DUAL);
         if (!mbar_wait_cluster(tempty_bar(acc), acc_phase ^ 1u, abort_flag)) { ok = false; break; }
         tc_fence_after();
-        const uint32_t d0 = tmem_base + (uint32_t)(acc * 2 * q.bn), d1 = d0 + (uint32_t)q.bn;
+        const uint32_t d0 = tmem_base + (uint32_t)(acc * q.nb * q.bn), d1 = d0 + (uint32_t)q.bn;
         for (int kb = 0; kb < SEGMENTS * q.n_kb; ++kb) {
           if (!mbar_wait(full_bar(stage), phase, abort_flag)) { ok = false; break; }
           tc_fence_after();
@@ -263,8 +273,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
       ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_phase, abort_flag));
       if (!ok) break;
       tc_fence_after();
-      const uint32_t t0 = tmem_base + ((uint32_t)(warp * 32) << 16) + (uint32_t)(acc * 2 * q.bn);
-      const int cols = min(pr.n - u.n0, DUAL ? q.bn : 2 * q.bn);
+      const uint32_t t0 = tmem_base + ((uint32_t)(warp * 32) << 16) + (uint32_t)(acc * q.nb * q.bn);
+      const int cols = min(pr.n - u.n0, DUAL ? q.bn : q.nb * q.bn);
       if constexpr (MODE == FFN_GATE_UP) {
         __nv_bfloat16* const h = q.h + row * q.h_ld + u.n0;
         const bool keep = q.g != nullptr;
@@ -513,6 +523,45 @@ __global__ void __launch_bounds__(S_THREADS) k_ffn_few(const FfnFew q) {
 // ------------------------------------------------------------------------------------------------ host side
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
+// Lets a kernel use `bytes` of dynamic shared memory; asks the driver once per kernel, device and growth.
+template <auto KERN>
+cudaError_t allow_smem(int bytes) {
+  static std::atomic<int> allowed[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  std::atomic<int>& ok = allowed[dev & 63];
+  if (dev < 64 && ok.load(std::memory_order_relaxed) >= bytes) return cudaSuccess;
+  e = cudaFuncSetAttribute(KERN, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) ok.store(bytes, std::memory_order_relaxed);
+  return e;
+}
+// chained: the kernel may start while the one before it in the stream ends (it waits for that itself, griddepcontrol).
+template <typename A>
+cudaError_t launch_chained(void (*kern)(A), const A& args, int grid_x, int grid_y, int cluster_y, int threads, int smem, bool chained,
+                           cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid_x, (unsigned)grid_y);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  int n = 0;
+  if (cluster_y > 1) {
+    at[n].id = cudaLaunchAttributeClusterDimension;
+    at[n].val.clusterDim.x = 1; at[n].val.clusterDim.y = (unsigned)cluster_y; at[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (chained) {
+    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n].val.programmaticStreamSerializationAllowed = 1;
+    ++n;
+  }
+  cfg.attrs = at;
+  cfg.numAttrs = (unsigned)n;
+  return cudaLaunchKernelEx(&cfg, kern, args);
+}
+
 struct FfnShape {
   int64_t T;
   int D, F, ld;
@@ -546,19 +595,22 @@ FfnLayout ffn_layout(const FfnShape& s, bool backward) {
   return l;
 }
 
-// Columns per B tile: 256 gives the least traffic per product (48 KB per CTA and k block for 8.4 Mflop), fewer columns
-// give more work units where the tiles would leave pairs idle in the last round.  The cost of a round is taken as the
-// longer of its products and its loads.
-int choose_bn(long long m_tiles, int n, bool dual, int min_bn, int n_pairs) {
-  int best = 256;
+// Columns per B tile and B tiles per work unit.  512 columns (2 x 256) give the least traffic per product (48 KB per CTA
+// and k block for 8.4 Mflop), fewer columns give more work units where the tiles would leave pairs idle in the last
+// round.  The cost of a round is taken as the longer of its products and its loads plus a share for what a unit costs
+// beside its k blocks.
+struct Tile { int bn, nb; };
+Tile choose_tile(long long m_tiles, int n, bool dual, int min_bn, int n_kb, int n_pairs) {
+  Tile best{256, 2};
   double best_cost = 1e300;
-  for (int bn = 256; bn >= min_bn; bn >>= 1) {
-    const int per = dual ? bn : 2 * bn;
-    const long long units = m_tiles * ((n + per - 1) / per);
-    const double mma = bn / 256.0, load = 0.8 * (16.0 + bn / 8.0) / 48.0;
-    const double cost = (double)((units + n_pairs - 1) / n_pairs) * (mma > load ? mma : load);
-    if (cost < best_cost * 0.97) { best = bn; best_cost = cost; }
-  }
+  for (int bn = 256; bn >= min_bn; bn >>= 1)
+    for (int nb = 2; nb >= (dual || bn > min_bn ? 2 : 1); --nb) {
+      const int per = dual ? bn : nb * bn;
+      const long long units = m_tiles * ((n + per - 1) / per);
+      const double mma = nb * bn / 512.0, load = 0.8 * (16.0 + nb * bn / 16.0) / 48.0;
+      const double cost = (double)((units + n_pairs - 1) / n_pairs) * ((mma > load ? mma : load) + 2.0 * mma / n_kb);
+      if (cost < best_cost * 0.97) { best = Tile{bn, nb}; best_cost = cost; }
+    }
   return best;
 }
 
@@ -569,31 +621,38 @@ bool enc(CUtensorMap* out, const void* p, long long rows, long long cols, long l
 bool wide_rows(const void* p, long long ld) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0 && ld % 16 == 0; }
 
 template <int MODE>
-cudaError_t launch_gemm(FfnGemm& q, int bn, int n_pairs, cudaStream_t st) {
-  q.bn = bn;
-  q.n_acc = bn <= 128 ? 2 : 1;
-  const int stage = G_A_BYTES + bn * 128;
+cudaError_t launch_gemm(FfnGemm& q, Tile t, int n_pairs, bool first, cudaStream_t st) {
+  q.bn = t.bn; q.nb = t.nb;
+  q.clear_status = first;
+  q.n_acc = t.nb * t.bn <= 256 ? 2 : 1;
+  const int stage = G_A_BYTES + t.nb * t.bn * 64;
   q.n_stages = G_RING_BYTES / stage < G_MAX_STAGES ? G_RING_BYTES / stage : G_MAX_STAGES;
   int units = 0;
   for (int p = 0; p < q.n_prob; ++p) {
-    const int per = MODE == FFN_GATE_UP ? bn : 2 * bn;
+    const int per = MODE == FFN_GATE_UP ? t.bn : t.nb * t.bn;
     q.prob[p].n_tiles = (q.prob[p].n + per - 1) / per;
     q.prob[p].unit0 = units;
     units += ((q.prob[p].m + G_TILE_M - 1) / G_TILE_M) * q.prob[p].n_tiles;
   }
   q.n_units = units;
-  const cudaError_t e = cudaFuncSetAttribute(k_ffn_gemm<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, G_SMEM_BYTES);
+  cudaError_t e = allow_smem<k_ffn_gemm<MODE>>(G_SMEM_BYTES);
   if (e != cudaSuccess) return e;
   const int pairs = units < n_pairs ? units : n_pairs;
-  k_ffn_gemm<MODE><<<2 * pairs, G_THREADS, G_SMEM_BYTES, st>>>(q);
-  return cudaGetLastError();
+  return launch_chained(k_ffn_gemm<MODE>, q, 2 * pairs, 1, 1, G_THREADS, G_SMEM_BYTES, !first, st);
 }
 
-int sm_pairs() {
-  int dev = 0, sms = 148;
-  cudaGetDevice(&dev);
-  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  return sms / 2;
+int sm_count() {                     // of the process's GPUs, which are all alike
+  static std::atomic<int> known;
+  int sms = known.load(std::memory_order_relaxed);
+  if (sms == 0) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+      cudaGetLastError();
+      return 148;
+    }
+    known.store(sms, std::memory_order_relaxed);
+  }
+  return sms;
 }
 
 constexpr int FEW_TOKENS = 32;     // up to here the streaming kernels
@@ -672,9 +731,11 @@ extern "C" int camera_ffn_forward(const camera_ffn_t* f, const void* x, int64_t 
     FFN_CK((launch_few<false, 1>(w, st)));
     return CAMERA_OK;
   }
-  FFN_CK(cudaMemsetAsync(ws, 0, sizeof(PlanTotals), st));
-  if (n_tokens == 0) return CAMERA_OK;
-  const int n_pairs = sm_pairs();
+  if (n_tokens == 0) {
+    FFN_CK(cudaMemsetAsync(ws, 0, sizeof(PlanTotals), st));
+    return CAMERA_OK;
+  }
+  const int n_pairs = sm_count() / 2;
   const long long m_tiles = (s.T + G_TILE_M - 1) / G_TILE_M;
   FfnGemm q;
   memset(&q, 0, sizeof(q));
@@ -689,16 +750,16 @@ extern "C" int camera_ffn_forward(const camera_ffn_t* f, const void* x, int64_t 
   q.n_prob = 1;
   q.prob[0] = FfnProblem{(int)s.T, s.F, 0, 0, nullptr, 0, 0};
   q.n_kb = (s.D + UMMA_BK - 1) / UMMA_BK;
-  int bn = choose_bn(m_tiles, s.F, true, 32, n_pairs);
-  if (!enc(&q.a[0], x, s.T, s.D, s.D, 128) || !enc(&q.b[0], f->w_gate, s.F, s.D, s.D, bn / 2) ||
-      !enc(&q.b[1], f->w_up, s.F, s.D, s.D, bn / 2))
+  Tile t = choose_tile(m_tiles, s.F, true, 32, q.n_kb, n_pairs);
+  if (!enc(&q.a[0], x, s.T, s.D, s.D, 128) || !enc(&q.b[0], f->w_gate, s.F, s.D, s.D, t.bn / 2) ||
+      !enc(&q.b[1], f->w_up, s.F, s.D, s.D, t.bn / 2))
     return CAMERA_ERR_CUDA;
-  FFN_CK(launch_gemm<FFN_GATE_UP>(q, bn, n_pairs, st));
+  FFN_CK(launch_gemm<FFN_GATE_UP>(q, t, n_pairs, true, st));
   q.prob[0] = FfnProblem{(int)s.T, s.D, 0, 0, static_cast<__nv_bfloat16*>(y), s.D, wide_rows(y, s.D)};
   q.n_kb = (s.F + UMMA_BK - 1) / UMMA_BK;
-  bn = choose_bn(m_tiles, s.D, false, 32, n_pairs);
-  if (!enc(&q.a[0], q.h, s.T, s.F, s.fp, 128) || !enc(&q.b[0], f->w_down, s.D, s.F, s.ld, bn / 2)) return CAMERA_ERR_CUDA;
-  FFN_CK(launch_gemm<FFN_DOWN>(q, bn, n_pairs, st));
+  t = choose_tile(m_tiles, s.D, false, 32, q.n_kb, n_pairs);
+  if (!enc(&q.a[0], q.h, s.T, s.F, s.fp, 128) || !enc(&q.b[0], f->w_down, s.D, s.F, s.ld, t.bn / 2)) return CAMERA_ERR_CUDA;
+  FFN_CK(launch_gemm<FFN_DOWN>(q, t, n_pairs, false, st));
   return CAMERA_OK;
 }
 
@@ -720,8 +781,8 @@ extern "C" int camera_ffn_backward(const camera_ffn_t* f, const void* x, const v
     return CAMERA_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   char* const ws = static_cast<char*>(workspace);
-  FFN_CK(cudaMemsetAsync(ws, 0, sizeof(PlanTotals), st));
   if (n_tokens == 0) {                          // sums over no token
+    FFN_CK(cudaMemsetAsync(ws, 0, sizeof(PlanTotals), st));
     if (weights) {
       FFN_CK(cudaMemsetAsync(dw_gate, 0, (size_t)2 * s.F * s.D, st));
       FFN_CK(cudaMemsetAsync(dw_up, 0, (size_t)2 * s.F * s.D, st));
@@ -729,7 +790,7 @@ extern "C" int camera_ffn_backward(const camera_ffn_t* f, const void* x, const v
     }
     return CAMERA_OK;
   }
-  const int n_pairs = sm_pairs();
+  const int n_pairs = sm_count() / 2;
   const long long m_tiles = (s.T + G_TILE_M - 1) / G_TILE_M;
   FfnGemm q;
   memset(&q, 0, sizeof(q));
@@ -747,17 +808,17 @@ extern "C" int camera_ffn_backward(const camera_ffn_t* f, const void* x, const v
   q.n_prob = 1;
   q.prob[0] = FfnProblem{(int)s.T, s.F, 0, 0, nullptr, 0, 0};
   q.n_kb = (s.D + UMMA_BK - 1) / UMMA_BK;
-  int bn = choose_bn(m_tiles, s.F, false, 128, n_pairs);
+  Tile t = choose_tile(m_tiles, s.F, false, 128, q.n_kb, n_pairs);
   if (!enc(&q.a[0], dy, s.T, s.D, s.D, 128) || !enc(&q.b[0], f->w_down, s.D, s.F, s.ld, 64)) return CAMERA_ERR_CUDA;
-  FFN_CK(launch_gemm<FFN_DH>(q, bn, n_pairs, st));
+  FFN_CK(launch_gemm<FFN_DH>(q, t, n_pairs, true, st));
   if (dx != nullptr) {
     q.prob[0] = FfnProblem{(int)s.T, s.D, 0, 0, static_cast<__nv_bfloat16*>(dx), s.D, wide_rows(dx, s.D)};
     q.n_kb = (s.F + UMMA_BK - 1) / UMMA_BK;
-    bn = choose_bn(m_tiles, s.D, false, 128, n_pairs);
+    t = choose_tile(m_tiles, s.D, false, 128, 2 * q.n_kb, n_pairs);
     if (!enc(&q.a[0], q.dg, s.T, s.F, q.act_ld, 128) || !enc(&q.a[1], q.du, s.T, s.F, q.act_ld, 128) ||
         !enc(&q.b[0], f->w_gate, s.F, s.D, s.D, 64) || !enc(&q.b[1], f->w_up, s.F, s.D, s.D, 64))
       return CAMERA_ERR_CUDA;
-    FFN_CK(launch_gemm<FFN_DX>(q, bn, n_pairs, st));
+    FFN_CK(launch_gemm<FFN_DX>(q, t, n_pairs, false, st));
   }
   if (weights) {
     q.n_prob = 3;
@@ -766,12 +827,12 @@ extern "C" int camera_ffn_backward(const camera_ffn_t* f, const void* x, const v
     q.prob[2] = FfnProblem{s.D, s.F, 0, 0, static_cast<__nv_bfloat16*>(dw_down), s.ld, wide_rows(dw_down, s.ld)};
     q.n_kb = (int)((s.T + UMMA_BK - 1) / UMMA_BK);
     // the third problem has as many tiles as either of the others, up to their edges
-    bn = choose_bn(3ll * ((s.F + G_TILE_M - 1) / G_TILE_M), s.D, false, 128, n_pairs);
+    t = choose_tile(3ll * ((s.F + G_TILE_M - 1) / G_TILE_M), s.D, false, 128, q.n_kb, n_pairs);
     if (!enc(&q.a[0], q.dg, s.T, s.F, q.act_ld, 64) || !enc(&q.a[1], q.du, s.T, s.F, q.act_ld, 64) ||
         !enc(&q.a[2], dy, s.T, s.D, s.D, 64) || !enc(&q.b[0], x, s.T, s.D, s.D, 64) || !enc(&q.b[2], q.h, s.T, s.F, s.fp, 64))
       return CAMERA_ERR_CUDA;
     q.b[1] = q.b[0];
-    FFN_CK(launch_gemm<FFN_DW>(q, bn, n_pairs, st));
+    FFN_CK(launch_gemm<FFN_DW>(q, t, n_pairs, false, st));
   }
   return CAMERA_OK;
 }
