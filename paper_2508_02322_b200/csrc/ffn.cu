@@ -49,6 +49,7 @@ struct FfnGemm {
   FfnProblem prob[3];
   int n_prob, n_units;
   int n_kb;                 // k blocks per segment
+  int kps;                  // k blocks per stage of the ring (1 or 2)
   int bn, nb;               // columns per B tile; B tiles per work unit (GATE_UP: 2, one of each matrix)
   int n_stages, n_acc;      // ring depth; accumulator sets in tensor memory
   uint16_t *g, *u;          // GATE_UP: where to keep G and U (or null); DH: inputs.  Upper halves of the 24 bits kept,
@@ -92,6 +93,57 @@ __device__ __forceinline__ unsigned long long make_smem_desc_mn(uint32_t addr) {
   d |= (unsigned long long)1 << 46;
   d |= (unsigned long long)2 << 61;
   return d;
+}
+
+// The producer and the issuer are whole warps that walk their loops together and let one lane (`lead`) issue: TMA and
+// tcgen05 instructions take their operands from the warp's uniform registers, and in a branch of one lane the compiler has
+// to move every operand there first (about 100 cycles an MMA).
+__device__ __forceinline__ void tma_load_lead(uint32_t lead, uint32_t dst, const void* tmap, uint32_t bar_cluster_addr, int x, int y) {
+  asm volatile(
+      "{\n"
+      ".reg .pred q;\n"
+      "setp.ne.b32 q, %5, 0;\n"
+      "@q cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n"
+      "}\n" ::"r"(dst), "l"(tmap), "r"(bar_cluster_addr), "r"(x), "r"(y), "r"(lead)
+      : "memory");
+}
+__device__ __forceinline__ void umma_lead(uint32_t lead, uint32_t d_tmem, unsigned long long a, unsigned long long b, uint32_t idesc,
+                                          uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      "setp.ne.b32 p, %4, 0;\n"
+      "setp.ne.b32 q, %5, 0;\n"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n"
+      "}\n" ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(lead)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit_lead(uint32_t lead, uint32_t bar) {
+  const uint16_t mask = 3;
+  asm volatile(
+      "{\n"
+      ".reg .pred q;\n"
+      "setp.ne.b32 q, %2, 0;\n"
+      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n"
+      "}\n" ::"r"(bar), "h"(mask), "r"(lead)
+      : "memory");
+}
+// Whether the phase has ended, without waiting (try_wait may suspend the thread for a while).
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+      "selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
@@ -148,12 +200,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
   volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(tail + 8);
 
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const uint32_t rank = cluster_ctarank();
   const int n_pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
   const int half = q.bn >> 1;                               // columns of a B tile this CTA supplies
   const int b_bytes = half * 128;
-  const int stage_bytes = G_A_BYTES + q.nb * b_bytes;
+  const int block_bytes = G_A_BYTES + q.nb * b_bytes;      // operands of one k block
+  const int stage_bytes = q.kps * block_bytes;
 
   if (tid == 0) {
     for (int s = 0; s < q.n_stages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
@@ -183,80 +236,102 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
 
   if (warp == 4) {
     // ------------------------------------------------------------------ TMA producer (each CTA loads its own share)
-    if (lane == 0) {
-      int stage = 0;
-      uint32_t phase = 0;
-      bool ok = true;
-      for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
-        const FfnUnit u = decode(q, unit, DUAL);
-        const int am = u.m0 + 128 * (int)rank, bn0 = u.n0 + half * (int)rank;
-        for (int seg = 0; ok && seg < SEGMENTS; ++seg) {
-          const CUtensorMap* const map_a = &q.a[MODE == FFN_DX ? seg : u.p];
-          const CUtensorMap* const map_b = &q.b[MODE == FFN_DX ? seg : u.p];
-          const CUtensorMap* const map_b2 = DUAL ? &q.b[1] : map_b;
-          const int bn1 = DUAL ? bn0 : bn0 + q.bn;
-          for (int kb = 0; kb < q.n_kb; ++kb) {
-            if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) { ok = false; break; }
-            const uint32_t dst = base + stage * stage_bytes;
-            const uint32_t full0 = map_to_cta(full_bar(stage), 0);
-            const int k0 = kb * UMMA_BK;
-            if (rank == 0) mbar_expect_tx(full_bar(stage), 2 * (G_A_BYTES + (u.two ? 2 : 1) * b_bytes));
+    const uint32_t lead = lane == 0;
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
+      const FfnUnit u = decode(q, unit, DUAL);
+      const int am = u.m0 + 128 * (int)rank, bn0 = u.n0 + half * (int)rank;
+      for (int seg = 0; ok && seg < SEGMENTS; ++seg) {
+        const CUtensorMap* const map_a = &q.a[MODE == FFN_DX ? seg : u.p];
+        const CUtensorMap* const map_b = &q.b[MODE == FFN_DX ? seg : u.p];
+        const CUtensorMap* const map_b2 = DUAL ? &q.b[1] : map_b;
+        const int bn1 = DUAL ? bn0 : bn0 + q.bn;
+        for (int kb = 0; kb < q.n_kb; kb += q.kps) {
+          ok = warp_wait(empty_bar(stage), phase ^ 1u, abort_flag);
+          if (!ok) break;
+          const uint32_t full0 = map_to_cta(full_bar(stage), 0);
+          const int blocks = min(q.kps, q.n_kb - kb);
+          if (rank == 0 && lane == 0) mbar_expect_tx(full_bar(stage), 2 * blocks * (G_A_BYTES + (u.two ? 2 : 1) * b_bytes));
+          __syncwarp();
+          uint32_t dst = base + stage * stage_bytes;
+          for (int k0 = kb * UMMA_BK; k0 < (kb + blocks) * UMMA_BK; k0 += UMMA_BK, dst += block_bytes) {
             // whatever lies past a matrix's last row or column arrives as zeros
             if (A_MN) {
-              tma_load_2d_pair(dst, map_a, full0, am, k0);
-              tma_load_2d_pair(dst + 8192, map_a, full0, am + 64, k0);
+              tma_load_lead(lead, dst, map_a, full0, am, k0);
+              tma_load_lead(lead, dst + 8192, map_a, full0, am + 64, k0);
             } else {
-              tma_load_2d_pair(dst, map_a, full0, k0, am);
+              tma_load_lead(lead, dst, map_a, full0, k0, am);
             }
             const uint32_t dst_b = dst + G_A_BYTES;
             if (B_MN) {
-              for (int j = 0; j < half; j += 64) tma_load_2d_pair(dst_b + j * 128, map_b, full0, bn0 + j, k0);
-              if (u.two)
-                for (int j = 0; j < half; j += 64) tma_load_2d_pair(dst_b + b_bytes + j * 128, map_b2, full0, bn1 + j, k0);
+              tma_load_lead(lead, dst_b, map_b, full0, bn0, k0);
+              if (half > 64) tma_load_lead(lead, dst_b + 8192, map_b, full0, bn0 + 64, k0);
+              if (u.two) {
+                tma_load_lead(lead, dst_b + b_bytes, map_b2, full0, bn1, k0);
+                if (half > 64) tma_load_lead(lead, dst_b + b_bytes + 8192, map_b2, full0, bn1 + 64, k0);
+              }
             } else {
-              tma_load_2d_pair(dst_b, map_b, full0, k0, bn0);
-              if (u.two) tma_load_2d_pair(dst_b + b_bytes, map_b2, full0, k0, bn1);
+              tma_load_lead(lead, dst_b, map_b, full0, k0, bn0);
+              if (u.two) tma_load_lead(lead, dst_b + b_bytes, map_b2, full0, k0, bn1);
             }
-            if (++stage == q.n_stages) { stage = 0; phase ^= 1u; }
           }
+          if (++stage == q.n_stages) { stage = 0; phase ^= 1u; }
         }
       }
-      if (!ok) {             // copies in flight land before the CTA's shared memory is given up
-        const unsigned long long t0 = globaltimer_ns();
-        while (globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
-      }
+    }
+    if (!ok) {               // copies in flight land before the CTA's shared memory is given up
+      const unsigned long long t0 = globaltimer_ns();
+      while (globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
     }
   } else if (warp == 5) {
     // ------------------------------------------------------------------ MMA issuer (first CTA of the pair only)
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
+      const uint32_t lead = lane == 0;
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0;
-      bool ok = true;
+      bool ok = true, ready = false;       // ready: the next stage has been seen full
       const uint32_t idesc = make_idesc_pair(q.bn) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
       constexpr unsigned long long A_STEP = A_MN ? 2048 >> 4 : 32 >> 4, B_STEP = B_MN ? 2048 >> 4 : 32 >> 4;
+      constexpr int STEPS = UMMA_BK / 16;
+      const unsigned long long a_first = A_MN ? make_smem_desc_mn(base) : make_smem_desc(base);
+      const unsigned long long b_first = B_MN ? make_smem_desc_mn(base + G_A_BYTES) : make_smem_desc(base + G_A_BYTES);
+      const unsigned long long b2_off = (unsigned long long)(b_bytes >> 4);
       for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
         const FfnUnit u = decode(q, unit, DUAL);
-        if (!mbar_wait_cluster(tempty_bar(acc), acc_phase ^ 1u, abort_flag)) { ok = false; break; }
+        ok = __all_sync(0xffffffffu, mbar_wait_cluster(tempty_bar(acc), acc_phase ^ 1u, abort_flag));
+        if (!ok) break;
         tc_fence_after();
         const uint32_t d0 = tmem_base + (uint32_t)(acc * q.nb * q.bn), d1 = d0 + (uint32_t)q.bn;
-        for (int kb = 0; kb < SEGMENTS * q.n_kb; ++kb) {
-          if (!mbar_wait(full_bar(stage), phase, abort_flag)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t a_addr = base + stage * stage_bytes;
-          const unsigned long long a_desc = A_MN ? make_smem_desc_mn(a_addr) : make_smem_desc(a_addr);
-          const unsigned long long b_desc = B_MN ? make_smem_desc_mn(a_addr + G_A_BYTES) : make_smem_desc(a_addr + G_A_BYTES);
-          const unsigned long long b2_desc = b_desc + (unsigned long long)(b_bytes >> 4);
+        const uint32_t lead2 = u.two ? lead : 0u;
+        uint32_t accumulate = 0;
+        for (int seg = 0; ok && seg < SEGMENTS; ++seg) {
+          for (int kb = 0; kb < q.n_kb; kb += q.kps) {
+            if (!ready) {
+              ok = warp_wait(full_bar(stage), phase, abort_flag);
+              if (!ok) break;
+            }
+            tc_fence_after();
+            unsigned long long at = (unsigned long long)((uint32_t)(stage * stage_bytes) >> 4);
+            const uint32_t done = empty_bar(stage);
+            if (++stage == q.n_stages) { stage = 0; phase ^= 1u; }
+            for (int block = min(q.kps, q.n_kb - kb); block > 0; --block, at += (unsigned long long)(block_bytes >> 4)) {
+              const unsigned long long a_desc = a_first + at, b_desc = b_first + at, b2_desc = b_desc + b2_off;
 #pragma unroll
-          for (int k = 0; k < UMMA_BK / 16; ++k) {
-            const uint32_t accumulate = (uint32_t)((kb | k) != 0);
-            umma_bf16_pair(d0, a_desc + A_STEP * k, b_desc + B_STEP * k, idesc, accumulate);
-            if (u.two) umma_bf16_pair(d1, a_desc + A_STEP * k, b2_desc + B_STEP * k, idesc, accumulate);
+              for (int k = 0; k < STEPS; ++k) {
+                umma_lead(lead, d0, a_desc + A_STEP * k, b_desc + B_STEP * k, idesc, accumulate);
+                umma_lead(lead2, d1, a_desc + A_STEP * k, b2_desc + B_STEP * k, idesc, accumulate);
+                accumulate = 1;
+              }
+            }
+            // The tensor pipe holds only a few MMAs: a look at the next stage's barrier while they run.
+            ready = __all_sync(0xffffffffu, mbar_test(full_bar(stage), phase));
+            umma_commit_lead(lead, done);
           }
-          umma_commit_pair(empty_bar(stage));
-          if (++stage == q.n_stages) { stage = 0; phase ^= 1u; }
         }
         if (!ok) break;
-        umma_commit_pair(tfull_bar(acc));
+        umma_commit_lead(lead, tfull_bar(acc));
         if (++acc == q.n_acc) { acc = 0; acc_phase ^= 1u; }
       }
     }
@@ -625,7 +700,11 @@ cudaError_t launch_gemm(FfnGemm& q, Tile t, int n_pairs, bool first, cudaStream_
   q.bn = t.bn; q.nb = t.nb;
   q.clear_status = first;
   q.n_acc = t.nb * t.bn <= 256 ? 2 : 1;
-  const int stage = G_A_BYTES + t.nb * t.bn * 64;
+  // A stage costs the issuing thread about 400 cycles beside the MMAs of its k blocks (wait, fence, commit), and a k block
+  // of up to 256 columns 409 to 512 cycles of the tensor pipe, which holds too few MMAs to bridge that: such tiles get
+  // two k blocks per stage (256 x 128 tile, K 4096, one unit per pair: 0.42 -> 0.31 us per k block).
+  q.kps = t.nb * t.bn <= 256 ? 2 : 1;
+  const int stage = q.kps * (G_A_BYTES + t.nb * t.bn * 64);
   q.n_stages = G_RING_BYTES / stage < G_MAX_STAGES ? G_RING_BYTES / stage : G_MAX_STAGES;
   int units = 0;
   for (int p = 0; p < q.n_prob; ++p) {
