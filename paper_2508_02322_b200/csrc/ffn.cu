@@ -449,14 +449,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
 
 // ------------------------------------------------------------------------------------------------ few tokens
 // Up to 8 * NT tokens: the work is reading the weights once.  A tensor-core tile of 256 rows would be mostly padding and
-// its column tiles too few to keep every SM's loads in flight, so these kernels stream the weights from global memory
-// straight into the A fragments of mma.sync (m16n8k16): a lane loads 16 bytes = 8 consecutive k of its row, which is the
-// lane's share of two MMAs once the k index is permuted the same way in both operands; no shared memory, no barriers in
-// the loop.  The tokens are the n index; their fragments come the same way from x or h (small, L1 and L2 hits).
-// A CTA owns R tiles of 16 weight rows and splits k over its 8 warps; the partial sums meet in shared memory in a fixed
-// order.  GATE_UP tiles are 8 rows of Wg over the same 8 rows of Wu: a thread then holds gate and up of one element.
+// its column tiles too few to keep every SM's loads in flight, so these kernels stream the weights into the A fragments of
+// mma.sync (m16n8k16).  A lane takes 16 bytes = 8 consecutive k of its row, which is its share of two MMAs once the k
+// index is permuted the same way in both operands; it copies them itself (cp.async) into its own places of a ring in
+// shared memory, so a warp waits for nothing but its own copies.  The tokens are the n index; their fragments come the
+// same way from x or h, through L1.
+// The 8 warps of a CTA lie WK along k and 8 / WK along the rows, a warp has R tiles of 16 rows: at a step the CTA reads
+// 128 WK contiguous bytes of each of its 16 R 8 / WK rows (DRAM wants runs), and its warps read the tokens' fragments
+// 8 / WK times.  GATE_UP tiles are 8 rows of Wg over the same 8 rows of Wu, so that a thread ends with gate and up of one
+// element.  Where that gives too few CTAs to fill the GPU, k is split further over the CTAs of a cluster (up to 8).  The
+// sums of the warps and CTAs along k meet through (distributed) shared memory in a fixed order.
+// Bound by the weights' bytes; one token through 2560 micro-experts of d_model 3584 also by two kernels' start and end.
 constexpr int S_WARPS = 8;
 constexpr int S_THREADS = 32 * S_WARPS;
+constexpr int S_STEP_BYTES = S_THREADS * 64;       // a step of one tile per warp
 
 struct FfnFew {
   const __nv_bfloat16 *w0, *w1;    // GATE_UP: Wg, Wu; DOWN: Wd in both
@@ -469,11 +475,6 @@ struct FfnFew {
   PlanTotals* totals;
 };
 
-__device__ __forceinline__ uint4 ld_weights(const void* p) {      // read once: past L1
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
 __device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -486,26 +487,101 @@ __device__ __forceinline__ uint4 first_n(uint4 v, int n) {
   for (int i = 0; i < 4; ++i) w[i] &= (2 * i < n ? 0xffffu : 0u) | (2 * i + 1 < n ? 0xffff0000u : 0u);
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
+__device__ __forceinline__ float ld_cluster_f32(uint32_t cluster_addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  __syncthreads();
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
 
-template <bool GATE_UP, int R, int NT>
-__global__ void __launch_bounds__(S_THREADS) k_ffn_few(const FfnFew q) {
-  constexpr int UNROLL = R == 1 ? 4 : R == 2 ? 2 : 1;      // steps of 64 k whose loads are issued together
-  constexpr int VALS = R * NT * 4;
-  extern __shared__ float part[];                           // [S_WARPS][VALS][32]
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, tg = lane & 3;
-  const int row0 = blockIdx.x * (GATE_UP ? 8 : 16) * R;
-  if (blockIdx.x == 0 && threadIdx.x == 0 && q.totals != nullptr) q.totals->status = 0;    // nothing here can fail
-  // rows of this lane: tile r, halves 0 / 1
+// One element's results: gate and up of (token, micro-expert), or one (GATE_UP false: lo) or two rows of y.
+template <bool GATE_UP>
+__device__ __forceinline__ void few_store(const FfnFew& q, int row, int tok, float lo, float hi) {
+  if (tok >= q.T) return;
+  if (GATE_UP) {
+    if (row >= q.rows) return;
+    q.out[(size_t)tok * q.out_ld + row] = __float2bfloat16_rn(lo * sigmoid(lo) * hi);
+    if (q.g != nullptr) {
+      const size_t ga = (size_t)tok * q.act_ld + row, ua = ga + q.u_off;
+      uint8_t* const low = reinterpret_cast<uint8_t*>(q.g) + q.lo_off;
+      const uint32_t gb = __float_as_uint(lo), ub = __float_as_uint(hi);
+      q.g[ga] = (uint16_t)(gb >> 16); low[ga] = (uint8_t)(gb >> 8);
+      q.g[ua] = (uint16_t)(ub >> 16); low[ua] = (uint8_t)(ub >> 8);
+    }
+  } else {
+    if (row < q.rows) q.out[(size_t)tok * q.out_ld + row] = __float2bfloat16_rn(lo);
+    if (row + 8 < q.rows) q.out[(size_t)tok * q.out_ld + row + 8] = __float2bfloat16_rn(hi);
+  }
+}
+
+// SLOTS: steps in the ring.  AHEAD: the tokens' fragments of a step are loaded during the step before.
+template <bool GATE_UP, int WK, int R, int NT, int SLOTS, int CTAS>
+__global__ void __launch_bounds__(S_THREADS, CTAS) k_ffn_few(const FfnFew q) {
+  constexpr bool AHEAD = NT <= 4;
+  extern __shared__ __align__(16) uint8_t few_ring[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, tg = lane & 3;
+  const int splits = gridDim.y, split = blockIdx.y;
+  constexpr int TILE = GATE_UP ? 8 : 16;                    // rows of the result per tile
+  constexpr int TILES = S_WARPS / WK * R, KSTEP = 64 * WK;  // tiles of the CTA; k of a step
+  const int warp_k = warp % WK, warp_r = warp / WK;
+  const int row0 = (blockIdx.x * TILES + warp_r * R) * TILE;
+  if (GATE_UP) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (blockIdx.x == 0 && split == 0 && tid == 0) q.totals->status = 0;       // nothing here can fail
+  }
+  const int steps = (q.k + KSTEP - 1) / KSTEP;
+  const int s0 = steps * split / splits, s1 = steps * (split + 1) / splits;
+  // this lane's two weight rows of each tile; a row past the last one, and k past the end, are filled with zeros
   const __nv_bfloat16* w[R][2];
-  bool has[R][2];
+  uint32_t has = 0;
 #pragma unroll
   for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int row = GATE_UP ? row0 + 8 * r + g : row0 + 16 * r + 8 * e + g;
-      has[r][e] = row < q.rows;
-      w[r][e] = (GATE_UP && e ? q.w1 : q.w0) + (size_t)row * q.w_ld;
+      const int row = row0 + r * TILE + g + (GATE_UP ? 0 : 8 * e);
+      if (row < q.rows) has |= 1u << (2 * r + e);
+      w[r][e] = (e ? q.w1 : q.w0) + (row < q.rows ? (size_t)row * q.w_ld : 0) + tg * 8;
     }
+  const uint32_t mine = smem_u32(few_ring) + tid * 16;
+  auto issue = [&](int s) {
+    if (s < s1) {
+      const uint32_t dst = mine + (uint32_t)((s - s0) % SLOTS) * (R * S_STEP_BYTES);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int k = s * KSTEP + warp_k * 64 + j * 32, bytes = min(16, max(0, 2 * (q.k - k - tg * 8)));
+        const int at = bytes > 0 ? k : 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + (uint32_t)((2 * r + e) * 2 + j) * S_THREADS * 16),
+                         "l"(w[r][e] + at), "r"((has >> (2 * r + e)) & 1u ? bytes : 0)
+                         : "memory");
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < SLOTS; ++i) issue(s0 + i);
+  if (!GATE_UP) asm volatile("griddepcontrol.wait;" ::: "memory");     // the weights are on their way; h is the kernel before's
+
+  const __nv_bfloat16* const in = q.in + (size_t)g * q.in_ld + warp_k * 64 + tg * 8;
+  auto load_tokens = [&](int s, uint4 (*b)[2]) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int k = s * KSTEP + warp_k * 64 + j * 32 + tg * 8;
+        b[n][j] = make_uint4(0, 0, 0, 0);
+        if (s < s1 && 8 * n + g < q.T && k < q.k)
+          b[n][j] = *reinterpret_cast<const uint4*>(in + (size_t)(8 * n) * q.in_ld + s * KSTEP + j * 32);
+        if (!GATE_UP && k + 8 > q.k) b[n][j] = first_n(b[n][j], q.k - k);
+      }
+  };
   float acc[R][NT][4];
 #pragma unroll
   for (int r = 0; r < R; ++r)
@@ -513,86 +589,72 @@ __global__ void __launch_bounds__(S_THREADS) k_ffn_few(const FfnFew q) {
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[r][n][i] = 0.f;
-
-  const int steps = (q.k + 63) / 64;
-  const int s0 = steps * warp / S_WARPS, s1 = steps * (warp + 1) / S_WARPS;
-  const uint4 zero = make_uint4(0, 0, 0, 0);
-  for (int s = s0; s < s1; s += UNROLL) {
-    uint4 a[UNROLL][R][2][2];
+  uint4 b[NT][2], next[AHEAD ? NT : 1][2];
+  if (AHEAD) load_tokens(s0, b);
+  for (int s = s0; s < s1; ++s) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(SLOTS - 1) : "memory");
+    const uint8_t* const at = few_ring + ((s - s0) % SLOTS) * (R * S_STEP_BYTES) + tid * 16;
+    if constexpr (AHEAD) load_tokens(s + 1, next); else load_tokens(s, b);
 #pragma unroll
-    for (int t = 0; t < UNROLL; ++t)
+    for (int r = 0; r < R; ++r) {
+      uint4 a[2][2];
 #pragma unroll
-      for (int r = 0; r < R; ++r)
+      for (int e = 0; e < 2; ++e)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int j = 0; j < 2; ++j) a[e][j] = *reinterpret_cast<const uint4*>(at + ((2 * r + e) * 2 + j) * S_THREADS * 16);
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int k = (s + t) * 64 + j * 32 + tg * 8;
-            a[t][r][e][j] = has[r][e] && s + t < s1 && k < q.k ? ld_weights(w[r][e] + k) : zero;
-          }
-#pragma unroll
-    for (int t = 0; t < UNROLL; ++t) {
-      if (s + t >= s1) break;
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int k = (s + t) * 64 + j * 32 + tg * 8;
-        if (!GATE_UP && k + 8 > q.k) {
-#pragma unroll
-          for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) a[t][r][e][j] = first_n(a[t][r][e][j], q.k - k);
-        }
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const int tok = 8 * n + g;
-          uint4 b = zero;
-          if (tok < q.T && k < q.k) b = *reinterpret_cast<const uint4*>(q.in + (size_t)tok * q.in_ld + k);
-          if (!GATE_UP && k + 8 > q.k) b = first_n(b, q.k - k);
-#pragma unroll
-          for (int r = 0; r < R; ++r) {
-            const uint4 a0 = a[t][r][0][j], a1 = a[t][r][1][j];
-            mma16816(acc[r][n], a0.x, a1.x, a0.y, a1.y, b.x, b.y);
-            mma16816(acc[r][n], a0.z, a1.z, a0.w, a1.w, b.z, b.w);
-          }
+          mma16816(acc[r][n], a[0][j].x, a[1][j].x, a[0][j].y, a[1][j].y, b[n][j].x, b[n][j].y);
+          mma16816(acc[r][n], a[0][j].z, a[1][j].z, a[0][j].w, a[1][j].w, b[n][j].z, b[n][j].w);
         }
-      }
+    }
+    issue(s + SLOTS);
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) { b[n][0] = next[n][0]; b[n][1] = next[n][1]; }
     }
   }
+  // acc[r][n][i]: weight row g (i < 2) or g + 8 of the warp's tile r, token 8 n + 2 tg + i % 2
+  if (WK == 1 && splits == 1) {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          few_store<GATE_UP>(q, row0 + r * TILE + g, 8 * n + 2 * tg + i, acc[r][n][i], acc[r][n][2 + i]);
+    return;
+  }
+  // every warp leaves its sums in its CTA's shared memory (the ring is empty by now); the CTAs of a cluster share the
+  // adding up
+  __syncthreads();
+  float* const part = reinterpret_cast<float*>(few_ring);
 #pragma unroll
   for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) part[(warp * VALS + (r * NT + n) * 4 + i) * 32 + lane] = acc[r][n][i];
-  __syncthreads();
-  // element (r, n, i) of lane l: weight row g (i < 2) or g + 8 of tile r, token 8 n + 2 (l % 4) + i % 2
-  for (int at = threadIdx.x; at < R * NT * 2 * 32; at += S_THREADS) {
-    const int l = at & 31, i = (at >> 5) & 1, rn = at >> 6;
+      for (int i = 0; i < 4; ++i) part[(((warp_k * TILES + warp_r * R + r) * NT + n) * 4 + i) * 32 + lane] = acc[r][n][i];
+  if (splits > 1) cluster_barrier(); else __syncthreads();
+  const int share = TILES * NT * 2 * 32 / splits;
+  for (int p = split * share + tid; p < (split + 1) * share; p += S_THREADS) {
+    const int l = p & 31, i = (p >> 5) & 1, n = (p >> 6) % NT, t = (p >> 6) / NT;
+    const float* const src = part + ((t * NT + n) * 4 + i) * 32 + l;
     float lo = 0.f, hi = 0.f;
+    for (int c = 0; c < splits; ++c) {
+      const uint32_t from = map_to_cta(smem_u32(src), (uint32_t)c);
 #pragma unroll
-    for (int v = 0; v < S_WARPS; ++v) {
-      lo += part[(v * VALS + rn * 4 + i) * 32 + l];
-      hi += part[(v * VALS + rn * 4 + 2 + i) * 32 + l];
-    }
-    const int r = rn / NT, tok = 8 * (rn % NT) + 2 * (l & 3) + i;
-    if (tok >= q.T) continue;
-    if (GATE_UP) {
-      const int f = row0 + 8 * r + (l >> 2);
-      if (f >= q.rows) continue;
-      q.out[(size_t)tok * q.out_ld + f] = __float2bfloat16_rn(lo * sigmoid(lo) * hi);
-      if (q.g != nullptr) {
-        const size_t ga = (size_t)tok * q.act_ld + f, ua = ga + q.u_off;
-        uint8_t* const low = reinterpret_cast<uint8_t*>(q.g) + q.lo_off;
-        const uint32_t gb = __float_as_uint(lo), ub = __float_as_uint(hi);
-        q.g[ga] = (uint16_t)(gb >> 16); low[ga] = (uint8_t)(gb >> 8);
-        q.g[ua] = (uint16_t)(ub >> 16); low[ua] = (uint8_t)(ub >> 8);
+      for (int k = 0; k < WK; ++k) {
+        const int off = k * TILES * NT * 4 * 32;
+        lo += splits > 1 ? ld_cluster_f32(from + 4 * off) : src[off];
+        hi += splits > 1 ? ld_cluster_f32(from + 4 * (off + 2 * 32)) : src[off + 2 * 32];
       }
-    } else {
-      const int d = row0 + 16 * r + (l >> 2);
-      if (d < q.rows) q.out[(size_t)tok * q.out_ld + d] = __float2bfloat16_rn(lo);
-      if (d + 8 < q.rows) q.out[(size_t)tok * q.out_ld + d + 8] = __float2bfloat16_rn(hi);
     }
+    few_store<GATE_UP>(q, (blockIdx.x * TILES + t) * TILE + (l >> 2), 8 * n + 2 * (l & 3) + i, lo, hi);
   }
+  if (splits > 1) cluster_barrier();        // nobody leaves while its sums are read
 }
 
 // ------------------------------------------------------------------------------------------------ host side
@@ -734,26 +796,29 @@ int sm_count() {                     // of the process's GPUs, which are all ali
   return sms;
 }
 
-constexpr int FEW_TOKENS = 32;     // up to here the streaming kernels
+constexpr int FEW_TOKENS = 64;     // up to here the streaming kernels
 
-template <bool GATE_UP, int R>
+template <bool GATE_UP, int WK, int R, int NT, int SLOTS, int CTAS>
+cudaError_t launch_few_as(const FfnFew& q, cudaStream_t st) {
+  constexpr int SMEM = SLOTS * R * S_STEP_BYTES, ROWS = (GATE_UP ? 8 : 16) * S_WARPS / WK * R;
+  static_assert(SMEM >= S_WARPS * R * NT * 4 * 32 * 4, "the warps' sums take the ring's room");
+  const cudaError_t e = allow_smem<k_ffn_few<GATE_UP, WK, R, NT, SLOTS, CTAS>>(SMEM);
+  if (e != cudaSuccess) return e;
+  const int row_ctas = (q.rows + ROWS - 1) / ROWS, steps = (q.k + 64 * WK - 1) / (64 * WK);
+  // split k over a cluster until there is a CTA per SM or a CTA has fewer steps than its ring
+  int splits = 1;
+  while (splits < 8 && row_ctas * splits < sm_count() && steps >= splits * SLOTS) splits *= 2;
+  return launch_chained(k_ffn_few<GATE_UP, WK, R, NT, SLOTS, CTAS>, q, row_ctas, splits, splits, S_THREADS, SMEM, !GATE_UP, st);
+}
+template <bool GATE_UP>
 cudaError_t launch_few(const FfnFew& q, cudaStream_t st) {
-  const int per = (GATE_UP ? 8 : 16) * R;
-  const unsigned grid = (unsigned)((q.rows + per - 1) / per);
   const int nt = (q.T + 7) / 8;
-  auto go = [&](auto kern, int n) {
-    const int smem = S_WARPS * R * n * 4 * 32 * (int)sizeof(float);
-    if (smem > 48 * 1024) {
-      const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-      if (e != cudaSuccess) return e;
-    }
-    kern<<<grid, S_THREADS, smem, st>>>(q);
-    return cudaGetLastError();
-  };
-  if (nt <= 1) return go(k_ffn_few<GATE_UP, R, 1>, 1);
-  if (nt <= 2) return go(k_ffn_few<GATE_UP, R, 2>, 2);
-  if (nt <= 3) return go(k_ffn_few<GATE_UP, R, 3>, 3);
-  return go(k_ffn_few<GATE_UP, R, 4>, 4);
+  if (nt <= 1) return launch_few_as<GATE_UP, 8, 1, 1, 4, 3>(q, st);
+  if (nt <= 2) return launch_few_as<GATE_UP, 8, 2, 2, 3, 2>(q, st);
+  if (nt <= 3) return launch_few_as<GATE_UP, 8, 2, 3, 3, 2>(q, st);
+  if (nt <= 4) return launch_few_as<GATE_UP, 8, 2, 4, 3, 2>(q, st);
+  if (nt <= 6) return launch_few_as<GATE_UP, 2, 1, 6, 6, 2>(q, st);
+  return launch_few_as<GATE_UP, 2, 1, 8, 6, 2>(q, st);
 }
 
 #define FFN_CK(expr)                               \
@@ -801,13 +866,12 @@ extern "C" int camera_ffn_forward(const camera_ffn_t* f, const void* x, int64_t 
     w.out = reinterpret_cast<__nv_bfloat16*>(ws + l.h);
     w.g = static_cast<uint16_t*>(saved); w.u_off = s.fp; w.lo_off = (long long)saved_lo_offset(s); w.act_ld = 2 * s.fp;
     w.totals = reinterpret_cast<PlanTotals*>(ws);
-    // one tile of rows per CTA while that gives each SM two or three CTAs, then more rows per CTA (fewer reads of x)
-    FFN_CK(s.F <= 4096 ? (launch_few<true, 1>(w, st)) : (launch_few<true, 2>(w, st)));
+    FFN_CK(launch_few<true>(w, st));
     w.w0 = w.w1 = static_cast<const __nv_bfloat16*>(f->w_down);
     w.in = w.out; w.out = static_cast<__nv_bfloat16*>(y);
     w.w_ld = s.ld; w.in_ld = s.fp; w.out_ld = s.D; w.rows = s.D; w.k = s.F;
     w.g = nullptr; w.totals = nullptr;
-    FFN_CK((launch_few<false, 1>(w, st)));
+    FFN_CK(launch_few<false>(w, st));
     return CAMERA_OK;
   }
   if (n_tokens == 0) {
