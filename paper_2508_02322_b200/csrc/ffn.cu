@@ -817,8 +817,8 @@ cudaError_t launch_few(const FfnFew& q, cudaStream_t st) {
   if (nt <= 2) return launch_few_as<GATE_UP, 8, 2, 2, 3, 2>(q, st);
   if (nt <= 3) return launch_few_as<GATE_UP, 8, 2, 3, 3, 2>(q, st);
   if (nt <= 4) return launch_few_as<GATE_UP, 8, 2, 4, 3, 2>(q, st);
-  if (nt <= 6) return launch_few_as<GATE_UP, 2, 1, 6, 6, 2>(q, st);
-  return launch_few_as<GATE_UP, 2, 1, 8, 6, 2>(q, st);
+  if (nt <= 6) return launch_few_as<GATE_UP, 4, 1, 6, 6, 2>(q, st);
+  return launch_few_as<GATE_UP, 4, 1, 8, 6, 2>(q, st);
 }
 
 #define FFN_CK(expr)                               \

@@ -16,7 +16,7 @@ from .binding import CAMERA_BF16, CAMERA_F32, CameraError, _check, alloc_workspa
 
 CAMERA_DISTILL_TAIL = 1
 CAMERA_MAX_TOP = 128
-_F32 = torch.float32
+_F32, _BF16 = torch.float32, torch.bfloat16
 _DTYPE = {torch.bfloat16: CAMERA_BF16, torch.float32: CAMERA_F32}
 
 
@@ -77,6 +77,7 @@ class Ffn:
         self.device = w_gate.device
         self.c = camera_ffn_t(d, f, self.down_ld, w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr())
         self._ref = C.byref(self.c)
+        self._saved_bytes: Dict[int, int] = {}
 
 
 def camera_ffn_workspace_bytes(ffn: Ffn, n_tokens: int, *, backward: bool = False) -> int:
@@ -87,14 +88,22 @@ def camera_ffn_workspace_bytes(ffn: Ffn, n_tokens: int, *, backward: bool = Fals
 
 
 def camera_ffn_saved_bytes(ffn: Ffn, n_tokens: int) -> int:
-    return int(lib.camera_ffn_saved_bytes(ffn._ref, n_tokens))
+    n = ffn._saved_bytes.get(n_tokens)
+    if n is None:
+        n = ffn._saved_bytes[n_tokens] = int(lib.camera_ffn_saved_bytes(ffn._ref, n_tokens))
+    return n
 
 
 def _tokens(t: torch.Tensor, ffn: Ffn, name: str) -> int:
-    if not (t.is_contiguous() and t.dtype == torch.bfloat16 and t.dim() == 2 and t.shape[1] == ffn.d_model
-            and t.device == ffn.device):
+    if t.dtype is not _BF16 or t.dim() != 2 or t.shape[1] != ffn.d_model or not t.is_contiguous() or t.device != ffn.device:
         raise ValueError(f"{name} must be a contiguous bf16 [n_tokens, d_model] tensor on the device of the block")
     return t.data_ptr()
+
+
+def _saved(saved: torch.Tensor, ffn: Ffn, n_tokens: int) -> int:
+    if saved.numel() * saved.element_size() < camera_ffn_saved_bytes(ffn, n_tokens) or saved.device != ffn.device:
+        raise ValueError("saved must have camera_ffn_saved_bytes bytes on the device of the block")
+    return saved.data_ptr()
 
 
 @_on_stream
@@ -106,13 +115,11 @@ def camera_ffn_forward(ffn: Ffn, x: torch.Tensor, *, y: Optional[torch.Tensor] =
     n = x.shape[0]
     if y is None:
         y = torch.empty_like(x)
-    elif _tokens(y, ffn, "y") and y.shape[0] != n:
+    elif _tokens(y, ffn, "y") is None or y.shape[0] != n:
         raise ValueError("y must have the shape of x")
     if workspace is None:
         workspace = alloc_workspace(camera_ffn_workspace_bytes(ffn, n), ffn.device)
-    if saved is not None and saved.numel() * saved.element_size() < camera_ffn_saved_bytes(ffn, n):
-        raise ValueError("saved is smaller than camera_ffn_saved_bytes")
-    _check(lib.camera_ffn_forward(ffn._ref, xp, n, y.data_ptr(), None if saved is None else saved.data_ptr(),
+    _check(lib.camera_ffn_forward(ffn._ref, xp, n, y.data_ptr(), None if saved is None else _saved(saved, ffn, n),
                                   workspace.data_ptr(), workspace.numel(), _raw_stream(x.get_device())), "camera_ffn_forward")
     return y
 
@@ -125,28 +132,27 @@ def camera_ffn_backward(ffn: Ffn, x: torch.Tensor, dy: torch.Tensor, saved: torc
     d_model], w_down [d_model, down_ld] (want_weights; columns of w_down from d_ff on are not written).  `out` names
     tensors of those shapes to write to."""
     xp, dyp = _tokens(x, ffn, "x"), _tokens(dy, ffn, "dy")
-    n = x.shape[0]
+    n, f, d = x.shape[0], ffn.d_ff, ffn.d_model
     if dy.shape[0] != n:
         raise ValueError("dy must have the shape of x")
-    if saved.numel() * saved.element_size() < camera_ffn_saved_bytes(ffn, n):
-        raise ValueError("saved is smaller than camera_ffn_saved_bytes")
-    shapes = {"x": (n, ffn.d_model)} if want_x else {}
-    if want_weights:
-        shapes.update(w_gate=(ffn.d_ff, ffn.d_model), w_up=(ffn.d_ff, ffn.d_model), w_down=(ffn.d_model, ffn.down_ld))
-    res = {}
-    for name, shape in shapes.items():
-        t = None if out is None else out.get(name)
+    sp = _saved(saved, ffn, n)
+    res: Dict[str, torch.Tensor] = {}
+    ptr = [None, None, None, None]
+    for i, (name, rows, cols, want) in enumerate((("x", n, d, want_x), ("w_gate", f, d, want_weights),
+                                                  ("w_up", f, d, want_weights), ("w_down", d, ffn.down_ld, want_weights))):
+        if not want:
+            continue
+        t = out.get(name) if out else None
         if t is None:
-            t = torch.empty(shape, dtype=torch.bfloat16, device=ffn.device)
-        elif not (t.is_contiguous() and t.dtype == torch.bfloat16 and tuple(t.shape) == shape and t.device == ffn.device):
-            raise ValueError(f"out[{name!r}] must be a contiguous bf16 tensor of shape {shape}")
+            t = torch.empty((rows, cols), dtype=_BF16, device=ffn.device)
+        elif t.dtype is not _BF16 or t.shape != (rows, cols) or not t.is_contiguous() or t.device != ffn.device:
+            raise ValueError(f"out[{name!r}] must be a contiguous bf16 tensor of shape {(rows, cols)}")
         res[name] = t
+        ptr[i] = t.data_ptr()
     if workspace is None:
         workspace = alloc_workspace(camera_ffn_workspace_bytes(ffn, n, backward=True), ffn.device)
-    ptr = {name: t.data_ptr() for name, t in res.items()}
-    _check(lib.camera_ffn_backward(ffn._ref, xp, dyp, n, saved.data_ptr(), ptr.get("x"), ptr.get("w_gate"), ptr.get("w_up"),
-                                   ptr.get("w_down"), workspace.data_ptr(), workspace.numel(),
-                                   _raw_stream(x.get_device())), "camera_ffn_backward")
+    _check(lib.camera_ffn_backward(ffn._ref, xp, dyp, n, sp, ptr[0], ptr[1], ptr[2], ptr[3], workspace.data_ptr(),
+                                   workspace.numel(), _raw_stream(x.get_device())), "camera_ffn_backward")
     return res
 
 
