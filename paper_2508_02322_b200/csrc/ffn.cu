@@ -732,21 +732,24 @@ FfnLayout ffn_layout(const FfnShape& s, bool backward) {
   return l;
 }
 
-// Columns per B tile and B tiles per work unit.  512 columns (2 x 256) give the least traffic per product (48 KB per CTA
-// and k block for 8.4 Mflop), fewer columns give more work units where the tiles would leave pairs idle in the last
-// round.  The cost of a round is taken as the longer of its products and its loads plus a share for what a unit costs
-// beside its k blocks.
+// Columns per B tile and B tiles per work unit: the choice with the least estimated time, rounds of units over the pairs
+// times a unit's time.  Measured per k block (us): 0.58 for 512 columns, of which the products alone take 0.54 at
+// 1.9 GHz; 0.37 for 256; 0.34 and 0.33 for 128 and 64, where the issue of the MMAs bounds it.  So 512 columns give the
+// highest rate, and fewer give more units where 512 would leave pairs idle.  `epilogue` (us): what a unit of 512 columns,
+// whose accumulators fill tensor memory, adds after its last k block; smaller units have two sets and overlap it.  (8192
+// tokens, d_model 3584, d_ff 2560: dX with 512 columns 231 us, with 256 241 us; 4096 tokens, d_ff 20480: dH with 256
+// columns 650 us, with 512 970 us, whose epilogue reads and writes 12 bytes an element.)
 struct Tile { int bn, nb; };
-Tile choose_tile(long long m_tiles, int n, bool dual, int min_bn, int n_kb, int n_pairs) {
+Tile choose_tile(long long m_tiles, int n, bool dual, int min_bn, int n_kb, double epilogue, int n_pairs) {
   Tile best{256, 2};
   double best_cost = 1e300;
   for (int bn = 256; bn >= min_bn; bn >>= 1)
-    for (int nb = 2; nb >= (dual || bn > min_bn ? 2 : 1); --nb) {
-      const int per = dual ? bn : nb * bn;
+    for (int nb = 2; nb >= (dual ? 2 : 1); --nb) {
+      const int cols = nb * bn, per = dual ? bn : cols;
       const long long units = m_tiles * ((n + per - 1) / per);
-      const double mma = nb * bn / 512.0, load = 0.8 * (16.0 + nb * bn / 16.0) / 48.0;
-      const double cost = (double)((units + n_pairs - 1) / n_pairs) * ((mma > load ? mma : load) + 2.0 * mma / n_kb);
-      if (cost < best_cost * 0.97) { best = Tile{bn, nb}; best_cost = cost; }
+      const double k_block = cols >= 512 ? 0.58 : cols >= 256 ? 0.37 : cols >= 128 ? 0.34 : 0.33;
+      const double cost = (double)((units + n_pairs - 1) / n_pairs) * (n_kb * k_block + (cols >= 512 ? epilogue : 1.0));
+      if (cost < best_cost * 0.98) { best = Tile{bn, nb}; best_cost = cost; }
     }
   return best;
 }
@@ -893,14 +896,14 @@ extern "C" int camera_ffn_forward(const camera_ffn_t* f, const void* x, int64_t 
   q.n_prob = 1;
   q.prob[0] = FfnProblem{(int)s.T, s.F, 0, 0, nullptr, 0, 0};
   q.n_kb = (s.D + UMMA_BK - 1) / UMMA_BK;
-  Tile t = choose_tile(m_tiles, s.F, true, 32, q.n_kb, n_pairs);
+  Tile t = choose_tile(m_tiles, s.F, true, 32, q.n_kb, saved ? 6.0 : 3.0, n_pairs);
   if (!enc(&q.a[0], x, s.T, s.D, s.D, 128) || !enc(&q.b[0], f->w_gate, s.F, s.D, s.D, t.bn / 2) ||
       !enc(&q.b[1], f->w_up, s.F, s.D, s.D, t.bn / 2))
     return CAMERA_ERR_CUDA;
   FFN_CK(launch_gemm<FFN_GATE_UP>(q, t, n_pairs, true, st));
   q.prob[0] = FfnProblem{(int)s.T, s.D, 0, 0, static_cast<__nv_bfloat16*>(y), s.D, wide_rows(y, s.D)};
   q.n_kb = (s.F + UMMA_BK - 1) / UMMA_BK;
-  t = choose_tile(m_tiles, s.D, false, 32, q.n_kb, n_pairs);
+  t = choose_tile(m_tiles, s.D, false, 32, q.n_kb, 3.0, n_pairs);
   if (!enc(&q.a[0], q.h, s.T, s.F, s.fp, 128) || !enc(&q.b[0], f->w_down, s.D, s.F, s.ld, t.bn / 2)) return CAMERA_ERR_CUDA;
   FFN_CK(launch_gemm<FFN_DOWN>(q, t, n_pairs, false, st));
   return CAMERA_OK;
@@ -951,13 +954,13 @@ extern "C" int camera_ffn_backward(const camera_ffn_t* f, const void* x, const v
   q.n_prob = 1;
   q.prob[0] = FfnProblem{(int)s.T, s.F, 0, 0, nullptr, 0, 0};
   q.n_kb = (s.D + UMMA_BK - 1) / UMMA_BK;
-  Tile t = choose_tile(m_tiles, s.F, false, 128, q.n_kb, n_pairs);
+  Tile t = choose_tile(m_tiles, s.F, false, 128, q.n_kb, 20.0, n_pairs);
   if (!enc(&q.a[0], dy, s.T, s.D, s.D, 128) || !enc(&q.b[0], f->w_down, s.D, s.F, s.ld, 64)) return CAMERA_ERR_CUDA;
   FFN_CK(launch_gemm<FFN_DH>(q, t, n_pairs, true, st));
   if (dx != nullptr) {
     q.prob[0] = FfnProblem{(int)s.T, s.D, 0, 0, static_cast<__nv_bfloat16*>(dx), s.D, wide_rows(dx, s.D)};
     q.n_kb = (s.F + UMMA_BK - 1) / UMMA_BK;
-    t = choose_tile(m_tiles, s.D, false, 128, 2 * q.n_kb, n_pairs);
+    t = choose_tile(m_tiles, s.D, false, 128, 2 * q.n_kb, 3.0, n_pairs);
     if (!enc(&q.a[0], q.dg, s.T, s.F, q.act_ld, 128) || !enc(&q.a[1], q.du, s.T, s.F, q.act_ld, 128) ||
         !enc(&q.b[0], f->w_gate, s.F, s.D, s.D, 64) || !enc(&q.b[1], f->w_up, s.F, s.D, s.D, 64))
       return CAMERA_ERR_CUDA;
@@ -970,7 +973,7 @@ extern "C" int camera_ffn_backward(const camera_ffn_t* f, const void* x, const v
     q.prob[2] = FfnProblem{s.D, s.F, 0, 0, static_cast<__nv_bfloat16*>(dw_down), s.ld, wide_rows(dw_down, s.ld)};
     q.n_kb = (int)((s.T + UMMA_BK - 1) / UMMA_BK);
     // the third problem has as many tiles as either of the others, up to their edges
-    t = choose_tile(3ll * ((s.F + G_TILE_M - 1) / G_TILE_M), s.D, false, 128, q.n_kb, n_pairs);
+    t = choose_tile(3ll * ((s.F + G_TILE_M - 1) / G_TILE_M), s.D, false, 128, q.n_kb, 3.0, n_pairs);
     if (!enc(&q.a[0], q.dg, s.T, s.F, q.act_ld, 64) || !enc(&q.a[1], q.du, s.T, s.F, q.act_ld, 64) ||
         !enc(&q.a[2], dy, s.T, s.D, s.D, 64) || !enc(&q.b[0], x, s.T, s.D, s.D, 64) || !enc(&q.b[2], q.h, s.T, s.F, s.fp, 64))
       return CAMERA_ERR_CUDA;
