@@ -6,8 +6,10 @@
 //   s = sum 2^(x c - m)   and, for the entropy,   t = sum 2^(x c - m) (x c - m);
 // the threads' sums are joined by scaling with 2^(m_i - max m).  One pass over the row then gives
 //   ln sum exp z = (m + log2 s) ln 2,   log p_v = (x_v c - m - log2 s) ln 2,   H = (log2 s - t / s) ln 2.
-// The reference does not follow the maximum: fp32 holds 2^(x c - m) for any x c up to m + 127, and scaling loses no
-// precision, so no logit has to be compared.  A row whose sum ends outside
+// The reference does not follow the maximum closely: fp32 holds 2^(x c - m) for any x c up to m + 127, and scaling loses
+// no precision in s.  Only the entropy wants it within a few powers of two of the largest logit, because log2 s and t / s
+// cancel (4095 rows: error of the entropies against 64 bits 9.6e-6 without, 6e-7 with): where it is asked for, a thread
+// raises its reference when a chunk's maximum exceeds it by more than 2^REF_SLACK.  A row whose sum ends outside
 // [2^-60, 2^120] (masked at the start, larger further on, all of it the type's lowest value, NaN, infinity: nothing an
 // ordinary row does) is walked again with differences formed before the scaling and a running maximum (walk_careful).
 // All sums are fp32 over at most a few hundred terms a thread, then a tree in a fixed order.
@@ -32,6 +34,7 @@ constexpr int V_THREADS = 256;
 constexpr int V_WARPS = V_THREADS / 32;
 constexpr int V_MAX_SPLIT = 8;             // CTAs that can share a row
 constexpr float D_FLOOR = -150.f;          // 2^-150 is 0 in fp32: a floor for exponents that multiply a zero weight
+constexpr float REF_SLACK = 3.f;
 constexpr float LN2 = 0.693147180559945309f;
 constexpr float LOG2E = 1.44269504088896341f;
 
@@ -280,9 +283,11 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
   constexpr uint32_t NI = Elem<T>::NEG_INF;
   const uint4 nothing = make_uint4(NI, NI, NI, NI);          // minus infinity has no weight
   const int tid = threadIdx.x;
-  uint32_t big[RG::PER];                                     // running maxima in the raw form
+  uint32_t big[TOP ? RG::PER : 1];                           // running maxima in the raw form
+  if (TOP) {
 #pragma unroll
-  for (int u = 0; u < RG::PER; ++u) big[u] = NI;
+    for (int u = 0; u < RG::PER; ++u) big[u] = NI;
+  }
   float2 s2 = make_float2(0.f, 0.f), t2 = make_float2(0.f, 0.f);
   const float2 c2 = make_float2(c, c);
   float2 ref2 = make_float2(0.f, 0.f);
@@ -314,17 +319,26 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
       }
       mark += RG::CHUNK / 32;
     }
-    if (TOP || first) {
+    if (ENT || TOP || first) {
+      uint32_t chunk = NI;
 #pragma unroll
-      for (int u = 0; u < RG::PER; ++u) big[u] = Elem<T>::max_word(big[u], Elem<T>::max_vec(raw[u]));
-    }
-    if (first) {
-      float m = fmaxf(single[0], single[1]);
-#pragma unroll
-      for (int u = 0; u < RG::PER; ++u) m = fmaxf(m, Elem<T>::max_of(big[u]));
-      m = fmaxf(m * c, -126.f);
-      ref2 = make_float2(-m, -m);
-      first = false;
+      for (int u = 0; u < RG::PER; ++u) {
+        const uint32_t w = Elem<T>::max_vec(raw[u]);
+        if (TOP) big[u] = Elem<T>::max_word(big[u], w);
+        chunk = Elem<T>::max_word(chunk, w);
+      }
+      float m = Elem<T>::max_of(chunk) * c;
+      if (first) {
+        m = fmaxf(fmaxf(m, fmaxf(single[0], single[1]) * c), -126.f);
+        ref2 = make_float2(-m, -m);
+        first = false;
+      } else if (ENT && m > REF_SLACK - ref2.x) {            // the entropy's digits (see above)
+        const float d = -ref2.x - m, f = ex2(d), dd = fmaxf(d, D_FLOOR);
+        const float2 f2 = make_float2(f, f), dd2 = make_float2(dd, dd);
+        t2 = mul2(f2, fma2(dd2, s2, t2));
+        s2 = mul2(s2, f2);
+        ref2 = make_float2(-m, -m);
+      }
     }
 #pragma unroll
     for (int u = 0; u < RG::PER; ++u) {
