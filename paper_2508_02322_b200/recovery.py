@@ -7,7 +7,6 @@ are allocated on the stream the call runs on.
 from __future__ import annotations
 
 import ctypes as C
-import functools
 from typing import Dict, Optional, Tuple
 
 import torch
@@ -26,15 +25,10 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _on_stream(fn):
-    """Runs the call with `stream` (if given) as the current stream, so that what it allocates belongs there."""
-    @functools.wraps(fn)
-    def wrapper(*args, stream: Optional[torch.cuda.Stream] = None, **kw):
-        if stream is None:
-            return fn(*args, **kw)
-        with torch.cuda.stream(stream):
-            return fn(*args, **kw)
-    return wrapper
+def _elsewhere(stream: Optional[torch.cuda.Stream], fn, *args, **kw):
+    """The call with `stream` as the current one, so that what it allocates belongs there."""
+    with torch.cuda.stream(stream):
+        return fn(*args, **kw)
 
 
 def _rows(t: torch.Tensor, name: str) -> int:
@@ -106,11 +100,13 @@ def _saved(saved: torch.Tensor, ffn: Ffn, n_tokens: int) -> int:
     return saved.data_ptr()
 
 
-@_on_stream
 def camera_ffn_forward(ffn: Ffn, x: torch.Tensor, *, y: Optional[torch.Tensor] = None, saved: Optional[torch.Tensor] = None,
-                       workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+                       workspace: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """y = (SiLU(x W_gate^T) * (x W_up^T)) W_down^T, bf16 [n_tokens, d_model].  `saved` (camera_ffn_saved_bytes bytes)
     receives what camera_ffn_backward needs."""
+    if stream is not None:
+        return _elsewhere(stream, camera_ffn_forward, ffn, x, y=y, saved=saved, workspace=workspace)
     xp = _tokens(x, ffn, "x")
     n = x.shape[0]
     if y is None:
@@ -124,13 +120,16 @@ def camera_ffn_forward(ffn: Ffn, x: torch.Tensor, *, y: Optional[torch.Tensor] =
     return y
 
 
-@_on_stream
 def camera_ffn_backward(ffn: Ffn, x: torch.Tensor, dy: torch.Tensor, saved: torch.Tensor, *, want_x: bool = True,
                         want_weights: bool = True, out: Optional[Dict[str, torch.Tensor]] = None,
-                        workspace: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
+                        workspace: Optional[torch.Tensor] = None,
+                        stream: Optional[torch.cuda.Stream] = None) -> Dict[str, torch.Tensor]:
     """Gradients of camera_ffn_forward(ffn, x, saved=saved) given dy: a dict with x (want_x) and w_gate, w_up [d_ff,
     d_model], w_down [d_model, down_ld] (want_weights; columns of w_down from d_ff on are not written).  `out` names
     tensors of those shapes to write to."""
+    if stream is not None:
+        return _elsewhere(stream, camera_ffn_backward, ffn, x, dy, saved, want_x=want_x, want_weights=want_weights, out=out,
+                          workspace=workspace)
     xp, dyp = _tokens(x, ffn, "x"), _tokens(dy, ffn, "dy")
     n, f, d = x.shape[0], ffn.d_ff, ffn.d_model
     if dy.shape[0] != n:
@@ -156,12 +155,14 @@ def camera_ffn_backward(ffn: Ffn, x: torch.Tensor, dy: torch.Tensor, saved: torc
     return res
 
 
-@_on_stream
 def camera_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, *, top_n: int = 0,
-                          temperature: float = 1.0, entropy: bool = True) -> Dict[str, torch.Tensor]:
+                          temperature: float = 1.0, entropy: bool = True,
+                          stream: Optional[torch.cuda.Stream] = None) -> Dict[str, torch.Tensor]:
     """Log-probability of targets[r] (int64 [n_rows]) under softmax(logits[r] / temperature), the entropy of that
     distribution, and its top_n alternatives.  Returns a dict with logprob (if targets are given), entropy (unless
     entropy=False), and for top_n > 0 top_idx (int32) and top_logprob [n_rows, top_n]."""
+    if stream is not None:
+        return _elsewhere(stream, camera_token_logprobs, logits, targets, top_n=top_n, temperature=temperature, entropy=entropy)
     ld = _rows(logits, "logits")
     rows, vocab = logits.shape
     out: Dict[str, torch.Tensor] = {}
@@ -175,12 +176,14 @@ def camera_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] 
         out["entropy"] = t = torch.empty(rows, dtype=_F32, device=dev)
         h_ptr = t.data_ptr()
     if top_n > 0:
-        out["top_idx"] = t = torch.empty((rows, top_n), dtype=torch.int32, device=dev)
+        out["top_idx"] = t = torch.empty(rows, top_n, dtype=torch.int32, device=dev)
         i_ptr = t.data_ptr()
-        out["top_logprob"] = t = torch.empty((rows, top_n), dtype=torch.float32, device=dev)
+        out["top_logprob"] = t = torch.empty(rows, top_n, dtype=_F32, device=dev)
         v_ptr = t.data_ptr()
-    _check(lib.camera_token_logprobs(logits.data_ptr(), _DTYPE[logits.dtype], ld, rows, vocab, t_ptr, top_n, temperature,
-                                     lp_ptr, h_ptr, i_ptr, v_ptr, _raw_stream(logits.get_device())), "camera_token_logprobs")
+    status = lib.camera_token_logprobs(logits.data_ptr(), _DTYPE[logits.dtype], ld, rows, vocab, t_ptr, top_n, temperature,
+                                       lp_ptr, h_ptr, i_ptr, v_ptr, _raw_stream(logits.get_device()))
+    if status:
+        _check(status, "camera_token_logprobs")
     return out
 
 
@@ -205,27 +208,32 @@ def _gradient(logits: torch.Tensor, d_logits: Optional[torch.Tensor], ld: int) -
     return d_logits, _rows(d_logits, "d_logits")
 
 
-@_on_stream
 def camera_distill_forward(logits: torch.Tensor, teacher_idx: torch.Tensor, teacher_logprob: torch.Tensor, *,
-                           temperature: float = 1.0, tail: bool = False) -> Dict[str, torch.Tensor]:
+                           temperature: float = 1.0, tail: bool = False,
+                           stream: Optional[torch.cuda.Stream] = None) -> Dict[str, torch.Tensor]:
     """Divergence of the student (softmax(logits / temperature)) from the teacher's list (int32 / fp32 [n_rows, k], as
     camera_token_logprobs returns them) per row.  Returns a dict with loss [n_rows] and what camera_distill_backward
     takes: lse and, with tail=True (the rest of the vocabulary as one more class), log_tail."""
+    if stream is not None:
+        return _elsewhere(stream, camera_distill_forward, logits, teacher_idx, teacher_logprob, temperature=temperature, tail=tail)
     d = _distill(logits, teacher_idx, teacher_logprob, temperature, tail)
-    out = {name: torch.empty(d.n_rows, dtype=torch.float32, device=logits.device)
+    out = {name: torch.empty(d.n_rows, dtype=_F32, device=logits.device)
            for name in (("loss", "lse", "log_tail") if tail else ("loss", "lse"))}
     _check(lib.camera_distill_forward(C.byref(d), out["loss"].data_ptr(), out["lse"].data_ptr(),
                                       out["log_tail"].data_ptr() if tail else None, _raw_stream(logits.get_device())), "camera_distill_forward")
     return out
 
 
-@_on_stream
 def camera_distill_backward(logits: torch.Tensor, teacher_idx: torch.Tensor, teacher_logprob: torch.Tensor,
                             d_loss: torch.Tensor, lse: torch.Tensor, log_tail: Optional[torch.Tensor] = None, *,
                             temperature: float = 1.0, tail: bool = False,
-                            d_logits: Optional[torch.Tensor] = None) -> torch.Tensor:
+                            d_logits: Optional[torch.Tensor] = None,
+                            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Gradient by the logits, d_loss [n_rows] being the gradient by the losses; lse and log_tail are the forward
     call's.  d_logits may be the logits themselves."""
+    if stream is not None:
+        return _elsewhere(stream, camera_distill_backward, logits, teacher_idx, teacher_logprob, d_loss, lse, log_tail,
+                          temperature=temperature, tail=tail, d_logits=d_logits)
     d = _distill(logits, teacher_idx, teacher_logprob, temperature, tail)
     rows = (d.n_rows,)
     if tail and log_tail is None:
@@ -238,14 +246,17 @@ def camera_distill_backward(logits: torch.Tensor, teacher_idx: torch.Tensor, tea
     return d_logits
 
 
-@_on_stream
 def camera_distill_step(logits: torch.Tensor, teacher_idx: torch.Tensor, teacher_logprob: torch.Tensor,
                         d_loss: torch.Tensor, *, temperature: float = 1.0, tail: bool = False,
-                        d_logits: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+                        d_logits: Optional[torch.Tensor] = None,
+                        stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Loss and gradient from one call, for a d_loss known beforehand.  Returns (loss, d_logits)."""
+    if stream is not None:
+        return _elsewhere(stream, camera_distill_step, logits, teacher_idx, teacher_logprob, d_loss, temperature=temperature,
+                          tail=tail, d_logits=d_logits)
     d = _distill(logits, teacher_idx, teacher_logprob, temperature, tail)
     d_logits, d_ld = _gradient(logits, d_logits, d.ld)
-    loss = torch.empty(d.n_rows, dtype=torch.float32, device=logits.device)
+    loss = torch.empty(d.n_rows, dtype=_F32, device=logits.device)
     _check(lib.camera_distill_step(C.byref(d), _vector(d_loss, logits, torch.float32, (d.n_rows,), "d_loss"),
                                    loss.data_ptr(), d_logits.data_ptr(), d_ld, _raw_stream(logits.get_device())), "camera_distill_step")
     return loss, d_logits
