@@ -107,6 +107,32 @@ __device__ __forceinline__ void tma_load_lead(uint32_t lead, uint32_t dst, const
       "}\n" ::"r"(dst), "l"(tmap), "r"(bar_cluster_addr), "r"(x), "r"(y), "r"(lead)
       : "memory");
 }
+// The MMAs of one k block (four steps of 16) on one B tile in one piece of assembly, so that predicates are set once and
+// the descriptors' steps are plain additions (0.38 -> 0.32 us per k block).  Two B tiles in turn are better off as single
+// MMAs (0.39 us; in one piece 0.49).
+template <int A_STEP, int B_STEP>
+__device__ __forceinline__ void umma_block(uint32_t lead, uint32_t d0, unsigned long long a, unsigned long long b, uint32_t idesc,
+                                           uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q, t;\n"
+      ".reg .b64 a1, a2, a3, b1, b2, b3;\n"
+      "setp.ne.b32 q, %5, 0;\n"
+      "setp.ne.b32 p, %4, 0;\n"
+      "setp.eq.b32 t, 0, 0;\n"
+      "add.s64 a1, %1, %6;\n"
+      "add.s64 b1, %2, %7;\n"
+      "add.s64 a2, %1, 2 * %6;\n"
+      "add.s64 b2, %2, 2 * %7;\n"
+      "add.s64 a3, %1, 3 * %6;\n"
+      "add.s64 b3, %2, 3 * %7;\n"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], a1, b1, %3, t;\n"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], a2, b2, %3, t;\n"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], a3, b3, %3, t;\n"
+      "}\n" ::"r"(d0), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(lead), "n"(A_STEP), "n"(B_STEP)
+      : "memory");
+}
 __device__ __forceinline__ void umma_lead(uint32_t lead, uint32_t d_tmem, unsigned long long a, unsigned long long b, uint32_t idesc,
                                           uint32_t accumulate) {
   asm volatile(
@@ -293,8 +319,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true, ready = false;       // ready: the next stage has been seen full
       const uint32_t idesc = make_idesc_pair(q.bn) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
-      constexpr unsigned long long A_STEP = A_MN ? 2048 >> 4 : 32 >> 4, B_STEP = B_MN ? 2048 >> 4 : 32 >> 4;
-      constexpr int STEPS = UMMA_BK / 16;
+      constexpr int A_STEP = A_MN ? 2048 >> 4 : 32 >> 4, B_STEP = B_MN ? 2048 >> 4 : 32 >> 4;     // 16 k further
       const unsigned long long a_first = A_MN ? make_smem_desc_mn(base) : make_smem_desc(base);
       const unsigned long long b_first = B_MN ? make_smem_desc_mn(base + G_A_BYTES) : make_smem_desc(base + G_A_BYTES);
       const unsigned long long b2_off = (unsigned long long)(b_bytes >> 4);
@@ -304,7 +329,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
         if (!ok) break;
         tc_fence_after();
         const uint32_t d0 = tmem_base + (uint32_t)(acc * q.nb * q.bn), d1 = d0 + (uint32_t)q.bn;
-        const uint32_t lead2 = u.two ? lead : 0u;
         uint32_t accumulate = 0;
         for (int seg = 0; ok && seg < SEGMENTS; ++seg) {
           for (int kb = 0; kb < q.n_kb; kb += q.kps) {
@@ -317,13 +341,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
             const uint32_t done = empty_bar(stage);
             if (++stage == q.n_stages) { stage = 0; phase ^= 1u; }
             for (int block = min(q.kps, q.n_kb - kb); block > 0; --block, at += (unsigned long long)(block_bytes >> 4)) {
-              const unsigned long long a_desc = a_first + at, b_desc = b_first + at, b2_desc = b_desc + b2_off;
+              const unsigned long long a_desc = a_first + at, b_desc = b_first + at;
+              if (u.two) {
+                const unsigned long long b2_desc = b_desc + b2_off;
 #pragma unroll
-              for (int k = 0; k < STEPS; ++k) {
-                umma_lead(lead, d0, a_desc + A_STEP * k, b_desc + B_STEP * k, idesc, accumulate);
-                umma_lead(lead2, d1, a_desc + A_STEP * k, b2_desc + B_STEP * k, idesc, accumulate);
-                accumulate = 1;
+                for (int k = 0; k < UMMA_BK / 16; ++k) {
+                  umma_lead(lead, d0, a_desc + A_STEP * k, b_desc + B_STEP * k, idesc, accumulate | (uint32_t)k);
+                  umma_lead(lead, d1, a_desc + A_STEP * k, b2_desc + B_STEP * k, idesc, accumulate | (uint32_t)k);
+                }
+              } else {
+                umma_block<A_STEP, B_STEP>(lead, d0, a_desc, b_desc, idesc, accumulate);
               }
+              accumulate = 1;
             }
             // The tensor pipe holds only a few MMAs: a look at the next stage's barrier while they run.
             ready = __all_sync(0xffffffffu, mbar_test(full_bar(stage), phase));
@@ -733,8 +762,9 @@ FfnLayout ffn_layout(const FfnShape& s, bool backward) {
 }
 
 // Columns per B tile and B tiles per work unit: the choice with the least estimated time, rounds of units over the pairs
-// times a unit's time.  Measured per k block (us): 0.58 for 512 columns, of which the products alone take 0.54 at
-// 1.9 GHz; 0.37 for 256; 0.34 and 0.33 for 128 and 64, where the issue of the MMAs bounds it.  So 512 columns give the
+// times a unit's time.  Measured per k block (us): 0.60 for 512 columns, of which the products alone take 0.54 at
+// 1.9 GHz; 0.43 for one tile of 256, 0.40 for two of 128; 0.39 for two and 0.32 for one tile of up to 128 columns, where
+// the issue of the MMAs bounds it.  So 512 columns give the
 // highest rate, and fewer give more units where 512 would leave pairs idle.  `epilogue` (us): what a unit of 512 columns,
 // whose accumulators fill tensor memory, adds after its last k block; smaller units have two sets and overlap it.  (8192
 // tokens, d_model 3584, d_ff 2560: dX with 512 columns 231 us, with 256 241 us; 4096 tokens, d_ff 20480: dH with 256
@@ -747,9 +777,9 @@ Tile choose_tile(long long m_tiles, int n, bool dual, int min_bn, int n_kb, doub
     for (int nb = 2; nb >= (dual ? 2 : 1); --nb) {
       const int cols = nb * bn, per = dual ? bn : cols;
       const long long units = m_tiles * ((n + per - 1) / per);
-      const double k_block = cols >= 512 ? 0.58 : cols >= 256 ? 0.37 : cols >= 128 ? 0.34 : 0.33;
+      const double k_block = cols >= 512 ? 0.60 : bn >= 256 ? 0.43 : cols >= 256 ? 0.40 : nb == 2 ? 0.39 : 0.32;
       const double cost = (double)((units + n_pairs - 1) / n_pairs) * (n_kb * k_block + (cols >= 512 ? epilogue : 1.0));
-      if (cost < best_cost * 0.98) { best = Tile{bn, nb}; best_cost = cost; }
+      if (cost < best_cost * 0.99) { best = Tile{bn, nb}; best_cost = cost; }
     }
   return best;
 }
