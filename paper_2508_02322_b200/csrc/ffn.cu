@@ -25,7 +25,9 @@ namespace camera {
 
 namespace {
 
-constexpr int G_THREADS = 192;               // warps 0-3 epilogue, warp 4 TMA producer, warp 5 MMA issuer
+constexpr int G_EPI_WARPS = 8;               // epilogue: two warps per 32 rows, which take 16-column chunks in turn
+constexpr int G_PRODUCER = G_EPI_WARPS, G_ISSUER = G_EPI_WARPS + 1;
+constexpr int G_THREADS = 32 * (G_EPI_WARPS + 2);
 constexpr int G_TILE_M = 256;                // rows of the output a pair computes: 128 per CTA
 constexpr int G_A_BYTES = 128 * 128;         // this CTA's 128 rows x 64 k
 constexpr int G_MAX_STAGES = 8;
@@ -206,6 +208,26 @@ __device__ __forceinline__ float kept24(const uint32_t* h, const uint32_t* l, in
   const uint32_t top = j & 1 ? h[j >> 1] & 0xffff0000u : h[j >> 1] << 16;
   return __uint_as_float(top | (((l[j >> 2] >> (8 * (j & 3))) & 0xffu) << 8));
 }
+// 16 kept elements of G and U on their way from memory.
+struct Kept {
+  uint4 g[2], u[2], g_lo, u_lo;
+  __device__ __forceinline__ void load(const FfnGemm& q, long long at) {
+    const long long u_off = q.u - q.g;
+    const uint8_t* const lo = reinterpret_cast<const uint8_t*>(q.g) + q.lo_off;
+    const uint4* const gp = reinterpret_cast<const uint4*>(q.g + at);
+    const uint4* const up = reinterpret_cast<const uint4*>(q.g + at + u_off);
+    g[0] = gp[0]; g[1] = gp[1];
+    u[0] = up[0]; u[1] = up[1];
+    g_lo = *reinterpret_cast<const uint4*>(lo + at);
+    u_lo = *reinterpret_cast<const uint4*>(lo + at + u_off);
+  }
+  __device__ __forceinline__ float gate(int j) const {
+    return kept24(reinterpret_cast<const uint32_t*>(g), reinterpret_cast<const uint32_t*>(&g_lo), j);
+  }
+  __device__ __forceinline__ float up(int j) const {
+    return kept24(reinterpret_cast<const uint32_t*>(u), reinterpret_cast<const uint32_t*>(&u_lo), j);
+  }
+};
 __device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
 
 template <int MODE>
@@ -221,7 +243,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
   auto full_bar = [&](int s) { return bars + 8u * s; };                                 // first CTA
   auto empty_bar = [&](int s) { return bars + 8u * (G_MAX_STAGES + s); };               // each CTA
   auto tfull_bar = [&](int a) { return bars + 8u * (2 * G_MAX_STAGES + a); };           // each CTA
-  auto tempty_bar = [&](int a) { return bars + 8u * (2 * G_MAX_STAGES + 2 + a); };      // first CTA, 256 readers
+  auto tempty_bar = [&](int a) { return bars + 8u * (2 * G_MAX_STAGES + 2 + a); };      // first CTA, the pair's epilogue threads
   uint8_t* const tail = base_ptr + G_RING_BYTES + 8 * (2 * G_MAX_STAGES + 4);
   volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(tail + 8);
@@ -236,12 +258,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
 
   if (tid == 0) {
     for (int s = 0; s < q.n_stages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 256); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 2 * 32 * G_EPI_WARPS); }
     wait_state_init(abort_flag, q.wait_limit_ns);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == 5) {
+  if (warp == G_ISSUER) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_slot)),
                  "r"(G_TMEM_COLS)
                  : "memory");
@@ -260,7 +282,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
   // ran out at the earliest, when every CTA of the grid (one per SM) has long started.
   if (q.clear_status && blockIdx.x == 0 && tid == 0) atomicExch(&q.totals->status, 0);
 
-  if (warp == 4) {
+  if (warp == G_PRODUCER) {
     // ------------------------------------------------------------------ TMA producer (each CTA loads its own share)
     const uint32_t lead = lane == 0;
     int stage = 0;
@@ -311,7 +333,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
       const unsigned long long t0 = globaltimer_ns();
       while (globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
     }
-  } else if (warp == 5) {
+  } else if (warp == G_ISSUER) {
     // ------------------------------------------------------------------ MMA issuer (first CTA of the pair only)
     if (rank == 0) {
       const uint32_t lead = lane == 0;
@@ -366,66 +388,71 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
     }
   } else {
     // ------------------------------------------------------------------ epilogue: a thread owns a row of the output
+    // Loads of the next chunk (tensor memory, and for DH the kept products from global memory) fly while one is worked on.
     int acc = 0;
     uint32_t acc_phase = 0;
     bool ok = true;
+    const int c_first = 16 * (warp >> 2), c_step = 16 * (G_EPI_WARPS / 4);
     for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
       const FfnUnit u = decode(q, unit, DUAL);
       const FfnProblem& pr = q.prob[u.p];
-      const long long row = (long long)u.m0 + 128 * (int)rank + warp * 32 + lane;
+      const long long row = (long long)u.m0 + 128 * (int)rank + (warp & 3) * 32 + lane;
       const bool live = row < pr.m;
+      const int cols = min(pr.n - u.n0, DUAL ? q.bn : q.nb * q.bn);
+      [[maybe_unused]] Kept next;
+      if constexpr (MODE == FFN_DH) {
+        if (live && c_first < cols) next.load(q, row * q.act_ld + u.n0 + c_first);
+      }
       ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_phase, abort_flag));
       if (!ok) break;
       tc_fence_after();
-      const uint32_t t0 = tmem_base + ((uint32_t)(warp * 32) << 16) + (uint32_t)(acc * q.nb * q.bn);
-      const int cols = min(pr.n - u.n0, DUAL ? q.bn : q.nb * q.bn);
+      const uint32_t t0 = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(acc * q.nb * q.bn);
       if constexpr (MODE == FFN_GATE_UP) {
         __nv_bfloat16* const h = q.h + row * q.h_ld + u.n0;
         const bool keep = q.g != nullptr;
         const long long g_at = row * q.act_ld + u.n0, u_at = g_at + (q.u - q.g);
         uint8_t* const lo = reinterpret_cast<uint8_t*>(q.g) + q.lo_off;
-        for (int c = 0; c < cols; c += 16) {
-          uint32_t vg[16], vu[16], p[8];
-          tmem_ld16(t0 + c, vg);
-          tmem_ld16(t0 + q.bn + c, vu);
-          tmem_ld_wait(vg, vu);
+        auto put = [&](const uint32_t* vg, const uint32_t* vu, int c) {
+          if (!live) return;
+          uint32_t p[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const float g0 = __uint_as_float(vg[2 * j]), g1 = __uint_as_float(vg[2 * j + 1]);
             p[j] = pack_bf16(g0 * sigmoid(g0) * __uint_as_float(vu[2 * j]), g1 * sigmoid(g1) * __uint_as_float(vu[2 * j + 1]));
           }
-          if (live) st_global_v8(h + c, p);            // the pitches of h, g, u are multiples of 64: whole chunks fit
-          if (live && keep) {
+          st_global_v8(h + c, p);                      // the pitches of h, g, u are multiples of 64: whole chunks fit
+          if (keep) {
             keep24(q.g + g_at + c, lo + g_at + c, vg);
             keep24(q.g + u_at + c, lo + u_at + c, vu);
           }
+        };
+        uint32_t g0[16], u0[16], g1[16], u1[16];
+        int c = c_first;
+        if (c < cols) { tmem_ld16(t0 + c, g0); tmem_ld16(t0 + q.bn + c, u0); }
+        for (; c < cols; c += 2 * c_step) {
+          const int c1 = c + c_step, c2 = c1 + c_step;
+          tmem_ld_wait(g0, u0);
+          if (c1 < cols) { tmem_ld16(t0 + c1, g1); tmem_ld16(t0 + q.bn + c1, u1); }
+          put(g0, u0, c);
+          if (c1 >= cols) break;
+          tmem_ld_wait(g1, u1);
+          if (c2 < cols) { tmem_ld16(t0 + c2, g0); tmem_ld16(t0 + q.bn + c2, u0); }
+          put(g1, u1, c1);
         }
       } else if constexpr (MODE == FFN_DH) {
-        const long long at = row * q.act_ld + u.n0, u_off = q.u - q.g;
-        const uint8_t* const lo = reinterpret_cast<const uint8_t*>(q.g) + q.lo_off;
-        for (int c = 0; c < cols; c += 16) {
+        const long long at = row * q.act_ld + u.n0;
+        for (int c = c_first; c < cols; c += c_step) {
           uint32_t v[16], pg[8], pu[8], ph[8];
           tmem_ld16(t0 + c, v);
-          uint4 gi[2], ui[2], gl, ul;
-          if (live) {
-            const uint4* const gp = reinterpret_cast<const uint4*>(q.g + at + c);
-            const uint4* const up = reinterpret_cast<const uint4*>(q.g + at + u_off + c);
-            gi[0] = gp[0]; gi[1] = gp[1];
-            ui[0] = up[0]; ui[1] = up[1];
-            gl = *reinterpret_cast<const uint4*>(lo + at + c);
-            ul = *reinterpret_cast<const uint4*>(lo + at + u_off + c);
-          }
+          const Kept kept = next;
+          if (live && c + c_step < cols) next.load(q, at + c + c_step);
           tmem_ld_wait(v);
-          const uint32_t* const gw = reinterpret_cast<const uint32_t*>(gi);
-          const uint32_t* const uw = reinterpret_cast<const uint32_t*>(ui);
-          const uint32_t* const gb = reinterpret_cast<const uint32_t*>(&gl);
-          const uint32_t* const ub = reinterpret_cast<const uint32_t*>(&ul);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             float dg[2], du[2], h[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float g = kept24(gw, gb, 2 * j + e), up = kept24(uw, ub, 2 * j + e);
+              const float g = kept.gate(2 * j + e), up = kept.up(2 * j + e);
               const float dh = __uint_as_float(v[2 * j + e]), s = sigmoid(g), act = g * s;
               h[e] = act * up;
               du[e] = dh * act;
@@ -443,21 +470,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
         }
       } else {
         __nv_bfloat16* const out = pr.out + row * pr.ld + u.n0;
-        for (int c = 0; c < cols; c += 16) {
-          uint32_t v[16], p[8];
-          tmem_ld16(t0 + c, v);
-          tmem_ld_wait(v);
+        const bool wide = pr.wide;
+        auto put = [&](const uint32_t* v, int c) {
+          if (!live) return;
+          uint32_t p[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) p[j] = pack_bf16(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
-          if (!live) continue;
           if (c + 16 <= cols) {
-            store16(out + c, p, pr.wide);
+            store16(out + c, p, wide);
           } else {
 #pragma unroll
             for (int j = 0; j < 16; ++j)
               if (c + j < cols)
                 out[c + j] = __ushort_as_bfloat16((unsigned short)(j & 1 ? p[j >> 1] >> 16 : p[j >> 1] & 0xffffu));
           }
+        };
+        uint32_t v0[16], v1[16];
+        int c = c_first;
+        if (c < cols) tmem_ld16(t0 + c, v0);
+        for (; c < cols; c += 2 * c_step) {
+          const int c1 = c + c_step, c2 = c1 + c_step;
+          tmem_ld_wait(v0);
+          if (c1 < cols) tmem_ld16(t0 + c1, v1);
+          put(v0, c);
+          if (c1 >= cols) break;
+          tmem_ld_wait(v1);
+          if (c2 < cols) tmem_ld16(t0 + c2, v0);
+          put(v1, c1);
         }
       }
       tc_fence_before();
@@ -470,7 +509,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
   __syncthreads();
   if (*abort_flag && tid == 0) atomicExch(&q.totals->status, (int)CAMERA_ERR_DEVICE_TIMEOUT);
   cluster_sync_all();     // neither CTA leaves while the other may still read its shared or tensor memory
-  if (warp == 5) {
+  if (warp == G_ISSUER) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(G_TMEM_COLS) : "memory");
   }
