@@ -51,6 +51,8 @@ struct FfnGemm {
   FfnProblem prob[3];
   int n_prob, n_units;
   int n_kb;                 // k blocks per segment
+  int splits, tiles;        // DOWN, DX: parts of the sum over k, each a work unit per tile; tiles of one part
+  float* part;              // splits > 1: where the parts' sums go, [splits][m][n] fp32
   int kps;                  // k blocks per stage of the ring (1 or 2)
   int bn, nb;               // columns per B tile; B tiles per work unit (GATE_UP: 2, one of each matrix)
   int n_stages, n_acc;      // ring depth; accumulator sets in tensor memory
@@ -63,14 +65,26 @@ struct FfnGemm {
   unsigned long long wait_limit_ns;
 };
 
-struct FfnUnit { int p, m0, n0, two; };
+struct FfnUnit { int p, m0, n0, two, k0, k1, split; };
 
 // Units of a problem are numbered group by group of G_GROUP_M row tiles, inside a group column tile by column tile and
 // the row tile fastest: the pairs at work at one time share a few column tiles of B and a block of rows of A, both of
 // which stay in L2.
-__device__ __forceinline__ FfnUnit decode(const FfnGemm& q, int unit, bool dual) {
+template <int MODE>
+__device__ __forceinline__ FfnUnit decode(const FfnGemm& q, int unit) {
+  constexpr bool dual = MODE == FFN_GATE_UP, SPLIT = MODE == FFN_DOWN || MODE == FFN_DX;
   FfnUnit r;
   r.p = 0;
+  r.split = 0;
+  r.k0 = 0;
+  r.k1 = MODE == FFN_DX ? 2 * q.n_kb : q.n_kb;
+  if (SPLIT && q.splits > 1) {
+    r.split = unit / q.tiles;
+    unit -= r.split * q.tiles;
+    const int all = r.k1;
+    r.k0 = all * r.split / q.splits;
+    r.k1 = all * (r.split + 1) / q.splits;
+  }
   while (r.p + 1 < q.n_prob && unit >= q.prob[r.p + 1].unit0) ++r.p;
   const FfnProblem& pr = q.prob[r.p];
   const int m_tiles = (pr.m + G_TILE_M - 1) / G_TILE_M;
@@ -235,7 +249,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
   constexpr bool A_MN = MODE == FFN_DW;
   constexpr bool B_MN = MODE == FFN_DH || MODE == FFN_DX || MODE == FFN_DW;
   constexpr bool DUAL = MODE == FFN_GATE_UP;
-  constexpr int SEGMENTS = MODE == FFN_DX ? 2 : 1;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -289,44 +302,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
     uint32_t phase = 0;
     bool ok = true;
     for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
-      const FfnUnit u = decode(q, unit, DUAL);
+      const FfnUnit u = decode<MODE>(q, unit);
       const int am = u.m0 + 128 * (int)rank, bn0 = u.n0 + half * (int)rank;
-      for (int seg = 0; ok && seg < SEGMENTS; ++seg) {
+      for (int t = u.k0, blocks; t < u.k1; t += blocks) {
+        const int seg = MODE == FFN_DX && t >= q.n_kb, kb = t - seg * q.n_kb;
         const CUtensorMap* const map_a = &q.a[MODE == FFN_DX ? seg : u.p];
         const CUtensorMap* const map_b = &q.b[MODE == FFN_DX ? seg : u.p];
         const CUtensorMap* const map_b2 = DUAL ? &q.b[1] : map_b;
         const int bn1 = DUAL ? bn0 : bn0 + q.bn;
-        for (int kb = 0; kb < q.n_kb; kb += q.kps) {
-          ok = warp_wait(empty_bar(stage), phase ^ 1u, abort_flag);
-          if (!ok) break;
-          const uint32_t full0 = map_to_cta(full_bar(stage), 0);
-          const int blocks = min(q.kps, q.n_kb - kb);
-          if (rank == 0 && lane == 0) mbar_expect_tx(full_bar(stage), 2 * blocks * (G_A_BYTES + (u.two ? 2 : 1) * b_bytes));
-          __syncwarp();
-          uint32_t dst = base + stage * stage_bytes;
-          for (int k0 = kb * UMMA_BK; k0 < (kb + blocks) * UMMA_BK; k0 += UMMA_BK, dst += block_bytes) {
-            // whatever lies past a matrix's last row or column arrives as zeros
-            if (A_MN) {
-              tma_load_lead(lead, dst, map_a, full0, am, k0);
-              tma_load_lead(lead, dst + 8192, map_a, full0, am + 64, k0);
-            } else {
-              tma_load_lead(lead, dst, map_a, full0, k0, am);
-            }
-            const uint32_t dst_b = dst + G_A_BYTES;
-            if (B_MN) {
-              tma_load_lead(lead, dst_b, map_b, full0, bn0, k0);
-              if (half > 64) tma_load_lead(lead, dst_b + 8192, map_b, full0, bn0 + 64, k0);
-              if (u.two) {
-                tma_load_lead(lead, dst_b + b_bytes, map_b2, full0, bn1, k0);
-                if (half > 64) tma_load_lead(lead, dst_b + b_bytes + 8192, map_b2, full0, bn1 + 64, k0);
-              }
-            } else {
-              tma_load_lead(lead, dst_b, map_b, full0, k0, bn0);
-              if (u.two) tma_load_lead(lead, dst_b + b_bytes, map_b2, full0, k0, bn1);
-            }
+        blocks = min(q.kps, min(q.n_kb - kb, u.k1 - t));
+        ok = warp_wait(empty_bar(stage), phase ^ 1u, abort_flag);
+        if (!ok) break;
+        const uint32_t full0 = map_to_cta(full_bar(stage), 0);
+        if (rank == 0 && lane == 0) mbar_expect_tx(full_bar(stage), 2 * blocks * (G_A_BYTES + (u.two ? 2 : 1) * b_bytes));
+        __syncwarp();
+        uint32_t dst = base + stage * stage_bytes;
+        for (int k0 = kb * UMMA_BK; k0 < (kb + blocks) * UMMA_BK; k0 += UMMA_BK, dst += block_bytes) {
+          // whatever lies past a matrix's last row or column arrives as zeros
+          if (A_MN) {
+            tma_load_lead(lead, dst, map_a, full0, am, k0);
+            tma_load_lead(lead, dst + 8192, map_a, full0, am + 64, k0);
+          } else {
+            tma_load_lead(lead, dst, map_a, full0, k0, am);
           }
-          if (++stage == q.n_stages) { stage = 0; phase ^= 1u; }
+          const uint32_t dst_b = dst + G_A_BYTES;
+          if (B_MN) {
+            tma_load_lead(lead, dst_b, map_b, full0, bn0, k0);
+            if (half > 64) tma_load_lead(lead, dst_b + 8192, map_b, full0, bn0 + 64, k0);
+            if (u.two) {
+              tma_load_lead(lead, dst_b + b_bytes, map_b2, full0, bn1, k0);
+              if (half > 64) tma_load_lead(lead, dst_b + b_bytes + 8192, map_b2, full0, bn1 + 64, k0);
+            }
+          } else {
+            tma_load_lead(lead, dst_b, map_b, full0, k0, bn0);
+            if (u.two) tma_load_lead(lead, dst_b + b_bytes, map_b2, full0, k0, bn1);
+          }
         }
+        if (++stage == q.n_stages) { stage = 0; phase ^= 1u; }
       }
     }
     if (!ok) {               // copies in flight land before the CTA's shared memory is given up
@@ -346,40 +358,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
       const unsigned long long b_first = B_MN ? make_smem_desc_mn(base + G_A_BYTES) : make_smem_desc(base + G_A_BYTES);
       const unsigned long long b2_off = (unsigned long long)(b_bytes >> 4);
       for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
-        const FfnUnit u = decode(q, unit, DUAL);
+        const FfnUnit u = decode<MODE>(q, unit);
         ok = __all_sync(0xffffffffu, mbar_wait_cluster(tempty_bar(acc), acc_phase ^ 1u, abort_flag));
         if (!ok) break;
         tc_fence_after();
         const uint32_t d0 = tmem_base + (uint32_t)(acc * q.nb * q.bn), d1 = d0 + (uint32_t)q.bn;
         uint32_t accumulate = 0;
-        for (int seg = 0; ok && seg < SEGMENTS; ++seg) {
-          for (int kb = 0; kb < q.n_kb; kb += q.kps) {
-            if (!ready) {
-              ok = warp_wait(full_bar(stage), phase, abort_flag);
-              if (!ok) break;
-            }
-            tc_fence_after();
-            unsigned long long at = (unsigned long long)((uint32_t)(stage * stage_bytes) >> 4);
-            const uint32_t done = empty_bar(stage);
-            if (++stage == q.n_stages) { stage = 0; phase ^= 1u; }
-            for (int block = min(q.kps, q.n_kb - kb); block > 0; --block, at += (unsigned long long)(block_bytes >> 4)) {
-              const unsigned long long a_desc = a_first + at, b_desc = b_first + at;
-              if (u.two) {
-                const unsigned long long b2_desc = b_desc + b2_off;
-#pragma unroll
-                for (int k = 0; k < UMMA_BK / 16; ++k) {
-                  umma_lead(lead, d0, a_desc + A_STEP * k, b_desc + B_STEP * k, idesc, accumulate | (uint32_t)k);
-                  umma_lead(lead, d1, a_desc + A_STEP * k, b2_desc + B_STEP * k, idesc, accumulate | (uint32_t)k);
-                }
-              } else {
-                umma_block<A_STEP, B_STEP>(lead, d0, a_desc, b_desc, idesc, accumulate);
-              }
-              accumulate = 1;
-            }
-            // The tensor pipe holds only a few MMAs: a look at the next stage's barrier while they run.
-            ready = __all_sync(0xffffffffu, mbar_test(full_bar(stage), phase));
-            umma_commit_lead(lead, done);
+        for (int t = u.k0, blocks; t < u.k1; t += blocks) {
+          blocks = min(q.kps, u.k1 - t);
+          if (MODE == FFN_DX && t < q.n_kb) blocks = min(blocks, q.n_kb - t);      // a stage holds one segment's blocks
+          if (!ready) {
+            ok = warp_wait(full_bar(stage), phase, abort_flag);
+            if (!ok) break;
           }
+          tc_fence_after();
+          unsigned long long at = (unsigned long long)((uint32_t)(stage * stage_bytes) >> 4);
+          const uint32_t done = empty_bar(stage);
+          if (++stage == q.n_stages) { stage = 0; phase ^= 1u; }
+          for (int block = blocks; block > 0; --block, at += (unsigned long long)(block_bytes >> 4)) {
+            const unsigned long long a_desc = a_first + at, b_desc = b_first + at;
+            if (u.two) {
+              const unsigned long long b2_desc = b_desc + b2_off;
+#pragma unroll
+              for (int k = 0; k < UMMA_BK / 16; ++k) {
+                umma_lead(lead, d0, a_desc + A_STEP * k, b_desc + B_STEP * k, idesc, accumulate | (uint32_t)k);
+                umma_lead(lead, d1, a_desc + A_STEP * k, b2_desc + B_STEP * k, idesc, accumulate | (uint32_t)k);
+              }
+            } else {
+              umma_block<A_STEP, B_STEP>(lead, d0, a_desc, b_desc, idesc, accumulate);
+            }
+            accumulate = 1;
+          }
+          // The tensor pipe holds only a few MMAs: a look at the next stage's barrier while they run.
+          ready = __all_sync(0xffffffffu, mbar_test(full_bar(stage), phase));
+          umma_commit_lead(lead, done);
         }
         if (!ok) break;
         umma_commit_lead(lead, tfull_bar(acc));
@@ -394,7 +406,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
     bool ok = true;
     const int c_first = 16 * (warp >> 2), c_step = 16 * (G_EPI_WARPS / 4);
     for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
-      const FfnUnit u = decode(q, unit, DUAL);
+      const FfnUnit u = decode<MODE>(q, unit);
       const FfnProblem& pr = q.prob[u.p];
       const long long row = (long long)u.m0 + 128 * (int)rank + (warp & 3) * 32 + lane;
       const bool live = row < pr.m;
@@ -470,9 +482,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
         }
       } else {
         __nv_bfloat16* const out = pr.out + row * pr.ld + u.n0;
-        const bool wide = pr.wide;
+        const bool wide = pr.wide, whole = q.splits <= 1;
+        float* const part = q.part + ((long long)u.split * pr.m + row) * pr.n + u.n0;
         auto put = [&](const uint32_t* v, int c) {
           if (!live) return;
+          if (!whole) {                    // n is a multiple of 8 here (d_model)
+            st_global_v8(part + c, v);
+            if (c + 16 <= cols) st_global_v8(part + c + 8, v + 8);
+            return;
+          }
           uint32_t p[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) p[j] = pack_bf16(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
@@ -513,6 +531,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(G_TMEM_COLS) : "memory");
   }
+}
+
+// Sums of the parts of a split k in order, rounded: 8 elements per thread.
+__global__ void __launch_bounds__(256) k_ffn_join(const FfnGemm q) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const long long n = (long long)q.prob[0].m * q.prob[0].n, i = 8 * ((long long)blockIdx.x * 256 + threadIdx.x);
+  if (i >= n) return;
+  float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < q.splits; ++s) {
+    const float4* const src = reinterpret_cast<const float4*>(q.part + s * n + i);
+    const float4 a = src[0], b = src[1];
+    sum[0] += a.x; sum[1] += a.y; sum[2] += a.z; sum[3] += a.w;
+    sum[4] += b.x; sum[5] += b.y; sum[6] += b.z; sum[7] += b.w;
+  }
+  // the output's rows are as long as they are wide (y, dx)
+  *reinterpret_cast<uint4*>(q.prob[0].out + i) = make_uint4(pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]),
+                                                            pack_bf16(sum[4], sum[5]), pack_bf16(sum[6], sum[7]));
 }
 
 // ------------------------------------------------------------------------------------------------ few tokens
@@ -789,71 +825,6 @@ int check_ffn(const camera_ffn_t* f, int64_t T, FfnShape* s) {
 // `saved`: upper halves of G and U, [T][2 fp] 16-bit (a row holds G, then U), then their lower bytes, [T][2 fp].
 size_t saved_lo_offset(const FfnShape& s) { return up256((size_t)4 * s.T * s.fp + 1); }
 
-struct FfnLayout { size_t h, dg, du, total; };
-FfnLayout ffn_layout(const FfnShape& s, bool backward) {
-  FfnLayout l;
-  const size_t act = up256((size_t)2 * s.T * s.fp);
-  l.h = up256(sizeof(PlanTotals));
-  l.dg = l.h + act;
-  l.du = l.dg + act;
-  l.total = backward ? l.du + act : l.dg;
-  return l;
-}
-
-// Columns per B tile and B tiles per work unit: the choice with the least estimated time, rounds of units over the pairs
-// times a unit's time.  Measured per k block (us): 0.60 for 512 columns, of which the products alone take 0.54 at
-// 1.9 GHz; 0.43 for one tile of 256, 0.40 for two of 128; 0.39 for two and 0.32 for one tile of up to 128 columns, where
-// the issue of the MMAs bounds it.  So 512 columns give the
-// highest rate, and fewer give more units where 512 would leave pairs idle.  `epilogue` (us): what a unit of 512 columns,
-// whose accumulators fill tensor memory, adds after its last k block; smaller units have two sets and overlap it.  (8192
-// tokens, d_model 3584, d_ff 2560: dX with 512 columns 231 us, with 256 241 us; 4096 tokens, d_ff 20480: dH with 256
-// columns 650 us, with 512 970 us, whose epilogue reads and writes 12 bytes an element.)
-struct Tile { int bn, nb; };
-Tile choose_tile(long long m_tiles, int n, bool dual, int min_bn, int n_kb, double epilogue, int n_pairs) {
-  Tile best{256, 2};
-  double best_cost = 1e300;
-  for (int bn = 256; bn >= min_bn; bn >>= 1)
-    for (int nb = 2; nb >= (dual ? 2 : 1); --nb) {
-      const int cols = nb * bn, per = dual ? bn : cols;
-      const long long units = m_tiles * ((n + per - 1) / per);
-      const double k_block = cols >= 512 ? 0.60 : bn >= 256 ? 0.43 : cols >= 256 ? 0.40 : nb == 2 ? 0.39 : 0.32;
-      const double cost = (double)((units + n_pairs - 1) / n_pairs) * (n_kb * k_block + (cols >= 512 ? epilogue : 1.0));
-      if (cost < best_cost * 0.99) { best = Tile{bn, nb}; best_cost = cost; }
-    }
-  return best;
-}
-
-bool enc(CUtensorMap* out, const void* p, long long rows, long long cols, long long pitch, int box_rows) {
-  return encode_bf16_2d_pitch(out, p, (uint64_t)rows, (uint64_t)cols, (uint64_t)pitch, (uint32_t)box_rows);
-}
-
-bool wide_rows(const void* p, long long ld) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0 && ld % 16 == 0; }
-
-template <int MODE>
-cudaError_t launch_gemm(FfnGemm& q, Tile t, int n_pairs, bool first, cudaStream_t st) {
-  q.bn = t.bn; q.nb = t.nb;
-  q.clear_status = first;
-  q.n_acc = t.nb * t.bn <= 256 ? 2 : 1;
-  // A stage costs the issuing thread about 400 cycles beside the MMAs of its k blocks (wait, fence, commit), and a k block
-  // of up to 256 columns 409 to 512 cycles of the tensor pipe, which holds too few MMAs to bridge that: such tiles get
-  // two k blocks per stage (256 x 128 tile, K 4096, one unit per pair: 0.42 -> 0.31 us per k block).
-  q.kps = t.nb * t.bn <= 256 ? 2 : 1;
-  const int stage = q.kps * (G_A_BYTES + t.nb * t.bn * 64);
-  q.n_stages = G_RING_BYTES / stage < G_MAX_STAGES ? G_RING_BYTES / stage : G_MAX_STAGES;
-  int units = 0;
-  for (int p = 0; p < q.n_prob; ++p) {
-    const int per = MODE == FFN_GATE_UP ? t.bn : t.nb * t.bn;
-    q.prob[p].n_tiles = (q.prob[p].n + per - 1) / per;
-    q.prob[p].unit0 = units;
-    units += ((q.prob[p].m + G_TILE_M - 1) / G_TILE_M) * q.prob[p].n_tiles;
-  }
-  q.n_units = units;
-  cudaError_t e = allow_smem<k_ffn_gemm<MODE>>(G_SMEM_BYTES);
-  if (e != cudaSuccess) return e;
-  const int pairs = units < n_pairs ? units : n_pairs;
-  return launch_chained(k_ffn_gemm<MODE>, q, 2 * pairs, 1, 1, G_THREADS, G_SMEM_BYTES, !first, st);
-}
-
 int sm_count() {                     // of the process's GPUs, which are all alike
   static std::atomic<int> known;
   int sms = known.load(std::memory_order_relaxed);
@@ -869,6 +840,91 @@ int sm_count() {                     // of the process's GPUs, which are all ali
 }
 
 constexpr int FEW_TOKENS = 64;     // up to here the streaming kernels
+
+// Columns per B tile and B tiles per work unit: the choice with the least estimated time, rounds of units over the pairs
+// times a unit's time.  Measured per k block (us): 0.60 for 512 columns, of which the products alone take 0.54 at
+// 1.9 GHz; 0.43 for one tile of 256, 0.40 for two of 128; 0.39 for two and 0.32 for one tile of up to 128 columns, where
+// the issue of the MMAs bounds it.  So 512 columns give the
+// highest rate, and fewer give more units where 512 would leave pairs idle.  `epilogue` (us): what a unit of 512 columns,
+// whose accumulators fill tensor memory, adds after its last k block; smaller units have two sets and overlap it.  (8192
+// tokens, d_model 3584, d_ff 2560: dX with 512 columns 231 us, with 256 241 us; 4096 tokens, d_ff 20480: dH with 256
+// columns 650 us, with 512 970 us, whose epilogue reads and writes 12 bytes an element.)
+// max_splits > 1: the sum over k may also be cut into parts of their own units, whose fp32 sums a second kernel adds up
+// (4 us and their bytes): with few tiles and a long k, pairs would idle through it.
+struct Tile { int bn, nb, splits; };
+Tile choose_tile(long long m_tiles, int n, bool dual, int min_bn, int n_kb, double epilogue, int max_splits, double part_bytes, int n_pairs) {
+  Tile best{256, 2, 1};
+  double best_cost = 1e300;
+  for (int splits = 1; splits <= max_splits && 4 * splits <= n_kb + 3; ++splits)
+    for (int bn = 256; bn >= min_bn; bn >>= 1)
+      for (int nb = 2; nb >= (dual ? 2 : 1); --nb) {
+        const int cols = nb * bn, per = dual ? bn : cols;
+        const long long units = m_tiles * ((n + per - 1) / per) * splits;
+        const double k_block = cols >= 512 ? 0.60 : bn >= 256 ? 0.43 : cols >= 256 ? 0.40 : nb == 2 ? 0.39 : 0.32;
+        const double join = splits > 1 ? 4.0 + splits * 2.0 * part_bytes / 5.0e6 : 0.0;
+        const double cost = (double)((units + n_pairs - 1) / n_pairs) * ((n_kb + splits - 1) / splits * k_block + (cols >= 512 ? epilogue : 1.0)) + join;
+        if (cost < best_cost * 0.99) { best = Tile{bn, nb, splits}; best_cost = cost; }
+      }
+  return best;
+}
+
+// The tiles of y (one segment of k) and of dX (two).
+Tile out_tile(const FfnShape& s, bool dx, int n_pairs) {
+  const int n_kb = (dx ? 2 : 1) * ((s.F + UMMA_BK - 1) / UMMA_BK);
+  return choose_tile((s.T + G_TILE_M - 1) / G_TILE_M, s.D, false, dx ? 128 : 32, n_kb, 3.0, 8, 4.0 * s.T * s.D, n_pairs);
+}
+
+struct FfnLayout { size_t h, part, dg, du, total; };
+FfnLayout ffn_layout(const FfnShape& s, bool backward) {
+  FfnLayout l;
+  const size_t act = up256((size_t)2 * s.T * s.fp);
+  l.h = up256(sizeof(PlanTotals));
+  l.part = l.h + act;
+  const int n_pairs = sm_count() / 2;
+  int parts = 0;                          // fp32 sums [T][d_model] of a split k
+  if (s.T > FEW_TOKENS) parts = out_tile(s, false, n_pairs).splits;
+  if (backward && s.T > 0 && out_tile(s, true, n_pairs).splits > parts) parts = out_tile(s, true, n_pairs).splits;
+  l.dg = l.part + (parts > 1 ? up256((size_t)4 * parts * s.T * s.D) : 0);
+  l.du = l.dg + act;
+  l.total = backward ? l.du + act : l.dg;
+  return l;
+}
+
+bool enc(CUtensorMap* out, const void* p, long long rows, long long cols, long long pitch, int box_rows) {
+  return encode_bf16_2d_pitch(out, p, (uint64_t)rows, (uint64_t)cols, (uint64_t)pitch, (uint32_t)box_rows);
+}
+
+bool wide_rows(const void* p, long long ld) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0 && ld % 16 == 0; }
+
+template <int MODE>
+cudaError_t launch_gemm(FfnGemm& q, Tile t, int n_pairs, bool first, cudaStream_t st) {
+  q.bn = t.bn; q.nb = t.nb; q.splits = t.splits;
+  q.clear_status = first;
+  q.n_acc = t.nb * t.bn <= 256 ? 2 : 1;
+  // A stage costs the issuing thread about 400 cycles beside the MMAs of its k blocks (wait, fence, commit), and a k block
+  // of up to 256 columns 409 to 512 cycles of the tensor pipe, which holds too few MMAs to bridge that: such tiles get
+  // two k blocks per stage (256 x 128 tile, K 4096, one unit per pair: 0.42 -> 0.31 us per k block).
+  q.kps = t.nb * t.bn <= 256 ? 2 : 1;
+  const int stage = q.kps * (G_A_BYTES + t.nb * t.bn * 64);
+  q.n_stages = G_RING_BYTES / stage < G_MAX_STAGES ? G_RING_BYTES / stage : G_MAX_STAGES;
+  int units = 0;
+  for (int p = 0; p < q.n_prob; ++p) {
+    const int per = MODE == FFN_GATE_UP ? t.bn : t.nb * t.bn;
+    q.prob[p].n_tiles = (q.prob[p].n + per - 1) / per;
+    q.prob[p].unit0 = units;
+    units += ((q.prob[p].m + G_TILE_M - 1) / G_TILE_M) * q.prob[p].n_tiles;
+  }
+  q.tiles = units;
+  units *= t.splits;
+  q.n_units = units;
+  cudaError_t e = allow_smem<k_ffn_gemm<MODE>>(G_SMEM_BYTES);
+  if (e != cudaSuccess) return e;
+  const int pairs = units < n_pairs ? units : n_pairs;
+  e = launch_chained(k_ffn_gemm<MODE>, q, 2 * pairs, 1, 1, G_THREADS, G_SMEM_BYTES, !first, st);
+  if (e != cudaSuccess || t.splits == 1) return e;
+  const long long threads = ((long long)q.prob[0].m * q.prob[0].n + 7) / 8;
+  return launch_chained(k_ffn_join, q, (int)((threads + 255) / 256), 1, 1, 256, 0, true, st);
+}
 
 template <bool GATE_UP, int WK, int R, int NT, int SLOTS, int CTAS>
 cudaError_t launch_few_as(const FfnFew& q, cudaStream_t st) {
@@ -958,6 +1014,7 @@ extern "C" int camera_ffn_forward(const camera_ffn_t* f, const void* x, int64_t 
   q.wait_limit_ns = current_wait_limit_ns();
   q.h = reinterpret_cast<__nv_bfloat16*>(ws + l.h);
   q.h_ld = s.fp;
+  q.part = reinterpret_cast<float*>(ws + l.part);
   q.act_ld = 2 * s.fp;
   q.g = static_cast<uint16_t*>(saved);
   q.u = saved ? q.g + s.fp : nullptr;
@@ -965,14 +1022,14 @@ extern "C" int camera_ffn_forward(const camera_ffn_t* f, const void* x, int64_t 
   q.n_prob = 1;
   q.prob[0] = FfnProblem{(int)s.T, s.F, 0, 0, nullptr, 0, 0};
   q.n_kb = (s.D + UMMA_BK - 1) / UMMA_BK;
-  Tile t = choose_tile(m_tiles, s.F, true, 32, q.n_kb, saved ? 6.0 : 3.0, n_pairs);
+  Tile t = choose_tile(m_tiles, s.F, true, 32, q.n_kb, saved ? 6.0 : 3.0, 1, 0.0, n_pairs);
   if (!enc(&q.a[0], x, s.T, s.D, s.D, 128) || !enc(&q.b[0], f->w_gate, s.F, s.D, s.D, t.bn / 2) ||
       !enc(&q.b[1], f->w_up, s.F, s.D, s.D, t.bn / 2))
     return CAMERA_ERR_CUDA;
   FFN_CK(launch_gemm<FFN_GATE_UP>(q, t, n_pairs, true, st));
   q.prob[0] = FfnProblem{(int)s.T, s.D, 0, 0, static_cast<__nv_bfloat16*>(y), s.D, wide_rows(y, s.D)};
   q.n_kb = (s.F + UMMA_BK - 1) / UMMA_BK;
-  t = choose_tile(m_tiles, s.D, false, 32, q.n_kb, 3.0, n_pairs);
+  t = out_tile(s, false, n_pairs);
   if (!enc(&q.a[0], q.h, s.T, s.F, s.fp, 128) || !enc(&q.b[0], f->w_down, s.D, s.F, s.ld, t.bn / 2)) return CAMERA_ERR_CUDA;
   FFN_CK(launch_gemm<FFN_DOWN>(q, t, n_pairs, false, st));
   return CAMERA_OK;
@@ -1013,6 +1070,7 @@ extern "C" int camera_ffn_backward(const camera_ffn_t* f, const void* x, const v
   q.wait_limit_ns = current_wait_limit_ns();
   q.h = reinterpret_cast<__nv_bfloat16*>(ws + l.h);
   q.h_ld = s.fp;
+  q.part = reinterpret_cast<float*>(ws + l.part);
   q.act_ld = 2 * s.fp;          // dg and du share rows in the workspace as G and U do in `saved`
   q.g = static_cast<uint16_t*>(const_cast<void*>(saved));
   q.u = q.g + s.fp;
@@ -1023,13 +1081,13 @@ extern "C" int camera_ffn_backward(const camera_ffn_t* f, const void* x, const v
   q.n_prob = 1;
   q.prob[0] = FfnProblem{(int)s.T, s.F, 0, 0, nullptr, 0, 0};
   q.n_kb = (s.D + UMMA_BK - 1) / UMMA_BK;
-  Tile t = choose_tile(m_tiles, s.F, false, 128, q.n_kb, 20.0, n_pairs);
+  Tile t = choose_tile(m_tiles, s.F, false, 128, q.n_kb, 20.0, 1, 0.0, n_pairs);
   if (!enc(&q.a[0], dy, s.T, s.D, s.D, 128) || !enc(&q.b[0], f->w_down, s.D, s.F, s.ld, 64)) return CAMERA_ERR_CUDA;
   FFN_CK(launch_gemm<FFN_DH>(q, t, n_pairs, true, st));
   if (dx != nullptr) {
     q.prob[0] = FfnProblem{(int)s.T, s.D, 0, 0, static_cast<__nv_bfloat16*>(dx), s.D, wide_rows(dx, s.D)};
     q.n_kb = (s.F + UMMA_BK - 1) / UMMA_BK;
-    t = choose_tile(m_tiles, s.D, false, 128, 2 * q.n_kb, 3.0, n_pairs);
+    t = out_tile(s, true, n_pairs);
     if (!enc(&q.a[0], q.dg, s.T, s.F, q.act_ld, 128) || !enc(&q.a[1], q.du, s.T, s.F, q.act_ld, 128) ||
         !enc(&q.b[0], f->w_gate, s.F, s.D, s.D, 64) || !enc(&q.b[1], f->w_up, s.F, s.D, s.D, 64))
       return CAMERA_ERR_CUDA;
@@ -1042,7 +1100,7 @@ extern "C" int camera_ffn_backward(const camera_ffn_t* f, const void* x, const v
     q.prob[2] = FfnProblem{s.D, s.F, 0, 0, static_cast<__nv_bfloat16*>(dw_down), s.ld, wide_rows(dw_down, s.ld)};
     q.n_kb = (int)((s.T + UMMA_BK - 1) / UMMA_BK);
     // the third problem has as many tiles as either of the others, up to their edges
-    t = choose_tile(3ll * ((s.F + G_TILE_M - 1) / G_TILE_M), s.D, false, 128, q.n_kb, 3.0, n_pairs);
+    t = choose_tile(3ll * ((s.F + G_TILE_M - 1) / G_TILE_M), s.D, false, 128, q.n_kb, 3.0, 1, 0.0, n_pairs);
     if (!enc(&q.a[0], q.dg, s.T, s.F, q.act_ld, 64) || !enc(&q.a[1], q.du, s.T, s.F, q.act_ld, 64) ||
         !enc(&q.a[2], dy, s.T, s.D, s.D, 64) || !enc(&q.b[0], x, s.T, s.D, s.D, 64) || !enc(&q.b[2], q.h, s.T, s.F, s.fp, 64))
       return CAMERA_ERR_CUDA;
