@@ -32,6 +32,7 @@ namespace {
 
 constexpr int V_THREADS = 256;
 constexpr int V_WARPS = V_THREADS / 32;
+constexpr long long STEP_L2_BYTES = 60ll << 20;   // half of L2
 constexpr int V_MAX_SPLIT = 8;             // CTAs that can share a row
 constexpr float D_FLOOR = -150.f;          // 2^-150 is 0 in fp32: a floor for exponents that multiply a zero weight
 constexpr float REF_SLACK = 3.f;
@@ -1303,6 +1304,10 @@ cudaError_t launch_distill(DistillArgs& a, cudaStream_t st) {
   constexpr bool REST = TAIL && MODE != DISTILL_BACKWARD;
   const int sms = sm_count(), n_vec = a.vocab / Elem<T>::N;
   a.lg = split_for(a.rows, n_vec, sms);
+  // A step reads its rows again from L2: two CTAs share a row where the rows of all CTAs would not stay there beside the
+  // gradients on their way out (4096 rows of 151936 bf16 logits, 90 MB in flight: 688 us unshared, 629 us in pairs; in
+  // fours 827 us, the CTAs then wait for each other more often than the reads gain).
+  if (MODE == DISTILL_STEP && a.lg == 0 && 2ll * sms * n_vec * 16 > STEP_L2_BYTES) a.lg = 1;
   a.mark_words = REST ? ((n_vec >> a.lg) + RingDistill::CHUNK) / RingDistill::CHUNK * (RingDistill::CHUNK / 32) : 0;
   const int smem = RingDistill::BYTES + 8 * a.mark_words;
   return a.lg == 0 ? launch_rows<k_distill<T, MODE, TAIL, false>>(a, VD_THREADS, smem, sms, st)
