@@ -435,7 +435,8 @@ int camera_ffn_backward(const camera_ffn_t* ffn, const void* x, const void* dy, 
  * alignment of the element type.  vocab <= CAMERA_MAX_VOCAB.  The distribution of a row is softmax(x / temperature),
  * 0 < temperature < infinity.  A logit of minus infinity is a token that cannot occur; a row of nothing else has no
  * distribution ("empty", see each call).  A row with a NaN or a logit of plus infinity gives NaN.  All statistics are
- * fp32 sums.  Results do not depend on other rows and are the same bits on every run.  No workspace.
+ * fp32 sums.  A row's results do not depend on what other rows hold; calls of one shape give the same bits on every run.
+ * No workspace, and so no status word: a bounded wait between CTAs that share a row, should it run out, gives that row NaN.
  */
 #define CAMERA_MAX_VOCAB (1 << 20)
 #define CAMERA_MAX_TOP 128
@@ -481,6 +482,8 @@ typedef struct {
  * step: both from one call, for a d_loss known beforehand (a mean over tokens, a mask); loss of a row with d_loss 0 is 0.
  * A row with d_loss 0 has a gradient of 0 and its logits are not read.  An empty row has loss and gradient 0, and so has
  * one whose logits all overflow fp32 to minus infinity when divided by the temperature and multiplied by log2(e).
+ * backward takes lse as fp32: its rounding, 6e-8 of the size of the scaled logits, is a relative error of that gradient;
+ * step has no such error.
  * The factor temperature^2 that some recipes put before the loss goes into d_loss.
  */
 int camera_distill_forward(const camera_distill_t* d, float* loss, float* lse, float* log_tail, void* cuda_stream);

@@ -55,8 +55,8 @@ struct FfnGemm {
   int kps;                  // k blocks per stage of the ring (1 or 2)
   int bn, nb;               // columns per B tile; B tiles per work unit (GATE_UP: 2, one of each matrix)
   int n_stages, n_acc;      // ring depth; accumulator sets in tensor memory
-  uint16_t *g, *u;          // GATE_UP: where to keep G and U (or null); DH: inputs.  Upper halves of the 24 bits kept,
-  long long lo_off;         // with the lower byte of element i of g at ((uint8_t*)base)[lo_off + i], base the start of g's buffer
+  uint16_t *g, *u;          // GATE_UP: where to keep the upper halves of G and U (or null); DH: inputs
+  long long lo_off;         // the lower byte of the element at g + i is at (uint8_t*)g + lo_off + i
   __nv_bfloat16 *dg, *du, *h;   // DH outputs; GATE_UP: h
   long long act_ld, h_ld;   // pitch of g and u, dg and du; of h
   PlanTotals* totals;
@@ -194,7 +194,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 
 // G and U are kept for the backward pass with 24 of their 32 bits (15 of mantissa): rounding them to bf16 would add as
 // much error to the gradients as everything else together (relative error of the weight gradients against 64 bits
-// 3.5e-3 with bf16, 2.4e-3 with 24 bits, of which 1.7e-3 is the rounding of the result).  The cut is a truncation, so that NaN and infinity survive it.
+// 3.5e-3 with bf16, 2.4e-3 with 24 bits, of which 1.7e-3 is the rounding of the result).  The cut is a
+// truncation, so that NaN and infinity survive it.
 __device__ __forceinline__ void keep24(uint16_t* hi, uint8_t* lo, const uint32_t* v) {
   uint32_t h[8];
 #pragma unroll

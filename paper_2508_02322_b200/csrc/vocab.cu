@@ -197,12 +197,13 @@ struct Ring {
   static constexpr int BYTES = SLOTS * CHUNK * 16;
 };
 using RingStream = Ring<8, 3>;       // 96 KB: two CTAs fit an SM
-using RingDistill = Ring<4, 6>;
+using RingDistill = Ring<4, 6>;      // the same bytes in smaller pieces: registers for the second pass
 
 // The logits' way into the CTA: every thread copies its own 16-byte vectors with cp.async into its own places of a ring
 // in shared memory, over the ends of rows: while the sums of a row are joined and its results written, the next row is on
 // its way.  A thread reads only what it copied itself, so there is nothing to wait for but its own copies
-// (cp.async.wait_group) and no barrier.  One copy group is committed per chunk consumed.
+// (cp.async.wait_group) and no barrier.  One copy group is committed per chunk consumed.  twice: every row is sent two
+// times in a row, for the pass that sums it and the pass that writes its gradient.
 template <typename T, typename RG>
 struct Feed {
   const T* logits;
@@ -870,8 +871,8 @@ __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobAr
 //   loss   = sum p (ln p - ln q) [+ rest (ln rest - ln R)],  R = the student's share outside the list
 //   d loss / d x_v = (q_v - p_v) / temperature on the list,  q_v / temperature outside; with the rest as a class the
 //   latter is q_v (1 - rest / R) / temperature, because a token outside moves the rest's share as well.
-// R is summed over the tokens outside (a bitmap in shared memory says which they are), not formed as 1 - Q: once the
-// student is right, R is small and the difference would be noise.  The k terms of the list are taken in double: they are
+// R is summed over the tokens outside, not formed as 1 - Q: once the student is right, R is small and the difference would
+// be noise.  The 16-byte vectors that hold listed tokens are marked, left out by the walk and summed apart.  The k terms of the list are taken in double: they are
 // few, and the loss is a difference of nearly equal logarithms by the end of the training.
 struct DistillArgs {
   const void* logits;
@@ -1157,7 +1158,8 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
         if (!started) { cluster_all_started(); started = true; }
         st = exchange_sums<false, REST>(st, part, parts, a.c, ex, js);
       }
-      careful = !sums_ordinary(st);
+      // a reference that large would swallow digits of log2 s where the two are added (Softmax::k)
+      careful = !sums_ordinary(st) || fabsf(st.ref) > 4096.f;
       if (careful) {
         st = Sums{-FLT_MAX, 0.f, 0.f, 0.f};
         if (!lister) st = walk_careful<T, false, REST>(row, a.c, tl.idx, a.k);
@@ -1306,8 +1308,9 @@ cudaError_t launch_distill(DistillArgs& a, cudaStream_t st) {
   a.lg = split_for(a.rows, n_vec, sms);
   // A step reads its rows again from L2: two CTAs share a row where the rows of all CTAs would not stay there beside the
   // gradients on their way out (4096 rows of 151936 bf16 logits, 90 MB in flight: 688 us unshared, 629 us in pairs; in
-  // fours 827 us, the CTAs then wait for each other more often than the reads gain).
-  if (MODE == DISTILL_STEP && a.lg == 0 && 2ll * sms * n_vec * 16 > STEP_L2_BYTES) a.lg = 1;
+  // fours 827 us, the CTAs then wait for each other more often than the reads gain).  The
+  // loss alone is as fast either way and takes the same split, so that both calls give the same bits.
+  if (MODE != DISTILL_BACKWARD && a.lg == 0 && 2ll * sms * n_vec * 16 > STEP_L2_BYTES) a.lg = 1;
   a.mark_words = REST ? ((n_vec >> a.lg) + RingDistill::CHUNK) / RingDistill::CHUNK * (RingDistill::CHUNK / 32) : 0;
   const int smem = RingDistill::BYTES + 8 * a.mark_words;
   return a.lg == 0 ? launch_rows<k_distill<T, MODE, TAIL, false>>(a, VD_THREADS, smem, sms, st)

@@ -170,7 +170,7 @@ def ref_distill(z, idx, lp, tau, tail, d_loss):
         x = z[r] / tau
         on = np.array([0 <= i < vocab for i in idx[r].tolist()])
         i, l = idx[r].numpy()[on], lp[r][on]
-        if (x == -np.inf).all():
+        if (x * 1.4426950408889634 < -3.4028235e38).all():       # the documented rule for rows without a distribution
             continue
         if tail:
             p, rest = np.exp(l), max(0.0, 1.0 - np.exp(l).sum())
@@ -249,6 +249,38 @@ def test_distill_sizes_strides_alignments(P, dtype, tail, rows, vocab, k, tau, p
     if k == vocab and tail:
         lp = lp - 1e-6          # the whole vocabulary is on the list: what rounding leaves over is dropped
     check_distill(P, padded(z, pad, dtype, shift), idx, lp, tau, tail, d_loss)
+
+
+@pytest.mark.parametrize("dtype,vocab,pad", [(torch.bfloat16, 110001, 7), (torch.float32, 60001, 0)])
+def test_more_long_rows_than_run_at_one_time(P, dtype, vocab, pad):
+    """Every CTA walks several rows, long ones in pairs of CTAs; some do not count, one holds the lowest value only."""
+    rows, k, tau = 321, 40, 1.4
+    z = random_logits(rows, vocab, 12, dtype)
+    z[200] = torch.finfo(dtype).min
+    z[300, vocab // 3:] = -math.inf
+    g = torch.Generator().manual_seed(3)
+    idx = torch.stack([torch.randperm(vocab // 3, generator=g)[:k] for _ in range(rows)]).int()
+    lp = torch.log_softmax(torch.randn(rows, k, generator=g) * 2, 1) - 0.05
+    d_loss = torch.rand(rows, generator=g) + 0.5
+    d_loss[torch.rand(rows, generator=g) < 0.1] = 0.0
+    d_loss[200] = 0.0
+    view = padded(z, pad, dtype)
+    check_distill(P, view, idx, lp, tau, True, d_loss)
+    targets = torch.randint(0, vocab // 3, (rows,), generator=g)
+    check_logprobs(P, view, targets, 30, tau)
+
+
+@pytest.mark.parametrize("offset", [3e3, 1e5, -1e5, 1e8])
+@pytest.mark.parametrize("tail", [False, True])
+def test_step_does_not_depend_on_where_the_logits_lie(P, tail, offset):
+    """Differences decide: logits around a large value have the gradient of the stored values' differences."""
+    z = random_logits(5, 5003, 21, torch.float32) + offset
+    idx, lp = make_list(z - offset, 30, 1.0, 2)
+    d_loss = torch.ones(5)
+    loss, grad = ref_distill(z, idx, lp, 1.0, tail, d_loss)
+    got, g = P.camera_distill_step(z.to(DEV), idx.to(DEV), lp.to(DEV), d_loss.to(DEV), tail=tail)
+    close(got, loss, ABS * np.maximum(1.0, np.abs(loss)))
+    close(g, grad, ABS)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
