@@ -757,7 +757,9 @@ struct Softmax {
 };
 
 // A CTA, or (SPLIT) the CTAs of a cluster together, take row after row: blockIdx.x is the CTA's part of the row,
-// blockIdx.y its first row.
+// blockIdx.y its first row.  Two CTAs an SM with ring chunks of 32 KB: one selects alternatives while the other
+// reads.  4095 rows of 151936 bf16 logits with entropy take 215 us on the device (5.8 TB/s, exponentials at 72 % of their
+// rate; registers in place of the ring: 234 us), 2048 such rows with 64 alternatives 162 us.
 template <typename T, bool ENT, bool TOP, bool SPLIT>
 __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobArgs a) {
   using RG = RingStream;
@@ -1069,8 +1071,10 @@ __device__ __forceinline__ void write_row(const Row<T>& row, T* out, const Softm
 
 // A CTA, or (SPLIT) the CTAs of a cluster together, take row after row, like k_token_logprobs.  STEP sends every row
 // through the ring twice, once to sum it and once to write the gradient; the second time it comes from L2 (see Feed).  The
-// last warp looks after the teacher's lists: while the others sum a row it brings in the next
-// row's, and while they write the gradient it forms the loss.
+// last warp looks after the teacher's lists: while the others sum a row it brings in the next row's, and while they write
+// the gradient it forms the loss.  4096 rows of 151936 bf16 logits with 64 entries: 625 us, 250 to sum them (exponentials,
+// as above) and 380 for the gradient (an exponential, 12 to 15 instructions and a store for each read); reading the logits
+// and writing the gradient once would be 381 us.  250 rows of 32003 fp32 logits, loss alone: 12.6 us.
 constexpr int VD_THREADS = V_THREADS + 32;
 constexpr int VD_LISTS = 3;
 
@@ -1308,8 +1312,8 @@ cudaError_t launch_distill(DistillArgs& a, cudaStream_t st) {
   a.lg = split_for(a.rows, n_vec, sms);
   // A step reads its rows again from L2: two CTAs share a row where the rows of all CTAs would not stay there beside the
   // gradients on their way out (4096 rows of 151936 bf16 logits, 90 MB in flight: 688 us unshared, 629 us in pairs; in
-  // fours 827 us, the CTAs then wait for each other more often than the reads gain).  The
-  // loss alone is as fast either way and takes the same split, so that both calls give the same bits.
+  // fours 827 us, the CTAs then wait for each other more often than the reads gain).  The loss alone is as fast either way
+  // and takes the same split, so that both calls give the same bits.
   if (MODE != DISTILL_BACKWARD && a.lg == 0 && 2ll * sms * n_vec * 16 > STEP_L2_BYTES) a.lg = 1;
   a.mark_words = REST ? ((n_vec >> a.lg) + RingDistill::CHUNK) / RingDistill::CHUNK * (RingDistill::CHUNK / 32) : 0;
   const int smem = RingDistill::BYTES + 8 * a.mark_words;
