@@ -2,7 +2,8 @@
 // alternatives of its distribution, and the distillation loss against a teacher's top log-probabilities with its gradient.
 //
 // With z = x / temperature and c = log2(e) / temperature, a thread takes a reference m (x c for the largest x of the
-// first logits it reads) and sums over its share of the row
+// first chunk it reads that has a logit above -126 / c: a mask at the front of its share does not count) and sums over its
+// share of the row
 //   s = sum 2^(x c - m)   and, for the entropy,   t = sum 2^(x c - m) (x c - m);
 // the threads' sums are joined by scaling with 2^(m_i - max m).  One pass over the row then gives
 //   ln sum exp z = (m + log2 s) ln 2,   log p_v = (x_v c - m - log2 s) ln 2,   H = (log2 s - t / s) ln 2.
@@ -10,7 +11,7 @@
 // no precision in s.  Only the entropy wants it within a few powers of two of the largest logit, because log2 s and t / s
 // cancel (4095 rows: error of the entropies against 64 bits 9.6e-6 without, 6e-7 with): where it is asked for, a thread
 // raises its reference when a chunk's maximum exceeds it by more than 2^REF_SLACK.  A row whose sum ends outside
-// [2^-60, 2^120] (masked at the start, larger further on, all of it the type's lowest value, NaN, infinity: nothing an
+// [2^-60, 2^120] (logits far above a share's first, all of them the type's lowest value, NaN, infinity: nothing an
 // ordinary row does) is walked again with differences formed before the scaling and a running maximum (walk_careful).
 // All sums are fp32 over at most a few hundred terms a thread, then a tree in a fixed order.
 //
@@ -35,6 +36,8 @@ constexpr int V_WARPS = V_THREADS / 32;
 constexpr long long STEP_L2_BYTES = 60ll << 20;   // half of L2
 constexpr int V_MAX_SPLIT = 8;             // CTAs that can share a row
 constexpr float D_FLOOR = -150.f;          // 2^-150 is 0 in fp32: a floor for exponents that multiply a zero weight
+constexpr float D_PART = -100.f;           // the most a sum is scaled down in one step
+constexpr float REF_FLOOR = -126.f;        // references start here
 constexpr float REF_SLACK = 3.f;
 constexpr float LN2 = 0.693147180559945309f;
 constexpr float LOG2E = 1.44269504088896341f;
@@ -158,13 +161,16 @@ struct Row {
 struct Sums {
   float ref, s, t, r;
 };
-// The sums brought to the reference `to` >= ref; ENT and REST say whether t and r are in use.
+// The sums brought to the reference `to` >= ref; ENT and REST say whether t and r are in use.  A share whose reference is
+// far below the largest may all the same hold the largest weights (up to 2^127 of them: logits that start with a mask), so
+// a factor below fp32's range is applied in two parts; the first alone would be flushed to 0 and the share lost.
 template <bool CAREFUL, bool ENT, bool REST>
 __device__ __forceinline__ void raise(Sums& a, float to, float c) {
-  const float d = CAREFUL ? (a.ref - to) * c : a.ref - to, f = ex2(d);
-  if (ENT) a.t = f * fmaf(fmaxf(d, D_FLOOR), a.s, a.t);
-  a.s *= f;
-  if (REST) a.r *= f;
+  const float d = CAREFUL ? (a.ref - to) * c : a.ref - to, d0 = fmaxf(d, D_PART);
+  const float f = ex2(d0), f1 = ex2(d - d0);                 // f1: 1 unless d is below D_PART
+  if (ENT) a.t = f * fmaf(fmaxf(d, D_FLOOR), a.s, a.t) * f1;
+  a.s = a.s * f * f1;
+  if (REST) a.r = a.r * f * f1;
   a.ref = to;
 }
 
@@ -292,13 +298,13 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
   }
   float2 s2 = make_float2(0.f, 0.f), t2 = make_float2(0.f, 0.f);
   const float2 c2 = make_float2(c, c);
-  float2 ref2 = make_float2(0.f, 0.f);
+  float2 ref2 = make_float2(-REF_FLOOR, -REF_FLOOR);         // minus the reference
   float single[2] = {-INFINITY, -INFINITY}, on_list = 0.f;
   if (tid < row.head) single[0] = to_f32<T>(row.p[tid]);
   if (tid < row.tail) single[1] = to_f32<T>(row.p[row.tail_at + tid]);
   const uint8_t* const mine = ring + tid * 16;
   if (REST) mark += tid >> 5;
-  bool first = true;
+  bool unset = true;                                         // no logit above the floor has come by
   int left = row.v_end - row.v_begin;                        // vectors of the part not yet walked
   do {
     uint4 raw[RG::PER];
@@ -321,7 +327,7 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
       }
       mark += RG::CHUNK / 32;
     }
-    if (ENT || TOP || first) {
+    if (ENT || TOP || unset) {
       uint32_t chunk = NI;
 #pragma unroll
       for (int u = 0; u < RG::PER; ++u) {
@@ -330,16 +336,15 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
         chunk = Elem<T>::max_word(chunk, w);
       }
       float m = Elem<T>::max_of(chunk) * c;
-      if (first) {
-        m = fmaxf(fmaxf(m, fmaxf(single[0], single[1]) * c), -126.f);
-        ref2 = make_float2(-m, -m);
-        first = false;
-      } else if (ENT && m > REF_SLACK - ref2.x) {            // the entropy's digits (see above)
+      if (unset) m = fmaxf(m, fmaxf(single[0], single[1]) * c);
+      // the first logits above the floor, or for the entropy's digits (see above) larger ones further on
+      if (unset ? m > REF_FLOOR : ENT && m > REF_SLACK - ref2.x) {
         const float d = -ref2.x - m, f = ex2(d), dd = fmaxf(d, D_FLOOR);
         const float2 f2 = make_float2(f, f), dd2 = make_float2(dd, dd);
-        t2 = mul2(f2, fma2(dd2, s2, t2));
+        if (ENT) t2 = mul2(f2, fma2(dd2, s2, t2));
         s2 = mul2(s2, f2);
         ref2 = make_float2(-m, -m);
+        unset = false;
       }
     }
 #pragma unroll
@@ -950,7 +955,7 @@ __device__ __forceinline__ void load_teacher(const DistillArgs& a, long long r, 
 template <typename T>
 __device__ __forceinline__ Sums mark_list(const Row<T>& row, const TeacherList& tl, int k, float c, uint32_t* mark) {
   constexpr int N = Elem<T>::N;
-  Sums st{-126.f, 0.f, 0.f, 0.f};
+  Sums st{REF_FLOOR, 0.f, 0.f, 0.f};
   for (int j = threadIdx.x & 31; j < k; j += 32) {
     const int i = tl.idx[j];
     if (i < row.first || i >= row.tail_at) continue;
@@ -974,7 +979,7 @@ __device__ __forceinline__ Sums mark_list(const Row<T>& row, const TeacherList& 
     float m = x[0].x;
 #pragma unroll
     for (int q = 0; q < N; ++q) m = fmaxf(m, q & 1 ? x[q >> 1].y : x[q >> 1].x);
-    m = fmaxf(m * c, -126.f);
+    m = fmaxf(m * c, REF_FLOOR);
     if (m > st.ref) raise<false, false, true>(st, m, c);
 #pragma unroll
     for (int q = 0; q < N; ++q) {
@@ -1115,7 +1120,7 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
       if (STATS && part == 0 && tid == 0) a.loss[r] = 0.f;
     }
   }
-  Sums listed{-126.f, 0.f, 0.f, 0.f}, listed_next = listed;          // the lister's: of the vectors with listed tokens
+  Sums listed{REF_FLOOR, 0.f, 0.f, 0.f}, listed_next = listed;          // the lister's: of the vectors with listed tokens
   auto bring_list = [&](int r, TeacherList& tl, uint32_t* mark) {
     if (r >= a.rows) return;
     const Row<T> row(logits + r * a.ld, a.vocab, part, lg);
