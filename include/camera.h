@@ -463,7 +463,8 @@ typedef struct {
   int64_t n_rows;
   int32_t dtype;                  /* camera_dtype_t */
   int32_t vocab;
-  const int32_t* teacher_idx;     /* DEVICE [n_rows, k], distinct in a row; an index outside [0, vocab) is no entry */
+  const int32_t* teacher_idx;     /* DEVICE [n_rows, k], distinct in a row; an index outside [0, vocab) is no entry, unless
+                                     its log-probability is a NaN (what camera_token_logprobs writes for a row with one) */
   const float* teacher_logprob;   /* DEVICE [n_rows, k] log-probabilities at the same temperature (without TAIL any constant may be added) */
   int32_t k;                      /* 1 .. CAMERA_MAX_TOP */
   float temperature;
@@ -474,7 +475,10 @@ typedef struct {
  * Kullback-Leibler divergence of the student from the teacher's list, per row:
  *   loss = sum_j p_j (ln p_j - ln q_j),  p = softmax of the list;
  *   CAMERA_DISTILL_TAIL: p = exp(teacher_logprob), plus rest (ln rest - ln R), rest = max(0, 1 - sum p), R = the
- *   student's probability outside the list (dropped where the student has none there).
+ *   student's probability outside the list (the rest's term is dropped where the student has none there).
+ * The gradient is the derivative of that loss, whatever the list's probabilities add to.  A list without an entry, or
+ * whose entries have no probability, gives loss and gradient 0 without TAIL (with it, all of the teacher is the rest).  A NaN
+ * among a list's log-probabilities gives NaN.
  * forward: loss, and for a later backward lse (ln sum exp(x / temperature)) and, with TAIL, log_tail (the same sum over
  *   the tokens outside the list); lse and log_tail may be NULL.  All DEVICE fp32 [n_rows].
  * backward: d_logits = d_loss[r] d loss_r / d x, rows d_ld elements apart, dtype of the logits; d_logits may be the

@@ -876,8 +876,11 @@ __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobAr
 // Teacher: a list of k tokens with log-probabilities.  p is their softmax over the list, or, with the rest as one more
 // class (TAIL), p = exp(logprob) and rest = 1 - sum p.  Student: q = softmax(x / temperature) over the vocabulary.
 //   loss   = sum p (ln p - ln q) [+ rest (ln rest - ln R)],  R = the student's share outside the list
-//   d loss / d x_v = (q_v - p_v) / temperature on the list,  q_v / temperature outside; with the rest as a class the
-//   latter is q_v (1 - rest / R) / temperature, because a token outside moves the rest's share as well.
+//   d loss / d x_v = (M q_v - p_v) / temperature on the list,  M q_v / temperature outside,  M = sum p [+ rest]; with the
+//   rest as a class the latter is q_v (M - rest / R) / temperature, because a token outside moves the rest's share as well.
+// M is 1 for an ordinary list, 0 for one without an entry (its loss is 0 whatever the logits), above 1 where the listed
+// probabilities add to more (rest is 0 then), and sum p alone where the student has nothing outside and the rest's term is
+// dropped.
 // R is summed over the tokens outside, not formed as 1 - Q: once the student is right, R is small and the difference would
 // be noise.  The 16-byte vectors that hold listed tokens are marked, left out by the walk and summed apart.  The k terms of the list are taken in double: they are
 // few, and the loss is a difference of nearly equal logarithms by the end of the training.
@@ -903,7 +906,7 @@ struct TeacherList {
   float p[CAMERA_MAX_TOP];
   float log_p[CAMERA_MAX_TOP];
   float x[CAMERA_MAX_TOP];            // the student's logits of the listed tokens
-  double rest;
+  double mass, rest;                  // sum of p; NaN if the list holds one
 };
 
 __device__ __forceinline__ double warp_sum(double v) {
@@ -920,7 +923,10 @@ __device__ __forceinline__ void load_teacher(const DistillArgs& a, long long r, 
   for (int j = lane; j < a.k; j += 32) {
     int i = a.idx[r * a.k + j];
     float lp = a.logprob[r * a.k + j];
-    if (i < 0 || i >= a.vocab) { i = -1; lp = -INFINITY; }
+    if (i < 0 || i >= a.vocab) {        // no entry; a NaN stays (-1 / NaN: the teacher's row held one)
+      i = -1;
+      if (lp == lp) lp = -INFINITY;
+    }
     tl.idx[j] = i;
     tl.log_p[j] = lp;
     top = fmaxf(top, lp);
@@ -933,7 +939,10 @@ __device__ __forceinline__ void load_teacher(const DistillArgs& a, long long r, 
       sum += (double)p;                 // 1 - sum would lose the rest's digits in fp32
     }
     sum = warp_sum(sum);
-    if (lane == 0) tl.rest = 1.0 - sum < 0.0 ? 0.0 : 1.0 - sum;      // keeps a NaN
+    if (lane == 0) {
+      tl.mass = sum;
+      tl.rest = 1.0 - sum < 0.0 ? 0.0 : 1.0 - sum;                    // keeps a NaN
+    }
   } else {
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -946,7 +955,10 @@ __device__ __forceinline__ void load_teacher(const DistillArgs& a, long long r, 
       tl.p[j] = sum > 0.0 || sum != sum ? expf(lp) : 0.f;
       tl.log_p[j] = lp;
     }
-    if (lane == 0) tl.rest = 0.0;
+    if (lane == 0) {
+      tl.mass = sum > 0.0 ? 1.0 : sum;
+      tl.rest = 0.0;
+    }
   }
 }
 
@@ -1154,7 +1166,7 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
     uint32_t* const mark = marks + turn * a.mark_words;
     Sums st{-FLT_MAX, 0.f, 0.f, 0.f};        // joins as nothing
     bool careful = false, empty;
-    float coef = 1.f;
+    float mass = 0.f, coef = 0.f;            // M, and what q_v is multiplied by outside the list
     if (lister) {
       listed = listed_next;
       bring_list(r_next, lists[list_next], marks + (turn ^ 1) * a.mark_words);
@@ -1180,7 +1192,11 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
     if (STATS) {
       // no distribution: every logit minus infinity, or all of them beyond fp32's range once scaled
       empty = st.s == 0.f || (careful && st.ref * a.c < -FLT_MAX);
-      if (REST && tl.rest != 0.0) coef = st.r > 0.f || st.r != st.r ? 1.f - (float)tl.rest * (st.s / st.r) : 0.f;
+      mass = coef = (float)tl.mass;
+      if (REST && tl.rest != 0.0 && (st.r > 0.f || st.r != st.r)) {
+        mass = (float)(tl.mass + tl.rest);
+        coef = mass - (float)tl.rest * (st.s / st.r);
+      }
       if (lister) {
         if (REST) unmark_list<T>(row, tl, a.k, mark);
         if (part == 0) {
@@ -1195,6 +1211,7 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
           if (tid == V_THREADS) {
             if (REST && tl.rest != 0.0 && (st.r > 0.f || st.r != st.r))
               loss += tl.rest * (log(tl.rest) - log((double)st.r / (double)st.s));
+            if (tl.mass != tl.mass || st.s != st.s) loss = NAN;         // also where no entry brought it in
             a.loss[r] = empty ? 0.f : (float)loss;
             if (MODE == DISTILL_FORWARD) {
               const float ref = careful ? sm.m * a.inv_tau : sm.m * LN2;
@@ -1208,9 +1225,13 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
       const float lse = a.lse[r];
       empty = lse == -INFINITY;
       sm.k = lse * LOG2E;
+      mass = coef = (float)tl.mass;
       if (TAIL && tl.rest != 0.0) {
         const float lt = a.log_tail[r];
-        coef = lt == -INFINITY ? 0.f : 1.f - (float)tl.rest * expf(lse - lt);
+        if (lt != -INFINITY) {
+          mass = (float)(tl.mass + tl.rest);
+          coef = mass - (float)tl.rest * expf(lse - lt);
+        }
       }
     }
     if (GRAD) {
@@ -1223,7 +1244,7 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
       if (!STATS && SPLIT && a.in_place) cluster_barrier(); else __syncthreads();
       if (tid < a.k && !empty) {
         const int i = tl.idx[tid];
-        if (i >= 0 && row.holds(i)) out[i] = Elem<T>::put(w * (sm.q(tl.x[tid]) - tl.p[tid]));
+        if (i >= 0 && row.holds(i)) out[i] = Elem<T>::put(w * (mass * sm.q(tl.x[tid]) - tl.p[tid]));
       }
     }
     r = r_next;
