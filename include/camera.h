@@ -475,7 +475,7 @@ typedef struct {
  * Kullback-Leibler divergence of the student from the teacher's list, per row:
  *   loss = sum_j p_j (ln p_j - ln q_j),  p = softmax of the list;
  *   CAMERA_DISTILL_TAIL: p = exp(teacher_logprob), plus rest (ln rest - ln R), rest = max(0, 1 - sum p), R = the
- *   student's probability outside the list (the rest's term is dropped where the student has none there).
+ *   student's probability outside the list (below 2^-1022 it counts as none, and the rest's term is dropped).
  * The gradient is the derivative of that loss, whatever the list's probabilities add to.  A list without an entry, or
  * whose entries have no probability, gives loss and gradient 0 without TAIL (with it, all of the teacher is the rest).  A NaN
  * among a list's log-probabilities gives NaN.

@@ -156,22 +156,33 @@ struct Row {
   }
 };
 
-// Sums of a thread, a CTA or a row.  ref: the reference, in powers of two (or, of a careful walk, in logits); r: the part
-// of s from tokens outside the teacher's list.
+// Sums of a thread, a CTA or a row.  ref: the reference of s, in powers of two (or, of a careful walk, in logits).  ENT: t is
+// the entropy's sum.  REST: s counts the tokens outside the teacher's list alone, l those on it against a reference t of
+// their own, so that neither is lost where the other is larger by any factor.
 struct Sums {
-  float ref, s, t, r;
+  float ref, s, t, l;
 };
-// The sums brought to the reference `to` >= ref; ENT and REST say whether t and r are in use.  A share whose reference is
-// far below the largest may all the same hold the largest weights (up to 2^127 of them: logits that start with a mask), so
-// a factor below fp32's range is applied in two parts; the first alone would be flushed to 0 and the share lost.
-template <bool CAREFUL, bool ENT, bool REST>
+template <bool REST>
+__device__ __forceinline__ Sums no_sums() { return Sums{-FLT_MAX, 0.f, REST ? -FLT_MAX : 0.f, 0.f}; }
+// 2^d (d <= 0) times v.  A share whose reference is far below the largest may all the same hold the largest weights (up to
+// 2^127 of them: logits that start with a mask), so a factor below fp32's range is applied in two parts; at once it would be
+// flushed to 0 and the share lost.
+__device__ __forceinline__ float scale_down(float v, float d) {
+  const float d0 = fmaxf(d, D_PART);
+  return v * ex2(d0) * ex2(d - d0);                          // the last is 1 unless d is below D_PART
+}
+// s and (ENT) t brought to the reference `to` >= ref; l to `to` >= t.
+template <bool CAREFUL, bool ENT>
 __device__ __forceinline__ void raise(Sums& a, float to, float c) {
-  const float d = CAREFUL ? (a.ref - to) * c : a.ref - to, d0 = fmaxf(d, D_PART);
-  const float f = ex2(d0), f1 = ex2(d - d0);                 // f1: 1 unless d is below D_PART
-  if (ENT) a.t = f * fmaf(fmaxf(d, D_FLOOR), a.s, a.t) * f1;
-  a.s = a.s * f * f1;
-  if (REST) a.r = a.r * f * f1;
+  const float d = CAREFUL ? (a.ref - to) * c : a.ref - to;
+  if (ENT) a.t = scale_down(fmaf(fmaxf(d, D_FLOOR), a.s, a.t), d);
+  a.s = scale_down(a.s, d);
   a.ref = to;
+}
+template <bool CAREFUL>
+__device__ __forceinline__ void raise_listed(Sums& a, float to, float c) {
+  a.l = scale_down(a.l, CAREFUL ? (a.t - to) * c : a.t - to);
+  a.t = to;
 }
 
 // The rows first, first + stride, .. whose weight is not 0 (null: all rows).  Weights are read one row ahead, so that
@@ -299,9 +310,19 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
   float2 s2 = make_float2(0.f, 0.f), t2 = make_float2(0.f, 0.f);
   const float2 c2 = make_float2(c, c);
   float2 ref2 = make_float2(-REF_FLOOR, -REF_FLOOR);         // minus the reference
-  float single[2] = {-INFINITY, -INFINITY}, on_list = 0.f;
+  float single[2] = {-INFINITY, -INFINITY}, listed[2] = {-INFINITY, -INFINITY};     // of this thread: off and on the list
   if (tid < row.head) single[0] = to_f32<T>(row.p[tid]);
   if (tid < row.tail) single[1] = to_f32<T>(row.p[row.tail_at + tid]);
+  if (REST) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      if (tid >= (q == 0 ? row.head : row.tail)) continue;
+      const int i = q == 0 ? tid : row.tail_at + tid;
+      bool on = false;
+      for (int j = 0; j < k; ++j) on |= list[j] == i;
+      if (on) { listed[q] = single[q]; single[q] = -INFINITY; }
+    }
+  }
   const uint8_t* const mine = ring + tid * 16;
   if (REST) mark += tid >> 5;
   bool unset = true;                                         // no logit above the floor has come by
@@ -374,15 +395,12 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
     if (ENT) d = max_nan(d, D_FLOOR);
     const float e = ex2(d);
     if (ENT) st.t = fmaf(e, d, st.t);
-    bool listed = false;
-    if (REST) {
-      const int i = q == 0 ? tid : row.tail_at + tid;
-      for (int j = 0; j < k; ++j) listed |= list[j] == i;
-    }
-    if (listed) on_list += e; else st.s += e;
+    st.s += e;
   }
-  st.r = st.s;
-  if (REST) st.s += on_list;
+  if (REST) {
+    st.t = fmaxf(fmaxf(listed[0], listed[1]) * c, REF_FLOOR);
+    st.l = ex2(fmaf(listed[0], c, -st.t)) + ex2(fmaf(listed[1], c, -st.t));
+  }
   if (TOP) {
 #pragma unroll
     for (int u = 0; u < RG::PER; ++u) top[u] = Elem<T>::max_of(big[u]);
@@ -392,26 +410,38 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
 }
 
 // The same from global memory, with a running maximum and differences formed before the scaling: right for any row, and
-// how a NaN or an infinite logit (infinity minus itself) shows as a NaN sum, a row of minus infinities as s = 0.
+// how a NaN or an infinite logit (infinity minus itself) shows as a NaN sum, a row of minus infinities as s = 0.  Only
+// elements of marked vectors (see walk_row) and single ones are looked for on the list.
 template <typename T, bool ENT, bool REST>
-__device__ __noinline__ Sums walk_careful(const Row<T> row, float c, const int* list, int k) {
-  Sums st{-FLT_MAX, 0.f, 0.f, 0.f};
-  auto one = [&](int i) {
-    const float x = to_f32<T>(row.p[i]);
-    if (x > st.ref) raise<true, ENT, REST>(st, x, c);
+__device__ __noinline__ Sums walk_careful(const Row<T> row, float c, const uint32_t* mark, const int* list, int k) {
+  constexpr int N = Elem<T>::N;
+  Sums st = no_sums<REST>();
+  auto one = [&](float x, int i, bool look) {
+    if (REST && look) {
+      bool on = false;
+      for (int j = 0; j < k; ++j) on |= list[j] == i;
+      if (on) {
+        if (x > st.t) raise_listed<true>(st, x, c);
+        st.l += ex2((x - st.t) * c);
+        return;
+      }
+    }
+    if (x > st.ref) raise<true, ENT>(st, x, c);
     const float d = (x - st.ref) * c, e = ex2(d);
     st.s += e;
     if (ENT) st.t = fmaf(e, fmaxf(d, D_FLOOR), st.t);
-    if (REST) {
-      bool listed = false;
-      for (int j = 0; j < k; ++j) listed |= list[j] == i;
-      if (!listed) st.r += e;
-    }
   };
-  if ((int)threadIdx.x < row.head) one(threadIdx.x);
-  if ((int)threadIdx.x < row.tail) one(row.tail_at + threadIdx.x);
-  for (int v = row.v_begin + threadIdx.x; v < row.v_end; v += V_THREADS)
-    for (int i = 0; i < Elem<T>::N; ++i) one(row.vec_index(v) + i);
+  if ((int)threadIdx.x < row.head) one(to_f32<T>(row.p[threadIdx.x]), threadIdx.x, true);
+  if ((int)threadIdx.x < row.tail) one(to_f32<T>(row.p[row.tail_at + threadIdx.x]), row.tail_at + threadIdx.x, true);
+  for (int v = row.v_begin + threadIdx.x; v < row.v_end; v += V_THREADS) {
+    const uint4 raw = ld_stream(row.vec(v));
+    const int at = v - row.v_begin;
+    const bool look = REST && ((mark[at >> 5] >> (at & 31)) & 1u);
+    float2 x[N / 2];
+    Elem<T>::pairs(raw, x);
+#pragma unroll
+    for (int i = 0; i < N; ++i) one(i & 1 ? x[i >> 1].y : x[i >> 1].x, row.vec_index(v) + i, look);
+  }
   return st;
 }
 
@@ -424,15 +454,19 @@ struct JoinScratch {
 // The sums of WIDTH neighbouring lanes joined, in all of them.
 template <int WIDTH, bool CAREFUL, bool ENT, bool REST>
 __device__ __forceinline__ Sums join_lanes(Sums st, float c) {
-  float to = st.ref;
+  float to = st.ref, to_l = st.t;
 #pragma unroll
-  for (int o = WIDTH / 2; o; o >>= 1) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, o));
-  raise<CAREFUL, ENT, REST>(st, to, c);
+  for (int o = WIDTH / 2; o; o >>= 1) {
+    to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, o));
+    if (REST) to_l = fmaxf(to_l, __shfl_xor_sync(0xffffffffu, to_l, o));
+  }
+  raise<CAREFUL, ENT>(st, to, c);
+  if (REST) raise_listed<CAREFUL>(st, to_l, c);
 #pragma unroll
   for (int o = WIDTH / 2; o; o >>= 1) {
     st.s += __shfl_xor_sync(0xffffffffu, st.s, o);
     if (ENT) st.t += __shfl_xor_sync(0xffffffffu, st.t, o);
-    if (REST) st.r += __shfl_xor_sync(0xffffffffu, st.r, o);
+    if (REST) st.l += __shfl_xor_sync(0xffffffffu, st.l, o);
   }
   return st;
 }
@@ -446,7 +480,7 @@ __device__ __forceinline__ Sums join_cta(Sums st, float c, int& join_turn, JoinS
   if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = st;
   __syncthreads();
   const int from = threadIdx.x % WIDTH;
-  st = Sums{-FLT_MAX, 0.f, 0.f, 0.f};
+  st = no_sums<REST>();
   if (from < WARPS) st = slots[from];
   return join_lanes<WIDTH, CAREFUL, ENT, REST>(st, c);
 }
@@ -484,7 +518,7 @@ __device__ __forceinline__ void exchange_init(Exchange& ex, unsigned long long* 
 template <bool CAREFUL, bool ENT, bool REST>
 __device__ __forceinline__ Sums join_parts(const Sums* cta, int parts, float c) {
   const int lane = threadIdx.x % V_MAX_SPLIT;
-  Sums st{-FLT_MAX, 0.f, 0.f, 0.f};
+  Sums st = no_sums<REST>();
   if (lane < parts) st = cta[lane];
   return join_lanes<V_MAX_SPLIT, CAREFUL, ENT, REST>(st, c);
 }
@@ -498,7 +532,7 @@ __device__ __forceinline__ Sums exchange_sums(const Sums& own, int part, int par
   if ((int)threadIdx.x < parts) {
     asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
                  ::"r"(map_to_cta(smem_u32(&js.cta[ex.turn][part]), threadIdx.x)), "r"(__float_as_uint(own.ref)),
-                 "r"(__float_as_uint(own.s)), "r"(__float_as_uint(own.t)), "r"(__float_as_uint(own.r)),
+                 "r"(__float_as_uint(own.s)), "r"(__float_as_uint(own.t)), "r"(__float_as_uint(own.l)),
                  "r"(map_to_cta(bar, threadIdx.x))
                  : "memory");
   }
@@ -522,14 +556,18 @@ __device__ __forceinline__ Sums exchange_careful(const Sums& own, int part, int 
     st_cluster_u32(dst, __float_as_uint(own.ref));
     st_cluster_u32(dst + 4, __float_as_uint(own.s));
     st_cluster_u32(dst + 8, __float_as_uint(own.t));
-    st_cluster_u32(dst + 12, __float_as_uint(own.r));
+    st_cluster_u32(dst + 12, __float_as_uint(own.l));
   }
   cluster_barrier();
   const Sums st = join_parts<true, ENT, REST>(js.cta[2], parts, c);
   cluster_barrier();                // nobody overwrites what another still reads
   return st;
 }
-__device__ __forceinline__ bool sums_ordinary(const Sums& st) { return st.s >= 0x1p-60f && st.s <= 0x1p120f; }
+// REST: no bound below for l; what the walk's floor flushes there is nothing beside an ordinary s.
+template <bool REST>
+__device__ __forceinline__ bool sums_ordinary(const Sums& st) {
+  return st.s >= 0x1p-60f && st.s <= 0x1p120f && (!REST || st.l <= 0x1p120f);
+}
 
 // Order-preserving image of a float (both zeros alike) and the 64-bit key by which alternatives are ranked: larger value
 // first, then lower index.
@@ -805,9 +843,9 @@ __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobAr
       if (!started) { cluster_all_started(); started = true; }
       st = exchange_sums<ENT, false>(st, part, parts, a.c, ex, js);
     }
-    const bool careful = !sums_ordinary(st);
+    const bool careful = !sums_ordinary<false>(st);
     if (careful) {
-      st = join_cta<true, ENT, false, V_WARPS>(walk_careful<T, ENT, false>(row, a.c, nullptr, 0), a.c, join_turn, js);
+      st = join_cta<true, ENT, false, V_WARPS>(walk_careful<T, ENT, false>(row, a.c, nullptr, nullptr, 0), a.c, join_turn, js);
       if (SPLIT) st = exchange_careful<ENT, false>(st, part, parts, a.c, js);
     }
     const Softmax sm(st, careful, a.c, a.inv_tau);
@@ -877,12 +915,15 @@ __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobAr
 // class (TAIL), p = exp(logprob) and rest = 1 - sum p.  Student: q = softmax(x / temperature) over the vocabulary.
 //   loss   = sum p (ln p - ln q) [+ rest (ln rest - ln R)],  R = the student's share outside the list
 //   d loss / d x_v = (M q_v - p_v) / temperature on the list,  M q_v / temperature outside,  M = sum p [+ rest]; with the
-//   rest as a class the latter is q_v (M - rest / R) / temperature, because a token outside moves the rest's share as well.
+//   rest as a class the latter is q_v (M - rest / R) / temperature, because a token outside moves the rest's share as well.  It is formed as
+//   (q_v / R) (M R - rest): the student's distribution over the tokens outside, whose weights are of ordinary size however
+//   small R is, times a factor that cannot overflow.
 // M is 1 for an ordinary list, 0 for one without an entry (its loss is 0 whatever the logits), above 1 where the listed
 // probabilities add to more (rest is 0 then), and sum p alone where the student has nothing outside and the rest's term is
 // dropped.
 // R is summed over the tokens outside, not formed as 1 - Q: once the student is right, R is small and the difference would
-// be noise.  The 16-byte vectors that hold listed tokens are marked, left out by the walk and summed apart.  The k terms of the list are taken in double: they are
+// be noise.  It has its own reference, so that it holds down to SHARE_FLOOR; below that (float64's normal range, in which
+// the term is a number) the student counts as having nothing outside.  The 16-byte vectors that hold listed tokens are marked, left out by the walk and summed apart.  The k terms of the list are taken in double: they are
 // few, and the loss is a difference of nearly equal logarithms by the end of the training.
 struct DistillArgs {
   const void* logits;
@@ -900,6 +941,7 @@ struct DistillArgs {
   long long ld_grad;
 };
 enum { DISTILL_FORWARD = 0, DISTILL_BACKWARD = 1, DISTILL_STEP = 2 };
+constexpr float SHARE_FLOOR = -1022.f;       // log2 of the smallest share of the student that counts
 
 struct TeacherList {
   int idx[CAMERA_MAX_TOP];            // -1: no such entry
@@ -962,12 +1004,12 @@ __device__ __forceinline__ void load_teacher(const DistillArgs& a, long long r, 
   }
 }
 
-// Marks the part's vectors that hold listed tokens and sums them, listed and other elements apart (one warp).  Each such
-// vector is looked after by its first entry on the list.
+// Marks the part's vectors that hold listed tokens and sums them, listed and other elements apart, each against their own
+// reference (one warp).  Each such vector is looked after by its first entry on the list.
 template <typename T>
 __device__ __forceinline__ Sums mark_list(const Row<T>& row, const TeacherList& tl, int k, float c, uint32_t* mark) {
   constexpr int N = Elem<T>::N;
-  Sums st{REF_FLOOR, 0.f, 0.f, 0.f};
+  Sums st{REF_FLOOR, 0.f, REF_FLOOR, 0.f};
   for (int j = threadIdx.x & 31; j < k; j += 32) {
     const int i = tl.idx[j];
     if (i < row.first || i >= row.tail_at) continue;
@@ -988,16 +1030,21 @@ __device__ __forceinline__ Sums mark_list(const Row<T>& row, const TeacherList& 
     atomicOr(mark + (at >> 5), 1u << (at & 31));
     float2 x[N / 2];
     Elem<T>::pairs(raw, x);
-    float m = x[0].x;
-#pragma unroll
-    for (int q = 0; q < N; ++q) m = fmaxf(m, q & 1 ? x[q >> 1].y : x[q >> 1].x);
-    m = fmaxf(m * c, REF_FLOOR);
-    if (m > st.ref) raise<false, false, true>(st, m, c);
+    float m = -INFINITY, m_l = -INFINITY;
 #pragma unroll
     for (int q = 0; q < N; ++q) {
-      const float e = ex2(fmaf(q & 1 ? x[q >> 1].y : x[q >> 1].x, c, -st.ref));
-      st.s += e;
-      if (!((listed >> q) & 1u)) st.r += e;
+      const float v_q = q & 1 ? x[q >> 1].y : x[q >> 1].x;
+      if ((listed >> q) & 1u) m_l = fmaxf(m_l, v_q); else m = fmaxf(m, v_q);
+    }
+    m *= c;
+    m_l *= c;
+    if (m > st.ref) raise<false, false>(st, m, c);
+    if (m_l > st.t) raise_listed<false>(st, m_l, c);
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+      const bool on = (listed >> q) & 1u;
+      const float e = ex2(fmaf(q & 1 ? x[q >> 1].y : x[q >> 1].x, c, on ? -st.t : -st.ref));
+      if (on) st.l += e; else st.s += e;
     }
   }
   return st;
@@ -1132,7 +1179,7 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
       if (STATS && part == 0 && tid == 0) a.loss[r] = 0.f;
     }
   }
-  Sums listed{REF_FLOOR, 0.f, 0.f, 0.f}, listed_next = listed;          // the lister's: of the vectors with listed tokens
+  Sums listed{REF_FLOOR, 0.f, REF_FLOOR, 0.f}, listed_next = listed;    // the lister's: of the vectors with listed tokens
   auto bring_list = [&](int r, TeacherList& tl, uint32_t* mark) {
     if (r >= a.rows) return;
     const Row<T> row(logits + r * a.ld, a.vocab, part, lg);
@@ -1164,9 +1211,8 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
     const TeacherList& tl = lists[list];
     const int list_next = list + 1 == VD_LISTS ? 0 : list + 1;
     uint32_t* const mark = marks + turn * a.mark_words;
-    Sums st{-FLT_MAX, 0.f, 0.f, 0.f};        // joins as nothing
+    Sums st = no_sums<REST>();
     bool careful = false, empty;
-    float mass = 0.f, coef = 0.f;            // M, and what q_v is multiplied by outside the list
     if (lister) {
       listed = listed_next;
       bring_list(r_next, lists[list_next], marks + (turn ^ 1) * a.mark_words);
@@ -1180,22 +1226,35 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
         st = exchange_sums<false, REST>(st, part, parts, a.c, ex, js);
       }
       // a reference that large would swallow digits of log2 s where the two are added (Softmax::k)
-      careful = !sums_ordinary(st) || fabsf(st.ref) > 4096.f;
+      careful = !sums_ordinary<REST>(st) || fabsf(st.ref) > 4096.f || (REST && fabsf(st.t) > 4096.f);
       if (careful) {
-        st = Sums{-FLT_MAX, 0.f, 0.f, 0.f};
-        if (!lister) st = walk_careful<T, false, REST>(row, a.c, tl.idx, a.k);
+        st = no_sums<REST>();
+        if (!lister) st = walk_careful<T, false, REST>(row, a.c, mark, tl.idx, a.k);
         st = join_cta<true, false, REST, V_WARPS + 1>(st, a.c, join_turn, js);
         if (SPLIT) st = exchange_careful<false, REST>(st, part, parts, a.c, js);
       }
     }
-    Softmax sm(st, careful, a.c, a.inv_tau);
+    // of the whole row; with the rest as a class from both sums
+    Sums all = st;
+    if (REST) {
+      all.ref = fmaxf(st.ref, st.t);
+      const float unit = careful ? a.c : 1.f;
+      all.s = scale_down(st.s, (st.ref - all.ref) * unit) + scale_down(st.l, (st.t - all.ref) * unit);
+    }
+    Softmax sm(all, careful, a.c, a.inv_tau);
+    // Outside the list the gradient is `scale` times the weight by `out`; M is `mass`
+    Softmax out = sm;
+    float mass = (float)tl.mass, scale = mass;
     if (STATS) {
       // no distribution: every logit minus infinity, or all of them beyond fp32's range once scaled
-      empty = st.s == 0.f || (careful && st.ref * a.c < -FLT_MAX);
-      mass = coef = (float)tl.mass;
-      if (REST && tl.rest != 0.0 && (st.r > 0.f || st.r != st.r)) {
+      empty = all.s == 0.f || (careful && all.ref * a.c < -FLT_MAX);
+      const float to_rest = st.ref - all.ref;                            // REST: ln R = this (scaled) + ln(st.s / all.s)
+      const bool rest = REST && tl.rest != 0.0 &&
+                        !((careful ? to_rest * a.c : to_rest) + log2f(st.s) - sm.log2s < SHARE_FLOOR);       // a NaN counts
+      if (rest) {
         mass = (float)(tl.mass + tl.rest);
-        coef = mass - (float)tl.rest * (st.s / st.r);
+        out = Softmax(st, careful, a.c, a.inv_tau);
+        scale = mass * scale_down(st.s / all.s, careful ? to_rest * a.c : to_rest) - (float)tl.rest;
       }
       if (lister) {
         if (REST) unmark_list<T>(row, tl, a.k, mark);
@@ -1209,14 +1268,15 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
           }
           loss = warp_sum(loss);
           if (tid == V_THREADS) {
-            if (REST && tl.rest != 0.0 && (st.r > 0.f || st.r != st.r))
-              loss += tl.rest * (log(tl.rest) - log((double)st.r / (double)st.s));
-            if (tl.mass != tl.mass || st.s != st.s) loss = NAN;         // also where no entry brought it in
+            if (rest)
+              loss += tl.rest * (log(tl.rest) - log((double)st.s / (double)all.s) -
+                                 (double)to_rest * (careful ? (double)a.inv_tau : 0.6931471805599453));
+            if (tl.mass != tl.mass || all.s != all.s) loss = NAN;       // also where no entry brought it in
             a.loss[r] = empty ? 0.f : (float)loss;
             if (MODE == DISTILL_FORWARD) {
-              const float ref = careful ? sm.m * a.inv_tau : sm.m * LN2;
-              if (a.lse) a.lse[r] = empty ? -INFINITY : ref + sm.log2s * LN2;
-              if (TAIL && a.log_tail) a.log_tail[r] = empty || st.r == 0.f ? -INFINITY : ref + log2f(st.r) * LN2;
+              const float to_ln = careful ? a.inv_tau : LN2;
+              if (a.lse) a.lse[r] = empty ? -INFINITY : sm.m * to_ln + sm.log2s * LN2;
+              if (TAIL && a.log_tail) a.log_tail[r] = empty || st.s == 0.f ? -INFINITY : st.ref * to_ln + log2f(st.s) * LN2;
             }
           }
         }
@@ -1224,27 +1284,28 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
     } else {
       const float lse = a.lse[r];
       empty = lse == -INFINITY;
-      sm.k = lse * LOG2E;
-      mass = coef = (float)tl.mass;
+      sm.k = out.k = lse * LOG2E;
       if (TAIL && tl.rest != 0.0) {
-        const float lt = a.log_tail[r];
-        if (lt != -INFINITY) {
+        const float lt = a.log_tail[r], d = (lt - lse) * LOG2E;
+        if (!(d < SHARE_FLOOR)) {
           mass = (float)(tl.mass + tl.rest);
-          coef = mass - (float)tl.rest * expf(lse - lt);
+          out.k = lt * LOG2E;
+          scale = mass * ex2(d) - (float)tl.rest;
         }
       }
     }
     if (GRAD) {
       // In place: the barriers so far have seen every CTA of the row read its listed logits.
-      T* const out = static_cast<T*>(a.grad) + r * a.ld_grad;
+      T* const grad = static_cast<T*>(a.grad) + r * a.ld_grad;
       const float w = a.d_loss[r] * a.inv_tau;
+      const float on_list = tid < a.k ? w * (mass * sm.q(tl.x[tid]) - tl.p[tid]) : 0.f;
       if (!lister) {
-        write_row<T, RG>(row, out, sm, w * coef, empty, feed, ring, at);
+        write_row<T, RG>(row, grad, out, w * scale, empty, feed, ring, at);
       }
       if (!STATS && SPLIT && a.in_place) cluster_barrier(); else __syncthreads();
       if (tid < a.k && !empty) {
         const int i = tl.idx[tid];
-        if (i >= 0 && row.holds(i)) out[i] = Elem<T>::put(w * (mass * sm.q(tl.x[tid]) - tl.p[tid]));
+        if (i >= 0 && row.holds(i)) grad[i] = Elem<T>::put(on_list);
       }
     }
     r = r_next;
