@@ -325,7 +325,7 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
   }
   const uint8_t* const mine = ring + tid * 16;
   if (REST) mark += tid >> 5;
-  bool unset = true;                                         // no logit above the floor has come by
+  float raise_at = REF_FLOOR;                                // a maximum above this becomes the reference
   int left = row.v_end - row.v_begin;                        // vectors of the part not yet walked
   do {
     uint4 raw[RG::PER];
@@ -348,7 +348,7 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
       }
       mark += RG::CHUNK / 32;
     }
-    if (ENT || TOP || unset) {
+    if (ENT || TOP || raise_at == REF_FLOOR) {
       uint32_t chunk = NI;
 #pragma unroll
       for (int u = 0; u < RG::PER; ++u) {
@@ -356,16 +356,15 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
         if (TOP) big[u] = Elem<T>::max_word(big[u], w);
         chunk = Elem<T>::max_word(chunk, w);
       }
-      float m = Elem<T>::max_of(chunk) * c;
-      if (unset) m = fmaxf(m, fmaxf(single[0], single[1]) * c);
+      const float m = fmaxf(Elem<T>::max_of(chunk), fmaxf(single[0], single[1])) * c;
       // the first logits above the floor, or for the entropy's digits (see above) larger ones further on
-      if (unset ? m > REF_FLOOR : ENT && m > REF_SLACK - ref2.x) {
+      if (m > raise_at) {
         const float d = -ref2.x - m, f = ex2(d), dd = fmaxf(d, D_FLOOR);
         const float2 f2 = make_float2(f, f), dd2 = make_float2(dd, dd);
         if (ENT) t2 = mul2(f2, fma2(dd2, s2, t2));
         s2 = mul2(s2, f2);
         ref2 = make_float2(-m, -m);
-        unset = false;
+        raise_at = ENT ? m + REF_SLACK : INFINITY;
       }
     }
 #pragma unroll
