@@ -877,8 +877,8 @@ __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobAr
         }
       }
       if (part == 0) {
-        int* const out_i = a.top_idx + r * a.top_n;
-        float* const out_v = a.top_logprob + r * a.top_n;
+        int* const out_i = a.top_idx + (long long)r * a.top_n;
+        float* const out_v = a.top_logprob + (long long)r * a.top_n;
         for (int q = tid; q < n_cand; q += V_THREADS) {
           const unsigned long long k = cand[q];
           if (SPLIT && k == 0) continue;
