@@ -192,7 +192,7 @@ int camera_read_status(const void* workspace, void* cuda_stream, int32_t* status
 /*
  * Limit of the waits inside the tensor-core kernels (a thread that waits for a copy or for
  * another warp gives up after this long, the kernel records CAMERA_ERR_DEVICE_TIMEOUT and
- * returns normally).  Process wide, read by every later call; 4 s unless set.  1 us .. 600 s,
+ * returns normally), and of the waits between CTAs that share a row of logits.  Process wide, read by every later call; 4 s unless set.  1 us .. 600 s,
  * else CAMERA_ERR_INVALID_ARG.  The paper has no counterpart: this is the library's error
  * convention (device-side trouble surfaces through the status word, never as a trap or a hang).
  */
@@ -436,7 +436,8 @@ int camera_ffn_backward(const camera_ffn_t* ffn, const void* x, const void* dy, 
  * 0 < temperature < infinity.  A logit of minus infinity is a token that cannot occur; a row of nothing else has no
  * distribution ("empty", see each call).  A row with a NaN or a logit of plus infinity gives NaN.  All statistics are
  * fp32 sums.  A row's results do not depend on what other rows hold; calls of one shape give the same bits on every run.
- * No workspace, and so no status word: a bounded wait between CTAs that share a row, should it run out, gives that row NaN.
+ * No workspace, and so no status word: a bounded wait between CTAs that share a row (camera_set_wait_limit_ns), should it
+ * run out, gives NaN in that row and in the rows those CTAs have left to do.
  */
 #define CAMERA_MAX_VOCAB (1 << 20)
 #define CAMERA_MAX_TOP 128

@@ -447,8 +447,8 @@ __device__ __noinline__ Sums walk_careful(const Row<T> row, float c, const uint3
 // Shared memory of a CTA that joins sums.
 struct JoinScratch {
   Sums warp[2][2 * V_WARPS];       // joins alternate, so that none overwrites what another thread still reads
-  alignas(16) Sums cta[3][V_MAX_SPLIT];    // of the CTAs that share the row, written by each of them (see Exchange)
-  unsigned long long bars[2];
+  alignas(16) Sums cta[2][V_MAX_SPLIT];    // of the CTAs that share the row, written by each of them (see Exchange)
+  unsigned long long bars[3];
 };
 // The sums of WIDTH neighbouring lanes joined, in all of them.
 template <int WIDTH, bool CAREFUL, bool ENT, bool REST>
@@ -484,8 +484,8 @@ __device__ __forceinline__ Sums join_cta(Sums st, float c, int& join_turn, JoinS
   return join_lanes<WIDTH, CAREFUL, ENT, REST>(st, c);
 }
 // The CTAs of a cluster may write to each other's shared memory once all of them run: each says so when it starts and
-// waits for the others where it first needs them.  Barriers of the cluster without .aligned: their callers come out of
-// loops whose lanes end at different times, and the aligned form is an illegal instruction in a warp that is not together.
+// waits for the others where it first needs them.  Without .aligned, which asks for warps whose threads execute the
+// barrier together.
 __device__ __forceinline__ void cluster_started() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_all_started() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ void cluster_barrier() {
@@ -495,24 +495,47 @@ __device__ __forceinline__ void cluster_barrier() {
 }
 // How the CTAs that share a row exchange their sums: each writes its own into every CTA with a store that counts its bytes
 // on that CTA's barrier, and waits until all have come in.  (A cluster barrier would also wait for the gradients written
-// so far.)  Rows alternate between two places: a CTA sends the sums of row i + 2 only after those of row i + 1 have come
-// in from everyone, who had read row i's by then.
+// so far.)  Exchanges alternate between two places: a CTA sends the sums of exchange i + 2 only after those of i + 1 have
+// come in from everyone, who had read exchange i's by then.
+// A wait has a limit.  It cannot run out while the cluster's CTAs run; where one does, the whole CTA takes note (failed),
+// sends and waits no more, and gives NaN for this row and those it has left.  The others then miss its sums and fail
+// at their next exchange in turn, so that every CTA ends.  One that failed leaves last (see exchange_leave).
 struct Exchange {
-  uint32_t bar;                      // two mbarriers
-  uint32_t phase[2];
+  uint32_t bar;                      // three mbarriers: two for sums in turn, one for alternatives (first CTA)
+  uint32_t phase[2], top_phase;
   int turn;
+  bool failed;                       // the same in the whole CTA
+  unsigned long long limit_ns;
 };
-constexpr unsigned long long EXCHANGE_LIMIT_NS = 1000000000ull;
-__device__ __forceinline__ void exchange_init(Exchange& ex, unsigned long long* bars) {
+__device__ __forceinline__ void exchange_init(Exchange& ex, unsigned long long* bars, unsigned long long limit_ns) {
   ex.bar = smem_u32(bars);
-  ex.phase[0] = ex.phase[1] = 0;
+  ex.phase[0] = ex.phase[1] = ex.top_phase = 0;
   ex.turn = 0;
+  ex.failed = false;
+  ex.limit_ns = limit_ns;
   if (threadIdx.x == 0) {
-    mbar_init(ex.bar, 1);
-    mbar_init(ex.bar + 8, 1);
+    for (int i = 0; i < 3; ++i) mbar_init(ex.bar + 8 * i, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncthreads();
+}
+// What the barrier counts has come in; all threads of the CTA wait, and agree on the outcome.
+__device__ __forceinline__ bool exchange_wait(Exchange& ex, uint32_t bar, uint32_t phase) {
+  bool ok = mbar_try_wait_cluster(bar, phase);
+  if (!ok) {
+    const unsigned long long t0 = globaltimer_ns();
+    while (!(ok = mbar_try_wait_cluster(bar, phase)) && globaltimer_ns() - t0 < ex.limit_ns) {}
+  }
+  ex.failed = __syncthreads_or(!ok);
+  return !ex.failed;
+}
+// At the end of the kernel: a CTA that failed may still be written to by others that have not, and stays until all of them
+// have failed as well or are gone (the barrier counts those that ended), and what they sent has landed.
+__device__ __forceinline__ void exchange_leave(const Exchange& ex) {
+  if (!ex.failed) return;
+  cluster_barrier();
+  const unsigned long long t0 = globaltimer_ns();
+  while (globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
 }
 template <bool CAREFUL, bool ENT, bool REST>
 __device__ __forceinline__ Sums join_parts(const Sums* cta, int parts, float c) {
@@ -521,45 +544,26 @@ __device__ __forceinline__ Sums join_parts(const Sums* cta, int parts, float c) 
   if (lane < parts) st = cta[lane];
   return join_lanes<V_MAX_SPLIT, CAREFUL, ENT, REST>(st, c);
 }
-// The row's sums from this CTA's (in every thread of it).  A wait that runs out (it cannot while the cluster's CTAs run)
-// gives NaN.
-template <bool ENT, bool REST>
+// The row's sums from this CTA's (in every thread of it), NaN if the exchange failed.
+template <bool CAREFUL, bool ENT, bool REST>
 __device__ __forceinline__ Sums exchange_sums(const Sums& own, int part, int parts, float c, Exchange& ex, JoinScratch& js) {
   const uint32_t bar = ex.bar + 8 * ex.turn;
-  if (threadIdx.x == 0) mbar_expect_tx(bar, (uint32_t)parts * sizeof(Sums));
-  __syncwarp();
-  if ((int)threadIdx.x < parts) {
-    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
-                 ::"r"(map_to_cta(smem_u32(&js.cta[ex.turn][part]), threadIdx.x)), "r"(__float_as_uint(own.ref)),
-                 "r"(__float_as_uint(own.s)), "r"(__float_as_uint(own.t)), "r"(__float_as_uint(own.l)),
-                 "r"(map_to_cta(bar, threadIdx.x))
-                 : "memory");
+  if (!ex.failed) {
+    if (threadIdx.x == 0) mbar_expect_tx(bar, (uint32_t)parts * sizeof(Sums));
+    __syncwarp();
+    if ((int)threadIdx.x < parts) {
+      asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+                   ::"r"(map_to_cta(smem_u32(&js.cta[ex.turn][part]), threadIdx.x)), "r"(__float_as_uint(own.ref)),
+                   "r"(__float_as_uint(own.s)), "r"(__float_as_uint(own.t)), "r"(__float_as_uint(own.l)),
+                   "r"(map_to_cta(bar, threadIdx.x))
+                   : "memory");
+    }
+    exchange_wait(ex, bar, ex.phase[ex.turn]);
   }
-  bool ok = mbar_try_wait_cluster(bar, ex.phase[ex.turn]);
-  if (!ok) {
-    const unsigned long long t0 = globaltimer_ns();
-    while (!(ok = mbar_try_wait_cluster(bar, ex.phase[ex.turn])) && globaltimer_ns() - t0 < EXCHANGE_LIMIT_NS) {}
-  }
-  ok = __all_sync(0xffffffffu, ok);
-  Sums st = join_parts<false, ENT, REST>(js.cta[ex.turn], parts, c);
-  if (!ok) st.s = NAN;
+  if (ex.failed) return Sums{0.f, NAN, NAN, NAN};
+  const Sums st = join_parts<CAREFUL, ENT, REST>(js.cta[ex.turn], parts, c);
   ex.phase[ex.turn] ^= 1;
   ex.turn ^= 1;
-  return st;
-}
-// The same for the sums of a careful walk, which are rare: with barriers of the whole cluster.
-template <bool ENT, bool REST>
-__device__ __forceinline__ Sums exchange_careful(const Sums& own, int part, int parts, float c, JoinScratch& js) {
-  if ((int)threadIdx.x < parts) {
-    const uint32_t dst = map_to_cta(smem_u32(&js.cta[2][part]), threadIdx.x);
-    st_cluster_u32(dst, __float_as_uint(own.ref));
-    st_cluster_u32(dst + 4, __float_as_uint(own.s));
-    st_cluster_u32(dst + 8, __float_as_uint(own.t));
-    st_cluster_u32(dst + 12, __float_as_uint(own.l));
-  }
-  cluster_barrier();
-  const Sums st = join_parts<true, ENT, REST>(js.cta[2], parts, c);
-  cluster_barrier();                // nobody overwrites what another still reads
   return st;
 }
 // REST: no bound below for l; what the walk's floor flushes there is nothing beside an ordinary s.
@@ -775,6 +779,7 @@ struct LogprobArgs {
   int rows, vocab, top_n;
   int lg;                   // 2^lg CTAs share a row
   float c, inv_tau;         // log2(e) / temperature, 1 / temperature
+  unsigned long long wait_limit_ns;
   const long long* targets;
   float *logprob, *entropy, *top_logprob;
   int* top_idx;
@@ -813,8 +818,9 @@ __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobAr
   const int lg = SPLIT ? a.lg : 0, part = SPLIT ? blockIdx.x : 0, parts = 1 << lg;
   const int tid = threadIdx.x;
   Exchange ex;
+  ex.failed = false;
   if (SPLIT) {
-    exchange_init(ex, js.bars);
+    exchange_init(ex, js.bars, a.wait_limit_ns);
     cluster_started();
   }
   bool started = !SPLIT;
@@ -840,12 +846,12 @@ __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobAr
     st = join_cta<false, ENT, false, V_WARPS>(st, a.c, join_turn, js);
     if (SPLIT) {
       if (!started) { cluster_all_started(); started = true; }
-      st = exchange_sums<ENT, false>(st, part, parts, a.c, ex, js);
+      st = exchange_sums<false, ENT, false>(st, part, parts, a.c, ex, js);
     }
-    const bool careful = !sums_ordinary<false>(st);
+    const bool careful = !ex.failed && !sums_ordinary<false>(st);
     if (careful) {
       st = join_cta<true, ENT, false, V_WARPS>(walk_careful<T, ENT, false>(row, a.c, nullptr, nullptr, 0), a.c, join_turn, js);
-      if (SPLIT) st = exchange_careful<ENT, false>(st, part, parts, a.c, js);
+      if (SPLIT) st = exchange_sums<true, ENT, false>(st, part, parts, a.c, ex, js);
     }
     const Softmax sm(st, careful, a.c, a.inv_tau);
     if (first) {
@@ -854,26 +860,33 @@ __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobAr
     }
     if constexpr (TOP) {
       Scratch& sc = sc_raw;
-      const bool usable = st.s > 0.f;                    // false for a NaN
+      bool usable = st.s > 0.f;                          // false for a NaN
       int n_cand = 0, n_out = 0;
       const unsigned long long* cand = sc.cand;
       if (usable) {
         collect_top<T, RG, Scratch>(row, top, a.top_n, sc);
         __syncthreads();
         n_cand = n_out = sc.n_cand;
-        if (SPLIT) {                                     // this part's best n go to the first CTA
+        if (SPLIT) {                                     // this part's best n go to the first CTA, n from every part
+          const uint32_t bar = ex.bar + 16;
+          if (first) mbar_expect_tx(bar, (uint32_t)(parts * a.top_n * 8));
           for (int q = tid; q < max(n_cand, a.top_n); q += V_THREADS) {
             const unsigned long long k = q < n_cand ? cand[q] : 0ull;
             const int rank = q < n_cand ? rank_among(cand, n_cand, k) : q;
             if (rank < a.top_n) {
-              const uint32_t dst = map_to_cta(smem_u32(&merged[part * a.top_n + rank]), 0);
-              st_cluster_u32(dst, (uint32_t)k);
-              st_cluster_u32(dst + 4, (uint32_t)(k >> 32));
+              asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];"
+                           ::"r"(map_to_cta(smem_u32(&merged[part * a.top_n + rank]), 0)), "l"(k), "r"(map_to_cta(bar, 0))
+                           : "memory");
             }
           }
-          cluster_barrier();
           cand = merged;
           n_cand = n_out = parts * a.top_n;
+          // the next row's alternatives come after its sums, which the others have not had from this CTA before it is
+          // through with these
+          if (part == 0) {
+            if (!exchange_wait(ex, bar, ex.top_phase)) { usable = false; n_cand = n_out = 0; }
+            ex.top_phase ^= 1;
+          }
         }
       }
       if (part == 0) {
@@ -907,6 +920,7 @@ __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobAr
     }
   }
   if (SPLIT && !started) cluster_all_started();
+  if (SPLIT) exchange_leave(ex);
 }
 
 // ---------------------------------------------------------------------------------------------- distillation
@@ -932,6 +946,7 @@ struct DistillArgs {
   int in_place;             // the gradient takes the logits' room
   int mark_words;           // of one set of marks: a bit per vector of a part, rounded up to whole chunks
   float c, inv_tau;
+  unsigned long long wait_limit_ns;
   const int* idx;
   const float* logprob;
   const float* d_loss;
@@ -1156,8 +1171,9 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
   const T* const logits = static_cast<const T*>(a.logits);
   uint32_t* const marks = reinterpret_cast<uint32_t*>(ring + RG::BYTES);
   Exchange ex;
+  ex.failed = false;
   if (SPLIT) {
-    exchange_init(ex, js.bars);
+    exchange_init(ex, js.bars, a.wait_limit_ns);
     cluster_started();
   }
   bool started = !SPLIT;
@@ -1222,15 +1238,15 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
       st = join_cta<false, false, REST, V_WARPS + 1>(st, a.c, join_turn, js);
       if (SPLIT) {
         if (!started) { cluster_all_started(); started = true; }
-        st = exchange_sums<false, REST>(st, part, parts, a.c, ex, js);
+        st = exchange_sums<false, false, REST>(st, part, parts, a.c, ex, js);
       }
       // a reference that large would swallow digits of log2 s where the two are added (Softmax::k)
-      careful = !sums_ordinary<REST>(st) || fabsf(st.ref) > 4096.f || (REST && fabsf(st.t) > 4096.f);
+      careful = !ex.failed && (!sums_ordinary<REST>(st) || fabsf(st.ref) > 4096.f || (REST && fabsf(st.t) > 4096.f));
       if (careful) {
         st = no_sums<REST>();
         if (!lister) st = walk_careful<T, false, REST>(row, a.c, mark, tl.idx, a.k);
         st = join_cta<true, false, REST, V_WARPS + 1>(st, a.c, join_turn, js);
-        if (SPLIT) st = exchange_careful<false, REST>(st, part, parts, a.c, js);
+        if (SPLIT) st = exchange_sums<true, false, REST>(st, part, parts, a.c, ex, js);
       }
     }
     // of the whole row; with the rest as a class from both sums
@@ -1312,6 +1328,7 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
     list = list_next;
   }
   if (SPLIT && !started) cluster_all_started();
+  if (SPLIT) exchange_leave(ex);
 }
 
 // ------------------------------------------------------------------------------------------------ launches
@@ -1442,6 +1459,7 @@ DistillArgs distill_args(const camera_distill_t* d) {
   DistillArgs a;
   a.logits = d->logits; a.ld = d->ld; a.rows = (int)d->n_rows; a.lg = 0; a.in_place = 0; a.mark_words = 0; a.vocab = d->vocab; a.k = d->k;
   a.c = 1.44269504088896341f / d->temperature; a.inv_tau = 1.f / d->temperature;
+  a.wait_limit_ns = current_wait_limit_ns();
   a.idx = d->teacher_idx; a.logprob = d->teacher_logprob;
   a.d_loss = nullptr; a.loss = a.lse = a.log_tail = nullptr; a.grad = nullptr; a.ld_grad = 0;
   return a;
@@ -1460,7 +1478,8 @@ extern "C" int camera_token_logprobs(const void* logits, int32_t dtype, int64_t 
   if (top_n > CAMERA_MAX_TOP) return CAMERA_ERR_UNSUPPORTED_SHAPE;
   if (n_rows == 0) return CAMERA_OK;
   if (top_n > 0 && (top_idx == nullptr || top_logprob == nullptr)) return CAMERA_ERR_INVALID_ARG;
-  LogprobArgs a{logits, ld, (int)n_rows, vocab, top_n, 0, 1.44269504088896341f / temperature, 1.f / temperature, reinterpret_cast<const long long*>(targets),
+  LogprobArgs a{logits, ld, (int)n_rows, vocab, top_n, 0, 1.44269504088896341f / temperature, 1.f / temperature,
+                current_wait_limit_ns(), reinterpret_cast<const long long*>(targets),
                 logprob, entropy, top_logprob, top_idx};
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = dtype == CAMERA_BF16 ? launch_logprobs<__nv_bfloat16>(a, st) : launch_logprobs<float>(a, st);
