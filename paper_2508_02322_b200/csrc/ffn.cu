@@ -15,9 +15,8 @@
 #include <cuda.h>
 #include <string.h>
 
-#include <atomic>
-
 #include "common.cuh"
+#include "launch.cuh"
 #include "umma.cuh"
 #include "umma_pair.cuh"
 
@@ -787,19 +786,6 @@ __global__ void __launch_bounds__(S_THREADS, CTAS) k_ffn_few(const FfnFew q) {
 // ------------------------------------------------------------------------------------------------ host side
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
-// Lets a kernel use `bytes` of dynamic shared memory; asks the driver once per kernel, device and growth.
-template <auto KERN>
-cudaError_t allow_smem(int bytes) {
-  static std::atomic<int> allowed[64];
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  std::atomic<int>& ok = allowed[dev & 63];
-  if (dev < 64 && ok.load(std::memory_order_relaxed) >= bytes) return cudaSuccess;
-  e = cudaFuncSetAttribute(KERN, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess) ok.store(bytes, std::memory_order_relaxed);
-  return e;
-}
 // chained: the kernel may start while the one before it in the stream ends (it waits for that itself, griddepcontrol).
 template <typename A>
 cudaError_t launch_chained(void (*kern)(A), const A& args, int grid_x, int grid_y, int cluster_y, int threads, int smem, bool chained,
@@ -847,20 +833,6 @@ int check_ffn(const camera_ffn_t* f, int64_t T, FfnShape* s) {
 
 // `saved`: upper halves of G and U, [T][2 fp] 16-bit (a row holds G, then U), then their lower bytes, [T][2 fp].
 size_t saved_lo_offset(const FfnShape& s) { return up256((size_t)4 * s.T * s.fp + 1); }
-
-int sm_count() {                     // of the process's GPUs, which are all alike
-  static std::atomic<int> known;
-  int sms = known.load(std::memory_order_relaxed);
-  if (sms == 0) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
-      cudaGetLastError();
-      return 148;
-    }
-    known.store(sms, std::memory_order_relaxed);
-  }
-  return sms;
-}
 
 constexpr int FEW_TOKENS = 64;     // up to here the streaming kernels
 
@@ -938,7 +910,7 @@ cudaError_t launch_gemm(FfnGemm& q, Tile t, int n_pairs, bool first, cudaStream_
   q.tiles = units;
   units *= t.splits;
   q.n_units = units;
-  cudaError_t e = allow_smem<k_ffn_gemm<MODE>>(G_SMEM_BYTES);
+  cudaError_t e = allow_smem<k_ffn_gemm<MODE>, G_SMEM_BYTES>();
   if (e != cudaSuccess) return e;
   const int pairs = units < n_pairs ? units : n_pairs;
   e = launch_chained(k_ffn_gemm<MODE>, q, 2 * pairs, 1, 1, G_THREADS, G_SMEM_BYTES, !first, st);
@@ -951,7 +923,7 @@ template <bool GATE_UP, int WK, int R, int NT, int SLOTS, int CTAS>
 cudaError_t launch_few_as(const FfnFew& q, cudaStream_t st) {
   constexpr int SMEM = SLOTS * R * S_STEP_BYTES, ROWS = (GATE_UP ? 8 : 16) * S_WARPS / WK * R;
   static_assert(SMEM >= S_WARPS * R * NT * 4 * 32 * 4, "the warps' sums take the ring's room");
-  const cudaError_t e = allow_smem<k_ffn_few<GATE_UP, WK, R, NT, SLOTS, CTAS>>(SMEM);
+  const cudaError_t e = allow_smem<k_ffn_few<GATE_UP, WK, R, NT, SLOTS, CTAS>, SMEM>();
   if (e != cudaSuccess) return e;
   const int row_ctas = (q.rows + ROWS - 1) / ROWS, steps = (q.k + 64 * WK - 1) / (64 * WK);
   // split k over a cluster until there is a CTA per SM or a CTA has fewer steps than its ring

@@ -25,6 +25,7 @@
 #include <type_traits>
 
 #include "common.cuh"
+#include "launch.cuh"
 #include "umma_pair.cuh"
 
 namespace camera {
@@ -1332,19 +1333,6 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
 }
 
 // ------------------------------------------------------------------------------------------------ launches
-int sm_count() {                     // of the process's GPUs, which are all alike
-  static std::atomic<int> known;
-  int sms = known.load(std::memory_order_relaxed);
-  if (sms == 0) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
-      cudaGetLastError();
-      return 148;
-    }
-    known.store(sms, std::memory_order_relaxed);
-  }
-  return sms;
-}
 // CTAs that share a row when there are few: as many as keep the grid within two CTAs an SM and two vectors a thread.
 int split_for(int rows, int n_vec, int sms) {
   int lg = 0;
@@ -1364,19 +1352,13 @@ int clusters_at_once(K kern, cudaLaunchConfig_t& cfg, int lg, std::atomic<int>* 
   return n;
 }
 
-template <auto KERN, typename A>
+// MOST: the most shared memory a launch of this kernel takes.
+template <auto KERN, int MOST, typename A>
 cudaError_t launch_rows(const A& args, int threads, int smem, int sms, cudaStream_t st) {
-  static std::atomic<int> known[8], allowed[64];      // per size of cluster; shared memory asked for so far, per device
+  static std::atomic<int> known[8];                   // per size of cluster
   const auto kern = KERN;
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
+  const cudaError_t e = allow_smem<KERN, MOST>();
   if (e != cudaSuccess) return e;
-  std::atomic<int>& ok = allowed[dev & 63];
-  if (dev > 63 || ok.load(std::memory_order_relaxed) < smem) {
-    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
-    ok.store(smem, std::memory_order_relaxed);
-  }
   const int split = 1 << args.lg;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)split, (unsigned)args.rows);
@@ -1399,14 +1381,18 @@ template <typename T, bool ENT, bool TOP>
 cudaError_t launch_logprobs(LogprobArgs& a, cudaStream_t st) {
   const int sms = sm_count();
   a.lg = split_for(a.rows, a.vocab / Elem<T>::N, sms);
-  return a.lg == 0 ? launch_rows<k_token_logprobs<T, ENT, TOP, false>>(a, V_THREADS, RingStream::BYTES, sms, st)
-                   : launch_rows<k_token_logprobs<T, ENT, TOP, true>>(a, V_THREADS, RingStream::BYTES + (a.top_n * 8 << a.lg), sms, st);
+  constexpr int RING = RingStream::BYTES, MOST = RING + (TOP ? V_MAX_SPLIT * CAMERA_MAX_TOP * 8 : 0);
+  return a.lg == 0 ? launch_rows<k_token_logprobs<T, ENT, TOP, false>, RING>(a, V_THREADS, RING, sms, st)
+                   : launch_rows<k_token_logprobs<T, ENT, TOP, true>, MOST>(a, V_THREADS, RING + (a.top_n * 8 << a.lg), sms, st);
 }
 template <typename T>
 cudaError_t launch_logprobs(LogprobArgs& a, cudaStream_t st) {
   if (a.entropy) return a.top_n ? launch_logprobs<T, true, true>(a, st) : launch_logprobs<T, true, false>(a, st);
   return a.top_n ? launch_logprobs<T, false, true>(a, st) : launch_logprobs<T, false, false>(a, st);
 }
+
+// Words of one set of marks for parts of n_vec >> lg vectors, or one more.
+constexpr int mark_words(int n_vec, int lg) { return ((n_vec >> lg) + RingDistill::CHUNK) / RingDistill::CHUNK * (RingDistill::CHUNK / 32); }
 
 template <typename T, int MODE, bool TAIL>
 cudaError_t launch_distill(DistillArgs& a, cudaStream_t st) {
@@ -1418,10 +1404,11 @@ cudaError_t launch_distill(DistillArgs& a, cudaStream_t st) {
   // fours 827 us, the CTAs then wait for each other more often than the reads gain).  The loss alone is as fast either way
   // and takes the same split, so that both calls give the same bits.
   if (MODE != DISTILL_BACKWARD && a.lg == 0 && 2ll * sms * n_vec * 16 > STEP_L2_BYTES) a.lg = 1;
-  a.mark_words = REST ? ((n_vec >> a.lg) + RingDistill::CHUNK) / RingDistill::CHUNK * (RingDistill::CHUNK / 32) : 0;
+  a.mark_words = REST ? mark_words(n_vec, a.lg) : 0;
   const int smem = RingDistill::BYTES + 8 * a.mark_words;
-  return a.lg == 0 ? launch_rows<k_distill<T, MODE, TAIL, false>>(a, VD_THREADS, smem, sms, st)
-                   : launch_rows<k_distill<T, MODE, TAIL, true>>(a, VD_THREADS, smem, sms, st);
+  constexpr int MOST = RingDistill::BYTES + (REST ? 8 * mark_words(CAMERA_MAX_VOCAB / Elem<T>::N, 0) : 0);
+  return a.lg == 0 ? launch_rows<k_distill<T, MODE, TAIL, false>, MOST>(a, VD_THREADS, smem, sms, st)
+                   : launch_rows<k_distill<T, MODE, TAIL, true>, MOST>(a, VD_THREADS, smem, sms, st);
 }
 template <int MODE>
 cudaError_t launch_distill(DistillArgs& a, int dtype, bool tail, cudaStream_t st) {
