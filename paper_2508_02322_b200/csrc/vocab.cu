@@ -520,12 +520,19 @@ __device__ __forceinline__ void exchange_init(Exchange& ex, unsigned long long* 
   }
   __syncthreads();
 }
-// What the barrier counts has come in; all threads of the CTA wait, and agree on the outcome.
+// What the barrier counts has come in: one warp waits, all threads of the CTA agree on the outcome.  The clock is read
+// rarely (a read takes about as long as the exchange, and the CTA would wait for it).
 __device__ __forceinline__ bool exchange_wait(Exchange& ex, uint32_t bar, uint32_t phase) {
-  bool ok = mbar_try_wait_cluster(bar, phase);
-  if (!ok) {
-    const unsigned long long t0 = globaltimer_ns();
-    while (!(ok = mbar_try_wait_cluster(bar, phase)) && globaltimer_ns() - t0 < ex.limit_ns) {}
+  bool ok = true;
+  if (threadIdx.x < 32) {
+    unsigned long long t0 = 0;
+    unsigned spins = 0;
+    while (!(ok = mbar_try_wait_cluster(bar, phase))) {
+      if ((++spins & 31u) != 0u) continue;
+      const unsigned long long now = globaltimer_ns();
+      if (t0 == 0) t0 = now;
+      else if (now - t0 > ex.limit_ns) break;
+    }
   }
   ex.failed = __syncthreads_or(!ok);
   return !ex.failed;
