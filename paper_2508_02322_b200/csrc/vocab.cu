@@ -217,6 +217,10 @@ struct Ring {
 using RingStream = Ring<8, 3>;       // 96 KB: two CTAs fit an SM
 using RingDistill = Ring<4, 6>;      // the same bytes in smaller pieces: registers for the second pass
 
+// A quarter of a warp copies 128 bytes at a time: off a 128-byte boundary in shared memory each such piece takes two
+// requests of L2 (300 rows of 151936 fp32 logits, gradient alone: 3.6 -> 6.4 million requests, 74 -> 84 us).
+constexpr int RING_ALIGN = 128;
+
 // The logits' way into the CTA: every thread copies its own 16-byte vectors with cp.async into its own places of a ring
 // in shared memory, over the ends of rows: while the sums of a row are joined and its results written, the next row is on
 // its way.  A thread reads only what it copied itself, so there is nothing to wait for but its own copies
@@ -818,7 +822,7 @@ struct Softmax {
 template <typename T, bool ENT, bool TOP, bool SPLIT>
 __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobArgs a) {
   using RG = RingStream;
-  extern __shared__ __align__(16) uint8_t ring[];
+  extern __shared__ __align__(RING_ALIGN) uint8_t ring[];
   __shared__ JoinScratch js;
   using Scratch = TopScratch<SPLIT ? 512 : 1024, RG::PER * V_THREADS>;
   __shared__ typename std::conditional<TOP, Scratch, int>::type sc_raw;
@@ -1170,7 +1174,7 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
   constexpr bool GRAD = MODE != DISTILL_FORWARD;
   constexpr bool REST = STATS && TAIL;
   using RG = RingDistill;
-  extern __shared__ __align__(16) uint8_t ring[];     // the ring, then (REST) two sets of marks
+  extern __shared__ __align__(RING_ALIGN) uint8_t ring[];     // the ring, then (REST) two sets of marks
   __shared__ JoinScratch js;
   __shared__ TeacherList lists[VD_LISTS];
   const int lg = SPLIT ? a.lg : 0, part = SPLIT ? blockIdx.x : 0, parts = 1 << lg;
