@@ -35,7 +35,7 @@ namespace {
 constexpr int V_THREADS = 256;
 constexpr int V_WARPS = V_THREADS / 32;
 constexpr long long STEP_L2_BYTES = 60ll << 20;   // half of L2
-constexpr int V_MAX_SPLIT = 8;             // CTAs that can share a row
+constexpr int V_MAX_LG = 3, V_MAX_SPLIT = 1 << V_MAX_LG;       // CTAs that can share a row
 constexpr float D_FLOOR = -150.f;          // 2^-150 is 0 in fp32: a floor for exponents that multiply a zero weight
 constexpr float D_PART = -100.f;           // the most a sum is scaled down in one step
 constexpr float REF_FLOOR = -126.f;        // references start here
@@ -1351,23 +1351,25 @@ int split_for(int rows, int n_vec, int sms) {
   return lg;
 }
 
-// Clusters of 2^lg CTAs that run at one time (a cluster needs SMs of one GPC, so they do not always fill the GPU), asked
-// for once per kernel and size.
-template <typename K>
-int clusters_at_once(K kern, cudaLaunchConfig_t& cfg, int lg, std::atomic<int>* known) {
-  int n = known[lg].load(std::memory_order_relaxed);
-  if (n == 0) {
-    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) { cudaGetLastError(); n = 1; }
-    known[lg].store(n, std::memory_order_relaxed);
-  }
+// Clusters of 2^lg CTAs that run at one time (a cluster needs SMs of one GPC, so they do not always fill the GPU).  Kept per
+// kernel, device and size of cluster for the last amount of shared memory asked about (bytes << 32 | clusters); an answer
+// of the driver that is none is not kept.
+template <auto KERN>
+int clusters_at_once(cudaLaunchConfig_t& cfg, int lg) {
+  static std::atomic<unsigned long long> known[KNOWN_DEVICES][V_MAX_LG + 1];
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return 1; }
+  const bool keep = dev < KNOWN_DEVICES;
+  const unsigned long long seen = keep ? known[dev][lg].load(std::memory_order_relaxed) : 0;
+  if (seen != 0 && seen >> 32 == cfg.dynamicSmemBytes) return (int)(seen & 0xffffffffu);
+  if (cudaOccupancyMaxActiveClusters(&n, KERN, &cfg) != cudaSuccess || n < 1) { cudaGetLastError(); return 1; }
+  if (keep) known[dev][lg].store((unsigned long long)cfg.dynamicSmemBytes << 32 | (unsigned)n, std::memory_order_relaxed);
   return n;
 }
 
 // MOST: the most shared memory a launch of this kernel takes.
 template <auto KERN, int MOST, typename A>
 cudaError_t launch_rows(const A& args, int threads, int smem, int sms, cudaStream_t st) {
-  static std::atomic<int> known[8];                   // per size of cluster
-  const auto kern = KERN;
   const cudaError_t e = allow_smem<KERN, MOST>();
   if (e != cudaSuccess) return e;
   const int split = 1 << args.lg;
@@ -1383,9 +1385,9 @@ cudaError_t launch_rows(const A& args, int threads, int smem, int sms, cudaStrea
   cfg.numAttrs = split > 1 ? 1 : 0;
   // two CTAs fit an SM (one where long rows need more marks); each walks rows until none is left
   int clusters = 2 * sms / split;
-  if (split > 1 && args.rows > clusters / 2) clusters = clusters_at_once(kern, cfg, args.lg, known);
+  if (split > 1 && args.rows > clusters / 2) clusters = clusters_at_once<KERN>(cfg, args.lg);
   if (args.rows > clusters) cfg.gridDim.y = (unsigned)clusters;
-  return cudaLaunchKernelEx(&cfg, kern, args);
+  return cudaLaunchKernelEx(&cfg, KERN, args);
 }
 
 template <typename T, bool ENT, bool TOP>
