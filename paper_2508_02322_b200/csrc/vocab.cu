@@ -1465,6 +1465,13 @@ DistillArgs distill_args(const camera_distill_t* d) {
   return a;
 }
 
+// The status of a call from its launch's; an error is the call's, and not left for the caller's next check to find.
+int launch_status(cudaError_t e) {
+  if (e == cudaSuccess) return CAMERA_OK;
+  cudaGetLastError();
+  return CAMERA_ERR_CUDA;
+}
+
 }  // namespace
 }  // namespace camera
 
@@ -1482,8 +1489,7 @@ extern "C" int camera_token_logprobs(const void* logits, int32_t dtype, int64_t 
                 current_wait_limit_ns(), reinterpret_cast<const long long*>(targets),
                 logprob, entropy, top_logprob, top_idx};
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = dtype == CAMERA_BF16 ? launch_logprobs<__nv_bfloat16>(a, st) : launch_logprobs<float>(a, st);
-  return e == cudaSuccess ? CAMERA_OK : CAMERA_ERR_CUDA;
+  return launch_status(dtype == CAMERA_BF16 ? launch_logprobs<__nv_bfloat16>(a, st) : launch_logprobs<float>(a, st));
 }
 
 extern "C" int camera_distill_forward(const camera_distill_t* d, float* loss, float* lse, float* log_tail, void* cuda_stream) {
@@ -1494,8 +1500,7 @@ extern "C" int camera_distill_forward(const camera_distill_t* d, float* loss, fl
   if (loss == nullptr) return CAMERA_ERR_INVALID_ARG;
   DistillArgs a = distill_args(d);
   a.loss = loss; a.lse = lse; a.log_tail = log_tail;
-  return launch_distill<DISTILL_FORWARD>(a, d->dtype, d->flags & CAMERA_DISTILL_TAIL,
-                                         static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CAMERA_OK : CAMERA_ERR_CUDA;
+  return launch_status(launch_distill<DISTILL_FORWARD>(a, d->dtype, d->flags & CAMERA_DISTILL_TAIL, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 extern "C" int camera_distill_backward(const camera_distill_t* d, const float* d_loss, const float* lse, const float* log_tail,
@@ -1510,8 +1515,7 @@ extern "C" int camera_distill_backward(const camera_distill_t* d, const float* d
   DistillArgs a = distill_args(d);
   a.d_loss = d_loss; a.lse = const_cast<float*>(lse); a.log_tail = const_cast<float*>(log_tail);
   a.grad = d_logits; a.ld_grad = d_ld; a.in_place = d_logits == d->logits;
-  return launch_distill<DISTILL_BACKWARD>(a, d->dtype, d->flags & CAMERA_DISTILL_TAIL,
-                                          static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CAMERA_OK : CAMERA_ERR_CUDA;
+  return launch_status(launch_distill<DISTILL_BACKWARD>(a, d->dtype, d->flags & CAMERA_DISTILL_TAIL, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 extern "C" int camera_distill_step(const camera_distill_t* d, const float* d_loss, float* loss, void* d_logits, int64_t d_ld,
@@ -1523,6 +1527,5 @@ extern "C" int camera_distill_step(const camera_distill_t* d, const float* d_los
   if (d_loss == nullptr || loss == nullptr || !grad_ok(d, d_logits, d_ld)) return CAMERA_ERR_INVALID_ARG;
   DistillArgs a = distill_args(d);
   a.d_loss = d_loss; a.loss = loss; a.grad = d_logits; a.ld_grad = d_ld; a.in_place = d_logits == d->logits;
-  return launch_distill<DISTILL_STEP>(a, d->dtype, d->flags & CAMERA_DISTILL_TAIL,
-                                      static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? CAMERA_OK : CAMERA_ERR_CUDA;
+  return launch_status(launch_distill<DISTILL_STEP>(a, d->dtype, d->flags & CAMERA_DISTILL_TAIL, static_cast<cudaStream_t>(cuda_stream)));
 }
