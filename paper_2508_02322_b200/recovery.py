@@ -25,6 +25,21 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _enqueue(fn, t: torch.Tensor, *args) -> None:
+    """The C call `fn` on the device of t, whichever device is current, and on that device's current stream."""
+    device = t.get_device()
+    if device == _current_device():
+        status = fn(*args, _raw_stream(device))
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, _raw_stream(device))
+    if status:
+        _check(status, fn.__name__)
+
+
 def _elsewhere(stream: Optional[torch.cuda.Stream], fn, *args, **kw):
     """The call with `stream` as the current one, so that what it allocates belongs there."""
     with torch.cuda.stream(stream):
@@ -91,13 +106,24 @@ def camera_ffn_saved_bytes(ffn: Ffn, n_tokens: int) -> int:
 def _tokens(t: torch.Tensor, ffn: Ffn, name: str) -> int:
     if t.dtype is not _BF16 or t.dim() != 2 or t.shape[1] != ffn.d_model or not t.is_contiguous() or t.device != ffn.device:
         raise ValueError(f"{name} must be a contiguous bf16 [n_tokens, d_model] tensor on the device of the block")
+    if not t.is_cuda:
+        raise ValueError(f"the block and {name} must be on a GPU")
     return t.data_ptr()
 
 
 def _saved(saved: torch.Tensor, ffn: Ffn, n_tokens: int) -> int:
-    if saved.numel() * saved.element_size() < camera_ffn_saved_bytes(ffn, n_tokens) or saved.device != ffn.device:
-        raise ValueError("saved must have camera_ffn_saved_bytes bytes on the device of the block")
+    if saved.numel() * saved.element_size() < camera_ffn_saved_bytes(ffn, n_tokens) or saved.device != ffn.device or \
+            not saved.is_contiguous():
+        raise ValueError("saved must have camera_ffn_saved_bytes contiguous bytes on the device of the block")
     return saved.data_ptr()
+
+
+def _workspace(workspace: Optional[torch.Tensor], ffn: Ffn, n_tokens: int, backward: bool) -> torch.Tensor:
+    if workspace is None:
+        return alloc_workspace(camera_ffn_workspace_bytes(ffn, n_tokens, backward=backward), ffn.device)
+    if workspace.device != ffn.device or not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous, on the device of the block")
+    return workspace
 
 
 def camera_ffn_forward(ffn: Ffn, x: torch.Tensor, *, y: Optional[torch.Tensor] = None, saved: Optional[torch.Tensor] = None,
@@ -113,10 +139,9 @@ def camera_ffn_forward(ffn: Ffn, x: torch.Tensor, *, y: Optional[torch.Tensor] =
         y = torch.empty_like(x)
     elif _tokens(y, ffn, "y") is None or y.shape[0] != n:
         raise ValueError("y must have the shape of x")
-    if workspace is None:
-        workspace = alloc_workspace(camera_ffn_workspace_bytes(ffn, n), ffn.device)
-    _check(lib.camera_ffn_forward(ffn._ref, xp, n, y.data_ptr(), None if saved is None else _saved(saved, ffn, n),
-                                  workspace.data_ptr(), workspace.numel(), _raw_stream(x.get_device())), "camera_ffn_forward")
+    workspace = _workspace(workspace, ffn, n, False)
+    _enqueue(lib.camera_ffn_forward, x, ffn._ref, xp, n, y.data_ptr(), None if saved is None else _saved(saved, ffn, n),
+             workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return y
 
 
@@ -148,10 +173,9 @@ def camera_ffn_backward(ffn: Ffn, x: torch.Tensor, dy: torch.Tensor, saved: torc
             raise ValueError(f"out[{name!r}] must be a contiguous bf16 tensor of shape {(rows, cols)}")
         res[name] = t
         ptr[i] = t.data_ptr()
-    if workspace is None:
-        workspace = alloc_workspace(camera_ffn_workspace_bytes(ffn, n, backward=True), ffn.device)
-    _check(lib.camera_ffn_backward(ffn._ref, xp, dyp, n, sp, ptr[0], ptr[1], ptr[2], ptr[3], workspace.data_ptr(),
-                                   workspace.numel(), _raw_stream(x.get_device())), "camera_ffn_backward")
+    workspace = _workspace(workspace, ffn, n, True)
+    _enqueue(lib.camera_ffn_backward, x, ffn._ref, xp, dyp, n, sp, ptr[0], ptr[1], ptr[2], ptr[3], workspace.data_ptr(),
+             workspace.numel() * workspace.element_size())
     return res
 
 
@@ -180,10 +204,8 @@ def camera_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] 
         i_ptr = t.data_ptr()
         out["top_logprob"] = t = torch.empty(rows, top_n, dtype=_F32, device=dev)
         v_ptr = t.data_ptr()
-    status = lib.camera_token_logprobs(logits.data_ptr(), _DTYPE[logits.dtype], ld, rows, vocab, t_ptr, top_n, temperature,
-                                       lp_ptr, h_ptr, i_ptr, v_ptr, _raw_stream(logits.get_device()))
-    if status:
-        _check(status, "camera_token_logprobs")
+    _enqueue(lib.camera_token_logprobs, logits, logits.data_ptr(), _DTYPE[logits.dtype], ld, rows, vocab, t_ptr, top_n, temperature,
+             lp_ptr, h_ptr, i_ptr, v_ptr)
     return out
 
 
@@ -219,8 +241,8 @@ def camera_distill_forward(logits: torch.Tensor, teacher_idx: torch.Tensor, teac
     d = _distill(logits, teacher_idx, teacher_logprob, temperature, tail)
     out = {name: torch.empty(d.n_rows, dtype=_F32, device=logits.device)
            for name in (("loss", "lse", "log_tail") if tail else ("loss", "lse"))}
-    _check(lib.camera_distill_forward(C.byref(d), out["loss"].data_ptr(), out["lse"].data_ptr(),
-                                      out["log_tail"].data_ptr() if tail else None, _raw_stream(logits.get_device())), "camera_distill_forward")
+    _enqueue(lib.camera_distill_forward, logits, C.byref(d), out["loss"].data_ptr(), out["lse"].data_ptr(),
+             out["log_tail"].data_ptr() if tail else None)
     return out
 
 
@@ -239,10 +261,9 @@ def camera_distill_backward(logits: torch.Tensor, teacher_idx: torch.Tensor, tea
     if tail and log_tail is None:
         raise ValueError("log_tail is needed with tail=True")
     d_logits, d_ld = _gradient(logits, d_logits, d.ld)
-    _check(lib.camera_distill_backward(C.byref(d), _vector(d_loss, logits, torch.float32, rows, "d_loss"),
-                                       _vector(lse, logits, torch.float32, rows, "lse"),
-                                       _vector(log_tail, logits, torch.float32, rows, "log_tail") if tail else None,
-                                       d_logits.data_ptr(), d_ld, _raw_stream(logits.get_device())), "camera_distill_backward")
+    _enqueue(lib.camera_distill_backward, logits, C.byref(d), _vector(d_loss, logits, torch.float32, rows, "d_loss"),
+             _vector(lse, logits, torch.float32, rows, "lse"),
+             _vector(log_tail, logits, torch.float32, rows, "log_tail") if tail else None, d_logits.data_ptr(), d_ld)
     return d_logits
 
 
@@ -257,6 +278,6 @@ def camera_distill_step(logits: torch.Tensor, teacher_idx: torch.Tensor, teacher
     d = _distill(logits, teacher_idx, teacher_logprob, temperature, tail)
     d_logits, d_ld = _gradient(logits, d_logits, d.ld)
     loss = torch.empty(d.n_rows, dtype=_F32, device=logits.device)
-    _check(lib.camera_distill_step(C.byref(d), _vector(d_loss, logits, torch.float32, (d.n_rows,), "d_loss"),
-                                   loss.data_ptr(), d_logits.data_ptr(), d_ld, _raw_stream(logits.get_device())), "camera_distill_step")
+    _enqueue(lib.camera_distill_step, logits, C.byref(d), _vector(d_loss, logits, torch.float32, (d.n_rows,), "d_loss"),
+             loss.data_ptr(), d_logits.data_ptr(), d_ld)
     return loss, d_logits
