@@ -222,8 +222,11 @@ def _distill(logits, teacher_idx, teacher_logprob, temperature, tail) -> camera_
 
 
 def _gradient(logits: torch.Tensor, d_logits: Optional[torch.Tensor], ld: int) -> Tuple[torch.Tensor, int]:
-    """The gradient's tensor (allocated with the pitch of the logits, so that both are aligned alike) and its pitch."""
+    """The gradient's tensor and its pitch: where it is allocated, the vocabulary and what aligns its rows to 16 bytes as
+    those of the logits are, however far apart they lie."""
     if d_logits is None:
+        vocab = logits.shape[1]
+        ld = vocab + (ld - vocab) % (16 // logits.element_size())
         return torch.empty_strided(logits.shape, (ld, 1), dtype=logits.dtype, device=logits.device), ld
     if d_logits.shape != logits.shape or d_logits.dtype != logits.dtype or d_logits.device != logits.device:
         raise ValueError("d_logits must have the shape, dtype and device of the logits")

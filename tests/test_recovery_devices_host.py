@@ -81,3 +81,16 @@ def test_calls_go_to_the_tensors_device(P, monkeypatch):
     with pytest.raises(P.CameraError, match="camera_refused"):
         recovery._enqueue(camera_refused, OnDevice(1))
     assert current[0] == 0
+
+
+def test_the_gradients_room_follows_the_vocabulary_not_the_pitch(P):
+    from paper_2508_02322_b200 import recovery
+    z = torch.zeros(4, 50, 1000, dtype=torch.bfloat16)[:, -1]             # the last position of every sequence
+    g, ld = recovery._gradient(z, None, z.stride(0))
+    assert g.shape == z.shape and g.stride() == (ld, 1)
+    assert g.untyped_storage().nbytes() <= 2 * 4 * 1008
+    for vocab, pitch, dtype in ((1000, 1003, torch.bfloat16), (1001, 1001, torch.bfloat16), (999, 7777, torch.float32), (8, 8, torch.float32)):
+        z = torch.zeros(3, pitch, dtype=dtype)[:, :vocab]
+        g, ld = recovery._gradient(z, None, pitch)
+        per = 16 // z.element_size()
+        assert vocab <= ld < vocab + per and (ld - pitch) % per == 0     # rows aligned like those of the logits
