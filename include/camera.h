@@ -404,7 +404,9 @@ typedef struct {
 
 /* Scratch of camera_ffn_forward (backward = 0) and of camera_ffn_backward (1, which serves forward as well); size of the
  * gate and up products a forward call keeps for its backward call.  0 on invalid arguments.  The workspace starts with
- * a status word that camera_read_status reads. */
+ * a status word that camera_read_status reads.  A workspace of this size serves every call with no more tokens and no
+ * larger d_ff (of the same d_model) as well, although the query may name more for some of them: a call cuts its sums over
+ * d_ff into as many parts as it finds room for. */
 size_t camera_ffn_workspace_bytes(const camera_ffn_t* ffn, int64_t n_tokens, int32_t backward);
 size_t camera_ffn_saved_bytes(const camera_ffn_t* ffn, int64_t n_tokens);
 
@@ -421,7 +423,7 @@ int camera_ffn_forward(const camera_ffn_t* ffn, const void* x, int64_t n_tokens,
  * [n_tokens, d_model], dw_gate and dw_up [d_ff, d_model], dw_down [d_model, down_ld] (columns from d_ff on are not
  * written), all bf16, overwritten.  dx may be NULL; dw_* may be NULL together.  The gate and up products are kept, and
  * their gradients formed, in bf16 (rounded once from fp32); the sums over tokens and micro-experts are fp32.  `saved` is
- * left as it is.  Results are the same bits on every run.
+ * left as it is.  Results (of the forward call too) are the same bits on every run with a workspace of the same size.
  */
 int camera_ffn_backward(const camera_ffn_t* ffn, const void* x, const void* dy, int64_t n_tokens, const void* saved, void* dx,
                         void* dw_gate, void* dw_up, void* dw_down, void* workspace, size_t workspace_bytes,

@@ -863,25 +863,32 @@ Tile choose_tile(long long m_tiles, int n, bool dual, int min_bn, int n_kb, doub
   return best;
 }
 
-// The tiles of y (one segment of k) and of dX (two).
-Tile out_tile(const FfnShape& s, bool dx, int n_pairs) {
+// The tiles of y (one segment of k) and of dX (two).  room: bytes for the fp32 sums [T][d_model] of the parts of a split k.
+constexpr int MAX_PARTS = 8;
+Tile out_tile(const FfnShape& s, bool dx, int n_pairs, size_t room) {
   const int n_kb = (dx ? 2 : 1) * ((s.F + UMMA_BK - 1) / UMMA_BK);
-  return choose_tile((s.T + G_TILE_M - 1) / G_TILE_M, s.D, false, dx ? 128 : 32, n_kb, 3.0, 8, 4.0 * s.T * s.D, n_pairs);
+  const size_t fit = room / ((size_t)4 * s.T * s.D);
+  return choose_tile((s.T + G_TILE_M - 1) / G_TILE_M, s.D, false, dx ? 128 : 32, n_kb, 3.0, fit < MAX_PARTS ? (fit > 1 ? (int)fit : 1) : MAX_PARTS,
+                     4.0 * s.T * s.D, n_pairs);
 }
 
-struct FfnLayout { size_t h, part, dg, du, total; };
+// What a call cannot do without grows with tokens and d_ff; the parts of a split k, which a smaller call may want more
+// of, come last and take what room there is.  So a workspace of the query's size serves every smaller call.
+struct FfnLayout { size_t h, dg, part, total; };     // dg: its rows hold dU behind dG; total: with all the parts wanted
 FfnLayout ffn_layout(const FfnShape& s, bool backward) {
   FfnLayout l;
   const size_t act = up256((size_t)2 * s.T * s.fp);
   l.h = up256(sizeof(PlanTotals));
-  l.part = l.h + act;
+  l.dg = l.h + act;
+  l.part = l.dg + (backward ? 2 * act : 0);
   const int n_pairs = sm_count() / 2;
-  int parts = 0;                          // fp32 sums [T][d_model] of a split k
-  if (s.T > FEW_TOKENS) parts = out_tile(s, false, n_pairs).splits;
-  if (backward && s.T > 0 && out_tile(s, true, n_pairs).splits > parts) parts = out_tile(s, true, n_pairs).splits;
-  l.dg = l.part + (parts > 1 ? up256((size_t)4 * parts * s.T * s.D) : 0);
-  l.du = l.dg + act;
-  l.total = backward ? l.du + act : l.dg;
+  int parts = 0;
+  if (s.T > FEW_TOKENS) parts = out_tile(s, false, n_pairs, ~(size_t)0).splits;
+  if (backward && s.T > 0) {
+    const int dx = out_tile(s, true, n_pairs, ~(size_t)0).splits;
+    if (dx > parts) parts = dx;
+  }
+  l.total = l.part + (parts > 1 ? up256((size_t)4 * parts * s.T * s.D) : 0);
   return l;
 }
 
@@ -972,7 +979,7 @@ extern "C" int camera_ffn_forward(const camera_ffn_t* f, const void* x, int64_t 
   const int rc = check_ffn(f, n_tokens, &s);
   if (rc != CAMERA_OK) return rc;
   const FfnLayout l = ffn_layout(s, false);
-  if (workspace == nullptr || workspace_bytes < l.total || (reinterpret_cast<uintptr_t>(workspace) & 255)) return CAMERA_ERR_WORKSPACE;
+  if (workspace == nullptr || workspace_bytes < l.part || (reinterpret_cast<uintptr_t>(workspace) & 255)) return CAMERA_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   char* const ws = static_cast<char*>(workspace);
   if (n_tokens > 0 && (x == nullptr || y == nullptr || ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(y)) & 15) ||
@@ -1022,7 +1029,7 @@ extern "C" int camera_ffn_forward(const camera_ffn_t* f, const void* x, int64_t 
   FFN_CK(launch_gemm<FFN_GATE_UP>(q, t, n_pairs, true, st));
   q.prob[0] = FfnProblem{(int)s.T, s.D, 0, 0, static_cast<__nv_bfloat16*>(y), s.D};
   q.n_kb = (s.F + UMMA_BK - 1) / UMMA_BK;
-  t = out_tile(s, false, n_pairs);
+  t = out_tile(s, false, n_pairs, workspace_bytes - l.part);
   if (!enc(&q.a[0], q.h, s.T, s.F, s.fp, 128) || !enc(&q.b[0], f->w_down, s.D, s.F, s.ld, t.bn / 2)) return CAMERA_ERR_CUDA;
   FFN_CK(launch_gemm<FFN_DOWN>(q, t, n_pairs, false, st));
   return CAMERA_OK;
@@ -1036,7 +1043,7 @@ extern "C" int camera_ffn_backward(const camera_ffn_t* f, const void* x, const v
   const int rc = check_ffn(f, n_tokens, &s);
   if (rc != CAMERA_OK) return rc;
   const FfnLayout l = ffn_layout(s, true);
-  if (workspace == nullptr || workspace_bytes < l.total || (reinterpret_cast<uintptr_t>(workspace) & 255)) return CAMERA_ERR_WORKSPACE;
+  if (workspace == nullptr || workspace_bytes < l.part || (reinterpret_cast<uintptr_t>(workspace) & 255)) return CAMERA_ERR_WORKSPACE;
   const bool weights = dw_gate != nullptr;
   if ((dw_up != nullptr) != weights || (dw_down != nullptr) != weights || (!weights && dx == nullptr)) return CAMERA_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(dw_gate) | reinterpret_cast<uintptr_t>(dw_up) | reinterpret_cast<uintptr_t>(dw_down)) & 15)
@@ -1080,7 +1087,7 @@ extern "C" int camera_ffn_backward(const camera_ffn_t* f, const void* x, const v
   if (dx != nullptr) {
     q.prob[0] = FfnProblem{(int)s.T, s.D, 0, 0, static_cast<__nv_bfloat16*>(dx), s.D};
     q.n_kb = (s.F + UMMA_BK - 1) / UMMA_BK;
-    t = out_tile(s, true, n_pairs);
+    t = out_tile(s, true, n_pairs, workspace_bytes - l.part);
     if (!enc(&q.a[0], q.dg, s.T, s.F, q.act_ld, 128) || !enc(&q.a[1], q.du, s.T, s.F, q.act_ld, 128) ||
         !enc(&q.b[0], f->w_gate, s.F, s.D, s.D, 64) || !enc(&q.b[1], f->w_up, s.F, s.D, s.D, 64))
       return CAMERA_ERR_CUDA;
