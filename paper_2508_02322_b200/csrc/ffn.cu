@@ -1084,16 +1084,7 @@ extern "C" int camera_ffn_backward(const camera_ffn_t* f, const void* x, const v
   Tile t = choose_tile(m_tiles, s.F, false, 128, q.n_kb, 20.0, 1, 0.0, n_pairs);
   if (!enc(&q.a[0], dy, s.T, s.D, s.D, 128) || !enc(&q.b[0], f->w_down, s.D, s.F, s.ld, 64)) return CAMERA_ERR_CUDA;
   FFN_CK(launch_gemm<FFN_DH>(q, t, n_pairs, true, st));
-  if (dx != nullptr) {
-    q.prob[0] = FfnProblem{(int)s.T, s.D, 0, 0, static_cast<__nv_bfloat16*>(dx), s.D};
-    q.n_kb = (s.F + UMMA_BK - 1) / UMMA_BK;
-    t = out_tile(s, true, n_pairs, workspace_bytes - l.part);
-    if (!enc(&q.a[0], q.dg, s.T, s.F, q.act_ld, 128) || !enc(&q.a[1], q.du, s.T, s.F, q.act_ld, 128) ||
-        !enc(&q.b[0], f->w_gate, s.F, s.D, s.D, 64) || !enc(&q.b[1], f->w_up, s.F, s.D, s.D, 64))
-      return CAMERA_ERR_CUDA;
-    FFN_CK(launch_gemm<FFN_DX>(q, t, n_pairs, false, st));
-  }
-  if (weights) {
+  if (weights) {               // before dx, which may take the room of x or dy
     q.n_prob = 3;
     q.prob[0] = FfnProblem{s.F, s.D, 0, 0, static_cast<__nv_bfloat16*>(dw_gate), s.D};
     q.prob[1] = FfnProblem{s.F, s.D, 0, 0, static_cast<__nv_bfloat16*>(dw_up), s.D};
@@ -1106,6 +1097,16 @@ extern "C" int camera_ffn_backward(const camera_ffn_t* f, const void* x, const v
       return CAMERA_ERR_CUDA;
     q.b[1] = q.b[0];
     FFN_CK(launch_gemm<FFN_DW>(q, t, n_pairs, false, st));
+  }
+  if (dx != nullptr) {
+    q.n_prob = 1;
+    q.prob[0] = FfnProblem{(int)s.T, s.D, 0, 0, static_cast<__nv_bfloat16*>(dx), s.D};
+    q.n_kb = (s.F + UMMA_BK - 1) / UMMA_BK;
+    t = out_tile(s, true, n_pairs, workspace_bytes - l.part);
+    if (!enc(&q.a[0], q.dg, s.T, s.F, q.act_ld, 128) || !enc(&q.a[1], q.du, s.T, s.F, q.act_ld, 128) ||
+        !enc(&q.b[0], f->w_gate, s.F, s.D, s.D, 64) || !enc(&q.b[1], f->w_up, s.F, s.D, s.D, 64))
+      return CAMERA_ERR_CUDA;
+    FFN_CK(launch_gemm<FFN_DX>(q, t, n_pairs, false, st));
   }
   return CAMERA_OK;
 }

@@ -1,4 +1,4 @@
-"""Buffers of the feed-forward block: one workspace over calls of many sizes."""
+"""Buffers of the feed-forward block: one workspace over calls of many sizes, and gradients that take an input's room."""
 import pytest
 import torch
 
@@ -56,3 +56,17 @@ def test_the_teachers_workspace_serves_a_narrower_student(P):
         P.camera_ffn_forward(student, x, saved=saved, workspace=ws)
         P.camera_ffn_backward(student, x, dy, saved, workspace=ws)
         assert P.camera_read_status(ws) == 0
+
+
+@pytest.mark.parametrize("T,D,F,ld", [(40, 64, 48, 48), (300, 520, 333, 336), (1001, 1024, 845, 848)])
+def test_the_gradient_by_x_may_take_the_room_of_x_or_dy(P, T, D, F, ld):
+    ffn, x, dy = make(P, T, D, F, ld)
+    saved = P.alloc_workspace(P.camera_ffn_saved_bytes(ffn, T), DEV)
+    P.camera_ffn_forward(ffn, x, saved=saved)
+    w_down = lambda: torch.zeros(D, ld, dtype=torch.bfloat16, device=DEV)
+    want = P.camera_ffn_backward(ffn, x, dy, saved, out={"w_down": w_down()})
+    for over in ("x", "dy"):
+        x2, dy2 = x.clone(), dy.clone()
+        got = P.camera_ffn_backward(ffn, x2, dy2, saved, out={"x": x2 if over == "x" else dy2, "w_down": w_down()})
+        for name in want:
+            assert torch.equal(got[name], want[name]), (over, name)
