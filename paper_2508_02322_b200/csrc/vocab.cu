@@ -811,7 +811,7 @@ struct Softmax {
   __device__ __forceinline__ float logprob(float x) const {
     if (careful) return (x - m) * inv_tau - log2s * LN2;
     const float d = fmaf(x, c, -m);
-    return d < -1e30f ? x * inv_tau : (d - log2s) * LN2;     // far below fp32's range once scaled, the rest does not count
+    return d < -1e30f ? x * inv_tau - m * LN2 : (d - log2s) * LN2;     // x c may be beyond fp32's range; log2s does not count
   }
 };
 
