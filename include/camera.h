@@ -436,7 +436,7 @@ int camera_ffn_backward(const camera_ffn_t* ffn, const void* x, const void* dy, 
  *
  * Rows of logits: DEVICE [n_rows, vocab] in CAMERA_BF16 or CAMERA_F32, rows `ld` elements apart (ld >= vocab), any
  * alignment of the element type.  vocab <= CAMERA_MAX_VOCAB.  The distribution of a row is softmax(x / temperature),
- * 0 < temperature < infinity.  A logit of minus infinity is a token that cannot occur; a row of nothing else has no
+ * 0 < temperature < infinity, and 1.45 / temperature within fp32's range.  A logit of minus infinity is a token that cannot occur; a row of nothing else has no
  * distribution ("empty", see each call).  A row with a NaN or a logit of plus infinity gives NaN.  All statistics are
  * fp32 sums.  A row's results do not depend on what other rows hold; calls of one shape give the same bits on every run.
  * No workspace, and so no status word: a bounded wait between CTAs that share a row (camera_set_wait_limit_ns), should it

@@ -1432,7 +1432,8 @@ cudaError_t launch_distill(DistillArgs& a, int dtype, bool tail, cudaStream_t st
 
 int check_logits(const void* logits, int dtype, int64_t ld, int64_t n_rows, int32_t vocab, float temperature) {
   if (dtype != CAMERA_F32 && dtype != CAMERA_BF16) return CAMERA_ERR_INVALID_ARG;
-  if (n_rows < 0 || vocab < 1 || ld < vocab || !(temperature > 0.f) || isinf(temperature)) return CAMERA_ERR_INVALID_ARG;
+  if (n_rows < 0 || vocab < 1 || ld < vocab || !(temperature > 0.f) || isinf(temperature) || isinf(LOG2E / temperature))
+    return CAMERA_ERR_INVALID_ARG;
   if (vocab > CAMERA_MAX_VOCAB || n_rows > 0x3fffffff) return CAMERA_ERR_UNSUPPORTED_SHAPE;
   if (n_rows > 0 && (logits == nullptr || (reinterpret_cast<uintptr_t>(logits) & (dtype == CAMERA_BF16 ? 1 : 3))))
     return CAMERA_ERR_INVALID_ARG;
