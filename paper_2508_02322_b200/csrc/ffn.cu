@@ -743,16 +743,6 @@ __global__ void __launch_bounds__(S_THREADS, CTAS) k_ffn_few(const FfnFew q) {
     }
   }
   // acc[r][n][i]: weight row g (i < 2) or g + 8 of the warp's tile r, token 8 n + 2 tg + i % 2
-  if (WK == 1 && splits == 1) {
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          few_store<GATE_UP>(q, row0 + r * TILE + g, 8 * n + 2 * tg + i, acc[r][n][i], acc[r][n][2 + i]);
-    return;
-  }
   // every warp leaves its sums in its CTA's shared memory (the ring is empty by now); the CTAs of a cluster share the
   // adding up
   __syncthreads();
