@@ -539,6 +539,7 @@ __device__ __forceinline__ bool exchange_wait(Exchange& ex, uint32_t bar, uint32
     }
   }
   ex.failed = __syncthreads_or(!ok);
+  if (!ex.failed) mbar_try_wait_cluster(bar, phase);         // over by now: every thread acquires what came in
   return !ex.failed;
 }
 // At the end of the kernel: a CTA that failed may still be written to by others that have not, and stays until all of them
