@@ -40,6 +40,7 @@ constexpr float D_FLOOR = -150.f;          // 2^-150 is 0 in fp32: a floor for e
 constexpr float D_PART = -100.f;           // the most a sum is scaled down in one step
 constexpr float REF_FLOOR = -126.f;        // references start here
 constexpr float REF_SLACK = 3.f;
+constexpr float SHARE_FLOOR = -1022.f;     // log2 of the smallest share outside a teacher's list that counts
 constexpr float LN2 = 0.693147180559945309f;
 constexpr float LOG2E = 1.44269504088896341f;
 
@@ -331,6 +332,7 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
   const uint8_t* const mine = ring + tid * 16;
   if (REST) mark += tid >> 5;
   float raise_at = REF_FLOOR;                                // a maximum above this becomes the reference
+  float seen = -INFINITY;                                    // REST: the largest before one did
   int left = row.v_end - row.v_begin;                        // vectors of the part not yet walked
   do {
     uint4 raw[RG::PER];
@@ -362,6 +364,7 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
         chunk = Elem<T>::max_word(chunk, w);
       }
       const float m = fmaxf(Elem<T>::max_of(chunk), fmaxf(single[0], single[1])) * c;
+      if (REST) seen = fmaxf(seen, m);
       // the first logits above the floor, or for the entropy's digits (see above) larger ones further on
       if (m > raise_at) {
         const float d = -ref2.x - m, f = ex2(d), dd = fmaxf(d, D_FLOOR);
@@ -402,6 +405,7 @@ __device__ __forceinline__ Sums walk_row(const Row<T>& row, float c, Feed<T, RG>
     st.s += e;
   }
   if (REST) {
+    if (st.s == 0.f) st.ref = fmaxf(seen, -FLT_MAX);         // how far below the floor everything lies (see sums_ordinary)
     st.t = fmaxf(fmaxf(listed[0], listed[1]) * c, REF_FLOOR);
     st.l = ex2(fmaf(listed[0], c, -st.t)) + ex2(fmaf(listed[1], c, -st.t));
   }
@@ -579,11 +583,16 @@ __device__ __forceinline__ Sums exchange_sums(const Sums& own, int part, int par
   ex.turn ^= 1;
   return st;
 }
-// REST: no bound below for l; what the walk's floor flushes there is nothing beside an ordinary s.
+__device__ __forceinline__ bool in_range(float s) { return s >= 0x1p-60f && s <= 0x1p120f; }
+// REST: no bound below for l beside an ordinary s; what the walk's floor flushes there is nothing against s.  Nor has s one
+// where it is 0 and the largest logit outside the list, ref then, is so far below the list that a whole vocabulary of it
+// makes no share (a student whose other logits are masked).
 template <bool REST>
 __device__ __forceinline__ bool sums_ordinary(const Sums& st) {
-  return st.s >= 0x1p-60f && st.s <= 0x1p120f && (!REST || st.l <= 0x1p120f);
+  if (!REST) return in_range(st.s);
+  return st.s == 0.f ? in_range(st.l) && st.ref + 20.f < st.t + SHARE_FLOOR : in_range(st.s) && st.l <= 0x1p120f;
 }
+static_assert(CAMERA_MAX_VOCAB <= 1 << 20, "2^20 tokens at most");
 
 // Order-preserving image of a float (both zeros alike) and the 64-bit key by which alternatives are ranked: larger value
 // first, then lower index.
@@ -968,7 +977,6 @@ struct DistillArgs {
   long long ld_grad;
 };
 enum { DISTILL_FORWARD = 0, DISTILL_BACKWARD = 1, DISTILL_STEP = 2 };
-constexpr float SHARE_FLOOR = -1022.f;       // log2 of the smallest share of the student that counts
 
 struct TeacherList {
   int idx[CAMERA_MAX_TOP];            // -1: no such entry
@@ -1037,6 +1045,7 @@ template <typename T>
 __device__ __forceinline__ Sums mark_list(const Row<T>& row, const TeacherList& tl, int k, float c, uint32_t* mark) {
   constexpr int N = Elem<T>::N;
   Sums st{REF_FLOOR, 0.f, REF_FLOOR, 0.f};
+  float seen = -INFINITY;
   for (int j = threadIdx.x & 31; j < k; j += 32) {
     const int i = tl.idx[j];
     if (i < row.first || i >= row.tail_at) continue;
@@ -1065,6 +1074,7 @@ __device__ __forceinline__ Sums mark_list(const Row<T>& row, const TeacherList& 
     }
     m *= c;
     m_l *= c;
+    seen = fmaxf(seen, m);
     if (m > st.ref) raise<false, false>(st, m, c);
     if (m_l > st.t) raise_listed<false>(st, m_l, c);
 #pragma unroll
@@ -1074,6 +1084,7 @@ __device__ __forceinline__ Sums mark_list(const Row<T>& row, const TeacherList& 
       if (on) st.l += e; else st.s += e;
     }
   }
+  if (st.s == 0.f) st.ref = fmaxf(seen, -FLT_MAX);
   return st;
 }
 template <typename T>
@@ -1254,7 +1265,7 @@ __global__ void __launch_bounds__(VD_THREADS, 2) k_distill(const DistillArgs a) 
         st = exchange_sums<false, false, REST>(st, part, parts, a.c, ex, js);
       }
       // a reference that large would swallow digits of log2 s where the two are added (Softmax::k)
-      careful = !ex.failed && (!sums_ordinary<REST>(st) || fabsf(st.ref) > 4096.f || (REST && fabsf(st.t) > 4096.f));
+      careful = !ex.failed && (!sums_ordinary<REST>(st) || (st.s != 0.f && fabsf(st.ref) > 4096.f) || (REST && fabsf(st.t) > 4096.f));
       if (careful) {
         st = no_sums<REST>();
         if (!lister) st = walk_careful<T, false, REST>(row, a.c, mark, tl.idx, a.k);
