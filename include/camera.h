@@ -422,9 +422,10 @@ int camera_ffn_forward(const camera_ffn_t* ffn, const void* x, int64_t n_tokens,
  * Gradients of that call by its inputs, given dy (DEVICE [n_tokens, d_model] bf16) and what the call saved: dx
  * [n_tokens, d_model], dw_gate and dw_up [d_ff, d_model], dw_down [d_model, down_ld] (columns from d_ff on are not
  * written), all bf16, overwritten.  dx may be NULL, and may take the room of x or dy; no other output may overlap an input.
- * dw_* may be NULL together.  The gate and up products are kept, and
- * their gradients formed, in bf16 (rounded once from fp32); the sums over tokens and micro-experts are fp32.  `saved` is
- * left as it is.  Results (of the forward call too) are the same bits on every run with a workspace of the same size.
+ * dw_* may be NULL together.  The gate and up products are kept with 24 of fp32's 32 bits (cut), their gradients formed
+ * from those in fp32; h, dG and dU are rounded to bf16 as operands of the next product; the sums over tokens and
+ * micro-experts are fp32.  `saved` is left as it is.  Results (of the forward call too) are the same bits on every run with
+ * a workspace of the same size.
  */
 int camera_ffn_backward(const camera_ffn_t* ffn, const void* x, const void* dy, int64_t n_tokens, const void* saved, void* dx,
                         void* dw_gate, void* dw_up, void* dw_down, void* workspace, size_t workspace_bytes,

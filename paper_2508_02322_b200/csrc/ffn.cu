@@ -10,6 +10,9 @@
 //   DH       A = dY (K = d_model contiguous), B = Wd with N (d_ff) contiguous; epilogue reads G, U and writes dG, dU, H
 //   DX       A = dG then dU (K = d_ff contiguous), B = Wg then Wu with N (d_model) contiguous: one accumulator for both
 //   DW       three problems in one launch: A = dG / dU / dY, B = X / X / H, both with K (tokens) as the slow dimension
+// H, dG and dU are rounded to bf16, being operands of the next product on the tensor cores (camera_layer_forward rounds its h
+// likewise): results are 2.3e-3 to 2.5e-3 off 64 bits (root mean square, relative), products kept in 32 bits and rounded
+// once at the end 1.7e-3.
 // An operand whose M or N index is the contiguous one is loaded as boxes of 64 of those x 64 k and described to the MMA
 // as MN-major; nothing is transposed in memory.
 #include <cuda.h>
@@ -233,9 +236,10 @@ struct Kept {
 };
 __device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
 
-// Bound by the tensor pipe once tiles fill the 74 pairs: 4096 tokens, d_model 3584, d_ff 20480 forward 1200 to 1320 us
-// (1104 us at cuBLAS's burst rate, 1306 us at its rate under the power cap), a training pass over 8192 tokens at d_ff 2560
-// 1030 us on the device (828 and 980 us).  Smaller problems by the k blocks in a row, 0.32 to 0.39 us each.
+// Bound by the tensor pipe once tiles fill the 74 pairs, and by the power cap: 4096 tokens, d_model 3584, d_ff 20480
+// forward 1220 us after a pause and 1370 to 1410 us call after call (1104 us at cuBLAS's burst rate, 1306 us at its
+// rate under the cap), a training pass over 8192 tokens at d_ff 2560 1063 and 1190 to 1245 us (828 and 980 us).  Smaller
+// problems by the k blocks in a row, 0.32 to 0.39 us each.
 template <int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1) k_ffn_gemm(const __grid_constant__ FfnGemm q) {
   constexpr bool A_MN = MODE == FFN_DW;
@@ -584,8 +588,9 @@ __global__ void __launch_bounds__(256) k_ffn_join(const FfnGemm q) {
 // 8 / WK times.  GATE_UP tiles are 8 rows of Wg over the same 8 rows of Wu, so that a thread ends with gate and up of one
 // element.  Where that gives too few CTAs to fill the GPU, k is split further over the CTAs of a cluster (up to 8).  The
 // sums of the warps and CTAs along k meet through (distributed) shared memory in a fixed order.
-// Bound by the weights' bytes: 24 tokens through 20480 micro-experts of d_model 3584 take 106 us (4.2 TB/s; with 128-byte
-// runs a row 137 us), one token through 2560 of them 14.2 us (3.9 TB/s), two kernels' start and end among them.
+// Bound by the weights' bytes: 24 tokens through 20480 micro-experts of d_model 3584 take 101 to 105 us (4.2 TB/s; with
+// 128-byte runs a row 137 us), one token through 2560 of them 16.4 us a call (3.4 TB/s; 12.3 us where the weights of one
+// call after the other are found in L2), two kernels' start and end among them.
 constexpr int S_WARPS = 8;
 constexpr int S_THREADS = 32 * S_WARPS;
 constexpr int S_STEP_BYTES = S_THREADS * 64;       // a step of one tile per warp

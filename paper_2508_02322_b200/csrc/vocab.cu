@@ -12,8 +12,10 @@
 // cancel (4095 rows: error of the entropies against 64 bits 9.6e-6 without, 6e-7 with): where it is asked for, a thread
 // raises its reference when a chunk's maximum exceeds it by more than 2^REF_SLACK.  A row whose sum ends outside
 // [2^-60, 2^120] (logits far above a share's first, all of them the type's lowest value, NaN, infinity: nothing an
-// ordinary row does) is walked again with differences formed before the scaling and a running maximum (walk_careful).
-// All sums are fp32 over at most a few hundred terms a thread, then a tree in a fixed order.
+// ordinary row does) is walked again with differences formed before the scaling and a running maximum (walk_careful; two to
+// four times an ordinary row's time: 2048 rows of 151936 bf16 logits around -200, log-probabilities 107 -> 402 us,
+// distillation step 289 -> 1055 us).
+// All sums are fp32, over a few hundred terms a thread (4096 at the largest vocabulary), then a tree in a fixed order.
 //
 // Bound by reading the logits once; the arithmetic comes close behind (an exponential per logit: 16 a clock and SM), so
 // the multiply-adds run in pairs (f32x2) and the loop holds nothing else.  Few rows are split over the CTAs of a cluster,
@@ -827,8 +829,8 @@ struct Softmax {
 
 // A CTA, or (SPLIT) the CTAs of a cluster together, take row after row: blockIdx.x is the CTA's part of the row,
 // blockIdx.y its first row.  Two CTAs an SM with ring chunks of 32 KB: one selects alternatives while the other
-// reads.  4095 rows of 151936 bf16 logits with entropy take 215 us on the device (5.8 TB/s, exponentials at 72 % of their
-// rate; registers in place of the ring: 234 us), 2048 such rows with 64 alternatives 162 us.
+// reads.  4095 rows of 151936 bf16 logits with entropy take 227 to 241 us (5.2 to 5.5 TB/s of logits), 2048 such rows with
+// 64 alternatives 152 us; one row with 8 alternatives 10.6 us of the GPU, 13.9 us a call.
 template <typename T, bool ENT, bool TOP, bool SPLIT>
 __global__ void __launch_bounds__(V_THREADS, 2) k_token_logprobs(const LogprobArgs a) {
   using RG = RingStream;
@@ -1174,9 +1176,9 @@ __device__ __forceinline__ void write_row(const Row<T>& row, T* out, const Softm
 // A CTA, or (SPLIT) the CTAs of a cluster together, take row after row, like k_token_logprobs.  STEP sends every row
 // through the ring twice, once to sum it and once to write the gradient; the second time it comes from L2 (see Feed).  The
 // last warp looks after the teacher's lists: while the others sum a row it brings in the next row's, and while they write
-// the gradient it forms the loss.  4096 rows of 151936 bf16 logits with 64 entries: 625 us, 250 to sum them (exponentials,
-// as above) and 380 for the gradient (an exponential, 12 to 15 instructions and a store for each read); reading the logits
-// and writing the gradient once would be 381 us.  250 rows of 32003 fp32 logits, loss alone: 12.6 us.
+// the gradient it forms the loss.  4096 rows of 151936 bf16 logits with 64 entries: 584 us; reading the logits and writing the
+// gradient once would be 381 us, the rest is that a CTA sums and writes in turn, with a join in between.  250 rows of 32003 fp32
+// logits, loss alone: 12.3 us of the GPU, 13.6 us a call, most of it the first row's list, sums and logarithms one after the other.
 constexpr int VD_THREADS = V_THREADS + 32;
 constexpr int VD_LISTS = 3;
 
@@ -1425,8 +1427,8 @@ cudaError_t launch_distill(DistillArgs& a, cudaStream_t st) {
   const int sms = sm_count(), n_vec = a.vocab / Elem<T>::N;
   a.lg = split_for(a.rows, n_vec, sms);
   // A step reads its rows again from L2: two CTAs share a row where the rows of all CTAs would not stay there beside the
-  // gradients on their way out (4096 rows of 151936 bf16 logits, 90 MB in flight: 688 us unshared, 629 us in pairs; in
-  // fours 827 us, the CTAs then wait for each other more often than the reads gain).  The loss alone is as fast either way
+  // gradients on their way out (4096 rows of 151936 bf16 logits, 90 MB in flight: 602 us unshared, 584 us in pairs; in
+  // fours 817 us, the CTAs then wait for each other more often than the reads gain).  The loss alone is as fast either way
   // and takes the same split, so that both calls give the same bits.
   if (MODE != DISTILL_BACKWARD && a.lg == 0 && 2ll * sms * n_vec * 16 > STEP_L2_BYTES) a.lg = 1;
   a.mark_words = REST ? mark_words(n_vec, a.lg) : 0;

@@ -2,7 +2,9 @@
 backward pass, log-probabilities of given tokens, distillation from a teacher's top log-probabilities.
 
 Like binding.py: argument marshalling only, every function named as the C entry point it calls.  Tensors a call returns
-are allocated on the stream the call runs on.
+are allocated on the stream the call runs on.  Outputs have no autograd graph, whatever their inputs require: backward
+passes are calls of their own, and write gradients over what their outputs held (sums over micro-batches are the
+caller's).
 """
 from __future__ import annotations
 
