@@ -501,6 +501,108 @@ int camera_distill_backward(const camera_distill_t* d, const float* d_loss, cons
 int camera_distill_step(const camera_distill_t* d, const float* d_loss, float* loss, void* d_logits, int64_t d_ld,
                         void* cuda_stream);
 
+/*
+ * Training a sliced layer: what stands around its experts.  (The paper has no counterpart.)  Matrices of rows: DEVICE, in
+ * CAMERA_BF16 or CAMERA_F32, rows `ld` elements apart (ld >= their width), any alignment of the element type; rows that
+ * start on 16-byte boundaries are read and written 16 bytes at a time.  Sums are fp32, results rounded once.  Calls of one
+ * shape give the same bits on every run.  A result may take the room of an input where its comment says so (same address,
+ * same ld); otherwise outputs overlap nothing.
+ */
+
+/* camera_norm_t.flags */
+enum { CAMERA_NORM_RMS = 1u };    /* root mean square: no mean is taken off */
+
+/* The rows a norm works on and its weights. */
+typedef struct {
+  const void* x;                  /* [n_rows, d]; backward: what was normalised (`sum` where there was a residual) */
+  int64_t ld;
+  int64_t n_rows;
+  int32_t dtype;                  /* camera_dtype_t of all matrices of the call */
+  int32_t d;                      /* 1 .. 32768 */
+  const void* weight;             /* DEVICE [d] or NULL (ones) */
+  const void* bias;               /* DEVICE [d] or NULL (zeros) */
+  int32_t weight_dtype;           /* camera_dtype_t of weight and bias */
+  float eps;                      /* >= 0, finite */
+  uint32_t flags;
+} camera_norm_t;
+
+/*
+ * forward: z = x + residual, rounded to the dtype (z = x without one; sum [n_rows, d] receives z and goes with residual:
+ *   both or neither);  mu = mean z (0 with CAMERA_NORM_RMS), s = 1 / sqrt(mean (z - mu)^2 + eps), y = (z - mu) s weight + bias.
+ *   mean, rstd: DEVICE fp32 [n_rows], receive mu and s, either may be NULL.  y and sum may take the room of x or residual.
+ * backward, given dy, n->x = z, and mu and s as the forward call left them (mean may be NULL with CAMERA_NORM_RMS):
+ *   h = (z - mu) s, g = dy weight:  dx = s (g - mean g - h mean(g h)) + d_sum  (no mean g with CAMERA_NORM_RMS),
+ *   d_weight = sum over rows of dy h, d_bias = sum over rows of dy (DEVICE fp32 [d], overwritten).
+ *   d_sum: gradient of z from elsewhere (the residual stream's), or NULL.  dx is also the residual's gradient.  dx may be
+ *   NULL (then d_sum too), d_weight and d_bias may be NULL, not all three.  dx may take the room of dy, d_sum or z.
+ *   n->bias and n->eps are not read.
+ * A NaN or an infinity stays in its row (and reaches d_weight and d_bias).  A row without variance and with eps 0 gives NaN.
+ * workspace (needed for d_weight or d_bias): camera_norm_backward_workspace_bytes, which serves every call with no more
+ * rows of that width.  No kernel here waits, so it holds no status word.
+ */
+int camera_norm_forward(const camera_norm_t* n, const void* residual, int64_t residual_ld, void* sum, int64_t sum_ld, void* y,
+                        int64_t y_ld, float* mean, float* rstd, void* cuda_stream);
+size_t camera_norm_backward_workspace_bytes(int64_t n_rows, int32_t d);
+int camera_norm_backward(const camera_norm_t* n, const void* dy, int64_t dy_ld, const float* mean, const float* rstd,
+                         const void* d_sum, int64_t d_sum_ld, void* dx, int64_t dx_ld, float* d_weight, float* d_bias,
+                         void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Tokens sorted by expert and back.  topk_idx, rows: DEVICE int32 [n_tokens, top_k]; topk_w: DEVICE fp32 [n_tokens, top_k]
+ * or NULL (ones).  top_k 1 .. 16, n_experts 1 .. 1024, n_tokens * top_k < 2^31, d_model 1 .. 2^20.
+ * dispatch: the pairs (token t, slot j) in order of their expert topk_idx[t, j], within one by token and slot: rows[t, j] is the
+ *   pair's place, x_sorted[rows[t, j]] = x[t], and expert e's rows are offsets[e] .. offsets[e+1] (DEVICE int32 [n_experts + 1]).
+ *   A pair whose index lies outside [0, n_experts) is left out (rows -1).  Rows of x_sorted from offsets[n_experts] on are left
+ *   as they were; it has room for n_tokens * top_k rows.  A token may name an expert twice.
+ * combine: y[t] = add[t] + sum over j of topk_w[t, j] y_sorted[rows[t, j]], added in the order of the slots, add last.  add may
+ *   be NULL; y may take its room.  n_rows: rows that y_sorted has; an entry of `rows` outside [0, n_rows) adds nothing.  A weight
+ *   of 0 still multiplies its row (NaN and infinity there give NaN).
+ * combine_backward: dy_sorted[rows[t, j]] = topk_w[t, j] dy[t], d_topk_w[t, j] = <dy[t], y_sorted[rows[t, j]]> (0 for a pair that
+ *   was left out).  Either may be NULL, not both; y_sorted is read for d_topk_w only.  Rows of dy_sorted that no pair names are
+ *   left as they were.  Entries of `rows` are distinct.  dy_sorted may take the room of y_sorted.
+ * dispatch_backward: dx[t] = add[t] + sum over j of dx_sorted[rows[t, j]]: combine without weights.
+ * workspace: camera_moe_dispatch_workspace_bytes, which serves every call with no more tokens, slots and experts; no status word.
+ */
+size_t camera_moe_dispatch_workspace_bytes(int64_t n_tokens, int32_t top_k, int32_t n_experts);
+int camera_moe_dispatch(const void* x, int32_t dtype, int64_t ld, int64_t n_tokens, int32_t d_model, const int32_t* topk_idx,
+                        int32_t top_k, int32_t n_experts, void* x_sorted, int64_t sorted_ld, int32_t* rows, int32_t* offsets,
+                        void* workspace, size_t workspace_bytes, void* cuda_stream);
+int camera_moe_dispatch_backward(const void* dx_sorted, int32_t dtype, int64_t sorted_ld, int64_t n_rows, const int32_t* rows,
+                                 int64_t n_tokens, int32_t top_k, int32_t d_model, const void* add, int64_t add_ld, void* dx,
+                                 int64_t ld, void* cuda_stream);
+int camera_moe_combine(const void* y_sorted, int32_t dtype, int64_t sorted_ld, int64_t n_rows, const int32_t* rows,
+                       const float* topk_w, int64_t n_tokens, int32_t top_k, int32_t d_model, const void* add, int64_t add_ld,
+                       void* y, int64_t ld, void* cuda_stream);
+int camera_moe_combine_backward(const void* dy, int32_t dtype, int64_t ld, int64_t n_tokens, int32_t d_model, const int32_t* rows,
+                                const float* topk_w, int32_t top_k, const void* y_sorted, int64_t sorted_ld, int64_t n_rows,
+                                void* dy_sorted, int64_t dy_sorted_ld, float* d_topk_w, void* cuda_stream);
+
+/* One matrix of camera_orthogonalize. */
+typedef struct {
+  const void* in;                 /* DEVICE [rows, cols], rows in_ld elements apart */
+  void* out;                      /* DEVICE bf16 [rows, cols], rows out_ld elements apart; may be `in` (bf16, same ld) */
+  int64_t in_ld, out_ld;
+  int32_t rows, cols;             /* up to 131072, one of them up to 32768; either may be 0 */
+} camera_matrix_t;
+
+/*
+ * The updates of a layer's matrices, orthogonalised: X = in / (|in| + eps) with the Frobenius norm, then `steps` times
+ *   X <- a X + (b A + c A A) X,  A = X X^T (of the shorter side),
+ * which takes every singular value s to a s + b s^3 + c s^5; out = X.  coefficients: HOST [steps][3], (a, b, c) of each step.
+ * With those that take values towards 1, out is near the orthogonal factor of `in`.  mats: HOST [n_mats], in in `dtype`; the
+ * matrices of a call, whatever their shapes, are worked on together.  1 <= steps <= 64.  Coefficients under which a singular
+ * value or the step's factor of it could pass 1000 are refused (CAMERA_ERR_INVALID_ARG): they do not converge.
+ * Products of fp16 operands with fp32 sums; factors that keep them in range follow from the coefficients.  The result is
+ * about 1e-3 off 64 bits (root mean square, relative) before its rounding to bf16; directions whose singular value is below
+ * 1e-3 of the norm's share of the others are off by more.  A matrix of zeros gives zeros; one with a NaN or an infinity gives
+ * NaN and leaves the others of the call as they are.
+ * workspace: camera_orthogonalize_workspace_bytes of the same shapes (pointers are not read); it starts with a status word
+ * that camera_read_status reads.
+ */
+size_t camera_orthogonalize_workspace_bytes(const camera_matrix_t* mats, int32_t n_mats);
+int camera_orthogonalize(const camera_matrix_t* mats, int32_t n_mats, int32_t dtype, const float* coefficients, int32_t steps,
+                         float eps, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* Scratch for camera_analyze_layer_host: score + select scratch for one batch of tokens, two staging
  * buffers for batches of x, and the results. */
 size_t camera_analyze_workspace_bytes(const camera_layer_t* layer, int64_t n_tokens, int32_t n_levels);

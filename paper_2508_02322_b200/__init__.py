@@ -14,3 +14,7 @@ from .binding import (  # noqa: F401
 from .recovery import (  # noqa: F401
     Ffn, camera_ffn_workspace_bytes, camera_ffn_saved_bytes, camera_ffn_forward, camera_ffn_backward,
     camera_token_logprobs, camera_distill_forward, camera_distill_backward, camera_distill_step)
+from .training import (  # noqa: F401
+    camera_norm_forward, camera_norm_backward, camera_norm_backward_workspace_bytes, camera_moe_dispatch,
+    camera_moe_dispatch_workspace_bytes, camera_moe_dispatch_backward, camera_moe_combine, camera_moe_combine_backward,
+    camera_orthogonalize, camera_orthogonalize_workspace_bytes, NEWTON_SCHULZ)

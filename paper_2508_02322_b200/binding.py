@@ -48,6 +48,17 @@ class camera_distill_t(C.Structure):
                 ("temperature", C.c_float), ("flags", C.c_uint32)]
 
 
+class camera_norm_t(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("ld", C.c_int64), ("n_rows", C.c_int64), ("dtype", C.c_int32), ("d", C.c_int32),
+                ("weight", C.c_void_p), ("bias", C.c_void_p), ("weight_dtype", C.c_int32), ("eps", C.c_float),
+                ("flags", C.c_uint32)]
+
+
+class camera_matrix_t(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("in_ld", C.c_int64), ("out_ld", C.c_int64), ("rows", C.c_int32),
+                ("cols", C.c_int32)]
+
+
 class camera_score_aux_t(C.Structure):
     _fields_ = [("phi2", C.c_void_p), ("phi_inf_sq", C.c_void_p), ("omega2", C.c_void_p),
                 ("topk_idx", C.c_void_p), ("topk_w", C.c_void_p), ("topk_idx_in", C.c_void_p),
@@ -163,6 +174,22 @@ def _load() -> C.CDLL:
     lib.camera_distill_step.restype = C.c_int
     lib.camera_distill_step.argtypes = [C.POINTER(camera_distill_t), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
                                         C.c_void_p]
+    ptr, i32, i64, size = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
+    for name, res, args in (
+            ("camera_norm_forward", C.c_int, [C.POINTER(camera_norm_t), ptr, i64, ptr, i64, ptr, i64, ptr, ptr, ptr]),
+            ("camera_norm_backward_workspace_bytes", size, [i64, i32]),
+            ("camera_norm_backward", C.c_int, [C.POINTER(camera_norm_t), ptr, i64, ptr, ptr, ptr, i64, ptr, i64, ptr, ptr, ptr,
+                                               size, ptr]),
+            ("camera_moe_dispatch_workspace_bytes", size, [i64, i32, i32]),
+            ("camera_moe_dispatch", C.c_int, [ptr, i32, i64, i64, i32, ptr, i32, i32, ptr, i64, ptr, ptr, ptr, size, ptr]),
+            ("camera_moe_dispatch_backward", C.c_int, [ptr, i32, i64, i64, ptr, i64, i32, i32, ptr, i64, ptr, i64, ptr]),
+            ("camera_moe_combine", C.c_int, [ptr, i32, i64, i64, ptr, ptr, i64, i32, i32, ptr, i64, ptr, i64, ptr]),
+            ("camera_moe_combine_backward", C.c_int, [ptr, i32, i64, i64, i32, ptr, ptr, i32, ptr, i64, i64, ptr, i64, ptr, ptr]),
+            ("camera_orthogonalize_workspace_bytes", size, [C.POINTER(camera_matrix_t), i32]),
+            ("camera_orthogonalize", C.c_int, [C.POINTER(camera_matrix_t), i32, i32, C.POINTER(C.c_float), i32, C.c_float, ptr,
+                                               size, ptr])):
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = res, args
     return lib
 
 

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcamera_b200.so")
-SOURCES = ["api.cu", "compact.cu", "ffn.cu", "forward.cu", "router.cu", "router_umma.cu", "rownorm.cu", "score_simt.cu", "score_umma.cu", "score_umma2.cu", "select.cu", "vocab.cu"]
+SOURCES = ["api.cu", "compact.cu", "ffn.cu", "forward.cu", "moe.cu", "norm.cu", "ortho.cu", "router.cu", "router_umma.cu", "rownorm.cu", "score_simt.cu", "score_umma.cu", "score_umma2.cu", "select.cu", "vocab.cu"]
 
 
 def _nvcc() -> str:

@@ -1,0 +1,419 @@
+// Tokens sorted by expert and back, with the gradients of both.
+//   rows[t, j]  place of the pair (token t, slot j) when all pairs are sorted by expert (within one by t, then j)
+//   dispatch           xs[rows[t, j]] = x[t]
+//   combine            y[t] = add[t] + sum_j w[t, j] ys[rows[t, j]]
+//   combine, backward  dys[rows[t, j]] = w[t, j] dy[t],  dw[t, j] = <dy[t], ys[rows[t, j]]>
+//   dispatch, backward dx[t] = add[t] + sum_j dxs[rows[t, j]]  (a combine without weights)
+// All of it is moving rows: bound by HBM, dispatch by its writes.
+#include "common.cuh"
+#include "launch.cuh"
+#include "rowgroup.cuh"
+
+namespace camera {
+
+namespace {
+
+constexpr int MOE_MAX_EXPERTS = 1024, MOE_MAX_D = 1 << 20;
+constexpr int MOE_THREADS = 256, MOE_WARPS = MOE_THREADS / 32;
+// Up to so many pairs every CTA counts all of them for itself; beyond, a kernel before counts them chunk by chunk.
+constexpr long long MOE_SMALL = 16384;
+
+struct Dispatch {
+  const void* x;
+  void* xs;
+  long long x_ld, xs_ld;
+  const int32_t* idx;
+  int32_t *rows, *offsets;
+  int32_t* hist;                 // [chunks][experts] pairs per chunk and expert, or null
+  int tokens, k, experts, d;
+  int chunk;                     // tokens a CTA handles
+};
+
+__device__ __forceinline__ bool usable(int e, int experts) { return (unsigned)e < (unsigned)experts; }
+
+__global__ void __launch_bounds__(MOE_THREADS) k_moe_count(const Dispatch q) {
+  extern __shared__ int32_t count[];
+  for (int e = threadIdx.x; e < q.experts; e += MOE_THREADS) count[e] = 0;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  __syncthreads();
+  const long long p0 = (long long)blockIdx.x * q.chunk * q.k, p1 = min(p0 + (long long)q.chunk * q.k, (long long)q.tokens * q.k);
+  for (long long p = p0 + threadIdx.x; p < p1; p += MOE_THREADS) {
+    const int e = q.idx[p];
+    if (usable(e, q.experts)) atomicAdd(&count[e], 1);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < q.experts; e += MOE_THREADS) q.hist[(long long)blockIdx.x * q.experts + e] = count[e];
+}
+
+// A CTA takes a run of consecutive tokens: it finds where each expert's rows begin and how many pairs lie before its own,
+// ranks its pairs (a warp takes a run of them, 32 at a time), and copies its tokens, read once, to their k rows.
+template <typename T, int W>
+__global__ void __launch_bounds__(MOE_THREADS) k_moe_dispatch(const Dispatch q) {
+  using P = Pack<T, W>;
+  extern __shared__ int32_t sh[];
+  int32_t* const total = sh;                       // [experts]
+  int32_t* const before = sh + q.experts;          // [experts] pairs of the CTAs before this one
+  int32_t* const next = sh + 2 * q.experts;        // [warps][experts] pairs of the warp, then where its next one goes
+  __shared__ int32_t warp_sum[MOE_WARPS];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, E = q.experts;
+  for (int i = tid; i < (2 + MOE_WARPS) * E; i += MOE_THREADS) sh[i] = 0;
+  __syncthreads();
+  const long long pairs = (long long)q.tokens * q.k;
+  const long long p0 = (long long)blockIdx.x * q.chunk * q.k, p1 = min(p0 + (long long)q.chunk * q.k, pairs);
+  const long long seg = ((p1 - p0 + MOE_WARPS - 1) / MOE_WARPS + 31) & ~31ll;      // pairs a warp ranks
+  const long long w0 = min(p0 + warp * seg, p1), w1 = min(w0 + seg, p1);
+  for (long long p = w0 + lane; p < w1; p += 32) {
+    const int e = q.idx[p];
+    if (usable(e, E)) atomicAdd(&next[warp * E + e], 1);
+  }
+  if (q.hist == nullptr) {
+    for (long long p = tid; p < pairs; p += MOE_THREADS) {
+      const int e = q.idx[p];
+      if (usable(e, E)) {
+        atomicAdd(&total[e], 1);
+        if (p < p0) atomicAdd(&before[e], 1);
+      }
+    }
+  } else {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int slices = MOE_THREADS / E > 1 ? MOE_THREADS / E : 1, slice = tid / E;      // threads along the chunks
+    if (slices == 1 || slice < slices)
+      for (int e = slices == 1 ? tid : tid - slice * E; e < E; e += slices == 1 ? MOE_THREADS : E) {
+        int all = 0, mine = 0;
+#pragma unroll 8
+        for (int c = slices == 1 ? 0 : slice; c < (int)gridDim.x; c += slices) {
+          const int v = q.hist[(long long)c * E + e];
+          all += v;
+          if (c < (int)blockIdx.x) mine += v;
+        }
+        atomicAdd(&total[e], all);
+        atomicAdd(&before[e], mine);
+      }
+  }
+  __syncthreads();
+  // exclusive scan over the experts: a thread takes `per` consecutive ones
+  const int per = (E + MOE_THREADS - 1) / MOE_THREADS;
+  int sum = 0;
+  for (int i = 0; i < per; ++i) {
+    const int e = tid * per + i;
+    if (e < E) sum += total[e];
+  }
+  int scan = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, scan, o);
+    if (lane >= o) scan += v;
+  }
+  if (lane == 31) warp_sum[warp] = scan;
+  __syncthreads();
+  int at = scan - sum;
+  for (int i = 0; i < warp; ++i) at += warp_sum[i];
+  for (int i = 0; i < per; ++i) {
+    const int e = tid * per + i;
+    if (e >= E) break;
+    const int n = total[e];
+    if (blockIdx.x == 0) q.offsets[e] = at;
+    int go = at + before[e];
+    for (int w = 0; w < MOE_WARPS; ++w) {
+      const int v = next[w * E + e];
+      next[w * E + e] = go;
+      go += v;
+    }
+    at += n;
+    if (blockIdx.x == 0 && e == E - 1) q.offsets[E] = at;
+  }
+  __syncthreads();
+  for (long long p = w0; p < w1; p += 32) {
+    const bool here = p + lane < w1;
+    const int e = here ? q.idx[p + lane] : -1;
+    const bool ok = usable(e, E);
+    const unsigned same = __match_any_sync(0xffffffffu, ok ? e : -1 - lane);
+    int row = -1;
+    if (ok) row = next[warp * E + e] + __popc(same & ((1u << lane) - 1u));
+    __syncwarp();
+    if (ok && lane == 31 - __clz(same)) next[warp * E + e] = row + 1;
+    __syncwarp();
+    if (here) q.rows[p + lane] = row;
+  }
+  __syncthreads();
+  const T* const x = static_cast<const T*>(q.x);
+  T* const xs = static_cast<T*>(q.xs);
+  constexpr int U = 4;
+  const int t1 = min((int)(blockIdx.x + 1) * q.chunk, q.tokens);
+  for (int t = blockIdx.x * q.chunk + warp; t < t1; t += MOE_WARPS) {
+    const int mine = lane < q.k ? q.rows[(long long)t * q.k + lane] : -1;
+    for (int c0 = 0; c0 < q.d; c0 += U * 32 * W) {
+      P v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + (32 * u + lane) * W;
+        if (c < q.d) v[u] = *reinterpret_cast<const P*>(x + t * q.x_ld + c);
+      }
+      for (int j = 0; j < q.k; ++j) {
+        const int row = __shfl_sync(0xffffffffu, mine, j);
+        if (row < 0) continue;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int c = c0 + (32 * u + lane) * W;
+          if (c < q.d) *reinterpret_cast<P*>(xs + row * q.xs_ld + c) = v[u];
+        }
+      }
+    }
+  }
+}
+
+struct Combine {
+  const void *ys, *add, *dy;
+  void *y, *dys;
+  long long ys_ld, add_ld, y_ld, dy_ld, dys_ld;
+  long long n_rows;              // rows of ys: an entry of `rows` outside is no row
+  const int32_t* rows;
+  const float* w;                // or null: ones
+  float* dw;
+  int tokens, k, d;
+  int warps;                     // backward: warps that share a token
+};
+
+constexpr int SLOTS = 8;         // rows of a token in flight
+
+// A thread takes one pack of one token: k rows in flight, added in the order of the slots.
+template <typename T, int W>
+__global__ void __launch_bounds__(256) k_moe_combine(const Combine q) {
+  using P = Pack<T, W>;
+  const long long t = (long long)blockIdx.x * blockDim.y + threadIdx.y;
+  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * W;
+  if (t >= q.tokens || c >= q.d) return;
+  const T* const ys = static_cast<const T*>(q.ys) + c;
+  P extra;
+  if (q.add != nullptr) extra = *reinterpret_cast<const P*>(static_cast<const T*>(q.add) + t * q.add_ld + c);
+  float sum[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) sum[i] = 0.f;
+  for (int j0 = 0; j0 < q.k; j0 += SLOTS) {
+    int row[SLOTS];
+    float w[SLOTS];
+    P v[SLOTS];
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+      row[j] = j0 + j < q.k ? q.rows[t * q.k + j0 + j] : -1;
+      if (row[j] >= q.n_rows) row[j] = -1;
+      w[j] = row[j] >= 0 && q.w != nullptr ? q.w[t * q.k + j0 + j] : 1.f;
+    }
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j)
+      if (row[j] >= 0) v[j] = *reinterpret_cast<const P*>(ys + row[j] * q.ys_ld);
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j)
+      if (row[j] >= 0) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) sum[i] = fmaf(w[j], to_f32(v[j].v[i]), sum[i]);
+      }
+  }
+  P out;
+#pragma unroll
+  for (int i = 0; i < W; ++i) out.v[i] = from_f32<T>(q.add != nullptr ? sum[i] + to_f32(extra.v[i]) : sum[i]);
+  *reinterpret_cast<P*>(static_cast<T*>(q.y) + t * q.y_ld + c) = out;
+}
+
+template <typename T, int W>
+__global__ void __launch_bounds__(512, 1) k_moe_combine_backward(const Combine q) {
+  using P = Pack<T, W>;
+  const int threads = 32 * q.warps, group = threadIdx.x / threads, i0 = threadIdx.x - group * threads;
+  const long long t = (long long)blockIdx.x * (blockDim.x / threads) + group;
+  if (t >= q.tokens) return;
+  const T* const dy = static_cast<const T*>(q.dy) + t * q.dy_ld;
+  const T* const ys = static_cast<const T*>(q.ys);
+  T* const dys = static_cast<T*>(q.dys);
+  int buf = 0;
+  for (int j0 = 0; j0 < q.k; j0 += SLOTS) {
+    int row[SLOTS];
+    float w[SLOTS], dot[SLOTS];
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+      row[j] = j0 + j < q.k ? q.rows[t * q.k + j0 + j] : -1;
+      if (row[j] >= q.n_rows) row[j] = -1;
+      w[j] = row[j] >= 0 && q.w != nullptr ? q.w[t * q.k + j0 + j] : 1.f;
+      dot[j] = 0.f;
+    }
+    for (int c = i0 * W; c < q.d; c += threads * W) {
+      const P g = *reinterpret_cast<const P*>(dy + c);
+      P v[SLOTS];
+      if (q.dw != nullptr) {
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j)
+          if (row[j] >= 0) v[j] = *reinterpret_cast<const P*>(ys + row[j] * q.ys_ld + c);
+      }
+#pragma unroll
+      for (int j = 0; j < SLOTS; ++j)
+        if (row[j] >= 0) {
+          P out;
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            const float d = to_f32(g.v[i]);
+            out.v[i] = from_f32<T>(w[j] * d);
+            if (q.dw != nullptr) dot[j] = fmaf(d, to_f32(v[j].v[i]), dot[j]);
+          }
+          if (q.dys != nullptr) *reinterpret_cast<P*>(dys + row[j] * q.dys_ld + c) = out;
+        }
+    }
+    if (q.dw == nullptr) continue;
+    group_sum(dot, q.warps, group, buf);
+    if (i0 == 0) {
+#pragma unroll
+      for (int j = 0; j < SLOTS; ++j)
+        if (j0 + j < q.k) q.dw[t * q.k + j0 + j] = dot[j];
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+int moe_ctas(int64_t tokens) {
+  const int64_t most = 2 * (int64_t)sm_count();
+  return (int)(tokens < most ? tokens : most);
+}
+size_t moe_hist_bytes(int64_t tokens, int k, int experts) {
+  return tokens * k <= MOE_SMALL ? 0 : (size_t)4 * moe_ctas(tokens) * experts;
+}
+
+bool sizes_ok(int64_t tokens, int k, int d, int32_t dtype) {
+  return tokens >= 0 && k >= 1 && d >= 1 && (dtype == CAMERA_BF16 || dtype == CAMERA_F32);
+}
+bool sizes_fit(int64_t tokens, int k, int d) { return k <= MAX_TOPK && tokens < (1ll << 31) && tokens * k < (1ll << 31) && d <= MOE_MAX_D; }
+bool rows_fit(const void* p, int64_t ld, int d, int size) {
+  return p != nullptr && ld >= d && (reinterpret_cast<uintptr_t>(p) & (size - 1)) == 0;
+}
+bool words_ok(const void* p) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+
+#define MOE_CK(...)             \
+  do {                          \
+    if ((__VA_ARGS__) != cudaSuccess) { \
+      cudaGetLastError();       \
+      return CAMERA_ERR_CUDA;   \
+    }                           \
+  } while (0)
+
+template <typename T>
+cudaError_t launch_dispatch(const Dispatch& q, bool vec, int ctas, cudaStream_t st) {
+  constexpr int W = 16 / (int)sizeof(T);
+  const int smem = 4 * q.experts * (2 + MOE_WARPS);
+  return vec ? launch_chained(k_moe_dispatch<T, W>, q, ctas, 1, 1, MOE_THREADS, smem, q.hist != nullptr, st)
+             : launch_chained(k_moe_dispatch<T, 1>, q, ctas, 1, 1, MOE_THREADS, smem, q.hist != nullptr, st);
+}
+template <typename T, int W>
+cudaError_t launch_combine_as(const Combine& q, cudaStream_t st) {
+  const int packs = (q.d + W - 1) / W, slices = (packs + 255) / 256;
+  const int bx = ((packs + slices - 1) / slices + 31) & ~31, ty = 256 / bx;
+  k_moe_combine<T, W><<<dim3((unsigned)((q.tokens + ty - 1) / ty), (unsigned)slices), dim3((unsigned)bx, (unsigned)ty), 0, st>>>(q);
+  return cudaGetLastError();
+}
+template <typename T, int W>
+cudaError_t launch_combine_backward_as(const Combine& a, cudaStream_t st) {
+  Combine q = a;
+  const int packs = (q.d + W - 1) / W;
+  // four packs a thread; one where there are fewer tokens than CTAs the GPU holds
+  const int each = q.tokens < 2 * sm_count() ? 1 : 4;
+  q.warps = (packs + 32 * each - 1) / (32 * each);
+  if (q.warps > 16) q.warps = 16;
+  const int groups = q.warps >= 8 ? 1 : 8 / q.warps;
+  k_moe_combine_backward<T, W><<<(unsigned)((q.tokens + groups - 1) / groups), 32 * q.warps * groups, 0, st>>>(q);
+  return cudaGetLastError();
+}
+
+int combine(const void* ys, int32_t dtype, int64_t ys_ld, int64_t n_rows, const int32_t* rows, const float* w, int64_t tokens, int32_t k,
+            int32_t d, const void* add, int64_t add_ld, void* y, int64_t y_ld, void* cuda_stream) {
+  if (!sizes_ok(tokens, k, d, dtype) || n_rows < 0) return CAMERA_ERR_INVALID_ARG;
+  if (!sizes_fit(tokens, k, d)) return CAMERA_ERR_UNSUPPORTED_SHAPE;
+  const int size = dtype == CAMERA_BF16 ? 2 : 4;
+  if (tokens == 0) return CAMERA_OK;
+  if (!words_ok(rows) || (w != nullptr && !words_ok(w)) || !rows_fit(y, y_ld, d, size) || (n_rows > 0 && !rows_fit(ys, ys_ld, d, size)) ||
+      (add != nullptr && !rows_fit(add, add_ld, d, size)))
+    return CAMERA_ERR_INVALID_ARG;
+  Combine q = {};
+  q.ys = ys; q.add = add; q.y = y; q.ys_ld = ys_ld; q.add_ld = add_ld; q.y_ld = y_ld; q.n_rows = n_rows;
+  q.rows = rows; q.w = w; q.tokens = (int)tokens; q.k = k; q.d = d;
+  const bool vec = (d * size) % 16 == 0 && vec_ok(ys, ys_ld, size) && vec_ok(add, add_ld, size) && vec_ok(y, y_ld, size);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (size == 2) MOE_CK(vec ? launch_combine_as<__nv_bfloat16, 8>(q, st) : launch_combine_as<__nv_bfloat16, 1>(q, st));
+  else MOE_CK(vec ? launch_combine_as<float, 4>(q, st) : launch_combine_as<float, 1>(q, st));
+  return CAMERA_OK;
+}
+
+}  // namespace
+}  // namespace camera
+
+extern "C" size_t camera_moe_dispatch_workspace_bytes(int64_t n_tokens, int32_t top_k, int32_t n_experts) {
+  using namespace camera;
+  if (n_tokens < 0 || top_k < 1 || n_experts < 1 || n_experts > MOE_MAX_EXPERTS || !sizes_fit(n_tokens, top_k, 1)) return 0;
+  return 256 + moe_hist_bytes(n_tokens, top_k, n_experts);
+}
+
+extern "C" int camera_moe_dispatch(const void* x, int32_t dtype, int64_t ld, int64_t n_tokens, int32_t d_model,
+                                   const int32_t* topk_idx, int32_t top_k, int32_t n_experts, void* x_sorted, int64_t sorted_ld,
+                                   int32_t* rows, int32_t* offsets, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  using namespace camera;
+  if (!sizes_ok(n_tokens, top_k, d_model, dtype) || n_experts < 1) return CAMERA_ERR_INVALID_ARG;
+  if (!sizes_fit(n_tokens, top_k, d_model) || n_experts > MOE_MAX_EXPERTS) return CAMERA_ERR_UNSUPPORTED_SHAPE;
+  if (!words_ok(offsets)) return CAMERA_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (n_tokens == 0) {
+    MOE_CK(cudaMemsetAsync(offsets, 0, (size_t)4 * (n_experts + 1), st));
+    return CAMERA_OK;
+  }
+  const int size = dtype == CAMERA_BF16 ? 2 : 4;
+  if (!words_ok(topk_idx) || !words_ok(rows) || !rows_fit(x, ld, d_model, size) || !rows_fit(x_sorted, sorted_ld, d_model, size))
+    return CAMERA_ERR_INVALID_ARG;
+  const size_t hist = moe_hist_bytes(n_tokens, top_k, n_experts);
+  if (hist > 0 && (workspace == nullptr || workspace_bytes < hist || (reinterpret_cast<uintptr_t>(workspace) & 255))) return CAMERA_ERR_WORKSPACE;
+  Dispatch q = {};
+  q.x = x; q.xs = x_sorted; q.x_ld = ld; q.xs_ld = sorted_ld;
+  q.idx = topk_idx; q.rows = rows; q.offsets = offsets;
+  q.tokens = (int)n_tokens; q.k = top_k; q.experts = n_experts; q.d = d_model;
+  int ctas = moe_ctas(n_tokens);
+  q.chunk = (int)((n_tokens + ctas - 1) / ctas);
+  ctas = (int)((n_tokens + q.chunk - 1) / q.chunk);
+  if (hist > 0) {
+    q.hist = static_cast<int32_t*>(workspace);
+    MOE_CK(launch_chained(k_moe_count, q, ctas, 1, 1, MOE_THREADS, 4 * n_experts, false, st));
+  }
+  const bool vec = (d_model * size) % 16 == 0 && vec_ok(x, ld, size) && vec_ok(x_sorted, sorted_ld, size);
+  MOE_CK(size == 2 ? launch_dispatch<__nv_bfloat16>(q, vec, ctas, st) : launch_dispatch<float>(q, vec, ctas, st));
+  return CAMERA_OK;
+}
+
+extern "C" int camera_moe_combine(const void* y_sorted, int32_t dtype, int64_t sorted_ld, int64_t n_rows, const int32_t* rows,
+                                  const float* topk_w, int64_t n_tokens, int32_t top_k, int32_t d_model, const void* add,
+                                  int64_t add_ld, void* y, int64_t ld, void* cuda_stream) {
+  return camera::combine(y_sorted, dtype, sorted_ld, n_rows, rows, topk_w, n_tokens, top_k, d_model, add, add_ld, y, ld, cuda_stream);
+}
+
+extern "C" int camera_moe_dispatch_backward(const void* dx_sorted, int32_t dtype, int64_t sorted_ld, int64_t n_rows, const int32_t* rows,
+                                            int64_t n_tokens, int32_t top_k, int32_t d_model, const void* add, int64_t add_ld,
+                                            void* dx, int64_t ld, void* cuda_stream) {
+  return camera::combine(dx_sorted, dtype, sorted_ld, n_rows, rows, nullptr, n_tokens, top_k, d_model, add, add_ld, dx, ld, cuda_stream);
+}
+
+extern "C" int camera_moe_combine_backward(const void* dy, int32_t dtype, int64_t ld, int64_t n_tokens, int32_t d_model,
+                                           const int32_t* rows, const float* topk_w, int32_t top_k, const void* y_sorted,
+                                           int64_t sorted_ld, int64_t n_rows, void* dy_sorted, int64_t dy_sorted_ld,
+                                           float* d_topk_w, void* cuda_stream) {
+  using namespace camera;
+  if (!sizes_ok(n_tokens, top_k, d_model, dtype) || n_rows < 0 || (dy_sorted == nullptr && d_topk_w == nullptr))
+    return CAMERA_ERR_INVALID_ARG;
+  if (!sizes_fit(n_tokens, top_k, d_model)) return CAMERA_ERR_UNSUPPORTED_SHAPE;
+  if (n_tokens == 0) return CAMERA_OK;
+  const int size = dtype == CAMERA_BF16 ? 2 : 4;
+  if (!words_ok(rows) || (topk_w != nullptr && !words_ok(topk_w)) || (d_topk_w != nullptr && !words_ok(d_topk_w)) ||
+      !rows_fit(dy, ld, d_model, size) || (dy_sorted != nullptr && n_rows > 0 && !rows_fit(dy_sorted, dy_sorted_ld, d_model, size)) ||
+      (d_topk_w != nullptr && n_rows > 0 && !rows_fit(y_sorted, sorted_ld, d_model, size)))
+    return CAMERA_ERR_INVALID_ARG;
+  Combine q = {};
+  q.ys = y_sorted; q.dy = dy; q.dys = dy_sorted; q.dw = d_topk_w;
+  q.ys_ld = sorted_ld; q.dy_ld = ld; q.dys_ld = dy_sorted_ld; q.n_rows = n_rows;
+  q.rows = rows; q.w = topk_w; q.tokens = (int)n_tokens; q.k = top_k; q.d = d_model;
+  const bool vec = (d_model * size) % 16 == 0 && vec_ok(dy, ld, size) && vec_ok(dy_sorted, dy_sorted_ld, size) &&
+                   (d_topk_w == nullptr || vec_ok(y_sorted, sorted_ld, size));
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (size == 2) MOE_CK(vec ? launch_combine_backward_as<__nv_bfloat16, 8>(q, st) : launch_combine_backward_as<__nv_bfloat16, 1>(q, st));
+  else MOE_CK(vec ? launch_combine_backward_as<float, 4>(q, st) : launch_combine_backward_as<float, 1>(q, st));
+  return CAMERA_OK;
+}

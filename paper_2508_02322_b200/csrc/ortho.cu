@@ -1,0 +1,743 @@
+// Orthogonalised updates: an odd polynomial applied to the singular values of a matrix, a few times over, by products alone
+// (Newton-Schulz products).
+//   X = U / (|U|_F + eps);   each step:  A = X X^T,  B = a I + b A + c A A,  X <- B X
+// X is the matrix with its shorter side as rows (m), its longer as columns (n).  A and B are symmetric: only tiles on and
+// above the diagonal are computed, each stored twice.  A step is m^2 n + m^3 + 2 m^2 n operations, so all of this is bound by
+// the tensor pipe where matrices are large, and by the number of k blocks in a row where they are small.
+//
+// The operands of the products are fp16 with a power of two as factor, the sums fp32.  With h a bound of the singular values
+// of X, no element of X is larger than h, none of A than h^2, none of B than the polynomial's largest value over [0, h^2]: the
+// host follows these bounds from step to step (1 before the first) and picks the largest factors under which nothing can
+// overflow.  fp16 has 3 bits more than bf16: results are 1e-3 off 64 bits (root mean square, relative; bf16 operands 8e-3),
+// below their own rounding to bf16, 1.7e-3.  The first X is the matrix itself times a power of two, so bf16 inputs enter
+// exactly; 1 / (|U| + eps) goes into the factors of the first step.
+//
+// Matrices of one call lie one below the other in the workspace, padded with zeros to whole tiles of 256 rows and whole
+// 64 columns, so one tensor map serves them all and one launch walks the tiles of them all.
+#include <cuda.h>
+#include <cuda_fp16.h>
+#include <math.h>
+#include <string.h>
+
+#include "common.cuh"
+#include "launch.cuh"
+#include "umma.cuh"
+#include "umma_pair.cuh"
+
+namespace camera {
+
+namespace {
+
+constexpr int O_EPI_WARPS = 8;               // epilogue: two warps per 32 rows, each with half of the columns
+constexpr int O_PRODUCER = O_EPI_WARPS, O_ISSUER = O_EPI_WARPS + 1;
+constexpr int O_THREADS = 32 * (O_EPI_WARPS + 2);
+constexpr int O_TILE_M = 256;                // rows of the output a pair computes: 128 per CTA
+constexpr int O_A_BYTES = 128 * 128;         // this CTA's 128 rows x 64 k
+constexpr int O_MAX_STAGES = 8;
+constexpr int O_RING_BYTES = 192 * 1024;
+constexpr int O_SMEM_BYTES = O_RING_BYTES + 256 + 1024;
+constexpr int O_GROUP_M = 16;                // row tiles that are walked together
+constexpr int O_TMEM_COLS = 512;
+constexpr int O_MAX_MATS = 64;               // matrices of one round of launches
+constexpr long long O_MAX_ELEMS = 1ll << 27; // and the elements of X that close a round
+constexpr int O_MAX_SIDE = 1 << 17;
+
+enum { ORTHO_GRAM = 0, ORTHO_POLY = 1, ORTHO_APPLY = 2 };
+
+struct OrthoMat {
+  const void* in;
+  void* out;
+  long long in_ld, out_ld;
+  int m, n;                 // shorter and longer side
+  int row0;                 // first row in the packed buffers
+  int turned;               // in and out are [n, m]
+};
+
+struct OrthoBatch {
+  int n_mats;
+  OrthoMat mat[O_MAX_MATS];
+};
+
+struct OrthoGemm {
+  CUtensorMap a, b;
+  OrthoBatch batch;
+  int unit0[O_MAX_MATS + 1];
+  int n_units;
+  int bn, nb, kps, n_stages, n_acc;      // columns per B tile, B tiles per unit, k blocks per stage, ring depth, accumulators
+  const __half* aux;        // POLY: A
+  __half* out;              // packed result, or null: the caller's matrices
+  long long aux_ld, out_ld;
+  float f_acc, f_aux, f_diag;
+  const float* first;       // factor of each matrix's first X, or null
+  PlanTotals* totals;
+  unsigned long long wait_limit_ns;
+};
+
+static_assert(sizeof(OrthoGemm) <= 4096, "kernel arguments");
+
+__host__ __device__ __forceinline__ int pad_rows(int m) { return (m + O_TILE_M - 1) / O_TILE_M * O_TILE_M; }
+__host__ __device__ __forceinline__ int pad_cols(int n) { return (n + UMMA_BK - 1) / UMMA_BK * UMMA_BK; }
+
+// Units of one matrix: symmetric products take, per row tile of 256, the column tiles from the diagonal on; the others all.
+template <int MODE>
+__host__ __device__ __forceinline__ int units_of(int m, int n, int w) {
+  const int rt = pad_rows(m) / O_TILE_M;
+  if (MODE == ORTHO_APPLY) return rt * ((n + w - 1) / w);
+  int units = 0;
+  for (int i = 0; i < rt; ++i) units += ((rt - i) * O_TILE_M + w - 1) / w;
+  return units;
+}
+
+struct OrthoUnit { int e, m0, n0, two, kb, limit; };
+
+template <int MODE>
+__device__ __forceinline__ OrthoUnit ortho_unit(const OrthoGemm& q, int unit) {
+  OrthoUnit r;
+  r.e = upper_segment(q.unit0, q.batch.n_mats, unit);
+  int rem = unit - q.unit0[r.e];
+  const int m = q.batch.mat[r.e].m, n = q.batch.mat[r.e].n, w = q.nb * q.bn;
+  const int rt = pad_rows(m) / O_TILE_M;
+  if (MODE == ORTHO_APPLY) {
+    // row tiles in groups of O_GROUP_M, the row tile fastest: what runs at one time shares few column tiles and rows of B
+    const int ct = (n + w - 1) / w, per_group = O_GROUP_M * ct, grp = rem / per_group;
+    rem -= grp * per_group;
+    const int in_group = min(O_GROUP_M, rt - grp * O_GROUP_M);
+    r.m0 = (grp * O_GROUP_M + rem % in_group) * O_TILE_M;
+    r.n0 = (rem / in_group) * w;
+    r.limit = pad_cols(n);
+    r.kb = pad_cols(m) / UMMA_BK;
+  } else {
+    int i = 0;
+    for (;; ++i) {
+      const int c = ((rt - i) * O_TILE_M + w - 1) / w;
+      if (rem < c) break;
+      rem -= c;
+    }
+    r.m0 = i * O_TILE_M;
+    r.n0 = r.m0 + rem * w;
+    r.limit = rt * O_TILE_M;
+    r.kb = pad_cols(MODE == ORTHO_GRAM ? n : m) / UMMA_BK;
+  }
+  r.two = q.nb == 2 && r.n0 + q.bn < r.limit;
+  return r;
+}
+
+__device__ __forceinline__ uint32_t pack_half(float a, float b) {
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// The transpose of 16 columns of a warp's 32 rows: p[j] holds columns 2j and 2j + 1 of this lane's row.  Two lanes exchange
+// halves, so that each stores two neighbouring rows of a column in one word.  at: where column 0 of this warp's first row
+// goes; columns are ld elements apart, rows follow one another.
+__device__ __forceinline__ void store_turned(uint16_t* at, long long ld, const uint32_t* p, int lane, int rows, int cols, bool words) {
+  if (words && rows >= 32) {
+    const bool odd = lane & 1;
+    uint32_t* const dst = reinterpret_cast<uint32_t*>(at + (odd ? ld : 0) + (lane & ~1));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t other = __shfl_xor_sync(0xffffffffu, p[j], 1);
+      const uint32_t v = odd ? __byte_perm(other, p[j], 0x7632) : __byte_perm(p[j], other, 0x5410);
+      if (2 * j + odd < cols) *reinterpret_cast<uint32_t*>(reinterpret_cast<uint16_t*>(dst) + 2 * j * ld) = v;
+    }
+  } else if (lane < rows) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      if (j < cols) at[j * ld + lane] = (uint16_t)(j & 1 ? p[j >> 1] >> 16 : p[j >> 1] & 0xffffu);
+  }
+}
+
+template <int MODE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_ortho_gemm(const __grid_constant__ OrthoGemm q) {
+  constexpr bool B_MN = MODE == ORTHO_APPLY;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t bars = base + O_RING_BYTES;
+  auto full_bar = [&](int s) { return bars + 8u * s; };                                 // first CTA
+  auto empty_bar = [&](int s) { return bars + 8u * (O_MAX_STAGES + s); };               // each CTA
+  auto tfull_bar = [&](int a) { return bars + 8u * (2 * O_MAX_STAGES + a); };           // each CTA
+  auto tempty_bar = [&](int a) { return bars + 8u * (2 * O_MAX_STAGES + 2 + a); };      // first CTA, the pair's epilogue threads
+  uint8_t* const tail = base_ptr + O_RING_BYTES + 8 * (2 * O_MAX_STAGES + 4);
+  volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(tail + 8);
+
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int n_pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
+  const int half = q.bn >> 1;                               // columns of a B tile this CTA supplies
+  const int b_bytes = half * 128;
+  const int block_bytes = O_A_BYTES + q.nb * b_bytes;       // operands of one k block
+  const int stage_bytes = q.kps * block_bytes;
+
+  if (tid == 0) {
+    for (int s = 0; s < q.n_stages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 2 * 32 * O_EPI_WARPS); }
+    wait_state_init(abort_flag, q.wait_limit_ns);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == O_ISSUER) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_slot)),
+                 "r"(O_TMEM_COLS)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();     // the other CTA's barriers are initialised before anything arrives on them
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  if (warp == O_PRODUCER) {
+    // ------------------------------------------------------------------ TMA producer (each CTA loads its own share)
+    const uint32_t lead = lane == 0;
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
+      const OrthoUnit u = ortho_unit<MODE>(q, unit);
+      const int row0 = q.batch.mat[u.e].row0;
+      const int am = row0 + u.m0 + 128 * (int)rank, bn0 = u.n0 + half * (int)rank;
+      for (int kb = 0, blocks; kb < u.kb; kb += blocks) {
+        blocks = min(q.kps, u.kb - kb);
+        ok = warp_wait(empty_bar(stage), phase ^ 1u, abort_flag);
+        if (!ok) break;
+        const uint32_t full0 = map_to_cta(full_bar(stage), 0);
+        if (rank == 0 && lane == 0) mbar_expect_tx(full_bar(stage), 2 * blocks * (O_A_BYTES + (u.two ? 2 : 1) * b_bytes));
+        __syncwarp();
+        uint32_t dst = base + stage * stage_bytes;
+        for (int k0 = kb * UMMA_BK; k0 < (kb + blocks) * UMMA_BK; k0 += UMMA_BK, dst += block_bytes) {
+          tma_load_lead(lead, dst, &q.a, full0, k0, am);
+          const uint32_t dst_b = dst + O_A_BYTES;
+          if (B_MN) {
+            tma_load_lead(lead, dst_b, &q.b, full0, bn0, row0 + k0);
+            if (half > 64) tma_load_lead(lead, dst_b + 8192, &q.b, full0, bn0 + 64, row0 + k0);
+            if (u.two) {
+              tma_load_lead(lead, dst_b + b_bytes, &q.b, full0, bn0 + q.bn, row0 + k0);
+              if (half > 64) tma_load_lead(lead, dst_b + b_bytes + 8192, &q.b, full0, bn0 + q.bn + 64, row0 + k0);
+            }
+          } else {
+            tma_load_lead(lead, dst_b, &q.b, full0, k0, row0 + bn0);
+            if (u.two) tma_load_lead(lead, dst_b + b_bytes, &q.b, full0, k0, row0 + bn0 + q.bn);
+          }
+        }
+        if (++stage == q.n_stages) { stage = 0; phase ^= 1u; }
+      }
+    }
+    if (!ok) {               // copies in flight land before the CTA's shared memory is given up
+      const unsigned long long t0 = globaltimer_ns();
+      while (globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
+    }
+  } else if (warp == O_ISSUER) {
+    // ------------------------------------------------------------------ MMA issuer (first CTA of the pair only)
+    if (rank == 0) {
+      const uint32_t lead = lane == 0;
+      int stage = 0, acc = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      bool ok = true, ready = false;       // ready: the next stage has been seen full
+      const uint32_t idesc = make_idesc_pair_f16(q.bn) | (B_MN ? 1u << 16 : 0u);
+      constexpr int A_STEP = 32 >> 4, B_STEP = B_MN ? 2048 >> 4 : 32 >> 4;     // 16 k further
+      const unsigned long long a_first = make_smem_desc(base);
+      const unsigned long long b_first = B_MN ? make_smem_desc_mn(base + O_A_BYTES) : make_smem_desc(base + O_A_BYTES);
+      const unsigned long long b2_off = (unsigned long long)(b_bytes >> 4);
+      for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
+        const OrthoUnit u = ortho_unit<MODE>(q, unit);
+        ok = __all_sync(0xffffffffu, mbar_wait_cluster(tempty_bar(acc), acc_phase ^ 1u, abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t d0 = tmem_base + (uint32_t)(acc * q.nb * q.bn), d1 = d0 + (uint32_t)q.bn;
+        uint32_t accumulate = 0;
+        for (int kb = 0, blocks; kb < u.kb; kb += blocks) {
+          blocks = min(q.kps, u.kb - kb);
+          if (!ready) {
+            ok = warp_wait(full_bar(stage), phase, abort_flag);
+            if (!ok) break;
+          }
+          tc_fence_after();
+          unsigned long long at = (unsigned long long)((uint32_t)(stage * stage_bytes) >> 4);
+          const uint32_t done = empty_bar(stage);
+          if (++stage == q.n_stages) { stage = 0; phase ^= 1u; }
+          for (int block = blocks; block > 0; --block, at += (unsigned long long)(block_bytes >> 4)) {
+            const unsigned long long a_desc = a_first + at, b_desc = b_first + at;
+            if (u.two) {
+              const unsigned long long b2_desc = b_desc + b2_off;
+#pragma unroll
+              for (int k = 0; k < UMMA_BK / 16; ++k) {
+                umma_lead(lead, d0, a_desc + A_STEP * k, b_desc + B_STEP * k, idesc, accumulate | (uint32_t)k);
+                umma_lead(lead, d1, a_desc + A_STEP * k, b2_desc + B_STEP * k, idesc, accumulate | (uint32_t)k);
+              }
+            } else {
+              umma_block<A_STEP, B_STEP>(lead, d0, a_desc, b_desc, idesc, accumulate);
+            }
+            accumulate = 1;
+          }
+          ready = __all_sync(0xffffffffu, mbar_test(full_bar(stage), phase));
+          umma_commit_lead(lead, done);
+        }
+        if (!ok) break;
+        umma_commit_lead(lead, tfull_bar(acc));
+        if (++acc == q.n_acc) { acc = 0; acc_phase ^= 1u; }
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ epilogue: a thread owns a row of the output
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    bool ok = true;
+    const int c_half = q.nb * q.bn / 2, c_first = c_half * (warp >> 2);
+    for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
+      const OrthoUnit u = ortho_unit<MODE>(q, unit);
+      const OrthoMat& mat = q.batch.mat[u.e];
+      const int warp_row = u.m0 + 128 * (int)rank + (warp & 3) * 32, row = warp_row + lane;      // in the matrix, < pad_rows(m)
+      const int cols = min(u.limit - u.n0, c_first + c_half);       // where this warp's columns end
+      float f = q.f_acc;
+      if (q.first != nullptr) {
+        const float s = q.first[u.e];
+        f = MODE == ORTHO_GRAM ? f / s / s : f / s;
+      }
+      ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_phase, abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t t0 = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(acc * q.nb * q.bn);
+      const long long at = (long long)(mat.row0 + row) * q.out_ld + u.n0;
+      auto put = [&](const uint32_t* v, int c) {
+        uint32_t p[8];
+        if (MODE == ORTHO_APPLY && q.out == nullptr) {
+          // the result, in the caller's layout
+#pragma unroll
+          for (int j = 0; j < 8; ++j) p[j] = pack_bf16(__uint_as_float(v[2 * j]) * f, __uint_as_float(v[2 * j + 1]) * f);
+          const int left = mat.n - u.n0 - c;                        // columns there are
+          uint16_t* const out = static_cast<uint16_t*>(mat.out);
+          if (mat.turned) {
+            uint16_t* const to = out + (long long)(u.n0 + c) * mat.out_ld + warp_row;
+            store_turned(to, mat.out_ld, p, lane, mat.m - warp_row, left,
+                         ((reinterpret_cast<uintptr_t>(out) & 3) | (mat.out_ld & 1)) == 0);
+          } else if (row < mat.m) {
+            uint16_t* const to = out + row * mat.out_ld + u.n0 + c;
+            if (left >= 16 && (reinterpret_cast<uintptr_t>(to) & 31) == 0) {
+              st_global_v8(to, p);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                if (j < left) to[j] = (uint16_t)(j & 1 ? p[j >> 1] >> 16 : p[j >> 1] & 0xffffu);
+            }
+          }
+          return;
+        }
+        if (MODE == ORTHO_POLY) {
+          uint32_t a[8];
+          const uint4* const src = reinterpret_cast<const uint4*>(q.aux + (long long)(mat.row0 + row) * q.aux_ld + u.n0 + c);
+          *reinterpret_cast<uint4*>(a) = src[0];
+          *reinterpret_cast<uint4*>(a + 4) = src[1];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float2 old = __half22float2(*reinterpret_cast<const __half2*>(&a[j]));
+            float lo = fmaf(old.x, q.f_aux, __uint_as_float(v[2 * j]) * f), hi = fmaf(old.y, q.f_aux, __uint_as_float(v[2 * j + 1]) * f);
+            if (u.n0 + c + 2 * j == row) lo += q.f_diag;
+            if (u.n0 + c + 2 * j + 1 == row) hi += q.f_diag;
+            p[j] = pack_half(lo, hi);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) p[j] = pack_half(__uint_as_float(v[2 * j]) * f, __uint_as_float(v[2 * j + 1]) * f);
+        }
+        st_global_v8(q.out + at + c, p);
+        if (MODE != ORTHO_APPLY && u.n0 + c >= u.m0 + O_TILE_M)      // off the diagonal's block: the other half of the result
+          store_turned(reinterpret_cast<uint16_t*>(q.out) + (long long)(mat.row0 + u.n0 + c) * q.out_ld + warp_row, q.out_ld, p, lane, 32, 16,
+                       true);
+      };
+      uint32_t v0[16], v1[16];
+      int c = c_first;
+      if (c < cols) tmem_ld16(t0 + c, v0);
+      for (; c < cols; c += 32) {
+        const int c1 = c + 16, c2 = c1 + 16;
+        tmem_ld_wait(v0);
+        if (c1 < cols) tmem_ld16(t0 + c1, v1);
+        put(v0, c);
+        if (c1 >= cols) break;
+        tmem_ld_wait(v1);
+        if (c2 < cols) tmem_ld16(t0 + c2, v0);
+        put(v1, c1);
+      }
+      tc_fence_before();
+      mbar_arrive_cluster(map_to_cta(tempty_bar(acc), 0));
+      if (++acc == q.n_acc) { acc = 0; acc_phase ^= 1u; }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag && tid == 0) atomicExch(&q.totals->status, (int)CAMERA_ERR_DEVICE_TIMEOUT);
+  cluster_sync_all();     // neither CTA leaves while the other may still read its shared or tensor memory
+  if (warp == O_ISSUER) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(O_TMEM_COLS) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ the first X
+struct OrthoLoad {
+  OrthoBatch batch;
+  double* part;             // [mats][parts] sums of squares
+  int parts;
+  float* first;             // [mats] factor between X as stored and X
+  float eps;
+  __half* x;
+  long long x_ld;
+  PlanTotals* totals;
+  int clear_status;
+};
+constexpr int LOAD_THREADS = 256;
+
+__device__ __forceinline__ double block_sum(double v) {
+  __shared__ double sums[LOAD_THREADS / 32];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = 0.0;
+#pragma unroll
+  for (int i = 0; i < LOAD_THREADS / 32; ++i) v += sums[i];
+  return v;
+}
+
+// Sums of squares of runs of rows; in double, so that no square of an fp32 value overflows or is lost.
+template <typename T>
+__global__ void __launch_bounds__(LOAD_THREADS) k_ortho_norm(const __grid_constant__ OrthoLoad q) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (q.clear_status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) q.totals->status = 0;
+  const OrthoMat& mat = q.batch.mat[blockIdx.y];
+  const int rows = mat.turned ? mat.n : mat.m, cols = mat.turned ? mat.m : mat.n;
+  const T* const in = static_cast<const T*>(mat.in);
+  double s0 = 0.0, s1 = 0.0;
+  for (int r = blockIdx.x * (LOAD_THREADS / 32) + (threadIdx.x >> 5); r < rows; r += gridDim.x * (LOAD_THREADS / 32)) {
+    const T* const p = in + r * mat.in_ld;
+    int c = threadIdx.x & 31;
+    for (; c + 224 < cols; c += 256) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = to_f32(p[c + 32 * i]);
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) { s0 = fma((double)v[i], (double)v[i], s0); s1 = fma((double)v[i + 1], (double)v[i + 1], s1); }
+    }
+    for (; c < cols; c += 32) { const double v = to_f32(p[c]); s0 = fma(v, v, s0); }
+  }
+  const double s = block_sum(s0 + s1);
+  if (threadIdx.x == 0) q.part[blockIdx.y * q.parts + blockIdx.x] = s;
+}
+
+// X = U 2^p in fp16, shorter side as rows, zeros around it.  p puts 2^p (|U| + eps) into [2^14, 2^15): nothing overflows, and
+// what is below 2^-39 of the norm is lost.  A CTA turns tiles of 64 x 64 in shared memory.
+template <typename T>
+__global__ void __launch_bounds__(LOAD_THREADS) k_ortho_load(const __grid_constant__ OrthoLoad q) {
+  __shared__ __align__(16) __half tile[64][72];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const OrthoMat& mat = q.batch.mat[blockIdx.y];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < q.parts; i += LOAD_THREADS) s += q.part[blockIdx.y * q.parts + i];
+  const double norm = sqrt(block_sum(s)) + (double)q.eps;
+  int p = 0;
+  if (norm > 0.0 && norm < 1e300) {
+    int e;
+    frexp(norm, &e);                    // norm in [2^(e-1), 2^e)
+    p = 15 - e;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) q.first[blockIdx.y] = norm == 0.0 ? 1.f : norm < 1e300 ? (float)ldexp(norm, p) : __int_as_float(0x7fffffff);
+  const int rt = pad_rows(mat.m) / 64, ct = pad_cols(mat.n) / 64;
+  const T* const in = static_cast<const T*>(mat.in);
+  for (int t = blockIdx.x; t < rt * ct; t += gridDim.x) {
+    const int r0 = t / ct * 64, c0 = t % ct * 64;
+    __syncthreads();
+    const int a0 = mat.turned ? c0 : r0, b0 = mat.turned ? r0 : c0;         // in the caller's rows and columns
+    const int a_end = mat.turned ? mat.n : mat.m, b_end = mat.turned ? mat.m : mat.n;
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int k = threadIdx.x + LOAD_THREADS * i, a = k >> 6, b = k & 63;
+      v[i] = a0 + a < a_end && b0 + b < b_end ? to_f32(in[(a0 + a) * mat.in_ld + b0 + b]) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int k = threadIdx.x + LOAD_THREADS * i, a = k >> 6, b = k & 63;
+      const __half h = __float2half_rn(ldexpf(v[i], p));
+      if (mat.turned) tile[b][a] = h; else tile[a][b] = h;
+    }
+    __syncthreads();
+    const int r = threadIdx.x >> 2, part = (threadIdx.x & 3) * 16;
+    uint32_t w[8];
+    *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(&tile[r][part]);
+    *reinterpret_cast<uint4*>(w + 4) = *reinterpret_cast<const uint4*>(&tile[r][part + 8]);
+    st_global_v8(q.x + (long long)(mat.row0 + r0 + r) * q.x_ld + c0 + part, w);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+// One round of launches: matrices [begin, end) of the call, those without elements left out.
+struct OrthoRound {
+  int begin, end;
+  long long rows;           // of the packed buffers
+  int x_ld, a_ld;
+};
+OrthoRound ortho_round(const camera_matrix_t* mats, int n, int begin) {
+  OrthoRound r = {begin, begin, 0, 0, 0};
+  int count = 0;
+  for (; r.end < n && count < O_MAX_MATS; ++r.end) {
+    const camera_matrix_t& t = mats[r.end];
+    if (t.rows == 0 || t.cols == 0) continue;
+    const int m = t.rows < t.cols ? t.rows : t.cols, w = t.rows < t.cols ? t.cols : t.rows;
+    const long long rows = r.rows + pad_rows(m);
+    const int x_ld = pad_cols(w) > r.x_ld ? pad_cols(w) : r.x_ld, a_ld = pad_rows(m) > r.a_ld ? pad_rows(m) : r.a_ld;
+    if (count > 0 && rows * x_ld > O_MAX_ELEMS) break;
+    r.rows = rows; r.x_ld = x_ld; r.a_ld = a_ld;
+    ++count;
+  }
+  return r;
+}
+constexpr int MAX_PARTS = 296;
+struct OrthoLayout { size_t part, first, x0, x1, a, b, total; };
+OrthoLayout ortho_layout(const OrthoRound& r) {
+  OrthoLayout l;
+  l.part = up256(sizeof(PlanTotals));
+  l.first = l.part + up256((size_t)8 * O_MAX_MATS * MAX_PARTS);
+  l.x0 = l.first + up256(4 * O_MAX_MATS);
+  const size_t x = up256((size_t)2 * r.rows * r.x_ld), a = up256((size_t)2 * r.rows * r.a_ld);
+  l.x1 = l.x0 + x;
+  l.a = l.x1 + x;
+  l.b = l.a + a;
+  l.total = l.b + a;
+  return l;
+}
+
+int check_matrices(const camera_matrix_t* mats, int32_t n, int32_t dtype, bool pointers) {
+  if (n < 0 || (n > 0 && mats == nullptr) || (dtype != CAMERA_BF16 && dtype != CAMERA_F32)) return CAMERA_ERR_INVALID_ARG;
+  const uintptr_t mask = dtype == CAMERA_BF16 ? 1 : 3;
+  for (int i = 0; i < n; ++i) {
+    const camera_matrix_t& t = mats[i];
+    if (t.rows < 0 || t.cols < 0) return CAMERA_ERR_INVALID_ARG;
+    if (t.rows > O_MAX_SIDE || t.cols > O_MAX_SIDE || (t.rows > O_MAX_SIDE / 4 && t.cols > O_MAX_SIDE / 4)) return CAMERA_ERR_UNSUPPORTED_SHAPE;
+    if (!pointers || t.rows == 0 || t.cols == 0) continue;
+    if (t.in == nullptr || t.out == nullptr || t.in_ld < t.cols || t.out_ld < t.cols || (reinterpret_cast<uintptr_t>(t.in) & mask) ||
+        (reinterpret_cast<uintptr_t>(t.out) & 1))
+      return CAMERA_ERR_INVALID_ARG;
+  }
+  return CAMERA_OK;
+}
+
+// Bounds of what a step makes of singular values in [0, h]: of |a + b t + c t^2| over t in [0, h^2] (no element of B is
+// larger) and of s |a + b s^2 + c s^4| over [0, h] (the singular values after the step).
+struct StepBound { double b, h; };
+StepBound step_bound(const float* k, double h) {
+  const double a = k[0], b = k[1], c = k[2], t1 = h * h;
+  double ts[4] = {0.0, t1, t1, t1};
+  auto poly = [&](double t) { return fabs(a + t * (b + t * c)); };
+  StepBound r = {0.0, 0.0};
+  if (c != 0.0 && -b / (2 * c) > 0.0 && -b / (2 * c) < t1) ts[2] = -b / (2 * c);
+  for (double t : ts) r.b = fmax(r.b, poly(t));
+  ts[2] = ts[3] = t1;
+  const double disc = 9 * b * b - 20 * a * c;        // a + 3 b t + 5 c t^2 = 0
+  if (c != 0.0 && disc >= 0.0) {
+    const double s = sqrt(disc), u = (-3 * b + s) / (10 * c), v = (-3 * b - s) / (10 * c);
+    if (u > 0.0 && u < t1) ts[2] = u;
+    if (v > 0.0 && v < t1) ts[3] = v;
+  } else if (c == 0.0 && b != 0.0 && -a / (3 * b) > 0.0 && -a / (3 * b) < t1) {
+    ts[2] = -a / (3 * b);
+  }
+  for (double t : ts) r.h = fmax(r.h, sqrt(t) * poly(t));
+  return r;
+}
+constexpr double MARGIN = 1.02;         // for the roundings, which the bounds leave out (some 1e-3 a step)
+constexpr double MOST = 1e3;            // singular values beyond this: the polynomial is not one that converges
+double factor_for(double bound) { return ldexp(1.0, (int)floor(log2(65504.0 / fmax(bound * MARGIN, 1e-3)))); }
+
+// Tiles: the choice with the least estimated time, rounds of units over the pairs times a unit's time.  Per k block 0.60 us
+// for 512 columns, 0.43 for 256, 0.32 for 128 (measured in the feed-forward block's kernel, which feeds the pipe the same
+// way); a unit of 512 columns adds its epilogue, smaller ones have two accumulators and overlap it.
+struct OrthoTile { int bn, nb; };
+template <int MODE>
+OrthoTile choose_tile(const OrthoBatch& b, int n_pairs) {
+  static constexpr OrthoTile kinds[3] = {{256, 2}, {256, 1}, {128, 1}};
+  static constexpr double k_block[3] = {0.60, 0.43, 0.32};
+  OrthoTile best = kinds[0];
+  double best_cost = 1e300;
+  for (int i = 0; i < 3; ++i) {
+    long long units = 0, blocks = 0, longest = 0;
+    for (int e = 0; e < b.n_mats; ++e) {
+      const int u = units_of<MODE>(b.mat[e].m, b.mat[e].n, kinds[i].bn * kinds[i].nb);
+      const int kb = pad_cols(MODE == ORTHO_GRAM ? b.mat[e].n : b.mat[e].m) / UMMA_BK;
+      units += u;
+      blocks += (long long)u * kb;
+      if (kb > longest) longest = kb;
+    }
+    const double mean = (double)blocks / units, rounds = (double)((units + n_pairs - 1) / n_pairs);
+    const double cost = (rounds > 1 ? rounds * mean : (double)longest) * k_block[i] + rounds * (i == 0 ? 4.0 : 1.0);
+    if (cost < best_cost * 0.99) { best = kinds[i]; best_cost = cost; }
+  }
+  return best;
+}
+
+bool enc_f16(CUtensorMap* out, const void* p, long long rows, long long cols, int box_rows) {
+  // fp16 and bf16 differ in nothing a copy without arithmetic sees
+  return encode_bf16_2d_pitch(out, p, (uint64_t)rows, (uint64_t)cols, (uint64_t)cols, (uint32_t)box_rows);
+}
+
+#define ORTHO_CK(...)             \
+  do {                            \
+    if ((__VA_ARGS__) != cudaSuccess) { \
+      cudaGetLastError();         \
+      return CAMERA_ERR_CUDA;     \
+    }                             \
+  } while (0)
+
+// a, b: the packed operands (rows x cols); B of APPLY is read with its columns as N.
+template <int MODE>
+int launch_ortho(OrthoGemm& q, const __half* a, long long a_cols, const __half* b, long long b_cols, long long rows, int n_pairs,
+                 cudaStream_t st) {
+  const OrthoTile t = choose_tile<MODE>(q.batch, n_pairs);
+  q.bn = t.bn; q.nb = t.nb;
+  q.n_acc = t.nb * t.bn <= 256 ? 2 : 1;
+  q.kps = t.nb * t.bn <= 256 ? 2 : 1;
+  const int stage = q.kps * (O_A_BYTES + t.nb * t.bn * 64);
+  q.n_stages = O_RING_BYTES / stage < O_MAX_STAGES ? O_RING_BYTES / stage : O_MAX_STAGES;
+  int units = 0;
+  for (int e = 0; e < q.batch.n_mats; ++e) {
+    q.unit0[e] = units;
+    units += units_of<MODE>(q.batch.mat[e].m, q.batch.mat[e].n, t.nb * t.bn);
+  }
+  q.unit0[q.batch.n_mats] = units;
+  q.n_units = units;
+  if (!enc_f16(&q.a, a, rows, a_cols, 128) || !enc_f16(&q.b, b, rows, b_cols, MODE == ORTHO_APPLY ? 64 : t.bn / 2)) return CAMERA_ERR_CUDA;
+  ORTHO_CK(allow_smem<k_ortho_gemm<MODE>, O_SMEM_BYTES>());
+  ORTHO_CK(launch_chained(k_ortho_gemm<MODE>, q, 2 * (units < n_pairs ? units : n_pairs), 1, 1, O_THREADS, O_SMEM_BYTES, true, st));
+  return CAMERA_OK;
+}
+
+int run_round(const camera_matrix_t* mats, const OrthoRound& r, int32_t dtype, const float* coefficients, int32_t steps, float eps, char* ws,
+              bool first_round, cudaStream_t st) {
+  const OrthoLayout l = ortho_layout(r);
+  OrthoGemm q;
+  memset(&q, 0, sizeof(q));
+  long long row0 = 0, tiles = 0;
+  for (int i = r.begin; i < r.end; ++i) {
+    const camera_matrix_t& t = mats[i];
+    if (t.rows == 0 || t.cols == 0) continue;
+    OrthoMat& o = q.batch.mat[q.batch.n_mats++];
+    o.turned = t.rows > t.cols;
+    o.m = o.turned ? t.cols : t.rows;
+    o.n = o.turned ? t.rows : t.cols;
+    o.in = t.in; o.out = t.out; o.in_ld = t.in_ld; o.out_ld = t.out_ld;
+    o.row0 = (int)row0;
+    row0 += pad_rows(o.m);
+    const long long here = (long long)(pad_rows(o.m) / 64) * (pad_cols(o.n) / 64);
+    if (here > tiles) tiles = here;
+  }
+  if (q.batch.n_mats == 0) return CAMERA_OK;
+  const int sms = sm_count(), n_pairs = sms / 2;
+  __half* x = reinterpret_cast<__half*>(ws + l.x0);
+  __half* x_next = reinterpret_cast<__half*>(ws + l.x1);
+  __half* const a = reinterpret_cast<__half*>(ws + l.a);
+  __half* const b = reinterpret_cast<__half*>(ws + l.b);
+  OrthoLoad ld;
+  ld.batch = q.batch;
+  ld.part = reinterpret_cast<double*>(ws + l.part);
+  ld.first = reinterpret_cast<float*>(ws + l.first);
+  ld.eps = eps; ld.x = x; ld.x_ld = r.x_ld;
+  ld.totals = reinterpret_cast<PlanTotals*>(ws);
+  ld.clear_status = first_round;
+  ld.parts = 4 * sms / q.batch.n_mats;
+  if (ld.parts > MAX_PARTS) ld.parts = MAX_PARTS;
+  if (ld.parts < 8) ld.parts = 8;
+  long long load_ctas = 8ll * sms / q.batch.n_mats + 1;
+  if (load_ctas > tiles) load_ctas = tiles;
+  if (dtype == CAMERA_BF16) {
+    ORTHO_CK(launch_chained(k_ortho_norm<__nv_bfloat16>, ld, ld.parts, q.batch.n_mats, 1, LOAD_THREADS, 0, !first_round, st));
+    ORTHO_CK(launch_chained(k_ortho_load<__nv_bfloat16>, ld, (int)load_ctas, q.batch.n_mats, 1, LOAD_THREADS, 0, true, st));
+  } else {
+    ORTHO_CK(launch_chained(k_ortho_norm<float>, ld, ld.parts, q.batch.n_mats, 1, LOAD_THREADS, 0, !first_round, st));
+    ORTHO_CK(launch_chained(k_ortho_load<float>, ld, (int)load_ctas, q.batch.n_mats, 1, LOAD_THREADS, 0, true, st));
+  }
+  q.totals = ld.totals;
+  q.wait_limit_ns = current_wait_limit_ns();
+  double h = 1.0, sx = 1.0;             // the first X's factor is known on the device only
+  for (int s = 0; s < steps; ++s) {
+    const float* const k = coefficients + 3 * s;
+    const StepBound bound = step_bound(k, h * MARGIN);
+    const double sa = factor_for(h * h), sb = factor_for(bound.b), sn = factor_for(bound.h);
+    const bool last = s + 1 == steps;
+    q.first = s == 0 ? ld.first : nullptr;
+    q.out = a; q.out_ld = r.a_ld;
+    q.f_acc = (float)(sa / (sx * sx));
+    int rc = launch_ortho<ORTHO_GRAM>(q, x, r.x_ld, x, r.x_ld, r.rows, n_pairs, st);
+    if (rc != CAMERA_OK) return rc;
+    q.first = nullptr;
+    q.aux = a; q.aux_ld = r.a_ld;
+    q.out = b;
+    q.f_acc = (float)(sb * k[2] / (sa * sa)); q.f_aux = (float)(sb * k[1] / sa); q.f_diag = (float)(sb * k[0]);
+    rc = launch_ortho<ORTHO_POLY>(q, a, r.a_ld, a, r.a_ld, r.rows, n_pairs, st);
+    if (rc != CAMERA_OK) return rc;
+    q.first = s == 0 ? ld.first : nullptr;
+    q.out = last ? nullptr : x_next; q.out_ld = r.x_ld;
+    q.f_acc = (float)((last ? 1.0 : sn) / (sb * sx));
+    rc = launch_ortho<ORTHO_APPLY>(q, b, r.a_ld, x, r.x_ld, r.rows, n_pairs, st);
+    if (rc != CAMERA_OK) return rc;
+    __half* const swap = x; x = x_next; x_next = swap;
+    h = bound.h;
+    sx = sn;
+  }
+  return CAMERA_OK;
+}
+
+}  // namespace
+}  // namespace camera
+
+extern "C" size_t camera_orthogonalize_workspace_bytes(const camera_matrix_t* mats, int32_t n_mats) {
+  using namespace camera;
+  if (check_matrices(mats, n_mats, CAMERA_BF16, false) != CAMERA_OK) return 0;
+  size_t most = ortho_layout(OrthoRound{0, 0, 0, 0, 0}).total;
+  for (int at = 0; at < n_mats;) {
+    const OrthoRound r = ortho_round(mats, n_mats, at);
+    const size_t need = ortho_layout(r).total;
+    if (need > most) most = need;
+    at = r.end;
+  }
+  return most;
+}
+
+extern "C" int camera_orthogonalize(const camera_matrix_t* mats, int32_t n_mats, int32_t dtype, const float* coefficients, int32_t steps,
+                                    float eps, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  using namespace camera;
+  const int rc = check_matrices(mats, n_mats, dtype, true);
+  if (rc != CAMERA_OK) return rc;
+  if (steps < 1 || steps > 64 || coefficients == nullptr || !(eps >= 0.f) || !(eps < 3.0e38f)) return CAMERA_ERR_INVALID_ARG;
+  double h = 1.0;
+  for (int s = 0; s < steps; ++s) {
+    const StepBound b = step_bound(coefficients + 3 * s, h * MARGIN);
+    if (!(b.h <= MOST) || !(b.b <= MOST)) return CAMERA_ERR_INVALID_ARG;
+    h = b.h;
+  }
+  if (workspace == nullptr || workspace_bytes < camera_orthogonalize_workspace_bytes(mats, n_mats) ||
+      (reinterpret_cast<uintptr_t>(workspace) & 255))
+    return CAMERA_ERR_WORKSPACE;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  char* const ws = static_cast<char*>(workspace);
+  bool first = true;
+  for (int at = 0; at < n_mats;) {
+    const OrthoRound r = ortho_round(mats, n_mats, at);
+    const int e = run_round(mats, r, dtype, coefficients, steps, eps, ws, first, st);
+    if (e != CAMERA_OK) return e;
+    if (r.rows > 0) first = false;
+    at = r.end;
+  }
+  if (first) ORTHO_CK(cudaMemsetAsync(ws, 0, sizeof(PlanTotals), st));
+  return CAMERA_OK;
+}

@@ -64,6 +64,10 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const void* tmap,
 __device__ __forceinline__ uint32_t make_idesc_pair(int n) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((256u >> 4) << 24);
 }
+// The same for f16 x f16 -> fp32.
+__device__ __forceinline__ uint32_t make_idesc_pair_f16(int n) {
+  return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((256u >> 4) << 24);
+}
 __device__ __forceinline__ void umma_bf16_pair(uint32_t d_tmem, unsigned long long a, unsigned long long b, uint32_t idesc,
                                                uint32_t accumulate) {
   asm volatile(
@@ -81,6 +85,95 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                ::"r"(bar), "h"(mask)
                : "memory");
+}
+
+// Shared-memory descriptor of an MN-major tile of 16-bit elements: boxes of 64 k rows x 128 bytes (64 m or n) with the 128-byte
+// swizzle.  Groups of 8 k lie 1024 bytes apart (stride offset), blocks of 64 m or n one box apart (leading offset).
+__device__ __forceinline__ unsigned long long make_smem_desc_mn(uint32_t addr) {
+  unsigned long long d = 0;
+  d |= (unsigned long long)((addr & 0x3ffffu) >> 4);
+  d |= (unsigned long long)(8192 >> 4) << 16;
+  d |= (unsigned long long)(1024 >> 4) << 32;
+  d |= (unsigned long long)1 << 46;
+  d |= (unsigned long long)2 << 61;
+  return d;
+}
+
+// The producer and the issuer are whole warps that walk their loops together and let one lane (`lead`) issue: TMA and
+// tcgen05 instructions take their operands from the warp's uniform registers, and in a branch of one lane the compiler has
+// to move every operand there first (about 100 cycles an MMA).
+__device__ __forceinline__ void tma_load_lead(uint32_t lead, uint32_t dst, const void* tmap, uint32_t bar_cluster_addr, int x, int y) {
+  asm volatile(
+      "{\n"
+      ".reg .pred q;\n"
+      "setp.ne.b32 q, %5, 0;\n"
+      "@q cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n"
+      "}\n" ::"r"(dst), "l"(tmap), "r"(bar_cluster_addr), "r"(x), "r"(y), "r"(lead)
+      : "memory");
+}
+// The MMAs of one k block (four steps of 16) on one B tile in one piece of assembly, so that predicates are set once and
+// the descriptors' steps are plain additions (0.38 -> 0.32 us per k block).  Two B tiles in turn are better off as single
+// MMAs (0.39 us; in one piece 0.49).
+template <int A_STEP, int B_STEP>
+__device__ __forceinline__ void umma_block(uint32_t lead, uint32_t d0, unsigned long long a, unsigned long long b, uint32_t idesc,
+                                           uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q, t;\n"
+      ".reg .b64 a1, a2, a3, b1, b2, b3;\n"
+      "setp.ne.b32 q, %5, 0;\n"
+      "setp.ne.b32 p, %4, 0;\n"
+      "setp.eq.b32 t, 0, 0;\n"
+      "add.s64 a1, %1, %6;\n"
+      "add.s64 b1, %2, %7;\n"
+      "add.s64 a2, %1, 2 * %6;\n"
+      "add.s64 b2, %2, 2 * %7;\n"
+      "add.s64 a3, %1, 3 * %6;\n"
+      "add.s64 b3, %2, 3 * %7;\n"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], a1, b1, %3, t;\n"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], a2, b2, %3, t;\n"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], a3, b3, %3, t;\n"
+      "}\n" ::"r"(d0), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(lead), "n"(A_STEP), "n"(B_STEP)
+      : "memory");
+}
+__device__ __forceinline__ void umma_lead(uint32_t lead, uint32_t d_tmem, unsigned long long a, unsigned long long b, uint32_t idesc,
+                                          uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      "setp.ne.b32 p, %4, 0;\n"
+      "setp.ne.b32 q, %5, 0;\n"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n"
+      "}\n" ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(lead)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit_lead(uint32_t lead, uint32_t bar) {
+  const uint16_t mask = 3;
+  asm volatile(
+      "{\n"
+      ".reg .pred q;\n"
+      "setp.ne.b32 q, %2, 0;\n"
+      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n"
+      "}\n" ::"r"(bar), "h"(mask), "r"(lead)
+      : "memory");
+}
+// Whether the phase has ended, without waiting (try_wait may suspend the thread for a while).
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+      "selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
 }
 
 }  // namespace camera
