@@ -397,10 +397,10 @@ extern "C" int camera_moe_combine_backward(const void* dy, int32_t dtype, int64_
                                            int64_t sorted_ld, int64_t n_rows, void* dy_sorted, int64_t dy_sorted_ld,
                                            float* d_topk_w, void* cuda_stream) {
   using namespace camera;
-  if (!sizes_ok(n_tokens, top_k, d_model, dtype) || n_rows < 0 || (dy_sorted == nullptr && d_topk_w == nullptr))
-    return CAMERA_ERR_INVALID_ARG;
+  if (!sizes_ok(n_tokens, top_k, d_model, dtype) || n_rows < 0) return CAMERA_ERR_INVALID_ARG;
   if (!sizes_fit(n_tokens, top_k, d_model)) return CAMERA_ERR_UNSUPPORTED_SHAPE;
   if (n_tokens == 0) return CAMERA_OK;
+  if (dy_sorted == nullptr && d_topk_w == nullptr && n_rows > 0) return CAMERA_ERR_INVALID_ARG;
   const int size = dtype == CAMERA_BF16 ? 2 : 4;
   if (!words_ok(rows) || (topk_w != nullptr && !words_ok(topk_w)) || (d_topk_w != nullptr && !words_ok(d_topk_w)) ||
       !rows_fit(dy, ld, d_model, size) || (dy_sorted != nullptr && n_rows > 0 && !rows_fit(dy_sorted, dy_sorted_ld, d_model, size)) ||

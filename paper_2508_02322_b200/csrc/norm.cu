@@ -386,7 +386,7 @@ extern "C" int camera_norm_backward(const camera_norm_t* n, const void* dy, int6
   const int rc = check_norm(n);
   if (rc != CAMERA_OK) return rc;
   const bool want_w = d_weight != nullptr || d_bias != nullptr;
-  if ((dx == nullptr && !want_w) || (dx == nullptr && d_sum != nullptr)) return CAMERA_ERR_INVALID_ARG;
+  if (n->n_rows > 0 && dx == nullptr && (!want_w || d_sum != nullptr)) return CAMERA_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(mean) | reinterpret_cast<uintptr_t>(rstd) | reinterpret_cast<uintptr_t>(d_weight) |
        reinterpret_cast<uintptr_t>(d_bias)) & 3)
     return CAMERA_ERR_INVALID_ARG;

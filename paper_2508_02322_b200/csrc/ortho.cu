@@ -8,8 +8,11 @@
 // The operands of the products are fp16 with a power of two as factor, the sums fp32.  With h a bound of the singular values
 // of X, no element of X is larger than h, none of A than h^2, none of B than the polynomial's largest value over [0, h^2]: the
 // host follows these bounds from step to step (1 before the first) and picks the largest factors under which nothing can
-// overflow.  fp16 has 3 bits more than bf16: results are 1e-3 off 64 bits (root mean square, relative; bf16 operands 8e-3),
-// below their own rounding to bf16, 1.7e-3.  The first X is the matrix itself times a power of two, so bf16 inputs enter
+// overflow.  fp16 has 3 bits more than bf16.  The diagonals of A and B hold most of what they are, and in a matrix whose singular
+// values are alike all of it rounds the same way; so what their rounding leaves is kept in fp32 and enters the next product's
+// epilogue (a row of it for B X, a row and a column for A A).  Results are 4e-4 to 9e-4 off 64 bits (root mean square,
+// relative; up to 2.7e-3 without the diagonals' rests, 8e-3 with bf16 operands), below their own rounding to bf16, 1.7e-3.
+// The first X is the matrix itself times a power of two, so bf16 inputs enter
 // exactly; 1 / (|U| + eps) goes into the factors of the first step.
 //
 // Matrices of one call lie one below the other in the workspace, padded with zeros to whole tiles of 256 rows and whole
@@ -64,11 +67,15 @@ struct OrthoGemm {
   int unit0[O_MAX_MATS + 1];
   int n_units;
   int bn, nb, kps, n_stages, n_acc;      // columns per B tile, B tiles per unit, k blocks per stage, ring depth, accumulators
-  const __half* aux;        // POLY: A
+  const __half* aux;        // POLY: A; APPLY: X
   __half* out;              // packed result, or null: the caller's matrices
   long long aux_ld, out_ld;
+  const float* rest_in;     // [rows] what the rounding of the diagonal of A (POLY) or B (APPLY) left
+  float* rest_out;          // GRAM, POLY: the same of the result
   float f_acc, f_aux, f_diag;
   const float* first;       // factor of each matrix's first X, or null
+  const int* small;         // exponents by which matrices are smaller than the bounds (see scale_of), those of this step's X
+  int small_in, small_out;  // and of the next count from here on
   PlanTotals* totals;
   unsigned long long wait_limit_ns;
 };
@@ -87,6 +94,11 @@ __host__ __device__ __forceinline__ int units_of(int m, int n, int w) {
   for (int i = 0; i < rt; ++i) units += ((rt - i) * O_TILE_M + w - 1) / w;
   return units;
 }
+
+// A matrix whose norm is far below eps starts with singular values of 2^-small at most, where small = log2((|U| + eps) / |U|), and
+// would be lost in fp16 at the others' factors.  A step makes them larger by no more than the largest value of its polynomial, so
+// X keeps 2^(small - what the steps so far can have added) as a further factor, as long as that is above 1.
+__device__ __forceinline__ int scale_of(int small, int used) { return max(0, small - used); }
 
 struct OrthoUnit { int e, m0, n0, two, kb, limit; };
 
@@ -298,21 +310,46 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
       const int warp_row = u.m0 + 128 * (int)rank + (warp & 3) * 32, row = warp_row + lane;      // in the matrix, < pad_rows(m)
       const int cols = min(u.limit - u.n0, c_first + c_half);       // where this warp's columns end
       float f = q.f_acc;
-      if (q.first != nullptr) {
-        const float s = q.first[u.e];
-        f = MODE == ORTHO_GRAM ? f / s / s : f / s;
+      if (MODE != ORTHO_POLY) {
+        const int small = q.small[u.e];
+        const float s = q.first != nullptr ? q.first[u.e] : scalbnf(1.f, scale_of(small, q.small_in));
+        f = MODE == ORTHO_GRAM ? f / s / s : scalbnf(f / s, q.out != nullptr ? scale_of(small, q.small_out) : 0);
       }
       ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_phase, abort_flag));
       if (!ok) break;
       tc_fence_after();
       const uint32_t t0 = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(acc * q.nb * q.bn);
       const long long at = (long long)(mat.row0 + row) * q.out_ld + u.n0;
-      auto put = [&](const uint32_t* v, int c) {
+      const float rest = MODE == ORTHO_GRAM ? 0.f : q.rest_in[mat.row0 + row];
+      auto put = [&](const uint32_t* raw, int c) {
         uint32_t p[8];
+        float v[16];
+        if (MODE == ORTHO_GRAM) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(raw[j]) * f;
+        } else {
+          uint32_t a[8];
+          const uint4* const src = reinterpret_cast<const uint4*>(q.aux + (long long)(mat.row0 + row) * q.aux_ld + u.n0 + c);
+          *reinterpret_cast<uint4*>(a) = src[0];
+          *reinterpret_cast<uint4*>(a + 4) = src[1];
+#pragma unroll
+          for (int j = 0; j < 16; j += 2) {
+            const float2 old = __half22float2(*reinterpret_cast<const __half2*>(&a[j >> 1]));
+            if (MODE == ORTHO_APPLY) {                  // (B + rest) X
+              v[j] = fmaf(rest, old.x, __uint_as_float(raw[j])) * f;
+              v[j + 1] = fmaf(rest, old.y, __uint_as_float(raw[j + 1])) * f;
+            } else {                                    // (A + rest)^2 up to the square of the rest, and b (A + rest)
+              const float2 down = *reinterpret_cast<const float2*>(q.rest_in + mat.row0 + u.n0 + c + j);
+              const float x = u.n0 + c + j == row ? rest : 0.f, y = u.n0 + c + j + 1 == row ? rest : 0.f;
+              v[j] = fmaf(old.x + x, q.f_aux, fmaf(rest + down.x, old.x, __uint_as_float(raw[j])) * f);
+              v[j + 1] = fmaf(old.y + y, q.f_aux, fmaf(rest + down.y, old.y, __uint_as_float(raw[j + 1])) * f);
+            }
+          }
+        }
         if (MODE == ORTHO_APPLY && q.out == nullptr) {
           // the result, in the caller's layout
 #pragma unroll
-          for (int j = 0; j < 8; ++j) p[j] = pack_bf16(__uint_as_float(v[2 * j]) * f, __uint_as_float(v[2 * j + 1]) * f);
+          for (int j = 0; j < 8; ++j) p[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
           const int left = mat.n - u.n0 - c;                        // columns there are
           uint16_t* const out = static_cast<uint16_t*>(mat.out);
           if (mat.turned) {
@@ -331,23 +368,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
           }
           return;
         }
-        if (MODE == ORTHO_POLY) {
-          uint32_t a[8];
-          const uint4* const src = reinterpret_cast<const uint4*>(q.aux + (long long)(mat.row0 + row) * q.aux_ld + u.n0 + c);
-          *reinterpret_cast<uint4*>(a) = src[0];
-          *reinterpret_cast<uint4*>(a + 4) = src[1];
+        if (MODE != ORTHO_APPLY && u.n0 + c < warp_row + 32 && u.n0 + c + 16 > warp_row) {
+          // on the diagonal: what its rounding leaves is kept
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float2 old = __half22float2(*reinterpret_cast<const __half2*>(&a[j]));
-            float lo = fmaf(old.x, q.f_aux, __uint_as_float(v[2 * j]) * f), hi = fmaf(old.y, q.f_aux, __uint_as_float(v[2 * j + 1]) * f);
-            if (u.n0 + c + 2 * j == row) lo += q.f_diag;
-            if (u.n0 + c + 2 * j + 1 == row) hi += q.f_diag;
-            p[j] = pack_half(lo, hi);
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) p[j] = pack_half(__uint_as_float(v[2 * j]) * f, __uint_as_float(v[2 * j + 1]) * f);
+          for (int j = 0; j < 16; ++j)
+            if (u.n0 + c + j == row) {
+              v[j] += MODE == ORTHO_POLY ? q.f_diag : 0.f;
+              q.rest_out[mat.row0 + row] = v[j] - __half2float(__float2half_rn(v[j]));
+            }
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j] = pack_half(v[2 * j], v[2 * j + 1]);
         st_global_v8(q.out + at + c, p);
         if (MODE != ORTHO_APPLY && u.n0 + c >= u.m0 + O_TILE_M)      // off the diagonal's block: the other half of the result
           store_turned(reinterpret_cast<uint16_t*>(q.out) + (long long)(mat.row0 + u.n0 + c) * q.out_ld + warp_row, q.out_ld, p, lane, 32, 16,
@@ -388,6 +419,7 @@ struct OrthoLoad {
   double* part;             // [mats][parts] sums of squares
   int parts;
   float* first;             // [mats] factor between X as stored and X
+  int* small;               // [mats]
   float eps;
   __half* x;
   long long x_ld;
@@ -434,8 +466,8 @@ __global__ void __launch_bounds__(LOAD_THREADS) k_ortho_norm(const __grid_consta
   if (threadIdx.x == 0) q.part[blockIdx.y * q.parts + blockIdx.x] = s;
 }
 
-// X = U 2^p in fp16, shorter side as rows, zeros around it.  p puts 2^p (|U| + eps) into [2^14, 2^15): nothing overflows, and
-// what is below 2^-39 of the norm is lost.  A CTA turns tiles of 64 x 64 in shared memory.
+// X = U 2^p in fp16, shorter side as rows, zeros around it.  p puts 2^p |U| into [2^14, 2^15): nothing overflows, and what
+// is below 2^-39 of the norm is lost.  A CTA turns tiles of 64 x 64 in shared memory.
 template <typename T>
 __global__ void __launch_bounds__(LOAD_THREADS) k_ortho_load(const __grid_constant__ OrthoLoad q) {
   __shared__ __align__(16) __half tile[64][72];
@@ -444,14 +476,20 @@ __global__ void __launch_bounds__(LOAD_THREADS) k_ortho_load(const __grid_consta
   const OrthoMat& mat = q.batch.mat[blockIdx.y];
   double s = 0.0;
   for (int i = threadIdx.x; i < q.parts; i += LOAD_THREADS) s += q.part[blockIdx.y * q.parts + i];
-  const double norm = sqrt(block_sum(s)) + (double)q.eps;
+  const double norm = sqrt(block_sum(s));
   int p = 0;
   if (norm > 0.0 && norm < 1e300) {
     int e;
     frexp(norm, &e);                    // norm in [2^(e-1), 2^e)
     p = 15 - e;
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) q.first[blockIdx.y] = norm == 0.0 ? 1.f : norm < 1e300 ? (float)ldexp(norm, p) : __int_as_float(0x7fffffff);
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    const double all = norm + (double)q.eps;
+    q.first[blockIdx.y] = norm == 0.0 ? 1.f : norm < 1e300 ? (float)fmin(ldexp(all, p), 1e38) : __int_as_float(0x7fffffff);
+    int e = 1;
+    if (norm > 0.0 && norm < 1e300) frexp(all / norm, &e);       // all / norm in [2^(e-1), 2^e)
+    q.small[blockIdx.y] = min(e - 1, 100);
+  }
   const int rt = pad_rows(mat.m) / 64, ct = pad_cols(mat.n) / 64;
   const T* const in = static_cast<const T*>(mat.in);
   for (int t = blockIdx.x; t < rt * ct; t += gridDim.x) {
@@ -505,12 +543,14 @@ OrthoRound ortho_round(const camera_matrix_t* mats, int n, int begin) {
   return r;
 }
 constexpr int MAX_PARTS = 296;
-struct OrthoLayout { size_t part, first, x0, x1, a, b, total; };
+struct OrthoLayout { size_t part, first, rest_a, rest_b, x0, x1, a, b, total; };
 OrthoLayout ortho_layout(const OrthoRound& r) {
   OrthoLayout l;
   l.part = up256(sizeof(PlanTotals));
   l.first = l.part + up256((size_t)8 * O_MAX_MATS * MAX_PARTS);
-  l.x0 = l.first + up256(4 * O_MAX_MATS);
+  l.rest_a = l.first + up256(8 * O_MAX_MATS);
+  l.rest_b = l.rest_a + up256((size_t)4 * r.rows);
+  l.x0 = l.rest_b + up256((size_t)4 * r.rows);
   const size_t x = up256((size_t)2 * r.rows * r.x_ld), a = up256((size_t)2 * r.rows * r.a_ld);
   l.x1 = l.x0 + x;
   l.a = l.x1 + x;
@@ -651,8 +691,11 @@ int run_round(const camera_matrix_t* mats, const OrthoRound& r, int32_t dtype, c
   ld.batch = q.batch;
   ld.part = reinterpret_cast<double*>(ws + l.part);
   ld.first = reinterpret_cast<float*>(ws + l.first);
+  ld.small = reinterpret_cast<int*>(ld.first + O_MAX_MATS);
   ld.eps = eps; ld.x = x; ld.x_ld = r.x_ld;
   ld.totals = reinterpret_cast<PlanTotals*>(ws);
+  float* const rest_a = reinterpret_cast<float*>(ws + l.rest_a);
+  float* const rest_b = reinterpret_cast<float*>(ws + l.rest_b);
   ld.clear_status = first_round;
   ld.parts = 4 * sms / q.batch.n_mats;
   if (ld.parts > MAX_PARTS) ld.parts = MAX_PARTS;
@@ -668,7 +711,9 @@ int run_round(const camera_matrix_t* mats, const OrthoRound& r, int32_t dtype, c
   }
   q.totals = ld.totals;
   q.wait_limit_ns = current_wait_limit_ns();
+  q.small = ld.small;
   double h = 1.0, sx = 1.0;             // the first X's factor is known on the device only
+  double grown = 1.0;                   // what the steps so far can have made of a small singular value
   for (int s = 0; s < steps; ++s) {
     const float* const k = coefficients + 3 * s;
     const StepBound bound = step_bound(k, h * MARGIN);
@@ -676,17 +721,24 @@ int run_round(const camera_matrix_t* mats, const OrthoRound& r, int32_t dtype, c
     const bool last = s + 1 == steps;
     q.first = s == 0 ? ld.first : nullptr;
     q.out = a; q.out_ld = r.a_ld;
+    q.rest_out = rest_a;
     q.f_acc = (float)(sa / (sx * sx));
+    q.small_in = (int)ceil(log2(fmax(grown / h, 1.0)));
+    grown *= bound.b * MARGIN;
+    q.small_out = (int)ceil(log2(fmax(grown / bound.h, 1.0)));
     int rc = launch_ortho<ORTHO_GRAM>(q, x, r.x_ld, x, r.x_ld, r.rows, n_pairs, st);
     if (rc != CAMERA_OK) return rc;
     q.first = nullptr;
     q.aux = a; q.aux_ld = r.a_ld;
     q.out = b;
+    q.rest_in = rest_a; q.rest_out = rest_b;
     q.f_acc = (float)(sb * k[2] / (sa * sa)); q.f_aux = (float)(sb * k[1] / sa); q.f_diag = (float)(sb * k[0]);
     rc = launch_ortho<ORTHO_POLY>(q, a, r.a_ld, a, r.a_ld, r.rows, n_pairs, st);
     if (rc != CAMERA_OK) return rc;
     q.first = s == 0 ? ld.first : nullptr;
+    q.aux = x; q.aux_ld = r.x_ld;
     q.out = last ? nullptr : x_next; q.out_ld = r.x_ld;
+    q.rest_in = rest_b; q.rest_out = nullptr;
     q.f_acc = (float)((last ? 1.0 : sn) / (sb * sx));
     rc = launch_ortho<ORTHO_APPLY>(q, b, r.a_ld, x, r.x_ld, r.rows, n_pairs, st);
     if (rc != CAMERA_OK) return rc;
@@ -721,6 +773,8 @@ extern "C" int camera_orthogonalize(const camera_matrix_t* mats, int32_t n_mats,
   if (steps < 1 || steps > 64 || coefficients == nullptr || !(eps >= 0.f) || !(eps < 3.0e38f)) return CAMERA_ERR_INVALID_ARG;
   double h = 1.0;
   for (int s = 0; s < steps; ++s) {
+    for (int i = 0; i < 3; ++i)
+      if (!isfinite(coefficients[3 * s + i])) return CAMERA_ERR_INVALID_ARG;
     const StepBound b = step_bound(coefficients + 3 * s, h * MARGIN);
     if (!(b.h <= MOST) || !(b.b <= MOST)) return CAMERA_ERR_INVALID_ARG;
     h = b.h;
