@@ -178,7 +178,7 @@ constexpr int SLOTS = 8;         // rows of a token in flight
 
 // A thread takes one pack of one token: k rows in flight, added in the order of the slots.
 template <typename T, int W>
-__global__ void __launch_bounds__(256) k_moe_combine(const Combine q) {
+__global__ void __launch_bounds__(256, 4) k_moe_combine(const Combine q) {
   using P = Pack<T, W>;
   const long long t = (long long)blockIdx.x * blockDim.y + threadIdx.y;
   const int c = (blockIdx.y * blockDim.x + threadIdx.x) * W;
@@ -205,13 +205,20 @@ __global__ void __launch_bounds__(256) k_moe_combine(const Combine q) {
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j)
       if (row[j] >= 0) {
+        float f[W];
+        v[j].get(f);
 #pragma unroll
-        for (int i = 0; i < W; ++i) sum[i] = fmaf(w[j], to_f32(v[j].v[i]), sum[i]);
+        for (int i = 0; i < W; ++i) sum[i] = fmaf(w[j], f[i], sum[i]);
       }
   }
-  P out;
+  if (q.add != nullptr) {
+    float f[W];
+    extra.get(f);
 #pragma unroll
-  for (int i = 0; i < W; ++i) out.v[i] = from_f32<T>(q.add != nullptr ? sum[i] + to_f32(extra.v[i]) : sum[i]);
+    for (int i = 0; i < W; ++i) sum[i] += f[i];
+  }
+  P out;
+  out.set(sum);
   *reinterpret_cast<P*>(static_cast<T*>(q.y) + t * q.y_ld + c) = out;
 }
 
@@ -238,21 +245,26 @@ __global__ void __launch_bounds__(512, 1) k_moe_combine_backward(const Combine q
     for (int c = i0 * W; c < q.d; c += threads * W) {
       const P g = *reinterpret_cast<const P*>(dy + c);
       P v[SLOTS];
+      float d[W];
       if (q.dw != nullptr) {
 #pragma unroll
         for (int j = 0; j < SLOTS; ++j)
           if (row[j] >= 0) v[j] = *reinterpret_cast<const P*>(ys + row[j] * q.ys_ld + c);
       }
+      g.get(d);
 #pragma unroll
       for (int j = 0; j < SLOTS; ++j)
         if (row[j] >= 0) {
           P out;
+          float f[W];
+          if (q.dw != nullptr) {
+            v[j].get(f);
 #pragma unroll
-          for (int i = 0; i < W; ++i) {
-            const float d = to_f32(g.v[i]);
-            out.v[i] = from_f32<T>(w[j] * d);
-            if (q.dw != nullptr) dot[j] = fmaf(d, to_f32(v[j].v[i]), dot[j]);
+            for (int i = 0; i < W; ++i) dot[j] = fmaf(d[i], f[i], dot[j]);
           }
+#pragma unroll
+          for (int i = 0; i < W; ++i) f[i] = w[j] * d[i];
+          out.set(f);
           if (q.dys != nullptr) *reinterpret_cast<P*>(dys + row[j] * q.dys_ld + c) = out;
         }
     }

@@ -16,6 +16,10 @@ namespace {
 
 constexpr int NORM_MAX_D = 32768;          // 32 warps x 32 elements a thread
 constexpr int BACKWARD_ROWS = 2;            // a group's rows, at least
+constexpr int BACKWARD_THREADS = 512;       // threads an SM holds of the backward kernel (128 registers each)
+// Rows of a group in flight in the backward pass, of N 16-byte loads a thread and matrix: what 196 KB hold for 512 threads (16384 x
+// 3584 bf16: 2 stages 96 us, 3 stages 94, 4 stages 95).
+template <int N> constexpr int NORM_STAGES = N <= 2 ? 3 : N <= 8 ? 8 / N : 1;
 constexpr int NORM_GROUP_THREADS = 256;    // groups of fewer threads share a CTA up to this
 
 struct NormArgs {
@@ -29,12 +33,12 @@ struct NormArgs {
   bool w_f32, rms;
   float eps;
   float *mean, *rstd;                      // backward: inputs
-  float* part;                             // backward: [groups][2][d] partial sums of dw and db
-  bool want_w;
+  float* part;                             // backward: [groups][1 or 2][d] shares of dw and db
+  bool want_w, want_b;
 };
 
 template <int W>
-__device__ __forceinline__ void load_weight(const void* p, bool f32, int c, float absent, float* out) {
+__device__ __forceinline__ void load_weight(const void* p, bool f32, int c, float absent, float (&out)[W]) {
   if (p == nullptr) {
 #pragma unroll
     for (int i = 0; i < W; ++i) out[i] = absent;
@@ -47,9 +51,7 @@ __device__ __forceinline__ void load_weight(const void* p, bool f32, int c, floa
       for (int i = 0; i < V; ++i) out[k + i] = t.v[i];
     }
   } else {
-    const Pack<__nv_bfloat16, W> t = *reinterpret_cast<const Pack<__nv_bfloat16, W>*>(static_cast<const __nv_bfloat16*>(p) + c);
-#pragma unroll
-    for (int i = 0; i < W; ++i) out[i] = __bfloat162float(t.v[i]);
+    reinterpret_cast<const Pack<__nv_bfloat16, W>*>(static_cast<const __nv_bfloat16*>(p) + c)->get(out);
   }
 }
 
@@ -84,18 +86,23 @@ __global__ void __launch_bounds__(1024, 1) k_norm_forward(const NormArgs q) {
     for (int j = 0; j < N; ++j) {
       const int c = (j * threads + t) * W;
       if (c < q.d) {
-        P keep;
+        float v[W];
+        nx[j].get(v);
+        if (RES) {
+          float r[W];
+          P keep;
+          nr[j].get(r);
+#pragma unroll
+          for (int i = 0; i < W; ++i) v[i] += r[i];
+          keep.set(v);
+          keep.get(v);
+          *reinterpret_cast<P*>(static_cast<T*>(q.sum) + row * q.sum_ld + c) = keep;
+        }
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-          float v = to_f32(nx[j].v[i]);
-          if (RES) {
-            keep.v[i] = from_f32<T>(v + to_f32(nr[j].v[i]));
-            v = to_f32(keep.v[i]);
-          }
-          z[j * W + i] = v;
-          s[0] += v;
+          z[j * W + i] = v[i];
+          s[0] += v[i];
         }
-        if (RES) *reinterpret_cast<P*>(static_cast<T*>(q.sum) + row * q.sum_ld + c) = keep;
       }
     }
     if (AHEAD && row + step < q.rows) load(row + step);
@@ -129,19 +136,44 @@ __global__ void __launch_bounds__(1024, 1) k_norm_forward(const NormArgs q) {
         load_weight<W>(q.b, q.w_f32, c, 0.f, b);
         P out;
 #pragma unroll
-        for (int i = 0; i < W; ++i) out.v[i] = from_f32<T>(fmaf(z[j * W + i] * rstd, w[i], b[i]));
+        for (int i = 0; i < W; ++i) w[i] = fmaf(z[j * W + i] * rstd, w[i], b[i]);
+        out.set(w);
         *reinterpret_cast<P*>(static_cast<T*>(q.y) + row * q.y_ld + c) = out;
       }
     }
   }
 }
 
-// A thread keeps the columns it owns for all rows of its group, so their shares of dw and db stay in its registers; the
-// groups' shares are added up by k_norm_reduce in a fixed order.
-template <typename T, int W, int N>
-__global__ void __launch_bounds__(N * W <= 16 ? 512 : 1024, 1) k_norm_backward(const NormArgs q) {
+// The weights of the columns a thread owns, as pairs; columns past the end have weight 0.
+template <int W, int N>
+__device__ __forceinline__ void own_weights(const void* p, bool f32, int d, int threads, int t, float absent, F2 (&out)[N * W / 2]) {
+  float f[N * W];
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int c = (j * threads + t) * W;
+    float w[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = 0.f;
+    if (c < d) load_weight<W>(p, f32, c, absent, w);
+#pragma unroll
+    for (int i = 0; i < W; ++i) f[j * W + i] = w[i];
+  }
+#pragma unroll
+  for (int i = 0; i < N * W / 2; ++i) out[i] = f2(f[2 * i], f[2 * i + 1]);
+}
+
+// A thread keeps the columns it owns for all rows of its group, so their weights and their shares of dw and db stay in its
+// registers; the groups' shares are added up by k_norm_reduce in a fixed order.  Columns past the end read as zeros, which add
+// nothing.  RING: the next rows travel through shared memory, each thread copying (cp.async) what it will read itself, so that
+// a wait is the thread's own and the rows in flight cost no registers; without it (elements, which cp.async cannot copy one at
+// a time) the next row waits in registers.
+template <typename T, int W, int N, bool BIAS, bool RING, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1) k_norm_backward(const NormArgs q) {
   using P = Pack<T, W>;
-  constexpr bool AHEAD = N * W <= 16;
+  constexpr int E2 = N * W / 2;
+  constexpr bool AHEAD = !RING && N * W <= 16;
+  constexpr int STAGES = NORM_STAGES<N>;
+  extern __shared__ __align__(16) uint8_t ring[];
   const int threads = 32 * q.warps, group = threadIdx.x / threads, t = threadIdx.x - group * threads;
   const int groups = blockDim.x / threads;
   const long long step = (long long)gridDim.x * groups;
@@ -150,101 +182,173 @@ __global__ void __launch_bounds__(N * W <= 16 ? 512 : 1024, 1) k_norm_backward(c
   const T* const dy = static_cast<const T*>(q.dy);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   int buf = 0;
-  P nx[N], ny[N], nr[N];
-  float dw[N * W], db[N * W];
+  P now[3][RING ? 1 : N], next[3][AHEAD ? N : 1];
+  constexpr bool OWN_W = N * W <= 16;                  // weights in registers, or loaded again for each use
+  F2 dw[E2], db[BIAS ? E2 : 1], w[E2];
 #pragma unroll
-  for (int i = 0; i < N * W; ++i) dw[i] = db[i] = 0.f;
-  auto load = [&](long long row) {
+  for (int i = 0; i < E2; ++i) dw[i] = db[BIAS ? i : 0] = f2(0.f, 0.f);
+  if (OWN_W) own_weights<W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
+  const long long first = (long long)blockIdx.x * groups + group;
+  auto load = [&](P (*to)[RING ? 1 : N], long long row) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
+    for (int j = 0; j < (RING ? 0 : N); ++j) {
       const int c = (j * threads + t) * W;
+      to[0][j] = to[1][j] = to[2][j] = P();
       if (c < q.d) {
-        nx[j] = *reinterpret_cast<const P*>(x + row * q.x_ld + c);
-        ny[j] = *reinterpret_cast<const P*>(dy + row * q.dy_ld + c);
-        if (r != nullptr) nr[j] = *reinterpret_cast<const P*>(r + row * q.r_ld + c);
+        to[0][j] = *reinterpret_cast<const P*>(x + row * q.x_ld + c);
+        to[1][j] = *reinterpret_cast<const P*>(dy + row * q.dy_ld + c);
+        if (r != nullptr) to[2][j] = *reinterpret_cast<const P*>(r + row * q.r_ld + c);
       }
     }
   };
-  const long long first = (long long)blockIdx.x * groups + group;
-  if (AHEAD && first < q.rows) load(first);
-  for (long long row = first; row < q.rows; row += step) {
-    if (!AHEAD) load(row);
-    P cx[N], cy[N], cr[N];
+  const int parts = r != nullptr ? 3 : 2, line = N * 16 * (int)blockDim.x;
+  const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring) + 16 * threadIdx.x;
+  auto issue = [&](int stage, long long row) {
+    if (row < q.rows) {
+      const T* const src[3] = {x + row * q.x_ld, dy + row * q.dy_ld, r + row * q.r_ld};
 #pragma unroll
-    for (int j = 0; j < N; ++j) { cx[j] = nx[j]; cy[j] = ny[j]; cr[j] = nr[j]; }
-    if (AHEAD && row + step < q.rows) load(row + step);
-    const float mu = q.rms ? 0.f : q.mean[row], rstd = q.rstd[row];
-    float s[2] = {0.f, 0.f};
+      for (int p = 0; p < 3; ++p)
+        if (p < parts) {
+#pragma unroll
+          for (int j = 0; j < N; ++j) {
+            const int c = (j * threads + t) * W, at = c < q.d ? c : 0;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(mine + (stage * parts + p) * line + j * 16 * blockDim.x),
+                         "l"(src[p] + at), "r"(c < q.d ? 16 : 0)
+                         : "memory");
+          }
+        }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int stage = 0;
+  // the thread's elements of matrix p (x, dy, d_sum) of this row, from where they wait
+  auto get = [&](int p, F2 (&out)[E2]) {
+    P v[N];
+    const uint8_t* const at = ring + 16 * threadIdx.x + (stage * parts + p) * line;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const int c = (j * threads + t) * W;
-      if (c < q.d) {
-        float w[W];
-        load_weight<W>(q.w, q.w_f32, c, 1.f, w);
+      if constexpr (RING) v[j] = *reinterpret_cast<const P*>(at + j * 16 * blockDim.x);
+      else v[j] = now[p][j];
+    }
+    to_pairs<P, W, N>(v, out);
+  };
+  float rstd_next = 0.f, mu_next = 0.f;
+  auto stats = [&](long long row) {
+    if (row < q.rows) {
+      rstd_next = q.rstd[row];
+      mu_next = q.rms ? 0.f : q.mean[row];
+    }
+  };
+  stats(first);
+  if constexpr (RING) {
+    for (int s = 0; s < STAGES; ++s) issue(s, first + s * step);
+  } else if constexpr (AHEAD) {
+    if (first < q.rows) load(next, first);
+  }
+  for (long long row = first; row < q.rows; row += step) {
+    const float rstd = rstd_next, mu = mu_next;
+    stats(row + step);
+    if constexpr (RING) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+    } else if constexpr (AHEAD) {
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-          const float h = (to_f32(cx[j].v[i]) - mu) * rstd, d = to_f32(cy[j].v[i]), g = d * w[i];
-          s[0] += g;
-          s[1] = fmaf(g, h, s[1]);
-          dw[j * W + i] = fmaf(d, h, dw[j * W + i]);
-          db[j * W + i] += d;
-        }
+      for (int p = 0; p < 3; ++p)
+#pragma unroll
+        for (int j = 0; j < N; ++j) now[p][j] = next[p][j];
+      if (row + step < q.rows) load(next, row + step);
+    } else {
+      load(now, row);
+    }
+    const F2 minus_mu = f2(-mu, -mu), rs = f2(rstd, rstd);
+    F2 s0 = f2(0.f, 0.f), s1 = f2(0.f, 0.f);
+    {
+      F2 c[E2], d[E2];
+      get(0, c);
+      get(1, d);
+      if (!OWN_W) own_weights<W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
+#pragma unroll
+      for (int i = 0; i < E2; ++i) {
+        c[i] = add2(c[i], minus_mu);
+        dw[i] = fma2(mul2(d[i], rs), c[i], dw[i]);
+        if (BIAS) db[i] = add2(db[i], d[i]);
+        const F2 g = mul2(d[i], w[i]);
+        s0 = add2(s0, g);
+        s1 = fma2(g, c[i], s1);
       }
     }
-    if (q.y == nullptr) continue;
-    group_sum(s, q.warps, group, buf);
-    const float m1 = q.rms ? 0.f : s[0] / (float)q.d, m2 = s[1] / (float)q.d;
+    if (q.y != nullptr) {
+      float s[2], lo, hi;
+      split(s0, lo, hi);
+      s[0] = lo + hi;
+      split(s1, lo, hi);
+      s[1] = lo + hi;
+      group_sum(s, q.warps, group, buf);
+      // dx = s g - s mean g - c s^2 mean(g h),  mean(g h) = s mean(g c)
+      const float k1 = q.rms ? 0.f : -rstd * (s[0] / (float)q.d), k2 = -rstd * rstd * (rstd * (s[1] / (float)q.d));
+      const F2 k1s = f2(k1, k1), k2s = f2(k2, k2);
+      F2 c[E2], d[E2];
+      get(0, c);
+      get(1, d);
+      if (!OWN_W) own_weights<W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int c = (j * threads + t) * W;
-      if (c < q.d) {
-        float w[W];
-        load_weight<W>(q.w, q.w_f32, c, 1.f, w);
-        P out;
+      for (int i = 0; i < E2; ++i) c[i] = fma2(mul2(d[i], w[i]), rs, fma2(add2(c[i], minus_mu), k2s, k1s));
+      if (r != nullptr) {
+        get(2, d);
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-          const float h = (to_f32(cx[j].v[i]) - mu) * rstd, g = to_f32(cy[j].v[i]) * w[i];
-          float v = (g - m1 - h * m2) * rstd;
-          if (r != nullptr) v += to_f32(cr[j].v[i]);
-          out.v[i] = from_f32<T>(v);
-        }
-        *reinterpret_cast<P*>(static_cast<T*>(q.y) + row * q.y_ld + c) = out;
+        for (int i = 0; i < E2; ++i) c[i] = add2(c[i], d[i]);
       }
+      P out[N];
+      from_pairs<P, W, N>(c, out);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int at = (j * threads + t) * W;
+        if (at < q.d) *reinterpret_cast<P*>(static_cast<T*>(q.y) + row * q.y_ld + at) = out[j];
+      }
+    }
+    if constexpr (RING) {
+      issue(stage, row + STAGES * step);
+      if (++stage == STAGES) stage = 0;
     }
   }
-  if (!q.want_w) return;
-  float* const part = q.part + first * 2 * q.d;
+  // [groups][wanted][d]
+  const int wanted = q.want_w + q.want_b;
+  float* const part = q.part + first * wanted * q.d;
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int c = (j * threads + t) * W;
-    if (c < q.d) {
-      constexpr int V = W >= 4 ? 4 : 1;
+  for (int which = 0; which < (BIAS ? 2 : 1); ++which) {
+    if (!(which ? q.want_b : q.want_w)) continue;
+    float f[N * W];
 #pragma unroll
-      for (int k = 0; k < W; k += V) {
-        Pack<float, V> a, b;
+    for (int i = 0; i < E2; ++i) split(which ? db[i] : dw[i], f[2 * i], f[2 * i + 1]);
 #pragma unroll
-        for (int i = 0; i < V; ++i) { a.v[i] = dw[j * W + k + i]; b.v[i] = db[j * W + k + i]; }
-        *reinterpret_cast<Pack<float, V>*>(part + c + k) = a;
-        *reinterpret_cast<Pack<float, V>*>(part + q.d + c + k) = b;
+    for (int j = 0; j < N; ++j) {
+      const int c = (j * threads + t) * W;
+      if (c < q.d) {
+        constexpr int V = W >= 4 ? 4 : 1;
+#pragma unroll
+        for (int k = 0; k < W; k += V) {
+          Pack<float, V> a;
+#pragma unroll
+          for (int i = 0; i < V; ++i) a.v[i] = f[j * W + k + i];
+          *reinterpret_cast<Pack<float, V>*>(part + (which ? (wanted - 1) * q.d : 0) + c + k) = a;
+        }
       }
     }
   }
 }
 
 constexpr int REDUCE_WARPS = 16;
-struct NormReduce { const float* part; int groups, d; float *dw, *db; };
+struct NormReduce { const float* part; int groups, d, wanted; float *dw, *db; };
 // Columns of the groups' shares added up: a lane takes a column, the warps take every 16th group.
 __global__ void __launch_bounds__(32 * REDUCE_WARPS) k_norm_reduce(const NormReduce q) {
   __shared__ float sums[REDUCE_WARPS][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, which = blockIdx.y;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  float* const out = which ? q.db : q.dw;
-  if (out == nullptr) return;
+  float* const out = which || q.dw == nullptr ? q.db : q.dw;
   float s = 0.f;
   if (c < q.d) {
     const float* p = q.part + (long long)which * q.d + c;
 #pragma unroll 8
-    for (int g = warp; g < q.groups; g += REDUCE_WARPS) s += p[(long long)g * 2 * q.d];
+    for (int g = warp; g < q.groups; g += REDUCE_WARPS) s += p[(long long)g * q.wanted * q.d];
   }
   sums[warp][lane] = s;
   __syncthreads();
@@ -276,7 +380,7 @@ NormShape norm_shape(long long rows, int d, int per, int threads_sm, long long r
 
 // Elements a thread holds in the backward pass, and the groups that leave shares of dw and db.
 int backward_per(int d) { return d <= 16 * 512 ? 16 : 32; }
-NormShape backward_shape(long long rows, int d) { return norm_shape(rows, d, backward_per(d), 512, BACKWARD_ROWS); }
+NormShape backward_shape(long long rows, int d) { return norm_shape(rows, d, backward_per(d), BACKWARD_THREADS, BACKWARD_ROWS); }
 
 template <typename T, int W, int N>
 cudaError_t forward_as(const NormArgs& a, cudaStream_t st) {
@@ -298,18 +402,28 @@ cudaError_t forward_typed(const NormArgs& q, bool vec, cudaStream_t st) {
   return forward_as<T, W, 32 / W>(q, st);
 }
 
-template <typename T, int W, int N>
+template <typename T, int W, int N, bool BIAS, int THREADS>
 cudaError_t backward_as(const NormArgs& a, const NormShape& s, cudaStream_t st) {
+  constexpr bool RING = W * sizeof(T) == 16 && THREADS <= 512;
   NormArgs q = a;
   q.warps = s.warps;
-  return launch_chained(k_norm_backward<T, W, N>, q, s.ctas, 1, 1, 32 * s.warps * s.groups_per_cta, 0, false, st);
+  const int threads = 32 * s.warps * s.groups_per_cta;
+  int smem = 0;
+  if constexpr (RING) {
+    constexpr int MOST = NORM_STAGES<N> * 3 * N * 16 * THREADS;
+    static_assert(MOST <= 226 * 1024, "shared memory of an SM");
+    const cudaError_t e = allow_smem<k_norm_backward<T, W, N, BIAS, RING, THREADS>, MOST>();
+    if (e != cudaSuccess) return e;
+    smem = NORM_STAGES<N> * (q.r != nullptr ? 3 : 2) * N * threads * 16;
+  }
+  return launch_chained(k_norm_backward<T, W, N, BIAS, RING, THREADS>, q, s.ctas, 1, 1, threads, smem, false, st);
 }
-template <typename T>
+template <typename T, bool BIAS>
 cudaError_t backward_typed(const NormArgs& q, const NormShape& s, bool vec, cudaStream_t st) {
   constexpr int W = 16 / (int)sizeof(T);
-  const bool small = backward_per(q.d) == 16;
-  if (!vec) return small ? backward_as<T, 1, 16>(q, s, st) : backward_as<T, 1, 32>(q, s, st);
-  return small ? backward_as<T, W, 16 / W>(q, s, st) : backward_as<T, W, 32 / W>(q, s, st);
+  if (backward_per(q.d) == 16) return vec ? backward_as<T, W, 16 / W, BIAS, 512>(q, s, st) : backward_as<T, 1, 16, BIAS, 512>(q, s, st);
+  if (s.warps <= 16) return vec ? backward_as<T, W, 32 / W, BIAS, 512>(q, s, st) : backward_as<T, 1, 32, BIAS, 512>(q, s, st);
+  return vec ? backward_as<T, W, 32 / W, BIAS, 1024>(q, s, st) : backward_as<T, 1, 32, BIAS, 1024>(q, s, st);
 }
 
 int check_norm(const camera_norm_t* n) {
@@ -342,7 +456,7 @@ size_t norm_part_bytes(int64_t rows, int d) {
 // rounded up to whole CTAs, or as many as the GPU holds at one time.
 size_t norm_part_bound(int64_t rows, int d) {
   const int warps = (d + 32 * backward_per(d) - 1) / (32 * backward_per(d));
-  const int64_t want = (rows + BACKWARD_ROWS - 1) / BACKWARD_ROWS + NORM_GROUP_THREADS / 32, most = (int64_t)sm_count() * (16 / warps > 1 ? 16 / warps : 1);
+  const int64_t want = (rows + BACKWARD_ROWS - 1) / BACKWARD_ROWS + NORM_GROUP_THREADS / 32, most = (int64_t)sm_count() * (BACKWARD_THREADS / 32 / warps > 1 ? BACKWARD_THREADS / 32 / warps : 1);
   return (size_t)(want < most ? want : most) * 2 * d * 4;
 }
 
@@ -408,15 +522,16 @@ extern "C" int camera_norm_backward(const camera_norm_t* n, const void* dy, int6
   q.rows = n->n_rows; q.d = n->d;
   q.w = n->weight; q.w_f32 = n->weight_dtype == CAMERA_F32;
   q.rms = rms; q.mean = const_cast<float*>(mean); q.rstd = const_cast<float*>(rstd);
-  q.part = static_cast<float*>(workspace); q.want_w = want_w;
+  q.part = static_cast<float*>(workspace); q.want_w = d_weight != nullptr; q.want_b = d_bias != nullptr;
   const int size = n->dtype == CAMERA_BF16 ? 2 : 4;
   const bool vec = (n->d * size) % 16 == 0 && vec_ok(q.x, q.x_ld, size) && vec_ok(q.r, q.r_ld, size) && vec_ok(q.dy, q.dy_ld, size) &&
                    vec_ok(q.y, q.y_ld, size) && vec_ok(q.w, 0, 1);
   const NormShape s = backward_shape(q.rows, q.d);
-  NORM_CK(size == 2 ? backward_typed<__nv_bfloat16>(q, s, vec, st) : backward_typed<float>(q, s, vec, st));
+  if (size == 2) NORM_CK(q.want_b ? backward_typed<__nv_bfloat16, true>(q, s, vec, st) : backward_typed<__nv_bfloat16, false>(q, s, vec, st));
+  else NORM_CK(q.want_b ? backward_typed<float, true>(q, s, vec, st) : backward_typed<float, false>(q, s, vec, st));
   if (want_w) {
-    const NormReduce r = {q.part, s.ctas * s.groups_per_cta, q.d, d_weight, d_bias};
-    NORM_CK(launch_chained(k_norm_reduce, r, (q.d + 31) / 32, 2, 1, 32 * REDUCE_WARPS, 0, true, st));
+    const NormReduce r = {q.part, s.ctas * s.groups_per_cta, q.d, q.want_w + q.want_b, d_weight, d_bias};
+    NORM_CK(launch_chained(k_norm_reduce, r, (q.d + 31) / 32, r.wanted, 1, 32 * REDUCE_WARPS, 0, true, st));
   }
   return CAMERA_OK;
 }

@@ -5,11 +5,94 @@
 
 namespace camera {
 
-template <typename T, int W> struct alignas(sizeof(T) * W) Pack { T v[W]; };
+// W elements of a row as they lie in memory, loaded and stored at once.  bf16 pairs stay words: taken apart into 16-bit
+// elements each would hold a register of its own.
+template <typename T, int W> struct Pack;
+template <int W> struct alignas(4 * W) Pack<float, W> {
+  float v[W];
+  __device__ __forceinline__ void get(float (&f)[W]) const {
+#pragma unroll
+    for (int i = 0; i < W; ++i) f[i] = v[i];
+  }
+  __device__ __forceinline__ void set(const float (&f)[W]) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = f[i];
+  }
+};
+template <int W> struct alignas(2 * W) Pack<__nv_bfloat16, W> {
+  static_assert(W % 2 == 0, "pairs");
+  uint32_t v[W / 2];
+  __device__ __forceinline__ void get(float (&f)[W]) const {
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) {
+      f[2 * i] = __uint_as_float(v[i] << 16);
+      f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+    }
+  }
+  __device__ __forceinline__ void set(const float (&f)[W]) {
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) {
+      const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      v[i] = *reinterpret_cast<const uint32_t*>(&p);
+    }
+  }
+};
+template <> struct Pack<__nv_bfloat16, 1> {
+  uint16_t v;
+  __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = __uint_as_float((uint32_t)v << 16); }
+  __device__ __forceinline__ void set(const float (&f)[1]) { v = __bfloat16_as_ushort(__float2bfloat16_rn(f[0])); }
+};
 
-template <typename T> __device__ __forceinline__ T from_f32(float v);
-template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+// Two fp32 in a register pair, worked on by one instruction.
+struct F2 { unsigned long long v; };
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void split(F2 a, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.v)); }
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+// N packs of W elements as pairs, and back.
+template <typename P, int W, int N>
+__device__ __forceinline__ void to_pairs(const P (&p)[N], F2 (&out)[N * W / 2]) {
+  float f[N * W];
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    float g[W];
+    p[j].get(g);
+#pragma unroll
+    for (int i = 0; i < W; ++i) f[j * W + i] = g[i];
+  }
+#pragma unroll
+  for (int i = 0; i < N * W / 2; ++i) out[i] = f2(f[2 * i], f[2 * i + 1]);
+}
+template <typename P, int W, int N>
+__device__ __forceinline__ void from_pairs(const F2 (&in)[N * W / 2], P (&p)[N]) {
+  float f[N * W];
+#pragma unroll
+  for (int i = 0; i < N * W / 2; ++i) split(in[i], f[2 * i], f[2 * i + 1]);
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    float g[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) g[i] = f[j * W + i];
+    p[j].set(g);
+  }
+}
 
 // Sums over the warps that share a row; every thread gets them.  The buffers alternate, so one barrier a call is enough:
 // a buffer is written again only after the barrier of the call between.
