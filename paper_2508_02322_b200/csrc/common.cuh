@@ -162,6 +162,8 @@ int encode_router_maps(const ScoreCtx& c, void* host_maps, int which = MAPS_STAT
 bool encode_bf16_2d(void* out, const void* ptr, uint64_t rows, uint64_t d, uint32_t box_rows);
 // The same for rows of `cols` elements that lie `pitch` elements apart.
 bool encode_bf16_2d_pitch(void* out, const void* ptr, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows);
+// And for boxes of 32 columns with the 64-byte swizzle.
+bool encode_bf16_2d_narrow(void* out, const void* ptr, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows);
 
 // ---- device helpers ------------------------------------------------------------------------------
 template <typename T> __device__ __forceinline__ float to_f32(T v);

@@ -37,8 +37,13 @@ constexpr int O_THREADS = 32 * (O_EPI_WARPS + 2);
 constexpr int O_TILE_M = 256;                // rows of the output a pair computes: 128 per CTA
 constexpr int O_A_BYTES = 128 * 128;         // this CTA's 128 rows x 64 k
 constexpr int O_MAX_STAGES = 8;
-constexpr int O_RING_BYTES = 192 * 1024;
-constexpr int O_SMEM_BYTES = O_RING_BYTES + 256 + 1024;
+constexpr int O_RING_BYTES = 144 * 1024;
+constexpr int O_CHUNK = 32;                   // columns an epilogue warp handles at a time,
+constexpr int O_BUFS = 4;                    // and the chunks of 32 rows x 64 bytes it has in shared memory
+constexpr int O_BUF_BYTES = 32 * O_CHUNK * 2;
+constexpr int O_EPI_BYTES = O_EPI_WARPS * O_BUFS * O_BUF_BYTES;
+constexpr int O_REST_BYTES = O_EPI_WARPS * 256 * 4;      // POLY: the rests of the columns each epilogue warp works on
+constexpr int O_SMEM_BYTES = O_RING_BYTES + O_EPI_BYTES + O_REST_BYTES + 512 + 1024;
 constexpr int O_GROUP_M = 16;                // row tiles that are walked together
 constexpr int O_TMEM_COLS = 512;
 constexpr int O_MAX_MATS = 64;               // matrices of one round of launches
@@ -63,13 +68,13 @@ struct OrthoBatch {
 
 struct OrthoGemm {
   CUtensorMap a, b;
+  CUtensorMap aux_map, out_map;          // in boxes of 32 rows x O_CHUNK columns: aux, out
   OrthoBatch batch;
   int unit0[O_MAX_MATS + 1];
   int n_units;
   int bn, nb, kps, n_stages, n_acc;      // columns per B tile, B tiles per unit, k blocks per stage, ring depth, accumulators
-  const __half* aux;        // POLY: A; APPLY: X
   __half* out;              // packed result, or null: the caller's matrices
-  long long aux_ld, out_ld;
+  long long out_ld;
   const float* rest_in;     // [rows] what the rounding of the diagonal of A (POLY) or B (APPLY) left
   float* rest_out;          // GRAM, POLY: the same of the result
   float f_acc, f_aux, f_diag;
@@ -169,12 +174,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
-  const uint32_t bars = base + O_RING_BYTES;
+  const uint32_t bars = base + O_RING_BYTES + O_EPI_BYTES + O_REST_BYTES;
   auto full_bar = [&](int s) { return bars + 8u * s; };                                 // first CTA
   auto empty_bar = [&](int s) { return bars + 8u * (O_MAX_STAGES + s); };               // each CTA
   auto tfull_bar = [&](int a) { return bars + 8u * (2 * O_MAX_STAGES + a); };           // each CTA
   auto tempty_bar = [&](int a) { return bars + 8u * (2 * O_MAX_STAGES + 2 + a); };      // first CTA, the pair's epilogue threads
-  uint8_t* const tail = base_ptr + O_RING_BYTES + 8 * (2 * O_MAX_STAGES + 4);
+  auto aux_bar = [&](int i) { return bars + 8u * (2 * O_MAX_STAGES + 4 + i); };         // per epilogue warp and buffer
+  uint8_t* const tail = base_ptr + O_RING_BYTES + O_EPI_BYTES + O_REST_BYTES + 8 * (2 * O_MAX_STAGES + 4 + O_EPI_WARPS * O_BUFS);
   volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(tail + 8);
 
@@ -189,6 +195,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
   if (tid == 0) {
     for (int s = 0; s < q.n_stages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 2 * 32 * O_EPI_WARPS); }
+    for (int i = 0; i < O_EPI_WARPS * O_BUFS; ++i) mbar_init(aux_bar(i), 1);
     wait_state_init(abort_flag, q.wait_limit_ns);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -300,38 +307,64 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
     }
   } else {
     // ------------------------------------------------------------------ epilogue: a thread owns a row of the output
+    // What it reads beside the accumulators (this tile of A or X) and what it writes travel as boxes of 32 rows x 32 columns
+    // through the warp's buffers in shared memory, by TMA both ways: a lane's loads and stores of 32 bytes of its own row
+    // each take a request per lane (16 matrices of up to 1408 x 2048: POLY 62 us, APPLY 122 us; without their reads 46 and
+    // 91 us).  The result takes the place of what was read; three boxes are in flight ahead.
     int acc = 0;
-    uint32_t acc_phase = 0;
+    uint32_t acc_phase = 0, n = 0;                           // n: boxes so far; buffer n % O_BUFS
     bool ok = true;
     const int c_half = q.nb * q.bn / 2, c_first = c_half * (warp >> 2);
+    uint8_t* const bufs = base_ptr + O_RING_BYTES + warp * O_BUFS * O_BUF_BYTES;
+    [[maybe_unused]] float* const rests = reinterpret_cast<float*>(base_ptr + O_RING_BYTES + O_EPI_BYTES) + 256 * warp;
+    const uint32_t buf0 = smem_u32(bufs), swz = (uint32_t)(lane >> 1) & 3u;       // 64-byte swizzle: 16-byte piece i of a row at i ^ swz
+    const bool to_caller = MODE == ORTHO_APPLY && q.out == nullptr;
     for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
       const OrthoUnit u = ortho_unit<MODE>(q, unit);
       const OrthoMat& mat = q.batch.mat[u.e];
       const int warp_row = u.m0 + 128 * (int)rank + (warp & 3) * 32, row = warp_row + lane;      // in the matrix, < pad_rows(m)
-      const int cols = min(u.limit - u.n0, c_first + c_half);       // where this warp's columns end
+      const int cols = min(u.limit - u.n0, c_first + c_half);       // where this warp's columns end, a multiple of O_CHUNK
       float f = q.f_acc;
       if (MODE != ORTHO_POLY) {
         const int small = q.small[u.e];
         const float s = q.first != nullptr ? q.first[u.e] : scalbnf(1.f, scale_of(small, q.small_in));
         f = MODE == ORTHO_GRAM ? f / s / s : scalbnf(f / s, q.out != nullptr ? scale_of(small, q.small_out) : 0);
       }
+      const float rest = MODE == ORTHO_GRAM ? 0.f : q.rest_in[mat.row0 + row];
+      auto fetch = [&](int c, uint32_t box) {                      // lane 0: the box at column c on its way
+        if (MODE != ORTHO_GRAM && c < cols) {
+          const uint32_t bar = aux_bar(warp * O_BUFS + box % O_BUFS);
+          mbar_expect_tx(bar, O_BUF_BYTES);
+          tma_load_2d(buf0 + box % O_BUFS * O_BUF_BYTES, &q.aux_map, bar, u.n0 + c, mat.row0 + warp_row);
+        }
+      };
+      if (lane == 0) {
+#pragma unroll
+        for (int k = 0; k < O_BUFS - 1; ++k) fetch(c_first + O_CHUNK * k, n + k);
+      }
+      if (MODE == ORTHO_POLY) {
+        __syncwarp();
+        for (int i = 4 * lane; c_first + i < cols; i += 128)
+          *reinterpret_cast<float4*>(rests + i) = *reinterpret_cast<const float4*>(q.rest_in + mat.row0 + u.n0 + c_first + i);
+      }
+      __syncwarp();
       ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_phase, abort_flag));
       if (!ok) break;
       tc_fence_after();
       const uint32_t t0 = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(acc * q.nb * q.bn);
-      const long long at = (long long)(mat.row0 + row) * q.out_ld + u.n0;
-      const float rest = MODE == ORTHO_GRAM ? 0.f : q.rest_in[mat.row0 + row];
-      auto put = [&](const uint32_t* raw, int c) {
+      uint8_t* box_row = bufs;                                      // this lane's row of the box at work
+      auto put = [&](const uint32_t* raw, int k, int c) {
         uint32_t p[8];
         float v[16];
+        uint4* const piece0 = reinterpret_cast<uint4*>(box_row + (((2 * k) ^ swz) << 4));
+        uint4* const piece1 = reinterpret_cast<uint4*>(box_row + (((2 * k + 1) ^ swz) << 4));
         if (MODE == ORTHO_GRAM) {
 #pragma unroll
           for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(raw[j]) * f;
         } else {
           uint32_t a[8];
-          const uint4* const src = reinterpret_cast<const uint4*>(q.aux + (long long)(mat.row0 + row) * q.aux_ld + u.n0 + c);
-          *reinterpret_cast<uint4*>(a) = src[0];
-          *reinterpret_cast<uint4*>(a + 4) = src[1];
+          *reinterpret_cast<uint4*>(a) = *piece0;
+          *reinterpret_cast<uint4*>(a + 4) = *piece1;
 #pragma unroll
           for (int j = 0; j < 16; j += 2) {
             const float2 old = __half22float2(*reinterpret_cast<const __half2*>(&a[j >> 1]));
@@ -339,14 +372,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
               v[j] = fmaf(rest, old.x, __uint_as_float(raw[j])) * f;
               v[j + 1] = fmaf(rest, old.y, __uint_as_float(raw[j + 1])) * f;
             } else {                                    // (A + rest)^2 up to the square of the rest, and b (A + rest)
-              const float2 down = *reinterpret_cast<const float2*>(q.rest_in + mat.row0 + u.n0 + c + j);
+              const float2 down = *reinterpret_cast<const float2*>(rests + c - c_first + j);
               const float x = u.n0 + c + j == row ? rest : 0.f, y = u.n0 + c + j + 1 == row ? rest : 0.f;
               v[j] = fmaf(old.x + x, q.f_aux, fmaf(rest + down.x, old.x, __uint_as_float(raw[j])) * f);
               v[j + 1] = fmaf(old.y + y, q.f_aux, fmaf(rest + down.y, old.y, __uint_as_float(raw[j + 1])) * f);
             }
           }
         }
-        if (MODE == ORTHO_APPLY && q.out == nullptr) {
+        if (to_caller) {
           // the result, in the caller's layout
 #pragma unroll
           for (int j = 0; j < 8; ++j) p[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
@@ -379,27 +412,50 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) p[j] = pack_half(v[2 * j], v[2 * j + 1]);
-        st_global_v8(q.out + at + c, p);
+        *piece0 = make_uint4(p[0], p[1], p[2], p[3]);
+        *piece1 = make_uint4(p[4], p[5], p[6], p[7]);
         if (MODE != ORTHO_APPLY && u.n0 + c >= u.m0 + O_TILE_M)      // off the diagonal's block: the other half of the result
           store_turned(reinterpret_cast<uint16_t*>(q.out) + (long long)(mat.row0 + u.n0 + c) * q.out_ld + warp_row, q.out_ld, p, lane, 32, 16,
                        true);
       };
       uint32_t v0[16], v1[16];
-      int c = c_first;
-      if (c < cols) tmem_ld16(t0 + c, v0);
-      for (; c < cols; c += 32) {
-        const int c1 = c + 16, c2 = c1 + 16;
+      if (c_first < cols) tmem_ld16(t0 + c_first, v0);
+      for (int c = c_first; c < cols; c += O_CHUNK, ++n) {
+        const uint32_t box = n % O_BUFS;
+        box_row = bufs + box * O_BUF_BYTES + lane * (2 * O_CHUNK);
+        if (MODE != ORTHO_GRAM) {
+          ok = warp_wait(aux_bar(warp * O_BUFS + box), n / O_BUFS & 1u, abort_flag);
+          if (!ok) break;
+        }
         tmem_ld_wait(v0);
-        if (c1 < cols) tmem_ld16(t0 + c1, v1);
-        put(v0, c);
-        if (c1 >= cols) break;
+        tmem_ld16(t0 + c + 16, v1);
+        put(v0, 0, c);
         tmem_ld_wait(v1);
-        if (c2 < cols) tmem_ld16(t0 + c2, v0);
-        put(v1, c1);
+        if (c + O_CHUNK < cols) tmem_ld16(t0 + c + O_CHUNK, v0);
+        put(v1, 1, c + 16);
+        if (!to_caller) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          if (!to_caller) {
+            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(&q.out_map),
+                         "r"(buf0 + box * O_BUF_BYTES), "r"(u.n0 + c), "r"(mat.row0 + warp_row)
+                         : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");      // the box before has been read: its buffer is free
+          }
+          fetch(c + (O_BUFS - 1) * O_CHUNK, n + O_BUFS - 1);
+        }
+        __syncwarp();
       }
+      if (!ok) break;
       tc_fence_before();
       mbar_arrive_cluster(map_to_cta(tempty_bar(acc), 0));
       if (++acc == q.n_acc) { acc = 0; acc_phase ^= 1u; }
+    }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    if (!ok) {               // boxes on their way land before the CTA's shared memory is given up
+      const unsigned long long t0 = globaltimer_ns();
+      while (globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
     }
   }
 
@@ -440,7 +496,7 @@ __device__ __forceinline__ double block_sum(double v) {
   return v;
 }
 
-// Sums of squares of runs of rows; in double, so that no square of an fp32 value overflows or is lost.
+// Sums of squares of runs of rows; eight at a time in fp32 (added in double), in double where that could overflow or vanish.
 template <typename T>
 __global__ void __launch_bounds__(LOAD_THREADS) k_ortho_norm(const __grid_constant__ OrthoLoad q) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -449,20 +505,24 @@ __global__ void __launch_bounds__(LOAD_THREADS) k_ortho_norm(const __grid_consta
   const OrthoMat& mat = q.batch.mat[blockIdx.y];
   const int rows = mat.turned ? mat.n : mat.m, cols = mat.turned ? mat.m : mat.n;
   const T* const in = static_cast<const T*>(mat.in);
-  double s0 = 0.0, s1 = 0.0;
+  double sum = 0.0;
   for (int r = blockIdx.x * (LOAD_THREADS / 32) + (threadIdx.x >> 5); r < rows; r += gridDim.x * (LOAD_THREADS / 32)) {
     const T* const p = in + r * mat.in_ld;
-    int c = threadIdx.x & 31;
-    for (; c + 224 < cols; c += 256) {
-      float v[8];
+    for (int c = threadIdx.x & 31; c < cols; c += 256) {
+      float v[8], s = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = to_f32(p[c + 32 * i]);
+      for (int i = 0; i < 8; ++i) v[i] = c + 32 * i < cols ? to_f32(p[c + 32 * i]) : 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; i += 2) { s0 = fma((double)v[i], (double)v[i], s0); s1 = fma((double)v[i + 1], (double)v[i + 1], s1); }
+      for (int i = 0; i < 8; ++i) s = fmaf(v[i], v[i], s);
+      if (s > 1e-20f && s < 1e30f) {
+        sum += (double)s;
+      } else {                          // squares that fp32 may not hold
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = fma((double)v[i], (double)v[i], sum);
+      }
     }
-    for (; c < cols; c += 32) { const double v = to_f32(p[c]); s0 = fma(v, v, s0); }
   }
-  const double s = block_sum(s0 + s1);
+  const double s = block_sum(sum);
   if (threadIdx.x == 0) q.part[blockIdx.y * q.parts + blockIdx.x] = s;
 }
 
@@ -490,6 +550,7 @@ __global__ void __launch_bounds__(LOAD_THREADS) k_ortho_load(const __grid_consta
     if (norm > 0.0 && norm < 1e300) frexp(all / norm, &e);       // all / norm in [2^(e-1), 2^e)
     q.small[blockIdx.y] = min(e - 1, 100);
   }
+  const float up = scalbnf(1.f, p / 2), up2 = scalbnf(1.f, p - p / 2);
   const int rt = pad_rows(mat.m) / 64, ct = pad_cols(mat.n) / 64;
   const T* const in = static_cast<const T*>(mat.in);
   for (int t = blockIdx.x; t < rt * ct; t += gridDim.x) {
@@ -506,7 +567,7 @@ __global__ void __launch_bounds__(LOAD_THREADS) k_ortho_load(const __grid_consta
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int k = threadIdx.x + LOAD_THREADS * i, a = k >> 6, b = k & 63;
-      const __half h = __float2half_rn(ldexpf(v[i], p));
+      const __half h = __float2half_rn(v[i] * up * up2);
       if (mat.turned) tile[b][a] = h; else tile[a][b] = h;
     }
     __syncthreads();
@@ -626,10 +687,20 @@ OrthoTile choose_tile(const OrthoBatch& b, int n_pairs) {
   return best;
 }
 
-bool enc_f16(CUtensorMap* out, const void* p, long long rows, long long cols, int box_rows) {
-  // fp16 and bf16 differ in nothing a copy without arithmetic sees
-  return encode_bf16_2d_pitch(out, p, (uint64_t)rows, (uint64_t)cols, (uint64_t)cols, (uint32_t)box_rows);
-}
+// A packed buffer [rows, cols] and the tensor maps that read or write it: as an operand in boxes of 64 columns x 128 or 64 rows,
+// and in the epilogue's boxes.  (fp16 and bf16 differ in nothing a copy without arithmetic sees.)
+struct Packed {
+  __half* p;
+  long long ld;
+  CUtensorMap rows128, rows64, box;
+  bool encode(void* at, long long rows, long long cols) {
+    p = static_cast<__half*>(at);
+    ld = cols;
+    return encode_bf16_2d_pitch(&rows128, p, (uint64_t)rows, (uint64_t)cols, (uint64_t)cols, 128) &&
+           encode_bf16_2d_pitch(&rows64, p, (uint64_t)rows, (uint64_t)cols, (uint64_t)cols, 64) &&
+           encode_bf16_2d_narrow(&box, p, (uint64_t)rows, (uint64_t)cols, (uint64_t)cols, 32);
+  }
+};
 
 #define ORTHO_CK(...)             \
   do {                            \
@@ -639,10 +710,9 @@ bool enc_f16(CUtensorMap* out, const void* p, long long rows, long long cols, in
     }                             \
   } while (0)
 
-// a, b: the packed operands (rows x cols); B of APPLY is read with its columns as N.
+// B of APPLY is read with its columns as N.  aux: A or X, in out's columns, or null; out null: the caller's matrices.
 template <int MODE>
-int launch_ortho(OrthoGemm& q, const __half* a, long long a_cols, const __half* b, long long b_cols, long long rows, int n_pairs,
-                 cudaStream_t st) {
+int launch_ortho(OrthoGemm& q, const Packed& a, const Packed& b, const Packed* aux, const Packed* out, int n_pairs, cudaStream_t st) {
   const OrthoTile t = choose_tile<MODE>(q.batch, n_pairs);
   q.bn = t.bn; q.nb = t.nb;
   q.n_acc = t.nb * t.bn <= 256 ? 2 : 1;
@@ -656,7 +726,12 @@ int launch_ortho(OrthoGemm& q, const __half* a, long long a_cols, const __half* 
   }
   q.unit0[q.batch.n_mats] = units;
   q.n_units = units;
-  if (!enc_f16(&q.a, a, rows, a_cols, 128) || !enc_f16(&q.b, b, rows, b_cols, MODE == ORTHO_APPLY ? 64 : t.bn / 2)) return CAMERA_ERR_CUDA;
+  q.a = a.rows128;
+  q.b = MODE == ORTHO_APPLY || t.bn == 128 ? b.rows64 : b.rows128;
+  if (aux != nullptr) q.aux_map = aux->box;
+  if (out != nullptr) q.out_map = out->box;
+  q.out = out != nullptr ? out->p : nullptr;
+  q.out_ld = out != nullptr ? out->ld : 0;
   ORTHO_CK(allow_smem<k_ortho_gemm<MODE>, O_SMEM_BYTES>());
   ORTHO_CK(launch_chained(k_ortho_gemm<MODE>, q, 2 * (units < n_pairs ? units : n_pairs), 1, 1, O_THREADS, O_SMEM_BYTES, true, st));
   return CAMERA_OK;
@@ -683,16 +758,16 @@ int run_round(const camera_matrix_t* mats, const OrthoRound& r, int32_t dtype, c
   }
   if (q.batch.n_mats == 0) return CAMERA_OK;
   const int sms = sm_count(), n_pairs = sms / 2;
-  __half* x = reinterpret_cast<__half*>(ws + l.x0);
-  __half* x_next = reinterpret_cast<__half*>(ws + l.x1);
-  __half* const a = reinterpret_cast<__half*>(ws + l.a);
-  __half* const b = reinterpret_cast<__half*>(ws + l.b);
+  Packed xs[2], a, b;
+  if (!xs[0].encode(ws + l.x0, r.rows, r.x_ld) || !xs[1].encode(ws + l.x1, r.rows, r.x_ld) || !a.encode(ws + l.a, r.rows, r.a_ld) ||
+      !b.encode(ws + l.b, r.rows, r.a_ld))
+    return CAMERA_ERR_CUDA;
   OrthoLoad ld;
   ld.batch = q.batch;
   ld.part = reinterpret_cast<double*>(ws + l.part);
   ld.first = reinterpret_cast<float*>(ws + l.first);
   ld.small = reinterpret_cast<int*>(ld.first + O_MAX_MATS);
-  ld.eps = eps; ld.x = x; ld.x_ld = r.x_ld;
+  ld.eps = eps; ld.x = xs[0].p; ld.x_ld = r.x_ld;
   ld.totals = reinterpret_cast<PlanTotals*>(ws);
   float* const rest_a = reinterpret_cast<float*>(ws + l.rest_a);
   float* const rest_b = reinterpret_cast<float*>(ws + l.rest_b);
@@ -719,30 +794,25 @@ int run_round(const camera_matrix_t* mats, const OrthoRound& r, int32_t dtype, c
     const StepBound bound = step_bound(k, h * MARGIN);
     const double sa = factor_for(h * h), sb = factor_for(bound.b), sn = factor_for(bound.h);
     const bool last = s + 1 == steps;
+    const Packed& x = xs[s & 1];
     q.first = s == 0 ? ld.first : nullptr;
-    q.out = a; q.out_ld = r.a_ld;
     q.rest_out = rest_a;
     q.f_acc = (float)(sa / (sx * sx));
     q.small_in = (int)ceil(log2(fmax(grown / h, 1.0)));
     grown *= bound.b * MARGIN;
     q.small_out = (int)ceil(log2(fmax(grown / bound.h, 1.0)));
-    int rc = launch_ortho<ORTHO_GRAM>(q, x, r.x_ld, x, r.x_ld, r.rows, n_pairs, st);
+    int rc = launch_ortho<ORTHO_GRAM>(q, x, x, nullptr, &a, n_pairs, st);
     if (rc != CAMERA_OK) return rc;
     q.first = nullptr;
-    q.aux = a; q.aux_ld = r.a_ld;
-    q.out = b;
     q.rest_in = rest_a; q.rest_out = rest_b;
     q.f_acc = (float)(sb * k[2] / (sa * sa)); q.f_aux = (float)(sb * k[1] / sa); q.f_diag = (float)(sb * k[0]);
-    rc = launch_ortho<ORTHO_POLY>(q, a, r.a_ld, a, r.a_ld, r.rows, n_pairs, st);
+    rc = launch_ortho<ORTHO_POLY>(q, a, a, &a, &b, n_pairs, st);
     if (rc != CAMERA_OK) return rc;
     q.first = s == 0 ? ld.first : nullptr;
-    q.aux = x; q.aux_ld = r.x_ld;
-    q.out = last ? nullptr : x_next; q.out_ld = r.x_ld;
     q.rest_in = rest_b; q.rest_out = nullptr;
     q.f_acc = (float)((last ? 1.0 : sn) / (sb * sx));
-    rc = launch_ortho<ORTHO_APPLY>(q, b, r.a_ld, x, r.x_ld, r.rows, n_pairs, st);
+    rc = launch_ortho<ORTHO_APPLY>(q, b, x, &x, last ? nullptr : &xs[(s + 1) & 1], n_pairs, st);
     if (rc != CAMERA_OK) return rc;
-    __half* const swap = x; x = x_next; x_next = swap;
     h = bound.h;
     sx = sn;
   }

@@ -277,17 +277,18 @@ EncodeTiledFn get_encode_fn() {
   return fn;
 }
 
-// bf16 row-major [rows, d] matrix, box = 64 columns (128 bytes) x box_rows rows, 128-byte swizzle.
+// bf16 row-major [rows, d] matrix, box = 64 columns (128 bytes) x box_rows rows, 128-byte swizzle (32 columns: 64-byte swizzle).
 bool encode_2d(EncodeTiledFn fn, void* out, const void* ptr, uint64_t rows, uint64_t d, uint32_t box_rows,
-               uint64_t pitch = 0) {
+               uint64_t pitch = 0, uint32_t box_cols = U_BK) {
   if (ptr == nullptr || rows == 0 || d == 0) { memset(out, 0, 128); return true; }
   CUtensorMap m;
   const cuuint64_t dims[2] = {d, rows};
   const cuuint64_t strides[1] = {(pitch ? pitch : d) * 2};
-  const cuuint32_t box[2] = {(cuuint32_t)U_BK, box_rows};
+  const cuuint32_t box[2] = {(cuuint32_t)box_cols, box_rows};
   const cuuint32_t estr[2] = {1, 1};
   const CUresult r = fn(&m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr,
-                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return false;
   memcpy(out, &m, sizeof(m));
@@ -304,6 +305,11 @@ bool encode_bf16_2d(void* out, const void* ptr, uint64_t rows, uint64_t d, uint3
 bool encode_bf16_2d_pitch(void* out, const void* ptr, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows) {
   EncodeTiledFn fn = get_encode_fn();
   return fn != nullptr && encode_2d(fn, out, ptr, rows, cols, box_rows, pitch);
+}
+
+bool encode_bf16_2d_narrow(void* out, const void* ptr, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows) {
+  EncodeTiledFn fn = get_encode_fn();
+  return fn != nullptr && encode_2d(fn, out, ptr, rows, cols, box_rows, pitch, 32);
 }
 
 bool umma_shape_ok(const camera_layer_t* L) {
