@@ -16,7 +16,7 @@ namespace {
 constexpr int MOE_MAX_EXPERTS = 1024, MOE_MAX_D = 1 << 20;
 constexpr int MOE_THREADS = 256, MOE_WARPS = MOE_THREADS / 32;
 // Up to so many pairs every CTA counts all of them for itself; beyond, a kernel before counts them chunk by chunk.
-constexpr long long MOE_SMALL = 16384;
+constexpr long long MOE_SMALL = 8192;
 
 struct Dispatch {
   const void* x;
@@ -24,9 +24,10 @@ struct Dispatch {
   long long x_ld, xs_ld;
   const int32_t* idx;
   int32_t *rows, *offsets;
-  int32_t* hist;                 // [chunks][experts] pairs per chunk and expert, or null
+  int32_t* hist;                 // [experts][chunks] pairs per expert and chunk, then those of the chunks before; or null
+  int32_t* totals;               // [experts]
   int tokens, k, experts, d;
-  int chunk;                     // tokens a CTA handles
+  int chunk, chunks;             // tokens a CTA handles, CTAs
 };
 
 __device__ __forceinline__ bool usable(int e, int experts) { return (unsigned)e < (unsigned)experts; }
@@ -42,7 +43,36 @@ __global__ void __launch_bounds__(MOE_THREADS) k_moe_count(const Dispatch q) {
     if (usable(e, q.experts)) atomicAdd(&count[e], 1);
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < q.experts; e += MOE_THREADS) q.hist[(long long)blockIdx.x * q.experts + e] = count[e];
+  for (int e = threadIdx.x; e < q.experts; e += MOE_THREADS) q.hist[(long long)e * gridDim.x + blockIdx.x] = count[e];
+}
+
+// A warp per expert: exclusive sums over the chunks.  The kernel after it is let in when this one ends, not before: CTAs that
+// come while those of k_moe_count still run spread unevenly over the SMs (16384 tokens to 8 of 64 experts: 206 -> 245 us).
+constexpr int SCAN_WARPS = 4;
+__global__ void __launch_bounds__(32 * SCAN_WARPS) k_moe_scan(const Dispatch q) {
+  const int e = blockIdx.x * SCAN_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (e >= q.experts) return;
+  int32_t* const hist = q.hist + (long long)e * q.chunks;
+  constexpr int R = 10;              // chunks a lane holds at a time: 2 * 148 chunks are one pass
+  int before = 0;
+  for (int c0 = 0; c0 < q.chunks; c0 += 32 * R) {
+    int v[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) v[i] = c0 + 32 * i + lane < q.chunks ? hist[c0 + 32 * i + lane] : 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      int sum = v[i];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += up;
+      }
+      if (c0 + 32 * i + lane < q.chunks) hist[c0 + 32 * i + lane] = before + sum - v[i];
+      before += __shfl_sync(0xffffffffu, sum, 31);
+    }
+  }
+  if (lane == 0) q.totals[e] = before;
 }
 
 // A CTA takes a run of consecutive tokens: it finds where each expert's rows begin and how many pairs lie before its own,
@@ -76,19 +106,10 @@ __global__ void __launch_bounds__(MOE_THREADS) k_moe_dispatch(const Dispatch q) 
     }
   } else {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int slices = MOE_THREADS / E > 1 ? MOE_THREADS / E : 1, slice = tid / E;      // threads along the chunks
-    if (slices == 1 || slice < slices)
-      for (int e = slices == 1 ? tid : tid - slice * E; e < E; e += slices == 1 ? MOE_THREADS : E) {
-        int all = 0, mine = 0;
-#pragma unroll 8
-        for (int c = slices == 1 ? 0 : slice; c < (int)gridDim.x; c += slices) {
-          const int v = q.hist[(long long)c * E + e];
-          all += v;
-          if (c < (int)blockIdx.x) mine += v;
-        }
-        atomicAdd(&total[e], all);
-        atomicAdd(&before[e], mine);
-      }
+    for (int e = tid; e < E; e += MOE_THREADS) {
+      total[e] = q.totals[e];
+      before[e] = q.hist[(long long)e * q.chunks + blockIdx.x];
+    }
   }
   __syncthreads();
   // exclusive scan over the experts: a thread takes `per` consecutive ones
@@ -174,55 +195,66 @@ struct Combine {
   int warps;                     // backward: warps that share a token
 };
 
-constexpr int SLOTS = 8;         // rows of a token in flight
-
-// A thread takes one pack of one token: k rows in flight, added in the order of the slots.
-template <typename T, int W>
-__global__ void __launch_bounds__(256, 4) k_moe_combine(const Combine q) {
+// S rows of a token and U packs of each in flight a thread.
+// A thread takes U packs of one token, its k rows S at a time, added in the order of the slots.
+template <typename T, int W, int S, int U>
+__global__ void __launch_bounds__(256, U == 1 ? 4 : U == 2 ? 3 : 2) k_moe_combine(const Combine q) {
   using P = Pack<T, W>;
   const long long t = (long long)blockIdx.x * blockDim.y + threadIdx.y;
-  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * W;
-  if (t >= q.tokens || c >= q.d) return;
-  const T* const ys = static_cast<const T*>(q.ys) + c;
-  P extra;
-  if (q.add != nullptr) extra = *reinterpret_cast<const P*>(static_cast<const T*>(q.add) + t * q.add_ld + c);
-  float sum[W];
+  const int c0 = (blockIdx.y * U * blockDim.x + threadIdx.x) * W, step = blockDim.x * W;
+  if (t >= q.tokens) return;
+  const T* const ys = static_cast<const T*>(q.ys) + c0;
+  float sum[U][W];
 #pragma unroll
-  for (int i = 0; i < W; ++i) sum[i] = 0.f;
-  for (int j0 = 0; j0 < q.k; j0 += SLOTS) {
-    int row[SLOTS];
-    float w[SLOTS];
-    P v[SLOTS];
+  for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int j = 0; j < SLOTS; ++j) {
+    for (int i = 0; i < W; ++i) sum[u][i] = 0.f;
+  for (int j0 = 0; j0 < q.k; j0 += S) {
+    // Row numbers first, then all loads, weights when they are needed: registers decide how many threads an SM holds, and with them
+    // the loads in flight.
+    int row[S];
+    P v[S][U];
+#pragma unroll
+    for (int j = 0; j < S; ++j) {
       row[j] = j0 + j < q.k ? q.rows[t * q.k + j0 + j] : -1;
       if (row[j] >= q.n_rows) row[j] = -1;
-      w[j] = row[j] >= 0 && q.w != nullptr ? q.w[t * q.k + j0 + j] : 1.f;
     }
 #pragma unroll
-    for (int j = 0; j < SLOTS; ++j)
-      if (row[j] >= 0) v[j] = *reinterpret_cast<const P*>(ys + row[j] * q.ys_ld);
-#pragma unroll
-    for (int j = 0; j < SLOTS; ++j)
+    for (int j = 0; j < S; ++j)
       if (row[j] >= 0) {
-        float f[W];
-        v[j].get(f);
 #pragma unroll
-        for (int i = 0; i < W; ++i) sum[i] = fmaf(w[j], f[i], sum[i]);
+        for (int u = 0; u < U; ++u)
+          if (c0 + u * step < q.d) v[j][u] = *reinterpret_cast<const P*>(ys + row[j] * q.ys_ld + u * step);
+      }
+#pragma unroll
+    for (int j = 0; j < S; ++j)
+      if (row[j] >= 0) {
+        const float w = q.w != nullptr ? q.w[t * q.k + j0 + j] : 1.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float f[W];
+          v[j][u].get(f);
+#pragma unroll
+          for (int i = 0; i < W; ++i) sum[u][i] = fmaf(w, f[i], sum[u][i]);
+        }
       }
   }
-  if (q.add != nullptr) {
-    float f[W];
-    extra.get(f);
 #pragma unroll
-    for (int i = 0; i < W; ++i) sum[i] += f[i];
-  }
-  P out;
-  out.set(sum);
-  *reinterpret_cast<P*>(static_cast<T*>(q.y) + t * q.y_ld + c) = out;
+  for (int u = 0; u < U; ++u)
+    if (c0 + u * step < q.d) {
+      if (q.add != nullptr) {
+        float f[W];
+        reinterpret_cast<const P*>(static_cast<const T*>(q.add) + t * q.add_ld + c0 + u * step)->get(f);
+#pragma unroll
+        for (int i = 0; i < W; ++i) sum[u][i] += f[i];
+      }
+      P out;
+      out.set(sum[u]);
+      *reinterpret_cast<P*>(static_cast<T*>(q.y) + t * q.y_ld + c0 + u * step) = out;
+    }
 }
 
-template <typename T, int W>
+template <typename T, int W, int S, int U>
 __global__ void __launch_bounds__(512, 1) k_moe_combine_backward(const Combine q) {
   using P = Pack<T, W>;
   const int threads = 32 * q.warps, group = threadIdx.x / threads, i0 = threadIdx.x - group * threads;
@@ -232,47 +264,58 @@ __global__ void __launch_bounds__(512, 1) k_moe_combine_backward(const Combine q
   const T* const ys = static_cast<const T*>(q.ys);
   T* const dys = static_cast<T*>(q.dys);
   int buf = 0;
-  for (int j0 = 0; j0 < q.k; j0 += SLOTS) {
-    int row[SLOTS];
-    float w[SLOTS], dot[SLOTS];
+  for (int j0 = 0; j0 < q.k; j0 += S) {
+    int row[S];
+    float w[S], dot[S];
 #pragma unroll
-    for (int j = 0; j < SLOTS; ++j) {
+    for (int j = 0; j < S; ++j) {
       row[j] = j0 + j < q.k ? q.rows[t * q.k + j0 + j] : -1;
       if (row[j] >= q.n_rows) row[j] = -1;
       w[j] = row[j] >= 0 && q.w != nullptr ? q.w[t * q.k + j0 + j] : 1.f;
       dot[j] = 0.f;
     }
-    for (int c = i0 * W; c < q.d; c += threads * W) {
-      const P g = *reinterpret_cast<const P*>(dy + c);
-      P v[SLOTS];
-      float d[W];
+    const int step = threads * W;
+    for (int c0 = i0 * W; c0 < q.d; c0 += U * step) {
+      P g[U], v[S][U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c0 + u * step < q.d) g[u] = *reinterpret_cast<const P*>(dy + c0 + u * step);
       if (q.dw != nullptr) {
 #pragma unroll
-        for (int j = 0; j < SLOTS; ++j)
-          if (row[j] >= 0) v[j] = *reinterpret_cast<const P*>(ys + row[j] * q.ys_ld + c);
-      }
-      g.get(d);
+        for (int j = 0; j < S; ++j)
+          if (row[j] >= 0) {
 #pragma unroll
-      for (int j = 0; j < SLOTS; ++j)
-        if (row[j] >= 0) {
-          P out;
-          float f[W];
-          if (q.dw != nullptr) {
-            v[j].get(f);
-#pragma unroll
-            for (int i = 0; i < W; ++i) dot[j] = fmaf(d[i], f[i], dot[j]);
+            for (int u = 0; u < U; ++u)
+              if (c0 + u * step < q.d) v[j][u] = *reinterpret_cast<const P*>(ys + row[j] * q.ys_ld + c0 + u * step);
           }
+      }
 #pragma unroll
-          for (int i = 0; i < W; ++i) f[i] = w[j] * d[i];
-          out.set(f);
-          if (q.dys != nullptr) *reinterpret_cast<P*>(dys + row[j] * q.dys_ld + c) = out;
-        }
+      for (int u = 0; u < U; ++u) {
+        if (c0 + u * step >= q.d) break;
+        float d[W];
+        g[u].get(d);
+#pragma unroll
+        for (int j = 0; j < S; ++j)
+          if (row[j] >= 0) {
+            P out;
+            float f[W];
+            if (q.dw != nullptr) {
+              v[j][u].get(f);
+#pragma unroll
+              for (int i = 0; i < W; ++i) dot[j] = fmaf(d[i], f[i], dot[j]);
+            }
+#pragma unroll
+            for (int i = 0; i < W; ++i) f[i] = w[j] * d[i];
+            out.set(f);
+            if (q.dys != nullptr) *reinterpret_cast<P*>(dys + row[j] * q.dys_ld + c0 + u * step) = out;
+          }
+      }
     }
     if (q.dw == nullptr) continue;
     group_sum(dot, q.warps, group, buf);
     if (i0 == 0) {
 #pragma unroll
-      for (int j = 0; j < SLOTS; ++j)
+      for (int j = 0; j < S; ++j)
         if (j0 + j < q.k) q.dw[t * q.k + j0 + j] = dot[j];
     }
   }
@@ -284,7 +327,7 @@ int moe_ctas(int64_t tokens) {
   return (int)(tokens < most ? tokens : most);
 }
 size_t moe_hist_bytes(int64_t tokens, int k, int experts) {
-  return tokens * k <= MOE_SMALL ? 0 : (size_t)4 * moe_ctas(tokens) * experts;
+  return tokens * k <= MOE_SMALL ? 0 : (size_t)4 * (moe_ctas(tokens) + 1) * experts;
 }
 
 bool sizes_ok(int64_t tokens, int k, int d, int32_t dtype) {
@@ -311,24 +354,42 @@ cudaError_t launch_dispatch(const Dispatch& q, bool vec, int ctas, cudaStream_t 
   return vec ? launch_chained(k_moe_dispatch<T, W>, q, ctas, 1, 1, MOE_THREADS, smem, q.hist != nullptr, st)
              : launch_chained(k_moe_dispatch<T, 1>, q, ctas, 1, 1, MOE_THREADS, smem, q.hist != nullptr, st);
 }
-template <typename T, int W>
-cudaError_t launch_combine_as(const Combine& q, cudaStream_t st) {
-  const int packs = (q.d + W - 1) / W, slices = (packs + 255) / 256;
-  const int bx = ((packs + slices - 1) / slices + 31) & ~31, ty = 256 / bx;
-  k_moe_combine<T, W><<<dim3((unsigned)((q.tokens + ty - 1) / ty), (unsigned)slices), dim3((unsigned)bx, (unsigned)ty), 0, st>>>(q);
+// Slots S and packs U a thread: as many loads in flight whatever k is (8 vectors or 16 elements), but one pack a thread where one
+// wave of threads takes all of them.
+template <typename T, int W, int S, int U>
+cudaError_t combine_as(const Combine& q, cudaStream_t st) {
+  const int packs = (q.d + W - 1) / W, slices = (packs + 256 * U - 1) / (256 * U);
+  const int bx = ((packs + slices * U - 1) / (slices * U) + 31) & ~31, ty = 256 / bx;
+  k_moe_combine<T, W, S, U><<<dim3((unsigned)((q.tokens + ty - 1) / ty), (unsigned)slices), dim3((unsigned)bx, (unsigned)ty), 0, st>>>(q);
   return cudaGetLastError();
 }
 template <typename T, int W>
-cudaError_t launch_combine_backward_as(const Combine& a, cudaStream_t st) {
+cudaError_t launch_combine_as(const Combine& q, cudaStream_t st) {
+  constexpr int F = W > 1 ? 8 : 16;
+  const bool one = (long long)q.tokens * ((q.d + W - 1) / W) <= 1024ll * sm_count();
+  if (q.k == 1) return one ? combine_as<T, W, 1, 1>(q, st) : combine_as<T, W, 1, F>(q, st);
+  if (q.k == 2) return one ? combine_as<T, W, 2, 1>(q, st) : combine_as<T, W, 2, F / 2>(q, st);
+  if (q.k <= 4) return one ? combine_as<T, W, 4, 1>(q, st) : combine_as<T, W, 4, F / 4>(q, st);
+  return one || W > 1 ? combine_as<T, W, 8, 1>(q, st) : combine_as<T, W, 8, F / 8>(q, st);
+}
+template <typename T, int W, int S, int U>
+cudaError_t combine_backward_as(const Combine& a, int each, cudaStream_t st) {
   Combine q = a;
   const int packs = (q.d + W - 1) / W;
-  // four packs a thread; one where there are fewer tokens than CTAs the GPU holds
-  const int each = q.tokens < 2 * sm_count() ? 1 : 4;
   q.warps = (packs + 32 * each - 1) / (32 * each);
   if (q.warps > 16) q.warps = 16;
   const int groups = q.warps >= 8 ? 1 : 8 / q.warps;
-  k_moe_combine_backward<T, W><<<(unsigned)((q.tokens + groups - 1) / groups), 32 * q.warps * groups, 0, st>>>(q);
+  k_moe_combine_backward<T, W, S, U><<<(unsigned)((q.tokens + groups - 1) / groups), 32 * q.warps * groups, 0, st>>>(q);
   return cudaGetLastError();
+}
+template <typename T, int W>
+cudaError_t launch_combine_backward_as(const Combine& q, cudaStream_t st) {
+  // packs a thread: four or more; one where there are fewer tokens than CTAs the GPU holds
+  const bool few = q.tokens < 2 * sm_count();
+  if (q.k == 1) return few ? combine_backward_as<T, W, 1, 1>(q, 1, st) : combine_backward_as<T, W, 1, 8>(q, 8, st);
+  if (q.k == 2) return few ? combine_backward_as<T, W, 2, 1>(q, 1, st) : combine_backward_as<T, W, 2, 4>(q, 4, st);
+  if (q.k <= 4) return few ? combine_backward_as<T, W, 4, 1>(q, 1, st) : combine_backward_as<T, W, 4, 2>(q, 4, st);
+  return combine_backward_as<T, W, 8, 1>(q, few ? 1 : 4, st);
 }
 
 int combine(const void* ys, int32_t dtype, int64_t ys_ld, int64_t n_rows, const int32_t* rows, const float* w, int64_t tokens, int32_t k,
@@ -383,9 +444,12 @@ extern "C" int camera_moe_dispatch(const void* x, int32_t dtype, int64_t ld, int
   int ctas = moe_ctas(n_tokens);
   q.chunk = (int)((n_tokens + ctas - 1) / ctas);
   ctas = (int)((n_tokens + q.chunk - 1) / q.chunk);
+  q.chunks = ctas;
   if (hist > 0) {
-    q.hist = static_cast<int32_t*>(workspace);
+    q.totals = static_cast<int32_t*>(workspace);
+    q.hist = q.totals + n_experts;
     MOE_CK(launch_chained(k_moe_count, q, ctas, 1, 1, MOE_THREADS, 4 * n_experts, false, st));
+    MOE_CK(launch_chained(k_moe_scan, q, (n_experts + SCAN_WARPS - 1) / SCAN_WARPS, 1, 1, 32 * SCAN_WARPS, 0, true, st));
   }
   const bool vec = (d_model * size) % 16 == 0 && vec_ok(x, ld, size) && vec_ok(x_sorted, sorted_ld, size);
   MOE_CK(size == 2 ? launch_dispatch<__nv_bfloat16>(q, vec, ctas, st) : launch_dispatch<float>(q, vec, ctas, st));

@@ -16,10 +16,13 @@ namespace {
 
 constexpr int NORM_MAX_D = 32768;          // 32 warps x 32 elements a thread
 constexpr int BACKWARD_ROWS = 2;            // a group's rows, at least
+constexpr int FORWARD_THREADS = 1024;      // threads an SM may hold of the forward kernel
 constexpr int BACKWARD_THREADS = 512;       // threads an SM holds of the backward kernel (128 registers each)
-// Rows of a group in flight in the backward pass, of N 16-byte loads a thread and matrix: what 196 KB hold for 512 threads (16384 x
-// 3584 bf16: 2 stages 96 us, 3 stages 94, 4 stages 95).
+// Rows of a group in flight, of N 16-byte loads a thread and matrix: what 196 KB hold of the backward pass's three matrices for 512
+// threads (16384 x 3584 bf16: 2 stages 96 us, 3 stages 94, 4 stages 95).
 template <int N> constexpr int NORM_STAGES = N <= 2 ? 3 : N <= 8 ? 8 / N : 1;
+// The same of the forward pass's two.
+template <int N, int THREADS> constexpr int FORWARD_STAGES = THREADS <= 512 ? NORM_STAGES<N> : N <= 2 ? 3 : 1;
 constexpr int NORM_GROUP_THREADS = 256;    // groups of fewer threads share a CTA up to this
 
 struct NormArgs {
@@ -55,95 +58,6 @@ __device__ __forceinline__ void load_weight(const void* p, bool f32, int c, floa
   }
 }
 
-// W elements a load (16 bytes, or 1 element where rows or the width are not aligned for that), N loads a thread.
-template <typename T, int W, int N, bool RES>
-__global__ void __launch_bounds__(1024, 1) k_norm_forward(const NormArgs q) {
-  using P = Pack<T, W>;
-  constexpr bool AHEAD = N * W * (int)sizeof(T) <= 32;     // the next row in registers too
-  const int threads = 32 * q.warps, group = threadIdx.x / threads, t = threadIdx.x - group * threads;
-  const int groups = blockDim.x / threads;
-  const long long step = (long long)gridDim.x * groups;
-  const T* const x = static_cast<const T*>(q.x);
-  const T* const r = static_cast<const T*>(q.r);
-  int buf = 0;
-  P nx[N], nr[RES ? N : 1];
-  auto load = [&](long long row) {
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int c = (j * threads + t) * W;
-      if (c < q.d) {
-        nx[j] = *reinterpret_cast<const P*>(x + row * q.x_ld + c);
-        if (RES) nr[j] = *reinterpret_cast<const P*>(r + row * q.r_ld + c);
-      }
-    }
-  };
-  long long row = (long long)blockIdx.x * groups + group;
-  if (AHEAD && row < q.rows) load(row);
-  for (; row < q.rows; row += step) {
-    if (!AHEAD) load(row);
-    float z[N * W], s[1] = {0.f};
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int c = (j * threads + t) * W;
-      if (c < q.d) {
-        float v[W];
-        nx[j].get(v);
-        if (RES) {
-          float r[W];
-          P keep;
-          nr[j].get(r);
-#pragma unroll
-          for (int i = 0; i < W; ++i) v[i] += r[i];
-          keep.set(v);
-          keep.get(v);
-          *reinterpret_cast<P*>(static_cast<T*>(q.sum) + row * q.sum_ld + c) = keep;
-        }
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-          z[j * W + i] = v[i];
-          s[0] += v[i];
-        }
-      }
-    }
-    if (AHEAD && row + step < q.rows) load(row + step);
-    float mu = 0.f;
-    if (!q.rms) {
-      group_sum(s, q.warps, group, buf);
-      mu = s[0] / (float)q.d;
-    }
-    s[0] = 0.f;
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      if ((j * threads + t) * W < q.d) {
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-          z[j * W + i] -= mu;
-          s[0] = fmaf(z[j * W + i], z[j * W + i], s[0]);
-        }
-      }
-    group_sum(s, q.warps, group, buf);
-    const float rstd = 1.f / sqrtf(s[0] / (float)q.d + q.eps);
-    if (t == 0) {
-      if (q.mean != nullptr) q.mean[row] = mu;
-      if (q.rstd != nullptr) q.rstd[row] = rstd;
-    }
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int c = (j * threads + t) * W;
-      if (c < q.d) {
-        float w[W], b[W];
-        load_weight<W>(q.w, q.w_f32, c, 1.f, w);
-        load_weight<W>(q.b, q.w_f32, c, 0.f, b);
-        P out;
-#pragma unroll
-        for (int i = 0; i < W; ++i) w[i] = fmaf(z[j * W + i] * rstd, w[i], b[i]);
-        out.set(w);
-        *reinterpret_cast<P*>(static_cast<T*>(q.y) + row * q.y_ld + c) = out;
-      }
-    }
-  }
-}
-
 // The weights of the columns a thread owns, as pairs; columns past the end have weight 0.
 template <int W, int N>
 __device__ __forceinline__ void own_weights(const void* p, bool f32, int d, int threads, int t, float absent, F2 (&out)[N * W / 2]) {
@@ -160,6 +74,135 @@ __device__ __forceinline__ void own_weights(const void* p, bool f32, int d, int 
   }
 #pragma unroll
   for (int i = 0; i < N * W / 2; ++i) out[i] = f2(f[2 * i], f[2 * i + 1]);
+}
+
+// W elements a load (16 bytes, or 1 element where rows or the width are not aligned for that), N loads a thread and matrix.
+// Columns past the end read as zeros.  RING: the next rows travel through shared memory, each thread copying (cp.async) what it
+// will read itself, so that a wait is the thread's own and the rows in flight cost no registers.
+template <typename T, int W, int N, bool BIAS, bool RING, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1) k_norm_forward(const NormArgs q) {
+  using P = Pack<T, W>;
+  constexpr int E2 = N * W / 2, STAGES = FORWARD_STAGES<N, THREADS>;
+  constexpr bool OWN_W = THREADS <= 512 && N * W <= 16;                  // weights in registers, or loaded again for each use
+  extern __shared__ __align__(16) uint8_t ring[];
+  const int threads = 32 * q.warps, group = threadIdx.x / threads, t = threadIdx.x - group * threads;
+  const int groups = blockDim.x / threads;
+  const long long step = (long long)gridDim.x * groups;
+  const T* const x = static_cast<const T*>(q.x);
+  const T* const r = static_cast<const T*>(q.r);
+  int buf = 0, stage = 0;
+  F2 w[E2], b[BIAS ? E2 : 1];
+  if (OWN_W) {
+    own_weights<W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
+    if constexpr (BIAS) own_weights<W, N>(q.b, q.w_f32, q.d, threads, t, 0.f, b);
+  }
+  const int parts = r != nullptr ? 2 : 1, line = N * 16 * (int)blockDim.x;
+  const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring) + 16 * threadIdx.x;
+  auto issue = [&](int stage, long long row) {
+    if (row < q.rows) {
+      const T* const src[2] = {x + row * q.x_ld, r + row * q.r_ld};
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+        if (p < parts) {
+#pragma unroll
+          for (int j = 0; j < N; ++j) {
+            const int c = (j * threads + t) * W, at = c < q.d ? c : 0;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(mine + (stage * parts + p) * line + j * 16 * blockDim.x),
+                         "l"(src[p] + at), "r"(c < q.d ? 16 : 0)
+                         : "memory");
+          }
+        }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  const long long first = (long long)blockIdx.x * groups + group;
+  if constexpr (RING)
+    for (int s = 0; s < STAGES; ++s) issue(s, first + s * step);
+  for (long long row = first; row < q.rows; row += step) {
+    P px[N], pr[N];
+    if constexpr (RING) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+      const uint8_t* const at = ring + 16 * threadIdx.x + stage * parts * line;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        px[j] = *reinterpret_cast<const P*>(at + j * 16 * blockDim.x);
+        if (r != nullptr) pr[j] = *reinterpret_cast<const P*>(at + line + j * 16 * blockDim.x);
+      }
+      issue(stage, row + STAGES * step);
+      if (++stage == STAGES) stage = 0;
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int c = (j * threads + t) * W;
+        px[j] = pr[j] = P();
+        if (c < q.d) {
+          px[j] = *reinterpret_cast<const P*>(x + row * q.x_ld + c);
+          if (r != nullptr) pr[j] = *reinterpret_cast<const P*>(r + row * q.r_ld + c);
+        }
+      }
+    }
+    F2 z[E2];
+    to_pairs<P, W, N>(px, z);
+    if (r != nullptr) {
+      F2 v[E2];
+      to_pairs<P, W, N>(pr, v);
+#pragma unroll
+      for (int i = 0; i < E2; ++i) z[i] = add2(z[i], v[i]);
+      from_pairs<P, W, N>(z, px);
+      to_pairs<P, W, N>(px, z);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int c = (j * threads + t) * W;
+        if (c < q.d) *reinterpret_cast<P*>(static_cast<T*>(q.sum) + row * q.sum_ld + c) = px[j];
+      }
+    }
+    float s[1], lo, hi, mu = 0.f;
+    F2 acc = f2(0.f, 0.f);
+    if (!q.rms) {
+#pragma unroll
+      for (int i = 0; i < E2; ++i) acc = add2(acc, z[i]);
+      split(acc, lo, hi);
+      s[0] = lo + hi;
+      group_sum(s, q.warps, group, buf);
+      mu = s[0] / (float)q.d;
+      // around the mean; columns past the end stay zero
+      float f[N * W];
+#pragma unroll
+      for (int i = 0; i < E2; ++i) split(add2(z[i], f2(-mu, -mu)), f[2 * i], f[2 * i + 1]);
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if ((j * threads + t) * W >= q.d) {
+#pragma unroll
+          for (int i = 0; i < W; ++i) f[j * W + i] = 0.f;
+        }
+#pragma unroll
+      for (int i = 0; i < E2; ++i) z[i] = f2(f[2 * i], f[2 * i + 1]);
+    }
+    acc = f2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < E2; ++i) acc = fma2(z[i], z[i], acc);
+    split(acc, lo, hi);
+    s[0] = lo + hi;
+    group_sum(s, q.warps, group, buf);
+    const float rstd = 1.f / sqrtf(s[0] / (float)q.d + q.eps);
+    if (t == 0) {
+      if (q.mean != nullptr) q.mean[row] = mu;
+      if (q.rstd != nullptr) q.rstd[row] = rstd;
+    }
+    if (!OWN_W) {
+      own_weights<W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
+      if constexpr (BIAS) own_weights<W, N>(q.b, q.w_f32, q.d, threads, t, 0.f, b);
+    }
+    const F2 rs = f2(rstd, rstd);
+#pragma unroll
+    for (int i = 0; i < E2; ++i) z[i] = BIAS ? fma2(mul2(z[i], rs), w[i], b[BIAS ? i : 0]) : mul2(mul2(z[i], rs), w[i]);
+    from_pairs<P, W, N>(z, px);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int c = (j * threads + t) * W;
+      if (c < q.d) *reinterpret_cast<P*>(static_cast<T*>(q.y) + row * q.y_ld + c) = px[j];
+    }
+  }
 }
 
 // A thread keeps the columns it owns for all rows of its group, so their weights and their shares of dw and db stay in its
@@ -336,9 +379,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm_backward(const NormArgs q) 
   }
 }
 
-constexpr int REDUCE_WARPS = 16;
+constexpr int REDUCE_WARPS = 32;
 struct NormReduce { const float* part; int groups, d, wanted; float *dw, *db; };
-// Columns of the groups' shares added up: a lane takes a column, the warps take every 16th group.
+// Columns of the groups' shares added up: a lane takes a column, the warps take every 32nd group.
 __global__ void __launch_bounds__(32 * REDUCE_WARPS) k_norm_reduce(const NormReduce q) {
   __shared__ float sums[REDUCE_WARPS][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, which = blockIdx.y;
@@ -380,26 +423,39 @@ NormShape norm_shape(long long rows, int d, int per, int threads_sm, long long r
 
 // Elements a thread holds in the backward pass, and the groups that leave shares of dw and db.
 int backward_per(int d) { return d <= 16 * 512 ? 16 : 32; }
-NormShape backward_shape(long long rows, int d) { return norm_shape(rows, d, backward_per(d), BACKWARD_THREADS, BACKWARD_ROWS); }
+// Rows a group takes at least: a group's shares cost the second kernel as much as a few of its rows do here, more where rows are
+// read by elements.
+NormShape backward_shape(long long rows, int d, bool vec) {
+  return norm_shape(rows, d, backward_per(d), BACKWARD_THREADS, vec ? 2 * BACKWARD_ROWS : BACKWARD_ROWS);
+}
 
-template <typename T, int W, int N>
+template <typename T, int W, int N, bool BIAS, bool RING, int THREADS>
 cudaError_t forward_as(const NormArgs& a, cudaStream_t st) {
   NormArgs q = a;
-  const NormShape s = norm_shape(q.rows, q.d, N * W, 1024, 1);
+  const NormShape s = norm_shape(q.rows, q.d, N * W, RING ? FORWARD_THREADS : 1024, 1);
   q.warps = s.warps;
   const int threads = 32 * s.warps * s.groups_per_cta;
-  if (q.r != nullptr) k_norm_forward<T, W, N, true><<<s.ctas, threads, 0, st>>>(q);
-  else k_norm_forward<T, W, N, false><<<s.ctas, threads, 0, st>>>(q);
+  int smem = 0;
+  if constexpr (RING) {
+    constexpr int MOST = FORWARD_STAGES<N, THREADS> * 2 * N * 16 * THREADS;
+    static_assert(MOST <= 226 * 1024, "shared memory of an SM");
+    const cudaError_t e = allow_smem<k_norm_forward<T, W, N, BIAS, RING, THREADS>, MOST>();
+    if (e != cudaSuccess) return e;
+    smem = FORWARD_STAGES<N, THREADS> * (q.r != nullptr ? 2 : 1) * N * threads * 16;
+  }
+  k_norm_forward<T, W, N, BIAS, RING, THREADS><<<s.ctas, threads, smem, st>>>(q);
   return cudaGetLastError();
 }
-template <typename T>
+template <typename T, bool BIAS>
 cudaError_t forward_typed(const NormArgs& q, bool vec, cudaStream_t st) {
   constexpr int W = 16 / (int)sizeof(T);
-  if (!vec) return q.d <= 8 * 1024 ? forward_as<T, 1, 8>(q, st) : forward_as<T, 1, 32>(q, st);
-  // Few rows: one load a thread, so that a row's loads and sums are spread over most threads.
-  if (q.rows <= 2 * sm_count() && q.d <= W * 1024) return forward_as<T, W, 1>(q, st);
-  if (q.d <= 2 * W * 1024) return forward_as<T, W, 2>(q, st);
-  return forward_as<T, W, 32 / W>(q, st);
+  // Few rows: 8 elements a thread, so that a row's loads and sums are spread over most threads.
+  if (q.rows <= 2 * sm_count() && q.d <= 8 * 1024)
+    return vec ? forward_as<T, W, 8 / W, BIAS, false, 1024>(q, st) : forward_as<T, 1, 8, BIAS, false, 1024>(q, st);
+  if (q.d <= 16 * 512) return vec ? forward_as<T, W, 16 / W, BIAS, true, 512>(q, st) : forward_as<T, 1, 16, BIAS, false, 512>(q, st);
+  if (q.d <= 16 * 1024 && vec) return forward_as<T, W, 16 / W, BIAS, true, 1024>(q, st);
+  if (q.d <= 32 * 512) return forward_as<T, 1, 32, BIAS, false, 512>(q, st);
+  return vec ? forward_as<T, W, 32 / W, BIAS, false, 1024>(q, st) : forward_as<T, 1, 32, BIAS, false, 1024>(q, st);
 }
 
 template <typename T, int W, int N, bool BIAS, int THREADS>
@@ -448,12 +504,9 @@ bool rows_ok(const void* p, long long ld, const camera_norm_t* n) {
     }                           \
   } while (0)
 
-size_t norm_part_bytes(int64_t rows, int d) {
-  const NormShape s = backward_shape(rows, d);
-  return (size_t)s.ctas * s.groups_per_cta * 2 * d * 4;
-}
-// At least that, and no less for more rows, so that a workspace serves every smaller call: groups are what the rows ask for,
-// rounded up to whole CTAs, or as many as the GPU holds at one time.
+size_t norm_part_bytes(const NormShape& s, int d) { return (size_t)s.ctas * s.groups_per_cta * 2 * d * 4; }
+// At least that for any alignment, and no less for more rows, so that a workspace serves every smaller call: groups are what the rows
+// ask for, rounded up to whole CTAs, or as many as the GPU holds at one time.
 size_t norm_part_bound(int64_t rows, int d) {
   const int warps = (d + 32 * backward_per(d) - 1) / (32 * backward_per(d));
   const int64_t want = (rows + BACKWARD_ROWS - 1) / BACKWARD_ROWS + NORM_GROUP_THREADS / 32, most = (int64_t)sm_count() * (BACKWARD_THREADS / 32 / warps > 1 ? BACKWARD_THREADS / 32 / warps : 1);
@@ -484,7 +537,8 @@ extern "C" int camera_norm_forward(const camera_norm_t* n, const void* residual,
   const bool vec = (n->d * size) % 16 == 0 && vec_ok(q.x, q.x_ld, size) && vec_ok(q.r, q.r_ld, size) && vec_ok(q.sum, q.sum_ld, size) &&
                    vec_ok(q.y, q.y_ld, size) && vec_ok(q.w, 0, 1) && vec_ok(q.b, 0, 1);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  NORM_CK(size == 2 ? forward_typed<__nv_bfloat16>(q, vec, st) : forward_typed<float>(q, vec, st));
+  if (size == 2) NORM_CK(q.b != nullptr ? forward_typed<__nv_bfloat16, true>(q, vec, st) : forward_typed<__nv_bfloat16, false>(q, vec, st));
+  else NORM_CK(q.b != nullptr ? forward_typed<float, true>(q, vec, st) : forward_typed<float, false>(q, vec, st));
   return CAMERA_OK;
 }
 
@@ -508,8 +562,6 @@ extern "C" int camera_norm_backward(const camera_norm_t* n, const void* dy, int6
   if (n->n_rows > 0 && (!rows_ok(n->x, n->ld, n) || !rows_ok(dy, dy_ld, n) || (dx != nullptr && !rows_ok(dx, dx_ld, n)) ||
                         (d_sum != nullptr && !rows_ok(d_sum, d_sum_ld, n)) || rstd == nullptr || (mean == nullptr && !rms)))
     return CAMERA_ERR_INVALID_ARG;
-  if (want_w && (workspace == nullptr || workspace_bytes < norm_part_bytes(n->n_rows, n->d) || (reinterpret_cast<uintptr_t>(workspace) & 255)))
-    return CAMERA_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (n->n_rows == 0) {                         // sums over no row
     if (d_weight != nullptr) NORM_CK(cudaMemsetAsync(d_weight, 0, (size_t)4 * n->d, st));
@@ -526,7 +578,9 @@ extern "C" int camera_norm_backward(const camera_norm_t* n, const void* dy, int6
   const int size = n->dtype == CAMERA_BF16 ? 2 : 4;
   const bool vec = (n->d * size) % 16 == 0 && vec_ok(q.x, q.x_ld, size) && vec_ok(q.r, q.r_ld, size) && vec_ok(q.dy, q.dy_ld, size) &&
                    vec_ok(q.y, q.y_ld, size) && vec_ok(q.w, 0, 1);
-  const NormShape s = backward_shape(q.rows, q.d);
+  const NormShape s = backward_shape(q.rows, q.d, vec);
+  if (want_w && (workspace == nullptr || workspace_bytes < norm_part_bytes(s, q.d) || (reinterpret_cast<uintptr_t>(workspace) & 255)))
+    return CAMERA_ERR_WORKSPACE;
   if (size == 2) NORM_CK(q.want_b ? backward_typed<__nv_bfloat16, true>(q, s, vec, st) : backward_typed<__nv_bfloat16, false>(q, s, vec, st));
   else NORM_CK(q.want_b ? backward_typed<float, true>(q, s, vec, st) : backward_typed<float, false>(q, s, vec, st));
   if (want_w) {

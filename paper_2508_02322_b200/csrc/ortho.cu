@@ -24,6 +24,7 @@
 
 #include "common.cuh"
 #include "launch.cuh"
+#include "rowgroup.cuh"
 #include "umma.cuh"
 #include "umma_pair.cuh"
 
@@ -40,6 +41,7 @@ constexpr int O_MAX_STAGES = 8;
 constexpr int O_RING_BYTES = 144 * 1024;
 constexpr int O_CHUNK = 32;                   // columns an epilogue warp handles at a time,
 constexpr int O_BUFS = 4;                    // and the chunks of 32 rows x 64 bytes it has in shared memory
+constexpr int O_AHEAD = 2;                   // boxes on their way before they are needed
 constexpr int O_BUF_BYTES = 32 * O_CHUNK * 2;
 constexpr int O_EPI_BYTES = O_EPI_WARPS * O_BUFS * O_BUF_BYTES;
 constexpr int O_REST_BYTES = O_EPI_WARPS * 256 * 4;      // POLY: the rests of the columns each epilogue warp works on
@@ -340,7 +342,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
       };
       if (lane == 0) {
 #pragma unroll
-        for (int k = 0; k < O_BUFS - 1; ++k) fetch(c_first + O_CHUNK * k, n + k);
+        for (int k = 0; k < O_AHEAD; ++k) fetch(c_first + O_CHUNK * k, n + k);
       }
       if (MODE == ORTHO_POLY) {
         __syncwarp();
@@ -358,9 +360,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
         float v[16];
         uint4* const piece0 = reinterpret_cast<uint4*>(box_row + (((2 * k) ^ swz) << 4));
         uint4* const piece1 = reinterpret_cast<uint4*>(box_row + (((2 * k + 1) ^ swz) << 4));
+        const F2 f_2 = f2(f, f);
         if (MODE == ORTHO_GRAM) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(raw[j]) * f;
+          for (int j = 0; j < 16; j += 2) split(mul2(f2(__uint_as_float(raw[j]), __uint_as_float(raw[j + 1])), f_2), v[j], v[j + 1]);
         } else {
           uint32_t a[8];
           *reinterpret_cast<uint4*>(a) = *piece0;
@@ -368,14 +371,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
 #pragma unroll
           for (int j = 0; j < 16; j += 2) {
             const float2 old = __half22float2(*reinterpret_cast<const __half2*>(&a[j >> 1]));
+            const F2 old2 = f2(old.x, old.y), sum = f2(__uint_as_float(raw[j]), __uint_as_float(raw[j + 1]));
             if (MODE == ORTHO_APPLY) {                  // (B + rest) X
-              v[j] = fmaf(rest, old.x, __uint_as_float(raw[j])) * f;
-              v[j + 1] = fmaf(rest, old.y, __uint_as_float(raw[j + 1])) * f;
-            } else {                                    // (A + rest)^2 up to the square of the rest, and b (A + rest)
+              split(mul2(fma2(f2(rest, rest), old2, sum), f_2), v[j], v[j + 1]);
+            } else {                                    // (A + rest)^2 up to the square of the rest, and b A (b rest: below)
               const float2 down = *reinterpret_cast<const float2*>(rests + c - c_first + j);
-              const float x = u.n0 + c + j == row ? rest : 0.f, y = u.n0 + c + j + 1 == row ? rest : 0.f;
-              v[j] = fmaf(old.x + x, q.f_aux, fmaf(rest + down.x, old.x, __uint_as_float(raw[j])) * f);
-              v[j + 1] = fmaf(old.y + y, q.f_aux, fmaf(rest + down.y, old.y, __uint_as_float(raw[j + 1])) * f);
+              split(fma2(old2, f2(q.f_aux, q.f_aux), mul2(fma2(add2(f2(rest, rest), f2(down.x, down.y)), old2, sum), f_2)), v[j], v[j + 1]);
             }
           }
         }
@@ -406,7 +407,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
 #pragma unroll
           for (int j = 0; j < 16; ++j)
             if (u.n0 + c + j == row) {
-              v[j] += MODE == ORTHO_POLY ? q.f_diag : 0.f;
+              if (MODE == ORTHO_POLY) v[j] += fmaf(rest, q.f_aux, q.f_diag);
               q.rest_out[mat.row0 + row] = v[j] - __half2float(__float2half_rn(v[j]));
             }
         }
@@ -441,9 +442,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
                          "r"(buf0 + box * O_BUF_BYTES), "r"(u.n0 + c), "r"(mat.row0 + warp_row)
                          : "memory");
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");      // the box before has been read: its buffer is free
+            // the next box to fetch, or (GRAM) to write, takes the room of one whose store has read it by now
+            asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(MODE == ORTHO_GRAM ? O_BUFS - 1 : O_BUFS - O_AHEAD) : "memory");
           }
-          fetch(c + (O_BUFS - 1) * O_CHUNK, n + O_BUFS - 1);
+          fetch(c + O_AHEAD * O_CHUNK, n + O_AHEAD);
         }
         __syncwarp();
       }
@@ -496,30 +498,64 @@ __device__ __forceinline__ double block_sum(double v) {
   return v;
 }
 
-// Sums of squares of runs of rows; eight at a time in fp32 (added in double), in double where that could overflow or vanish.
+// Whether the matrix's rows all start on 16-byte boundaries.
 template <typename T>
-__global__ void __launch_bounds__(LOAD_THREADS) k_ortho_norm(const __grid_constant__ OrthoLoad q) {
+__device__ __forceinline__ bool rows_aligned(const OrthoMat& mat) {
+  return ((reinterpret_cast<uintptr_t>(mat.in) | (uintptr_t)(mat.in_ld * (long long)sizeof(T))) & 15) == 0;
+}
+// Eight squares, in fp32 (added up in double) or in double where fp32 might overflow or lose them.
+__device__ __forceinline__ double squares(const float (&v)[8]) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s = fmaf(v[i], v[i], s);
+  if (s > 1e-20f && s < 1e30f) return (double)s;
+  double d = 0.0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) d = fma((double)v[i], (double)v[i], d);
+  return d;
+}
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&v)[8]) {          // 16-byte aligned
+  constexpr int N = Vec16<T>::N;
+#pragma unroll
+  for (int i = 0; i < 8; i += N) Vec16<T>::load(p + i, v + i);
+}
+
+// Sums of squares of the rows each warp takes.
+template <typename T>
+__global__ void __launch_bounds__(LOAD_THREADS, 6) k_ortho_norm(const __grid_constant__ OrthoLoad q) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (q.clear_status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) q.totals->status = 0;
   const OrthoMat& mat = q.batch.mat[blockIdx.y];
-  const int rows = mat.turned ? mat.n : mat.m, cols = mat.turned ? mat.m : mat.n;
+  const int rows = mat.turned ? mat.n : mat.m, cols = mat.turned ? mat.m : mat.n, lane = threadIdx.x & 31;
   const T* const in = static_cast<const T*>(mat.in);
+  const bool vec = rows_aligned<T>(mat);
   double sum = 0.0;
   for (int r = blockIdx.x * (LOAD_THREADS / 32) + (threadIdx.x >> 5); r < rows; r += gridDim.x * (LOAD_THREADS / 32)) {
     const T* const p = in + r * mat.in_ld;
-    for (int c = threadIdx.x & 31; c < cols; c += 256) {
-      float v[8], s = 0.f;
+    int done = 0;
+    if (vec) {
+      done = cols & ~7;
+      for (int c = 8 * lane; c < done; c += 1024) {
+        float v[4][8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (c + 256 * k < done) {
+            load8(p + c + 256 * k, v[k]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[k][i] = 0.f;
+          }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum += squares(v[k]);
+      }
+    }
+    for (int c = done + lane; c < cols; c += 256) {
+      float v[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = c + 32 * i < cols ? to_f32(p[c + 32 * i]) : 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s = fmaf(v[i], v[i], s);
-      if (s > 1e-20f && s < 1e30f) {
-        sum += (double)s;
-      } else {                          // squares that fp32 may not hold
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fma((double)v[i], (double)v[i], sum);
-      }
+      sum += squares(v);
     }
   }
   const double s = block_sum(sum);
@@ -529,53 +565,76 @@ __global__ void __launch_bounds__(LOAD_THREADS) k_ortho_norm(const __grid_consta
 // X = U 2^p in fp16, shorter side as rows, zeros around it.  p puts 2^p |U| into [2^14, 2^15): nothing overflows, and what
 // is below 2^-39 of the norm is lost.  A CTA turns tiles of 64 x 64 in shared memory.
 template <typename T>
-__global__ void __launch_bounds__(LOAD_THREADS) k_ortho_load(const __grid_constant__ OrthoLoad q) {
+__global__ void __launch_bounds__(LOAD_THREADS, 6) k_ortho_load(const __grid_constant__ OrthoLoad q) {
   __shared__ __align__(16) __half tile[64][72];
+  __shared__ int power;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const OrthoMat& mat = q.batch.mat[blockIdx.y];
   double s = 0.0;
   for (int i = threadIdx.x; i < q.parts; i += LOAD_THREADS) s += q.part[blockIdx.y * q.parts + i];
-  const double norm = sqrt(block_sum(s));
-  int p = 0;
-  if (norm > 0.0 && norm < 1e300) {
-    int e;
-    frexp(norm, &e);                    // norm in [2^(e-1), 2^e)
-    p = 15 - e;
+  s = block_sum(s);
+  if (threadIdx.x == 0) {
+    const double norm = sqrt(s);
+    int p = 0;
+    if (norm > 0.0 && norm < 1e300) {
+      int e;
+      frexp(norm, &e);                    // norm in [2^(e-1), 2^e)
+      p = 15 - e;
+    }
+    power = p;
+    if (blockIdx.x == 0) {
+      const double all = norm + (double)q.eps;
+      q.first[blockIdx.y] = norm == 0.0 ? 1.f : norm < 1e300 ? (float)fmin(ldexp(all, p), 1e38) : __int_as_float(0x7fffffff);
+      int e = 1;
+      if (norm > 0.0 && norm < 1e300) frexp(all / norm, &e);       // all / norm in [2^(e-1), 2^e)
+      q.small[blockIdx.y] = min(e - 1, 100);
+    }
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    const double all = norm + (double)q.eps;
-    q.first[blockIdx.y] = norm == 0.0 ? 1.f : norm < 1e300 ? (float)fmin(ldexp(all, p), 1e38) : __int_as_float(0x7fffffff);
-    int e = 1;
-    if (norm > 0.0 && norm < 1e300) frexp(all / norm, &e);       // all / norm in [2^(e-1), 2^e)
-    q.small[blockIdx.y] = min(e - 1, 100);
-  }
+  __syncthreads();
+  const int p = power;
   const float up = scalbnf(1.f, p / 2), up2 = scalbnf(1.f, p - p / 2);
   const int rt = pad_rows(mat.m) / 64, ct = pad_cols(mat.n) / 64;
   const T* const in = static_cast<const T*>(mat.in);
+  const bool vec = rows_aligned<T>(mat);
   for (int t = blockIdx.x; t < rt * ct; t += gridDim.x) {
     const int r0 = t / ct * 64, c0 = t % ct * 64;
-    __syncthreads();
     const int a0 = mat.turned ? c0 : r0, b0 = mat.turned ? r0 : c0;         // in the caller's rows and columns
     const int a_end = mat.turned ? mat.n : mat.m, b_end = mat.turned ? mat.m : mat.n;
-    float v[16];
+    // two runs of 8 elements a thread
+    float v[2][8];
+    const int b = (threadIdx.x & 7) * 8;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int k = threadIdx.x + LOAD_THREADS * i, a = k >> 6, b = k & 63;
-      v[i] = a0 + a < a_end && b0 + b < b_end ? to_f32(in[(a0 + a) * mat.in_ld + b0 + b]) : 0.f;
-    }
+    for (int k = 0; k < 2; ++k) {
+      const int a = (threadIdx.x >> 3) + 32 * k;
+      const T* const from = in + (a0 + a) * mat.in_ld + b0 + b;
+      if (vec && a0 + a < a_end && b0 + b + 8 <= b_end) {
+        load8(from, v[k]);
+      } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int k = threadIdx.x + LOAD_THREADS * i, a = k >> 6, b = k & 63;
-      const __half h = __float2half_rn(v[i] * up * up2);
-      if (mat.turned) tile[b][a] = h; else tile[a][b] = h;
+        for (int i = 0; i < 8; ++i) v[k][i] = a0 + a < a_end && b0 + b + i < b_end ? to_f32(from[i]) : 0.f;
+      }
     }
     __syncthreads();
-    const int r = threadIdx.x >> 2, part = (threadIdx.x & 3) * 16;
-    uint32_t w[8];
-    *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(&tile[r][part]);
-    *reinterpret_cast<uint4*>(w + 4) = *reinterpret_cast<const uint4*>(&tile[r][part + 8]);
-    st_global_v8(q.x + (long long)(mat.row0 + r0 + r) * q.x_ld + c0 + part, w);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int a = (threadIdx.x >> 3) + 32 * k;
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = pack_half(v[k][2 * i] * up * up2, v[k][2 * i + 1] * up * up2);
+      if (mat.turned) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) tile[b + i][a] = __ushort_as_half((unsigned short)(i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu));
+      } else {
+        *reinterpret_cast<uint4*>(&tile[a][b]) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int r = (threadIdx.x >> 3) + 32 * k;
+      *reinterpret_cast<uint4*>(q.x + (long long)(mat.row0 + r0 + r) * q.x_ld + c0 + b) = *reinterpret_cast<const uint4*>(&tile[r][b]);
+    }
   }
 }
 
@@ -772,7 +831,7 @@ int run_round(const camera_matrix_t* mats, const OrthoRound& r, int32_t dtype, c
   float* const rest_a = reinterpret_cast<float*>(ws + l.rest_a);
   float* const rest_b = reinterpret_cast<float*>(ws + l.rest_b);
   ld.clear_status = first_round;
-  ld.parts = 4 * sms / q.batch.n_mats;
+  ld.parts = 8 * sms / q.batch.n_mats;
   if (ld.parts > MAX_PARTS) ld.parts = MAX_PARTS;
   if (ld.parts < 8) ld.parts = 8;
   long long load_ctas = 8ll * sms / q.batch.n_mats + 1;
