@@ -24,23 +24,32 @@ _DTYPE = {torch.bfloat16: CAMERA_BF16, torch.float32: CAMERA_F32}
 def _matrix(t: torch.Tensor, name: str, like: Optional[torch.Tensor] = None, rows: Optional[int] = None,
             cols: Optional[int] = None) -> int:
     """Distance of the rows of a [rows, cols] matrix in elements; like: whose dtype and device it shares."""
-    if not (t.is_cuda and t.dim() == 2 and t.dtype in _DTYPE):
+    if like is not None:
+        if t.dtype is not like.dtype or t.get_device() != like.get_device():
+            raise ValueError(f"{name} must have the dtype and device of the other matrices of the call")
+    elif not t.is_cuda or t.dtype not in _DTYPE:
         raise ValueError(f"{name} must be a bf16 or fp32 matrix on the GPU")
-    if like is not None and (t.dtype is not like.dtype or t.device != like.device):
-        raise ValueError(f"{name} must have the dtype and device of the other matrices of the call")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix")
     r, c = t.shape
     if (rows is not None and r != rows) or (cols is not None and c != cols):
         raise ValueError(f"{name} must have the shape {(rows if rows is not None else r, cols if cols is not None else c)}")
     ld, one = t.stride()
-    if r <= 1 and ld < c:
-        ld = c
-    if (one != 1 and c > 1) or ld < c:
-        raise ValueError(f"{name} must have contiguous, non-overlapping rows")
+    if ld < c or one != 1:
+        if r <= 1 and ld < c:
+            ld = c
+        if (one != 1 and c > 1) or ld < c:
+            raise ValueError(f"{name} must have contiguous, non-overlapping rows")
     return ld
 
 
+def _result(like: torch.Tensor, rows: int, cols: int) -> Tuple[torch.Tensor, int]:
+    """A new matrix of the dtype and device of `like`, and the distance of its rows."""
+    return like.new_empty((rows, cols)), cols
+
+
 def _array(t: torch.Tensor, like: torch.Tensor, dtype, shape, name: str) -> int:
-    if t.dtype is not dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != like.device:
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != like.get_device():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on the device of the matrices")
     return t.data_ptr()
 
@@ -85,22 +94,24 @@ def camera_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, 
         return _elsewhere(stream, camera_norm_forward, x, weight, bias, residual=residual, eps=eps, rms=rms, stats=stats, out=out)
     n = _norm(x, weight, bias, eps, rms)
     rows, d = x.shape
-    res: Dict[str, torch.Tensor] = {}
-    place = {}
-    for name in ("y", "sum") if residual is not None else ("y",):
-        t = out.get(name) if out else None
-        res[name] = t = torch.empty((rows, d), dtype=x.dtype, device=x.device) if t is None else t
-        place[name] = (t.data_ptr(), _matrix(t, f"out[{name!r}]", x, rows, d))
-    r_ptr, r_ld = (residual.data_ptr(), _matrix(residual, "residual", x, rows, d)) if residual is not None else (None, 0)
-    m_ptr = s_ptr = None
+    y = out.get("y") if out else None
+    y, y_ld = _result(x, rows, d) if y is None else (y, _matrix(y, "out['y']", x, rows, d))
+    res: Dict[str, torch.Tensor] = {"y": y}
+    r_ptr = z_ptr = m_ptr = s_ptr = None
+    r_ld = z_ld = 0
+    if residual is not None:
+        r_ptr, r_ld = residual.data_ptr(), _matrix(residual, "residual", x, rows, d)
+        z = out.get("sum") if out else None
+        z, z_ld = _result(x, rows, d) if z is None else (z, _matrix(z, "out['sum']", x, rows, d))
+        z_ptr = z.data_ptr()
+        res["sum"] = z
     if stats:
         if not rms:
-            res["mean"] = t = torch.empty(rows, dtype=_F32, device=x.device)
+            res["mean"] = t = x.new_empty(rows, dtype=_F32)
             m_ptr = t.data_ptr()
-        res["rstd"] = t = torch.empty(rows, dtype=_F32, device=x.device)
+        res["rstd"] = t = x.new_empty(rows, dtype=_F32)
         s_ptr = t.data_ptr()
-    z_ptr, z_ld = place.get("sum", (None, 0))
-    _enqueue(lib.camera_norm_forward, x, C.byref(n), r_ptr, r_ld, z_ptr, z_ld, *place["y"], m_ptr, s_ptr)
+    _enqueue(lib.camera_norm_forward, x, C.byref(n), r_ptr, r_ld, z_ptr, z_ld, y.data_ptr(), y_ld, m_ptr, s_ptr)
     return res
 
 
@@ -132,13 +143,13 @@ def camera_norm_backward(dy: torch.Tensor, x: torch.Tensor, rstd: torch.Tensor, 
     res: Dict[str, torch.Tensor] = {}
     dx_ptr, dx_ld, w_ptr, b_ptr, ws_ptr, ws_n = None, 0, None, None, None, 0
     if want_x:
-        res["x"] = out = torch.empty((rows, d), dtype=x.dtype, device=x.device) if out is None else out
-        dx_ptr, dx_ld = out.data_ptr(), _matrix(out, "out", x, rows, d)
+        out, dx_ld = _result(x, rows, d) if out is None else (out, _matrix(out, "out", x, rows, d))
+        res["x"], dx_ptr = out, out.data_ptr()
     if want_weight:
-        res["weight"] = t = torch.empty(d, dtype=_F32, device=x.device)
+        res["weight"] = t = x.new_empty(d, dtype=_F32)
         w_ptr = t.data_ptr()
     if want_bias:
-        res["bias"] = t = torch.empty(d, dtype=_F32, device=x.device)
+        res["bias"] = t = x.new_empty(d, dtype=_F32)
         b_ptr = t.data_ptr()
     if want_weight or want_bias:
         workspace = _scratch(workspace, lambda: camera_norm_backward_workspace_bytes(rows, d), x.device)
@@ -150,7 +161,7 @@ def camera_norm_backward(dy: torch.Tensor, x: torch.Tensor, rstd: torch.Tensor, 
 
 # ------------------------------------------------------------------------------------------------ tokens to experts and back
 def _pairs(t: torch.Tensor, dtype, like: torch.Tensor, name: str) -> Tuple[int, int]:
-    if t.dtype is not dtype or t.dim() != 2 or t.shape[1] < 1 or not t.is_contiguous() or t.device != like.device:
+    if t.dtype is not dtype or t.dim() != 2 or t.shape[1] < 1 or not t.is_contiguous() or t.get_device() != like.get_device():
         raise ValueError(f"{name} must be a contiguous {dtype} [n_tokens, top_k] tensor on the device of the matrices")
     return t.shape
 
@@ -177,12 +188,13 @@ def camera_moe_dispatch(x: torch.Tensor, topk_idx: torch.Tensor, n_experts: int,
     if t != tokens:
         raise ValueError("topk_idx must have a row for each token")
     if out is None:
-        out = torch.empty((tokens * k, d), dtype=x.dtype, device=x.device)
-    elif out.dim() == 2 and out.shape[0] < tokens * k:
-        raise ValueError("out must have room for n_tokens * top_k rows")
-    out_ld = _matrix(out, "out", x, None, d)
-    rows = torch.empty((tokens, k), dtype=_I32, device=x.device)
-    offsets = torch.empty(max(int(n_experts), 0) + 1, dtype=_I32, device=x.device)
+        out, out_ld = _result(x, tokens * k, d)
+    else:
+        out_ld = _matrix(out, "out", x, None, d)
+        if out.shape[0] < tokens * k:
+            raise ValueError("out must have room for n_tokens * top_k rows")
+    rows = topk_idx.new_empty((tokens, k))
+    offsets = topk_idx.new_empty(max(int(n_experts), 0) + 1)
     workspace = _scratch(workspace, lambda: camera_moe_dispatch_workspace_bytes(tokens, k, n_experts), x.device)
     _enqueue(lib.camera_moe_dispatch, x, x.data_ptr(), _DTYPE[x.dtype], ld, tokens, d, topk_idx.data_ptr(), k, n_experts,
              out.data_ptr(), out_ld, rows.data_ptr(), offsets.data_ptr(), workspace.data_ptr(),
@@ -197,9 +209,7 @@ def _back(fn, sorted_rows, rows, topk_w, add, out):
     w = () if fn is lib.camera_moe_dispatch_backward else \
         (None if topk_w is None else _array(topk_w, sorted_rows, _F32, (tokens, k), "topk_w"),)
     a_ptr, a_ld = (None, 0) if add is None else (add.data_ptr(), _matrix(add, "add", sorted_rows, tokens, d))
-    if out is None:
-        out = torch.empty((tokens, d), dtype=sorted_rows.dtype, device=sorted_rows.device)
-    out_ld = _matrix(out, "out", sorted_rows, tokens, d)
+    out, out_ld = _result(sorted_rows, tokens, d) if out is None else (out, _matrix(out, "out", sorted_rows, tokens, d))
     _enqueue(fn, sorted_rows, sorted_rows.data_ptr(), _DTYPE[sorted_rows.dtype], ld, n, rows.data_ptr(), *w, tokens, k, d, a_ptr,
              a_ld, out.data_ptr(), out_ld)
     return out
@@ -245,10 +255,10 @@ def camera_moe_combine_backward(dy: torch.Tensor, y_sorted: torch.Tensor, rows: 
     res: Dict[str, torch.Tensor] = {}
     o_ptr, o_ld, dw_ptr = None, 0, None
     if want_y:
-        res["y"] = out = torch.empty((n, d), dtype=dy.dtype, device=dy.device) if out is None else out
-        o_ptr, o_ld = out.data_ptr(), _matrix(out, "out", dy, n, d)
+        out, o_ld = _result(dy, n, d) if out is None else (out, _matrix(out, "out", dy, n, d))
+        res["y"], o_ptr = out, out.data_ptr()
     if want_weights:
-        res["weights"] = w = torch.empty((tokens, k), dtype=_F32, device=dy.device)
+        res["weights"] = w = dy.new_empty((tokens, k), dtype=_F32)
         dw_ptr = w.data_ptr()
     _enqueue(lib.camera_moe_combine_backward, dy, dy.data_ptr(), _DTYPE[dy.dtype], ld, tokens, d, rows.data_ptr(), w_ptr, k,
              y_sorted.data_ptr(), ys_ld, n, o_ptr, o_ld, dw_ptr)
