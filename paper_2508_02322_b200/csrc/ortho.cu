@@ -22,6 +22,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <atomic>
+
 #include "common.cuh"
 #include "launch.cuh"
 #include "rowgroup.cuh"
@@ -51,6 +53,7 @@ constexpr int O_TMEM_COLS = 512;
 constexpr int O_MAX_MATS = 64;               // matrices of one round of launches
 constexpr long long O_MAX_ELEMS = 1ll << 27; // and the elements of X that close a round
 constexpr int O_MAX_SIDE = 1 << 17;
+constexpr int O_MAX_STEPS = 64;
 
 enum { ORTHO_GRAM = 0, ORTHO_POLY = 1, ORTHO_APPLY = 2 };
 
@@ -68,55 +71,70 @@ struct OrthoBatch {
   OrthoMat mat[O_MAX_MATS];
 };
 
-struct OrthoGemm {
-  CUtensorMap a, b;
-  CUtensorMap aux_map, out_map;          // in boxes of 32 rows x O_CHUNK columns: aux, out
+// Factors of one step (see the top of the file): of the sums of GRAM, POLY and APPLY, of A and on the diagonal in POLY; and what the
+// steps so far can have made of a small matrix (see scale_of), before and after this one.
+struct OrthoStep {
+  float f_gram, f_poly, f_aux, f_diag, f_apply;
+  int small_in, small_out;
+};
+
+// A packed buffer's tensor maps: as an operand in boxes of 64 columns x 128 or 64 rows, and in the epilogue's boxes.
+struct OrthoMaps { CUtensorMap rows128, rows64, box; };
+enum { BUF_X0 = 0, BUF_X1 = 1, BUF_A = 2, BUF_B = 3 };
+
+struct OrthoRun {
+  OrthoMaps maps[4];
   OrthoBatch batch;
-  int unit0[O_MAX_MATS + 1];
-  int n_units;
+  int unit0[3][O_MAX_MATS + 1];          // per product: first unit of each matrix
+  int per_step, n_units, n_steps;        // units of one step; of all steps
   int bn, nb, kps, n_stages, n_acc;      // columns per B tile, B tiles per unit, k blocks per stage, ring depth, accumulators
-  __half* out;              // packed result, or null: the caller's matrices
+  OrthoStep step[O_MAX_STEPS];
+  __half* out[2];                        // A and B
   long long out_ld;
-  const float* rest_in;     // [rows] what the rounding of the diagonal of A (POLY) or B (APPLY) left
-  float* rest_out;          // GRAM, POLY: the same of the result
-  float f_acc, f_aux, f_diag;
-  const float* first;       // factor of each matrix's first X, or null
-  const int* small;         // exponents by which matrices are smaller than the bounds (see scale_of), those of this step's X
-  int small_in, small_out;  // and of the next count from here on
+  float* rest[2];                        // [rows] what the rounding of the diagonals of A and B left
+  const float* first;                    // factor of each matrix's first X
+  const int* small;                      // exponents by which matrices are smaller than the bounds
+  int* done;                             // [mats] warps that have finished with a unit of this matrix
   PlanTotals* totals;
   unsigned long long wait_limit_ns;
 };
 
-static_assert(sizeof(OrthoGemm) <= 4096, "kernel arguments");
+static_assert(sizeof(OrthoRun) <= 16384, "kernel arguments");
 
 __host__ __device__ __forceinline__ int pad_rows(int m) { return (m + O_TILE_M - 1) / O_TILE_M * O_TILE_M; }
 __host__ __device__ __forceinline__ int pad_cols(int n) { return (n + UMMA_BK - 1) / UMMA_BK * UMMA_BK; }
-
-// Units of one matrix: symmetric products take, per row tile of 256, the column tiles from the diagonal on; the others all.
-template <int MODE>
-__host__ __device__ __forceinline__ int units_of(int m, int n, int w) {
-  const int rt = pad_rows(m) / O_TILE_M;
-  if (MODE == ORTHO_APPLY) return rt * ((n + w - 1) / w);
-  int units = 0;
-  for (int i = 0; i < rt; ++i) units += ((rt - i) * O_TILE_M + w - 1) / w;
-  return units;
-}
 
 // A matrix whose norm is far below eps starts with singular values of 2^-small at most, where small = log2((|U| + eps) / |U|), and
 // would be lost in fp16 at the others' factors.  A step makes them larger by no more than the largest value of its polynomial, so
 // X keeps 2^(small - what the steps so far can have added) as a further factor, as long as that is above 1.
 __device__ __forceinline__ int scale_of(int small, int used) { return max(0, small - used); }
 
-struct OrthoUnit { int e, m0, n0, two, kb, limit; };
+// need: how many warps must have finished with this matrix before the unit's operands are there.
+struct OrthoUnit { int step, mode, e, m0, n0, two, kb, limit, need; };
 
-template <int MODE>
-__device__ __forceinline__ OrthoUnit ortho_unit(const OrthoGemm& q, int unit) {
+// All steps' units in one row: step by step, in a step GRAM, POLY and APPLY, in each matrix by matrix.  A unit needs what the
+// products before its own have made of its matrix, all of which lies before it in the row; so as long as CTAs take their units in
+// order (and run at one time), somebody can always go on.
+__device__ __forceinline__ OrthoUnit ortho_unit(const OrthoRun& q, int unit) {
   OrthoUnit r;
-  r.e = upper_segment(q.unit0, q.batch.n_mats, unit);
-  int rem = unit - q.unit0[r.e];
+  const int mats = q.batch.n_mats;
+  r.step = unit / q.per_step;
+  int rem = unit - r.step * q.per_step;
+  r.mode = ORTHO_GRAM;
+  while (r.mode < ORTHO_APPLY && rem >= q.unit0[r.mode][mats]) rem -= q.unit0[r.mode++][mats];
+  r.e = upper_segment(q.unit0[r.mode], mats, rem);
+  rem -= q.unit0[r.mode][r.e];
+  int before = 0, whole = 0;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const int u = q.unit0[k][r.e + 1] - q.unit0[k][r.e];
+    whole += u;
+    before += k < r.mode ? u : 0;
+  }
+  r.need = (r.step * whole + before) * 2 * O_EPI_WARPS;
   const int m = q.batch.mat[r.e].m, n = q.batch.mat[r.e].n, w = q.nb * q.bn;
   const int rt = pad_rows(m) / O_TILE_M;
-  if (MODE == ORTHO_APPLY) {
+  if (r.mode == ORTHO_APPLY) {
     // row tiles in groups of O_GROUP_M, the row tile fastest: what runs at one time shares few column tiles and rows of B
     const int ct = (n + w - 1) / w, per_group = O_GROUP_M * ct, grp = rem / per_group;
     rem -= grp * per_group;
@@ -135,10 +153,28 @@ __device__ __forceinline__ OrthoUnit ortho_unit(const OrthoGemm& q, int unit) {
     r.m0 = i * O_TILE_M;
     r.n0 = r.m0 + rem * w;
     r.limit = rt * O_TILE_M;
-    r.kb = pad_cols(MODE == ORTHO_GRAM ? n : m) / UMMA_BK;
+    r.kb = pad_cols(r.mode == ORTHO_GRAM ? n : m) / UMMA_BK;
   }
   r.two = q.nb == 2 && r.n0 + q.bn < r.limit;
   return r;
+}
+
+// Waits (one lane) until `need` warps have finished with a matrix, then lets the asynchronous proxy see what they wrote.
+__device__ __forceinline__ bool wait_done(const int* done, int need, volatile int* abort_flag) {
+  unsigned long long t0 = 0;
+  for (unsigned spins = 0;; ++spins) {
+    int v;
+    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(done) : "memory");
+    if (v >= need) break;
+    if (spins == 0) t0 = globaltimer_ns();
+    if ((spins & 15u) == 15u) {
+      if (*abort_flag) return false;
+      if (globaltimer_ns() - t0 > wait_limit_ns(abort_flag)) { *abort_flag = 1; return false; }
+    }
+    __nanosleep(64);
+  }
+  asm volatile("fence.proxy.async;" ::: "memory");
+  return true;
 }
 
 __device__ __forceinline__ uint32_t pack_half(float a, float b) {
@@ -170,9 +206,11 @@ __device__ __forceinline__ void store_turned(uint16_t* at, long long ld, const u
   }
 }
 
-template <int MODE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_ortho_gemm(const __grid_constant__ OrthoGemm q) {
-  constexpr bool B_MN = MODE == ORTHO_APPLY;
+template <int M> struct Mode { static constexpr int value = M; };
+
+// All products of all steps in one launch: CTAs stay, and a unit starts when the units it depends on have been reported finished (a
+// counter per matrix).  With a launch per product (15 of them) 7 matrices of 53 x 62 took 96 us and 94 us of the host's time.
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_ortho(const __grid_constant__ OrthoRun q) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* const base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -213,8 +251,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
   cluster_sync_all();     // the other CTA's barriers are initialised before anything arrives on them
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
 
   if (warp == O_PRODUCER) {
     // ------------------------------------------------------------------ TMA producer (each CTA loads its own share)
@@ -223,10 +259,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
     uint32_t phase = 0;
     bool ok = true;
     for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
-      const OrthoUnit u = ortho_unit<MODE>(q, unit);
+      const OrthoUnit u = ortho_unit(q, unit);
       const int row0 = q.batch.mat[u.e].row0;
       const int am = row0 + u.m0 + 128 * (int)rank, bn0 = u.n0 + half * (int)rank;
-      for (int kb = 0, blocks; kb < u.kb; kb += blocks) {
+      const bool B_MN = u.mode == ORTHO_APPLY;
+      const OrthoMaps& from = q.maps[u.mode == ORTHO_GRAM ? u.step & 1 : u.mode == ORTHO_POLY ? BUF_A : BUF_B];
+      const CUtensorMap* const map_a = &from.rows128;
+      const CUtensorMap* const map_b = B_MN ? &q.maps[u.step & 1].rows64 : half > 64 ? &from.rows128 : &from.rows64;
+      ok = __all_sync(0xffffffffu, lane != 0 || wait_done(q.done + u.e, u.need, abort_flag));
+      for (int kb = 0, blocks; ok && kb < u.kb; kb += blocks) {
         blocks = min(q.kps, u.kb - kb);
         ok = warp_wait(empty_bar(stage), phase ^ 1u, abort_flag);
         if (!ok) break;
@@ -235,18 +276,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
         __syncwarp();
         uint32_t dst = base + stage * stage_bytes;
         for (int k0 = kb * UMMA_BK; k0 < (kb + blocks) * UMMA_BK; k0 += UMMA_BK, dst += block_bytes) {
-          tma_load_lead(lead, dst, &q.a, full0, k0, am);
+          tma_load_lead(lead, dst, map_a, full0, k0, am);
           const uint32_t dst_b = dst + O_A_BYTES;
           if (B_MN) {
-            tma_load_lead(lead, dst_b, &q.b, full0, bn0, row0 + k0);
-            if (half > 64) tma_load_lead(lead, dst_b + 8192, &q.b, full0, bn0 + 64, row0 + k0);
+            tma_load_lead(lead, dst_b, map_b, full0, bn0, row0 + k0);
+            if (half > 64) tma_load_lead(lead, dst_b + 8192, map_b, full0, bn0 + 64, row0 + k0);
             if (u.two) {
-              tma_load_lead(lead, dst_b + b_bytes, &q.b, full0, bn0 + q.bn, row0 + k0);
-              if (half > 64) tma_load_lead(lead, dst_b + b_bytes + 8192, &q.b, full0, bn0 + q.bn + 64, row0 + k0);
+              tma_load_lead(lead, dst_b + b_bytes, map_b, full0, bn0 + q.bn, row0 + k0);
+              if (half > 64) tma_load_lead(lead, dst_b + b_bytes + 8192, map_b, full0, bn0 + q.bn + 64, row0 + k0);
             }
           } else {
-            tma_load_lead(lead, dst_b, &q.b, full0, k0, row0 + bn0);
-            if (u.two) tma_load_lead(lead, dst_b + b_bytes, &q.b, full0, k0, row0 + bn0 + q.bn);
+            tma_load_lead(lead, dst_b, map_b, full0, k0, row0 + bn0);
+            if (u.two) tma_load_lead(lead, dst_b + b_bytes, map_b, full0, k0, row0 + bn0 + q.bn);
           }
         }
         if (++stage == q.n_stages) { stage = 0; phase ^= 1u; }
@@ -263,13 +304,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true, ready = false;       // ready: the next stage has been seen full
-      const uint32_t idesc = make_idesc_pair_f16(q.bn) | (B_MN ? 1u << 16 : 0u);
-      constexpr int A_STEP = 32 >> 4, B_STEP = B_MN ? 2048 >> 4 : 32 >> 4;     // 16 k further
+      constexpr int A_STEP = 32 >> 4;                                          // 16 k further
       const unsigned long long a_first = make_smem_desc(base);
-      const unsigned long long b_first = B_MN ? make_smem_desc_mn(base + O_A_BYTES) : make_smem_desc(base + O_A_BYTES);
       const unsigned long long b2_off = (unsigned long long)(b_bytes >> 4);
       for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
-        const OrthoUnit u = ortho_unit<MODE>(q, unit);
+        const OrthoUnit u = ortho_unit(q, unit);
+        const bool B_MN = u.mode == ORTHO_APPLY;
+        const uint32_t idesc = make_idesc_pair_f16(q.bn) | (B_MN ? 1u << 16 : 0u);
+        const unsigned long long b_first = B_MN ? make_smem_desc_mn(base + O_A_BYTES) : make_smem_desc(base + O_A_BYTES);
         ok = __all_sync(0xffffffffu, mbar_wait_cluster(tempty_bar(acc), acc_phase ^ 1u, abort_flag));
         if (!ok) break;
         tc_fence_after();
@@ -289,13 +331,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
             const unsigned long long a_desc = a_first + at, b_desc = b_first + at;
             if (u.two) {
               const unsigned long long b2_desc = b_desc + b2_off;
+              const int b_step = B_MN ? 2048 >> 4 : 32 >> 4;
 #pragma unroll
               for (int k = 0; k < UMMA_BK / 16; ++k) {
-                umma_lead(lead, d0, a_desc + A_STEP * k, b_desc + B_STEP * k, idesc, accumulate | (uint32_t)k);
-                umma_lead(lead, d1, a_desc + A_STEP * k, b2_desc + B_STEP * k, idesc, accumulate | (uint32_t)k);
+                umma_lead(lead, d0, a_desc + A_STEP * k, b_desc + b_step * k, idesc, accumulate | (uint32_t)k);
+                umma_lead(lead, d1, a_desc + A_STEP * k, b2_desc + b_step * k, idesc, accumulate | (uint32_t)k);
               }
+            } else if (B_MN) {
+              umma_block<A_STEP, (2048 >> 4)>(lead, d0, a_desc, b_desc, idesc, accumulate);
             } else {
-              umma_block<A_STEP, B_STEP>(lead, d0, a_desc, b_desc, idesc, accumulate);
+              umma_block<A_STEP, (32 >> 4)>(lead, d0, a_desc, b_desc, idesc, accumulate);
             }
             accumulate = 1;
           }
@@ -314,44 +359,49 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
     // each take a request per lane (16 matrices of up to 1408 x 2048: POLY 62 us, APPLY 122 us; without their reads 46 and
     // 91 us).  The result takes the place of what was read; three boxes are in flight ahead.
     int acc = 0;
-    uint32_t acc_phase = 0, n = 0;                           // n: boxes so far; buffer n % O_BUFS
+    uint32_t acc_phase = 0, n = 0, loads = 0;                // boxes so far, in buffer n % O_BUFS; those of them that were loaded
     bool ok = true;
     const int c_half = q.nb * q.bn / 2, c_first = c_half * (warp >> 2);
     uint8_t* const bufs = base_ptr + O_RING_BYTES + warp * O_BUFS * O_BUF_BYTES;
     [[maybe_unused]] float* const rests = reinterpret_cast<float*>(base_ptr + O_RING_BYTES + O_EPI_BYTES) + 256 * warp;
     const uint32_t buf0 = smem_u32(bufs), swz = (uint32_t)(lane >> 1) & 3u;       // 64-byte swizzle: 16-byte piece i of a row at i ^ swz
-    const bool to_caller = MODE == ORTHO_APPLY && q.out == nullptr;
-    for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
-      const OrthoUnit u = ortho_unit<MODE>(q, unit);
+    auto unit_done = [&](auto mode, const OrthoUnit& u) {           // false: a wait ran out
+      constexpr int MODE = decltype(mode)::value;
+      const OrthoStep& st = q.step[u.step];
+      const bool to_caller = MODE == ORTHO_APPLY && u.step + 1 == q.n_steps;
       const OrthoMat& mat = q.batch.mat[u.e];
       const int warp_row = u.m0 + 128 * (int)rank + (warp & 3) * 32, row = warp_row + lane;      // in the matrix, < pad_rows(m)
       const int cols = min(u.limit - u.n0, c_first + c_half);       // where this warp's columns end, a multiple of O_CHUNK
-      float f = q.f_acc;
+      const CUtensorMap* const aux_map = &q.maps[MODE == ORTHO_POLY ? BUF_A : u.step & 1].box;
+      const CUtensorMap* const out_map = &q.maps[MODE == ORTHO_GRAM ? BUF_A : MODE == ORTHO_POLY ? BUF_B : (u.step + 1) & 1].box;
+      __half* const out_rows = q.out[MODE == ORTHO_POLY];
+      float f = MODE == ORTHO_GRAM ? st.f_gram : MODE == ORTHO_POLY ? st.f_poly : st.f_apply;
       if (MODE != ORTHO_POLY) {
         const int small = q.small[u.e];
-        const float s = q.first != nullptr ? q.first[u.e] : scalbnf(1.f, scale_of(small, q.small_in));
-        f = MODE == ORTHO_GRAM ? f / s / s : scalbnf(f / s, q.out != nullptr ? scale_of(small, q.small_out) : 0);
+        const float s = u.step == 0 ? q.first[u.e] : scalbnf(1.f, scale_of(small, st.small_in));
+        f = MODE == ORTHO_GRAM ? f / s / s : scalbnf(f / s, to_caller ? 0 : scale_of(small, st.small_out));
       }
-      const float rest = MODE == ORTHO_GRAM ? 0.f : q.rest_in[mat.row0 + row];
-      auto fetch = [&](int c, uint32_t box) {                      // lane 0: the box at column c on its way
+      if (MODE != ORTHO_GRAM && !__all_sync(0xffffffffu, lane != 0 || wait_done(q.done + u.e, u.need, abort_flag))) return false;
+      const float* const rest_in = q.rest[MODE == ORTHO_APPLY] + mat.row0;
+      const float rest = MODE == ORTHO_GRAM ? 0.f : __ldcg(rest_in + row);
+      auto fetch = [&](int c, uint32_t k) {                        // lane 0: the k-th box from here, at column c, on its way
         if (MODE != ORTHO_GRAM && c < cols) {
-          const uint32_t bar = aux_bar(warp * O_BUFS + box % O_BUFS);
+          const uint32_t bar = aux_bar(warp * O_BUFS + (loads + k) % O_BUFS);
           mbar_expect_tx(bar, O_BUF_BYTES);
-          tma_load_2d(buf0 + box % O_BUFS * O_BUF_BYTES, &q.aux_map, bar, u.n0 + c, mat.row0 + warp_row);
+          tma_load_2d(buf0 + (n + k) % O_BUFS * O_BUF_BYTES, aux_map, bar, u.n0 + c, mat.row0 + warp_row);
         }
       };
       if (lane == 0) {
 #pragma unroll
-        for (int k = 0; k < O_AHEAD; ++k) fetch(c_first + O_CHUNK * k, n + k);
+        for (int k = 0; k < O_AHEAD; ++k) fetch(c_first + O_CHUNK * k, k);
       }
       if (MODE == ORTHO_POLY) {
         __syncwarp();
         for (int i = 4 * lane; c_first + i < cols; i += 128)
-          *reinterpret_cast<float4*>(rests + i) = *reinterpret_cast<const float4*>(q.rest_in + mat.row0 + u.n0 + c_first + i);
+          *reinterpret_cast<float4*>(rests + i) = __ldcg(reinterpret_cast<const float4*>(rest_in + u.n0 + c_first + i));
       }
       __syncwarp();
-      ok = __all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_phase, abort_flag));
-      if (!ok) break;
+      if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_phase, abort_flag))) return false;
       tc_fence_after();
       const uint32_t t0 = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(acc * q.nb * q.bn);
       uint8_t* box_row = bufs;                                      // this lane's row of the box at work
@@ -376,7 +426,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
               split(mul2(fma2(f2(rest, rest), old2, sum), f_2), v[j], v[j + 1]);
             } else {                                    // (A + rest)^2 up to the square of the rest, and b A (b rest: below)
               const float2 down = *reinterpret_cast<const float2*>(rests + c - c_first + j);
-              split(fma2(old2, f2(q.f_aux, q.f_aux), mul2(fma2(add2(f2(rest, rest), f2(down.x, down.y)), old2, sum), f_2)), v[j], v[j + 1]);
+              split(fma2(old2, f2(st.f_aux, st.f_aux), mul2(fma2(add2(f2(rest, rest), f2(down.x, down.y)), old2, sum), f_2)), v[j], v[j + 1]);
             }
           }
         }
@@ -407,8 +457,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
 #pragma unroll
           for (int j = 0; j < 16; ++j)
             if (u.n0 + c + j == row) {
-              if (MODE == ORTHO_POLY) v[j] += fmaf(rest, q.f_aux, q.f_diag);
-              q.rest_out[mat.row0 + row] = v[j] - __half2float(__float2half_rn(v[j]));
+              if (MODE == ORTHO_POLY) v[j] += fmaf(rest, st.f_aux, st.f_diag);
+              q.rest[MODE == ORTHO_POLY][mat.row0 + row] = v[j] - __half2float(__float2half_rn(v[j]));
             }
         }
 #pragma unroll
@@ -416,17 +466,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
         *piece0 = make_uint4(p[0], p[1], p[2], p[3]);
         *piece1 = make_uint4(p[4], p[5], p[6], p[7]);
         if (MODE != ORTHO_APPLY && u.n0 + c >= u.m0 + O_TILE_M)      // off the diagonal's block: the other half of the result
-          store_turned(reinterpret_cast<uint16_t*>(q.out) + (long long)(mat.row0 + u.n0 + c) * q.out_ld + warp_row, q.out_ld, p, lane, 32, 16,
+          store_turned(reinterpret_cast<uint16_t*>(out_rows) + (long long)(mat.row0 + u.n0 + c) * q.out_ld + warp_row, q.out_ld, p, lane, 32, 16,
                        true);
       };
       uint32_t v0[16], v1[16];
       if (c_first < cols) tmem_ld16(t0 + c_first, v0);
-      for (int c = c_first; c < cols; c += O_CHUNK, ++n) {
+      for (int c = c_first; c < cols; c += O_CHUNK, ++n, loads += MODE != ORTHO_GRAM) {
         const uint32_t box = n % O_BUFS;
         box_row = bufs + box * O_BUF_BYTES + lane * (2 * O_CHUNK);
         if (MODE != ORTHO_GRAM) {
-          ok = warp_wait(aux_bar(warp * O_BUFS + box), n / O_BUFS & 1u, abort_flag);
-          if (!ok) break;
+          if (!warp_wait(aux_bar(warp * O_BUFS + loads % O_BUFS), loads / O_BUFS & 1u, abort_flag)) return false;
         }
         tmem_ld_wait(v0);
         tmem_ld16(t0 + c + 16, v1);
@@ -438,23 +487,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
         __syncwarp();
         if (lane == 0) {
           if (!to_caller) {
-            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(&q.out_map),
+            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(out_map),
                          "r"(buf0 + box * O_BUF_BYTES), "r"(u.n0 + c), "r"(mat.row0 + warp_row)
                          : "memory");
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             // the next box to fetch, or (GRAM) to write, takes the room of one whose store has read it by now
             asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(MODE == ORTHO_GRAM ? O_BUFS - 1 : O_BUFS - O_AHEAD) : "memory");
           }
-          fetch(c + O_AHEAD * O_CHUNK, n + O_AHEAD);
+          fetch(c + O_AHEAD * O_CHUNK, O_AHEAD);
         }
         __syncwarp();
       }
-      if (!ok) break;
       tc_fence_before();
       mbar_arrive_cluster(map_to_cta(tempty_bar(acc), 0));
       if (++acc == q.n_acc) { acc = 0; acc_phase ^= 1u; }
+      // While the next unit's products run: what this warp wrote (boxes, mirrored words, rests) is there for everybody.
+      if (!to_caller) {
+        if (lane == 0) {
+          asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+          asm volatile("fence.proxy.async;" ::: "memory");
+        }
+        __threadfence();
+        __syncwarp();
+        if (lane == 0) asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(q.done + u.e) : "memory");
+      }
+      return true;
+    };
+    for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
+      const OrthoUnit u = ortho_unit(q, unit);
+      ok = u.mode == ORTHO_GRAM ? unit_done(Mode<ORTHO_GRAM>(), u) : u.mode == ORTHO_POLY ? unit_done(Mode<ORTHO_POLY>(), u) : unit_done(Mode<ORTHO_APPLY>(), u);
     }
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     if (!ok) {               // boxes on their way land before the CTA's shared memory is given up
       const unsigned long long t0 = globaltimer_ns();
       while (globaltimer_ns() - t0 < 2000000ull) __nanosleep(1000);
@@ -478,6 +540,7 @@ struct OrthoLoad {
   int parts;
   float* first;             // [mats] factor between X as stored and X
   int* small;               // [mats]
+  int* done;                // [mats], cleared here
   float eps;
   __half* x;
   long long x_ld;
@@ -527,6 +590,7 @@ __global__ void __launch_bounds__(LOAD_THREADS, 6) k_ortho_norm(const __grid_con
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (q.clear_status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) q.totals->status = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) q.done[blockIdx.y] = 0;
   const OrthoMat& mat = q.batch.mat[blockIdx.y];
   const int rows = mat.turned ? mat.n : mat.m, cols = mat.turned ? mat.m : mat.n, lane = threadIdx.x & 31;
   const T* const in = static_cast<const T*>(mat.in);
@@ -668,7 +732,7 @@ OrthoLayout ortho_layout(const OrthoRound& r) {
   OrthoLayout l;
   l.part = up256(sizeof(PlanTotals));
   l.first = l.part + up256((size_t)8 * O_MAX_MATS * MAX_PARTS);
-  l.rest_a = l.first + up256(8 * O_MAX_MATS);
+  l.rest_a = l.first + up256(12 * O_MAX_MATS);
   l.rest_b = l.rest_a + up256((size_t)4 * r.rows);
   l.x0 = l.rest_b + up256((size_t)4 * r.rows);
   const size_t x = up256((size_t)2 * r.rows * r.x_ld), a = up256((size_t)2 * r.rows * r.a_ld);
@@ -720,46 +784,63 @@ constexpr double MARGIN = 1.02;         // for the roundings, which the bounds l
 constexpr double MOST = 1e3;            // singular values beyond this: the polynomial is not one that converges
 double factor_for(double bound) { return ldexp(1.0, (int)floor(log2(65504.0 / fmax(bound * MARGIN, 1e-3)))); }
 
-// Tiles: the choice with the least estimated time, rounds of units over the pairs times a unit's time.  Per k block 0.60 us
-// for 512 columns, 0.43 for 256, 0.32 for 128 (measured in the feed-forward block's kernel, which feeds the pipe the same
-// way); a unit of 512 columns adds its epilogue, smaller ones have two accumulators and overlap it.
+// Units of one matrix: symmetric products take, per row tile of 256, the column tiles from the diagonal on; APPLY all.
+int units_of(int mode, const OrthoMat& t, int w) {
+  const int rt = pad_rows(t.m) / O_TILE_M;
+  if (mode == ORTHO_APPLY) return rt * ((t.n + w - 1) / w);
+  int units = 0;
+  for (int i = 0; i < rt; ++i) units += ((rt - i) * O_TILE_M + w - 1) / w;
+  return units;
+}
+
+// Tiles: the choice with the least estimated time of a step.  A k block takes 0.60 us for 512 columns, 0.43 for 256, 0.32 for 128:
+// all three are what bringing its operands from L2 takes (77 GB/s an SM), of which wide tiles need least.  A unit of 512 columns
+// adds its epilogue; smaller ones have two accumulators and overlap it.  A product's units spread over the pairs, those of a later
+// product of another matrix fill what they leave (but not where there is one matrix); and no product is over before its longest unit.
 struct OrthoTile { int bn, nb; };
-template <int MODE>
 OrthoTile choose_tile(const OrthoBatch& b, int n_pairs) {
   static constexpr OrthoTile kinds[3] = {{256, 2}, {256, 1}, {128, 1}};
-  static constexpr double k_block[3] = {0.60, 0.43, 0.32};
+  static constexpr double k_block[3] = {0.60, 0.43, 0.32}, epilogue[3] = {5.0, 1.0, 0.7};
   OrthoTile best = kinds[0];
   double best_cost = 1e300;
   for (int i = 0; i < 3; ++i) {
-    long long units = 0, blocks = 0, longest = 0;
-    for (int e = 0; e < b.n_mats; ++e) {
-      const int u = units_of<MODE>(b.mat[e].m, b.mat[e].n, kinds[i].bn * kinds[i].nb);
-      const int kb = pad_cols(MODE == ORTHO_GRAM ? b.mat[e].n : b.mat[e].m) / UMMA_BK;
-      units += u;
-      blocks += (long long)u * kb;
-      if (kb > longest) longest = kb;
+    double cost = 0.0;
+    for (int mode = 0; mode < 3; ++mode) {
+      double sum = 0.0, longest = 0.0;
+      for (int e = 0; e < b.n_mats; ++e) {
+        const int u = units_of(mode, b.mat[e], kinds[i].bn * kinds[i].nb);
+        const double one = pad_cols(mode == ORTHO_GRAM ? b.mat[e].n : b.mat[e].m) / UMMA_BK * k_block[i] + epilogue[i];
+        sum += b.n_mats > 1 ? u * one / n_pairs : (double)((u + n_pairs - 1) / n_pairs) * one;
+        longest = fmax(longest, one);
+      }
+      cost += fmax(sum, longest);
     }
-    const double mean = (double)blocks / units, rounds = (double)((units + n_pairs - 1) / n_pairs);
-    const double cost = (rounds > 1 ? rounds * mean : (double)longest) * k_block[i] + rounds * (i == 0 ? 4.0 : 1.0);
     if (cost < best_cost * 0.99) { best = kinds[i]; best_cost = cost; }
   }
   return best;
 }
 
-// A packed buffer [rows, cols] and the tensor maps that read or write it: as an operand in boxes of 64 columns x 128 or 64 rows,
-// and in the epilogue's boxes.  (fp16 and bf16 differ in nothing a copy without arithmetic sees.)
-struct Packed {
-  __half* p;
-  long long ld;
-  CUtensorMap rows128, rows64, box;
-  bool encode(void* at, long long rows, long long cols) {
-    p = static_cast<__half*>(at);
-    ld = cols;
-    return encode_bf16_2d_pitch(&rows128, p, (uint64_t)rows, (uint64_t)cols, (uint64_t)cols, 128) &&
-           encode_bf16_2d_pitch(&rows64, p, (uint64_t)rows, (uint64_t)cols, (uint64_t)cols, 64) &&
-           encode_bf16_2d_narrow(&box, p, (uint64_t)rows, (uint64_t)cols, (uint64_t)cols, 32);
-  }
-};
+// (fp16 and bf16 differ in nothing a copy without arithmetic sees.)
+bool encode(OrthoMaps* m, const void* p, long long rows, long long cols) {
+  return encode_bf16_2d_pitch(&m->rows128, p, (uint64_t)rows, (uint64_t)cols, (uint64_t)cols, 128) &&
+         encode_bf16_2d_pitch(&m->rows64, p, (uint64_t)rows, (uint64_t)cols, (uint64_t)cols, 64) &&
+         encode_bf16_2d_narrow(&m->box, p, (uint64_t)rows, (uint64_t)cols, (uint64_t)cols, 32);
+}
+
+// Pairs of CTAs that run at one time, asked of the driver once per device.
+int pairs_at_once() {
+  static std::atomic<int> known[KNOWN_DEVICES];
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return 1; }
+  if (dev < KNOWN_DEVICES && (n = known[dev].load(std::memory_order_relaxed)) != 0) return n;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(sm_count() & ~1));
+  cfg.blockDim = dim3(O_THREADS);
+  cfg.dynamicSmemBytes = O_SMEM_BYTES;
+  if (cudaOccupancyMaxActiveClusters(&n, k_ortho, &cfg) != cudaSuccess || n < 1) { cudaGetLastError(); return 1; }
+  if (dev < KNOWN_DEVICES) known[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
 
 #define ORTHO_CK(...)             \
   do {                            \
@@ -769,37 +850,10 @@ struct Packed {
     }                             \
   } while (0)
 
-// B of APPLY is read with its columns as N.  aux: A or X, in out's columns, or null; out null: the caller's matrices.
-template <int MODE>
-int launch_ortho(OrthoGemm& q, const Packed& a, const Packed& b, const Packed* aux, const Packed* out, int n_pairs, cudaStream_t st) {
-  const OrthoTile t = choose_tile<MODE>(q.batch, n_pairs);
-  q.bn = t.bn; q.nb = t.nb;
-  q.n_acc = t.nb * t.bn <= 256 ? 2 : 1;
-  q.kps = t.nb * t.bn <= 256 ? 2 : 1;
-  const int stage = q.kps * (O_A_BYTES + t.nb * t.bn * 64);
-  q.n_stages = O_RING_BYTES / stage < O_MAX_STAGES ? O_RING_BYTES / stage : O_MAX_STAGES;
-  int units = 0;
-  for (int e = 0; e < q.batch.n_mats; ++e) {
-    q.unit0[e] = units;
-    units += units_of<MODE>(q.batch.mat[e].m, q.batch.mat[e].n, t.nb * t.bn);
-  }
-  q.unit0[q.batch.n_mats] = units;
-  q.n_units = units;
-  q.a = a.rows128;
-  q.b = MODE == ORTHO_APPLY || t.bn == 128 ? b.rows64 : b.rows128;
-  if (aux != nullptr) q.aux_map = aux->box;
-  if (out != nullptr) q.out_map = out->box;
-  q.out = out != nullptr ? out->p : nullptr;
-  q.out_ld = out != nullptr ? out->ld : 0;
-  ORTHO_CK(allow_smem<k_ortho_gemm<MODE>, O_SMEM_BYTES>());
-  ORTHO_CK(launch_chained(k_ortho_gemm<MODE>, q, 2 * (units < n_pairs ? units : n_pairs), 1, 1, O_THREADS, O_SMEM_BYTES, true, st));
-  return CAMERA_OK;
-}
-
 int run_round(const camera_matrix_t* mats, const OrthoRound& r, int32_t dtype, const float* coefficients, int32_t steps, float eps, char* ws,
               bool first_round, cudaStream_t st) {
   const OrthoLayout l = ortho_layout(r);
-  OrthoGemm q;
+  OrthoRun q;
   memset(&q, 0, sizeof(q));
   long long row0 = 0, tiles = 0;
   for (int i = r.begin; i < r.end; ++i) {
@@ -816,20 +870,15 @@ int run_round(const camera_matrix_t* mats, const OrthoRound& r, int32_t dtype, c
     if (here > tiles) tiles = here;
   }
   if (q.batch.n_mats == 0) return CAMERA_OK;
-  const int sms = sm_count(), n_pairs = sms / 2;
-  Packed xs[2], a, b;
-  if (!xs[0].encode(ws + l.x0, r.rows, r.x_ld) || !xs[1].encode(ws + l.x1, r.rows, r.x_ld) || !a.encode(ws + l.a, r.rows, r.a_ld) ||
-      !b.encode(ws + l.b, r.rows, r.a_ld))
-    return CAMERA_ERR_CUDA;
+  const int sms = sm_count();
   OrthoLoad ld;
   ld.batch = q.batch;
   ld.part = reinterpret_cast<double*>(ws + l.part);
   ld.first = reinterpret_cast<float*>(ws + l.first);
   ld.small = reinterpret_cast<int*>(ld.first + O_MAX_MATS);
-  ld.eps = eps; ld.x = xs[0].p; ld.x_ld = r.x_ld;
+  ld.done = ld.small + O_MAX_MATS;
+  ld.eps = eps; ld.x = reinterpret_cast<__half*>(ws + l.x0); ld.x_ld = r.x_ld;
   ld.totals = reinterpret_cast<PlanTotals*>(ws);
-  float* const rest_a = reinterpret_cast<float*>(ws + l.rest_a);
-  float* const rest_b = reinterpret_cast<float*>(ws + l.rest_b);
   ld.clear_status = first_round;
   ld.parts = 8 * sms / q.batch.n_mats;
   if (ld.parts > MAX_PARTS) ld.parts = MAX_PARTS;
@@ -837,43 +886,77 @@ int run_round(const camera_matrix_t* mats, const OrthoRound& r, int32_t dtype, c
   long long load_ctas = 8ll * sms / q.batch.n_mats + 1;
   if (load_ctas > tiles) load_ctas = tiles;
   if (dtype == CAMERA_BF16) {
-    ORTHO_CK(launch_chained(k_ortho_norm<__nv_bfloat16>, ld, ld.parts, q.batch.n_mats, 1, LOAD_THREADS, 0, !first_round, st));
+    ORTHO_CK(launch_chained(k_ortho_norm<__nv_bfloat16>, ld, ld.parts, q.batch.n_mats, 1, LOAD_THREADS, 0, false, st));
     ORTHO_CK(launch_chained(k_ortho_load<__nv_bfloat16>, ld, (int)load_ctas, q.batch.n_mats, 1, LOAD_THREADS, 0, true, st));
   } else {
-    ORTHO_CK(launch_chained(k_ortho_norm<float>, ld, ld.parts, q.batch.n_mats, 1, LOAD_THREADS, 0, !first_round, st));
+    ORTHO_CK(launch_chained(k_ortho_norm<float>, ld, ld.parts, q.batch.n_mats, 1, LOAD_THREADS, 0, false, st));
     ORTHO_CK(launch_chained(k_ortho_load<float>, ld, (int)load_ctas, q.batch.n_mats, 1, LOAD_THREADS, 0, true, st));
   }
-  q.totals = ld.totals;
+  if (!encode(&q.maps[BUF_X0], ws + l.x0, r.rows, r.x_ld) || !encode(&q.maps[BUF_X1], ws + l.x1, r.rows, r.x_ld) ||
+      !encode(&q.maps[BUF_A], ws + l.a, r.rows, r.a_ld) || !encode(&q.maps[BUF_B], ws + l.b, r.rows, r.a_ld))
+    return CAMERA_ERR_CUDA;
+  q.out[0] = reinterpret_cast<__half*>(ws + l.a);
+  q.out[1] = reinterpret_cast<__half*>(ws + l.b);
+  q.out_ld = r.a_ld;
+  q.rest[0] = reinterpret_cast<float*>(ws + l.rest_a);
+  q.rest[1] = reinterpret_cast<float*>(ws + l.rest_b);
+  q.first = ld.first; q.small = ld.small; q.done = ld.done; q.totals = ld.totals;
   q.wait_limit_ns = current_wait_limit_ns();
-  q.small = ld.small;
   double h = 1.0, sx = 1.0;             // the first X's factor is known on the device only
   double grown = 1.0;                   // what the steps so far can have made of a small singular value
   for (int s = 0; s < steps; ++s) {
     const float* const k = coefficients + 3 * s;
     const StepBound bound = step_bound(k, h * MARGIN);
     const double sa = factor_for(h * h), sb = factor_for(bound.b), sn = factor_for(bound.h);
-    const bool last = s + 1 == steps;
-    const Packed& x = xs[s & 1];
-    q.first = s == 0 ? ld.first : nullptr;
-    q.rest_out = rest_a;
-    q.f_acc = (float)(sa / (sx * sx));
-    q.small_in = (int)ceil(log2(fmax(grown / h, 1.0)));
+    OrthoStep& o = q.step[s];
+    o.f_gram = (float)(sa / (sx * sx));
+    o.f_poly = (float)(sb * k[2] / (sa * sa)); o.f_aux = (float)(sb * k[1] / sa); o.f_diag = (float)(sb * k[0]);
+    o.f_apply = (float)((s + 1 == steps ? 1.0 : sn) / (sb * sx));
+    o.small_in = (int)ceil(log2(fmax(grown / h, 1.0)));
     grown *= bound.b * MARGIN;
-    q.small_out = (int)ceil(log2(fmax(grown / bound.h, 1.0)));
-    int rc = launch_ortho<ORTHO_GRAM>(q, x, x, nullptr, &a, n_pairs, st);
-    if (rc != CAMERA_OK) return rc;
-    q.first = nullptr;
-    q.rest_in = rest_a; q.rest_out = rest_b;
-    q.f_acc = (float)(sb * k[2] / (sa * sa)); q.f_aux = (float)(sb * k[1] / sa); q.f_diag = (float)(sb * k[0]);
-    rc = launch_ortho<ORTHO_POLY>(q, a, a, &a, &b, n_pairs, st);
-    if (rc != CAMERA_OK) return rc;
-    q.first = s == 0 ? ld.first : nullptr;
-    q.rest_in = rest_b; q.rest_out = nullptr;
-    q.f_acc = (float)((last ? 1.0 : sn) / (sb * sx));
-    rc = launch_ortho<ORTHO_APPLY>(q, b, x, &x, last ? nullptr : &xs[(s + 1) & 1], n_pairs, st);
-    if (rc != CAMERA_OK) return rc;
+    o.small_out = (int)ceil(log2(fmax(grown / bound.h, 1.0)));
     h = bound.h;
     sx = sn;
+  }
+  ORTHO_CK(allow_smem<k_ortho, O_SMEM_BYTES>());
+  int pairs = pairs_at_once();
+  const OrthoTile t = choose_tile(q.batch, pairs);
+  q.bn = t.bn; q.nb = t.nb;
+  q.n_acc = t.nb * t.bn <= 256 ? 2 : 1;
+  q.kps = t.nb * t.bn <= 256 ? 2 : 1;
+  const int stage = q.kps * (O_A_BYTES + t.nb * t.bn * 64);
+  q.n_stages = O_RING_BYTES / stage < O_MAX_STAGES ? O_RING_BYTES / stage : O_MAX_STAGES;
+  int most = 0;
+  for (int mode = 0; mode < 3; ++mode) {
+    int units = 0;
+    for (int e = 0; e < q.batch.n_mats; ++e) {
+      q.unit0[mode][e] = units;
+      units += units_of(mode, q.batch.mat[e], t.nb * t.bn);
+    }
+    q.unit0[mode][q.batch.n_mats] = units;
+    q.per_step += units;
+    if (units > most) most = units;
+  }
+  q.n_steps = steps;
+  q.n_units = steps * q.per_step;
+  // with one matrix a product's units are all there is to do at one time
+  if (q.batch.n_mats == 1 && most < pairs) pairs = most;
+  if (q.per_step < pairs) pairs = q.per_step;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * pairs));
+  cfg.blockDim = dim3(O_THREADS);
+  cfg.dynamicSmemBytes = O_SMEM_BYTES;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeCooperative;        // units wait for those of other CTAs, so all run at one time
+  at[0].val.cooperative = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, k_ortho, q) != cudaSuccess) {
+    cudaGetLastError();                             // a context without cooperative launches: one pair, which waits for nobody else
+    cfg.gridDim = dim3(2);
+    cfg.numAttrs = 0;
+    ORTHO_CK(cudaLaunchKernelEx(&cfg, k_ortho, q));
   }
   return CAMERA_OK;
 }
@@ -899,7 +982,7 @@ extern "C" int camera_orthogonalize(const camera_matrix_t* mats, int32_t n_mats,
   using namespace camera;
   const int rc = check_matrices(mats, n_mats, dtype, true);
   if (rc != CAMERA_OK) return rc;
-  if (steps < 1 || steps > 64 || coefficients == nullptr || !(eps >= 0.f) || !(eps < 3.0e38f)) return CAMERA_ERR_INVALID_ARG;
+  if (steps < 1 || steps > O_MAX_STEPS || coefficients == nullptr || !(eps >= 0.f) || !(eps < 3.0e38f)) return CAMERA_ERR_INVALID_ARG;
   double h = 1.0;
   for (int s = 0; s < steps; ++s) {
     for (int i = 0; i < 3; ++i)
