@@ -800,7 +800,7 @@ int units_of(int mode, const OrthoMat& t, int w) {
 struct OrthoTile { int bn, nb; };
 OrthoTile choose_tile(const OrthoBatch& b, int n_pairs) {
   static constexpr OrthoTile kinds[3] = {{256, 2}, {256, 1}, {128, 1}};
-  static constexpr double k_block[3] = {0.60, 0.43, 0.32}, epilogue[3] = {5.0, 1.0, 0.7};
+  static constexpr double k_block[3] = {0.60, 0.43, 0.32}, epilogue[3] = {7.0, 1.0, 0.7};
   OrthoTile best = kinds[0];
   double best_cost = 1e300;
   for (int i = 0; i < 3; ++i) {
@@ -923,7 +923,7 @@ int run_round(const camera_matrix_t* mats, const OrthoRound& r, int32_t dtype, c
   const OrthoTile t = choose_tile(q.batch, pairs);
   q.bn = t.bn; q.nb = t.nb;
   q.n_acc = t.nb * t.bn <= 256 ? 2 : 1;
-  q.kps = t.nb * t.bn <= 256 ? 2 : 1;
+  q.kps = t.nb * t.bn <= 128 ? 2 : 1;        // two small k blocks a stage: a stage costs the issuing thread as much as one takes
   const int stage = q.kps * (O_A_BYTES + t.nb * t.bn * 64);
   q.n_stages = O_RING_BYTES / stage < O_MAX_STAGES ? O_RING_BYTES / stage : O_MAX_STAGES;
   int most = 0;
