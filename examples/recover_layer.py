@@ -86,7 +86,7 @@ def slice_layer(norm_weight, w_router, w_gate, w_up, w_down, x, top_k, prune):
     return [P.Ffn(out["w_gate"][e], out["w_up"][e], out["w_down"][e], d_ff=f) for e, f in enumerate(kept) if f > 0], kept
 
 
-def recover(d_model=256, d_ff=512, n_experts=8, top_k=2, tokens=1024, prune=0.4, steps=60, lr=0.003, momentum=0.9, seed=0, device="cuda", log=print):
+def recover(d_model=256, d_ff=512, n_experts=8, top_k=2, tokens=1024, prune=0.4, steps=60, lr=0.001, momentum=0.9, rank=16, seed=0, device="cuda", log=print):
     g = torch.Generator(device=device).manual_seed(seed)
     rnd = lambda *s: torch.randn(s, device=device, generator=g)
     strength = lambda: torch.exp(rnd(d_ff, 1) * 0.7)
@@ -95,7 +95,9 @@ def recover(d_model=256, d_ff=512, n_experts=8, top_k=2, tokens=1024, prune=0.4,
     w_down = [(rnd(d_model, d_ff) * d_ff ** -0.5).bfloat16() for _ in range(n_experts)]
     w_router = (rnd(n_experts, d_model) * d_model ** -0.5).bfloat16()
     norm_weight = (1 + 0.1 * rnd(d_model)).bfloat16()
-    data = lambda: rnd(tokens, d_model).bfloat16()
+    # hidden states lie near a few directions, which is why the remaining micro-experts can stand in for the others
+    basis = rnd(rank, d_model)
+    data = lambda: (rnd(tokens, rank) @ basis * rank ** -0.5).bfloat16()
 
     teacher = Block(norm_weight, w_router, [P.Ffn(*m) for m in zip(w_gate, w_up, w_down)], top_k, tokens)
     experts, kept = slice_layer(norm_weight, w_router, w_gate, w_up, w_down, data(), top_k, prune)
@@ -123,7 +125,7 @@ def recover(d_model=256, d_ff=512, n_experts=8, top_k=2, tokens=1024, prune=0.4,
                 v.add_(t)
         for m, v, o in zip(master, views, P.camera_orthogonalize(velocity, workspace=scratch)):
             # an orthogonal matrix's elements are sqrt(1 / longer side) in size: brought to the size of the weights' own
-            m.sub_(o.float(), alpha=lr * max(m.shape) ** 0.5)
+            m.sub_(o.float(), alpha=lr * (1 - step / steps) * max(m.shape) ** 0.5)
             v.copy_(m)
         if step % 20 == 0:
             log(f"step {step:3d}  squared error {losses[-1]:.5f}")
