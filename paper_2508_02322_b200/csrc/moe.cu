@@ -16,7 +16,7 @@ namespace {
 constexpr int MOE_MAX_EXPERTS = 1024, MOE_MAX_D = 1 << 20;
 constexpr int MOE_THREADS = 256, MOE_WARPS = MOE_THREADS / 32;
 // Up to so many pairs every CTA counts all of them for itself; beyond, a kernel before counts them chunk by chunk.
-constexpr long long MOE_SMALL = 8192;
+constexpr long long MOE_SMALL = 16384;
 
 struct Dispatch {
   const void* x;
