@@ -37,6 +37,21 @@ cudaError_t allow_smem() {
   return e;
 }
 
+// CTAs of `threads` threads and `smem` bytes of dynamic shared memory that an SM holds of a kernel: asked of the driver, the last
+// answer kept per kernel and device.
+template <auto KERN>
+int ctas_per_sm(int threads, int smem) {
+  static std::atomic<unsigned long long> known[KNOWN_DEVICES];          // smem << 32 | threads << 8 | CTAs
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return 1; }
+  const unsigned long long key = (unsigned long long)smem << 32 | (unsigned)threads << 8;
+  const unsigned long long seen = dev < KNOWN_DEVICES ? known[dev].load(std::memory_order_relaxed) : 0;
+  if ((seen & 0xff) != 0 && (seen & ~0xffull) == key) return (int)(seen & 0xff);
+  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, KERN, threads, (size_t)smem) != cudaSuccess || n < 1) { cudaGetLastError(); return 1; }
+  if (dev < KNOWN_DEVICES) known[dev].store(key | (unsigned)n, std::memory_order_relaxed);
+  return n;
+}
+
 // chained: the kernel may start while the one before it in the stream ends (it waits for that itself, griddepcontrol).
 template <typename A>
 inline cudaError_t launch_chained(void (*kern)(A), const A& args, int grid_x, int grid_y, int cluster_y, int threads, int smem, bool chained,

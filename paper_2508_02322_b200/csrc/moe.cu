@@ -161,6 +161,26 @@ __global__ void __launch_bounds__(MOE_THREADS) k_moe_dispatch(const Dispatch q) 
   T* const xs = static_cast<T*>(q.xs);
   constexpr int U = 4;
   const int t1 = min((int)(blockIdx.x + 1) * q.chunk, q.tokens);
+  if (q.d <= 32 * W) {                  // short rows: a token's in one load, U tokens at a time
+    for (int t0 = blockIdx.x * q.chunk + warp; t0 < t1; t0 += U * MOE_WARPS) {
+      const int c = lane * W;
+      P v[U];
+      int mine[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int t = t0 + u * MOE_WARPS;
+        if (t < t1 && c < q.d) v[u] = *reinterpret_cast<const P*>(x + t * q.x_ld + c);
+        mine[u] = t < t1 && lane < q.k ? q.rows[(long long)t * q.k + lane] : -1;
+      }
+      for (int j = 0; j < q.k; ++j)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int row = __shfl_sync(0xffffffffu, mine[u], j);
+          if (row >= 0 && c < q.d) *reinterpret_cast<P*>(xs + row * q.xs_ld + c) = v[u];
+        }
+    }
+    return;
+  }
   for (int t = blockIdx.x * q.chunk + warp; t < t1; t += MOE_WARPS) {
     const int mine = lane < q.k ? q.rows[(long long)t * q.k + lane] : -1;
     for (int c0 = 0; c0 < q.d; c0 += U * 32 * W) {
@@ -204,6 +224,12 @@ __global__ void __launch_bounds__(256, U == 1 ? 4 : U == 2 ? 3 : 2) k_moe_combin
   const int c0 = (blockIdx.y * U * blockDim.x + threadIdx.x) * W, step = blockDim.x * W;
   if (t >= q.tokens) return;
   const T* const ys = static_cast<const T*>(q.ys) + c0;
+  P extra[U];
+  if (q.add != nullptr) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (c0 + u * step < q.d) extra[u] = *reinterpret_cast<const P*>(static_cast<const T*>(q.add) + t * q.add_ld + c0 + u * step);
+  }
   float sum[U][W];
 #pragma unroll
   for (int u = 0; u < U; ++u)
@@ -244,7 +270,7 @@ __global__ void __launch_bounds__(256, U == 1 ? 4 : U == 2 ? 3 : 2) k_moe_combin
     if (c0 + u * step < q.d) {
       if (q.add != nullptr) {
         float f[W];
-        reinterpret_cast<const P*>(static_cast<const T*>(q.add) + t * q.add_ld + c0 + u * step)->get(f);
+        extra[u].get(f);
 #pragma unroll
         for (int i = 0; i < W; ++i) sum[u][i] += f[i];
       }
@@ -348,11 +374,10 @@ bool words_ok(const void* p) { return p != nullptr && (reinterpret_cast<uintptr_
   } while (0)
 
 template <typename T>
-cudaError_t launch_dispatch(const Dispatch& q, bool vec, int ctas, cudaStream_t st) {
-  constexpr int W = 16 / (int)sizeof(T);
+cudaError_t launch_dispatch(const Dispatch& q, int access, int ctas, cudaStream_t st) {
   const int smem = 4 * q.experts * (2 + MOE_WARPS);
-  return vec ? launch_chained(k_moe_dispatch<T, W>, q, ctas, 1, 1, MOE_THREADS, smem, q.hist != nullptr, st)
-             : launch_chained(k_moe_dispatch<T, 1>, q, ctas, 1, 1, MOE_THREADS, smem, q.hist != nullptr, st);
+  return launch_chained(access == BY_16 ? k_moe_dispatch<T, 16 / (int)sizeof(T)> : access == BY_TWO ? k_moe_dispatch<T, 2> : k_moe_dispatch<T, 1>, q, ctas, 1, 1,
+                        MOE_THREADS, smem, q.hist != nullptr, st);
 }
 // Slots S and packs U a thread: as many loads in flight whatever k is (8 vectors or 16 elements), but one pack a thread where one
 // wave of threads takes all of them.
@@ -365,12 +390,14 @@ cudaError_t combine_as(const Combine& q, cudaStream_t st) {
 }
 template <typename T, int W>
 cudaError_t launch_combine_as(const Combine& q, cudaStream_t st) {
-  constexpr int F = W > 1 ? 8 : 16;
+  constexpr bool VEC = W * sizeof(T) == 16;
+  constexpr int F = VEC ? 8 : 16;
   const bool one = (long long)q.tokens * ((q.d + W - 1) / W) <= 1024ll * sm_count();
-  if (q.k == 1) return one ? combine_as<T, W, 1, 1>(q, st) : combine_as<T, W, 1, F>(q, st);
+  if (q.k == 1) return one ? combine_as<T, W, 1, 1>(q, st) : combine_as<T, W, 1, F / 2>(q, st);
   if (q.k == 2) return one ? combine_as<T, W, 2, 1>(q, st) : combine_as<T, W, 2, F / 2>(q, st);
   if (q.k <= 4) return one ? combine_as<T, W, 4, 1>(q, st) : combine_as<T, W, 4, F / 4>(q, st);
-  return one || W > 1 ? combine_as<T, W, 8, 1>(q, st) : combine_as<T, W, 8, F / 8>(q, st);
+  if constexpr (VEC) return combine_as<T, W, 8, 1>(q, st);
+  else return one ? combine_as<T, W, 8, 1>(q, st) : combine_as<T, W, 8, F / 8>(q, st);
 }
 template <typename T, int W, int S, int U>
 cudaError_t combine_backward_as(const Combine& a, int each, cudaStream_t st) {
@@ -378,7 +405,7 @@ cudaError_t combine_backward_as(const Combine& a, int each, cudaStream_t st) {
   const int packs = (q.d + W - 1) / W;
   q.warps = (packs + 32 * each - 1) / (32 * each);
   if (q.warps > 16) q.warps = 16;
-  const int groups = q.warps >= 8 ? 1 : 8 / q.warps;
+  const int groups = q.warps >= 4 ? 1 : 4 / q.warps;
   k_moe_combine_backward<T, W, S, U><<<(unsigned)((q.tokens + groups - 1) / groups), 32 * q.warps * groups, 0, st>>>(q);
   return cudaGetLastError();
 }
@@ -390,6 +417,28 @@ cudaError_t launch_combine_backward_as(const Combine& q, cudaStream_t st) {
   if (q.k == 2) return few ? combine_backward_as<T, W, 2, 1>(q, 1, st) : combine_backward_as<T, W, 2, 4>(q, 4, st);
   if (q.k <= 4) return few ? combine_backward_as<T, W, 4, 1>(q, 1, st) : combine_backward_as<T, W, 4, 2>(q, 4, st);
   return combine_backward_as<T, W, 8, 1>(q, few ? 1 : 4, st);
+}
+
+// How all matrices of a call can be accessed; p and ld of each (p null: none).
+struct Rows { const void* p; long long ld; };
+template <int K>
+int access_of(const Rows (&m)[K], int d, int size) {
+  bool by16 = (d * size) % 16 == 0, by2 = d % 2 == 0;
+  for (const Rows& r : m) {
+    by16 = by16 && rows_on(r.p, r.ld, size, 16);
+    by2 = by2 && rows_on(r.p, r.ld, size, 2 * size);
+  }
+  return by16 ? BY_16 : by2 ? BY_TWO : BY_ONE;
+}
+template <typename T>
+cudaError_t launch_combine(const Combine& q, int access, cudaStream_t st) {
+  return access == BY_16 ? launch_combine_as<T, 16 / (int)sizeof(T)>(q, st) : access == BY_TWO ? launch_combine_as<T, 2>(q, st) : launch_combine_as<T, 1>(q, st);
+}
+template <typename T>
+cudaError_t launch_combine_backward(const Combine& q, int access, cudaStream_t st) {
+  return access == BY_16 ? launch_combine_backward_as<T, 16 / (int)sizeof(T)>(q, st)
+       : access == BY_TWO ? launch_combine_backward_as<T, 2>(q, st)
+                          : launch_combine_backward_as<T, 1>(q, st);
 }
 
 int combine(const void* ys, int32_t dtype, int64_t ys_ld, int64_t n_rows, const int32_t* rows, const float* w, int64_t tokens, int32_t k,
@@ -404,10 +453,9 @@ int combine(const void* ys, int32_t dtype, int64_t ys_ld, int64_t n_rows, const 
   Combine q = {};
   q.ys = ys; q.add = add; q.y = y; q.ys_ld = ys_ld; q.add_ld = add_ld; q.y_ld = y_ld; q.n_rows = n_rows;
   q.rows = rows; q.w = w; q.tokens = (int)tokens; q.k = k; q.d = d;
-  const bool vec = (d * size) % 16 == 0 && vec_ok(ys, ys_ld, size) && vec_ok(add, add_ld, size) && vec_ok(y, y_ld, size);
+  const int access = access_of({Rows{ys, ys_ld}, Rows{add, add_ld}, Rows{y, y_ld}}, d, size);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (size == 2) MOE_CK(vec ? launch_combine_as<__nv_bfloat16, 8>(q, st) : launch_combine_as<__nv_bfloat16, 1>(q, st));
-  else MOE_CK(vec ? launch_combine_as<float, 4>(q, st) : launch_combine_as<float, 1>(q, st));
+  MOE_CK(size == 2 ? launch_combine<__nv_bfloat16>(q, access, st) : launch_combine<float>(q, access, st));
   return CAMERA_OK;
 }
 
@@ -451,8 +499,8 @@ extern "C" int camera_moe_dispatch(const void* x, int32_t dtype, int64_t ld, int
     MOE_CK(launch_chained(k_moe_count, q, ctas, 1, 1, MOE_THREADS, 4 * n_experts, false, st));
     MOE_CK(launch_chained(k_moe_scan, q, (n_experts + SCAN_WARPS - 1) / SCAN_WARPS, 1, 1, 32 * SCAN_WARPS, 0, true, st));
   }
-  const bool vec = (d_model * size) % 16 == 0 && vec_ok(x, ld, size) && vec_ok(x_sorted, sorted_ld, size);
-  MOE_CK(size == 2 ? launch_dispatch<__nv_bfloat16>(q, vec, ctas, st) : launch_dispatch<float>(q, vec, ctas, st));
+  const int access = access_of({Rows{x, ld}, Rows{x_sorted, sorted_ld}}, d_model, size);
+  MOE_CK(size == 2 ? launch_dispatch<__nv_bfloat16>(q, access, ctas, st) : launch_dispatch<float>(q, access, ctas, st));
   return CAMERA_OK;
 }
 
@@ -486,10 +534,8 @@ extern "C" int camera_moe_combine_backward(const void* dy, int32_t dtype, int64_
   q.ys = y_sorted; q.dy = dy; q.dys = dy_sorted; q.dw = d_topk_w;
   q.ys_ld = sorted_ld; q.dy_ld = ld; q.dys_ld = dy_sorted_ld; q.n_rows = n_rows;
   q.rows = rows; q.w = topk_w; q.tokens = (int)n_tokens; q.k = top_k; q.d = d_model;
-  const bool vec = (d_model * size) % 16 == 0 && vec_ok(dy, ld, size) && vec_ok(dy_sorted, dy_sorted_ld, size) &&
-                   (d_topk_w == nullptr || vec_ok(y_sorted, sorted_ld, size));
+  const int access = access_of({Rows{dy, ld}, Rows{dy_sorted, dy_sorted_ld}, Rows{d_topk_w != nullptr ? y_sorted : nullptr, sorted_ld}}, d_model, size);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (size == 2) MOE_CK(vec ? launch_combine_backward_as<__nv_bfloat16, 8>(q, st) : launch_combine_backward_as<__nv_bfloat16, 1>(q, st));
-  else MOE_CK(vec ? launch_combine_backward_as<float, 4>(q, st) : launch_combine_backward_as<float, 1>(q, st));
+  MOE_CK(size == 2 ? launch_combine_backward<__nv_bfloat16>(q, access, st) : launch_combine_backward<float>(q, access, st));
   return CAMERA_OK;
 }

@@ -15,14 +15,15 @@ namespace camera {
 namespace {
 
 constexpr int NORM_MAX_D = 32768;          // 32 warps x 32 elements a thread
-constexpr int BACKWARD_ROWS = 2;            // a group's rows, at least
-constexpr int FORWARD_THREADS = 1024;      // threads an SM may hold of the forward kernel
-constexpr int BACKWARD_THREADS = 512;       // threads an SM holds of the backward kernel (128 registers each)
+constexpr int NORM_BOTH_D = 28672;         // up to here shared memory holds shares of dw and db
+constexpr int BACKWARD_ROWS = 2;           // a group's rows in the backward pass, at least
+// Rows of a group worked on together, so that their sums and barriers overlap: two in the backward pass (16384 x 3584 bf16: 90 us by
+// one, 83 by two) and in the forward pass of layer norms with their two sums (12743 x 4608 bf16 with bias and residual: 125 and 105),
+// one in that of root-mean-square norms (16384 x 3584: 86 and 89).
+template <int THREADS> constexpr int BACKWARD_TOGETHER = THREADS > 512 ? 1 : 2;
 // Rows of a group in flight, of N 16-byte loads a thread and matrix: what 196 KB hold of the backward pass's three matrices for 512
-// threads (16384 x 3584 bf16: 2 stages 96 us, 3 stages 94, 4 stages 95).
-template <int N> constexpr int NORM_STAGES = N <= 2 ? 3 : N <= 8 ? 8 / N : 1;
-// The same of the forward pass's two.
-template <int N, int THREADS> constexpr int FORWARD_STAGES = THREADS <= 512 ? NORM_STAGES<N> : N <= 2 ? 3 : 1;
+// threads; one where a CTA has up to 1024 for a long row.
+template <int N, int THREADS, int E> constexpr int NORM_STAGES = THREADS > 512 && E > 8 ? 1 : N <= 2 ? 4 : 2;
 constexpr int NORM_GROUP_THREADS = 256;    // groups of fewer threads share a CTA up to this
 
 struct NormArgs {
@@ -46,7 +47,7 @@ __device__ __forceinline__ void load_weight(const void* p, bool f32, int c, floa
 #pragma unroll
     for (int i = 0; i < W; ++i) out[i] = absent;
   } else if (f32) {
-    constexpr int V = W >= 4 ? 4 : 1;
+    constexpr int V = W >= 4 ? 4 : W;
 #pragma unroll
     for (int k = 0; k < W; k += V) {
       const Pack<float, V> t = *reinterpret_cast<const Pack<float, V>*>(static_cast<const float*>(p) + c + k);
@@ -79,11 +80,12 @@ __device__ __forceinline__ void own_weights(const void* p, bool f32, int d, int 
 // W elements a load (16 bytes, or 1 element where rows or the width are not aligned for that), N loads a thread and matrix.
 // Columns past the end read as zeros.  RING: the next rows travel through shared memory, each thread copying (cp.async) what it
 // will read itself, so that a wait is the thread's own and the rows in flight cost no registers.
-template <typename T, int W, int N, bool BIAS, bool RING, int THREADS>
+template <typename T, int W, int N, bool BIAS, bool RING, int THREADS, int ROWS>
 __global__ void __launch_bounds__(THREADS, 1) k_norm_forward(const NormArgs q) {
   using P = Pack<T, W>;
-  constexpr int E2 = N * W / 2, STAGES = FORWARD_STAGES<N, THREADS>;
-  constexpr bool OWN_W = THREADS <= 512 && N * W <= 16;                  // weights in registers, or loaded again for each use
+  constexpr int E2 = N * W / 2, STAGES = NORM_STAGES<N, THREADS, N * W>;
+  constexpr bool OWN_W = N * W <= 8 || (THREADS <= 512 && N * W <= 16);   // weights in registers, or loaded again for each use
+  constexpr bool AHEAD = !RING && N * W <= 8;                             // the next row waits in registers
   extern __shared__ __align__(16) uint8_t ring[];
   const int threads = 32 * q.warps, group = threadIdx.x / threads, t = threadIdx.x - group * threads;
   const int groups = blockDim.x / threads;
@@ -115,140 +117,169 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm_forward(const NormArgs q) {
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  const long long first = (long long)blockIdx.x * groups + group;
-  if constexpr (RING)
-    for (int s = 0; s < STAGES; ++s) issue(s, first + s * step);
-  for (long long row = first; row < q.rows; row += step) {
-    P px[N], pr[N];
-    if constexpr (RING) {
-      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
-      const uint8_t* const at = ring + 16 * threadIdx.x + stage * parts * line;
+  P nx[N], nr[N];
+  auto load = [&](long long row) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        px[j] = *reinterpret_cast<const P*>(at + j * 16 * blockDim.x);
-        if (r != nullptr) pr[j] = *reinterpret_cast<const P*>(at + line + j * 16 * blockDim.x);
+    for (int j = 0; j < N; ++j) {
+      const int c = (j * threads + t) * W;
+      nx[j] = nr[j] = P();
+      if (c < q.d) {
+        nx[j] = *reinterpret_cast<const P*>(x + row * q.x_ld + c);
+        if (r != nullptr) nr[j] = *reinterpret_cast<const P*>(r + row * q.r_ld + c);
       }
-      issue(stage, row + STAGES * step);
-      if (++stage == STAGES) stage = 0;
-    } else {
+    }
+  };
+  const long long first = (long long)blockIdx.x * groups + group;
+  if constexpr (RING) {
+    for (int s = 0; s < STAGES; ++s) issue(s, first + s * step);
+  } else if constexpr (AHEAD) {
+    if (first < q.rows) load(first);
+  }
+  for (long long row0 = first; row0 < q.rows; row0 += ROWS * step) {
+    F2 z[ROWS][E2];
+    float mu[ROWS], s[ROWS], lo, hi;
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const int c = (j * threads + t) * W;
-        px[j] = pr[j] = P();
-        if (c < q.d) {
-          px[j] = *reinterpret_cast<const P*>(x + row * q.x_ld + c);
-          if (r != nullptr) pr[j] = *reinterpret_cast<const P*>(r + row * q.r_ld + c);
+    for (int k = 0; k < ROWS; ++k) {
+      const long long row = row0 + k * step;
+      P px[N], pr[N];
+      if constexpr (RING) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+        const uint8_t* const at = ring + 16 * threadIdx.x + stage * parts * line;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          px[j] = *reinterpret_cast<const P*>(at + j * 16 * blockDim.x);
+          if (r != nullptr) pr[j] = *reinterpret_cast<const P*>(at + line + j * 16 * blockDim.x);
+        }
+        issue(stage, row + STAGES * step);
+        if (++stage == STAGES) stage = 0;
+      } else {
+        if (!AHEAD) load(row);
+#pragma unroll
+        for (int j = 0; j < N; ++j) { px[j] = nx[j]; pr[j] = nr[j]; }
+        if (AHEAD && row + step < q.rows) load(row + step);
+      }
+      to_pairs<P, W, N>(px, z[k]);
+      if (r != nullptr) {
+        F2 v[E2];
+        to_pairs<P, W, N>(pr, v);
+#pragma unroll
+        for (int i = 0; i < E2; ++i) z[k][i] = add2(z[k][i], v[i]);
+        from_pairs<P, W, N>(z[k], px);
+        to_pairs<P, W, N>(px, z[k]);
+        if (row < q.rows) {
+#pragma unroll
+          for (int j = 0; j < N; ++j) {
+            const int c = (j * threads + t) * W;
+            if (c < q.d) *reinterpret_cast<P*>(static_cast<T*>(q.sum) + row * q.sum_ld + c) = px[j];
+          }
         }
       }
-    }
-    F2 z[E2];
-    to_pairs<P, W, N>(px, z);
-    if (r != nullptr) {
-      F2 v[E2];
-      to_pairs<P, W, N>(pr, v);
+      mu[k] = 0.f;
+      F2 acc = f2(0.f, 0.f);
 #pragma unroll
-      for (int i = 0; i < E2; ++i) z[i] = add2(z[i], v[i]);
-      from_pairs<P, W, N>(z, px);
-      to_pairs<P, W, N>(px, z);
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const int c = (j * threads + t) * W;
-        if (c < q.d) *reinterpret_cast<P*>(static_cast<T*>(q.sum) + row * q.sum_ld + c) = px[j];
-      }
+      for (int i = 0; i < E2; ++i) acc = q.rms ? fma2(z[k][i], z[k][i], acc) : add2(acc, z[k][i]);
+      split(acc, lo, hi);
+      s[k] = lo + hi;
     }
-    float s[1], lo, hi, mu = 0.f;
-    F2 acc = f2(0.f, 0.f);
+    group_sum(s, q.warps, group, buf);
     if (!q.rms) {
 #pragma unroll
-      for (int i = 0; i < E2; ++i) acc = add2(acc, z[i]);
-      split(acc, lo, hi);
-      s[0] = lo + hi;
-      group_sum(s, q.warps, group, buf);
-      mu = s[0] / (float)q.d;
-      // around the mean; columns past the end stay zero
-      float f[N * W];
+      for (int k = 0; k < ROWS; ++k) {
+        mu[k] = s[k] / (float)q.d;
+        // around the mean; columns past the end stay zero
+        float f[N * W];
 #pragma unroll
-      for (int i = 0; i < E2; ++i) split(add2(z[i], f2(-mu, -mu)), f[2 * i], f[2 * i + 1]);
+        for (int i = 0; i < E2; ++i) split(add2(z[k][i], f2(-mu[k], -mu[k])), f[2 * i], f[2 * i + 1]);
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-        if ((j * threads + t) * W >= q.d) {
+        for (int j = 0; j < N; ++j)
+          if ((j * threads + t) * W >= q.d) {
 #pragma unroll
-          for (int i = 0; i < W; ++i) f[j * W + i] = 0.f;
+            for (int i = 0; i < W; ++i) f[j * W + i] = 0.f;
+          }
+        F2 acc = f2(0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < E2; ++i) {
+          z[k][i] = f2(f[2 * i], f[2 * i + 1]);
+          acc = fma2(z[k][i], z[k][i], acc);
         }
-#pragma unroll
-      for (int i = 0; i < E2; ++i) z[i] = f2(f[2 * i], f[2 * i + 1]);
-    }
-    acc = f2(0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < E2; ++i) acc = fma2(z[i], z[i], acc);
-    split(acc, lo, hi);
-    s[0] = lo + hi;
-    group_sum(s, q.warps, group, buf);
-    const float rstd = 1.f / sqrtf(s[0] / (float)q.d + q.eps);
-    if (t == 0) {
-      if (q.mean != nullptr) q.mean[row] = mu;
-      if (q.rstd != nullptr) q.rstd[row] = rstd;
+        split(acc, lo, hi);
+        s[k] = lo + hi;
+      }
+      group_sum(s, q.warps, group, buf);
     }
     if (!OWN_W) {
       own_weights<W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
       if constexpr (BIAS) own_weights<W, N>(q.b, q.w_f32, q.d, threads, t, 0.f, b);
     }
-    const F2 rs = f2(rstd, rstd);
 #pragma unroll
-    for (int i = 0; i < E2; ++i) z[i] = BIAS ? fma2(mul2(z[i], rs), w[i], b[BIAS ? i : 0]) : mul2(mul2(z[i], rs), w[i]);
-    from_pairs<P, W, N>(z, px);
+    for (int k = 0; k < ROWS; ++k) {
+      const long long row = row0 + k * step;
+      if (row >= q.rows) break;
+      const float rstd = 1.f / sqrtf(s[k] / (float)q.d + q.eps);
+      if (t == 0) {
+        if (q.mean != nullptr) q.mean[row] = mu[k];
+        if (q.rstd != nullptr) q.rstd[row] = rstd;
+      }
+      const F2 rs = f2(rstd, rstd);
+      P out[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int c = (j * threads + t) * W;
-      if (c < q.d) *reinterpret_cast<P*>(static_cast<T*>(q.y) + row * q.y_ld + c) = px[j];
+      for (int i = 0; i < E2; ++i) z[k][i] = BIAS ? fma2(mul2(z[k][i], rs), w[i], b[BIAS ? i : 0]) : mul2(mul2(z[k][i], rs), w[i]);
+      from_pairs<P, W, N>(z[k], out);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int c = (j * threads + t) * W;
+        if (c < q.d) *reinterpret_cast<P*>(static_cast<T*>(q.y) + row * q.y_ld + c) = out[j];
+      }
     }
   }
 }
 
 // A thread keeps the columns it owns for all rows of its group, so their weights and their shares of dw and db stay in its
-// registers; the groups' shares are added up by k_norm_reduce in a fixed order.  Columns past the end read as zeros, which add
-// nothing.  RING: the next rows travel through shared memory, each thread copying (cp.async) what it will read itself, so that
-// a wait is the thread's own and the rows in flight cost no registers; without it (elements, which cp.async cannot copy one at
-// a time) the next row waits in registers.
+// registers (in its own places of shared memory where a row is long); the groups' shares are added up by k_norm_reduce in a fixed
+// order.  Columns past the end read as zeros, which add nothing.  RING as above; without it both passes over a row load it.
 template <typename T, int W, int N, bool BIAS, bool RING, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1) k_norm_backward(const NormArgs q) {
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) k_norm_backward(const NormArgs q) {
   using P = Pack<T, W>;
-  constexpr int E2 = N * W / 2;
-  constexpr bool AHEAD = !RING && N * W <= 16;
-  constexpr int STAGES = NORM_STAGES<N>;
+  constexpr bool LONG = THREADS > 512 && N * W >= 16;
+  constexpr int E2 = N * W / 2, STAGES = NORM_STAGES<N, THREADS, N * W>;
+  constexpr int G = W == 1 ? 2 : 1, PR = W == 1 ? 1 : W / 2;           // packs worked on at a time, and their pairs
+  constexpr int ROWS = BACKWARD_TOGETHER<THREADS>;
   extern __shared__ __align__(16) uint8_t ring[];
   const int threads = 32 * q.warps, group = threadIdx.x / threads, t = threadIdx.x - group * threads;
   const int groups = blockDim.x / threads;
   const long long step = (long long)gridDim.x * groups;
-  const T* const x = static_cast<const T*>(q.x);
-  const T* const r = static_cast<const T*>(q.r);
-  const T* const dy = static_cast<const T*>(q.dy);
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  int buf = 0;
-  P now[3][RING ? 1 : N], next[3][AHEAD ? N : 1];
-  constexpr bool OWN_W = N * W <= 16;                  // weights in registers, or loaded again for each use
-  F2 dw[E2], db[BIAS ? E2 : 1], w[E2];
-#pragma unroll
-  for (int i = 0; i < E2; ++i) dw[i] = db[BIAS ? i : 0] = f2(0.f, 0.f);
-  if (OWN_W) own_weights<W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
+  const T* const src[3] = {static_cast<const T*>(q.x), static_cast<const T*>(q.dy), static_cast<const T*>(q.r)};
+  const long long ld[3] = {q.x_ld, q.dy_ld, q.r_ld};
+  const bool has_r = q.r != nullptr;
+  const int parts = has_r ? 3 : 2, line = N * 16 * (int)blockDim.x;
   const long long first = (long long)blockIdx.x * groups + group;
-  auto load = [&](P (*to)[RING ? 1 : N], long long row) {
+  const int wanted = q.want_w + q.want_b;
+  float* const part = q.part + first * wanted * q.d;                   // [groups][wanted][d]
+  // LONG: pair i of the thread's share of dw at i * blockDim.x + threadIdx.x, db's behind it, or in memory where there is no room
+  F2* const acc = reinterpret_cast<F2*>(ring + (RING ? STAGES * parts * line : 0)) + threadIdx.x;
+  F2* const acc_b = acc + E2 * blockDim.x;
+  const bool far = LONG && BIAS && q.d > NORM_BOTH_D;
+  float* const part_b = part + (wanted - 1) * q.d;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  int buf = 0, stage = 0;
+  F2 dw[LONG ? 1 : E2], db[BIAS && !LONG ? E2 : 1], w[LONG ? 1 : E2];
 #pragma unroll
-    for (int j = 0; j < (RING ? 0 : N); ++j) {
-      const int c = (j * threads + t) * W;
-      to[0][j] = to[1][j] = to[2][j] = P();
-      if (c < q.d) {
-        to[0][j] = *reinterpret_cast<const P*>(x + row * q.x_ld + c);
-        to[1][j] = *reinterpret_cast<const P*>(dy + row * q.dy_ld + c);
-        if (r != nullptr) to[2][j] = *reinterpret_cast<const P*>(r + row * q.r_ld + c);
-      }
+  for (int i = 0; i < (LONG ? 1 : E2); ++i) dw[i] = db[BIAS && !LONG ? i : 0] = f2(0.f, 0.f);
+  if constexpr (LONG) {
+    for (int i = 0; i < E2; ++i) {
+      acc[i * blockDim.x] = f2(0.f, 0.f);
+      if (BIAS && !far) acc_b[i * blockDim.x] = f2(0.f, 0.f);
     }
-  };
-  const int parts = r != nullptr ? 3 : 2, line = N * 16 * (int)blockDim.x;
+    if (far)
+      for (int j = 0; j < N; ++j)
+        for (int i = 0; i < W; ++i)
+          if ((j * threads + t) * W + i < q.d) part_b[(j * threads + t) * W + i] = 0.f;
+  } else {
+    own_weights<W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
+  }
   const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring) + 16 * threadIdx.x;
   auto issue = [&](int stage, long long row) {
     if (row < q.rows) {
-      const T* const src[3] = {x + row * q.x_ld, dy + row * q.dy_ld, r + row * q.r_ld};
 #pragma unroll
       for (int p = 0; p < 3; ++p)
         if (p < parts) {
@@ -256,123 +287,176 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm_backward(const NormArgs q) 
           for (int j = 0; j < N; ++j) {
             const int c = (j * threads + t) * W, at = c < q.d ? c : 0;
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(mine + (stage * parts + p) * line + j * 16 * blockDim.x),
-                         "l"(src[p] + at), "r"(c < q.d ? 16 : 0)
+                         "l"(src[p] + row * ld[p] + at), "r"(c < q.d ? 16 : 0)
                          : "memory");
           }
         }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  int stage = 0;
-  // the thread's elements of matrix p (x, dy, d_sum) of this row, from where they wait
-  auto get = [&](int p, F2 (&out)[E2]) {
-    P v[N];
-    const uint8_t* const at = ring + 16 * threadIdx.x + (stage * parts + p) * line;
+  // pairs of packs j .. j + G - 1 of matrix p (x, dy, d_sum) of this row, from where they wait
+  auto get = [&](int p, int j, int k_row, long long row, F2 (&out)[PR]) {
+    P v[G];
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      if constexpr (RING) v[j] = *reinterpret_cast<const P*>(at + j * 16 * blockDim.x);
-      else v[j] = now[p][j];
+    for (int k = 0; k < G; ++k) {
+      if constexpr (RING) {
+        v[k] = *reinterpret_cast<const P*>(ring + 16 * threadIdx.x + ((stage + k_row) % STAGES * parts + p) * line + (j + k) * 16 * blockDim.x);
+      } else {
+        const int c = ((j + k) * threads + t) * W;
+        v[k] = P();
+        if (c < q.d) v[k] = *reinterpret_cast<const P*>(src[p] + row * ld[p] + c);
+      }
     }
-    to_pairs<P, W, N>(v, out);
+    to_pairs<P, W, G>(v, out);
   };
-  float rstd_next = 0.f, mu_next = 0.f;
-  auto stats = [&](long long row) {
-    if (row < q.rows) {
-      rstd_next = q.rstd[row];
-      mu_next = q.rms ? 0.f : q.mean[row];
+  auto weights = [&](int j, F2 (&out)[PR]) {
+    if constexpr (LONG) {
+      float f[G * W];
+#pragma unroll
+      for (int k = 0; k < G; ++k) {
+        const int c = ((j + k) * threads + t) * W;
+        float v[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] = 0.f;
+        if (c < q.d) load_weight<W>(q.w, q.w_f32, c, 1.f, v);
+#pragma unroll
+        for (int i = 0; i < W; ++i) f[k * W + i] = v[i];
+      }
+#pragma unroll
+      for (int i = 0; i < PR; ++i) out[i] = f2(f[2 * i], f[2 * i + 1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PR; ++i) out[i] = w[j / G * PR + i];
+    }
+  };
+  float rstd_next[ROWS], mu_next[ROWS];
+  auto stats = [&](long long row0) {
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+      const long long row = row0 + k * step;
+      rstd_next[k] = row < q.rows ? q.rstd[row] : 0.f;
+      mu_next[k] = row < q.rows && !q.rms ? q.mean[row] : 0.f;
     }
   };
   stats(first);
-  if constexpr (RING) {
+  if constexpr (RING)
     for (int s = 0; s < STAGES; ++s) issue(s, first + s * step);
-  } else if constexpr (AHEAD) {
-    if (first < q.rows) load(next, first);
-  }
-  for (long long row = first; row < q.rows; row += step) {
-    const float rstd = rstd_next, mu = mu_next;
-    stats(row + step);
-    if constexpr (RING) {
-      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
-    } else if constexpr (AHEAD) {
+  for (long long row0 = first; row0 < q.rows; row0 += ROWS * step) {
+    float rstd[ROWS], s[2 * ROWS];
+    F2 minus_mu[ROWS];
 #pragma unroll
-      for (int p = 0; p < 3; ++p)
-#pragma unroll
-        for (int j = 0; j < N; ++j) now[p][j] = next[p][j];
-      if (row + step < q.rows) load(next, row + step);
-    } else {
-      load(now, row);
+    for (int k = 0; k < ROWS; ++k) {
+      rstd[k] = rstd_next[k];
+      minus_mu[k] = f2(-mu_next[k], -mu_next[k]);
     }
-    const F2 minus_mu = f2(-mu, -mu), rs = f2(rstd, rstd);
-    F2 s0 = f2(0.f, 0.f), s1 = f2(0.f, 0.f);
-    {
-      F2 c[E2], d[E2];
-      get(0, c);
-      get(1, d);
-      if (!OWN_W) own_weights<W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
+    stats(row0 + ROWS * step);
+    if constexpr (RING) asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - ROWS) : "memory");
 #pragma unroll
-      for (int i = 0; i < E2; ++i) {
-        c[i] = add2(c[i], minus_mu);
-        dw[i] = fma2(mul2(d[i], rs), c[i], dw[i]);
-        if (BIAS) db[i] = add2(db[i], d[i]);
-        const F2 g = mul2(d[i], w[i]);
-        s0 = add2(s0, g);
-        s1 = fma2(g, c[i], s1);
+    for (int k = 0; k < ROWS; ++k) {
+      const long long row = row0 + k * step;
+      F2 s0 = f2(0.f, 0.f), s1 = f2(0.f, 0.f);
+      if (row < q.rows) {
+        const F2 rs = f2(rstd[k], rstd[k]);
+#pragma unroll
+        for (int j = 0; j < N; j += G) {
+          F2 c[PR], d[PR], wj[PR];
+          get(0, j, k, row, c);
+          get(1, j, k, row, d);
+          weights(j, wj);
+#pragma unroll
+          for (int i = 0; i < PR; ++i) {
+            const int at = j / G * PR + i;
+            c[i] = add2(c[i], minus_mu[k]);
+            const F2 g = mul2(d[i], wj[i]), dr = mul2(d[i], rs);
+            s0 = add2(s0, g);
+            s1 = fma2(g, c[i], s1);
+            if constexpr (LONG) {
+              acc[at * blockDim.x] = fma2(dr, c[i], acc[at * blockDim.x]);
+              if (BIAS && !far) acc_b[at * blockDim.x] = add2(acc_b[at * blockDim.x], d[i]);
+              if (far) {
+                float lo, hi;
+                split(d[i], lo, hi);
+                const int c0 = (j * threads + t) * W + 2 * i, c1 = W == 1 ? c0 + threads : c0 + 1;
+                if (c0 < q.d) part_b[c0] += lo;
+                if (c1 < q.d) part_b[c1] += hi;
+              }
+            } else {
+              dw[at] = fma2(dr, c[i], dw[at]);
+              if (BIAS) db[at] = add2(db[at], d[i]);
+            }
+          }
+        }
       }
+      float lo, hi;
+      split(s0, lo, hi);
+      s[2 * k] = lo + hi;
+      split(s1, lo, hi);
+      s[2 * k + 1] = lo + hi;
     }
     if (q.y != nullptr) {
-      float s[2], lo, hi;
-      split(s0, lo, hi);
-      s[0] = lo + hi;
-      split(s1, lo, hi);
-      s[1] = lo + hi;
       group_sum(s, q.warps, group, buf);
-      // dx = s g - s mean g - c s^2 mean(g h),  mean(g h) = s mean(g c)
-      const float k1 = q.rms ? 0.f : -rstd * (s[0] / (float)q.d), k2 = -rstd * rstd * (rstd * (s[1] / (float)q.d));
-      const F2 k1s = f2(k1, k1), k2s = f2(k2, k2);
-      F2 c[E2], d[E2];
-      get(0, c);
-      get(1, d);
-      if (!OWN_W) own_weights<W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
 #pragma unroll
-      for (int i = 0; i < E2; ++i) c[i] = fma2(mul2(d[i], w[i]), rs, fma2(add2(c[i], minus_mu), k2s, k1s));
-      if (r != nullptr) {
-        get(2, d);
+      for (int k = 0; k < ROWS; ++k) {
+        const long long row = row0 + k * step;
+        if (row >= q.rows) break;
+        // dx = s g - s mean g - c s^2 mean(g h),  mean(g h) = s mean(g c)
+        const float k1 = q.rms ? 0.f : -rstd[k] * (s[2 * k] / (float)q.d), k2 = -rstd[k] * rstd[k] * (rstd[k] * (s[2 * k + 1] / (float)q.d));
+        const F2 k1s = f2(k1, k1), k2s = f2(k2, k2), rs = f2(rstd[k], rstd[k]);
 #pragma unroll
-        for (int i = 0; i < E2; ++i) c[i] = add2(c[i], d[i]);
-      }
-      P out[N];
-      from_pairs<P, W, N>(c, out);
+        for (int j = 0; j < N; j += G) {
+          F2 c[PR], d[PR], wj[PR];
+          get(0, j, k, row, c);
+          get(1, j, k, row, d);
+          weights(j, wj);
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const int at = (j * threads + t) * W;
-        if (at < q.d) *reinterpret_cast<P*>(static_cast<T*>(q.y) + row * q.y_ld + at) = out[j];
+          for (int i = 0; i < PR; ++i) c[i] = fma2(mul2(d[i], wj[i]), rs, fma2(add2(c[i], minus_mu[k]), k2s, k1s));
+          if (has_r) {
+            get(2, j, k, row, d);
+#pragma unroll
+            for (int i = 0; i < PR; ++i) c[i] = add2(c[i], d[i]);
+          }
+          P out[G];
+          from_pairs<P, W, G>(c, out);
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const int at = ((j + g) * threads + t) * W;
+            if (at < q.d) *reinterpret_cast<P*>(static_cast<T*>(q.y) + row * q.y_ld + at) = out[g];
+          }
+        }
       }
     }
     if constexpr (RING) {
-      issue(stage, row + STAGES * step);
-      if (++stage == STAGES) stage = 0;
+#pragma unroll
+      for (int k = 0; k < ROWS; ++k) {
+        issue(stage, row0 + (STAGES + k) * step);
+        if (++stage == STAGES) stage = 0;
+      }
     }
   }
-  // [groups][wanted][d]
-  const int wanted = q.want_w + q.want_b;
-  float* const part = q.part + first * wanted * q.d;
 #pragma unroll
   for (int which = 0; which < (BIAS ? 2 : 1); ++which) {
     if (!(which ? q.want_b : q.want_w)) continue;
+    float* const to = part + (which ? (wanted - 1) * q.d : 0);
+    if (which && far) continue;
     float f[N * W];
 #pragma unroll
-    for (int i = 0; i < E2; ++i) split(which ? db[i] : dw[i], f[2 * i], f[2 * i + 1]);
+    for (int i = 0; i < E2; ++i) {
+      F2 v;
+      if constexpr (LONG) v = (which ? acc_b : acc)[i * blockDim.x];
+      else v = which ? db[BIAS ? i : 0] : dw[i];
+      split(v, f[2 * i], f[2 * i + 1]);
+    }
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const int c = (j * threads + t) * W;
       if (c < q.d) {
-        constexpr int V = W >= 4 ? 4 : 1;
+        constexpr int V = W >= 4 ? 4 : W;
 #pragma unroll
         for (int k = 0; k < W; k += V) {
           Pack<float, V> a;
 #pragma unroll
           for (int i = 0; i < V; ++i) a.v[i] = f[j * W + k + i];
-          *reinterpret_cast<Pack<float, V>*>(part + (which ? (wanted - 1) * q.d : 0) + c + k) = a;
+          *reinterpret_cast<Pack<float, V>*>(to + c + k) = a;
         }
       }
     }
@@ -406,80 +490,133 @@ __global__ void __launch_bounds__(32 * REDUCE_WARPS) k_norm_reduce(const NormRed
 // ------------------------------------------------------------------------------------------------ host side
 struct NormShape { int warps, groups_per_cta, ctas; };
 
-// Warps a row and groups a CTA for `per` elements a thread; threads_sm: threads an SM holds of the kernel.
-NormShape norm_shape(long long rows, int d, int per, int threads_sm, long long rows_per_group) {
+// Warps a row and groups a CTA for `per` elements a thread.
+NormShape norm_shape(long long rows, int d, int per, long long rows_per_group) {
   NormShape s;
   s.warps = (d + 32 * per - 1) / (32 * per);
   s.groups_per_cta = NORM_GROUP_THREADS / (32 * s.warps);
   if (s.groups_per_cta < 1) s.groups_per_cta = 1;
-  const int sms = sm_count();
   const long long want = (rows + rows_per_group - 1) / rows_per_group;       // groups
-  while (s.groups_per_cta > 1 && (want + s.groups_per_cta - 1) / s.groups_per_cta < sms) --s.groups_per_cta;
-  const int per_sm = threads_sm / (32 * s.warps * s.groups_per_cta);
-  const long long most = (long long)sms * (per_sm > 1 ? per_sm : 1), need = (want + s.groups_per_cta - 1) / s.groups_per_cta;
-  s.ctas = (int)(need < most ? need : most);
+  while (s.groups_per_cta > 1 && (want + s.groups_per_cta - 1) / s.groups_per_cta < sm_count()) --s.groups_per_cta;
+  s.ctas = 0;
   return s;
 }
-
-// Elements a thread holds in the backward pass, and the groups that leave shares of dw and db.
-int backward_per(int d) { return d <= 16 * 512 ? 16 : 32; }
-// Rows a group takes at least: a group's shares cost the second kernel as much as a few of its rows do here, more where rows are
-// read by elements.
-NormShape backward_shape(long long rows, int d, bool vec) {
-  return norm_shape(rows, d, backward_per(d), BACKWARD_THREADS, vec ? 2 * BACKWARD_ROWS : BACKWARD_ROWS);
+// And CTAs: as many as the rows ask for, or the GPU holds at one time.
+void set_ctas(NormShape& s, long long rows, long long rows_per_group, int per_sm) {
+  const long long want = (rows + rows_per_group - 1) / rows_per_group, need = (want + s.groups_per_cta - 1) / s.groups_per_cta;
+  const long long most = (long long)sm_count() * (per_sm > 1 ? per_sm : 1);
+  s.ctas = (int)(need < most ? need : most);
 }
 
-template <typename T, int W, int N, bool BIAS, bool RING, int THREADS>
+template <typename T, int W, int E, bool BIAS, bool RING, int THREADS, int ROWS = 1>
 cudaError_t forward_as(const NormArgs& a, cudaStream_t st) {
+  constexpr int N = E / W, STAGES = NORM_STAGES<N, THREADS, E>;
+  constexpr auto KERN = k_norm_forward<T, W, N, BIAS, RING, THREADS, ROWS>;
   NormArgs q = a;
-  const NormShape s = norm_shape(q.rows, q.d, N * W, RING ? FORWARD_THREADS : 1024, 1);
+  NormShape s = norm_shape(q.rows, q.d, E, 1);
   q.warps = s.warps;
   const int threads = 32 * s.warps * s.groups_per_cta;
   int smem = 0;
   if constexpr (RING) {
-    constexpr int MOST = FORWARD_STAGES<N, THREADS> * 2 * N * 16 * THREADS;
+    constexpr int MOST = STAGES * 2 * N * 16 * THREADS;
     static_assert(MOST <= 226 * 1024, "shared memory of an SM");
-    const cudaError_t e = allow_smem<k_norm_forward<T, W, N, BIAS, RING, THREADS>, MOST>();
+    const cudaError_t e = allow_smem<KERN, MOST>();
     if (e != cudaSuccess) return e;
-    smem = FORWARD_STAGES<N, THREADS> * (q.r != nullptr ? 2 : 1) * N * threads * 16;
+    smem = STAGES * (q.r != nullptr ? 2 : 1) * N * threads * 16;
   }
-  k_norm_forward<T, W, N, BIAS, RING, THREADS><<<s.ctas, threads, smem, st>>>(q);
+  set_ctas(s, q.rows, 1, ctas_per_sm<KERN>(threads, smem));
+  KERN<<<s.ctas, threads, smem, st>>>(q);
   return cudaGetLastError();
 }
-template <typename T, bool BIAS>
-cudaError_t forward_typed(const NormArgs& q, bool vec, cudaStream_t st) {
-  constexpr int W = 16 / (int)sizeof(T);
-  // Few rows: 8 elements a thread, so that a row's loads and sums are spread over most threads.
-  if (q.rows <= 2 * sm_count() && q.d <= 8 * 1024)
-    return vec ? forward_as<T, W, 8 / W, BIAS, false, 1024>(q, st) : forward_as<T, 1, 8, BIAS, false, 1024>(q, st);
-  if (q.d <= 16 * 512) return vec ? forward_as<T, W, 16 / W, BIAS, true, 512>(q, st) : forward_as<T, 1, 16, BIAS, false, 512>(q, st);
-  if (q.d <= 16 * 1024 && vec) return forward_as<T, W, 16 / W, BIAS, true, 1024>(q, st);
-  if (q.d <= 32 * 512) return forward_as<T, 1, 32, BIAS, false, 512>(q, st);
-  return vec ? forward_as<T, W, 32 / W, BIAS, false, 1024>(q, st) : forward_as<T, 1, 32, BIAS, false, 1024>(q, st);
+// Elements a thread: 8 where there are few rows (a row's loads and sums spread over most threads), where rows are short, and where
+// they are read by elements (the next row then fits the registers); 16 in rings; 32 where 1024 threads have to hold a longer row.
+template <typename T, int W, bool BIAS>
+cudaError_t forward_by(const NormArgs& q, cudaStream_t st) {
+  constexpr bool VEC = W * sizeof(T) == 16;
+  if (q.d <= 256 || (q.d <= 8192 && (!VEC || q.rows <= 2 * sm_count()))) return forward_as<T, W, 8, BIAS, false, 1024>(q, st);
+  if constexpr (VEC) {
+    if (q.d <= 8192) return q.rms ? forward_as<T, W, 16, BIAS, true, 512>(q, st) : forward_as<T, W, 16, BIAS, true, 512, 2>(q, st);
+    if (q.d <= 16384) return forward_as<T, W, 16, BIAS, true, 1024>(q, st);
+  }
+  return forward_as<T, W, 32, BIAS, false, 1024>(q, st);
 }
 
-template <typename T, int W, int N, bool BIAS, int THREADS>
-cudaError_t backward_as(const NormArgs& a, const NormShape& s, cudaStream_t st) {
-  constexpr bool RING = W * sizeof(T) == 16 && THREADS <= 512;
+// The backward pass: threads an SM is given (of 64 or 128 registers), and rows a group takes at least: a group's shares cost the second
+// kernel as much as a few of its rows do here, more where rows are not read by 16 bytes.
+constexpr int backward_threads(int per) { return per <= 8 ? 1024 : 512; }
+int backward_rows(bool vec) { return vec ? 2 * BACKWARD_ROWS : BACKWARD_ROWS; }
+
+template <typename T, int W, int E, bool BIAS, int THREADS>
+cudaError_t backward_as(const NormArgs& a, size_t room, bool* fits, int* groups, cudaStream_t st) {
+  constexpr int N = E / W, STAGES = NORM_STAGES<N, THREADS, E>;
+  constexpr bool VEC = W * sizeof(T) == 16, LONG = THREADS > 512 && E >= 16;
+  constexpr bool RING = VEC && (!LONG || (E == 16 && sizeof(T) == 2));
+  constexpr auto KERN = k_norm_backward<T, W, N, BIAS, RING, THREADS>;
   NormArgs q = a;
-  q.warps = s.warps;
+  NormShape s = norm_shape(q.rows, q.d, E, backward_rows(VEC));
   const int threads = 32 * s.warps * s.groups_per_cta;
-  int smem = 0;
-  if constexpr (RING) {
-    constexpr int MOST = NORM_STAGES<N> * 3 * N * 16 * THREADS;
-    static_assert(MOST <= 226 * 1024, "shared memory of an SM");
-    const cudaError_t e = allow_smem<k_norm_backward<T, W, N, BIAS, RING, THREADS>, MOST>();
+  set_ctas(s, q.rows, backward_rows(VEC), backward_threads(E) / threads);
+  q.warps = s.warps;
+  *groups = s.ctas * s.groups_per_cta;
+  *fits = (size_t)*groups * (q.want_w + q.want_b) * q.d * 4 <= room;
+  if (!*fits) return cudaSuccess;
+  constexpr int ACC = LONG ? 4 * (BIAS ? 2 : 1) : 0;                    // bytes a column
+  constexpr int MOST = (RING ? STAGES * 3 * N * 16 * THREADS : 0) + ACC * (E * THREADS < NORM_MAX_D ? E * THREADS : BIAS ? NORM_BOTH_D : NORM_MAX_D);
+  static_assert(MOST <= 226 * 1024, "shared memory of an SM");
+  const int smem = (RING ? STAGES * (q.r != nullptr ? 3 : 2) * N * threads * 16 : 0) + (q.d <= NORM_BOTH_D ? ACC : ACC > 0 ? 4 : 0) * E * threads;
+  if constexpr (MOST > 0) {
+    const cudaError_t e = allow_smem<KERN, MOST>();
     if (e != cudaSuccess) return e;
-    smem = NORM_STAGES<N> * (q.r != nullptr ? 3 : 2) * N * threads * 16;
   }
-  return launch_chained(k_norm_backward<T, W, N, BIAS, RING, THREADS>, q, s.ctas, 1, 1, threads, smem, false, st);
+  return launch_chained(KERN, q, s.ctas, 1, 1, threads, smem, false, st);
+}
+template <typename T, int W, bool BIAS>
+cudaError_t backward_by(const NormArgs& q, size_t room, bool* fits, int* groups, cudaStream_t st) {
+  constexpr bool VEC = W * sizeof(T) == 16;
+  if constexpr (VEC) {
+    if (q.d <= 256) return backward_as<T, W, 8, BIAS, 256>(q, room, fits, groups, st);
+    if (q.d <= 8192) return backward_as<T, W, 16, BIAS, 512>(q, room, fits, groups, st);
+    if (q.d <= 16384) return backward_as<T, W, 16, BIAS, 1024>(q, room, fits, groups, st);
+  } else {
+    if (q.d <= 128) return backward_as<T, W, 4, BIAS, 1024>(q, room, fits, groups, st);
+    if (q.d <= 8192) return backward_as<T, W, 8, BIAS, 1024>(q, room, fits, groups, st);
+  }
+  return backward_as<T, W, 32, BIAS, 1024>(q, room, fits, groups, st);
+}
+
+// Shares of any alignment, and no fewer bytes for more rows, so that a workspace serves every smaller call: groups are what the rows
+// ask for, rounded up to whole CTAs, or as many as the GPU holds at one time.
+size_t norm_part_bound(int64_t rows, int d) {
+  // of 8 elements a thread, or of 16
+  const int short_sm = backward_threads(8) / 32 / ((d + 255) / 256), long_sm = backward_threads(16) / 32 / ((d + 511) / 512);
+  const int most_sm = short_sm > long_sm ? short_sm : long_sm;
+  const int64_t want = (rows + BACKWARD_ROWS - 1) / BACKWARD_ROWS + NORM_GROUP_THREADS / 32, most = (int64_t)sm_count() * (most_sm > 1 ? most_sm : 1);
+  return (size_t)(want < most ? want : most) * 2 * d * 4;
+}
+
+// How all matrices of a call can be accessed; p and ld of each (p null: none), and the weights.
+struct Rows { const void* p; long long ld; };
+template <int K>
+int access_of(const Rows (&m)[K], int d, int size, const void* w, const void* b, int w_size) {
+  bool by16 = (d * size) % 16 == 0, by2 = d % 2 == 0;
+  for (const Rows& r : m) {
+    by16 = by16 && rows_on(r.p, r.ld, size, 16);
+    by2 = by2 && rows_on(r.p, r.ld, size, 2 * size);
+  }
+  by16 = by16 && rows_on(w, 0, 1, 16) && rows_on(b, 0, 1, 16);
+  by2 = by2 && rows_on(w, 0, 1, 2 * w_size) && rows_on(b, 0, 1, 2 * w_size);
+  return by16 ? BY_16 : by2 ? BY_TWO : BY_ONE;
+}
+
+template <typename T, bool BIAS>
+cudaError_t forward_any(const NormArgs& q, int access, cudaStream_t st) {
+  return access == BY_16 ? forward_by<T, 16 / (int)sizeof(T), BIAS>(q, st) : access == BY_TWO ? forward_by<T, 2, BIAS>(q, st) : forward_by<T, 1, BIAS>(q, st);
 }
 template <typename T, bool BIAS>
-cudaError_t backward_typed(const NormArgs& q, const NormShape& s, bool vec, cudaStream_t st) {
-  constexpr int W = 16 / (int)sizeof(T);
-  if (backward_per(q.d) == 16) return vec ? backward_as<T, W, 16 / W, BIAS, 512>(q, s, st) : backward_as<T, 1, 16, BIAS, 512>(q, s, st);
-  if (s.warps <= 16) return vec ? backward_as<T, W, 32 / W, BIAS, 512>(q, s, st) : backward_as<T, 1, 32, BIAS, 512>(q, s, st);
-  return vec ? backward_as<T, W, 32 / W, BIAS, 1024>(q, s, st) : backward_as<T, 1, 32, BIAS, 1024>(q, s, st);
+cudaError_t backward_any(const NormArgs& q, int access, size_t room, bool* fits, int* groups, cudaStream_t st) {
+  return access == BY_16 ? backward_by<T, 16 / (int)sizeof(T), BIAS>(q, room, fits, groups, st)
+       : access == BY_TWO ? backward_by<T, 2, BIAS>(q, room, fits, groups, st)
+                          : backward_by<T, 1, BIAS>(q, room, fits, groups, st);
 }
 
 int check_norm(const camera_norm_t* n) {
@@ -504,15 +641,6 @@ bool rows_ok(const void* p, long long ld, const camera_norm_t* n) {
     }                           \
   } while (0)
 
-size_t norm_part_bytes(const NormShape& s, int d) { return (size_t)s.ctas * s.groups_per_cta * 2 * d * 4; }
-// At least that for any alignment, and no less for more rows, so that a workspace serves every smaller call: groups are what the rows
-// ask for, rounded up to whole CTAs, or as many as the GPU holds at one time.
-size_t norm_part_bound(int64_t rows, int d) {
-  const int warps = (d + 32 * backward_per(d) - 1) / (32 * backward_per(d));
-  const int64_t want = (rows + BACKWARD_ROWS - 1) / BACKWARD_ROWS + NORM_GROUP_THREADS / 32, most = (int64_t)sm_count() * (BACKWARD_THREADS / 32 / warps > 1 ? BACKWARD_THREADS / 32 / warps : 1);
-  return (size_t)(want < most ? want : most) * 2 * d * 4;
-}
-
 }  // namespace
 }  // namespace camera
 
@@ -534,11 +662,10 @@ extern "C" int camera_norm_forward(const camera_norm_t* n, const void* residual,
   q.w = n->weight; q.b = n->bias; q.w_f32 = n->weight_dtype == CAMERA_F32;
   q.rms = n->flags & CAMERA_NORM_RMS; q.eps = n->eps; q.mean = mean; q.rstd = rstd;
   const int size = n->dtype == CAMERA_BF16 ? 2 : 4;
-  const bool vec = (n->d * size) % 16 == 0 && vec_ok(q.x, q.x_ld, size) && vec_ok(q.r, q.r_ld, size) && vec_ok(q.sum, q.sum_ld, size) &&
-                   vec_ok(q.y, q.y_ld, size) && vec_ok(q.w, 0, 1) && vec_ok(q.b, 0, 1);
+  const int access = access_of({Rows{q.x, q.x_ld}, Rows{q.r, q.r_ld}, Rows{q.sum, q.sum_ld}, Rows{q.y, q.y_ld}}, q.d, size, q.w, q.b, q.w_f32 ? 4 : 2);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (size == 2) NORM_CK(q.b != nullptr ? forward_typed<__nv_bfloat16, true>(q, vec, st) : forward_typed<__nv_bfloat16, false>(q, vec, st));
-  else NORM_CK(q.b != nullptr ? forward_typed<float, true>(q, vec, st) : forward_typed<float, false>(q, vec, st));
+  if (size == 2) NORM_CK(q.b != nullptr ? forward_any<__nv_bfloat16, true>(q, access, st) : forward_any<__nv_bfloat16, false>(q, access, st));
+  else NORM_CK(q.b != nullptr ? forward_any<float, true>(q, access, st) : forward_any<float, false>(q, access, st));
   return CAMERA_OK;
 }
 
@@ -576,15 +703,19 @@ extern "C" int camera_norm_backward(const camera_norm_t* n, const void* dy, int6
   q.rms = rms; q.mean = const_cast<float*>(mean); q.rstd = const_cast<float*>(rstd);
   q.part = static_cast<float*>(workspace); q.want_w = d_weight != nullptr; q.want_b = d_bias != nullptr;
   const int size = n->dtype == CAMERA_BF16 ? 2 : 4;
-  const bool vec = (n->d * size) % 16 == 0 && vec_ok(q.x, q.x_ld, size) && vec_ok(q.r, q.r_ld, size) && vec_ok(q.dy, q.dy_ld, size) &&
-                   vec_ok(q.y, q.y_ld, size) && vec_ok(q.w, 0, 1);
-  const NormShape s = backward_shape(q.rows, q.d, vec);
-  if (want_w && (workspace == nullptr || workspace_bytes < norm_part_bytes(s, q.d) || (reinterpret_cast<uintptr_t>(workspace) & 255)))
-    return CAMERA_ERR_WORKSPACE;
-  if (size == 2) NORM_CK(q.want_b ? backward_typed<__nv_bfloat16, true>(q, s, vec, st) : backward_typed<__nv_bfloat16, false>(q, s, vec, st));
-  else NORM_CK(q.want_b ? backward_typed<float, true>(q, s, vec, st) : backward_typed<float, false>(q, s, vec, st));
+  const int access = access_of({Rows{q.x, q.x_ld}, Rows{q.r, q.r_ld}, Rows{q.dy, q.dy_ld}, Rows{q.y, q.y_ld}}, q.d, size, q.w, nullptr, q.w_f32 ? 4 : 2);
+  if (want_w && (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255))) return CAMERA_ERR_WORKSPACE;
+  bool fits = false;
+  int groups = 0;
+  if (size == 2)
+    NORM_CK(q.want_b ? backward_any<__nv_bfloat16, true>(q, access, workspace_bytes, &fits, &groups, st)
+                     : backward_any<__nv_bfloat16, false>(q, access, workspace_bytes, &fits, &groups, st));
+  else
+    NORM_CK(q.want_b ? backward_any<float, true>(q, access, workspace_bytes, &fits, &groups, st)
+                     : backward_any<float, false>(q, access, workspace_bytes, &fits, &groups, st));
+  if (!fits) return CAMERA_ERR_WORKSPACE;
   if (want_w) {
-    const NormReduce r = {q.part, s.ctas * s.groups_per_cta, q.d, q.want_w + q.want_b, d_weight, d_bias};
+    const NormReduce r = {q.part, groups, q.d, q.want_w + q.want_b, d_weight, d_bias};
     NORM_CK(launch_chained(k_norm_reduce, r, (q.d + 31) / 32, r.wanted, 1, 32 * REDUCE_WARPS, 0, true, st));
   }
   return CAMERA_OK;

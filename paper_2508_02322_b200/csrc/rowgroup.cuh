@@ -118,9 +118,11 @@ __device__ __forceinline__ void group_sum(float (&v)[K], int warps, int group, i
   buf ^= 1;
 }
 
-// Whether rows from p, ld elements of `size` bytes apart, all start on 16-byte boundaries.
-inline bool vec_ok(const void* p, long long ld, int size) {
-  return p == nullptr || ((reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld * size) % 16 == 0);
+// Whether rows from p, ld elements of `size` bytes apart, all start on boundaries of `unit` bytes.
+inline bool rows_on(const void* p, long long ld, int size, int unit) {
+  return p == nullptr || ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) & (uintptr_t)(unit - 1)) == 0;
 }
+// How a call's rows can be accessed: 16 bytes at a time, two elements, or one.
+enum { BY_16 = 0, BY_TWO = 1, BY_ONE = 2 };
 
 }  // namespace camera
