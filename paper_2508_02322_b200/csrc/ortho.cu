@@ -177,6 +177,25 @@ __device__ __forceinline__ bool wait_done(const int* done, int need, volatile in
   return true;
 }
 
+// The same within a CTA: until its producer has seen the operands of its k-th unit.  A poller per CTA instead of nine lets the
+// reports through sooner (7 matrices of 1487 x 245: 170 -> XXX us).
+__device__ __forceinline__ bool wait_seen(uint32_t seen, int k, volatile int* abort_flag) {
+  unsigned long long t0 = 0;
+  for (unsigned spins = 0;; ++spins) {
+    int v;
+    asm volatile("ld.acquire.cta.shared.s32 %0, [%1];" : "=r"(v) : "r"(seen) : "memory");
+    if (v > k) break;
+    if (spins == 0) t0 = globaltimer_ns();
+    if ((spins & 15u) == 15u) {
+      if (*abort_flag) return false;
+      if (globaltimer_ns() - t0 > wait_limit_ns(abort_flag)) { *abort_flag = 1; return false; }
+    }
+    __nanosleep(32);
+  }
+  asm volatile("fence.proxy.async;" ::: "memory");
+  return true;
+}
+
 __device__ __forceinline__ uint32_t pack_half(float a, float b) {
   const __half2 v = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&v);
@@ -206,6 +225,25 @@ __device__ __forceinline__ void store_turned(uint16_t* at, long long ld, const u
   }
 }
 
+// A box of 32 x 32 elements in shared memory (64-byte swizzle) to rows of `to` that are ld elements apart, V's size at a time, so that
+// the lanes store whole runs of a row.
+template <typename V>
+__device__ __forceinline__ void box_out(uint16_t* to, long long ld, uint32_t box, int lane, int rows, int cols) {
+  constexpr int E = sizeof(V) / 2, LANES = O_CHUNK / E;          // elements a lane stores, lanes a row
+  const int c = lane % LANES * E;
+  if (c >= cols) return;
+#pragma unroll
+  for (int r = lane / LANES; r < 32; r += 32 / LANES) {
+    if (r >= rows) break;
+    const uint32_t at = box + r * (2 * O_CHUNK) + (((c >> 3) ^ (r >> 1 & 3)) << 4) + 2 * (c & 7);
+    V v;
+    if constexpr (E == 8) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    else if constexpr (E == 2) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at));
+    else asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(at));
+    *reinterpret_cast<V*>(to + r * ld + c) = v;
+  }
+}
+
 template <int M> struct Mode { static constexpr int value = M; };
 
 // All products of all steps in one launch: CTAs stay, and a unit starts when the units it depends on have been reported finished (a
@@ -224,6 +262,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
   volatile uint32_t* const tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(tail + 8);
 
+  volatile int* const seen = reinterpret_cast<volatile int*>(tail + 32);                    // units whose operands are there
+
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const uint32_t rank = cluster_ctarank();
   const int n_pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
@@ -237,6 +277,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
     for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 2 * 32 * O_EPI_WARPS); }
     for (int i = 0; i < O_EPI_WARPS * O_BUFS; ++i) mbar_init(aux_bar(i), 1);
     wait_state_init(abort_flag, q.wait_limit_ns);
+    *seen = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -258,7 +299,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
+    for (int unit = pair, k = 0; ok && unit < q.n_units; unit += n_pairs) {
       const OrthoUnit u = ortho_unit(q, unit);
       const int row0 = q.batch.mat[u.e].row0;
       const int am = row0 + u.m0 + 128 * (int)rank, bn0 = u.n0 + half * (int)rank;
@@ -267,6 +308,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
       const CUtensorMap* const map_a = &from.rows128;
       const CUtensorMap* const map_b = B_MN ? &q.maps[u.step & 1].rows64 : half > 64 ? &from.rows128 : &from.rows64;
       ok = __all_sync(0xffffffffu, lane != 0 || wait_done(q.done + u.e, u.need, abort_flag));
+      if (ok && lane == 0) asm volatile("st.release.cta.shared.s32 [%0], %1;" ::"r"(smem_u32((const void*)seen)), "r"(++k) : "memory");
       for (int kb = 0, blocks; ok && kb < u.kb; kb += blocks) {
         blocks = min(q.kps, u.kb - kb);
         ok = warp_wait(empty_bar(stage), phase ^ 1u, abort_flag);
@@ -365,7 +407,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
     uint8_t* const bufs = base_ptr + O_RING_BYTES + warp * O_BUFS * O_BUF_BYTES;
     [[maybe_unused]] float* const rests = reinterpret_cast<float*>(base_ptr + O_RING_BYTES + O_EPI_BYTES) + 256 * warp;
     const uint32_t buf0 = smem_u32(bufs), swz = (uint32_t)(lane >> 1) & 3u;       // 64-byte swizzle: 16-byte piece i of a row at i ^ swz
-    auto unit_done = [&](auto mode, const OrthoUnit& u) {           // false: a wait ran out
+    auto unit_done = [&](auto mode, const OrthoUnit& u, int k) {    // the k-th of this CTA; false: a wait ran out
       constexpr int MODE = decltype(mode)::value;
       const OrthoStep& st = q.step[u.step];
       const bool to_caller = MODE == ORTHO_APPLY && u.step + 1 == q.n_steps;
@@ -375,14 +417,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
       const CUtensorMap* const aux_map = &q.maps[MODE == ORTHO_POLY ? BUF_A : u.step & 1].box;
       const CUtensorMap* const out_map = &q.maps[MODE == ORTHO_GRAM ? BUF_A : MODE == ORTHO_POLY ? BUF_B : (u.step + 1) & 1].box;
       __half* const out_rows = q.out[MODE == ORTHO_POLY];
+      // read while the products run: the first use of an argument costs a microsecond (POLY's epilogue of one tile: 3.5 us and XXX)
+      float f_aux = MODE == ORTHO_POLY ? st.f_aux : 0.f, f_diag = MODE == ORTHO_POLY ? st.f_diag : 0.f;
+      const float* rest_in = q.rest[MODE == ORTHO_APPLY] + mat.row0;
+      float* rest_out = q.rest[MODE == ORTHO_POLY] + mat.row0;
+      asm volatile("" : "+f"(f_aux), "+f"(f_diag), "+l"(rest_in), "+l"(rest_out));
+      uint16_t* const out = static_cast<uint16_t*>(mat.out);
       float f = MODE == ORTHO_GRAM ? st.f_gram : MODE == ORTHO_POLY ? st.f_poly : st.f_apply;
       if (MODE != ORTHO_POLY) {
         const int small = q.small[u.e];
         const float s = u.step == 0 ? q.first[u.e] : scalbnf(1.f, scale_of(small, st.small_in));
         f = MODE == ORTHO_GRAM ? f / s / s : scalbnf(f / s, to_caller ? 0 : scale_of(small, st.small_out));
       }
-      if (MODE != ORTHO_GRAM && !__all_sync(0xffffffffu, lane != 0 || wait_done(q.done + u.e, u.need, abort_flag))) return false;
-      const float* const rest_in = q.rest[MODE == ORTHO_APPLY] + mat.row0;
+      if (MODE != ORTHO_GRAM && !__all_sync(0xffffffffu, lane != 0 || wait_seen(smem_u32((const void*)seen), k, abort_flag))) return false;
       const float rest = MODE == ORTHO_GRAM ? 0.f : __ldcg(rest_in + row);
       auto fetch = [&](int c, uint32_t k) {                        // lane 0: the k-th box from here, at column c, on its way
         if (MODE != ORTHO_GRAM && c < cols) {
@@ -426,7 +473,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
               split(mul2(fma2(f2(rest, rest), old2, sum), f_2), v[j], v[j + 1]);
             } else {                                    // (A + rest)^2 up to the square of the rest, and b A (b rest: below)
               const float2 down = *reinterpret_cast<const float2*>(rests + c - c_first + j);
-              split(fma2(old2, f2(st.f_aux, st.f_aux), mul2(fma2(add2(f2(rest, rest), f2(down.x, down.y)), old2, sum), f_2)), v[j], v[j + 1]);
+              split(fma2(old2, f2(f_aux, f_aux), mul2(fma2(add2(f2(rest, rest), f2(down.x, down.y)), old2, sum), f_2)), v[j], v[j + 1]);
             }
           }
         }
@@ -434,32 +481,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
           // the result, in the caller's layout
 #pragma unroll
           for (int j = 0; j < 8; ++j) p[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
-          const int left = mat.n - u.n0 - c;                        // columns there are
-          uint16_t* const out = static_cast<uint16_t*>(mat.out);
           if (mat.turned) {
-            uint16_t* const to = out + (long long)(u.n0 + c) * mat.out_ld + warp_row;
-            store_turned(to, mat.out_ld, p, lane, mat.m - warp_row, left,
+            store_turned(out + (long long)(u.n0 + c) * mat.out_ld + warp_row, mat.out_ld, p, lane, mat.m - warp_row, mat.n - u.n0 - c,
                          ((reinterpret_cast<uintptr_t>(out) & 3) | (mat.out_ld & 1)) == 0);
-          } else if (row < mat.m) {
-            uint16_t* const to = out + row * mat.out_ld + u.n0 + c;
-            if (left >= 16 && (reinterpret_cast<uintptr_t>(to) & 31) == 0) {
-              st_global_v8(to, p);
-            } else {
-#pragma unroll
-              for (int j = 0; j < 16; ++j)
-                if (j < left) to[j] = (uint16_t)(j & 1 ? p[j >> 1] >> 16 : p[j >> 1] & 0xffffu);
-            }
+          } else {
+            *piece0 = make_uint4(p[0], p[1], p[2], p[3]);
+            *piece1 = make_uint4(p[4], p[5], p[6], p[7]);
           }
           return;
         }
         if (MODE != ORTHO_APPLY && u.n0 + c < warp_row + 32 && u.n0 + c + 16 > warp_row) {
-          // on the diagonal: what its rounding leaves is kept
+          // on the diagonal: what its rounding leaves is kept (by selections: 16 branches that one lane each takes cost 0.7 us)
+          const int own = row - u.n0 - c;
+          float mine = 0.f;
 #pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (u.n0 + c + j == row) {
-              if (MODE == ORTHO_POLY) v[j] += fmaf(rest, st.f_aux, st.f_diag);
-              q.rest[MODE == ORTHO_POLY][mat.row0 + row] = v[j] - __half2float(__float2half_rn(v[j]));
-            }
+          for (int j = 0; j < 16; ++j) mine = j == own ? v[j] : mine;
+          if (MODE == ORTHO_POLY) mine += fmaf(rest, f_aux, f_diag);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j] = j == own ? mine : v[j];
+          if (own >= 0 && own < 16) rest_out[row] = mine - __half2float(__float2half_rn(mine));
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) p[j] = pack_half(v[2 * j], v[2 * j + 1]);
@@ -485,6 +525,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
         put(v1, 1, c + 16);
         if (!to_caller) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
+        if (to_caller && !mat.turned) {
+          // the box's rows as they lie in memory: by 16 bytes, by two elements or by one
+          uint16_t* const to = out + warp_row * mat.out_ld + u.n0 + c;
+          const uint32_t from = buf0 + box * O_BUF_BYTES;
+          const int rows = mat.m - warp_row, left = mat.n - u.n0 - c;
+          const unsigned on = (unsigned)reinterpret_cast<uintptr_t>(out) | 2u * (unsigned)mat.out_ld | 2u * (unsigned)mat.n;
+          if ((on & 15u) == 0) box_out<uint4>(to, mat.out_ld, from, lane, rows, left);
+          else if ((on & 3u) == 0) box_out<uint32_t>(to, mat.out_ld, from, lane, rows, left);
+          else box_out<uint16_t>(to, mat.out_ld, from, lane, rows, left);
+        }
         if (lane == 0) {
           if (!to_caller) {
             asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(out_map),
@@ -503,19 +553,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
       if (++acc == q.n_acc) { acc = 0; acc_phase ^= 1u; }
       // While the next unit's products run: what this warp wrote (boxes, mirrored words, rests) is there for everybody.
       if (!to_caller) {
+        __syncwarp();
         if (lane == 0) {
           asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
           asm volatile("fence.proxy.async;" ::: "memory");
+          asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(q.done + u.e) : "memory");
         }
-        __threadfence();
-        __syncwarp();
-        if (lane == 0) asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(q.done + u.e) : "memory");
       }
       return true;
     };
-    for (int unit = pair; ok && unit < q.n_units; unit += n_pairs) {
+    for (int unit = pair, k = 0; ok && unit < q.n_units; unit += n_pairs, ++k) {
       const OrthoUnit u = ortho_unit(q, unit);
-      ok = u.mode == ORTHO_GRAM ? unit_done(Mode<ORTHO_GRAM>(), u) : u.mode == ORTHO_POLY ? unit_done(Mode<ORTHO_POLY>(), u) : unit_done(Mode<ORTHO_APPLY>(), u);
+      ok = u.mode == ORTHO_GRAM   ? unit_done(Mode<ORTHO_GRAM>(), u, k)
+           : u.mode == ORTHO_POLY ? unit_done(Mode<ORTHO_POLY>(), u, k)
+                                  : unit_done(Mode<ORTHO_APPLY>(), u, k);
     }
     if (!ok) {               // boxes on their way land before the CTA's shared memory is given up
       const unsigned long long t0 = globaltimer_ns();
