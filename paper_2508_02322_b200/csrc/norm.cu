@@ -6,6 +6,8 @@
 // A row is held in the registers of a group of warps: it is read once, the sums are taken in two passes over registers
 // (the second around the mean, so that a large mean costs no digits), and the next row of the group is on its way
 // meanwhile.  All sums are fp32.
+// Bound: HBM.  16384 x 3584 bf16, root mean square, with residual: forward 87 us, backward with d_sum and weight gradient 83 us, 470 MB
+// each, 5.4 and 5.7 TB/s (copy 6.5).  One row: 2.5 us, which is a load, two barriers and a store.
 #include "common.cuh"
 #include "launch.cuh"
 #include "rowgroup.cuh"
@@ -37,11 +39,30 @@ struct NormArgs {
   bool w_f32, rms;
   float eps;
   float *mean, *rstd;                      // backward: inputs
-  float* part;                             // backward: [groups][1 or 2][d] shares of dw and db
+  float* part;                             // backward: [CTAs][1 or 2][d] shares of dw and db
   bool want_w, want_b;
 };
 
-template <int W>
+// W elements from p on: at once, or (LOOSE) one by one, from any address.
+template <bool LOOSE, typename T, int W>
+__device__ __forceinline__ Pack<T, W> load_pack(const T* p) {
+  if constexpr (LOOSE && sizeof(T) == 2) {
+    const uint16_t* const e = reinterpret_cast<const uint16_t*>(p);
+    Pack<T, W> v;
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) v.v[i] = (uint32_t)e[2 * i] | (uint32_t)e[2 * i + 1] << 16;
+    return v;
+  } else if constexpr (LOOSE) {
+    Pack<T, W> v;
+#pragma unroll
+    for (int i = 0; i < W; ++i) v.v[i] = p[i];
+    return v;
+  } else {
+    return *reinterpret_cast<const Pack<T, W>*>(p);
+  }
+}
+
+template <bool LOOSE, int W>
 __device__ __forceinline__ void load_weight(const void* p, bool f32, int c, float absent, float (&out)[W]) {
   if (p == nullptr) {
 #pragma unroll
@@ -50,17 +71,17 @@ __device__ __forceinline__ void load_weight(const void* p, bool f32, int c, floa
     constexpr int V = W >= 4 ? 4 : W;
 #pragma unroll
     for (int k = 0; k < W; k += V) {
-      const Pack<float, V> t = *reinterpret_cast<const Pack<float, V>*>(static_cast<const float*>(p) + c + k);
+      const Pack<float, V> t = load_pack<LOOSE, float, V>(static_cast<const float*>(p) + c + k);
 #pragma unroll
       for (int i = 0; i < V; ++i) out[k + i] = t.v[i];
     }
   } else {
-    reinterpret_cast<const Pack<__nv_bfloat16, W>*>(static_cast<const __nv_bfloat16*>(p) + c)->get(out);
+    load_pack<LOOSE, __nv_bfloat16, W>(static_cast<const __nv_bfloat16*>(p) + c).get(out);
   }
 }
 
 // The weights of the columns a thread owns, as pairs; columns past the end have weight 0.
-template <int W, int N>
+template <bool LOOSE, int W, int N>
 __device__ __forceinline__ void own_weights(const void* p, bool f32, int d, int threads, int t, float absent, F2 (&out)[N * W / 2]) {
   float f[N * W];
 #pragma unroll
@@ -69,7 +90,7 @@ __device__ __forceinline__ void own_weights(const void* p, bool f32, int d, int 
     float w[W];
 #pragma unroll
     for (int i = 0; i < W; ++i) w[i] = 0.f;
-    if (c < d) load_weight<W>(p, f32, c, absent, w);
+    if (c < d) load_weight<LOOSE, W>(p, f32, c, absent, w);
 #pragma unroll
     for (int i = 0; i < W; ++i) f[j * W + i] = w[i];
   }
@@ -80,12 +101,12 @@ __device__ __forceinline__ void own_weights(const void* p, bool f32, int d, int 
 // W elements a load (16 bytes, or 1 element where rows or the width are not aligned for that), N loads a thread and matrix.
 // Columns past the end read as zeros.  RING: the next rows travel through shared memory, each thread copying (cp.async) what it
 // will read itself, so that a wait is the thread's own and the rows in flight cost no registers.
-template <typename T, int W, int N, bool BIAS, bool RING, int THREADS, int ROWS>
+template <typename T, int W, int N, bool BIAS, bool RING, bool LOOSE, int THREADS, int ROWS>
 __global__ void __launch_bounds__(THREADS, 1) k_norm_forward(const NormArgs q) {
   using P = Pack<T, W>;
   constexpr int E2 = N * W / 2, STAGES = NORM_STAGES<N, THREADS, N * W>;
   constexpr bool OWN_W = N * W <= 8 || (THREADS <= 512 && N * W <= 16);   // weights in registers, or loaded again for each use
-  constexpr bool AHEAD = !RING && N * W <= 8;                             // the next row waits in registers
+  constexpr bool AHEAD = !RING && (N * W <= 8 || THREADS <= 512);         // the next row waits in registers
   extern __shared__ __align__(16) uint8_t ring[];
   const int threads = 32 * q.warps, group = threadIdx.x / threads, t = threadIdx.x - group * threads;
   const int groups = blockDim.x / threads;
@@ -95,8 +116,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm_forward(const NormArgs q) {
   int buf = 0, stage = 0;
   F2 w[E2], b[BIAS ? E2 : 1];
   if (OWN_W) {
-    own_weights<W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
-    if constexpr (BIAS) own_weights<W, N>(q.b, q.w_f32, q.d, threads, t, 0.f, b);
+    own_weights<LOOSE, W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
+    if constexpr (BIAS) own_weights<LOOSE, W, N>(q.b, q.w_f32, q.d, threads, t, 0.f, b);
   }
   const int parts = r != nullptr ? 2 : 1, line = N * 16 * (int)blockDim.x;
   const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring) + 16 * threadIdx.x;
@@ -124,8 +145,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm_forward(const NormArgs q) {
       const int c = (j * threads + t) * W;
       nx[j] = nr[j] = P();
       if (c < q.d) {
-        nx[j] = *reinterpret_cast<const P*>(x + row * q.x_ld + c);
-        if (r != nullptr) nr[j] = *reinterpret_cast<const P*>(r + row * q.r_ld + c);
+        nx[j] = load_pack<LOOSE, T, W>(x + row * q.x_ld + c);
+        if (r != nullptr) nr[j] = load_pack<LOOSE, T, W>(r + row * q.r_ld + c);
       }
     }
   };
@@ -208,8 +229,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm_forward(const NormArgs q) {
       group_sum(s, q.warps, group, buf);
     }
     if (!OWN_W) {
-      own_weights<W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
-      if constexpr (BIAS) own_weights<W, N>(q.b, q.w_f32, q.d, threads, t, 0.f, b);
+      own_weights<LOOSE, W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
+      if constexpr (BIAS) own_weights<LOOSE, W, N>(q.b, q.w_f32, q.d, threads, t, 0.f, b);
     }
 #pragma unroll
     for (int k = 0; k < ROWS; ++k) {
@@ -235,9 +256,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm_forward(const NormArgs q) {
 }
 
 // A thread keeps the columns it owns for all rows of its group, so their weights and their shares of dw and db stay in its
-// registers (in its own places of shared memory where a row is long); the groups' shares are added up by k_norm_reduce in a fixed
-// order.  Columns past the end read as zeros, which add nothing.  RING as above; without it both passes over a row load it.
-template <typename T, int W, int N, bool BIAS, bool RING, int THREADS>
+// registers (in its own places of shared memory where a row is long); the groups of a CTA add theirs up in shared memory, the CTAs'
+// shares are added up by k_norm_reduce, all in a fixed order (a share per group: 39156 x 90 bf16 37 us, one per CTA 20).  Columns past the end read as zeros, which add nothing.  RING as above; without it both passes over a row load it.
+template <typename T, int W, int N, bool BIAS, bool RING, bool LOOSE, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) k_norm_backward(const NormArgs q) {
   using P = Pack<T, W>;
   constexpr bool LONG = THREADS > 512 && N * W >= 16;
@@ -254,7 +275,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) k_norm_backwa
   const int parts = has_r ? 3 : 2, line = N * 16 * (int)blockDim.x;
   const long long first = (long long)blockIdx.x * groups + group;
   const int wanted = q.want_w + q.want_b;
-  float* const part = q.part + first * wanted * q.d;                   // [groups][wanted][d]
+  float* const part = q.part + (long long)blockIdx.x * wanted * q.d;
   // LONG: pair i of the thread's share of dw at i * blockDim.x + threadIdx.x, db's behind it, or in memory where there is no room
   F2* const acc = reinterpret_cast<F2*>(ring + (RING ? STAGES * parts * line : 0)) + threadIdx.x;
   F2* const acc_b = acc + E2 * blockDim.x;
@@ -275,7 +296,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) k_norm_backwa
         for (int i = 0; i < W; ++i)
           if ((j * threads + t) * W + i < q.d) part_b[(j * threads + t) * W + i] = 0.f;
   } else {
-    own_weights<W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
+    own_weights<LOOSE, W, N>(q.w, q.w_f32, q.d, threads, t, 1.f, w);
   }
   const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring) + 16 * threadIdx.x;
   auto issue = [&](int stage, long long row) {
@@ -304,7 +325,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) k_norm_backwa
       } else {
         const int c = ((j + k) * threads + t) * W;
         v[k] = P();
-        if (c < q.d) v[k] = *reinterpret_cast<const P*>(src[p] + row * ld[p] + c);
+        if (c < q.d) v[k] = load_pack<LOOSE, T, W>(src[p] + row * ld[p] + c);
       }
     }
     to_pairs<P, W, G>(v, out);
@@ -318,7 +339,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) k_norm_backwa
         float v[W];
 #pragma unroll
         for (int i = 0; i < W; ++i) v[i] = 0.f;
-        if (c < q.d) load_weight<W>(q.w, q.w_f32, c, 1.f, v);
+        if (c < q.d) load_weight<LOOSE, W>(q.w, q.w_f32, c, 1.f, v);
 #pragma unroll
         for (int i = 0; i < W; ++i) f[k * W + i] = v[i];
       }
@@ -433,30 +454,42 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) k_norm_backwa
       }
     }
   }
+  float* const shares = reinterpret_cast<float*>(ring);
+  for (int g = 0; g < groups; ++g) {
+    if (groups > 1) __syncthreads();
+    if (g != group) continue;
 #pragma unroll
-  for (int which = 0; which < (BIAS ? 2 : 1); ++which) {
-    if (!(which ? q.want_b : q.want_w)) continue;
-    float* const to = part + (which ? (wanted - 1) * q.d : 0);
-    if (which && far) continue;
-    float f[N * W];
+    for (int which = 0; which < (BIAS ? 2 : 1); ++which) {
+      if (!(which ? q.want_b : q.want_w)) continue;
+      const int at = which ? (wanted - 1) * q.d : 0;
+      if (which && far) continue;
+      float f[N * W];
 #pragma unroll
-    for (int i = 0; i < E2; ++i) {
-      F2 v;
-      if constexpr (LONG) v = (which ? acc_b : acc)[i * blockDim.x];
-      else v = which ? db[BIAS ? i : 0] : dw[i];
-      split(v, f[2 * i], f[2 * i + 1]);
-    }
+      for (int i = 0; i < E2; ++i) {
+        F2 v;
+        if constexpr (LONG) v = (which ? acc_b : acc)[i * blockDim.x];
+        else v = which ? db[BIAS ? i : 0] : dw[i];
+        split(v, f[2 * i], f[2 * i + 1]);
+      }
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int c = (j * threads + t) * W;
-      if (c < q.d) {
-        constexpr int V = W >= 4 ? 4 : W;
+      for (int j = 0; j < N; ++j) {
+        const int c = (j * threads + t) * W;
+        if (c < q.d) {
+          constexpr int V = W >= 4 ? 4 : W;
 #pragma unroll
-        for (int k = 0; k < W; k += V) {
-          Pack<float, V> a;
+          for (int k = 0; k < W; k += V) {
+            Pack<float, V> a;
 #pragma unroll
-          for (int i = 0; i < V; ++i) a.v[i] = f[j * W + k + i];
-          *reinterpret_cast<Pack<float, V>*>(to + c + k) = a;
+            for (int i = 0; i < V; ++i) a.v[i] = f[j * W + k + i];
+            Pack<float, V>* const here = reinterpret_cast<Pack<float, V>*>(shares + at + c + k);
+            if (g > 0) {
+              const Pack<float, V> before = *here;
+#pragma unroll
+              for (int i = 0; i < V; ++i) a.v[i] += before.v[i];
+            }
+            if (g + 1 < groups) *here = a;
+            else *reinterpret_cast<Pack<float, V>*>(part + at + c + k) = a;
+          }
         }
       }
     }
@@ -464,8 +497,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) k_norm_backwa
 }
 
 constexpr int REDUCE_WARPS = 32;
-struct NormReduce { const float* part; int groups, d, wanted; float *dw, *db; };
-// Columns of the groups' shares added up: a lane takes a column, the warps take every 32nd group.
+struct NormReduce { const float* part; int ctas, d, wanted; float *dw, *db; };
+// Columns of the CTAs' shares added up: a lane takes a column, the warps take every 32nd CTA.
 __global__ void __launch_bounds__(32 * REDUCE_WARPS) k_norm_reduce(const NormReduce q) {
   __shared__ float sums[REDUCE_WARPS][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, which = blockIdx.y;
@@ -475,7 +508,7 @@ __global__ void __launch_bounds__(32 * REDUCE_WARPS) k_norm_reduce(const NormRed
   if (c < q.d) {
     const float* p = q.part + (long long)which * q.d + c;
 #pragma unroll 8
-    for (int g = warp; g < q.groups; g += REDUCE_WARPS) s += p[(long long)g * q.wanted * q.d];
+    for (int g = warp; g < q.ctas; g += REDUCE_WARPS) s += p[(long long)g * q.wanted * q.d];
   }
   sums[warp][lane] = s;
   __syncthreads();
@@ -508,10 +541,10 @@ void set_ctas(NormShape& s, long long rows, long long rows_per_group, int per_sm
   s.ctas = (int)(need < most ? need : most);
 }
 
-template <typename T, int W, int E, bool BIAS, bool RING, int THREADS, int ROWS = 1>
+template <typename T, int W, int E, bool BIAS, bool RING, bool LOOSE, int THREADS, int ROWS = 1>
 cudaError_t forward_as(const NormArgs& a, cudaStream_t st) {
   constexpr int N = E / W, STAGES = NORM_STAGES<N, THREADS, E>;
-  constexpr auto KERN = k_norm_forward<T, W, N, BIAS, RING, THREADS, ROWS>;
+  constexpr auto KERN = k_norm_forward<T, W, N, BIAS, RING, LOOSE, THREADS, ROWS>;
   NormArgs q = a;
   NormShape s = norm_shape(q.rows, q.d, E, 1);
   q.warps = s.warps;
@@ -529,16 +562,20 @@ cudaError_t forward_as(const NormArgs& a, cudaStream_t st) {
   return cudaGetLastError();
 }
 // Elements a thread: 8 where there are few rows (a row's loads and sums spread over most threads), where rows are short, and where
-// they are read by elements (the next row then fits the registers); 16 in rings; 32 where 1024 threads have to hold a longer row.
-template <typename T, int W, bool BIAS>
+// they are read by elements (the next row then fits the registers of 1024 threads); 16 in rings, and of loose rows up to where the next
+// row fits the registers of 512 threads; 32 where 1024 threads have to hold a longer row.
+template <typename T, int W, bool LOOSE, bool BIAS>
 cudaError_t forward_by(const NormArgs& q, cudaStream_t st) {
-  constexpr bool VEC = W * sizeof(T) == 16;
-  if (q.d <= 256 || (q.d <= 8192 && (!VEC || q.rows <= 2 * sm_count()))) return forward_as<T, W, 8, BIAS, false, 1024>(q, st);
-  if constexpr (VEC) {
-    if (q.d <= 8192) return q.rms ? forward_as<T, W, 16, BIAS, true, 512>(q, st) : forward_as<T, W, 16, BIAS, true, 512, 2>(q, st);
-    if (q.d <= 16384) return forward_as<T, W, 16, BIAS, true, 1024>(q, st);
+  constexpr bool RING = W * sizeof(T) == 16 && !LOOSE;
+  if (q.d <= 256 || (q.d <= 8192 && ((!RING && !LOOSE) || q.rows <= 2 * sm_count()))) return forward_as<T, W, 8, BIAS, false, LOOSE, 1024>(q, st);
+  if constexpr (LOOSE) {
+    if (q.d <= 8192) return forward_as<T, W, 16, BIAS, false, true, 512>(q, st);
   }
-  return forward_as<T, W, 32, BIAS, false, 1024>(q, st);
+  if constexpr (RING) {
+    if (q.d <= 8192) return q.rms ? forward_as<T, W, 16, BIAS, true, false, 512>(q, st) : forward_as<T, W, 16, BIAS, true, false, 512, 2>(q, st);
+  }
+  if (q.d <= 16384) return forward_as<T, W, 16, BIAS, RING, LOOSE, 1024>(q, st);
+  return forward_as<T, W, 32, BIAS, false, LOOSE, 1024>(q, st);
 }
 
 // The backward pass: threads an SM is given (of 64 or 128 registers), and rows a group takes at least: a group's shares cost the second
@@ -546,46 +583,49 @@ cudaError_t forward_by(const NormArgs& q, cudaStream_t st) {
 constexpr int backward_threads(int per) { return per <= 8 ? 1024 : 512; }
 int backward_rows(bool vec) { return vec ? 2 * BACKWARD_ROWS : BACKWARD_ROWS; }
 
-template <typename T, int W, int E, bool BIAS, int THREADS>
-cudaError_t backward_as(const NormArgs& a, size_t room, bool* fits, int* groups, cudaStream_t st) {
+template <typename T, int W, int E, bool BIAS, bool LOOSE, int THREADS>
+cudaError_t backward_as(const NormArgs& a, size_t room, bool* fits, int* ctas, cudaStream_t st) {
   constexpr int N = E / W, STAGES = NORM_STAGES<N, THREADS, E>;
   constexpr bool VEC = W * sizeof(T) == 16, LONG = THREADS > 512 && E >= 16;
-  constexpr bool RING = VEC && (!LONG || (E == 16 && sizeof(T) == 2));
-  constexpr auto KERN = k_norm_backward<T, W, N, BIAS, RING, THREADS>;
+  constexpr bool RING = VEC && !LOOSE && (!LONG || (E == 16 && sizeof(T) == 2));
+  constexpr auto KERN = k_norm_backward<T, W, N, BIAS, RING, LOOSE, THREADS>;
   NormArgs q = a;
   NormShape s = norm_shape(q.rows, q.d, E, backward_rows(VEC));
   const int threads = 32 * s.warps * s.groups_per_cta;
   set_ctas(s, q.rows, backward_rows(VEC), backward_threads(E) / threads);
   q.warps = s.warps;
-  *groups = s.ctas * s.groups_per_cta;
-  *fits = (size_t)*groups * (q.want_w + q.want_b) * q.d * 4 <= room;
+  *ctas = s.ctas;
+  *fits = (size_t)s.ctas * (q.want_w + q.want_b) * q.d * 4 <= room;
   if (!*fits) return cudaSuccess;
   constexpr int ACC = LONG ? 4 * (BIAS ? 2 : 1) : 0;                    // bytes a column
   constexpr int MOST = (RING ? STAGES * 3 * N * 16 * THREADS : 0) + ACC * (E * THREADS < NORM_MAX_D ? E * THREADS : BIAS ? NORM_BOTH_D : NORM_MAX_D);
   static_assert(MOST <= 226 * 1024, "shared memory of an SM");
-  const int smem = (RING ? STAGES * (q.r != nullptr ? 3 : 2) * N * threads * 16 : 0) + (q.d <= NORM_BOTH_D ? ACC : ACC > 0 ? 4 : 0) * E * threads;
+  // the groups' shares of a CTA take the ring's room, which is larger
+  const int shares = s.groups_per_cta > 1 && !RING ? 4 * (q.want_w + q.want_b) * q.d : 0;
+  static_assert(RING || LONG || 2 * 4 * (NORM_GROUP_THREADS / 2) * E <= 48 * 1024, "what a kernel may use without asking");
+  const int smem = shares + (RING ? STAGES * (q.r != nullptr ? 3 : 2) * N * threads * 16 : 0) + (q.d <= NORM_BOTH_D ? ACC : ACC > 0 ? 4 : 0) * E * threads;
   if constexpr (MOST > 0) {
     const cudaError_t e = allow_smem<KERN, MOST>();
     if (e != cudaSuccess) return e;
   }
   return launch_chained(KERN, q, s.ctas, 1, 1, threads, smem, false, st);
 }
-template <typename T, int W, bool BIAS>
-cudaError_t backward_by(const NormArgs& q, size_t room, bool* fits, int* groups, cudaStream_t st) {
+template <typename T, int W, bool LOOSE, bool BIAS>
+cudaError_t backward_by(const NormArgs& q, size_t room, bool* fits, int* ctas, cudaStream_t st) {
   constexpr bool VEC = W * sizeof(T) == 16;
   if constexpr (VEC) {
-    if (q.d <= 256) return backward_as<T, W, 8, BIAS, 256>(q, room, fits, groups, st);
-    if (q.d <= 8192) return backward_as<T, W, 16, BIAS, 512>(q, room, fits, groups, st);
-    if (q.d <= 16384) return backward_as<T, W, 16, BIAS, 1024>(q, room, fits, groups, st);
+    if (q.d <= 256) return backward_as<T, W, 8, BIAS, LOOSE, 256>(q, room, fits, ctas, st);
+    if (q.d <= 8192) return backward_as<T, W, 16, BIAS, LOOSE, 512>(q, room, fits, ctas, st);
   } else {
-    if (q.d <= 128) return backward_as<T, W, 4, BIAS, 1024>(q, room, fits, groups, st);
-    if (q.d <= 8192) return backward_as<T, W, 8, BIAS, 1024>(q, room, fits, groups, st);
+    if (q.d <= 128) return backward_as<T, W, 4, BIAS, LOOSE, 1024>(q, room, fits, ctas, st);
+    if (q.d <= 8192) return backward_as<T, W, 8, BIAS, LOOSE, 1024>(q, room, fits, ctas, st);
   }
-  return backward_as<T, W, 32, BIAS, 1024>(q, room, fits, groups, st);
+  if (q.d <= 16384) return backward_as<T, W, 16, BIAS, LOOSE, 1024>(q, room, fits, ctas, st);
+  return backward_as<T, W, 32, BIAS, LOOSE, 1024>(q, room, fits, ctas, st);
 }
 
-// Shares of any alignment, and no fewer bytes for more rows, so that a workspace serves every smaller call: groups are what the rows
-// ask for, rounded up to whole CTAs, or as many as the GPU holds at one time.
+// Shares of any alignment, and no fewer bytes for more rows, so that a workspace serves every smaller call: no more CTAs than groups,
+// and those are what the rows ask for, rounded up to whole CTAs, or as many as the GPU holds at one time.
 size_t norm_part_bound(int64_t rows, int d) {
   // of 8 elements a thread, or of 16
   const int short_sm = backward_threads(8) / 32 / ((d + 255) / 256), long_sm = backward_threads(16) / 32 / ((d + 511) / 512);
@@ -594,29 +634,35 @@ size_t norm_part_bound(int64_t rows, int d) {
   return (size_t)(want < most ? want : most) * 2 * d * 4;
 }
 
-// How all matrices of a call can be accessed; p and ld of each (p null: none), and the weights.
+// How the matrices of a call can be accessed; p and ld of each (p null: none), and the weights.  BY_LOOSE: what is written is on 16-byte
+// boundaries, what is read is not; a thread then still takes 16 bytes in a row, read one by one (rows on odd elements, bf16: layer norm
+// of 1354 x 7872 48 us by single elements, 24 so; backward with d_sum and bias, 1259 x 8768, 378 and 73).
+constexpr int BY_LOOSE = BY_ONE + 1;
 struct Rows { const void* p; long long ld; };
-template <int K>
-int access_of(const Rows (&m)[K], int d, int size, const void* w, const void* b, int w_size) {
-  bool by16 = (d * size) % 16 == 0, by2 = d % 2 == 0;
-  for (const Rows& r : m) {
-    by16 = by16 && rows_on(r.p, r.ld, size, 16);
-    by2 = by2 && rows_on(r.p, r.ld, size, 2 * size);
-  }
-  by16 = by16 && rows_on(w, 0, 1, 16) && rows_on(b, 0, 1, 16);
-  by2 = by2 && rows_on(w, 0, 1, 2 * w_size) && rows_on(b, 0, 1, 2 * w_size);
-  return by16 ? BY_16 : by2 ? BY_TWO : BY_ONE;
+template <int K, int L>
+int access_of(const Rows (&in)[K], const Rows (&out)[L], int d, int size, const void* w, const void* b, int w_size) {
+  auto all = [&](const auto& m, int unit) {
+    bool on = true;
+    for (const Rows& r : m) on = on && rows_on(r.p, r.ld, size, unit);
+    return on;
+  };
+  if ((d * size) % 16 == 0 && all(out, 16)) return all(in, 16) && rows_on(w, 0, 1, 16) && rows_on(b, 0, 1, 16) ? BY_16 : BY_LOOSE;
+  return d % 2 == 0 && all(in, 2 * size) && all(out, 2 * size) && rows_on(w, 0, 1, 2 * w_size) && rows_on(b, 0, 1, 2 * w_size) ? BY_TWO : BY_ONE;
 }
 
 template <typename T, bool BIAS>
 cudaError_t forward_any(const NormArgs& q, int access, cudaStream_t st) {
-  return access == BY_16 ? forward_by<T, 16 / (int)sizeof(T), BIAS>(q, st) : access == BY_TWO ? forward_by<T, 2, BIAS>(q, st) : forward_by<T, 1, BIAS>(q, st);
+  return access == BY_16    ? forward_by<T, 16 / (int)sizeof(T), false, BIAS>(q, st)
+       : access == BY_LOOSE ? forward_by<T, 16 / (int)sizeof(T), true, BIAS>(q, st)
+       : access == BY_TWO   ? forward_by<T, 2, false, BIAS>(q, st)
+                            : forward_by<T, 1, false, BIAS>(q, st);
 }
 template <typename T, bool BIAS>
-cudaError_t backward_any(const NormArgs& q, int access, size_t room, bool* fits, int* groups, cudaStream_t st) {
-  return access == BY_16 ? backward_by<T, 16 / (int)sizeof(T), BIAS>(q, room, fits, groups, st)
-       : access == BY_TWO ? backward_by<T, 2, BIAS>(q, room, fits, groups, st)
-                          : backward_by<T, 1, BIAS>(q, room, fits, groups, st);
+cudaError_t backward_any(const NormArgs& q, int access, size_t room, bool* fits, int* ctas, cudaStream_t st) {
+  return access == BY_16    ? backward_by<T, 16 / (int)sizeof(T), false, BIAS>(q, room, fits, ctas, st)
+       : access == BY_LOOSE ? backward_by<T, 16 / (int)sizeof(T), true, BIAS>(q, room, fits, ctas, st)
+       : access == BY_TWO   ? backward_by<T, 2, false, BIAS>(q, room, fits, ctas, st)
+                            : backward_by<T, 1, false, BIAS>(q, room, fits, ctas, st);
 }
 
 int check_norm(const camera_norm_t* n) {
@@ -662,7 +708,7 @@ extern "C" int camera_norm_forward(const camera_norm_t* n, const void* residual,
   q.w = n->weight; q.b = n->bias; q.w_f32 = n->weight_dtype == CAMERA_F32;
   q.rms = n->flags & CAMERA_NORM_RMS; q.eps = n->eps; q.mean = mean; q.rstd = rstd;
   const int size = n->dtype == CAMERA_BF16 ? 2 : 4;
-  const int access = access_of({Rows{q.x, q.x_ld}, Rows{q.r, q.r_ld}, Rows{q.sum, q.sum_ld}, Rows{q.y, q.y_ld}}, q.d, size, q.w, q.b, q.w_f32 ? 4 : 2);
+  const int access = access_of({Rows{q.x, q.x_ld}, Rows{q.r, q.r_ld}}, {Rows{q.sum, q.sum_ld}, Rows{q.y, q.y_ld}}, q.d, size, q.w, q.b, q.w_f32 ? 4 : 2);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (size == 2) NORM_CK(q.b != nullptr ? forward_any<__nv_bfloat16, true>(q, access, st) : forward_any<__nv_bfloat16, false>(q, access, st));
   else NORM_CK(q.b != nullptr ? forward_any<float, true>(q, access, st) : forward_any<float, false>(q, access, st));
@@ -703,19 +749,19 @@ extern "C" int camera_norm_backward(const camera_norm_t* n, const void* dy, int6
   q.rms = rms; q.mean = const_cast<float*>(mean); q.rstd = const_cast<float*>(rstd);
   q.part = static_cast<float*>(workspace); q.want_w = d_weight != nullptr; q.want_b = d_bias != nullptr;
   const int size = n->dtype == CAMERA_BF16 ? 2 : 4;
-  const int access = access_of({Rows{q.x, q.x_ld}, Rows{q.r, q.r_ld}, Rows{q.dy, q.dy_ld}, Rows{q.y, q.y_ld}}, q.d, size, q.w, nullptr, q.w_f32 ? 4 : 2);
+  const int access = access_of({Rows{q.x, q.x_ld}, Rows{q.r, q.r_ld}, Rows{q.dy, q.dy_ld}}, {Rows{q.y, q.y_ld}}, q.d, size, q.w, nullptr, q.w_f32 ? 4 : 2);
   if (want_w && (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255))) return CAMERA_ERR_WORKSPACE;
   bool fits = false;
-  int groups = 0;
+  int ctas = 0;
   if (size == 2)
-    NORM_CK(q.want_b ? backward_any<__nv_bfloat16, true>(q, access, workspace_bytes, &fits, &groups, st)
-                     : backward_any<__nv_bfloat16, false>(q, access, workspace_bytes, &fits, &groups, st));
+    NORM_CK(q.want_b ? backward_any<__nv_bfloat16, true>(q, access, workspace_bytes, &fits, &ctas, st)
+                     : backward_any<__nv_bfloat16, false>(q, access, workspace_bytes, &fits, &ctas, st));
   else
-    NORM_CK(q.want_b ? backward_any<float, true>(q, access, workspace_bytes, &fits, &groups, st)
-                     : backward_any<float, false>(q, access, workspace_bytes, &fits, &groups, st));
+    NORM_CK(q.want_b ? backward_any<float, true>(q, access, workspace_bytes, &fits, &ctas, st)
+                     : backward_any<float, false>(q, access, workspace_bytes, &fits, &ctas, st));
   if (!fits) return CAMERA_ERR_WORKSPACE;
   if (want_w) {
-    const NormReduce r = {q.part, groups, q.d, q.want_w + q.want_b, d_weight, d_bias};
+    const NormReduce r = {q.part, ctas, q.d, q.want_w + q.want_b, d_weight, d_bias};
     NORM_CK(launch_chained(k_norm_reduce, r, (q.d + 31) / 32, r.wanted, 1, 32 * REDUCE_WARPS, 0, true, st));
   }
   return CAMERA_OK;

@@ -2,8 +2,10 @@
 // (Newton-Schulz products).
 //   X = U / (|U|_F + eps);   each step:  A = X X^T,  B = a I + b A + c A A,  X <- B X
 // X is the matrix with its shorter side as rows (m), its longer as columns (n).  A and B are symmetric: only tiles on and
-// above the diagonal are computed, each stored twice.  A step is m^2 n + m^3 + 2 m^2 n operations, so all of this is bound by
-// the tensor pipe where matrices are large, and by the number of k blocks in a row where they are small.
+// above the diagonal are computed, each stored twice.  A step is m^2 n + m^3 + 2 m^2 n operations.  Bounds: where matrices are large,
+// bringing the operands of the products from L2 to the SMs, to which an epilogue adds its reads and writes (16 matrices of 1408 .. 853
+// x 2048, five steps: 766 GFLOP in 930 us, 0.82 PFLOP/s; a second tile of a unit some k blocks behind the first, so that no epilogue
+// is waited for, changed nothing); where they are small, the chain of products, 5 us each (5 matrices of 241 x 56: 91 us for fifteen).
 //
 // The operands of the products are fp16 with a power of two as factor, the sums fp32.  With h a bound of the singular values
 // of X, no element of X is larger than h, none of A than h^2, none of B than the polynomial's largest value over [0, h^2]: the
@@ -12,8 +14,8 @@
 // values are alike all of it rounds the same way; so what their rounding leaves is kept in fp32 and enters the next product's
 // epilogue (a row of it for B X, a row and a column for A A).  Results are 4e-4 to 9e-4 off 64 bits (root mean square,
 // relative; up to 2.7e-3 without the diagonals' rests, 8e-3 with bf16 operands), below their own rounding to bf16, 1.7e-3.
-// The first X is the matrix itself times a power of two, so bf16 inputs enter
-// exactly; 1 / (|U| + eps) goes into the factors of the first step.
+// The first X is the matrix itself times a power of two, so bf16 inputs enter exactly; 1 / (|U| + eps) goes into the factors of the
+// first step.
 //
 // Matrices of one call lie one below the other in the workspace, padded with zeros to whole tiles of 256 rows and whole
 // 64 columns, so one tensor map serves them all and one launch walks the tiles of them all.
@@ -178,7 +180,7 @@ __device__ __forceinline__ bool wait_done(const int* done, int need, volatile in
 }
 
 // The same within a CTA: until its producer has seen the operands of its k-th unit.  A poller per CTA instead of nine lets the
-// reports through sooner (7 matrices of 1487 x 245: 170 -> XXX us).
+// reports through sooner (7 matrices of 1487 x 245: 174 -> 165 us; polling more often than every 64 ns made it slower).
 __device__ __forceinline__ bool wait_seen(uint32_t seen, int k, volatile int* abort_flag) {
   unsigned long long t0 = 0;
   for (unsigned spins = 0;; ++spins) {
@@ -417,7 +419,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
       const CUtensorMap* const aux_map = &q.maps[MODE == ORTHO_POLY ? BUF_A : u.step & 1].box;
       const CUtensorMap* const out_map = &q.maps[MODE == ORTHO_GRAM ? BUF_A : MODE == ORTHO_POLY ? BUF_B : (u.step + 1) & 1].box;
       __half* const out_rows = q.out[MODE == ORTHO_POLY];
-      // read while the products run: the first use of an argument costs a microsecond (POLY's epilogue of one tile: 3.5 us and XXX)
+      // read while the products run: an argument's first use takes a while (POLY's epilogue of one tile: 3.5 and 2.9 us)
       float f_aux = MODE == ORTHO_POLY ? st.f_aux : 0.f, f_diag = MODE == ORTHO_POLY ? st.f_diag : 0.f;
       const float* rest_in = q.rest[MODE == ORTHO_APPLY] + mat.row0;
       float* rest_out = q.rest[MODE == ORTHO_POLY] + mat.row0;
