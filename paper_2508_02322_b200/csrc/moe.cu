@@ -285,8 +285,8 @@ __global__ void __launch_bounds__(256, U == 1 ? 4 : U == 2 ? 3 : 2) k_moe_combin
 
 // A group of warps takes a token: its row of dy goes, times each weight, to its k rows, and meets the k rows of ys in dot products that
 // stay in registers until the row's end (fp32; a product is rounded once, where it is stored).  S slots at a time, so that dy is read
-// from L2 again only beyond eight.
-template <typename T, int W, int S, int U>
+// from L2 again only beyond eight.  DOTS: with the gradient of the weights; without it nothing is read but dy.
+template <typename T, int W, int S, int U, bool DOTS>
 __global__ void __launch_bounds__(512, 1) k_moe_combine_backward(const Combine q) {
   using P = Pack<T, W>;
   const int threads = 32 * q.warps, group = threadIdx.x / threads, i0 = threadIdx.x - group * threads;
@@ -308,11 +308,11 @@ __global__ void __launch_bounds__(512, 1) k_moe_combine_backward(const Combine q
     }
     const int step = threads * W;
     for (int c0 = i0 * W; c0 < q.d; c0 += U * step) {
-      P g[U], v[S][U];
+      P g[U], v[DOTS ? S : 1][U];
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (c0 + u * step < q.d) g[u] = *reinterpret_cast<const P*>(dy + c0 + u * step);
-      if (q.dw != nullptr) {
+      if constexpr (DOTS) {
 #pragma unroll
         for (int j = 0; j < S; ++j)
           if (row[j] >= 0) {
@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(512, 1) k_moe_combine_backward(const Combine q
           if (row[j] >= 0) {
             P out;
             float f[W];
-            if (q.dw != nullptr) {
+            if constexpr (DOTS) {
               v[j][u].get(f);
 #pragma unroll
               for (int i = 0; i < W; ++i) dot[j] = fmaf(d[i], f[i], dot[j]);
@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(512, 1) k_moe_combine_backward(const Combine q
           }
       }
     }
-    if (q.dw == nullptr) continue;
+    if constexpr (!DOTS) continue;
     group_sum(dot, q.warps, group, buf);
     if (i0 == 0) {
 #pragma unroll
@@ -405,20 +405,26 @@ cudaError_t launch_combine_as(const Combine& q, cudaStream_t st) {
   if constexpr (VEC) return combine_as<T, W, 8, 1>(q, st);
   else return one ? combine_as<T, W, 8, 1>(q, st) : combine_as<T, W, 8, F / 8>(q, st);
 }
-template <typename T, int W, int S, int U>
+template <typename T, int W, int S, int U, bool DOTS = true>
 cudaError_t combine_backward_as(const Combine& a, int each, cudaStream_t st) {
   Combine q = a;
   const int packs = (q.d + W - 1) / W;
   q.warps = (packs + 32 * each - 1) / (32 * each);
   if (q.warps > 16) q.warps = 16;
   const int groups = q.warps >= 4 ? 1 : 4 / q.warps;
-  k_moe_combine_backward<T, W, S, U><<<(unsigned)((q.tokens + groups - 1) / groups), 32 * q.warps * groups, 0, st>>>(q);
+  k_moe_combine_backward<T, W, S, U, DOTS><<<(unsigned)((q.tokens + groups - 1) / groups), 32 * q.warps * groups, 0, st>>>(q);
   return cudaGetLastError();
 }
 template <typename T, int W>
 cudaError_t launch_combine_backward_as(const Combine& q, cudaStream_t st) {
   // packs a thread: four or more; one where there are fewer tokens than CTAs the GPU holds
   const bool few = q.tokens < 2 * sm_count();
+  if (q.dw == nullptr) {
+    // only dy is in flight then: four packs a thread whatever k is, eight where k is 1 (12729 tokens of 2624 bf16 to 6 slots, 30 % of them
+    // left out: 110 us with one pack, 58 with four)
+    if (q.k == 1) return few ? combine_backward_as<T, W, 1, 1, false>(q, 1, st) : combine_backward_as<T, W, 1, 8, false>(q, 8, st);
+    return few ? combine_backward_as<T, W, 8, 1, false>(q, 1, st) : combine_backward_as<T, W, 8, 4, false>(q, 4, st);
+  }
   if (q.k == 1) return few ? combine_backward_as<T, W, 1, 1>(q, 1, st) : combine_backward_as<T, W, 1, 8>(q, 8, st);
   if (q.k == 2) return few ? combine_backward_as<T, W, 2, 1>(q, 1, st) : combine_backward_as<T, W, 2, 4>(q, 4, st);
   if (q.k <= 4) return few ? combine_backward_as<T, W, 4, 1>(q, 1, st) : combine_backward_as<T, W, 4, 2>(q, 4, st);
