@@ -224,3 +224,31 @@ def test_a_captured_pass_replays_with_new_inputs(P):
     torch.cuda.synchronize()
     y2, g2 = both()
     assert torch.equal(y, y2) and torch.equal(grads["x"], g2["x"]) and torch.equal(grads["weight"], g2["weight"])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,d,pad,first", [
+    (1, 64, 1, 1), (900, 64, 3, 0), (2000, 264, 1, 1), (600, 2048, 1, 0), (333, 8192, 1, 3), (300, 8704, 1, 0), (20, 17024, 1, 1), (3, 32768, 1, 0)])
+def test_rows_off_their_boundaries(P, rows, d, pad, first, dtype):
+    """What is read lies on odd elements, what is written on boundaries of 16 bytes; weights at an odd place too."""
+    for rms in (False, True):
+        x, r, w, b, dy, ds, out, grads = run(P, rows, d, dtype, rms, True, not rms, F32, pad=pad, first=first)
+        off = torch.empty(d + 1, device=DEV)[1:]
+        off.copy_(w)
+        again = P.camera_norm_forward(x, off, b, residual=r, rms=rms)
+        assert torch.equal(again["y"], out["y"])
+        tight = P.camera_norm_forward(x.contiguous(), w, b, residual=r.contiguous(), rms=rms)
+        check(out | tight, forward_ref(out["sum"], w, b, 1e-6, rms, dtype), ["y", "rstd"])
+        g2 = P.camera_norm_backward(dy, out["sum"], out["rstd"], out.get("mean"), off, d_sum=ds, want_bias=True)
+        for k in grads:
+            assert torch.equal(g2[k], grads[k]), k
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,d", [(20000, 600), (20000, 602), (20000, 601), (9000, 96), (9000, 97), (7000, 1200), (40000, 1)])
+def test_many_groups_of_a_cta_share_their_sums(P, rows, d, dtype):
+    for bias in (False, True):
+        x, r, w, b, dy, ds, out, grads = run(P, rows, d, dtype, True, False, False, F32)
+        only = P.camera_norm_backward(dy, x, out["rstd"], None, w, want_x=False, want_weight=not bias, want_bias=bias)
+        for k in only:
+            assert torch.equal(only[k], grads[k]), k
