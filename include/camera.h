@@ -535,7 +535,7 @@ typedef struct {
  *   d_weight = sum over rows of dy h, d_bias = sum over rows of dy (DEVICE fp32 [d], overwritten).
  *   d_sum: gradient of z from elsewhere (the residual stream's), or NULL.  dx is also the residual's gradient.  dx may be
  *   NULL (then d_sum too), d_weight and d_bias may be NULL, not all three.  dx may take the room of dy, d_sum or z.
- *   n->bias and n->eps are not read.
+ *   n->bias and n->eps do not enter; they are checked as in the forward call.
  * A NaN or an infinity stays in its row (and reaches d_weight and d_bias).  A row without variance and with eps 0 gives NaN.
  * workspace (needed for d_weight or d_bias): camera_norm_backward_workspace_bytes, which serves every call with no more
  * rows of that width.  No kernel here waits, so it holds no status word.
