@@ -31,7 +31,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     """Compile every kernel for sm_100a and link libcamera_b200.so.  Returns its path."""
     if not force and not needs_build():
         return LIB
-    cmd = [_nvcc(), "-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",
+    cmd = [_nvcc(), "-std=c++17", "-O3", "-lineinfo", "--threads", "0", "-gencode", "arch=compute_100a,code=sm_100a",
            "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     if verbose:
         cmd += ["-Xptxas", "-v"]
