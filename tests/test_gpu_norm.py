@@ -252,3 +252,20 @@ def test_many_groups_of_a_cta_share_their_sums(P, rows, d, dtype):
         only = P.camera_norm_backward(dy, x, out["rstd"], None, w, want_x=False, want_weight=not bias, want_bias=bias)
         for k in only:
             assert torch.equal(only[k], grads[k]), k
+
+
+@pytest.mark.parametrize("rows,d", [(1, 64), (3, 1000), (1, 3584), (2, 32768), (16, 256)])
+def test_few_rows_and_gradients_at_odd_places(P, rows, d):
+    """One CTA writes the weights' gradients itself, unless they lie off 16-byte boundaries; nothing around them is written."""
+    import ctypes as C
+    x, r, w, b, dy, ds, out, grads = run(P, rows, d, F32, False, False, True, F32)
+    ws = P.alloc_workspace(P.camera_norm_backward_workspace_bytes(rows, d), DEV)
+    from paper_2508_02322_b200.binding import CAMERA_F32, camera_norm_t
+    n = camera_norm_t(x.data_ptr(), d, rows, CAMERA_F32, d, w.data_ptr(), None, CAMERA_F32, 0.0, 0)
+    for at in (0, 1, 3):
+        dw, db = torch.full((d + 8,), 7.0, device=DEV), torch.full((d + 8,), 7.0, device=DEV)
+        assert P.lib.camera_norm_backward(C.byref(n), dy.data_ptr(), d, out["mean"].data_ptr(), out["rstd"].data_ptr(), None, 0, None, 0,
+                                          dw[at:].data_ptr(), db[at:].data_ptr(), ws.data_ptr(), ws.numel(),
+                                          torch.cuda.current_stream().cuda_stream) == 0
+        assert torch.equal(dw[at:at + d], grads["weight"]) and torch.equal(db[at:at + d], grads["bias"])
+        assert (dw[:at] == 7.0).all() and (dw[at + d:] == 7.0).all() and (db[:at] == 7.0).all() and (db[at + d:] == 7.0).all()
