@@ -63,6 +63,18 @@ __device__ __forceinline__ Pack<T, W> load_pack(const T* p) {
   }
 }
 
+// 16 bytes on their way to shared memory (zeros where there are none), in words if LOOSE.
+template <bool LOOSE>
+__device__ __forceinline__ void copy_pack(uint32_t to, const void* from, bool there) {
+  if constexpr (LOOSE) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + i), "l"(static_cast<const char*>(from) + i), "r"(there ? 4 : 0) : "memory");
+  } else {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+  }
+}
+
 template <bool LOOSE, int W>
 __device__ __forceinline__ void load_weight(const void* p, bool f32, int c, float absent, float (&out)[W]) {
   if (p == nullptr) {
@@ -131,9 +143,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_norm_forward(const NormArgs q) {
 #pragma unroll
           for (int j = 0; j < N; ++j) {
             const int c = (j * threads + t) * W, at = c < q.d ? c : 0;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(mine + (stage * parts + p) * line + j * 16 * blockDim.x),
-                         "l"(src[p] + at), "r"(c < q.d ? 16 : 0)
-                         : "memory");
+            copy_pack<false>(mine + (stage * parts + p) * line + j * 16 * blockDim.x, src[p] + at, c < q.d);
           }
         }
     }
@@ -310,9 +320,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 4 : 1) k_norm_backwa
 #pragma unroll
           for (int j = 0; j < N; ++j) {
             const int c = (j * threads + t) * W, at = c < q.d ? c : 0;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(mine + (stage * parts + p) * line + j * 16 * blockDim.x),
-                         "l"(src[p] + row * ld[p] + at), "r"(c < q.d ? 16 : 0)
-                         : "memory");
+            copy_pack<LOOSE>(mine + (stage * parts + p) * line + j * 16 * blockDim.x, src[p] + row * ld[p] + at, c < q.d);
           }
         }
     }
@@ -575,11 +583,10 @@ template <typename T, int W, bool LOOSE, bool BIAS>
 cudaError_t forward_by(const NormArgs& q, cudaStream_t st) {
   constexpr bool RING = W * sizeof(T) == 16 && !LOOSE;
   if (q.d <= 256 || (q.d <= 8192 && ((!RING && !LOOSE) || q.rows <= 2 * sm_count()))) return forward_as<T, W, 8, BIAS, false, LOOSE, 1024>(q, st);
-  if constexpr (LOOSE) {
-    if (q.d <= 8192) return forward_as<T, W, 16, BIAS, false, true, 512>(q, st);
-  }
   if constexpr (RING) {
     if (q.d <= 8192) return q.rms ? forward_as<T, W, 16, BIAS, true, false, 512>(q, st) : forward_as<T, W, 16, BIAS, true, false, 512, 2>(q, st);
+  } else if constexpr (LOOSE) {
+    if (q.d <= 8192) return forward_as<T, W, 16, BIAS, false, true, 512>(q, st);
   }
   if (q.d <= 16384) return forward_as<T, W, 16, BIAS, RING, LOOSE, 1024>(q, st);
   return forward_as<T, W, 32, BIAS, false, LOOSE, 1024>(q, st);
@@ -595,7 +602,9 @@ template <typename T, int W, int E, bool BIAS, bool LOOSE, int THREADS>
 cudaError_t backward_as(const NormArgs& a, size_t room, bool* fits, int* ctas, cudaStream_t st) {
   constexpr int N = E / W, STAGES = NORM_STAGES<N, THREADS, E>;
   constexpr bool VEC = W * sizeof(T) == 16, LONG = THREADS > 512 && E >= 16;
-  constexpr bool RING = VEC && !LOOSE && (!LONG || (E == 16 && sizeof(T) == 2));
+  // fp32 rows off 16-byte boundaries are copied by words (24630 x 1192 with d_sum and bias: 205 us without the ring, 124 with it; short rows
+  // lose by it: 30000 x 128 20 and 29 us)
+  constexpr bool RING = VEC && (!LOOSE || (sizeof(T) == 4 && E == 16)) && (!LONG || (E == 16 && sizeof(T) == 2));
   constexpr auto KERN = k_norm_backward<T, W, N, BIAS, RING, LOOSE, THREADS>;
   NormArgs q = a;
   NormShape s = norm_shape(q.rows, q.d, E, backward_rows(VEC), true);
