@@ -164,17 +164,17 @@ __global__ void __launch_bounds__(MOE_THREADS) k_moe_dispatch(const Dispatch q) 
   const T* const x = static_cast<const T*>(q.x);
   T* const xs = static_cast<T*>(q.xs);
   constexpr int U = 4;
-  const int t1 = min((int)(blockIdx.x + 1) * q.chunk, q.tokens);
+  const long long first = (long long)blockIdx.x * q.chunk, t1 = min(first + q.chunk, (long long)q.tokens);
   if (q.d <= 32 * W) {                  // short rows: a token's in one load, U tokens at a time
-    for (int t0 = blockIdx.x * q.chunk + warp; t0 < t1; t0 += U * MOE_WARPS) {
+    for (long long t0 = first + warp; t0 < t1; t0 += U * MOE_WARPS) {
       const int c = lane * W;
       P v[U];
       int mine[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int t = t0 + u * MOE_WARPS;
+        const long long t = t0 + u * MOE_WARPS;
         if (t < t1 && c < q.d) v[u] = *reinterpret_cast<const P*>(x + t * q.x_ld + c);
-        mine[u] = t < t1 && lane < q.k ? q.rows[(long long)t * q.k + lane] : -1;
+        mine[u] = t < t1 && lane < q.k ? q.rows[t * q.k + lane] : -1;
       }
       for (int j = 0; j < q.k; ++j)
 #pragma unroll
@@ -185,8 +185,8 @@ __global__ void __launch_bounds__(MOE_THREADS) k_moe_dispatch(const Dispatch q) 
     }
     return;
   }
-  for (int t = blockIdx.x * q.chunk + warp; t < t1; t += MOE_WARPS) {
-    const int mine = lane < q.k ? q.rows[(long long)t * q.k + lane] : -1;
+  for (long long t = first + warp; t < t1; t += MOE_WARPS) {
+    const int mine = lane < q.k ? q.rows[t * q.k + lane] : -1;
     for (int c0 = 0; c0 < q.d; c0 += U * 32 * W) {
       P v[U];
 #pragma unroll
@@ -392,7 +392,7 @@ template <typename T, int W, int S, int U>
 cudaError_t combine_as(const Combine& q, cudaStream_t st) {
   const int packs = (q.d + W - 1) / W, slices = (packs + 256 * U - 1) / (256 * U);
   const int bx = ((packs + slices * U - 1) / (slices * U) + 31) & ~31, ty = 256 / bx;
-  k_moe_combine<T, W, S, U><<<dim3((unsigned)((q.tokens + ty - 1) / ty), (unsigned)slices), dim3((unsigned)bx, (unsigned)ty), 0, st>>>(q);
+  k_moe_combine<T, W, S, U><<<dim3((unsigned)(((long long)q.tokens + ty - 1) / ty), (unsigned)slices), dim3((unsigned)bx, (unsigned)ty), 0, st>>>(q);
   return cudaGetLastError();
 }
 template <typename T, int W>
@@ -413,7 +413,7 @@ cudaError_t combine_backward_as(const Combine& a, int each, cudaStream_t st) {
   q.warps = (packs + 32 * each - 1) / (32 * each);
   if (q.warps > 16) q.warps = 16;
   const int groups = q.warps >= 4 ? 1 : 4 / q.warps;
-  k_moe_combine_backward<T, W, S, U, DOTS><<<(unsigned)((q.tokens + groups - 1) / groups), 32 * q.warps * groups, 0, st>>>(q);
+  k_moe_combine_backward<T, W, S, U, DOTS><<<(unsigned)(((long long)q.tokens + groups - 1) / groups), 32 * q.warps * groups, 0, st>>>(q);
   return cudaGetLastError();
 }
 template <typename T, int W>

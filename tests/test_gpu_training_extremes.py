@@ -139,3 +139,29 @@ def test_a_refused_call_leaves_no_error_behind(P):
         P.camera_moe_combine(x, torch.zeros(8, 2, dtype=torch.int64, device=DEV))
     torch.cuda.synchronize()
     assert torch.isfinite(P.camera_norm_forward(x)["y"]).all()
+
+
+def test_almost_2_31_tokens(P):
+    """As many tokens as a call takes, one column: token numbers and counts of CTAs near the end of 31 bits."""
+    T = 2 ** 31 - 5
+    idx = torch.zeros(T, 1, dtype=torch.int32, device=DEV)
+    idx[-3:] = 1
+    idx[5] = -1
+    x = torch.empty(T, 1, dtype=BF, device=DEV).random_(0, 200)
+    s = P.camera_moe_dispatch(x, idx, 2)
+    assert s["offsets"].tolist() == [0, T - 4, T - 1]
+    rows, step = s["rows"].view(-1), 2 ** 28
+    for a in range(0, T, step):
+        want = torch.arange(a, min(a + step, T), device=DEV)
+        want = torch.where(want == 5, -1, want - (want > 5).long())
+        assert torch.equal(rows[a:a + step].long(), want)
+        del want
+    assert torch.equal(s["x"][:5], x[:5]) and torch.equal(s["x"][5:-1], x[6:])
+    del idx
+    y = P.camera_moe_combine(s["x"][:-1], s["rows"])
+    assert y[5, 0] == 0 and torch.equal(y[:5], x[:5]) and torch.equal(y[6:], x[6:])
+    s["x"][-1] = 3.0
+    back = P.camera_moe_combine_backward(y, s["x"], s["rows"], want_weights=False)["y"]
+    assert torch.equal(back[:5], x[:5]) and torch.equal(back[5:-1], x[6:])
+    del x, s, y, back, rows
+    torch.cuda.empty_cache()
