@@ -432,6 +432,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
         f = MODE == ORTHO_GRAM ? f / s / s : scalbnf(f / s, to_caller ? 0 : scale_of(small, st.small_out));
       }
       if (MODE != ORTHO_GRAM && !__all_sync(0xffffffffu, lane != 0 || wait_seen(smem_u32((const void*)seen), k, abort_flag))) return false;
+      __syncwarp();                                                // a vote orders no memory: what lane 0 acquired is there for all lanes
       const float rest = MODE == ORTHO_GRAM ? 0.f : __ldcg(rest_in + row);
       auto fetch = [&](int c, uint32_t k) {                        // lane 0: the k-th box from here, at column c, on its way
         if (MODE != ORTHO_GRAM && c < cols) {
