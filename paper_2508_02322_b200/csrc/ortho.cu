@@ -526,7 +526,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
         tmem_ld_wait(v1);
         if (c + O_CHUNK < cols) tmem_ld16(t0 + c + O_CHUNK, v0);
         put(v1, 1, c + 16);
-        if (!to_caller) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        // before a box leaves by TMA, and before one (the result's too) takes the room of what lanes wrote or read
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (to_caller && !mat.turned) {
           // the box's rows as they lie in memory: by 16 bytes, by two elements or by one
