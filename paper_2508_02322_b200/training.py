@@ -296,9 +296,10 @@ def camera_orthogonalize(updates: Updates, *, steps: int = 5, coefficients=NEWTO
         return _elsewhere(stream, camera_orthogonalize, updates, steps=steps, coefficients=coefficients, eps=eps, out=out,
                           workspace=workspace)
     mats = _list(updates)
-    flat = [float(v) for c in coefficients for v in c] if isinstance(coefficients[0], (tuple, list)) else list(coefficients) * steps
-    if len(flat) % 3 or not flat:
+    each = [tuple(coefficients)] * steps if len(coefficients) == 3 and not any(isinstance(c, (tuple, list)) for c in coefficients) else coefficients
+    if not each or not all(isinstance(c, (tuple, list)) and len(c) == 3 for c in each):
         raise ValueError("coefficients must be three numbers, or three for each step")
+    flat = [float(v) for c in each for v in c]
     if out is None:
         out = torch.empty(updates.shape, dtype=_BF16, device=updates.device) if isinstance(updates, torch.Tensor) else \
             [torch.empty(t.shape, dtype=_BF16, device=t.device) for t in mats]

@@ -142,3 +142,14 @@ def test_tensors_are_checked_in_python(P):
     with pytest.raises(P.CameraError):
         P.camera_norm_backward_workspace_bytes(4, 1 << 20)
     assert P.camera_orthogonalize_workspace_bytes([z]) > 0    # shapes may be asked about anywhere
+
+
+def test_coefficients_are_three_numbers_or_a_list_of_such(P):
+    z = torch.zeros(4, 16)
+    six = (3.0, -3.2, 1.2) * 2
+    for bad in (six, six[:5], (), [six], [(3.0, -3.2, 1.2), (1.0, 2.0)], [(1.0, 2.0, 3.0), 4.0]):
+        with pytest.raises(ValueError, match="coefficients must be"):
+            P.camera_orthogonalize([z], coefficients=bad)
+    for good in (P.NEWTON_SCHULZ, list(P.NEWTON_SCHULZ), [P.NEWTON_SCHULZ] * 5, [list(P.NEWTON_SCHULZ)]):
+        with pytest.raises(ValueError, match="on the GPU"):   # past the coefficients
+            P.camera_orthogonalize([z], coefficients=good)
