@@ -286,19 +286,23 @@ def camera_orthogonalize_workspace_bytes(updates: Updates) -> int:
     return n
 
 
-def camera_orthogonalize(updates: Updates, *, steps: int = 5, coefficients=NEWTON_SCHULZ, eps: float = 1e-7,
+def camera_orthogonalize(updates: Updates, *, steps: Optional[int] = None, coefficients=NEWTON_SCHULZ, eps: float = 1e-7,
                          out: Optional[Updates] = None, workspace: Optional[torch.Tensor] = None,
                          stream: Optional[torch.cuda.Stream] = None) -> Updates:
     """The matrices of `updates` (bf16 or fp32, a list of any shapes or a tensor [n, rows, cols]), each over its norm (plus
-    eps) and with every singular value s taken to a s + b s^3 + c s^5, `steps` times over.  coefficients: (a, b, c), or a
-    list of such for each step.  Returns bf16 matrices of the same shapes (`out`, if given; may be bf16 updates themselves)."""
+    eps) and with every singular value s taken to a s + b s^3 + c s^5, `steps` times over (5 if not given).  coefficients:
+    (a, b, c), or a list of such for each step, as many as there are steps.  Returns bf16 matrices of the same shapes (`out`,
+    if given; may be bf16 updates themselves)."""
     if stream is not None:
         return _elsewhere(stream, camera_orthogonalize, updates, steps=steps, coefficients=coefficients, eps=eps, out=out,
                           workspace=workspace)
     mats = _list(updates)
-    each = [tuple(coefficients)] * steps if len(coefficients) == 3 and not any(isinstance(c, (tuple, list)) for c in coefficients) else coefficients
+    one = len(coefficients) == 3 and not any(isinstance(c, (tuple, list)) for c in coefficients)
+    each = [tuple(coefficients)] * (5 if steps is None else steps) if one else coefficients
     if not each or not all(isinstance(c, (tuple, list)) and len(c) == 3 for c in each):
         raise ValueError("coefficients must be three numbers, or three for each step")
+    if steps is not None and len(each) != steps:
+        raise ValueError(f"coefficients of {len(each)} steps, and steps = {steps}")
     flat = [float(v) for c in each for v in c]
     if out is None:
         out = torch.empty(updates.shape, dtype=_BF16, device=updates.device) if isinstance(updates, torch.Tensor) else \

@@ -153,3 +153,14 @@ def test_coefficients_are_three_numbers_or_a_list_of_such(P):
     for good in (P.NEWTON_SCHULZ, list(P.NEWTON_SCHULZ), [P.NEWTON_SCHULZ] * 5, [list(P.NEWTON_SCHULZ)]):
         with pytest.raises(ValueError, match="on the GPU"):   # past the coefficients
             P.camera_orthogonalize([z], coefficients=good)
+
+
+def test_steps_and_a_list_of_coefficients_agree(P):
+    z = torch.zeros(4, 16)
+    three = [P.NEWTON_SCHULZ] * 3
+    for bad in (1, 5, 0):
+        with pytest.raises(ValueError, match="steps"):
+            P.camera_orthogonalize([z], steps=bad, coefficients=three)
+    for kw in (dict(coefficients=three), dict(steps=3, coefficients=three), dict(steps=7), dict()):
+        with pytest.raises(ValueError, match="on the GPU"):   # past the coefficients
+            P.camera_orthogonalize([z], **kw)
