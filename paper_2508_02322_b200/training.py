@@ -92,6 +92,9 @@ def camera_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, 
     rstd and (unless rms) mean, fp32 [n_rows].  `out` names tensors to write y and sum to; both may be x or residual."""
     if stream is not None:
         return _elsewhere(stream, camera_norm_forward, x, weight, bias, residual=residual, eps=eps, rms=rms, stats=stats, out=out)
+    for name in out or ():
+        if out[name] is not None and name != "y" and (name != "sum" or residual is None):
+            raise ValueError(f"out names y and, with a residual, sum: not {name}")
     n = _norm(x, weight, bias, eps, rms)
     rows, d = x.shape
     y = out.get("y") if out else None

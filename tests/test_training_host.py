@@ -164,3 +164,15 @@ def test_steps_and_a_list_of_coefficients_agree(P):
     for kw in (dict(coefficients=three), dict(steps=3, coefficients=three), dict(steps=7), dict()):
         with pytest.raises(ValueError, match="on the GPU"):   # past the coefficients
             P.camera_orthogonalize([z], **kw)
+
+
+def test_unknown_names_of_results_are_refused(P):
+    z = torch.zeros(4, 16)
+    for out in ({"rstd": z[:, 0]}, {"y": z, "mean": z[:, 0]}, {"x": z}):
+        with pytest.raises(ValueError, match="out"):
+            P.camera_norm_forward(z, residual=z, out=out)
+    with pytest.raises(ValueError, match="out"):
+        P.camera_norm_forward(z, out={"sum": z})              # there is no sum without a residual
+    for kw in (dict(out={"y": z}), dict(residual=z, out={"y": z, "sum": z}), dict(out={}), dict(out={"sum": None})):
+        with pytest.raises(ValueError, match="on the GPU"):
+            P.camera_norm_forward(z, **kw)
