@@ -198,6 +198,18 @@ __device__ __forceinline__ bool wait_seen(uint32_t seen, int k, volatile int* ab
   return true;
 }
 
+// What other CTAs have written during this launch: read from L2, and not before the waits that stand above in the program.
+__device__ __forceinline__ float load_written(const float* p) {
+  float v;
+  asm volatile("ld.global.cg.f32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 load_written(const float4* p) {
+  float4 v;
+  asm volatile("ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p) : "memory");
+  return v;
+}
+
 __device__ __forceinline__ uint32_t pack_half(float a, float b) {
   const __half2 v = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&v);
@@ -433,7 +445,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
       }
       if (MODE != ORTHO_GRAM && !__all_sync(0xffffffffu, lane != 0 || wait_seen(smem_u32((const void*)seen), k, abort_flag))) return false;
       __syncwarp();                                                // a vote orders no memory: what lane 0 acquired is there for all lanes
-      const float rest = MODE == ORTHO_GRAM ? 0.f : __ldcg(rest_in + row);
+      const float rest = MODE == ORTHO_GRAM ? 0.f : load_written(rest_in + row);
       auto fetch = [&](int c, uint32_t k) {                        // lane 0: the k-th box from here, at column c, on its way
         if (MODE != ORTHO_GRAM && c < cols) {
           const uint32_t bar = aux_bar(warp * O_BUFS + (loads + k) % O_BUFS);
@@ -448,7 +460,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
       if (MODE == ORTHO_POLY) {
         __syncwarp();
         for (int i = 4 * lane; c_first + i < cols; i += 128)
-          *reinterpret_cast<float4*>(rests + i) = __ldcg(reinterpret_cast<const float4*>(rest_in + u.n0 + c_first + i));
+          *reinterpret_cast<float4*>(rests + i) = load_written(reinterpret_cast<const float4*>(rest_in + u.n0 + c_first + i));
       }
       __syncwarp();
       if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(acc), acc_phase, abort_flag))) return false;
