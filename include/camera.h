@@ -592,10 +592,11 @@ typedef struct {
  * With those that take values towards 1, out is near the orthogonal factor of `in`.  mats: HOST [n_mats], in in `dtype`; the
  * matrices of a call, whatever their shapes, are worked on together.  1 <= steps <= 64.  Coefficients under which a singular
  * value or the step's factor of it could pass 1000 are refused (CAMERA_ERR_INVALID_ARG): they do not converge.
- * Products of fp16 operands with fp32 sums; factors that keep them in range follow from the coefficients.  The result is
- * about 1e-3 off 64 bits (root mean square, relative) before its rounding to bf16; directions whose singular value is below
- * 1e-3 of the norm's share of the others are off by more.  A matrix of zeros gives zeros; one with a NaN or an infinity gives
- * NaN and leaves the others of the call as they are.
+ * Products of fp16 operands with fp32 sums; factors that keep them in range follow from the coefficients; X itself is kept
+ * in 22 bits.  Before its rounding to bf16, which adds 1.7e-3, the result is about 1e-3 off 64 bits (root mean square over the
+ * matrix, relative), whatever the matrix' rank, and up to 4e-3 where the shorter side is below 16.  Where `in` has nothing,
+ * roundings grow by the product of the steps' a (485 for five of 3.4445); beyond 1e4 they show.  A matrix of zeros gives zeros;
+ * one with a NaN or an infinity gives NaN and leaves the others of the call as they are.
  * workspace: camera_orthogonalize_workspace_bytes of the same shapes (pointers are not read); it starts with a status word
  * that camera_read_status reads.
  */

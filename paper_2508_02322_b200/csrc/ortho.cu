@@ -12,8 +12,15 @@
 // host follows these bounds from step to step (1 before the first) and picks the largest factors under which nothing can
 // overflow.  fp16 has 3 bits more than bf16.  The diagonals of A and B hold most of what they are, and in a matrix whose singular
 // values are alike all of it rounds the same way; so what their rounding leaves is kept in fp32 and enters the next product's
-// epilogue (a row of it for B X, a row and a column for A A).  Results are 4e-4 to 9e-4 off 64 bits (root mean square,
-// relative; up to 2.7e-3 without the diagonals' rests, 8e-3 with bf16 operands), below their own rounding to bf16, 1.7e-3.
+// epilogue (a row of it for B X, a row and a column for A A).
+//
+// X itself is held as two fp16 numbers, X + L, 22 bits.  Its rounding reaches directions in which the matrix has nothing (a gradient made
+// from few tokens), and there every step left multiplies it by a: 485 times in five steps, where what the matrix does have grows to 1.
+// There B is a I, so B L is a L, which an epilogue adds by element; no product needs L.  In the directions the matrix has, the rounding
+// does not grow, and B L is nearer to the diagonal of B times L.  The factor lies between the two, nearer to a the more the steps left can
+// make of it (f_low).  The rest of B L is left out.  1000 x 2048, fp32, made from 1, 8, 64, 256 and 2048 tokens: 1.7, 1.7, 1.9, 1.9 and 1.7e-3
+// off 64 bits (root mean square, relative), of which the result's rounding to bf16 alone makes 1.7e-3; with X in one fp16 it was 0.15, 4.2e-2,
+// 2.1e-2, 7.7e-3 and 1.9e-3.  It costs a product's epilogue its reads and writes: sixteen matrices 940 -> 1000 us, three 225 -> 243.
 // The first X is the matrix itself times a power of two, so bf16 inputs enter exactly; 1 / (|U| + eps) goes into the factors of the
 // first step.
 //
@@ -76,7 +83,7 @@ struct OrthoBatch {
 // Factors of one step (see the top of the file): of the sums of GRAM, POLY and APPLY, of A and on the diagonal in POLY; and what the
 // steps so far can have made of a small matrix (see scale_of), before and after this one.
 struct OrthoStep {
-  float f_gram, f_poly, f_aux, f_diag, f_apply;
+  float f_gram, f_poly, f_aux, f_diag, f_apply, f_low;      // f_low: share of B's diagonal (over that of a) in the factor of X's low half
   int small_in, small_out;
 };
 
@@ -94,6 +101,10 @@ struct OrthoRun {
   __half* out[2];                        // A and B
   long long out_ld;
   float* rest[2];                        // [rows] what the rounding of the diagonals of A and B left
+  float* low_f;                          // [rows] factor of a row of X's low half
+  uint4* low;                            // the low half of X, in place through all steps (see low_at)
+  int low_ld;                            // and the columns its rows have
+  int low_first;                         // whether the first X has one
   const float* first;                    // factor of each matrix's first X
   const int* small;                      // exponents by which matrices are smaller than the bounds
   int* done;                             // [mats] warps that have finished with a unit of this matrix
@@ -110,6 +121,10 @@ __host__ __device__ __forceinline__ int pad_cols(int n) { return (n + UMMA_BK - 
 // would be lost in fp16 at the others' factors.  A step makes them larger by no more than the largest value of its polynomial, so
 // X keeps 2^(small - what the steps so far can have added) as a further factor, as long as that is above 1.
 __device__ __forceinline__ int scale_of(int small, int used) { return max(0, small - used); }
+
+// Where eight elements of X's low half lie, from column c on (a multiple of 8): rows in groups of 32, so that the lanes of an epilogue
+// warp, each with its row, read and write 512 bytes in a row.
+__host__ __device__ __forceinline__ long long low_at(int row, int c, int ld) { return ((long long)(row >> 5) * (ld >> 3) + (c >> 3)) * 32 + (row & 31); }
 
 // need: how many warps must have finished with this matrix before the unit's operands are there.
 struct OrthoUnit { int step, mode, e, m0, n0, two, kb, limit, need; };
@@ -209,10 +224,20 @@ __device__ __forceinline__ float4 load_written(const float4* p) {
   asm volatile("ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p) : "memory");
   return v;
 }
+__device__ __forceinline__ uint4 load_written(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.cg.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
 
 __device__ __forceinline__ uint32_t pack_half(float a, float b) {
   const __half2 v = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&v);
+}
+// What the rounding of a and b to the halves in p leaves.
+__device__ __forceinline__ uint32_t pack_low(float a, float b, uint32_t p) {
+  const float2 high = __half22float2(*reinterpret_cast<const __half2*>(&p));
+  return pack_half(a - high.x, b - high.y);
 }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
@@ -446,6 +471,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
       if (MODE != ORTHO_GRAM && !__all_sync(0xffffffffu, lane != 0 || wait_seen(smem_u32((const void*)seen), k, abort_flag))) return false;
       __syncwarp();                                                // a vote orders no memory: what lane 0 acquired is there for all lanes
       const float rest = MODE == ORTHO_GRAM ? 0.f : load_written(rest_in + row);
+      const float low_f = MODE == ORTHO_APPLY ? load_written(q.low_f + mat.row0 + row) : 0.f;
+      const bool has_low = MODE == ORTHO_APPLY && (u.step > 0 || q.low_first);
+      uint4* const low_row = q.low + low_at(mat.row0 + row, u.n0, q.low_ld);
+      uint4 low[4], low_next[4];                                   // this lane's of the chunk at work and of the next
+      auto fetch_low = [&](int c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) low_next[i] = has_low && c < cols ? load_written(low_row + 4 * c + 32 * i) : make_uint4(0, 0, 0, 0);
+      };
+      if (MODE == ORTHO_APPLY) fetch_low(c_first);
       auto fetch = [&](int c, uint32_t k) {                        // lane 0: the k-th box from here, at column c, on its way
         if (MODE != ORTHO_GRAM && c < cols) {
           const uint32_t bar = aux_bar(warp * O_BUFS + (loads + k) % O_BUFS);
@@ -484,8 +518,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
           for (int j = 0; j < 16; j += 2) {
             const float2 old = __half22float2(*reinterpret_cast<const __half2*>(&a[j >> 1]));
             const F2 old2 = f2(old.x, old.y), sum = f2(__uint_as_float(raw[j]), __uint_as_float(raw[j + 1]));
-            if (MODE == ORTHO_APPLY) {                  // (B + rest) X
-              split(mul2(fma2(f2(rest, rest), old2, sum), f_2), v[j], v[j + 1]);
+            if (MODE == ORTHO_APPLY) {                  // (B + rest) X, and of its low half what matters of B
+              const uint4& piece = low[2 * k + (j >> 3)];
+              const uint32_t word = (j >> 1 & 3) == 0 ? piece.x : (j >> 1 & 3) == 1 ? piece.y : (j >> 1 & 3) == 2 ? piece.z : piece.w;
+              const float2 lo = __half22float2(*reinterpret_cast<const __half2*>(&word));
+              split(mul2(fma2(f2(low_f, low_f), f2(lo.x, lo.y), fma2(f2(rest, rest), old2, sum)), f_2), v[j], v[j + 1]);
             } else {                                    // (A + rest)^2 up to the square of the rest, and b A (b rest: below)
               const float2 down = *reinterpret_cast<const float2*>(rests + c - c_first + j);
               split(fma2(old2, f2(f_aux, f_aux), mul2(fma2(add2(f2(rest, rest), f2(down.x, down.y)), old2, sum), f_2)), v[j], v[j + 1]);
@@ -514,10 +551,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
           if (MODE == ORTHO_POLY) mine += fmaf(rest, f_aux, f_diag);
 #pragma unroll
           for (int j = 0; j < 16; ++j) v[j] = j == own ? mine : v[j];
-          if (own >= 0 && own < 16) rest_out[row] = mine - __half2float(__float2half_rn(mine));
+          if (own >= 0 && own < 16) {
+            rest_out[row] = mine - __half2float(__float2half_rn(mine));
+            if (MODE == ORTHO_POLY) q.low_f[mat.row0 + row] = mat.m == 1 ? mine : fmaf(st.f_low, mine - f_diag, f_diag);     // one row: B is its diagonal
+          }
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) p[j] = pack_half(v[2 * j], v[2 * j + 1]);
+        if (MODE == ORTHO_APPLY) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            low_row[4 * c + 32 * i] = make_uint4(pack_low(v[8 * i], v[8 * i + 1], p[4 * i]), pack_low(v[8 * i + 2], v[8 * i + 3], p[4 * i + 1]),
+                                                 pack_low(v[8 * i + 4], v[8 * i + 5], p[4 * i + 2]), pack_low(v[8 * i + 6], v[8 * i + 7], p[4 * i + 3]));
+        }
         *piece0 = make_uint4(p[0], p[1], p[2], p[3]);
         *piece1 = make_uint4(p[4], p[5], p[6], p[7]);
         if (MODE != ORTHO_APPLY && u.n0 + c >= u.m0 + O_TILE_M)      // off the diagonal's block: the other half of the result
@@ -529,6 +575,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
       for (int c = c_first; c < cols; c += O_CHUNK, ++n, loads += MODE != ORTHO_GRAM) {
         const uint32_t box = n % O_BUFS;
         box_row = bufs + box * O_BUF_BYTES + lane * (2 * O_CHUNK);
+        if (MODE == ORTHO_APPLY) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) low[i] = low_next[i];
+          fetch_low(c + O_CHUNK);
+        }
         if (MODE != ORTHO_GRAM) {
           if (!warp_wait(aux_bar(warp * O_BUFS + loads % O_BUFS), loads / O_BUFS & 1u, abort_flag)) return false;
         }
@@ -611,6 +662,7 @@ struct OrthoLoad {
   float eps;
   __half* x;
   long long x_ld;
+  uint4* low;               // fp32: the low half of X
   PlanTotals* totals;
   int clear_status;
 };
@@ -693,11 +745,12 @@ __global__ void __launch_bounds__(LOAD_THREADS, 6) k_ortho_norm(const __grid_con
   if (threadIdx.x == 0) q.part[blockIdx.y * q.parts + blockIdx.x] = s;
 }
 
-// X = U 2^p in fp16, shorter side as rows, zeros around it.  p puts 2^p |U| into [2^14, 2^15): nothing overflows, and what
+// X = U 2^p in fp16 (of fp32 matrices a second fp16 holds what the rounding leaves), shorter side as rows, zeros around it.  p puts 2^p |U| into [2^14, 2^15): nothing overflows, and what
 // is below 2^-39 of the norm is lost.  A CTA turns tiles of 64 x 64 in shared memory.
 template <typename T>
 __global__ void __launch_bounds__(LOAD_THREADS, 6) k_ortho_load(const __grid_constant__ OrthoLoad q) {
-  __shared__ __align__(16) __half tile[64][72];
+  constexpr bool LOW = sizeof(T) == 4;
+  __shared__ __align__(16) __half tile[LOW ? 2 : 1][64][72];
   __shared__ int power;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -750,21 +803,28 @@ __global__ void __launch_bounds__(LOAD_THREADS, 6) k_ortho_load(const __grid_con
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int a = (threadIdx.x >> 3) + 32 * k;
-      uint32_t w[4];
+      uint32_t w[LOW ? 2 : 1][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = pack_half(v[k][2 * i] * up * up2, v[k][2 * i + 1] * up * up2);
-      if (mat.turned) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) tile[b + i][a] = __ushort_as_half((unsigned short)(i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu));
-      } else {
-        *reinterpret_cast<uint4*>(&tile[a][b]) = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int i = 0; i < 4; ++i) {
+        const float a0 = v[k][2 * i] * up * up2, a1 = v[k][2 * i + 1] * up * up2;
+        w[0][i] = pack_half(a0, a1);
+        if constexpr (LOW) w[1][i] = pack_low(a0, a1, w[0][i]);
       }
+#pragma unroll
+      for (int h = 0; h < (LOW ? 2 : 1); ++h)
+        if (mat.turned) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) tile[h][b + i][a] = __ushort_as_half((unsigned short)(i & 1 ? w[h][i >> 1] >> 16 : w[h][i >> 1] & 0xffffu));
+        } else {
+          *reinterpret_cast<uint4*>(&tile[h][a][b]) = make_uint4(w[h][0], w[h][1], w[h][2], w[h][3]);
+        }
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int r = (threadIdx.x >> 3) + 32 * k;
-      *reinterpret_cast<uint4*>(q.x + (long long)(mat.row0 + r0 + r) * q.x_ld + c0 + b) = *reinterpret_cast<const uint4*>(&tile[r][b]);
+      *reinterpret_cast<uint4*>(q.x + (long long)(mat.row0 + r0 + r) * q.x_ld + c0 + b) = *reinterpret_cast<const uint4*>(&tile[0][r][b]);
+      if constexpr (LOW) q.low[low_at(mat.row0 + r0 + r, c0 + b, (int)q.x_ld)] = *reinterpret_cast<const uint4*>(&tile[1][r][b]);
     }
   }
 }
@@ -794,17 +854,19 @@ OrthoRound ortho_round(const camera_matrix_t* mats, int n, int begin) {
   return r;
 }
 constexpr int MAX_PARTS = 296;
-struct OrthoLayout { size_t part, first, rest_a, rest_b, x0, x1, a, b, total; };
+struct OrthoLayout { size_t part, first, rest_a, rest_b, low_f, x0, x1, low, a, b, total; };
 OrthoLayout ortho_layout(const OrthoRound& r) {
   OrthoLayout l;
   l.part = up256(sizeof(PlanTotals));
   l.first = l.part + up256((size_t)8 * O_MAX_MATS * MAX_PARTS);
   l.rest_a = l.first + up256(12 * O_MAX_MATS);
   l.rest_b = l.rest_a + up256((size_t)4 * r.rows);
-  l.x0 = l.rest_b + up256((size_t)4 * r.rows);
+  l.low_f = l.rest_b + up256((size_t)4 * r.rows);
+  l.x0 = l.low_f + up256((size_t)4 * r.rows);
   const size_t x = up256((size_t)2 * r.rows * r.x_ld), a = up256((size_t)2 * r.rows * r.a_ld);
   l.x1 = l.x0 + x;
-  l.a = l.x1 + x;
+  l.low = l.x1 + x;
+  l.a = l.low + x;
   l.b = l.a + a;
   l.total = l.b + a;
   return l;
@@ -945,6 +1007,7 @@ int run_round(const camera_matrix_t* mats, const OrthoRound& r, int32_t dtype, c
   ld.small = reinterpret_cast<int*>(ld.first + O_MAX_MATS);
   ld.done = ld.small + O_MAX_MATS;
   ld.eps = eps; ld.x = reinterpret_cast<__half*>(ws + l.x0); ld.x_ld = r.x_ld;
+  ld.low = reinterpret_cast<uint4*>(ws + l.low);
   ld.totals = reinterpret_cast<PlanTotals*>(ws);
   ld.clear_status = first_round;
   ld.parts = 8 * sms / q.batch.n_mats;
@@ -967,6 +1030,8 @@ int run_round(const camera_matrix_t* mats, const OrthoRound& r, int32_t dtype, c
   q.out_ld = r.a_ld;
   q.rest[0] = reinterpret_cast<float*>(ws + l.rest_a);
   q.rest[1] = reinterpret_cast<float*>(ws + l.rest_b);
+  q.low_f = reinterpret_cast<float*>(ws + l.low_f);
+  q.low = ld.low; q.low_ld = r.x_ld; q.low_first = dtype == CAMERA_F32;
   q.first = ld.first; q.small = ld.small; q.done = ld.done; q.totals = ld.totals;
   q.wait_limit_ns = current_wait_limit_ns();
   double h = 1.0, sx = 1.0;             // the first X's factor is known on the device only
@@ -984,6 +1049,9 @@ int run_round(const camera_matrix_t* mats, const OrthoRound& r, int32_t dtype, c
     o.small_out = (int)ceil(log2(fmax(grown / bound.h, 1.0)));
     h = bound.h;
     sx = sn;
+    double growth = 1.0;
+    for (int later = s + 1; later < steps; ++later) growth = fmin(growth * fmax(fabs((double)coefficients[3 * later]), 1.0), 1e30);
+    o.f_low = (float)(1.0 / (1.0 + (growth / 8) * (growth / 8)));
   }
   ORTHO_CK(allow_smem<k_ortho, O_SMEM_BYTES>());
   int pairs = pairs_at_once();
