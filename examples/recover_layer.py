@@ -1,4 +1,4 @@
-"""Train what a slicing left of a whole MoE layer: norm, router, experts, residual, and an orthogonalised update.
+"""Train the experts that a slicing left of a whole MoE layer (norm, router, experts, residual) with orthogonalised updates.
 
     python examples/recover_layer.py [--prune 0.4] [--steps 60] [--tokens 1024]
 
@@ -10,7 +10,9 @@ experts; what is left (experts of different heights) is trained so that the laye
   camera_moe_combine_backward, camera_ffn_backward, camera_moe_dispatch_backward, camera_norm_backward     its gradients
   camera_orthogonalize                                                                  the update of the experts' matrices
 
-Weights and hidden states are synthetic (random); the router and its gradient are plain matrix products.
+The experts' matrices are what is trained; the gradients of the norm's weight and of the router come out of the same backward
+pass and are left unused here.  Weights and hidden states are synthetic (random); the router and its gradient are plain matrix
+products.
 """
 import argparse
 import os
@@ -123,7 +125,8 @@ def recover(d_model=256, d_ff=512, n_experts=8, top_k=2, tokens=1024, prune=0.4,
             v.mul_(momentum)
             if t is not None:
                 v.add_(t)
-        for m, v, o in zip(master, views, P.camera_orthogonalize(velocity, workspace=scratch)):
+        updates = P.camera_orthogonalize(velocity, workspace=scratch)
+        for m, v, o in zip(master, views, updates):
             # an orthogonal matrix's elements are sqrt(1 / longer side) in size: brought to the size of the weights' own
             m.sub_(o.float(), alpha=lr * (1 - step / steps) * max(m.shape) ** 0.5)
             v.copy_(m)
@@ -131,7 +134,7 @@ def recover(d_model=256, d_ff=512, n_experts=8, top_k=2, tokens=1024, prune=0.4,
             log(f"step {step:3d}  squared error {losses[-1]:.5f}")
     assert P.camera_read_status(scratch) == 0 and P.camera_read_status(student.workspace) == 0
     log(f"squared error {losses[0]:.5f} -> {losses[-1]:.5f}")
-    return {"kept": kept, "losses": losses, "student": student}
+    return {"kept": kept, "losses": losses, "student": student, "velocity": velocity, "updates": updates}
 
 
 if __name__ == "__main__":

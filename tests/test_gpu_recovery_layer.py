@@ -97,3 +97,23 @@ def test_the_block_on_another_stream_gives_the_same_bits():
     side.synchronize()
     for a, b in zip(first, second):
         assert torch.equal(a, b)
+
+
+def test_the_examples_updates_have_the_polynomials_singular_values():
+    """Singular values of a matrix and of one that is off by E differ by at most |E| (2-norm over all of them): E is about 1e-3 of the
+    result and its rounding to bf16 (2^-8 / sqrt(3) at most, root mean square); twice the sum of both is allowed."""
+    import paper_2508_02322_b200 as P
+    from recover_layer import recover
+    r = recover(d_model=128, d_ff=256, n_experts=4, top_k=2, tokens=300, prune=0.3, steps=3, log=lambda *_: None)
+    assert len(r["updates"]) == len(r["velocity"]) == 12
+    for u, o in zip(r["velocity"], r["updates"]):
+        s = torch.linalg.svdvals(u.double())
+        s = s / u.double().norm()
+        for _ in range(5):
+            a, b, c = P.NEWTON_SCHULZ
+            s = s * (a + b * s ** 2 + c * s ** 4)
+        got = torch.linalg.svdvals(o.double())
+        off = got - s.sort(descending=True).values
+        assert float(off.norm()) <= 2 * (1e-3 + 2.0 ** -8 / 3 ** 0.5) * float(s.norm())
+        # the same directions: the update points where the matrix does
+        assert float((u.double() * o.double()).sum()) > 0
