@@ -137,6 +137,8 @@ def camera_norm_backward(dy: torch.Tensor, x: torch.Tensor, rstd: torch.Tensor, 
     if stream is not None:
         return _elsewhere(stream, camera_norm_backward, dy, x, rstd, mean, weight, d_sum=d_sum, want_x=want_x,
                           want_weight=want_weight, want_bias=want_bias, out=out, workspace=workspace)
+    if not want_x and out is not None:
+        raise ValueError("out belongs to the gradient of x: not with want_x=False")
     n = _norm(x, weight, None, 0.0, mean is None)
     rows, d = x.shape
     dy_ld = _matrix(dy, "dy", x, rows, d)
@@ -247,6 +249,8 @@ def camera_moe_combine_backward(dy: torch.Tensor, y_sorted: torch.Tensor, rows: 
     if stream is not None:
         return _elsewhere(stream, camera_moe_combine_backward, dy, y_sorted, rows, topk_w, want_y=want_y,
                           want_weights=want_weights, out=out)
+    if not want_y and out is not None:
+        raise ValueError("out belongs to the gradient of y_sorted: not with want_y=False")
     ld = _matrix(dy, "dy")
     tokens, d = dy.shape
     ys_ld = _matrix(y_sorted, "y_sorted", dy, None, d)

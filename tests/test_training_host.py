@@ -176,3 +176,15 @@ def test_unknown_names_of_results_are_refused(P):
     for kw in (dict(out={"y": z}), dict(residual=z, out={"y": z, "sum": z}), dict(out={}), dict(out={"sum": None})):
         with pytest.raises(ValueError, match="on the GPU"):
             P.camera_norm_forward(z, **kw)
+
+
+def test_room_for_a_result_that_is_not_asked_for_is_refused(P):
+    z, idx = torch.zeros(4, 16), torch.zeros(4, 2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="want_x"):
+        P.camera_norm_backward(z, z, z[:, 0], want_x=False, out=z)
+    with pytest.raises(ValueError, match="want_y"):
+        P.camera_moe_combine_backward(z, z, idx, want_y=False, out=z)
+    for call in (lambda: P.camera_norm_backward(z, z, z[:, 0], want_x=False), lambda: P.camera_norm_backward(z, z, z[:, 0], out=z, d_sum=z),
+                 lambda: P.camera_moe_combine_backward(z, z, idx, out=z), lambda: P.camera_moe_combine_backward(z, z, idx, want_y=False)):
+        with pytest.raises(ValueError, match="on the GPU"):
+            call()
