@@ -537,6 +537,7 @@ typedef struct {
  *   NULL (then d_sum too), d_weight and d_bias may be NULL, not all three.  dx may take the room of dy, d_sum or z.
  *   n->bias and n->eps do not enter; they are checked as in the forward call.
  * A NaN or an infinity stays in its row (and reaches d_weight and d_bias).  A row without variance and with eps 0 gives NaN.
+ * Squares and sums are fp32: elements beyond about 1e17 (and, with eps 0, deviations below 1e-18) leave its range.
  * workspace (needed for d_weight or d_bias): camera_norm_backward_workspace_bytes, which serves every call with no more
  * rows of that width.  No kernel here waits, so it holds no status word.
  */

@@ -116,3 +116,18 @@ def test_the_weight_gradient_of_more_than_2_31_elements(P):
         check({"x": grads["x"][part]}, ref, ["x"])
     del x, dy, grads
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("scale", [1e17, 1e-17])
+def test_norms_of_large_and_small_rows(P, scale, dtype):
+    """Near the ends of what squares in fp32 hold; eps does not enter."""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    for rows, d in ((700, 1000), (5, 33), (300, 9000)):
+        x, dy = rows_of(g, rows, d, dtype).clamp_(-3, 3).mul_(scale / 3), rows_of(g, rows, d, dtype, scale=0.1)
+        w = 1 + 0.2 * torch.randn(d, device=DEV, generator=g)
+        for rms in (False, True):
+            out = P.camera_norm_forward(x, w, eps=0.0, rms=rms)
+            check(out, forward_ref(x, w, None, 0.0, rms, dtype), ["y", "rstd"] + ([] if rms else ["mean"]))
+            grads = P.camera_norm_backward(dy, x, out["rstd"], out.get("mean"), w, want_bias=True)
+            check(grads, backward_ref(dy, x, out.get("mean"), out["rstd"], w, None, dtype, rows), ["x", "weight", "bias"])
