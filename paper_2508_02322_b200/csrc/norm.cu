@@ -3,11 +3,14 @@
 //   y = (z - mu) s w + b
 //   h = (z - mu) s, g = dy w:  dx = s (g - mean g - h mean(g h)) + d_sum (no mean g for RMS),  dw = sum_rows dy h,
 //   db = sum_rows dy
-// A row is held in the registers of a group of warps: it is read once, the sums are taken in two passes over registers
-// (the second around the mean, so that a large mean costs no digits), and the next row of the group is on its way
-// meanwhile.  All sums are fp32.
-// Bound: HBM.  16384 x 3584 bf16, root mean square, with residual: forward 87 us, backward with d_sum and weight gradient 83 us, 470 MB
-// each, 5.4 and 5.7 TB/s (copy 6.5).  One row: 2.5 us, which is a load, two barriers and a store.
+// A row is held by the threads of a group of warps: it is read once, the sums are taken in two passes over what they hold
+// (the second around the mean, so that a large mean costs no digits), and up to 8192 columns the next rows of the group are on
+// their way meanwhile.  All sums are fp32.
+// Bound: HBM.  16384 x 3584 bf16, root mean square, with residual: forward 88 us, backward with d_sum and weight gradient 84 us by itself
+// and 92 us among other calls, 470 MB each, 5.3 and 5.1 to 5.6 TB/s (copy 6.5).  One row: 2.5 us, which is a load, two barriers and a store.
+// Longer rows: registers.  Of 8193 to 16384 columns one row is in flight (6000 rows of 12288 bf16: forward 0.55, backward 0.39 of the copy
+// rate); beyond, 32 elements a thread beside their weights do not fit 64 registers: the forward kernels keep 270 to 2120 bytes a thread in
+// local memory (20480 columns: 0.38, backward 0.37).
 #include "common.cuh"
 #include "launch.cuh"
 #include "rowgroup.cuh"

@@ -3,9 +3,11 @@
 //   X = U / (|U|_F + eps);   each step:  A = X X^T,  B = a I + b A + c A A,  X <- B X
 // X is the matrix with its shorter side as rows (m), its longer as columns (n).  A and B are symmetric: only tiles on and
 // above the diagonal are computed, each stored twice.  A step is m^2 n + m^3 + 2 m^2 n operations.  Bounds: where matrices are large,
-// bringing the operands of the products from L2 to the SMs, to which an epilogue adds its reads and writes (16 matrices of 1408 .. 853
-// x 2048, five steps: 766 GFLOP in 930 us, 0.82 PFLOP/s; a second tile of a unit some k blocks behind the first, so that no epilogue
-// is waited for, changed nothing); where they are small, the chain of products, 5 us each (5 matrices of 241 x 56: 91 us for fifteen).
+// what is computed beyond that (rows are padded to 256, blocks on the diagonal computed whole: 999 GFLOP for the 766 that 16 matrices of
+// 1408 .. 853 x 2048 need in five steps), and then bringing the operands of the products from L2 to the SMs, to which an epilogue adds
+// its reads and writes (the same: 1000 us, 1.0 PFLOP/s of what is computed; a second tile of a unit some k blocks behind the first, so that
+// no epilogue is waited for, changed nothing); where they are small, the chain of products, 6 us each, of which 3 to 4 are its way through
+// global memory: first operand, stores, report and polling (5 matrices of 241 x 56: 99 us for fifteen).
 //
 // The operands of the products are fp16 with a power of two as factor, the sums fp32.  With h a bound of the singular values
 // of X, no element of X is larger than h, none of A than h^2, none of B than the polynomial's largest value over [0, h^2]: the
@@ -438,7 +440,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
     // What it reads beside the accumulators (this tile of A or X) and what it writes travel as boxes of 32 rows x 32 columns
     // through the warp's buffers in shared memory, by TMA both ways: a lane's loads and stores of 32 bytes of its own row
     // each take a request per lane (16 matrices of up to 1408 x 2048: POLY 62 us, APPLY 122 us; without their reads 46 and
-    // 91 us).  The result takes the place of what was read; three boxes are in flight ahead.
+    // 91 us).  The result takes the place of what was read; two boxes are in flight ahead.
     int acc = 0;
     uint32_t acc_phase = 0, n = 0, loads = 0;                // boxes so far, in buffer n % O_BUFS; those of them that were loaded
     bool ok = true;
