@@ -16,13 +16,14 @@
 // values are alike all of it rounds the same way; so what their rounding leaves is kept in fp32 and enters the next product's
 // epilogue (a row of it for B X, a row and a column for A A).
 //
-// X itself is held as two fp16 numbers, X + L, 22 bits.  Its rounding reaches directions in which the matrix has nothing (a gradient made
-// from few tokens), and there every step left multiplies it by a: 485 times in five steps, where what the matrix does have grows to 1.
-// There B is a I, so B L is a L, which an epilogue adds by element; no product needs L.  In the directions the matrix has, the rounding
-// does not grow, and B L is nearer to the diagonal of B times L.  The factor lies between the two, nearer to a the more the steps left can
-// make of it (f_low).  The rest of B L is left out.  1000 x 2048, fp32, made from 1, 8, 64, 256 and 2048 tokens: 1.7, 1.7, 1.9, 1.9 and 1.7e-3
-// off 64 bits (root mean square, relative), of which the result's rounding to bf16 alone makes 1.7e-3; with X in one fp16 it was 0.15, 4.2e-2,
-// 2.1e-2, 7.7e-3 and 1.9e-3.  It costs a product's epilogue its reads and writes: sixteen matrices 940 -> 1000 us, three 225 -> 243.
+// X itself is held as two fp16 numbers, X + L: 22 bits, down to 2^-39 of the norm.  Its rounding reaches directions in which the matrix
+// has nothing (a gradient made from few tokens), and there every step left multiplies it by a: 485 times in five steps, where what the
+// matrix does have grows to 1.  There B is a I, so B L is a L, which an epilogue adds by element; no product needs L.  In the directions the
+// matrix has, the rounding does not grow, and B L is nearer to the diagonal of B times L.  The factor lies between the two, nearer to a the
+// more the steps left can make of it (f_low).  The rest of B L is left out.  1000 x 2048, fp32, made from 1, 8, 64, 256 and 2048 tokens: 1.7, 1.7,
+// 1.9, 1.9 and 1.7e-3 off 64 bits (root mean square, relative), of which the result's rounding to bf16 alone makes 1.7e-3; with X in one fp16 it
+// was 0.15, 4.2e-2, 2.1e-2, 7.7e-3 and 1.9e-3.  It costs a product's epilogue its reads and writes: sixteen matrices 940 -> 1000 us, three 225 ->
+// 243.
 // The first X is the matrix itself times a power of two, so bf16 inputs enter exactly; 1 / (|U| + eps) goes into the factors of the
 // first step.
 //
@@ -555,7 +556,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(O_THREADS, 1) k_orth
           for (int j = 0; j < 16; ++j) v[j] = j == own ? mine : v[j];
           if (own >= 0 && own < 16) {
             rest_out[row] = mine - __half2float(__float2half_rn(mine));
-            if (MODE == ORTHO_POLY) q.low_f[mat.row0 + row] = mat.m == 1 ? mine : fmaf(st.f_low, mine - f_diag, f_diag);     // one row: B is its diagonal
+            // (one row: B is its diagonal)
+            if (MODE == ORTHO_POLY) q.low_f[mat.row0 + row] = mat.m == 1 ? mine : fmaf(st.f_low, mine - f_diag, f_diag);
           }
         }
 #pragma unroll
@@ -747,8 +749,9 @@ __global__ void __launch_bounds__(LOAD_THREADS, 6) k_ortho_norm(const __grid_con
   if (threadIdx.x == 0) q.part[blockIdx.y * q.parts + blockIdx.x] = s;
 }
 
-// X = U 2^p in fp16 (of fp32 matrices a second fp16 holds what the rounding leaves), shorter side as rows, zeros around it.  p puts 2^p |U| into [2^14, 2^15): nothing overflows, and what
-// is below 2^-39 of the norm is lost.  A CTA turns tiles of 64 x 64 in shared memory.
+// X = U 2^p in fp16 (of fp32 matrices a second fp16 holds what the rounding leaves), shorter side as rows, zeros around it.  p puts
+// 2^p |U| into [2^14, 2^15): nothing overflows, and what is below 2^-39 of the norm is lost.  A CTA turns tiles of 64 x 64 in shared
+// memory.
 template <typename T>
 __global__ void __launch_bounds__(LOAD_THREADS, 6) k_ortho_load(const __grid_constant__ OrthoLoad q) {
   constexpr bool LOW = sizeof(T) == 4;

@@ -116,3 +116,19 @@ def test_other_polynomials(P, name):
         check(P.camera_orthogonalize([u], coefficients=coefficients)[0], u, coefficients)
         small = u * 1e-9
         check(P.camera_orthogonalize([small], coefficients=coefficients, eps=0.0)[0], u, coefficients)
+
+
+@pytest.mark.parametrize("shapes,dtype", [
+    ([(3329, 3555)], F32), ([(3600, 3333)], BF), ([(2048, 8192)], F32), ([(2810, 2603)], BF),
+    ([(1408 - 37 * i, 2048) if i % 3 else (2048, 1408 - 37 * i) for i in range(16)], F32)], ids=lambda v: str(v[0]) if isinstance(v, list) else "")
+def test_gradients_of_few_tokens_in_wide_tiles(P, shapes, dtype):
+    """Tiles of 256 and of twice 256 columns.  Sums of k products: sqrt(k / 16) 2^-23, as above, grown by the slopes."""
+    g = torch.Generator(device=DEV).manual_seed(len(shapes))
+    coefficients = [P.NEWTON_SCHULZ] * 5
+    us = [of_rank(g, r, c, 1 + 7 * (i % 5), dtype) for i, (r, c) in enumerate(shapes)]
+    for u, o in zip(us, P.camera_orthogonalize(us)):
+        want = modelled(u, coefficients, False)
+        off = float((modelled(u, coefficients, True) - want).norm())
+        sums = (min(u.shape) / 16) ** 0.5 * 2.0 ** -23 * P.NEWTON_SCHULZ[0] ** 5
+        bound = 2 * off + (2.0 ** -8 / 3 ** 0.5 + sums) * float(want.norm())
+        assert float((o.double() - want).norm()) <= bound, (float((o.double() - want).norm()), bound)
